@@ -24,7 +24,8 @@
  *   - Work is enqueued on `stream` (a hipStream_t passed as void*; NULL is the
  *     null stream).  Calls return before the work completes; a device fault
  *     surfaces at the caller's next synchronization.  Only
- *     tiga_csr_validate(level 2) and tiga_radius_neighbors synchronize.
+ *     tiga_csr_validate(level 2), tiga_radius_neighbors and
+ *     tiga_cache_validate synchronize.
  *   - Outputs are overwritten, never accumulated into.
  *   - fp32 features are row-major [rows, feat], of any width.  Rows need only
  *     the alignment of floats; some paths are faster where feat % 4 == 0 and
@@ -346,6 +347,9 @@ int tiga_mp_edgenn_bwd(int64_t n, int32_t feat, int32_t hidden, int32_t out, con
 /* 16-bit input types of the attention path. */
 enum tiga_dtype { TIGA_DT_F16 = 0 /* IEEE binary16 */, TIGA_DT_BF16 = 1 /* bfloat16 */ };
 
+/* fp32, which only the rotary positions take besides. */
+#define TIGA_DT_F32 2
+
 /* Implicit relations of the attention path (no edge array). */
 enum tiga_relation {
     TIGA_REL_TRIANGULAR = 0, /* N(i) = {0, ..., i}: causal, the diagonal included */
@@ -377,6 +381,190 @@ enum tiga_relation {
  * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EDEVICE. */
 int tiga_mp_attention_fwd(int64_t n, int32_t heads, int32_t width, int dtype, const void *q, const void *k,
                           const void *v, float scale, int relation, void *y, float *lse, void *stream);
+
+/* ------------------- online softmax over a rectangular relation (cross attention) */
+
+/* A strided view of a [batch, heads, rows, width] tensor: element (b, h, r, d)
+ * is data[b * batch + h * head + r * row + d] (strides in elements, the width
+ * contiguous).  The struct lives in HOST memory, the data on the device.  A
+ * stride of 0 repeats an input along that axis; outputs must not overlap. */
+typedef struct {
+    void *data;
+    int64_t batch, head, row;
+} tiga_view;
+
+/* The dense relation between num_dst destinations (queries) and num_src sources
+ * (keys and values: an encoder's states, a document's) of each sequence of a
+ * padded batch.  Destination head h reads source head h / (heads / kv_heads).
+ *   src_len: device int32 [batch], the sources of each sequence,
+ *            N(b, i) = {0, ..., src_len[b] - 1}; NULL: num_src for all.  A value
+ *            outside [0, num_src] is taken as the nearer bound.
+ * The struct lives in HOST memory. */
+typedef struct {
+    int64_t num_dst, num_src;
+    int32_t batch, heads, kv_heads, width;
+    int32_t dtype; /* TIGA_DT_F16 or TIGA_DT_BF16 */
+    const int32_t *src_len;
+} tiga_cross;
+
+/* Workspace bytes for tiga_mp_attention_cross_fwd (0 on error). */
+size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
+
+/* The online-softmax reducer of tiga_mp_attention_fwd over a rectangular
+ * relation: for sequence b, head h and destination i,
+ *   s_ij = scale * <q_i, k_j>,  lse_i = log sum_{j in N(b,i)} exp(s_ij),
+ *   y_i  = sum_{j in N(b,i)} exp(s_ij - lse_i) v_j.
+ * A destination without sources (src_len[b] == 0) finalizes the reducer's
+ * identity: y = 0, lse = -inf.  Sources at and past src_len[b] are not read.
+ *   q, y: [batch, heads, num_dst, width];  k, v: [batch, kv_heads, num_src, width]
+ *         of dtype, 16-byte aligned, strides multiples of 8; y is overwritten.
+ *   lse:  fp32 [batch, heads, num_dst], contiguous, or NULL.
+ * Products of the inputs are exact and summed in fp32; the mass is the fp32 sum
+ * of the fp32 weights; the weights enter the value product rounded to dtype.
+ * Deterministic.  Requires width 64 or 128 (TIGA_EUNSUPPORTED otherwise), heads
+ * a multiple of kv_heads, num_dst and num_src < 2^31 - 1024, batch * heads *
+ * num_dst < 2^40, batch * kv_heads < 2^20, scale finite and > 0.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
+int tiga_mp_attention_cross_fwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+                                float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes for tiga_mp_attention_cross_bwd (0 on error). */
+size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel);
+
+/* Vector-Jacobian product of tiga_mp_attention_cross_fwd.  With the forward's y
+ * and lse, p_ij = exp(s_ij - lse_i) and delta_i = <dy_i, y_i>:
+ *   ds_ij = p_ij (<dy_i, v_j> - delta_i)
+ *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dy_i
+ * where the sums over i also run over the heads that share source head j's.
+ * Gradients of sources at and past src_len[b] are 0.
+ *   dy: as y; dq as q, dk and dv as k and v, of dtype, overwritten; each may be
+ *   NULL (skipped).  p and ds enter the products rounded to dtype; sums in fp32.
+ * Deterministic (no atomics).  Requirements and errors as the forward. */
+int tiga_mp_attention_cross_bwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+                                const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
+                                const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,
+                                size_t ws_bytes, void *stream);
+
+/* ----------------------------------------------------------- rotary positions */
+
+/* How the elements of a row pair up (rot elements from the front take part). */
+enum tiga_pairs {
+    TIGA_PAIRS_HALF = 0,    /* (i, i + rot / 2) */
+    TIGA_PAIRS_ADJACENT = 1 /* (2 i, 2 i + 1) */
+};
+
+/* The rotation of a row at position p: pair i = (a, b) becomes
+ *   amplitude * (a cos t - b sin t, a sin t + b cos t),  t = p * freq[i].
+ * The struct lives in HOST memory. */
+typedef struct {
+    const double *freq; /* device fp64 [rot / 2], radians a position */
+    int32_t rot;        /* even, 0 < rot <= width; elements past it are copied */
+    int32_t pairs;      /* tiga_pairs */
+    float amplitude;
+} tiga_rotary;
+
+/* How tiga_rotary_frequencies stretches the frequencies for contexts `factor`
+ * times the trained length. */
+enum tiga_rotary_scaling {
+    TIGA_ROTARY_PLAIN = 0,  /* f_i = base^(-2 i / rot) */
+    TIGA_ROTARY_LINEAR = 1, /* f_i / factor (positions interpolated) */
+    TIGA_ROTARY_BASE = 2,   /* f_i of base * factor^(rot / (rot - 2)) */
+    TIGA_ROTARY_BANDS = 3   /* by the turns r = trained f_i / 2 pi over the trained length: f_i / factor
+                               where r <= low, f_i where r >= high, in between the two weighted linearly */
+};
+
+/* Fill the HOST array freq [rot / 2].  trained, low and high only matter for
+ * TIGA_ROTARY_BANDS (low < high).  Enqueues nothing. */
+int tiga_rotary_frequencies(int32_t rot, double base, int scaling, double factor, double trained, double low,
+                            double high, double *freq);
+
+/* Rotate every row of x [batch, heads, rows, width] by its position into y
+ * (y == x, same strides, rotates in place; y must not overlap x otherwise).
+ *   dtype: TIGA_DT_F16, TIGA_DT_BF16 or TIGA_DT_F32; x, y strides any.
+ *   pos:   device int32, the position of row (b, r) at pos[b * pos_batch + r]
+ *          (pos_batch 0 shares one row of positions); NULL: r itself.
+ * The angle is formed and reduced in fp64, sine and cosine in fp32, the
+ * rotation in fp32, rounded once.  Elements past rot are copied unchanged.
+ * Requires width < 2^16, batch * heads * rows < 2^40, amplitude finite.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EDEVICE. */
+int tiga_mp_rotary_fwd(int32_t batch, int32_t heads, int64_t rows, int32_t width, int dtype, const tiga_view *x,
+                       const int32_t *pos, int64_t pos_batch, const tiga_rotary *rot, const tiga_view *y,
+                       void *stream);
+
+/* Vector-Jacobian product of tiga_mp_rotary_fwd: dy turned back by the same
+ * angles into dx, with the same amplitude.  Arguments as the forward. */
+int tiga_mp_rotary_bwd(int32_t batch, int32_t heads, int64_t rows, int32_t width, int dtype, const tiga_view *dy,
+                       const int32_t *pos, int64_t pos_batch, const tiga_rotary *rot, const tiga_view *dx,
+                       void *stream);
+
+/* ------------------------------------------------- attention over a paged cache */
+
+/* Keys and values of a batch of sequences in pages.  Position p of sequence b
+ * lies in row p % page_size of page table[b * table_width + p / page_size].
+ *   k, v:   views [num_pages, kv_heads, page_size, width] (batch is the page
+ *           stride) of dtype, 16-byte aligned, strides multiples of 8.
+ *   table:  device int32 [batch, table_width]; entries past a sequence's length
+ *           are not read.
+ *   length: device int32 [batch], positions of each sequence, the new ones of a
+ *           call included.
+ * Sequences may share pages that no call writes.  page_size is a power of two,
+ * at most 2^15.  The struct lives in HOST memory. */
+typedef struct {
+    int64_t num_pages;
+    int32_t page_size, kv_heads, width;
+    int32_t dtype; /* TIGA_DT_F16 or TIGA_DT_BF16 */
+    int32_t batch, table_width;
+    tiga_view k, v;
+    const int32_t *table;
+    const int32_t *length;
+} tiga_cache;
+
+/* The new tokens of a call are rows of one packed axis: sequence b owns rows
+ * [dst_ptr[b], dst_ptr[b + 1]), dst_ptr device int32 [batch + 1], non-decreasing,
+ * dst_ptr[batch] <= num_dst, and row dst_ptr[b] + t, of c = dst_ptr[b + 1] -
+ * dst_ptr[b], is at position length[b] - c + t.
+ *
+ * tiga_cache_validate checks dst_ptr, length and the table entries that the
+ * lengths need on the host and describes the first violation (TIGA_EGRAPH).
+ * Synchronizes `stream`; not on the serving path. */
+int tiga_cache_validate(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, void *stream);
+
+/* Store the new tokens' keys and values in their pages: k rotated by its position
+ * (rot != NULL) and v unchanged.  With q, the queries of the same tokens are
+ * rotated by the same positions into q_out in the same launch (rot required;
+ * q_out may be q).
+ *   k, v: [1, kv_heads, num_dst, width]; q, q_out: [1, heads, num_dst, width] of
+ *   the cache's dtype (the views' batch strides are not used).
+ * Rows outside every sequence, and rows whose position is negative or past the
+ * table, or whose page is not in [0, num_pages), store nothing; their q is
+ * copied unrotated if the row has no position and rotated otherwise.  Rows
+ * behind dst_ptr[batch] are left as they were.
+ * No two rows of one call may fall on the same place of a page.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EDEVICE. */
+int tiga_mp_cache_append(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, const tiga_view *k,
+                         const tiga_view *v, const tiga_rotary *rot, int32_t heads, const tiga_view *q,
+                         const tiga_view *q_out, void *stream);
+
+/* Workspace bytes for tiga_mp_attention_paged_fwd (0 on error). */
+size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads);
+
+/* Causal attention of the new tokens over the cache, their own keys and values
+ * already in it: the row at position p of sequence b reads positions 0..p,
+ * N(b, p) = {0, ..., p}, otherwise as tiga_mp_attention_cross_fwd.  One token a
+ * sequence (generation), chunks of prompts, or both mixed.
+ *   q, y: [1, heads, num_dst, width] (the views' batch strides are not used);
+ *   lse: fp32 [heads, num_dst] or NULL.
+ * A row with a negative position gives y = 0, lse = -inf.  A row that needs a
+ * position past the table or a page outside [0, num_pages) gives NaN (nothing
+ * is read there).  Rows behind dst_ptr[batch] are left as they were.  A value
+ * row that is not finite reaches every row of its sequence's new tokens that
+ * it shares a tile with: new tokens' values must be finite.
+ * Requires heads a multiple of kv_heads, width 64 or 128, num_dst < 2^31 / heads,
+ * batch < 2^16, scale finite and > 0.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
+int tiga_mp_attention_paged_fwd(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,
+                                const tiga_view *q, float scale, const tiga_view *y, float *lse, void *ws,
+                                size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------- profiling */
 

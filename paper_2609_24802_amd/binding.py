@@ -21,8 +21,10 @@ LIB_PATH = os.path.join(_HERE, "libtiga_mp.so")
 TIGA_OK, TIGA_EINVAL, TIGA_EGRAPH, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE = 0, -1, -2, -3, -4, -5
 REDUCE_SUM, REDUCE_MAX = 0, 1
 MSG_SRC, MSG_EDGE_SCALED_SRC = 0, 1
-DT_F16, DT_BF16 = 0, 1
+DT_F16, DT_BF16, DT_F32 = 0, 1, 2
 REL_TRIANGULAR, REL_DENSE = 0, 1
+PAIRS_HALF, PAIRS_ADJACENT = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS = 0, 1, 2, 3
 _STATUS = {0: "TIGA_OK", -1: "TIGA_EINVAL", -2: "TIGA_EGRAPH", -3: "TIGA_EUNSUPPORTED",
            -4: "TIGA_EWORKSPACE", -5: "TIGA_EDEVICE"}
 
@@ -40,6 +42,25 @@ class _Csr(C.Structure):
 
 class _CsrT(C.Structure):
     _fields_ = [("src_ptr", C.c_void_p), ("edge_id", C.c_void_p)]
+
+
+class _View(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("row", C.c_int64)]
+
+
+class _Cross(C.Structure):
+    _fields_ = [("num_dst", C.c_int64), ("num_src", C.c_int64), ("batch", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32), ("src_len", C.c_void_p)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rot", C.c_int32), ("pairs", C.c_int32), ("amplitude", C.c_float)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("num_pages", C.c_int64), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("width", C.c_int32),
+                ("dtype", C.c_int32), ("batch", C.c_int32), ("table_width", C.c_int32), ("k", _View), ("v", _View),
+                ("table", C.c_void_p), ("length", C.c_void_p)]
 
 
 _lib = None
@@ -87,6 +108,24 @@ _SIGS = {
                                   C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tiga_mp_attention_fwd": (C.c_int, [C.c_int64, C.c_int32, C.c_int32, C.c_int, C.c_void_p, C.c_void_p,
                                         C.c_void_p, C.c_float, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "tiga_mp_attention_cross_fwd_workspace": (C.c_size_t, [C.c_void_p]),
+    "tiga_mp_attention_cross_fwd": (C.c_int, [C.c_void_p] * 4 + [C.c_float] + [C.c_void_p] * 3 +
+                                    [C.c_size_t, C.c_void_p]),
+    "tiga_mp_attention_cross_bwd_workspace": (C.c_size_t, [C.c_void_p]),
+    "tiga_mp_attention_cross_bwd": (C.c_int, [C.c_void_p] * 7 + [C.c_float] + [C.c_void_p] * 4 +
+                                    [C.c_size_t, C.c_void_p]),
+    "tiga_rotary_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double,
+                                          C.c_double, C.c_void_p]),
+    "tiga_mp_rotary_fwd": (C.c_int, [C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int, C.c_void_p, C.c_void_p,
+                                     C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "tiga_mp_rotary_bwd": (C.c_int, [C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int, C.c_void_p, C.c_void_p,
+                                     C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "tiga_cache_validate": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "tiga_mp_cache_append": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "tiga_mp_attention_paged_fwd_workspace": (C.c_size_t, [C.c_void_p, C.c_int64, C.c_int32]),
+    "tiga_mp_attention_paged_fwd": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_float,
+                                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tiga_mp_set_kernel_events": (C.c_int, [C.c_void_p, C.c_void_p]),
 }
 
@@ -496,6 +535,302 @@ def tiga_mp_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sca
     return (y, lse) if want_lse else y
 
 
+# ------------------------------------------- rectangular relations: cross attention, paged cache, rotary positions
+
+_HALF_TYPES = {torch.float16: DT_F16, torch.bfloat16: DT_BF16}
+_ROTARY_TYPES = {torch.float16: DT_F16, torch.bfloat16: DT_BF16, torch.float32: DT_F32}
+
+
+def _on(device, **tensors):
+    """The call's tensors lie on one device, and that is the current one (whose stream the work goes to)."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is {torch.cuda.current_device()}")
+
+
+def _rows(t, name, layout, dtype=None, shape=None, out=False):
+    """t in the axis order [batch, heads, rows, width] (any strides, the width contiguous) and its view.
+
+    layout names t's own axes: "bhnd" or "bnhd", or without a batch "hnd" or "nhd"."""
+    order = {"bhnd": None, "bnhd": (0, 2, 1, 3), "hnd": None, "nhd": (1, 0, 2)}
+    if layout not in order:
+        raise ValueError(f"unknown layout {layout!r}")
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != len(layout):
+        raise ValueError(f"{name} must have {len(layout)} dimensions (layout {layout!r})")
+    if order[layout] is not None:
+        t = t.permute(order[layout])
+    if t.dim() == 3:
+        t = t.unsqueeze(0)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has [batch, heads, rows, width] {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.shape[3] > 1 and t.numel() and t.stride(3) != 1:
+        raise ValueError(f"{name}: the width must be contiguous")
+    # the stride of an axis with one entry is never used; torch leaves anything there
+    st = [t.stride(a) if t.shape[a] > 1 else 0 for a in range(3)]
+    return t, _View(t.data_ptr() if t.numel() else None, *st)
+
+
+def _like(t, layout):
+    """A new contiguous tensor of t's shape and layout, and its view."""
+    y = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return y, _rows(y, "output", layout)[1]
+
+
+def _cross(q, k, v, src_len, layout):
+    if len(layout) != 4:
+        raise ValueError(f"unknown layout {layout!r}")
+    if not isinstance(q, torch.Tensor) or q.dtype not in _HALF_TYPES:
+        raise TypeError("q must be a float16 or bfloat16 tensor")
+    qt, qv = _rows(q, "q", layout)
+    kt, kv = _rows(k, "k", layout, q.dtype)
+    B, H, N, D = qt.shape
+    Hk, S = kt.shape[1], kt.shape[2]
+    _, kv = _rows(k, "k", layout, q.dtype, (B, Hk, S, D))
+    _, vv = _rows(v, "v", layout, q.dtype, (B, Hk, S, D))
+    _on(q.device, k=k, v=v, src_len=src_len)
+    if src_len is not None:
+        _dev(src_len, torch.int32, "src_len", (B,))
+    rel = _Cross(N, S, B, H, Hk, D, _HALF_TYPES[q.dtype], src_len.data_ptr() if src_len is not None else None)
+    return rel, qv, kv, vv
+
+
+def tiga_mp_attention_cross_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                                src_len: torch.Tensor | None = None, scale: float | None = None,
+                                want_lse: bool = False, layout: str = "bhnd", ws=None):
+    """Online-softmax attention of num_dst destinations over num_src sources a sequence (an encoder's states).
+
+    q: float16 or bfloat16 [batch, heads, num_dst, width] (layout "bhnd"; "bnhd" has rows before heads);
+    k, v: [batch, kv_heads, num_src, width], heads a multiple of kv_heads.  Any strides that are multiples
+    of 8 elements, the width contiguous.  src_len: int32 [batch] on the device, the sources of each sequence
+    (None: all).  A sequence without sources gives y = 0, lse = -inf.  scale defaults to width ** -0.5.
+    Returns y in q's shape (and lse fp32 [batch, heads, num_dst] when want_lse)."""
+    lib = load()
+    rel, qv, kv, vv = _cross(q, k, v, src_len, layout)
+    y, yv = _like(q, layout)
+    lse = torch.empty(rel.batch, rel.heads, rel.num_dst, dtype=torch.float32, device=q.device) if want_lse else None
+    ref = C.byref
+    if ws is None:
+        ws = _workspace(lib.tiga_mp_attention_cross_fwd_workspace(ref(rel)), q.device)
+    _check(lib.tiga_mp_attention_cross_fwd(ref(rel), ref(qv), ref(kv), ref(vv),
+                                           float(rel.width ** -0.5 if scale is None else scale), ref(yv), _ptr(lse),
+                                           _ptr(ws), ws.numel(), _stream()))
+    return (y, lse) if want_lse else y
+
+
+def tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy, src_len: torch.Tensor | None = None,
+                                scale: float | None = None, want=("dq", "dk", "dv"), layout: str = "bhnd", ws=None):
+    """The VJP of tiga_mp_attention_cross_fwd for the cotangent dy, from the forward's y and lse; returns a
+    dict of the wanted gradients in the inputs' shapes.  Gradients of sources past src_len are 0."""
+    lib = load()
+    rel, qv, kv, vv = _cross(q, k, v, src_len, layout)
+    shape = (rel.batch, rel.heads, rel.num_dst, rel.width)
+    _, yv = _rows(y, "y", layout, q.dtype, shape)
+    _, dyv = _rows(dy, "dy", layout, q.dtype, shape)
+    _on(q.device, y=y, dy=dy, lse=lse)
+    _dev(lse, torch.float32, "lse", shape[:3])
+    out, views = {}, dict(dq=None, dk=None, dv=None)
+    for name, t in (("dq", q), ("dk", k), ("dv", v)):
+        if name in want:
+            out[name], views[name] = _like(t, layout)
+    ref = C.byref
+    if ws is None:
+        ws = _workspace(lib.tiga_mp_attention_cross_bwd_workspace(ref(rel)), q.device)
+    opt = lambda name: ref(views[name]) if views[name] is not None else None
+    _check(lib.tiga_mp_attention_cross_bwd(ref(rel), ref(qv), ref(kv), ref(vv), ref(yv), _ptr(lse), ref(dyv),
+                                           float(rel.width ** -0.5 if scale is None else scale), opt("dq"), opt("dk"),
+                                           opt("dv"), _ptr(ws), ws.numel(), _stream()))
+    return out
+
+
+def tiga_rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                            trained: float = 0.0, low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """Radians a position of each of the rot / 2 pairs: float64 on the host.
+
+    scaling stretches them for contexts `factor` times the trained length: "linear" (all by the factor),
+    "base" (a larger base) or "bands" (pairs of at most `low` turns over the trained length by the factor,
+    of at least `high` turns not at all)."""
+    kinds = dict(plain=ROTARY_PLAIN, linear=ROTARY_LINEAR, base=ROTARY_BASE, bands=ROTARY_BANDS)
+    if scaling not in kinds:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    freq = torch.empty(max(int(rot), 2) // 2, dtype=torch.float64)
+    _check(load().tiga_rotary_frequencies(int(rot), float(base), kinds[scaling], float(factor), float(trained),
+                                          float(low), float(high), _ptr(freq)))
+    return freq
+
+
+class Rotary:
+    """A rotation by positions: freq float64 [rot / 2] on the device (radians a position), the pairs (i, i + rot / 2)
+    or (interleaved) (2 i, 2 i + 1), and an amplitude that multiplies the rotated elements."""
+
+    def __init__(self, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
+        self.freq = _dev(freq, torch.float64, "freq")
+        if freq.dim() != 1:
+            raise ValueError("freq must have one dimension")
+        self._c = _Rotary(freq.data_ptr() if freq.numel() else None, 2 * freq.numel(),
+                          PAIRS_ADJACENT if interleaved else PAIRS_HALF, float(amplitude))
+
+    @property
+    def ref(self):
+        return C.byref(self._c)
+
+
+def _rotary_call(name, x, pos, rot, layout, out):
+    lib = load()
+    if not isinstance(x, torch.Tensor) or x.dtype not in _ROTARY_TYPES:
+        raise TypeError("x must be a float16, bfloat16 or float32 tensor")
+    xt, xv = _rows(x, "x", layout)
+    B, H, N, D = xt.shape
+    pos_batch = 0
+    if pos is not None:
+        if pos.dim() == 2:
+            _dev(pos, torch.int32, "pos", (B, N))
+            pos_batch = N
+        else:
+            _dev(pos, torch.int32, "pos", (N,))
+    _on(x.device, pos=pos, freq=rot.freq, out=out)
+    if out is None:
+        out, ov = _like(x, layout)
+    else:
+        _, ov = _rows(out, "out", layout, x.dtype, xt.shape)
+    _check(getattr(lib, name)(B, H, N, D, _ROTARY_TYPES[x.dtype], C.byref(xv), _ptr(pos), pos_batch, rot.ref,
+                              C.byref(ov), _stream()))
+    return out
+
+
+def tiga_mp_rotary_fwd(x: torch.Tensor, pos: torch.Tensor | None, rot: Rotary, layout: str = "bhnd", out=None):
+    """Every row of x rotated by its position: pair (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t)
+    with t = position * freq; elements past the rotated part are copied.
+
+    x: float16, bfloat16 or float32, layout "bhnd", "bnhd", "hnd" or "nhd", any strides with a contiguous
+    width.  pos: int32 [batch, rows] or [rows], None for the row's index.  out may be x (in place)."""
+    return _rotary_call("tiga_mp_rotary_fwd", x, pos, rot, layout, out)
+
+
+def tiga_mp_rotary_bwd(dy: torch.Tensor, pos: torch.Tensor | None, rot: Rotary, layout: str = "bhnd", out=None):
+    """The VJP of tiga_mp_rotary_fwd: dy turned back by the same angles."""
+    return _rotary_call("tiga_mp_rotary_bwd", dy, pos, rot, layout, out)
+
+
+class KvCache:
+    """A paged cache on the device.
+
+    k_pages, v_pages: float16 or bfloat16 [num_pages, kv_heads, page_size, width], any strides that are
+    multiples of 8 elements with a contiguous width (pages stored rows first are passed permuted);
+    table: int32 [batch, table_width], position p of sequence b is row p % page_size of page
+    table[b, p // page_size]; length: int32 [batch], positions of each sequence with the new ones of a
+    call.  The tensors are the caller's; their contents may change between calls."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
+        if not isinstance(k_pages, torch.Tensor) or k_pages.dtype not in _HALF_TYPES:
+            raise TypeError("k_pages must be a float16 or bfloat16 tensor")
+        kt, kv = _rows(k_pages, "k_pages", "bhnd")
+        _, vv = _rows(v_pages, "v_pages", "bhnd", k_pages.dtype, kt.shape)
+        self.table = _dev(table, torch.int32, "table")
+        if table.dim() != 2:
+            raise ValueError("table must be [batch, table_width]")
+        self.length = _dev(length, torch.int32, "length", (table.shape[0],))
+        for name, t in (("v_pages", v_pages), ("table", table), ("length", length)):
+            if t.device != k_pages.device:
+                raise ValueError(f"{name} is on {t.device}, expected {k_pages.device}")
+        self.k_pages, self.v_pages = k_pages, v_pages
+        P, H, R, D = kt.shape
+        self.kv_heads, self.width, self.batch = H, D, table.shape[0]
+        self._c = _Cache(P, R, H, D, _HALF_TYPES[k_pages.dtype], table.shape[0], table.shape[1], kv, vv,
+                         table.data_ptr() if table.numel() else None, length.data_ptr() if length.numel() else None)
+
+    @property
+    def ref(self):
+        return C.byref(self._c)
+
+
+def _new_rows(cache, t, name, layout, heads=None):
+    """A packed tensor of new tokens in the cache's type and width."""
+    if len(layout) != 3:
+        raise ValueError(f"unknown layout {layout!r}")
+    tt, view = _rows(t, name, layout, cache.k_pages.dtype)
+    if tt.shape[3] != cache.width or (heads is not None and tt.shape[1] != heads):
+        raise ValueError(f"{name} has [heads, rows, width] {tuple(tt.shape[1:])}, expected "
+                         f"{heads if heads is not None else 'heads'} heads of width {cache.width}")
+    return tt, view
+
+
+def tiga_cache_validate(cache: KvCache, num_dst: int, dst_ptr: torch.Tensor):
+    """Raise TigaError (TIGA_EGRAPH) if dst_ptr, the lengths or the pages they need are inconsistent.  Synchronizes."""
+    _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    _on(cache.k_pages.device, dst_ptr=dst_ptr)
+    _check(load().tiga_cache_validate(cache.ref, int(num_dst), _ptr(dst_ptr), _stream()))
+
+
+def tiga_mp_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, dst_ptr: torch.Tensor,
+                         rot: Rotary | None = None, q: torch.Tensor | None = None, layout: str = "hnd", q_out=None):
+    """Store new tokens' keys (rotated by their positions with rot) and values in the cache's pages.
+
+    k, v: [kv_heads, rows, width] (layout "hnd"; "nhd" has rows first) of the cache's type, the new tokens
+    of all sequences packed: sequence b owns rows dst_ptr[b] to dst_ptr[b + 1] (int32 [batch + 1]), its last
+    row at position length[b] - 1.  With q [heads, rows, width] the queries are rotated by the same
+    positions in the same launch and returned (q_out may be q)."""
+    lib = load()
+    _, kv = _new_rows(cache, k, "k", layout, cache.kv_heads)
+    kt, vv = _new_rows(cache, v, "v", layout, cache.kv_heads)
+    rows = _rows(k, "k", layout)[0].shape[2]
+    if kt.shape[2] != rows:
+        raise ValueError(f"v has {kt.shape[2]} rows, k has {rows}")
+    _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    heads, qv, ov = 0, None, None
+    if q is not None:
+        if rot is None:
+            raise ValueError("q is only taken to be rotated: rot is missing")
+        qt, qv = _new_rows(cache, q, "q", layout)
+        heads = qt.shape[1]
+        if qt.shape[2] != rows:
+            raise ValueError(f"q has {qt.shape[2]} rows, k has {rows}")
+        if q_out is None:
+            q_out, ov = _like(q, layout)
+        else:
+            _, ov = _rows(q_out, "q_out", layout, q.dtype, qt.shape)
+    _on(cache.k_pages.device, k=k, v=v, dst_ptr=dst_ptr, q=q, q_out=q_out, freq=rot.freq if rot else None)
+    ref = C.byref
+    _check(lib.tiga_mp_cache_append(cache.ref, rows, _ptr(dst_ptr), ref(kv), ref(vv), rot.ref if rot else None, heads,
+                                    ref(qv) if qv else None, ref(ov) if ov else None, _stream()))
+    return q_out
+
+
+def tiga_mp_attention_paged_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.Tensor, scale: float | None = None,
+                                want_lse: bool = False, layout: str = "hnd", y=None, ws=None):
+    """Causal attention of new tokens over a paged cache that already holds their own keys and values.
+
+    q: [heads, rows, width] (layout "hnd"; "nhd" has rows first) packed as in tiga_mp_cache_append, heads a
+    multiple of the cache's; the row at position p reads positions 0 to p of its sequence.  Rows behind
+    dst_ptr[batch] of y are left as they were.  Returns y in q's shape (and lse fp32 [heads, rows])."""
+    lib = load()
+    qt, qv = _new_rows(cache, q, "q", layout)
+    heads, rows = qt.shape[1], qt.shape[2]
+    _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    if y is None:
+        y, yv = _like(q, layout)
+    else:
+        _, yv = _rows(y, "y", layout, q.dtype, qt.shape)
+    _on(cache.k_pages.device, q=q, y=y, dst_ptr=dst_ptr)
+    lse = torch.empty(heads, rows, dtype=torch.float32, device=q.device) if want_lse else None
+    ref = C.byref
+    if ws is None:
+        ws = _workspace(lib.tiga_mp_attention_paged_fwd_workspace(cache.ref, rows, heads), q.device)
+    _check(lib.tiga_mp_attention_paged_fwd(cache.ref, rows, _ptr(dst_ptr), heads, ref(qv),
+                                           float(cache.width ** -0.5 if scale is None else scale), ref(yv), _ptr(lse),
+                                           _ptr(ws), ws.numel(), _stream()))
+    return (y, lse) if want_lse else y
+
+
 # ------------------------------------------------------------ autograd wrappers
 #
 # The paper's Torch interop (the fused operator as a differentiable function):
@@ -580,3 +915,57 @@ class EdgeMLP(torch.autograd.Function):
 
 def edge_mlp(pos, x, W1, b1, W2, b2, radius):
     return EdgeMLP.apply(pos, x, W1, b1, W2, b2, radius)
+
+
+class CrossAttention(torch.autograd.Function):
+    """y_i = sum_j softmax_j(scale <q_i, k_j>) v_j over the sources of a padded batch (lengths not differentiated)."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, src_len, scale, layout):
+        y, lse = tiga_mp_attention_cross_fwd(q, k, v, src_len, scale, want_lse=True, layout=layout)
+        ctx.scale, ctx.layout = scale, layout
+        ctx.save_for_backward(q, k, v, src_len, y, lse)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        q, k, v, src_len, y, lse = ctx.saved_tensors
+        want = [n for n, need in zip(("dq", "dk", "dv"), ctx.needs_input_grad) if need]
+        if not want:
+            return None, None, None, None, None, None
+        if _unreadable(dy):
+            dy = dy.clone(memory_format=torch.contiguous_format)
+        g = tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy, src_len, ctx.scale, want=want, layout=ctx.layout)
+        return g.get("dq"), g.get("dk"), g.get("dv"), None, None, None
+
+
+def _unreadable(t):
+    """Whether a cotangent's strides or alignment are none the kernels take (autograd may hand over any)."""
+    return t.stride(-1) != 1 or t.data_ptr() % 16 != 0 or any(s % 8 for s in t.stride()[:-1])
+
+
+def cross_attention(q, k, v, src_len: torch.Tensor | None = None, scale: float | None = None, layout: str = "bhnd"):
+    """Differentiable cross attention; see tiga_mp_attention_cross_fwd."""
+    return CrossAttention.apply(q, k, v, src_len, scale, layout)
+
+
+class RotaryPositions(torch.autograd.Function):
+    """Rows rotated by their positions (positions and frequencies not differentiated)."""
+
+    @staticmethod
+    def forward(ctx, x, pos, rot, layout):
+        ctx.rot, ctx.layout = rot, layout
+        ctx.save_for_backward(pos)
+        return tiga_mp_rotary_fwd(x, pos, rot, layout)
+
+    @staticmethod
+    def backward(ctx, dy):
+        (pos,) = ctx.saved_tensors
+        if dy.stride(-1) != 1:
+            dy = dy.contiguous()
+        return tiga_mp_rotary_bwd(dy, pos, ctx.rot, ctx.layout), None, None, None
+
+
+def rotary(x: torch.Tensor, pos: torch.Tensor | None, rot: Rotary, layout: str = "bhnd") -> torch.Tensor:
+    """Differentiable rotary positions; see tiga_mp_rotary_fwd."""
+    return RotaryPositions.apply(x, pos, rot, layout)

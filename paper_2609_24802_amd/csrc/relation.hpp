@@ -1,0 +1,56 @@
+// Device-side addressing of the rectangular relations: which sources a destination row has and where
+// their keys and values lie.
+#pragma once
+
+#include "common.hpp"
+
+namespace tiga {
+namespace relattn {
+
+// Element strides of a view as the kernels take them.
+struct Rows {
+    const uint16_t *p;
+    int64_t batch, head, row;
+};
+inline Rows rows_of(const tiga_view &v) { return Rows{static_cast<const uint16_t *>(v.data), v.batch, v.head, v.row}; }
+
+// A paged cache: the page of position p is table[p >> shift], its row p & mask.
+struct Pages {
+    Rows k, v;
+    const int32_t *table;
+    const int32_t *length;
+    const int32_t *dst_ptr;
+    int64_t num_pages;
+    int32_t batch, table_width, shift;
+    int32_t num_dst;
+};
+inline Pages pages_of(const tiga_cache &c, int64_t num_dst, const int32_t *dst_ptr) {
+    int shift = 0;
+    while ((1 << shift) < c.page_size) ++shift;
+    return Pages{rows_of(c.k), rows_of(c.v), c.table, c.length, dst_ptr, c.num_pages, c.batch, c.table_width, shift,
+                 static_cast<int32_t>(num_dst)};
+}
+
+// Rows [first, first + count) of sequence b and their positions pos0 + t.  Pointers that run
+// backwards or past num_dst give an empty or a shortened range, never one outside the tensors.
+struct Chunk {
+    int32_t first, count;
+    int64_t pos0;
+};
+__device__ __forceinline__ Chunk chunk_of(const Pages &c, int b) {
+    int32_t s = c.dst_ptr[b], e = c.dst_ptr[b + 1];
+    s = s < 0 ? 0 : (s > c.num_dst ? c.num_dst : s);
+    e = e < s ? s : (e > c.num_dst ? c.num_dst : e);
+    return Chunk{s, e - s, static_cast<int64_t>(c.length[b]) - (e - s)};
+}
+
+// The page of position pos (>= 0) of sequence b, -1 where the table does not reach or names no page.
+__device__ __forceinline__ int32_t page_at(const Pages &c, int b, int64_t pos) {
+    const int64_t e = pos >> c.shift;
+    if (e >= c.table_width) return -1;
+    const int32_t id = c.table[static_cast<int64_t>(b) * c.table_width + e];
+    return id >= 0 && id < c.num_pages ? id : -1;
+}
+
+}  // namespace relattn
+}  // namespace tiga
