@@ -422,8 +422,8 @@ size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
  * Products of the inputs are exact and summed in fp32; the mass is the fp32 sum
  * of the fp32 weights; the weights enter the value product rounded to dtype.
  * Deterministic.  Requires width 64 or 128 (TIGA_EUNSUPPORTED otherwise), heads
- * a multiple of kv_heads, num_dst and num_src < 2^31 - 1024, batch * heads *
- * num_dst < 2^40, batch * kv_heads < 2^20, scale finite and > 0.
+ * a multiple of kv_heads, num_src and num_dst * heads / kv_heads < 2^31 - 1024,
+ * batch * heads * num_dst < 2^40, batch * kv_heads < 2^20, scale finite and > 0.
  * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
 int tiga_mp_attention_cross_fwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
                                 float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
@@ -559,7 +559,8 @@ size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t nu
  * is read there).  Rows behind dst_ptr[batch] are left as they were.  A value
  * row that is not finite reaches every row of its sequence's new tokens that
  * it shares a tile with: new tokens' values must be finite.
- * Requires heads a multiple of kv_heads, width 64 or 128, num_dst < 2^31 / heads,
+ * Requires heads a multiple of kv_heads, width 64 or 128, num_dst * heads <
+ * 2^31 - 1024, table_width * page_size < 2^31 - 1024,
  * batch < 2^16, scale finite and > 0.
  * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
 int tiga_mp_attention_paged_fwd(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,

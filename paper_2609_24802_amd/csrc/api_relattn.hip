@@ -59,6 +59,8 @@ int check_cross(const tiga_cross *rel) {
         return fail(TIGA_EUNSUPPORTED, "%s: batch * kv_heads must be < 2^20", what);
     if (static_cast<double>(rel->batch) * rel->heads * static_cast<double>(rel->num_dst) >= 1099511627776.0)
         return fail(TIGA_EUNSUPPORTED, "%s: batch * heads * num_dst must be < 2^40", what);
+    if (rel->kv_heads && rel->num_dst * (rel->heads / rel->kv_heads) >= kMaxRows)
+        return fail(TIGA_EUNSUPPORTED, "%s: num_dst * heads / kv_heads must be < 2^31 - 1024", what);
     return TIGA_OK;
 }
 
@@ -91,8 +93,8 @@ int check_cache_data(const char *what, const tiga_cache *c, const int32_t *dst_p
 
 int check_packed(const char *what, int64_t num_dst, int32_t heads) {
     if (num_dst < 0) return fail(TIGA_EINVAL, "%s: negative num_dst", what);
-    if (num_dst >= kMaxRows || num_dst * heads >= (int64_t(1) << 31))
-        return fail(TIGA_EUNSUPPORTED, "%s: num_dst * heads must be < 2^31", what);
+    if (num_dst >= kMaxRows || num_dst * heads >= kMaxRows)
+        return fail(TIGA_EUNSUPPORTED, "%s: num_dst * heads must be < 2^31 - 1024", what);
     return TIGA_OK;
 }
 

@@ -1,5 +1,18 @@
-// Online-softmax reducer over rectangular relations, forward: cross attention and causal attention of
-// new tokens over a paged cache.  One wavefront a destination row and head; the lanes hold the width.
+// Online-softmax reducer over rectangular relations, forward: cross attention over strided sources and causal
+// attention of new tokens over a paged cache.  With the reducer state of Section 5.2 (running maximum m, mass l,
+// accumulator o; states combine by rescaling into the common maximum):
+//   s_ij = scale * <q_i, k_j>,  y_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij),  lse_i = log sum_j exp(s_ij).
+//
+// Rows.  The heads that share a source head are rows over the same keys, so a sequence's rows for one source head are
+// (token, head of the group), `group` heads to a token; a tile holds BM of them.  An item is one (sequence, source
+// head, row tile).
+//
+// Work.  An item's keys come in tiles of BN.  Either every block takes whole items (direct), or the key tiles of all
+// items are laid end to end and every block takes an equal run of them: then a run's first and last item may be
+// parts, whose states (o, m, l) go to the workspace, and merge_kernel joins the parts of an item in order.  A run is
+// found from the lengths on the device, so neither sizes nor results depend on anything but the lengths, and a
+// captured call follows lengths that change between replays.
+#include "mfma16.hpp"
 #include "relation.hpp"
 #include "relattn.hpp"
 
@@ -8,129 +21,657 @@ namespace relattn {
 
 namespace {
 
-constexpr int kRows = 4;  // wavefronts (rows) per block
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr float kMassCap = 4096.0f;  // largest tile mass of a lane (and so weight) that keeps the reference point
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-struct F16 {
-    static __device__ __forceinline__ float get(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
-    static __device__ __forceinline__ uint16_t put(float f) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(f)); }
-};
-struct BF16 {
-    static __device__ __forceinline__ float get(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
-    static __device__ __forceinline__ uint16_t put(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
+struct Args {
+    Rows q, y;
+    float *lse;
+    int64_t lse_batch, lse_head;
+    float c;  // scale * log2 e: scores are kept in the log2 domain
+    int kv_heads, group;
+    // strided sources
+    Rows k, v;
+    const int32_t *len;
+    int32_t num_dst, num_src, batch;
+    // paged sources
+    Pages pages;
+    // split: partial states, 2 slots a block, and what they are of; NULL: direct
+    float *part;
+    int4 *rec;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int d = 1; d < kWave; d <<= 1) v += shfl_xor_f(v, d);
-    return v;
-}
+// What lies in the place of a page that the cache does not have: keys that give NaN to the rows that need them,
+// values that give nothing to the others.
+__device__ const uint32_t kNanRow[64] = {
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu,
+    0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+__device__ const uint32_t kZeroRow[64] = {0};
 
-struct State {
-    float m, l, o[2];
+// ------------------------------------------------------------------------------------------ work partition
+
+// A sequence: its rows [0, rows) (token first + r / group), and the keys that row r sees.
+struct Seq {
+    int32_t first, tokens, rows;
+    int64_t keys0;  // keys that token 0 sees; token t sees keys0 + t of a paged relation, keys0 of a strided one
 };
-
-template <class T, int D>
-__device__ __forceinline__ void key_step(State &s, const float *q, const uint16_t *k, const uint16_t *v, float c, bool bad) {
-    float dot = 0.0f;
-    for (int i = 0; i < D / 64; ++i) dot += q[i] * T::get(k[i * 64 + lane_id()]);
-    float t = wave_sum(dot) * c;
-    if (bad) t = __builtin_nanf("");
-    if (!(t <= s.m)) {
-        const float a = s.m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(s.m - t);
-        s.m = t;
-        s.l *= a;
-        for (int i = 0; i < D / 64; ++i) s.o[i] *= a;
+template <bool PAGED>
+__device__ __forceinline__ Seq seq_of(const Args &a, int b) {
+    if constexpr (PAGED) {
+        const Chunk ch = chunk_of(a.pages, b);
+        return Seq{ch.first, ch.count, ch.count * a.group, ch.pos0 + 1};
+    } else {
+        int32_t n = a.num_src;
+        if (a.len) n = a.len[b] < 0 ? 0 : (a.len[b] > n ? n : a.len[b]);
+        return Seq{0, a.num_dst, a.num_dst * a.group, n};
     }
-    const float p = s.m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(t - s.m);
-    s.l += p;
-    for (int i = 0; i < D / 64; ++i) s.o[i] += p * T::get(v[i * 64 + lane_id()]);
+}
+// Keys that row r of the sequence sees, at least 0.
+template <bool PAGED>
+__device__ __forceinline__ int64_t keys_of(const Args &a, const Seq &s, int r) {
+    const int64_t n = PAGED ? s.keys0 + r / a.group : s.keys0;
+    return n < 0 ? 0 : n;
 }
 
-template <class T, int D>
-__device__ __forceinline__ void finish(const State &s, uint16_t *y, float *lse) {
-    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;
-    for (int i = 0; i < D / 64; ++i) y[i * 64 + lane_id()] = T::put(s.o[i] * inv);
-    if (lse && lane_id() == 0) *lse = (s.m + __log2f(s.l)) * kLn2;
-}
-
-template <class T, int D>
-__global__ __launch_bounds__(kRows * kWave) void cross_kernel(Rows q, Rows k, Rows v, Rows y, float *lse,
-                                                             const int32_t *len, int64_t num_dst, int64_t num_src,
-                                                             int batch, int heads, int group, float c) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kWave;
-    if (r >= static_cast<int64_t>(batch) * heads * num_dst) return;
-    const int64_t i = r % num_dst;
-    const int h = static_cast<int>(r / num_dst % heads), b = static_cast<int>(r / num_dst / heads);
-    int64_t n = num_src;
-    if (len) n = len[b] < 0 ? 0 : (len[b] > num_src ? num_src : len[b]);
-    float qr[2];
-    for (int e = 0; e < D / 64; ++e) qr[e] = T::get(q.p[b * q.batch + h * q.head + i * q.row + e * 64 + lane_id()]);
-    const uint16_t *kp = k.p + b * k.batch + h / group * k.head, *vp = v.p + b * v.batch + h / group * v.head;
-    State s{-__builtin_inff(), 0.0f, {0.0f, 0.0f}};
-    for (int64_t j = 0; j < n; ++j) key_step<T, D>(s, qr, kp + j * k.row, vp + j * v.row, c, false);
-    finish<T, D>(s, const_cast<uint16_t *>(y.p) + b * y.batch + h * y.head + i * y.row, lse ? lse + r : nullptr);
-}
-
-template <class T, int D>
-__global__ __launch_bounds__(kRows * kWave) void paged_kernel(Pages cache, Rows q, Rows y, float *lse, int heads, int group,
-                                                             float c) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kWave;
-    if (r >= static_cast<int64_t>(cache.num_dst) * heads) return;
-    const int i = static_cast<int>(r / heads), h = static_cast<int>(r % heads);
-    for (int b = 0; b < cache.batch; ++b) {
-        const Chunk ch = chunk_of(cache, b);
-        if (i < ch.first || i >= ch.first + ch.count) continue;
-        const int64_t last = ch.pos0 + (i - ch.first);
-        float qr[2];
-        for (int e = 0; e < D / 64; ++e) qr[e] = T::get(q.p[h * q.head + i * q.row + e * 64 + lane_id()]);
-        State s{-__builtin_inff(), 0.0f, {0.0f, 0.0f}};
-        for (int64_t j = 0; j <= last; ++j) {
-            const int32_t page = page_at(cache, b, j);
-            const int64_t pg = page < 0 ? 0 : page, row = j & ((1 << cache.shift) - 1);
-            key_step<T, D>(s, qr, cache.k.p + pg * cache.k.batch + h / group * cache.k.head + row * cache.k.row,
-                           cache.v.p + pg * cache.v.batch + h / group * cache.v.head + row * cache.v.row, c, page < 0);
+// The row tiles of a sequence for one source head, weighted by their key tiles: tile j starts at start(j).  Causal
+// tiles see more keys the later they are; between the first and the last tile's count the weights rise
+// linearly (the weight only balances the blocks: a part of an item takes its share of the real key tiles).
+template <int BM, int BN>
+struct Tiles {
+    int32_t count;
+    int64_t w0;
+    double slope;  // (last - first) / (2 count)
+    template <bool PAGED>
+    static __device__ __forceinline__ Tiles of(const Args &a, const Seq &s, bool split) {
+        Tiles t;
+        t.count = (s.rows + BM - 1) / BM;
+        t.w0 = 1;
+        t.slope = 0.0;
+        if (split && t.count > 0) {
+            const int64_t n0 = keys_of<PAGED>(a, s, min(BM, s.rows) - 1), n1 = keys_of<PAGED>(a, s, s.rows - 1);
+            t.w0 = max(int64_t(1), (n0 + BN - 1) / BN);
+            const int64_t w1 = max(int64_t(1), (n1 + BN - 1) / BN);
+            t.slope = static_cast<double>(w1 - t.w0) / (2.0 * t.count);
         }
-        finish<T, D>(s, const_cast<uint16_t *>(y.p) + h * y.head + i * y.row,
-                     lse ? lse + static_cast<int64_t>(h) * cache.num_dst + i : nullptr);
-        return;
+        return t;
     }
+    __device__ __forceinline__ int64_t start(int64_t j) const {
+        return j * w0 + static_cast<int64_t>(slope * static_cast<double>(j) * static_cast<double>(j));
+    }
+    __device__ __forceinline__ int64_t total() const { return start(count); }
+    // the tile that holds weight position u < total()
+    __device__ __forceinline__ int32_t find(int64_t u) const {
+        int32_t lo = 0, hi = count - 1;
+        while (lo < hi) {
+            const int32_t mid = lo + (hi - lo + 1) / 2;
+            if (start(mid) <= u) lo = mid;
+            else hi = mid - 1;
+        }
+        return lo;
+    }
+};
+
+// One wavefront walks the run of its block: the wavefronts of a block do it alike.
+template <bool PAGED, int BM, int BN>
+struct Walk {
+    typedef Tiles<BM, BN> T;
+    int64_t u, end;   // position and end of the run
+    int64_t base;     // where sequence b starts
+    int32_t b;
+    Seq s;
+    T t;
+
+    __device__ __forceinline__ int64_t weight(const Args &a, int e) const {
+        if (e >= batch(a)) return 0;
+        return T::template of<PAGED>(a, seq_of<PAGED>(a, e), a.part != nullptr).total() * a.kv_heads;
+    }
+    static __device__ __forceinline__ int batch(const Args &a) { return PAGED ? a.pages.batch : a.batch; }
+
+    __device__ __forceinline__ void begin(const Args &a, int w, int blocks) {
+        int64_t all = 0;
+        const int nb = batch(a);
+        const int64_t first = weight(a, lane_id());
+        if constexpr (!PAGED) {
+            if (!a.len || !a.part) all = uniform64(first) * nb;  // every sequence alike
+        }
+        if (all == 0)
+            for (int e = 0; e < nb; e += kWave) all += wave_total(e == 0 ? first : weight(a, e + lane_id()));
+        const int64_t per = all / blocks, rem = all % blocks;
+        u = w * per + (w < rem ? w : rem);
+        end = u + per + (w < rem ? 1 : 0);
+        base = 0;
+        b = 0;
+        if (u >= end) return;
+        if constexpr (!PAGED) {
+            if (!a.len || !a.part) {
+                b = static_cast<int32_t>(u / uniform64(first));
+                base = b * uniform64(first);
+                load(a);
+                return;
+            }
+        }
+        for (int e = 0; e < nb; e += kWave) {
+            const int64_t mine = e == 0 ? first : weight(a, e + lane_id());
+            const int64_t incl = wave_incl_scan(mine);
+            const uint64_t past = __ballot(base + incl > u);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                b = e + l;
+                base += __shfl(incl - mine, l, kWave);
+                break;
+            }
+            base += __shfl(incl, kWave - 1, kWave);
+        }
+        base = uniform64(base);
+        b = uniform(b);
+        load(a);
+    }
+    static __device__ __forceinline__ int64_t wave_total(int64_t v) {
+        return uniform64(__shfl(wave_incl_scan(v), kWave - 1, kWave));
+    }
+    __device__ __forceinline__ void load(const Args &a) {
+        s = seq_of<PAGED>(a, b);
+        t = T::template of<PAGED>(a, s, a.part != nullptr);
+    }
+    // The next part of an item of the run: row tile j of source head `head`, key tiles [t0, t1) of n.  starts / ends:
+    // whether it holds the item's first and last share.
+    struct Piece {
+        int32_t head, j;
+        int32_t t0, t1, n;
+        bool starts, ends;
+    };
+    __device__ __forceinline__ bool next(const Args &a, Piece &p) {
+        if (u >= end) return false;
+        while (u >= base + t.total() * a.kv_heads) {  // the run is not at its end, so a later sequence holds u
+            base += t.total() * a.kv_heads;
+            ++b;
+            load(a);
+        }
+        const int64_t in = u - base;
+        p.head = static_cast<int32_t>(in / t.total());
+        const int64_t r = in - p.head * t.total();
+        p.j = t.find(r);
+        const int64_t at = t.start(p.j), w = t.start(p.j + 1) - at, off = r - at;
+        const int64_t take = min(w - off, end - u);
+        const int64_t keys = keys_of<PAGED>(a, s, min((p.j + 1) * BM, s.rows) - 1);
+        p.n = static_cast<int32_t>((keys + BN - 1) / BN);
+        p.t0 = static_cast<int32_t>(off * p.n / w);
+        p.t1 = static_cast<int32_t>((off + take) * p.n / w);
+        p.starts = off == 0;
+        p.ends = off + take == w;
+        u += take;
+        return true;
+    }
+};
+
+// ------------------------------------------------------------------------------------------ sources
+
+// Address of the 16-byte chunk `chunk` of the key and of the value row at position pos.
+template <bool PAGED>
+struct Source {
+    const uint16_t *k, *v;      // strided: the head's first row; paged: the head within page 0
+    int32_t b;
+    __device__ __forceinline__ void set(const Args &a, int b_, int head) {
+        b = b_;
+        if constexpr (PAGED) {
+            k = a.pages.k.p + head * a.pages.k.head;
+            v = a.pages.v.p + head * a.pages.v.head;
+        } else {
+            k = a.k.p + b * a.k.batch + head * a.k.head;
+            v = a.v.p + b * a.v.batch + head * a.v.head;
+        }
+    }
+    // the page of a position (paged only), looked up a tile ahead of its rows
+    __device__ __forceinline__ int32_t page(const Args &a, int64_t pos) const {
+        if constexpr (PAGED) return page_at(a.pages, b, pos);
+        return 0;
+    }
+    __device__ __forceinline__ const uint16_t *key(const Args &a, int64_t pos, int32_t page, int chunk) const {
+        if constexpr (PAGED) {
+            if (page < 0) return reinterpret_cast<const uint16_t *>(kNanRow) + 8 * chunk;
+            return k + page * a.pages.k.batch + (pos & ((1 << a.pages.shift) - 1)) * a.pages.k.row + 8 * chunk;
+        }
+        return k + pos * a.k.row + 8 * chunk;
+    }
+    __device__ __forceinline__ const uint16_t *value(const Args &a, int64_t pos, int32_t page, int chunk) const {
+        if constexpr (PAGED) {
+            if (page < 0) return reinterpret_cast<const uint16_t *>(kZeroRow) + 8 * chunk;
+            return v + page * a.pages.v.batch + (pos & ((1 << a.pages.shift) - 1)) * a.pages.v.row + 8 * chunk;
+        }
+        return v + pos * a.v.row + 8 * chunk;
+    }
+};
+
+// Start of row r's width in a [heads, rows, width] tensor of destinations, for source head `head`.
+__device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int b, const Seq &s, int head, int r) {
+    const int token = r / a.group, g = r - token * a.group;
+    return b * t.batch + static_cast<int64_t>(head * a.group + g) * t.head + static_cast<int64_t>(s.first + token) * t.row;
+}
+__device__ __forceinline__ int64_t lse_at(const Args &a, int b, const Seq &s, int head, int r) {
+    const int token = r / a.group, g = r - token * a.group;
+    return b * a.lse_batch + (head * a.group + g) * a.lse_head + s.first + token;
+}
+
+// ------------------------------------------------------------------------------------------ wide tiles
+
+template <int D>
+struct Geo {
+    static constexpr int BM = 128;                      // rows a tile: 32 a wavefront
+    static constexpr int CPR = D / 8;                   // 16-byte chunks per row
+    static constexpr int RB = 2 * D;                    // bytes per row
+    static constexpr int R = 256 / RB;                  // rows per 256-byte bank window
+    static constexpr int CH = D / 32;                   // 32-deep chunks of the score product
+    static constexpr int DB = D / 16;                   // 16-wide blocks of the output
+    static constexpr int BN = D == 64 ? 128 : 64;       // keys a tile
+    static constexpr int KB = BN / 16;                  // 16-key blocks of the score product
+    static constexpr int KC = BN / 32;                  // 32-key chunks of the value product
+    static constexpr int TILE = BN * RB;                // bytes of a K or V tile: 16 KB
+    static constexpr int LPW = TILE / 1024 / kWaves;    // 1-KB direct loads per wavefront, tile and operand
+};
+
+// LDS layouts, free of bank conflicts without padding: the 16-byte chunk c of key row k sits at chunk c ^ (k / R % CPR)
+// (16 keys of one chunk fall into 16 bank groups); the 32-byte block c / 2 of value row k at block c / 2 ^ (k / R % DB)
+// (the transposing read takes 4 keys x 16 widths per 16 lanes).
+template <int D>
+__device__ __forceinline__ int k_chunk(int k, int pc) { return pc ^ ((k / Geo<D>::R) % Geo<D>::CPR); }
+template <int D>
+__device__ __forceinline__ int v_chunk(int k, int pc) {
+    return (((pc >> 1) ^ ((k / Geo<D>::R) % Geo<D>::DB)) << 1) | (pc & 1);
+}
+
+template <class T, int D>
+struct State {
+    f4 o[Geo<D>::DB][2];
+    float m[2], l[2];  // l: this lane's share of the mass
+};
+
+// Weights 2^(c s - m) of query block qb and this lane's sum of them.  They enter the value product rounded to the
+// input type (the matrix cores' operand); the mass is of the unrounded fp32 weights.
+template <class T, int KB>
+__device__ __forceinline__ float weights(const f4 (*s)[2], int qb, float c, float m, u4 (*pb)[2]) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int kc = 0; kc < KB / 2; ++kc) {
+        float p[2][4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * kc + e][qb][i], c, -m));
+        sum += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
+        pb[kc][qb] = u4{T::pack(p[0][0], p[0][1]), T::pack(p[0][2], p[0][3]), T::pack(p[1][0], p[1][1]),
+                        T::pack(p[1][2], p[1][3])};
+    }
+    return sum;
+}
+
+// One key tile.  keys: how many of it the item sees; lim[qb]: how many this lane's row of block qb does.
+template <class T, int D>
+__device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<D>::CH], const uint8_t *kt,
+                                          const uint8_t *vt, const int *kr, const int *vr, float c, bool edge,
+                                          const int64_t *seen, int64_t k0, int g) {
+    using G = Geo<D>;
+    f4 s[G::KB][2];
+#pragma unroll
+    for (int ch = 0; ch < G::CH; ++ch)
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb) {
+            const u4 ka = *reinterpret_cast<const u4 *>(kt + kr[ch] + kb * 16 * G::RB);
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb)
+                s[kb][qb] = T::mma(ka, q[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[kb][qb]);
+        }
+    if (edge) {
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const int64_t left = seen[qb] - k0;
+            // key kb * 16 + 4 g + i is seen iff kb * 16 + i < left - 4 g
+            const int rel = static_cast<int>(left < 0 ? 0 : (left > G::BN ? G::BN : left)) - 4 * g;
+#pragma unroll
+            for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[kb][qb][i] = kb * 16 + i < rel ? s[kb][qb][i] : -__builtin_inff();
+        }
+    }
+    u4 pb[G::KC][2];
+    float sum[2];
+    __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) sum[qb] = weights<T, G::KB>(s, qb, c, st.m[qb], pb);
+    // Against the current reference point every weight is at most the lane's sum; up to the cap they stay inside
+    // every 16-bit type's range.  A larger sum, or NaN (the first tile, where m = -inf, always), moves the point.
+    if (!__all(sum[0] <= kMassCap && sum[1] <= kMassCap)) {
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            float mt = s[0][qb][0];
+#pragma unroll
+            for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[kb][qb][i]);
+            mt = column_max(mt) * c;
+            if (mt > st.m[qb]) {
+                const float alpha = __builtin_amdgcn_exp2f(st.m[qb] - mt);
+                st.m[qb] = mt;
+                st.l[qb] *= alpha;
+#pragma unroll
+                for (int db = 0; db < G::DB; ++db) st.o[db][qb] *= alpha;
+            }
+            // nothing seen so far: any finite point gives weights of 0
+            sum[qb] = weights<T, G::KB>(s, qb, c, st.m[qb] == -__builtin_inff() ? 0.0f : st.m[qb], pb);
+        }
+    }
+    st.l[0] += sum[0];
+    st.l[1] += sum[1];
+    __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+    for (int db = 0; db < G::DB; ++db)
+#pragma unroll
+        for (int kc = 0; kc < G::KC; ++kc) {
+            const u2 lo = lds_transposed16(vt + vr[db] + kc * 32 * G::RB);
+            const u2 hi = lds_transposed16(vt + vr[db] + (kc * 32 + 16) * G::RB);
+            const u4 va{lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) st.o[db][qb] = T::mma(va, pb[kc][qb], st.o[db][qb]);
+        }
+}
+
+// Partial state of a slot: o [rows of the tile][D], then m, then l [rows].
+template <int BM, int D>
+constexpr int64_t slot_floats() { return BM * (D + 2); }
+
+template <class T, int D, bool PAGED>
+__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args a) {
+    using G = Geo<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t k0buf[G::TILE], v0buf[G::TILE], k1buf[G::TILE], v1buf[G::TILE];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, g = lane >> 4;
+    const int block = static_cast<int>(xcd_block());
+
+    // where this lane's direct loads come from within a tile, and where it reads its operands
+    int krow[G::LPW], kch[G::LPW], vch[G::LPW], kr[G::CH], vr[G::DB];
+#pragma unroll
+    for (int r = 0; r < G::LPW; ++r) {
+        const int byte = (w * G::LPW + r) * 1024 + 16 * lane;
+        krow[r] = byte / G::RB;
+        kch[r] = k_chunk<D>(krow[r], byte % G::RB / 16);
+        vch[r] = v_chunk<D>(krow[r], byte % G::RB / 16);
+    }
+#pragma unroll
+    for (int ch = 0; ch < G::CH; ++ch) kr[ch] = col * G::RB + 16 * k_chunk<D>(col, ch * 4 + g);
+    {
+        const int row = 4 * g + col / 4, sw = (row / G::R) % G::DB;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) vr[db] = row * G::RB + 32 * (db ^ sw) + 8 * (col % 4);
+    }
+
+    Walk<PAGED, G::BM, G::BN> walk;
+    walk.begin(a, block, static_cast<int>(gridDim.x));
+    if (a.part && threadIdx.x == 0) {
+        a.rec[2 * block] = int4{0, 0, 0, 0};
+        a.rec[2 * block + 1] = int4{0, 0, 0, 0};
+    }
+    typename Walk<PAGED, G::BM, G::BN>::Piece pc;
+    while (walk.next(a, pc)) {
+        const Seq &s = walk.s;
+        const int r0 = pc.j * G::BM + w * 32;
+        Source<PAGED> src;
+        src.set(a, walk.b, pc.head);
+        const int64_t keys = keys_of<PAGED>(a, s, min((pc.j + 1) * G::BM, s.rows) - 1);  // of the tile's last row
+        u4 q[2][G::CH];
+        int64_t seen[2];
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const int r = min(r0 + qb * 16 + col, s.rows - 1);
+            const u4 *p = reinterpret_cast<const u4 *>(a.q.p + row_at(a, a.q, walk.b, s, pc.head, r));
+#pragma unroll
+            for (int ch = 0; ch < G::CH; ++ch) q[qb][ch] = p[ch * 4 + g];
+            seen[qb] = keys_of<PAGED>(a, s, r);
+        }
+        const bool any = r0 < s.rows;                                                      // rows of this wavefront
+        const int64_t least = keys_of<PAGED>(a, s, min(r0, s.rows - 1));                   // its first row sees
+        const int64_t most = keys_of<PAGED>(a, s, min(r0 + 31, s.rows - 1));               // its last row sees
+        State<T, D> st;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) st.o[db][0] = st.o[db][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        st.m[0] = st.m[1] = -__builtin_inff();
+        st.l[0] = st.l[1] = 0.0f;
+
+        // positions past the item's last key read that key: its scores there are masked
+        int32_t page[G::LPW];
+        auto at = [&](int kt, int r) { return min(static_cast<int64_t>(kt) * G::BN + krow[r], keys - 1); };
+        auto look_up = [&](int kt) {
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r) page[r] = src.page(a, at(kt, r));
+        };
+        auto stage = [&](int kt, uint8_t *kb, uint8_t *vb) {
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r) {
+                const int run = (w * G::LPW + r) * 1024;
+                const int64_t pos = at(kt, r);
+                load_to_lds16(src.key(a, pos, page[r], kch[r]), kb + run);
+                load_to_lds16(src.value(a, pos, page[r], vch[r]), vb + run);
+            }
+        };
+        auto step = [&](int kt, const uint8_t *kb, const uint8_t *vb) {
+            const int64_t k0 = static_cast<int64_t>(kt) * G::BN;
+            if (any && k0 < most) tile_step<T, D>(st, q, kb, vb, kr, vr, a.c, k0 + G::BN > least, seen, k0, g);
+        };
+        __syncthreads();  // the previous item's tiles are read
+        if (pc.t0 < pc.t1) {
+            look_up(pc.t0);
+            stage(pc.t0, k0buf, v0buf);
+            look_up(min(pc.t0 + 1, pc.t1 - 1));
+        }
+        for (int kt = pc.t0; kt < pc.t1; kt += 2) {
+            loads_arrived();
+            __syncthreads();
+            if (kt + 1 < pc.t1) stage(kt + 1, k1buf, v1buf);
+            look_up(min(kt + 2, pc.t1 - 1));
+            step(kt, k0buf, v0buf);
+            if (kt + 1 >= pc.t1) break;
+            loads_arrived();
+            __syncthreads();
+            if (kt + 2 < pc.t1) stage(kt + 2, k0buf, v0buf);
+            look_up(min(kt + 3, pc.t1 - 1));
+            step(kt + 1, k1buf, v1buf);
+        }
+
+        const bool whole = pc.starts && pc.ends;
+        const int slot = 2 * block + (pc.starts ? 1 : 0);
+        if (!whole && threadIdx.x == 0)
+            a.rec[slot] = int4{walk.b + 1, pc.head, pc.j, pc.ends ? 1 : 0};
+        float *const po = whole ? nullptr : a.part + slot * slot_floats<G::BM, D>();
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const float lt = column_sum(st.l[qb]);
+            const int r = r0 + qb * 16 + col;
+            if (r >= s.rows) continue;
+            if (whole) {
+                const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+                uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, walk.b, s, pc.head, r);
+#pragma unroll
+                for (int db = 0; db < G::DB; ++db) {
+                    const f4 v = st.o[db][qb] * inv;
+                    *reinterpret_cast<u2 *>(yr + db * 16 + g * 4) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+                }
+                if (a.lse && g == 0) a.lse[lse_at(a, walk.b, s, pc.head, r)] = (st.m[qb] + __log2f(lt)) * kLn2;
+            } else {
+                const int tr = r - pc.j * G::BM;
+#pragma unroll
+                for (int db = 0; db < G::DB; ++db) *reinterpret_cast<f4 *>(po + tr * D + db * 16 + g * 4) = st.o[db][qb];
+                if (g == 0) {
+                    po[G::BM * D + tr] = st.m[qb];
+                    po[G::BM * (D + 1) + tr] = lt;
+                }
+            }
+        }
+    }
+}
+
+// Joins the parts of the items that start in block x and end in a later one: a wavefront a row.
+template <class T, int D, bool PAGED, int BM>
+__global__ __launch_bounds__(kThreads) void merge_kernel(Args a, int blocks) {
+    constexpr int E = D / kWave;
+    const int x = blockIdx.x;
+    const int4 it = a.rec[2 * x + 1];
+    if (it.x == 0) return;
+    const int b = it.x - 1, head = it.y, j = it.z;
+    const Seq s = seq_of<PAGED>(a, b);
+    int last = x + 1;
+    while (last < blocks - 1 && a.rec[2 * last].w == 0) ++last;
+    const int rows = min(s.rows - j * BM, BM);
+    const int lane = lane_id();
+    for (int r = static_cast<int>(blockIdx.y) * kWaves + static_cast<int>(threadIdx.x) / kWave; r < rows;
+         r += static_cast<int>(gridDim.y) * kWaves) {
+        // part i: slot 1 of block x, then slot 0 of the blocks after it
+        auto part = [&](int i) { return a.part + (2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
+        const int n = last - x + 1;
+        float m = -__builtin_inff();
+        for (int i = lane; i < n; i += kWave) m = fmaxf(m, part(i)[BM * D + r]);
+        for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
+        const float ref = m == -__builtin_inff() ? 0.0f : m;
+        float l = 0.0f, o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.0f;
+        for (int i = 0; i < n; ++i) {
+            const float *p = part(i);
+            const float f = __builtin_amdgcn_exp2f(p[BM * D + r] - ref);
+            l += f * p[BM * (D + 1) + r];
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += f * p[r * D + lane * E + e];
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + lane * E;
+        if constexpr (E == 2) *reinterpret_cast<uint32_t *>(yr) = T::pack(o[0] * inv, o[1] * inv);
+        else *yr = static_cast<uint16_t>(T::pack(o[0] * inv, 0.0f));
+        if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launch
+
+// How a call is laid out, from what the host knows: sizes and upper bounds of the lengths.
+struct Plan {
+    int64_t blocks;
+    bool split;
+    size_t part_bytes, rec_bytes;
+};
+template <int BM, int BN, int D>
+Plan plan_for(int64_t items, int64_t longest) {
+    const int64_t resident = 2 * static_cast<int64_t>(device_cus());
+    const int64_t steps = ceil_div(longest < 1 ? 1 : longest, BN);
+    Plan p{items, false, 0, 0};
+    if (steps > 1 && items < 3 * resident) {
+        p.split = true;
+        p.blocks = items * steps < resident ? items * steps : resident;
+        p.part_bytes = sizeof(float) * 2 * p.blocks * slot_floats<BM, D>();
+        p.rec_bytes = sizeof(int4) * 2 * p.blocks;
+    }
+    return p;
+}
+
+template <class F>
+auto by_type(int dtype, int width, F f) {
+    if (dtype == TIGA_DT_F16) return width == 64 ? f(Half16{}, Geo<64>{}) : f(Half16{}, Geo<128>{});
+    return width == 64 ? f(Brain16{}, Geo<64>{}) : f(Brain16{}, Geo<128>{});
+}
+template <int D>
+constexpr int width_of(Geo<D>) { return D; }
+
+template <class G>
+Plan cross_plan(const tiga_cross &rel) {
+    const int64_t rows = rel.num_dst * (rel.heads / rel.kv_heads);
+    return plan_for<G::BM, G::BN, G::CPR * 8>(ceil_div(rows, G::BM) * rel.batch * rel.kv_heads, rel.num_src);
+}
+template <class G>
+Plan paged_plan(const tiga_cache &c, int64_t num_dst, int32_t heads) {
+    const int64_t rows = num_dst * (heads / c.kv_heads);
+    const int64_t some = num_dst < c.batch ? num_dst : c.batch;  // sequences with new tokens, at most
+    return plan_for<G::BM, G::BN, G::CPR * 8>((rows / G::BM + some) * c.kv_heads,
+                                              static_cast<int64_t>(c.table_width) * c.page_size);
+}
+
+size_t plan_ws(const Plan &p) {
+    Carve c(nullptr);
+    c.take<char>(p.part_bytes);
+    c.take<char>(p.rec_bytes);
+    return c.bytes() < 256 ? 256 : c.bytes();
+}
+
+template <class T, int D, bool PAGED>
+int run(const Plan &p, Args a, void *ws, hipStream_t stream) {
+    using G = Geo<D>;
+    if (p.blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "attention: too many row tiles (%lld)", (long long)p.blocks);
+    if (p.split) {
+        Carve c(ws);
+        a.part = reinterpret_cast<float *>(c.take<char>(p.part_bytes));
+        a.rec = reinterpret_cast<int4 *>(c.take<char>(p.rec_bytes));
+    }
+    prof_before(stream);
+    hipLaunchKernelGGL((wide_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks)), dim3(kThreads), 0, stream, a);
+    prof_after(stream);
+    if (int rc = check_launch("attention forward")) return rc;
+    if (!p.split) return TIGA_OK;
+    hipLaunchKernelGGL((merge_kernel<T, D, PAGED, G::BM>), dim3(static_cast<unsigned>(p.blocks), G::BM / 16),
+                       dim3(kThreads), 0, stream, a, static_cast<int>(p.blocks));
+    return check_launch("attention merge");
 }
 
 }  // namespace
 
-size_t cross_fwd_ws_bytes(const tiga_cross &) { return 256; }
-size_t paged_fwd_ws_bytes(const tiga_cache &, int64_t, int32_t) { return 256; }
+size_t cross_fwd_ws_bytes(const tiga_cross &rel) {
+    if (rel.kv_heads == 0) return 256;
+    return by_type(rel.dtype, rel.width, [&](auto, auto g) { return plan_ws(cross_plan<decltype(g)>(rel)); });
+}
+size_t paged_fwd_ws_bytes(const tiga_cache &c, int64_t num_dst, int32_t heads) {
+    if (c.kv_heads == 0) return 256;
+    return by_type(c.dtype, c.width, [&](auto, auto g) { return plan_ws(paged_plan<decltype(g)>(c, num_dst, heads)); });
+}
 
 int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, float scale,
-                  const tiga_view &y, float *lse, void *, hipStream_t stream) {
-    const int64_t blocks = ceil_div(rel.num_dst * rel.heads * rel.batch, kRows);
-    if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention: too many rows");
-    auto go = [&](auto kernel) {
-        prof_before(stream);
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kRows * kWave), 0, stream, rows_of(q),
-                           rows_of(k), rows_of(v), rows_of(y), lse, rel.src_len, rel.num_dst, rel.num_src, rel.batch,
-                           rel.heads, rel.heads / rel.kv_heads, scale * kLog2e);
-        prof_after(stream);
-        return check_launch("cross attention forward");
-    };
-    if (rel.dtype == TIGA_DT_F16) return rel.width == 64 ? go(cross_kernel<F16, 64>) : go(cross_kernel<F16, 128>);
-    return rel.width == 64 ? go(cross_kernel<BF16, 64>) : go(cross_kernel<BF16, 128>);
+                  const tiga_view &y, float *lse, void *ws, hipStream_t stream) {
+    Args a{};
+    a.q = rows_of(q);
+    a.y = rows_of(y);
+    a.lse = lse;
+    a.lse_head = rel.num_dst;
+    a.lse_batch = rel.num_dst * rel.heads;
+    a.c = scale * kLog2e;
+    a.kv_heads = rel.kv_heads;
+    a.group = rel.heads / rel.kv_heads;
+    a.k = rows_of(k);
+    a.v = rows_of(v);
+    a.len = rel.src_len;
+    a.num_dst = static_cast<int32_t>(rel.num_dst);
+    a.num_src = static_cast<int32_t>(rel.num_src);
+    a.batch = rel.batch;
+    return by_type(rel.dtype, rel.width, [&](auto t, auto g) {
+        return run<decltype(t), decltype(g)::CPR * 8, false>(cross_plan<decltype(g)>(rel), a, ws, stream);
+    });
 }
 
 int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads, const tiga_view &q,
-                  float scale, const tiga_view &y, float *lse, void *, hipStream_t stream) {
-    const int64_t blocks = ceil_div(num_dst * heads, kRows);
-    auto go = [&](auto kernel) {
-        prof_before(stream);
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kRows * kWave), 0, stream,
-                           pages_of(cache, num_dst, dst_ptr), rows_of(q), rows_of(y), lse, heads,
-                           heads / cache.kv_heads, scale * kLog2e);
-        prof_after(stream);
-        return check_launch("paged attention forward");
-    };
-    if (cache.dtype == TIGA_DT_F16) return cache.width == 64 ? go(paged_kernel<F16, 64>) : go(paged_kernel<F16, 128>);
-    return cache.width == 64 ? go(paged_kernel<BF16, 64>) : go(paged_kernel<BF16, 128>);
+                  float scale, const tiga_view &y, float *lse, void *ws, hipStream_t stream) {
+    Args a{};
+    a.q = rows_of(q);
+    a.y = rows_of(y);
+    a.lse = lse;
+    a.lse_head = num_dst;
+    a.c = scale * kLog2e;
+    a.kv_heads = cache.kv_heads;
+    a.group = heads / cache.kv_heads;
+    a.pages = pages_of(cache, num_dst, dst_ptr);
+    return by_type(cache.dtype, cache.width, [&](auto t, auto g) {
+        return run<decltype(t), decltype(g)::CPR * 8, true>(paged_plan<decltype(g)>(cache, num_dst, heads), a, ws, stream);
+    });
 }
 
 }  // namespace relattn
