@@ -516,6 +516,236 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args a) {
     }
 }
 
+// ------------------------------------------------------------------------------------------ narrow tiles
+
+// Few rows (single tokens): 16 rows a tile, so one column block of the matrix product, and the time is that of reading
+// the keys and values.  The four wavefronts take turns of KW keys each, with no barrier between them until the item's
+// end: a wavefront's keys go to registers in the operand's layout, its values through its own LDS for the
+// transposing read, both a step ahead (16 KB in flight a wavefront, 128 KB a compute unit).
+template <int D>
+struct Thin {
+    static constexpr int BM = 16;
+    static constexpr int KW = 4096 / D;                 // keys of a wavefront's step: 8 KB of keys, 8 KB of values
+    static constexpr int BN = kWaves * KW;
+    static constexpr int CPR = D / 8, RB = 2 * D, R = 256 / RB;
+    static constexpr int CH = D / 32, DB = D / 16;
+    static constexpr int KB = KW / 16, KC = KW / 32;
+    static constexpr int RUNS = KW * RB / 1024;         // 1-KB direct loads of values a step
+    static constexpr int LOADS = RUNS + KB * CH;        // loads a step
+};
+
+template <class T, int D>
+struct ThinState {
+    f4 o[Thin<D>::DB];
+    float m, l;
+};
+
+template <class T, int D>
+__device__ __forceinline__ void thin_step(ThinState<T, D> &st, const u4 *q, const u4 (&k)[Thin<D>::KB][Thin<D>::CH],
+                                          const uint8_t *vt, const int *vr, float c, bool edge, int64_t left, int g) {
+    using G = Thin<D>;
+    f4 s[G::KB];
+#pragma unroll
+    for (int ch = 0; ch < G::CH; ++ch)
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb) s[kb] = T::mma(k[kb][ch], q[ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[kb]);
+    if (edge) {
+        const int rel = static_cast<int>(left < 0 ? 0 : (left > G::KW ? G::KW : left)) - 4 * g;
+#pragma unroll
+        for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[kb][i] = kb * 16 + i < rel ? s[kb][i] : -__builtin_inff();
+    }
+    float mt = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < G::KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[kb][i]);
+    mt = column_max(mt) * c;
+    if (__any(mt > st.m)) {
+        const float m = fmaxf(mt, st.m);
+        const float alpha = m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m - m);
+        st.m = m;
+        st.l *= alpha;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) st.o[db] *= alpha;
+    }
+    const float ref = st.m == -__builtin_inff() ? 0.0f : st.m;  // nothing seen so far: weights of 0
+    u4 pb[G::KC];
+#pragma unroll
+    for (int kc = 0; kc < G::KC; ++kc) {
+        float p[2][4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * kc + e][i], c, -ref));
+        st.l += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
+        pb[kc] = u4{T::pack(p[0][0], p[0][1]), T::pack(p[0][2], p[0][3]), T::pack(p[1][0], p[1][1]),
+                    T::pack(p[1][2], p[1][3])};
+    }
+#pragma unroll
+    for (int db = 0; db < G::DB; ++db)
+#pragma unroll
+        for (int kc = 0; kc < G::KC; ++kc) {
+            const u2 lo = lds_transposed16(vt + vr[db] + kc * 32 * G::RB);
+            const u2 hi = lds_transposed16(vt + vr[db] + (kc * 32 + 16) * G::RB);
+            st.o[db] = T::mma(u4{lo.x, lo.y, hi.x, hi.y}, pb[kc], st.o[db]);
+        }
+}
+
+template <class T, int D, bool PAGED>
+__global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
+    using G = Thin<D>;
+    constexpr int WAVE = G::KW * G::RB;  // bytes of a wavefront's step of values: 8 KB, also 16 rows of fp32 states or more
+    static_assert(WAVE >= G::BM * D * 4, "a wavefront's state fits its buffer");
+    __shared__ __attribute__((aligned(1024))) uint8_t v0buf[kWaves * WAVE], v1buf[kWaves * WAVE];
+    __shared__ float ml[2][kWaves][G::BM];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, g = lane >> 4;
+    const int block = static_cast<int>(xcd_block());
+    uint8_t *const v0 = v0buf + w * WAVE, *const v1 = v1buf + w * WAVE;
+
+    int vr[G::DB];
+    {
+        const int row = 4 * g + col / 4, sw = (row / G::R) % G::DB;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) vr[db] = row * G::RB + 32 * (db ^ sw) + 8 * (col % 4);
+    }
+
+    Walk<PAGED, G::BM, G::BN> walk;
+    walk.begin(a, block, static_cast<int>(gridDim.x));
+    if (a.part && threadIdx.x == 0) {
+        a.rec[2 * block] = int4{0, 0, 0, 0};
+        a.rec[2 * block + 1] = int4{0, 0, 0, 0};
+    }
+    typename Walk<PAGED, G::BM, G::BN>::Piece pc;
+    while (walk.next(a, pc)) {
+        const Seq &s = walk.s;
+        const int r0 = pc.j * G::BM;
+        Source<PAGED> src;
+        src.set(a, walk.b, pc.head);
+        const int64_t keys = keys_of<PAGED>(a, s, min(r0 + G::BM, s.rows) - 1);
+        const int64_t least = keys_of<PAGED>(a, s, r0);
+        const int r = min(r0 + col, s.rows - 1);
+        const int64_t seen = keys_of<PAGED>(a, s, r);
+        u4 q[G::CH];
+        {
+            const u4 *p = reinterpret_cast<const u4 *>(a.q.p + row_at(a, a.q, walk.b, s, pc.head, r));
+#pragma unroll
+            for (int ch = 0; ch < G::CH; ++ch) q[ch] = p[ch * 4 + g];
+        }
+        ThinState<T, D> st;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) st.o[db] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        st.m = -__builtin_inff();
+        st.l = 0.0f;
+
+        // the step's first key; positions past the last key read that key (masked)
+        auto first = [&](int kt) { return (static_cast<int64_t>(kt) * kWaves + w) * G::KW; };
+        auto at = [&](int kt, int i) { return min(first(kt) + i, keys - 1); };
+        auto look_up = [&](int kt) { return src.page(a, at(min(kt, pc.t1 - 1), lane % G::KW)); };
+        auto stage = [&](int kt, int32_t pages, u4 (&k)[G::KB][G::CH], uint8_t *vb) {
+#pragma unroll
+            for (int e = 0; e < G::RUNS; ++e) {
+                const int row = (e * 1024 + 16 * lane) / G::RB, pcs = (e * 1024 + 16 * lane) % G::RB / 16;
+                const int32_t pg = PAGED ? __shfl(pages, row, kWave) : 0;
+                load_to_lds16(src.value(a, at(kt, row), pg, v_chunk<D>(row, pcs)), vb + e * 1024);
+            }
+#pragma unroll
+            for (int kb = 0; kb < G::KB; ++kb) {
+                const int32_t pg = PAGED ? __shfl(pages, kb * 16 + col, kWave) : 0;
+                const u4 *p = reinterpret_cast<const u4 *>(src.key(a, at(kt, kb * 16 + col), pg, 0));
+#pragma unroll
+                for (int ch = 0; ch < G::CH; ++ch) k[kb][ch] = p[ch * 4 + g];
+            }
+        };
+        // Loads of the step before the one just issued have arrived (the issued ones, and a paged call's look-up before
+        // them, may be in flight), and this wavefront's LDS reads are done, so its other buffer may be filled.
+        auto arrived = [&](bool more) {
+            if (more) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"i"(G::LOADS) : "memory");
+            else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        };
+        auto reads_done = [] { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+        auto step = [&](int kt, const u4 (&k)[G::KB][G::CH], const uint8_t *vb) {
+            const int64_t k0 = first(kt);
+            if (k0 < keys) thin_step<T, D>(st, q, k, vb, vr, a.c, k0 + G::KW > least, seen - k0, g);
+        };
+        u4 ka[G::KB][G::CH], kb[G::KB][G::CH];
+        if (pc.t0 < pc.t1) {
+            int32_t pages = look_up(pc.t0), ahead = look_up(pc.t0 + 1);
+            stage(pc.t0, pages, ka, v0);
+            for (int kt = pc.t0; kt < pc.t1; kt += 2) {
+                const bool more = kt + 1 < pc.t1;
+                reads_done();
+                pages = ahead;
+                ahead = look_up(kt + 2);
+                if (more) stage(kt + 1, pages, kb, v1);
+                arrived(more);
+                step(kt, ka, v0);
+                if (!more) break;
+                const bool more2 = kt + 2 < pc.t1;
+                reads_done();
+                pages = ahead;
+                ahead = look_up(kt + 3);
+                if (more2) stage(kt + 2, pages, ka, v0);
+                arrived(more2);
+                step(kt + 1, kb, v1);
+            }
+        }
+
+        // join the four wavefronts' states
+        const float lt = column_sum(st.l);
+        reads_done();
+        __syncthreads();
+        float *const mine = reinterpret_cast<float *>(v0);
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) *reinterpret_cast<f4 *>(mine + col * D + db * 16 + g * 4) = st.o[db];
+        if (g == 0) {
+            ml[0][w][col] = st.m;
+            ml[1][w][col] = lt;
+        }
+        __syncthreads();
+        const bool whole = pc.starts && pc.ends;
+        const int slot = 2 * block + (pc.starts ? 1 : 0);
+        if (!whole && threadIdx.x == 0) a.rec[slot] = int4{walk.b + 1, pc.head, pc.j, pc.ends ? 1 : 0};
+        constexpr int E = G::BM * D / kThreads;  // widths a thread: 4 or 8
+        const int tr = threadIdx.x * E / D, d0 = threadIdx.x * E % D;
+        if (r0 + tr < s.rows) {
+            float m = ml[0][0][tr], l = 0.0f, o[E];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i) m = fmaxf(m, ml[0][i][tr]);
+            const float ref = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const float f = __builtin_amdgcn_exp2f(ml[0][i][tr] - ref);
+                l += f * ml[1][i][tr];
+                const float *p = reinterpret_cast<const float *>(v0buf + i * WAVE) + tr * D + d0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += f * p[e];
+            }
+            if (whole) {
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, walk.b, s, pc.head, r0 + tr) + d0;
+#pragma unroll
+                for (int e = 0; e < E; e += 4)
+                    *reinterpret_cast<u2 *>(yr + e) = u2{T::pack(o[e] * inv, o[e + 1] * inv), T::pack(o[e + 2] * inv, o[e + 3] * inv)};
+                if (a.lse && d0 == 0) a.lse[lse_at(a, walk.b, s, pc.head, r0 + tr)] = (ref + __log2f(l)) * kLn2;
+            } else {
+                float *const po = a.part + slot * slot_floats<G::BM, D>();
+#pragma unroll
+                for (int e = 0; e < E; e += 4) *reinterpret_cast<f4 *>(po + tr * D + d0 + e) = f4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+                if (d0 == 0) {
+                    po[G::BM * D + tr] = m;
+                    po[G::BM * (D + 1) + tr] = l;
+                }
+            }
+        }
+        __syncthreads();  // the states are read before the next item's values arrive
+    }
+}
+
 // Joins the parts of the items that start in block x and end in a later one: a wavefront a row.
 template <class T, int D, bool PAGED, int BM>
 __global__ __launch_bounds__(kThreads) void merge_kernel(Args a, int blocks) {
@@ -578,24 +808,34 @@ Plan plan_for(int64_t items, int64_t longest) {
     return p;
 }
 
-template <class F>
-auto by_type(int dtype, int width, F f) {
-    if (dtype == TIGA_DT_F16) return width == 64 ? f(Half16{}, Geo<64>{}) : f(Half16{}, Geo<128>{});
-    return width == 64 ? f(Brain16{}, Geo<64>{}) : f(Brain16{}, Geo<128>{});
-}
-template <int D>
-constexpr int width_of(Geo<D>) { return D; }
+// The tile shape: narrow tiles where a sequence has few rows for a source head.
+constexpr int64_t kThinRows = 16;
 
+template <class F>
+auto by_type(int dtype, int width, bool thin, F f) {
+    auto go = [&](auto t) {
+        if (width == 64) return thin ? f(t, Thin<64>{}) : f(t, Geo<64>{});
+        return thin ? f(t, Thin<128>{}) : f(t, Geo<128>{});
+    };
+    return dtype == TIGA_DT_F16 ? go(Half16{}) : go(Brain16{});
+}
+
+bool cross_thin(const tiga_cross &rel) { return rel.num_dst * (rel.heads / rel.kv_heads) <= kThinRows; }
 template <class G>
 Plan cross_plan(const tiga_cross &rel) {
     const int64_t rows = rel.num_dst * (rel.heads / rel.kv_heads);
     return plan_for<G::BM, G::BN, G::CPR * 8>(ceil_div(rows, G::BM) * rel.batch * rel.kv_heads, rel.num_src);
 }
+
+// sequences with new tokens, at most
+int64_t some_sequences(const tiga_cache &c, int64_t num_dst) { return num_dst < c.batch ? num_dst : c.batch; }
+bool paged_thin(const tiga_cache &c, int64_t num_dst, int32_t heads) {
+    return num_dst * (heads / c.kv_heads) <= kThinRows * some_sequences(c, num_dst);
+}
 template <class G>
 Plan paged_plan(const tiga_cache &c, int64_t num_dst, int32_t heads) {
     const int64_t rows = num_dst * (heads / c.kv_heads);
-    const int64_t some = num_dst < c.batch ? num_dst : c.batch;  // sequences with new tokens, at most
-    return plan_for<G::BM, G::BN, G::CPR * 8>((rows / G::BM + some) * c.kv_heads,
+    return plan_for<G::BM, G::BN, G::CPR * 8>((rows / G::BM + some_sequences(c, num_dst)) * c.kv_heads,
                                               static_cast<int64_t>(c.table_width) * c.page_size);
 }
 
@@ -606,9 +846,9 @@ size_t plan_ws(const Plan &p) {
     return c.bytes() < 256 ? 256 : c.bytes();
 }
 
-template <class T, int D, bool PAGED>
+template <class T, class G, bool PAGED>
 int run(const Plan &p, Args a, void *ws, hipStream_t stream) {
-    using G = Geo<D>;
+    constexpr int D = G::CPR * 8;
     if (p.blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "attention: too many row tiles (%lld)", (long long)p.blocks);
     if (p.split) {
         Carve c(ws);
@@ -616,7 +856,9 @@ int run(const Plan &p, Args a, void *ws, hipStream_t stream) {
         a.rec = reinterpret_cast<int4 *>(c.take<char>(p.rec_bytes));
     }
     prof_before(stream);
-    hipLaunchKernelGGL((wide_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks)), dim3(kThreads), 0, stream, a);
+    const dim3 grid(static_cast<unsigned>(p.blocks));
+    if constexpr (G::BM == 16) hipLaunchKernelGGL((thin_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((wide_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
     prof_after(stream);
     if (int rc = check_launch("attention forward")) return rc;
     if (!p.split) return TIGA_OK;
@@ -629,11 +871,12 @@ int run(const Plan &p, Args a, void *ws, hipStream_t stream) {
 
 size_t cross_fwd_ws_bytes(const tiga_cross &rel) {
     if (rel.kv_heads == 0) return 256;
-    return by_type(rel.dtype, rel.width, [&](auto, auto g) { return plan_ws(cross_plan<decltype(g)>(rel)); });
+    return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto, auto g) { return plan_ws(cross_plan<decltype(g)>(rel)); });
 }
 size_t paged_fwd_ws_bytes(const tiga_cache &c, int64_t num_dst, int32_t heads) {
     if (c.kv_heads == 0) return 256;
-    return by_type(c.dtype, c.width, [&](auto, auto g) { return plan_ws(paged_plan<decltype(g)>(c, num_dst, heads)); });
+    return by_type(c.dtype, c.width, paged_thin(c, num_dst, heads),
+                   [&](auto, auto g) { return plan_ws(paged_plan<decltype(g)>(c, num_dst, heads)); });
 }
 
 int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, float scale,
@@ -653,8 +896,8 @@ int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k,
     a.num_dst = static_cast<int32_t>(rel.num_dst);
     a.num_src = static_cast<int32_t>(rel.num_src);
     a.batch = rel.batch;
-    return by_type(rel.dtype, rel.width, [&](auto t, auto g) {
-        return run<decltype(t), decltype(g)::CPR * 8, false>(cross_plan<decltype(g)>(rel), a, ws, stream);
+    return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto t, auto g) {
+        return run<decltype(t), decltype(g), false>(cross_plan<decltype(g)>(rel), a, ws, stream);
     });
 }
 
@@ -669,8 +912,8 @@ int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_p
     a.kv_heads = cache.kv_heads;
     a.group = heads / cache.kv_heads;
     a.pages = pages_of(cache, num_dst, dst_ptr);
-    return by_type(cache.dtype, cache.width, [&](auto t, auto g) {
-        return run<decltype(t), decltype(g)::CPR * 8, true>(paged_plan<decltype(g)>(cache, num_dst, heads), a, ws, stream);
+    return by_type(cache.dtype, cache.width, paged_thin(cache, num_dst, heads), [&](auto t, auto g) {
+        return run<decltype(t), decltype(g), true>(paged_plan<decltype(g)>(cache, num_dst, heads), a, ws, stream);
     });
 }
 
