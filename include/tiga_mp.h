@@ -417,7 +417,8 @@ size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
  * A destination without sources (src_len[b] == 0) finalizes the reducer's
  * identity: y = 0, lse = -inf.  Sources at and past src_len[b] are not read.
  *   q, y: [batch, heads, num_dst, width];  k, v: [batch, kv_heads, num_src, width]
- *         of dtype, 16-byte aligned, strides multiples of 8; y is overwritten.
+ *         of dtype, 16-byte aligned, strides multiples of 8 (row strides of k and
+ *         v below 2^23); y is overwritten.
  *   lse:  fp32 [batch, heads, num_dst], contiguous, or NULL.
  * Products of the inputs are exact and summed in fp32; the mass is the fp32 sum
  * of the fp32 weights; the weights enter the value product rounded to dtype.
@@ -502,7 +503,8 @@ int tiga_mp_rotary_bwd(int32_t batch, int32_t heads, int64_t rows, int32_t width
 /* Keys and values of a batch of sequences in pages.  Position p of sequence b
  * lies in row p % page_size of page table[b * table_width + p / page_size].
  *   k, v:   views [num_pages, kv_heads, page_size, width] (batch is the page
- *           stride) of dtype, 16-byte aligned, strides multiples of 8.
+ *           stride) of dtype, 16-byte aligned, strides multiples of 8, row
+ *           strides below 2^23.
  *   table:  device int32 [batch, table_width]; entries past a sequence's length
  *           are not read.
  *   length: device int32 [batch], positions of each sequence, the new ones of a

@@ -12,6 +12,12 @@ namespace {
 
 bool bad_float(float v) { return !(v > -3.0e38f) || !(v < 3.0e38f); }
 
+// Rows of keys and values lie within 2^23 elements of each other: a tile's offsets are 32-bit.
+int check_rows(const char *what, const char *name, const tiga_view *v) {
+    if (v->row >= (int64_t(1) << 23)) return fail(TIGA_EUNSUPPORTED, "%s: the row stride of %s must be below 2^23", what, name);
+    return TIGA_OK;
+}
+
 // A 16-bit tensor whose rows are read and written 16 bytes at a time.
 int check_view(const char *what, const char *name, const tiga_view *v, bool output, int64_t batch, int64_t heads,
                int64_t rows) {
@@ -83,6 +89,8 @@ int check_cache_data(const char *what, const tiga_cache *c, const int32_t *dst_p
     if (c->num_pages < 1) return fail(TIGA_EINVAL, "%s: the cache has no pages", what);
     if (int rc = check_view(what, "the cache's k", &c->k, true, c->num_pages, c->kv_heads, c->page_size)) return rc;
     if (int rc = check_view(what, "the cache's v", &c->v, true, c->num_pages, c->kv_heads, c->page_size)) return rc;
+    if (int rc = check_rows(what, "the cache's k", &c->k)) return rc;
+    if (int rc = check_rows(what, "the cache's v", &c->v)) return rc;
     if ((!c->table && c->table_width > 0) || !c->length || !dst_ptr)
         return fail(TIGA_EINVAL, "%s: table, length and dst_ptr are required", what);
     if ((reinterpret_cast<uintptr_t>(c->table) | reinterpret_cast<uintptr_t>(c->length) |
@@ -118,6 +126,8 @@ int tiga_mp_attention_cross_fwd(const tiga_cross *rel, const tiga_view *q, const
     if (rel->num_src > 0) {
         if (int rc = check_view(what, "k", k, false, 0, 0, 0)) return rc;
         if (int rc = check_view(what, "v", v, false, 0, 0, 0)) return rc;
+        if (int rc = check_rows(what, "k", k)) return rc;
+        if (int rc = check_rows(what, "v", v)) return rc;
     }
     if (int rc = check_view(what, "y", y, true, rel->batch, rel->heads, rel->num_dst)) return rc;
     if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(TIGA_EINVAL, "%s: lse misaligned", what);

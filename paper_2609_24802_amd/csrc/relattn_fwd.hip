@@ -24,21 +24,32 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kMassCap = 4096.0f;  // largest tile mass of a lane (and so weight) that keeps the reference point
+constexpr int kSchedMfma = 0x008, kSchedDsRead = 0x100;  // instruction classes of the scheduler's groups
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// Strided sources, and the pages of a cache.
+struct Strided {
+    Rows k, v;
+    const int32_t *len;
+    int32_t num_dst, num_src, batch;
+};
+template <bool PAGED>
+struct SourceArgs {
+    typedef Strided type;
+};
+template <>
+struct SourceArgs<true> {
+    typedef Pages type;
+};
+template <bool PAGED>
 struct Args {
+    typename SourceArgs<PAGED>::type src;
     Rows q, y;
     float *lse;
     int64_t lse_batch, lse_head;
     float c;  // scale * log2 e: scores are kept in the log2 domain
     int kv_heads, group;
-    // strided sources
-    Rows k, v;
-    const int32_t *len;
-    int32_t num_dst, num_src, batch;
-    // paged sources
-    Pages pages;
     // split: partial states, 2 slots a block, and what they are of; NULL: direct
     float *part;
     int4 *rec;
@@ -61,25 +72,30 @@ __device__ const uint32_t kZeroRow[64] = {0};
 
 // A sequence: its rows [0, rows) (token first + r / group), and the keys that row r sees.
 struct Seq {
-    int32_t first, tokens, rows;
+    int32_t first, rows;
     int64_t keys0;  // keys that token 0 sees; token t sees keys0 + t of a paged relation, keys0 of a strided one
 };
 template <bool PAGED>
-__device__ __forceinline__ Seq seq_of(const Args &a, int b) {
+__device__ __forceinline__ Seq seq_of(const Args<PAGED> &a, int b) {
     if constexpr (PAGED) {
-        const Chunk ch = chunk_of(a.pages, b);
-        return Seq{ch.first, ch.count, ch.count * a.group, ch.pos0 + 1};
+        const Chunk ch = chunk_of(a.src, b);
+        return Seq{ch.first, ch.count * a.group, ch.pos0 + 1};
     } else {
-        int32_t n = a.num_src;
-        if (a.len) n = a.len[b] < 0 ? 0 : (a.len[b] > n ? n : a.len[b]);
-        return Seq{0, a.num_dst, a.num_dst * a.group, n};
+        int32_t n = a.src.num_src;
+        if (a.src.len) n = a.src.len[b] < 0 ? 0 : (a.src.len[b] > n ? n : a.src.len[b]);
+        return Seq{0, a.src.num_dst * a.group, n};
     }
 }
-// Keys that row r of the sequence sees, at least 0.
+// Keys that row r of the sequence sees, at least 0.  A row past the table's end sees one position behind it, which is
+// no page: it needs no more of them to become NaN.
 template <bool PAGED>
-__device__ __forceinline__ int64_t keys_of(const Args &a, const Seq &s, int r) {
-    const int64_t n = PAGED ? s.keys0 + r / a.group : s.keys0;
-    return n < 0 ? 0 : n;
+__device__ __forceinline__ int32_t keys_of(const Args<PAGED> &a, const Seq &s, int r) {
+    if constexpr (PAGED) {
+        const int64_t n = s.keys0 + r / a.group, most = (static_cast<int64_t>(a.src.table_width) << a.src.shift) + 1;
+        return static_cast<int32_t>(n < 0 ? 0 : (n > most ? most : n));
+    } else {
+        return static_cast<int32_t>(s.keys0);
+    }
 }
 
 // The row tiles of a sequence for one source head, weighted by their key tiles: tile j starts at start(j).  Causal
@@ -91,16 +107,16 @@ struct Tiles {
     int64_t w0;
     double slope;  // (last - first) / (2 count)
     template <bool PAGED>
-    static __device__ __forceinline__ Tiles of(const Args &a, const Seq &s, bool split) {
+    static __device__ __forceinline__ Tiles of(const Args<PAGED> &a, const Seq &s, bool split) {
         Tiles t;
         t.count = (s.rows + BM - 1) / BM;
         t.w0 = 1;
         t.slope = 0.0;
         if (split && t.count > 0) {
-            const int64_t n0 = keys_of<PAGED>(a, s, min(BM, s.rows) - 1), n1 = keys_of<PAGED>(a, s, s.rows - 1);
-            t.w0 = max(int64_t(1), (n0 + BN - 1) / BN);
-            const int64_t w1 = max(int64_t(1), (n1 + BN - 1) / BN);
-            t.slope = static_cast<double>(w1 - t.w0) / (2.0 * t.count);
+            const int32_t n0 = keys_of<PAGED>(a, s, min(BM, s.rows) - 1), n1 = keys_of<PAGED>(a, s, s.rows - 1);
+            const int32_t w1 = max(1, (n1 + BN - 1) / BN);
+            t.w0 = max(1, (n0 + BN - 1) / BN);
+            t.slope = static_cast<double>(w1 - static_cast<int32_t>(t.w0)) / (2.0 * t.count);
         }
         return t;
     }
@@ -130,18 +146,18 @@ struct Walk {
     Seq s;
     T t;
 
-    __device__ __forceinline__ int64_t weight(const Args &a, int e) const {
+    __device__ __forceinline__ int64_t weight(const Args<PAGED> &a, int e) const {
         if (e >= batch(a)) return 0;
         return T::template of<PAGED>(a, seq_of<PAGED>(a, e), a.part != nullptr).total() * a.kv_heads;
     }
-    static __device__ __forceinline__ int batch(const Args &a) { return PAGED ? a.pages.batch : a.batch; }
+    static __device__ __forceinline__ int batch(const Args<PAGED> &a) { return a.src.batch; }
 
-    __device__ __forceinline__ void begin(const Args &a, int w, int blocks) {
+    __device__ __forceinline__ void begin(const Args<PAGED> &a, int w, int blocks) {
         int64_t all = 0;
         const int nb = batch(a);
         const int64_t first = weight(a, lane_id());
         if constexpr (!PAGED) {
-            if (!a.len || !a.part) all = uniform64(first) * nb;  // every sequence alike
+            if (!a.src.len || !a.part) all = uniform64(first) * nb;  // every sequence alike
         }
         if (all == 0)
             for (int e = 0; e < nb; e += kWave) all += wave_total(e == 0 ? first : weight(a, e + lane_id()));
@@ -152,7 +168,7 @@ struct Walk {
         b = 0;
         if (u >= end) return;
         if constexpr (!PAGED) {
-            if (!a.len || !a.part) {
+            if (!a.src.len || !a.part) {
                 b = static_cast<int32_t>(u / uniform64(first));
                 base = b * uniform64(first);
                 load(a);
@@ -178,7 +194,7 @@ struct Walk {
     static __device__ __forceinline__ int64_t wave_total(int64_t v) {
         return uniform64(__shfl(wave_incl_scan(v), kWave - 1, kWave));
     }
-    __device__ __forceinline__ void load(const Args &a) {
+    __device__ __forceinline__ void load(const Args<PAGED> &a) {
         s = seq_of<PAGED>(a, b);
         t = T::template of<PAGED>(a, s, a.part != nullptr);
     }
@@ -189,7 +205,7 @@ struct Walk {
         int32_t t0, t1, n;
         bool starts, ends;
     };
-    __device__ __forceinline__ bool next(const Args &a, Piece &p) {
+    __device__ __forceinline__ bool next(const Args<PAGED> &a, Piece &p) {
         if (u >= end) return false;
         while (u >= base + t.total() * a.kv_heads) {  // the run is not at its end, so a later sequence holds u
             base += t.total() * a.kv_heads;
@@ -202,8 +218,7 @@ struct Walk {
         p.j = t.find(r);
         const int64_t at = t.start(p.j), w = t.start(p.j + 1) - at, off = r - at;
         const int64_t take = min(w - off, end - u);
-        const int64_t keys = keys_of<PAGED>(a, s, min((p.j + 1) * BM, s.rows) - 1);
-        p.n = static_cast<int32_t>((keys + BN - 1) / BN);
+        p.n = (keys_of<PAGED>(a, s, min((p.j + 1) * BM, s.rows) - 1) + BN - 1) / BN;
         p.t0 = static_cast<int32_t>(off * p.n / w);
         p.t1 = static_cast<int32_t>((off + take) * p.n / w);
         p.starts = off == 0;
@@ -215,48 +230,46 @@ struct Walk {
 
 // ------------------------------------------------------------------------------------------ sources
 
-// Address of the 16-byte chunk `chunk` of the key and of the value row at position pos.
+// Where the keys (or values) of one source head lie.  A position's row is at `at(u, page) + off`, with u the uniform
+// part (the tile's first position k0) and off the lane's (its row i of the tile, at most 127 rows): tiles start at
+// multiples of BN, so a page of at most BN rows starts at one of the tile's rows, and a larger one holds the tile whole.
 template <bool PAGED>
 struct Source {
-    const uint16_t *k, *v;      // strided: the head's first row; paged: the head within page 0
-    int32_t b;
-    __device__ __forceinline__ void set(const Args &a, int b_, int head) {
-        b = b_;
+    const uint16_t *p;
+    int64_t row, page_stride;
+    int32_t mask;  // rows of a page - 1; strided: all ones
+    __device__ __forceinline__ void set(const Args<PAGED> &a, const Rows &t, int b, int head) {
+        p = t.p + head * t.head;
+        row = t.row;
         if constexpr (PAGED) {
-            k = a.pages.k.p + head * a.pages.k.head;
-            v = a.pages.v.p + head * a.pages.v.head;
+            page_stride = t.batch;
+            mask = (1 << a.src.shift) - 1;
         } else {
-            k = a.k.p + b * a.k.batch + head * a.k.head;
-            v = a.v.p + b * a.v.batch + head * a.v.head;
+            p += b * t.batch;
         }
     }
-    // the page of a position (paged only), looked up a tile ahead of its rows
-    __device__ __forceinline__ int32_t page(const Args &a, int64_t pos) const {
-        if constexpr (PAGED) return page_at(a.pages, b, pos);
-        return 0;
+    // elements from the start of row i's page (of the tile, if it is strided) to chunk `chunk` of row i
+    __device__ __forceinline__ int32_t offset(int32_t i, int chunk) const {
+        return (PAGED ? i & mask : i) * static_cast<int32_t>(row) + 8 * chunk;
     }
-    __device__ __forceinline__ const uint16_t *key(const Args &a, int64_t pos, int32_t page, int chunk) const {
-        if constexpr (PAGED) {
-            if (page < 0) return reinterpret_cast<const uint16_t *>(kNanRow) + 8 * chunk;
-            return k + page * a.pages.k.batch + (pos & ((1 << a.pages.shift) - 1)) * a.pages.k.row + 8 * chunk;
-        }
-        return k + pos * a.k.row + 8 * chunk;
+    __device__ __forceinline__ const uint16_t *tile(int32_t k0) const {
+        return p + static_cast<int64_t>(PAGED ? k0 & mask : k0) * row;
     }
-    __device__ __forceinline__ const uint16_t *value(const Args &a, int64_t pos, int32_t page, int chunk) const {
-        if constexpr (PAGED) {
-            if (page < 0) return reinterpret_cast<const uint16_t *>(kZeroRow) + 8 * chunk;
-            return v + page * a.pages.v.batch + (pos & ((1 << a.pages.shift) - 1)) * a.pages.v.row + 8 * chunk;
-        }
-        return v + pos * a.v.row + 8 * chunk;
+    // the row of any position (>= 0)
+    __device__ __forceinline__ const uint16_t *at(int32_t pos, int32_t page) const {
+        if constexpr (PAGED) return p + page * page_stride + static_cast<int64_t>(pos & mask) * row;
+        else return p + pos * row;
     }
 };
 
 // Start of row r's width in a [heads, rows, width] tensor of destinations, for source head `head`.
-__device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int b, const Seq &s, int head, int r) {
+template <bool PAGED>
+__device__ __forceinline__ int64_t row_at(const Args<PAGED> &a, const Rows &t, int b, const Seq &s, int head, int r) {
     const int token = r / a.group, g = r - token * a.group;
     return b * t.batch + static_cast<int64_t>(head * a.group + g) * t.head + static_cast<int64_t>(s.first + token) * t.row;
 }
-__device__ __forceinline__ int64_t lse_at(const Args &a, int b, const Seq &s, int head, int r) {
+template <bool PAGED>
+__device__ __forceinline__ int64_t lse_at(const Args<PAGED> &a, int b, const Seq &s, int head, int r) {
     const int token = r / a.group, g = r - token * a.group;
     return b * a.lse_batch + (head * a.group + g) * a.lse_head + s.first + token;
 }
@@ -316,25 +329,33 @@ __device__ __forceinline__ float weights(const f4 (*s)[2], int qb, float c, floa
 // One key tile.  keys: how many of it the item sees; lim[qb]: how many this lane's row of block qb does.
 template <class T, int D>
 __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<D>::CH], const uint8_t *kt,
-                                          const uint8_t *vt, const int *kr, const int *vr, float c, bool edge,
-                                          const int64_t *seen, int64_t k0, int g) {
+                                          const uint8_t *vt, int kr, int vr, float c, bool edge,
+                                          const int32_t *seen, int32_t k0, int g) {
     using G = Geo<D>;
     f4 s[G::KB][2];
 #pragma unroll
     for (int ch = 0; ch < G::CH; ++ch)
 #pragma unroll
         for (int kb = 0; kb < G::KB; ++kb) {
-            const u4 ka = *reinterpret_cast<const u4 *>(kt + kr[ch] + kb * 16 * G::RB);
+            const u4 ka = *reinterpret_cast<const u4 *>(kt + (kr ^ (64 * ch)) + kb * 16 * G::RB);
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb)
                 s[kb][qb] = T::mma(ka, q[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[kb][qb]);
         }
+    // the operand reads run 4 ahead of their products
+    constexpr int kReads = G::CH * G::KB;
+    __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
+#pragma unroll
+    for (int i = 0; i < kReads - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 8, 0);
     if (edge) {
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
-            const int64_t left = seen[qb] - k0;
-            // key kb * 16 + 4 g + i is seen iff kb * 16 + i < left - 4 g
-            const int rel = static_cast<int>(left < 0 ? 0 : (left > G::BN ? G::BN : left)) - 4 * g;
+            // key kb * 16 + 4 g + i is seen iff kb * 16 + i < seen - k0 - 4 g
+            const int rel = seen[qb] - k0 - 4 * g;
 #pragma unroll
             for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
@@ -375,12 +396,21 @@ __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<
     for (int db = 0; db < G::DB; ++db)
 #pragma unroll
         for (int kc = 0; kc < G::KC; ++kc) {
-            const u2 lo = lds_transposed16(vt + vr[db] + kc * 32 * G::RB);
-            const u2 hi = lds_transposed16(vt + vr[db] + (kc * 32 + 16) * G::RB);
+            const uint8_t *const p = vt + (vr ^ (32 * db)) + kc * 32 * G::RB;
+            const u2 lo = lds_transposed16(p), hi = lds_transposed16(p + 16 * G::RB);
             const u4 va{lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb) st.o[db][qb] = T::mma(va, pb[kc][qb], st.o[db][qb]);
         }
+    // the operand reads (two a product pair) run 3 pairs ahead
+    constexpr int kPairs = G::DB * G::KC;
+    __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 6, 0);
+#pragma unroll
+    for (int i = 0; i < kPairs - 3; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 6, 0);
 }
 
 // Partial state of a slot: o [rows of the tile][D], then m, then l [rows].
@@ -388,15 +418,16 @@ template <int BM, int D>
 constexpr int64_t slot_floats() { return BM * (D + 2); }
 
 template <class T, int D, bool PAGED>
-__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args a) {
+__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
     using G = Geo<D>;
     __shared__ __attribute__((aligned(1024))) uint8_t k0buf[G::TILE], v0buf[G::TILE], k1buf[G::TILE], v1buf[G::TILE];
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, g = lane >> 4;
     const int block = static_cast<int>(xcd_block());
 
-    // where this lane's direct loads come from within a tile, and where it reads its operands
-    int krow[G::LPW], kch[G::LPW], vch[G::LPW], kr[G::CH], vr[G::DB];
+    // the rows and chunks of a tile that this lane's direct loads fetch, and where it reads its operands: the swizzles
+    // only flip bits that chunk (64 ch bytes) and block (32 db bytes) offsets flip too
+    int krow[G::LPW], kch[G::LPW], vch[G::LPW];
 #pragma unroll
     for (int r = 0; r < G::LPW; ++r) {
         const int byte = (w * G::LPW + r) * 1024 + 16 * lane;
@@ -404,13 +435,9 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args a) {
         kch[r] = k_chunk<D>(krow[r], byte % G::RB / 16);
         vch[r] = v_chunk<D>(krow[r], byte % G::RB / 16);
     }
-#pragma unroll
-    for (int ch = 0; ch < G::CH; ++ch) kr[ch] = col * G::RB + 16 * k_chunk<D>(col, ch * 4 + g);
-    {
-        const int row = 4 * g + col / 4, sw = (row / G::R) % G::DB;
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db) vr[db] = row * G::RB + 32 * (db ^ sw) + 8 * (col % 4);
-    }
+    const int kr = col * G::RB + 16 * k_chunk<D>(col, g);
+    const int vrow = 4 * g + col / 4;
+    const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
     Walk<PAGED, G::BM, G::BN> walk;
     walk.begin(a, block, static_cast<int>(gridDim.x));
@@ -422,11 +449,12 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args a) {
     while (walk.next(a, pc)) {
         const Seq &s = walk.s;
         const int r0 = pc.j * G::BM + w * 32;
-        Source<PAGED> src;
-        src.set(a, walk.b, pc.head);
-        const int64_t keys = keys_of<PAGED>(a, s, min((pc.j + 1) * G::BM, s.rows) - 1);  // of the tile's last row
+        Source<PAGED> ks, vs;
+        ks.set(a, a.src.k, walk.b, pc.head);
+        vs.set(a, a.src.v, walk.b, pc.head);
+        const int32_t keys = keys_of<PAGED>(a, s, min((pc.j + 1) * G::BM, s.rows) - 1);  // of the tile's last row
         u4 q[2][G::CH];
-        int64_t seen[2];
+        int32_t seen[2];
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             const int r = min(r0 + qb * 16 + col, s.rows - 1);
@@ -436,32 +464,57 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args a) {
             seen[qb] = keys_of<PAGED>(a, s, r);
         }
         const bool any = r0 < s.rows;                                                      // rows of this wavefront
-        const int64_t least = keys_of<PAGED>(a, s, min(r0, s.rows - 1));                   // its first row sees
-        const int64_t most = keys_of<PAGED>(a, s, min(r0 + 31, s.rows - 1));               // its last row sees
+        const int32_t least = keys_of<PAGED>(a, s, min(r0, s.rows - 1));                   // its first row sees
+        const int32_t most = keys_of<PAGED>(a, s, min(r0 + 31, s.rows - 1));               // its last row sees
         State<T, D> st;
 #pragma unroll
         for (int db = 0; db < G::DB; ++db) st.o[db][0] = st.o[db][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         st.m[0] = st.m[1] = -__builtin_inff();
         st.l[0] = st.l[1] = 0.0f;
 
-        // positions past the item's last key read that key: its scores there are masked
-        int32_t page[G::LPW];
-        auto at = [&](int kt, int r) { return min(static_cast<int64_t>(kt) * G::BN + krow[r], keys - 1); };
-        auto look_up = [&](int kt) {
+        int32_t ko[G::LPW], vo[G::LPW], page[G::LPW];
 #pragma unroll
-            for (int r = 0; r < G::LPW; ++r) page[r] = src.page(a, at(kt, r));
+        for (int r = 0; r < G::LPW; ++r) {
+            ko[r] = ks.offset(krow[r], kch[r]);
+            vo[r] = vs.offset(krow[r], vch[r]);
+        }
+        // a paged tile's pages, looked up a tile ahead of its rows; positions past the item's last key read that key
+        // (its scores there are masked), and a page that the cache does not have is read from the constant rows
+        auto look_up = [&](int kt) {
+            if constexpr (PAGED) {
+#pragma unroll
+                for (int r = 0; r < G::LPW; ++r) page[r] = page_at(a.src, walk.b, min(kt * G::BN + krow[r], keys - 1));
+            }
         };
         auto stage = [&](int kt, uint8_t *kb, uint8_t *vb) {
+            const int32_t k0 = kt * G::BN;
+            const bool full = k0 + G::BN <= keys;
+            const uint16_t *const kt0 = ks.tile(k0), *const vt0 = vs.tile(k0);
 #pragma unroll
             for (int r = 0; r < G::LPW; ++r) {
+                const uint16_t *kp = kt0 + ko[r], *vp = vt0 + vo[r];
+                if constexpr (PAGED) {
+                    kp += page[r] * ks.page_stride;
+                    vp += page[r] * vs.page_stride;
+                }
+                if (!full) {
+                    const int32_t pos = min(k0 + krow[r], keys - 1);
+                    kp = ks.at(pos, PAGED ? page[r] : 0) + 8 * kch[r];
+                    vp = vs.at(pos, PAGED ? page[r] : 0) + 8 * vch[r];
+                }
+                if constexpr (PAGED) {
+                    if (page[r] < 0) {
+                        kp = reinterpret_cast<const uint16_t *>(kNanRow) + 8 * kch[r];
+                        vp = reinterpret_cast<const uint16_t *>(kZeroRow) + 8 * vch[r];
+                    }
+                }
                 const int run = (w * G::LPW + r) * 1024;
-                const int64_t pos = at(kt, r);
-                load_to_lds16(src.key(a, pos, page[r], kch[r]), kb + run);
-                load_to_lds16(src.value(a, pos, page[r], vch[r]), vb + run);
+                load_to_lds16(kp, kb + run);
+                load_to_lds16(vp, vb + run);
             }
         };
         auto step = [&](int kt, const uint8_t *kb, const uint8_t *vb) {
-            const int64_t k0 = static_cast<int64_t>(kt) * G::BN;
+            const int32_t k0 = kt * G::BN;
             if (any && k0 < most) tile_step<T, D>(st, q, kb, vb, kr, vr, a.c, k0 + G::BN > least, seen, k0, g);
         };
         __syncthreads();  // the previous item's tiles are read
@@ -542,7 +595,7 @@ struct ThinState {
 
 template <class T, int D>
 __device__ __forceinline__ void thin_step(ThinState<T, D> &st, const u4 *q, const u4 (&k)[Thin<D>::KB][Thin<D>::CH],
-                                          const uint8_t *vt, const int *vr, float c, bool edge, int64_t left, int g) {
+                                          const uint8_t *vt, int vr, float c, bool edge, int32_t left, int g) {
     using G = Thin<D>;
     f4 s[G::KB];
 #pragma unroll
@@ -550,7 +603,7 @@ __device__ __forceinline__ void thin_step(ThinState<T, D> &st, const u4 *q, cons
 #pragma unroll
         for (int kb = 0; kb < G::KB; ++kb) s[kb] = T::mma(k[kb][ch], q[ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[kb]);
     if (edge) {
-        const int rel = static_cast<int>(left < 0 ? 0 : (left > G::KW ? G::KW : left)) - 4 * g;
+        const int rel = left - 4 * g;
 #pragma unroll
         for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
@@ -587,14 +640,14 @@ __device__ __forceinline__ void thin_step(ThinState<T, D> &st, const u4 *q, cons
     for (int db = 0; db < G::DB; ++db)
 #pragma unroll
         for (int kc = 0; kc < G::KC; ++kc) {
-            const u2 lo = lds_transposed16(vt + vr[db] + kc * 32 * G::RB);
-            const u2 hi = lds_transposed16(vt + vr[db] + (kc * 32 + 16) * G::RB);
+            const uint8_t *const p = vt + (vr ^ (32 * db)) + kc * 32 * G::RB;
+            const u2 lo = lds_transposed16(p), hi = lds_transposed16(p + 16 * G::RB);
             st.o[db] = T::mma(u4{lo.x, lo.y, hi.x, hi.y}, pb[kc], st.o[db]);
         }
 }
 
 template <class T, int D, bool PAGED>
-__global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
+__global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
     using G = Thin<D>;
     constexpr int WAVE = G::KW * G::RB;  // bytes of a wavefront's step of values: 8 KB, also 16 rows of fp32 states or more
     static_assert(WAVE >= G::BM * D * 4, "a wavefront's state fits its buffer");
@@ -605,12 +658,8 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
     const int block = static_cast<int>(xcd_block());
     uint8_t *const v0 = v0buf + w * WAVE, *const v1 = v1buf + w * WAVE;
 
-    int vr[G::DB];
-    {
-        const int row = 4 * g + col / 4, sw = (row / G::R) % G::DB;
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db) vr[db] = row * G::RB + 32 * (db ^ sw) + 8 * (col % 4);
-    }
+    const int vrow = 4 * g + col / 4;
+    const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
     Walk<PAGED, G::BM, G::BN> walk;
     walk.begin(a, block, static_cast<int>(gridDim.x));
@@ -622,12 +671,13 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
     while (walk.next(a, pc)) {
         const Seq &s = walk.s;
         const int r0 = pc.j * G::BM;
-        Source<PAGED> src;
-        src.set(a, walk.b, pc.head);
-        const int64_t keys = keys_of<PAGED>(a, s, min(r0 + G::BM, s.rows) - 1);
-        const int64_t least = keys_of<PAGED>(a, s, r0);
+        Source<PAGED> ks, vs;
+        ks.set(a, a.src.k, walk.b, pc.head);
+        vs.set(a, a.src.v, walk.b, pc.head);
+        const int32_t keys = keys_of<PAGED>(a, s, min(r0 + G::BM, s.rows) - 1);
+        const int32_t least = keys_of<PAGED>(a, s, r0);
         const int r = min(r0 + col, s.rows - 1);
-        const int64_t seen = keys_of<PAGED>(a, s, r);
+        const int32_t seen = keys_of<PAGED>(a, s, r);
         u4 q[G::CH];
         {
             const u4 *p = reinterpret_cast<const u4 *>(a.q.p + row_at(a, a.q, walk.b, s, pc.head, r));
@@ -641,22 +691,28 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
         st.l = 0.0f;
 
         // the step's first key; positions past the last key read that key (masked)
-        auto first = [&](int kt) { return (static_cast<int64_t>(kt) * kWaves + w) * G::KW; };
+        auto first = [&](int kt) { return (kt * kWaves + w) * G::KW; };
         auto at = [&](int kt, int i) { return min(first(kt) + i, keys - 1); };
-        auto look_up = [&](int kt) { return src.page(a, at(min(kt, pc.t1 - 1), lane % G::KW)); };
+        auto look_up = [&](int kt) {
+            if constexpr (PAGED) return page_at(a.src, walk.b, at(min(kt, pc.t1 - 1), lane % G::KW));
+            else return int32_t(0);
+        };
         auto stage = [&](int kt, int32_t pages, u4 (&k)[G::KB][G::CH], uint8_t *vb) {
 #pragma unroll
             for (int e = 0; e < G::RUNS; ++e) {
-                const int row = (e * 1024 + 16 * lane) / G::RB, pcs = (e * 1024 + 16 * lane) % G::RB / 16;
-                const int32_t pg = PAGED ? __shfl(pages, row, kWave) : 0;
-                load_to_lds16(src.value(a, at(kt, row), pg, v_chunk<D>(row, pcs)), vb + e * 1024);
+                const int row = (e * 1024 + 16 * lane) / G::RB, ch = v_chunk<D>(row, (e * 1024 + 16 * lane) % G::RB / 16);
+                const int32_t page = PAGED ? __shfl(pages, row, kWave) : 0;
+                const uint16_t *p = vs.at(at(kt, row), page);
+                if (PAGED && page < 0) p = reinterpret_cast<const uint16_t *>(kZeroRow);
+                load_to_lds16(p + 8 * ch, vb + e * 1024);
             }
 #pragma unroll
             for (int kb = 0; kb < G::KB; ++kb) {
-                const int32_t pg = PAGED ? __shfl(pages, kb * 16 + col, kWave) : 0;
-                const u4 *p = reinterpret_cast<const u4 *>(src.key(a, at(kt, kb * 16 + col), pg, 0));
+                const int32_t page = PAGED ? __shfl(pages, kb * 16 + col, kWave) : 0;
+                const uint16_t *p = ks.at(at(kt, kb * 16 + col), page);
+                if (PAGED && page < 0) p = reinterpret_cast<const uint16_t *>(kNanRow);
 #pragma unroll
-                for (int ch = 0; ch < G::CH; ++ch) k[kb][ch] = p[ch * 4 + g];
+                for (int ch = 0; ch < G::CH; ++ch) k[kb][ch] = reinterpret_cast<const u4 *>(p)[ch * 4 + g];
             }
         };
         // Loads of the step before the one just issued have arrived (the issued ones, and a paged call's look-up before
@@ -667,7 +723,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
         };
         auto reads_done = [] { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
         auto step = [&](int kt, const u4 (&k)[G::KB][G::CH], const uint8_t *vb) {
-            const int64_t k0 = first(kt);
+            const int32_t k0 = first(kt);
             if (k0 < keys) thin_step<T, D>(st, q, k, vb, vr, a.c, k0 + G::KW > least, seen - k0, g);
         };
         u4 ka[G::KB][G::CH], kb[G::KB][G::CH];
@@ -746,24 +802,32 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args a) {
     }
 }
 
-// Joins the parts of the items that start in block x and end in a later one: a wavefront a row.
+// Joins the parts of the items that start in block x and end in a later one.  A block takes a row at a time; its
+// wavefronts take every fourth part, eight of them in flight, and their sums are added in order.
 template <class T, int D, bool PAGED, int BM>
-__global__ __launch_bounds__(kThreads) void merge_kernel(Args a, int blocks) {
-    constexpr int E = D / kWave;
+__global__ __launch_bounds__(kThreads) void merge_kernel(Args<PAGED> a, int blocks) {
+    constexpr int E = D / kWave, U = 8;
+    __shared__ float so[kWaves][D], sl[kWaves];
     const int x = blockIdx.x;
     const int4 it = a.rec[2 * x + 1];
     if (it.x == 0) return;
     const int b = it.x - 1, head = it.y, j = it.z;
     const Seq s = seq_of<PAGED>(a, b);
-    int last = x + 1;
-    while (last < blocks - 1 && a.rec[2 * last].w == 0) ++last;
     const int rows = min(s.rows - j * BM, BM);
-    const int lane = lane_id();
-    for (int r = static_cast<int>(blockIdx.y) * kWaves + static_cast<int>(threadIdx.x) / kWave; r < rows;
-         r += static_cast<int>(gridDim.y) * kWaves) {
-        // part i: slot 1 of block x, then slot 0 of the blocks after it
-        auto part = [&](int i) { return a.part + (2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
-        const int n = last - x + 1;
+    if (static_cast<int>(blockIdx.y) >= rows) return;
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    // the parts: slot 1 of block x, then slot 0 of the blocks after it up to the one that holds the item's end
+    int n = 2;
+    for (int from = x + 1;; from += kWave) {
+        const int at = from + lane;
+        const uint64_t ends = __ballot(at >= blocks - 1 || a.rec[2 * at].w != 0);
+        if (ends) {
+            n = from + __builtin_ctzll(ends) - x + 1;
+            break;
+        }
+    }
+    auto part = [&](int i) { return a.part + (2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
+    for (int r = blockIdx.y; r < rows; r += static_cast<int>(gridDim.y)) {
         float m = -__builtin_inff();
         for (int i = lane; i < n; i += kWave) m = fmaxf(m, part(i)[BM * D + r]);
         for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
@@ -771,18 +835,42 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args a, int blocks) {
         float l = 0.0f, o[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = 0.0f;
-        for (int i = 0; i < n; ++i) {
-            const float *p = part(i);
-            const float f = __builtin_amdgcn_exp2f(p[BM * D + r] - ref);
-            l += f * p[BM * (D + 1) + r];
+        for (int i0 = w; i0 < n; i0 += kWaves * U) {
+            float f[U], pl[U], po[U][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += f * p[r * D + lane * E + e];
+            for (int i = 0; i < U; ++i) {  // parts past the last read it again, with weight 0
+                const int k = i0 + i * kWaves;
+                const float *p = part(k < n ? k : n - 1);
+                f[i] = k < n ? __builtin_amdgcn_exp2f(p[BM * D + r] - ref) : 0.0f;
+                pl[i] = k < n ? p[BM * (D + 1) + r] : 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) po[i][e] = k < n ? p[r * D + lane * E + e] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                l += f[i] * pl[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += f[i] * po[i][e];
+            }
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + lane * E;
-        if constexpr (E == 2) *reinterpret_cast<uint32_t *>(yr) = T::pack(o[0] * inv, o[1] * inv);
-        else *yr = static_cast<uint16_t>(T::pack(o[0] * inv, 0.0f));
-        if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
+#pragma unroll
+        for (int e = 0; e < E; ++e) so[w][lane * E + e] = o[e];
+        if (lane == 0) sl[w] = l;
+        __syncthreads();
+        if (w == 0) {
+            l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int d = lane * E + e;
+                o[e] = ((so[0][d] + so[1][d]) + (so[2][d] + so[3][d])) * inv;
+            }
+            uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + lane * E;
+            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(yr) = T::pack(o[0], o[1]);
+            else *yr = static_cast<uint16_t>(T::pack(o[0], 0.0f));
+            if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
+        }
+        __syncthreads();
     }
 }
 
@@ -847,7 +935,7 @@ size_t plan_ws(const Plan &p) {
 }
 
 template <class T, class G, bool PAGED>
-int run(const Plan &p, Args a, void *ws, hipStream_t stream) {
+int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
     constexpr int D = G::CPR * 8;
     if (p.blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "attention: too many row tiles (%lld)", (long long)p.blocks);
     if (p.split) {
@@ -862,7 +950,7 @@ int run(const Plan &p, Args a, void *ws, hipStream_t stream) {
     prof_after(stream);
     if (int rc = check_launch("attention forward")) return rc;
     if (!p.split) return TIGA_OK;
-    hipLaunchKernelGGL((merge_kernel<T, D, PAGED, G::BM>), dim3(static_cast<unsigned>(p.blocks), G::BM / 16),
+    hipLaunchKernelGGL((merge_kernel<T, D, PAGED, G::BM>), dim3(static_cast<unsigned>(p.blocks), G::BM == 16 ? 8 : 32),
                        dim3(kThreads), 0, stream, a, static_cast<int>(p.blocks));
     return check_launch("attention merge");
 }
@@ -881,7 +969,7 @@ size_t paged_fwd_ws_bytes(const tiga_cache &c, int64_t num_dst, int32_t heads) {
 
 int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, float scale,
                   const tiga_view &y, float *lse, void *ws, hipStream_t stream) {
-    Args a{};
+    Args<false> a{};
     a.q = rows_of(q);
     a.y = rows_of(y);
     a.lse = lse;
@@ -890,12 +978,8 @@ int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k,
     a.c = scale * kLog2e;
     a.kv_heads = rel.kv_heads;
     a.group = rel.heads / rel.kv_heads;
-    a.k = rows_of(k);
-    a.v = rows_of(v);
-    a.len = rel.src_len;
-    a.num_dst = static_cast<int32_t>(rel.num_dst);
-    a.num_src = static_cast<int32_t>(rel.num_src);
-    a.batch = rel.batch;
+    a.src = Strided{rows_of(k), rows_of(v), rel.src_len, static_cast<int32_t>(rel.num_dst),
+                    static_cast<int32_t>(rel.num_src), rel.batch};
     return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto t, auto g) {
         return run<decltype(t), decltype(g), false>(cross_plan<decltype(g)>(rel), a, ws, stream);
     });
@@ -903,7 +987,7 @@ int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k,
 
 int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads, const tiga_view &q,
                   float scale, const tiga_view &y, float *lse, void *ws, hipStream_t stream) {
-    Args a{};
+    Args<true> a{};
     a.q = rows_of(q);
     a.y = rows_of(y);
     a.lse = lse;
@@ -911,7 +995,7 @@ int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_p
     a.c = scale * kLog2e;
     a.kv_heads = cache.kv_heads;
     a.group = heads / cache.kv_heads;
-    a.pages = pages_of(cache, num_dst, dst_ptr);
+    a.src = pages_of(cache, num_dst, dst_ptr);
     return by_type(cache.dtype, cache.width, paged_thin(cache, num_dst, heads), [&](auto t, auto g) {
         return run<decltype(t), decltype(g), true>(paged_plan<decltype(g)>(cache, num_dst, heads), a, ws, stream);
     });
