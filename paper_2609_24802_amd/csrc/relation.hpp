@@ -44,12 +44,20 @@ __device__ __forceinline__ Chunk chunk_of(const Pages &c, int b) {
     return Chunk{s, e - s, static_cast<int64_t>(c.length[b]) - (e - s)};
 }
 
-// The page of position pos (>= 0) of sequence b, -1 where the table does not reach or names no page.
-__device__ __forceinline__ int32_t page_at(const Pages &c, int b, int64_t pos) {
+// The table's entry for position pos (>= 0) of sequence b, -1 where the table does not reach.  Only an entry that
+// is_page() accepts names a page; the check is apart so that a look-up ahead of its use need not wait for the load.
+__device__ __forceinline__ int32_t entry_at(const Pages &c, int b, int64_t pos) {
     const int64_t e = pos >> c.shift;
     if (e >= c.table_width) return -1;
-    const int32_t id = c.table[static_cast<int64_t>(b) * c.table_width + e];
-    return id >= 0 && id < c.num_pages ? id : -1;
+    return c.table[static_cast<int64_t>(b) * c.table_width + e];
+}
+__device__ __forceinline__ bool is_page(const Pages &c, int32_t id) {
+    return static_cast<uint32_t>(id) < static_cast<uint32_t>(c.num_pages);  // num_pages < 2^31
+}
+// The page of a position, -1 if there is none.
+__device__ __forceinline__ int32_t page_at(const Pages &c, int b, int64_t pos) {
+    const int32_t id = entry_at(c, b, pos);
+    return is_page(c, id) ? id : -1;
 }
 
 }  // namespace relattn

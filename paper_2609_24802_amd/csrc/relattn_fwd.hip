@@ -7,11 +7,14 @@
 // (token, head of the group), `group` heads to a token; a tile holds BM of them.  An item is one (sequence, source
 // head, row tile).
 //
-// Work.  An item's keys come in tiles of BN.  Either every block takes whole items (direct), or the key tiles of all
-// items are laid end to end and every block takes an equal run of them: then a run's first and last item may be
-// parts, whose states (o, m, l) go to the workspace, and merge_kernel joins the parts of an item in order.  A run is
-// found from the lengths on the device, so neither sizes nor results depend on anything but the lengths, and a
-// captured call follows lengths that change between replays.
+// Work.  An item's keys come in tiles of BN.  Where the items alone do not fill the device they are cut along the
+// keys, the parts' states (o, m, l) go to the workspace in fp32, and merge_kernel joins the parts of an item in order:
+//  - narrow tiles (few rows, bound by reading the keys): the key tiles of all items are laid end to end and every
+//    block walks an equal run of them (Walk), whatever the sequences' lengths;
+//  - wide tiles (many rows, bound by the matrix cores): items are cut into chunks of one number of key tiles, and chunks
+//    of the same keys are neighbours (Deal), so that the row tiles of a head read them from one XCD's L2 at one time.
+// Both are found from the lengths on the device, so a captured call follows lengths that change between replays, and
+// the result depends on the sizes and lengths alone.
 #include "mfma16.hpp"
 #include "relation.hpp"
 #include "relattn.hpp"
@@ -50,9 +53,10 @@ struct Args {
     int64_t lse_batch, lse_head;
     float c;  // scale * log2 e: scores are kept in the log2 domain
     int kv_heads, group;
-    // split: partial states, 2 slots a block, and what they are of; NULL: direct
+    // partial states and what they are of; NULL: items are not cut
     float *part;
     int4 *rec;
+    int slots;  // wide tiles: partial states there is room for, as many as blocks run at once
 };
 
 // What lies in the place of a page that the cache does not have: keys that give NaN to the rows that need them,
@@ -228,16 +232,138 @@ struct Walk {
     }
 };
 
+// Wide tiles: pieces in the order (sequence, source head, chunk of keys, row tile), chunks of `chunk` key tiles.  The row
+// tiles that reach into a chunk are the last ones of a causal sequence, all of a strided one, and they come last first.
+template <bool PAGED, int BM, int BN>
+struct Deal {
+    struct Load {
+        int64_t keys0;
+        int32_t tiles;    // row tiles of a head
+        int32_t n0, n1;   // key tiles of the first and the last of them, at least 1
+    };
+    int64_t pieces;
+    int32_t chunk;
+
+    static __device__ __forceinline__ Load load(const Args<PAGED> &a, const Seq &s) {
+        Load l{s.keys0, (s.rows + BM - 1) / BM, 1, 1};
+        if (s.rows > 0) {
+            l.n0 = max(1, (keys_of<PAGED>(a, s, min(BM, s.rows) - 1) + BN - 1) / BN);
+            l.n1 = max(1, (keys_of<PAGED>(a, s, s.rows - 1) + BN - 1) / BN);
+        }
+        return l;
+    }
+    static __device__ __forceinline__ Load load(const Args<PAGED> &a, int e) {
+        return e < a.src.batch ? load(a, seq_of<PAGED>(a, e)) : Load{0, 0, 1, 1};
+    }
+    static __device__ __forceinline__ bool alike(const Args<PAGED> &a) {
+        if constexpr (PAGED) return false;
+        else return a.src.len == nullptr;
+    }
+    // Sum of f(load) over the sequences, times the heads.
+    template <class F>
+    static __device__ __forceinline__ int64_t total(const Args<PAGED> &a, const Load &first, F f) {
+        if (alike(a)) return uniform64(f(first)) * a.src.batch * a.kv_heads;
+        int64_t all = 0;
+        for (int e = 0; e < a.src.batch; e += kWave) {
+            int64_t v = e == 0 ? f(first) : f(load(a, e + lane_id()));
+            for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
+            all += v;
+        }
+        return uniform64(all) * a.kv_heads;
+    }
+    static __device__ __forceinline__ int32_t parts(int32_t n, int32_t chunk) { return static_cast<int32_t>((n + static_cast<int64_t>(chunk) - 1) / chunk); }
+    // Row tiles that see keys of chunk c: token t does if keys0 + t > c * chunk * BN.
+    static __device__ __forceinline__ int32_t reach(const Args<PAGED> &a, const Load &l, int32_t c, int32_t chunk) {
+        if constexpr (PAGED) {
+            const int64_t t = static_cast<int64_t>(c) * chunk * BN - l.keys0 + 1;
+            return c == 0 || t <= 0 ? l.tiles : l.tiles - static_cast<int32_t>(t * a.group / BM);
+        } else {
+            return l.tiles;
+        }
+    }
+    // Pieces of one head.
+    static __device__ __forceinline__ int64_t count(const Args<PAGED> &a, const Load &l, int32_t chunk) {
+        const int32_t n = parts(l.n1, chunk);
+        if constexpr (!PAGED) return static_cast<int64_t>(n) * l.tiles;
+        // the chunks below the first token's keys are whole
+        const int64_t below = l.keys0 > 0 ? (l.keys0 - 1) / (static_cast<int64_t>(chunk) * BN) + 1 : 1;
+        int64_t all = min(static_cast<int64_t>(n), below) * l.tiles;
+        for (int64_t c = below; c < n; ++c) all += reach(a, l, static_cast<int32_t>(c), chunk);
+        return all;
+    }
+
+    // Chunks as small as lets all pieces run at once, but not below 4 tiles, whose work a part's 64 KB of state, written
+    // and read again, are worth.
+    __device__ __forceinline__ void begin(const Args<PAGED> &a) {
+        const Load first = load(a, lane_id());
+        chunk = 0x7fffffff;
+        pieces = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles); });
+        if (!a.part || pieces > a.slots) return;
+        const int64_t work = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles) * ((l.n0 + l.n1 + 1) / 2); });
+        int64_t c = max(int64_t(4), (work + a.slots - 1) / a.slots);
+        do {
+            chunk = static_cast<int32_t>(min(c, int64_t(0x7fffffff)));
+            pieces = total(a, first, [&](const Load &l) { return count(a, l, chunk); });
+            c += max(int64_t(1), c / 16);
+        } while (pieces > a.slots);
+    }
+
+    struct Piece {
+        int32_t b, head, j;
+        int32_t t0, t1;        // key tiles
+        int32_t part, parts;   // of the item
+    };
+    __device__ __forceinline__ Piece piece(const Args<PAGED> &a, int64_t p, Seq &s) const {
+        int64_t base = 0;
+        int b = 0;
+        const Load first = load(a, lane_id());
+        if (alike(a)) {
+            const int64_t per = uniform64(count(a, first, chunk)) * a.kv_heads;
+            b = static_cast<int>(p / per);
+            base = b * per;
+        } else {
+            for (int e = 0; e < a.src.batch; e += kWave) {
+                const int64_t mine = count(a, e == 0 ? first : load(a, e + lane_id()), chunk) * a.kv_heads;
+                const int64_t incl = wave_incl_scan(mine);
+                const uint64_t past = __ballot(base + incl > p);
+                if (past) {
+                    const int i = __builtin_ctzll(past);
+                    b = e + i;
+                    base += __shfl(incl - mine, i, kWave);
+                    break;
+                }
+                base += __shfl(incl, kWave - 1, kWave);
+            }
+            base = uniform64(base);
+            b = uniform(b);
+        }
+        s = seq_of<PAGED>(a, b);
+        const Load l = load(a, s);
+        const int64_t per = count(a, l, chunk);
+        Piece r;
+        r.b = b;
+        r.head = static_cast<int32_t>((p - base) / per);
+        int64_t rest = p - base - r.head * per;
+        r.part = 0;
+        for (int32_t here; rest >= (here = reach(a, l, r.part, chunk)); ++r.part) rest -= here;
+        r.j = l.tiles - 1 - static_cast<int32_t>(rest);
+        const int32_t n = (keys_of<PAGED>(a, s, min((r.j + 1) * BM, s.rows) - 1) + BN - 1) / BN;
+        r.parts = parts(max(1, n), chunk);
+        r.t0 = static_cast<int32_t>(min(static_cast<int64_t>(r.part) * chunk, static_cast<int64_t>(n)));
+        r.t1 = static_cast<int32_t>(min((r.part + int64_t(1)) * chunk, static_cast<int64_t>(n)));
+        return r;
+    }
+};
+
 // ------------------------------------------------------------------------------------------ sources
 
-// Where the keys (or values) of one source head lie.  A position's row is at `at(u, page) + off`, with u the uniform
-// part (the tile's first position k0) and off the lane's (its row i of the tile, at most 127 rows): tiles start at
-// multiples of BN, so a page of at most BN rows starts at one of the tile's rows, and a larger one holds the tile whole.
+// Where the keys (or values) of one source head lie.  Tiles start at multiples of BN, so a page of at most BN rows
+// starts at one of the tile's rows, and a larger one holds the tile whole.
 template <bool PAGED>
 struct Source {
     const uint16_t *p;
     int64_t row, page_stride;
-    int32_t mask;  // rows of a page - 1; strided: all ones
+    int32_t mask;  // rows of a page - 1
     __device__ __forceinline__ void set(const Args<PAGED> &a, const Rows &t, int b, int head) {
         p = t.p + head * t.head;
         row = t.row;
@@ -248,12 +374,13 @@ struct Source {
             p += b * t.batch;
         }
     }
-    // elements from the start of row i's page (of the tile, if it is strided) to chunk `chunk` of row i
-    __device__ __forceinline__ int32_t offset(int32_t i, int chunk) const {
-        return (PAGED ? i & mask : i) * static_cast<int32_t>(row) + 8 * chunk;
-    }
+    // start of the tile at k0 within its page
     __device__ __forceinline__ const uint16_t *tile(int32_t k0) const {
         return p + static_cast<int64_t>(PAGED ? k0 & mask : k0) * row;
+    }
+    // elements from there to row i of the tile: row strides are below 2^23 and tiles have at most 128 rows
+    __device__ __forceinline__ int32_t offset(int32_t i) const {
+        return (PAGED ? i & mask : i) * static_cast<int32_t>(row);
     }
     // the row of any position (>= 0)
     __device__ __forceinline__ const uint16_t *at(int32_t pos, int32_t page) const {
@@ -423,7 +550,6 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
     __shared__ __attribute__((aligned(1024))) uint8_t k0buf[G::TILE], v0buf[G::TILE], k1buf[G::TILE], v1buf[G::TILE];
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, g = lane >> 4;
-    const int block = static_cast<int>(xcd_block());
 
     // the rows and chunks of a tile that this lane's direct loads fetch, and where it reads its operands: the swizzles
     // only flip bits that chunk (64 ch bytes) and block (32 db bytes) offsets flip too
@@ -439,26 +565,31 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
-    Walk<PAGED, G::BM, G::BN> walk;
-    walk.begin(a, block, static_cast<int>(gridDim.x));
-    if (a.part && threadIdx.x == 0) {
-        a.rec[2 * block] = int4{0, 0, 0, 0};
-        a.rec[2 * block + 1] = int4{0, 0, 0, 0};
-    }
-    typename Walk<PAGED, G::BM, G::BN>::Piece pc;
-    while (walk.next(a, pc)) {
-        const Seq &s = walk.s;
+    // the blocks of one XCD (every eighth) take neighbouring pieces
+    Deal<PAGED, G::BM, G::BN> deal;
+    deal.begin(a);
+    const int x = blockIdx.x % kXcds;
+    const int64_t per = deal.pieces / kXcds, rem = deal.pieces % kXcds;
+    if (a.part && threadIdx.x == 0 && deal.pieces + blockIdx.x < a.slots) a.rec[2 * (deal.pieces + blockIdx.x)] = int4{0, 0, 0, 0};
+    for (int64_t i = blockIdx.x / kXcds; i < per + (x < rem ? 1 : 0); i += gridDim.x / kXcds) {
+        const int64_t id = x * per + min(static_cast<int64_t>(x), rem) + i;
+        Seq s;
+        const typename Deal<PAGED, G::BM, G::BN>::Piece pc = deal.piece(a, id, s);
+        if (a.part && threadIdx.x == 0 && id < a.slots) {
+            a.rec[2 * id] = pc.part == 0 && pc.parts > 1 ? int4{pc.b + 1, pc.head, pc.j, pc.parts} : int4{0, 0, 0, 0};
+            a.rec[2 * id + 1] = int4{deal.chunk, 0, 0, 0};
+        }
         const int r0 = pc.j * G::BM + w * 32;
         Source<PAGED> ks, vs;
-        ks.set(a, a.src.k, walk.b, pc.head);
-        vs.set(a, a.src.v, walk.b, pc.head);
+        ks.set(a, a.src.k, pc.b, pc.head);
+        vs.set(a, a.src.v, pc.b, pc.head);
         const int32_t keys = keys_of<PAGED>(a, s, min((pc.j + 1) * G::BM, s.rows) - 1);  // of the tile's last row
         u4 q[2][G::CH];
         int32_t seen[2];
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             const int r = min(r0 + qb * 16 + col, s.rows - 1);
-            const u4 *p = reinterpret_cast<const u4 *>(a.q.p + row_at(a, a.q, walk.b, s, pc.head, r));
+            const u4 *p = reinterpret_cast<const u4 *>(a.q.p + row_at(a, a.q, pc.b, s, pc.head, r));
 #pragma unroll
             for (int ch = 0; ch < G::CH; ++ch) q[qb][ch] = p[ch * 4 + g];
             seen[qb] = keys_of<PAGED>(a, s, r);
@@ -472,45 +603,37 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
         st.m[0] = st.m[1] = -__builtin_inff();
         st.l[0] = st.l[1] = 0.0f;
 
-        int32_t ko[G::LPW], vo[G::LPW], page[G::LPW];
-#pragma unroll
-        for (int r = 0; r < G::LPW; ++r) {
-            ko[r] = ks.offset(krow[r], kch[r]);
-            vo[r] = vs.offset(krow[r], vch[r]);
-        }
-        // a paged tile's pages, looked up a tile ahead of its rows; positions past the item's last key read that key
-        // (its scores there are masked), and a page that the cache does not have is read from the constant rows
-        auto look_up = [&](int kt) {
+        // A load's 1 KB are 4 or 8 rows from a multiple of as many, so in pages of 8 rows or more they lie in one page.
+        // Lane r looks load r's page up, a tile ahead of the rows; the entry is read and checked when they are loaded.
+        // Positions past the item's last key read that key (its scores there are masked); a page that the cache does
+        // not have is read from the constant rows.
+        auto look_up = [&](int kt) -> int32_t {
             if constexpr (PAGED) {
-#pragma unroll
-                for (int r = 0; r < G::LPW; ++r) page[r] = page_at(a.src, walk.b, min(kt * G::BN + krow[r], keys - 1));
+                const int group = (w * G::LPW + lane % G::LPW) * (1024 / G::RB);
+                return entry_at(a.src, pc.b, min(kt * G::BN + group, keys - 1));
+            } else {
+                return 0;
             }
         };
-        auto stage = [&](int kt, uint8_t *kb, uint8_t *vb) {
+        auto stage = [&](int kt, int32_t entry, uint8_t *kb, uint8_t *vb) {
             const int32_t k0 = kt * G::BN;
-            const bool full = k0 + G::BN <= keys;
             const uint16_t *const kt0 = ks.tile(k0), *const vt0 = vs.tile(k0);
 #pragma unroll
             for (int r = 0; r < G::LPW; ++r) {
-                const uint16_t *kp = kt0 + ko[r], *vp = vt0 + vo[r];
-                if constexpr (PAGED) {
-                    kp += page[r] * ks.page_stride;
-                    vp += page[r] * vs.page_stride;
-                }
-                if (!full) {
-                    const int32_t pos = min(k0 + krow[r], keys - 1);
-                    kp = ks.at(pos, PAGED ? page[r] : 0) + 8 * kch[r];
-                    vp = vs.at(pos, PAGED ? page[r] : 0) + 8 * vch[r];
-                }
-                if constexpr (PAGED) {
-                    if (page[r] < 0) {
-                        kp = reinterpret_cast<const uint16_t *>(kNanRow) + 8 * kch[r];
-                        vp = reinterpret_cast<const uint16_t *>(kZeroRow) + 8 * vch[r];
-                    }
-                }
                 const int run = (w * G::LPW + r) * 1024;
-                load_to_lds16(kp, kb + run);
-                load_to_lds16(vp, vb + run);
+                const int32_t i = min(krow[r], keys - 1 - k0);
+                const uint16_t *kp = kt0, *vp = vt0;
+                int32_t ko = ks.offset(i), vo = vs.offset(i);
+                if constexpr (PAGED) {
+                    const int32_t page = __builtin_amdgcn_readlane(entry, r);
+                    const bool good = is_page(a.src, page);
+                    kp = good ? kp + page * ks.page_stride : reinterpret_cast<const uint16_t *>(kNanRow);
+                    vp = good ? vp + page * vs.page_stride : reinterpret_cast<const uint16_t *>(kZeroRow);
+                    ko = good ? ko : 0;
+                    vo = good ? vo : 0;
+                }
+                load_to_lds16(kp + ko + 8 * kch[r], kb + run);
+                load_to_lds16(vp + vo + 8 * vch[r], vb + run);
             }
         };
         auto step = [&](int kt, const uint8_t *kb, const uint8_t *vb) {
@@ -518,30 +641,27 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
             if (any && k0 < most) tile_step<T, D>(st, q, kb, vb, kr, vr, a.c, k0 + G::BN > least, seen, k0, g);
         };
         __syncthreads();  // the previous item's tiles are read
+        int32_t entry = 0;
         if (pc.t0 < pc.t1) {
-            look_up(pc.t0);
-            stage(pc.t0, k0buf, v0buf);
-            look_up(min(pc.t0 + 1, pc.t1 - 1));
+            stage(pc.t0, look_up(pc.t0), k0buf, v0buf);
+            entry = look_up(min(pc.t0 + 1, pc.t1 - 1));
         }
         for (int kt = pc.t0; kt < pc.t1; kt += 2) {
             loads_arrived();
             __syncthreads();
-            if (kt + 1 < pc.t1) stage(kt + 1, k1buf, v1buf);
-            look_up(min(kt + 2, pc.t1 - 1));
+            if (kt + 1 < pc.t1) stage(kt + 1, entry, k1buf, v1buf);
+            entry = look_up(min(kt + 2, pc.t1 - 1));
             step(kt, k0buf, v0buf);
             if (kt + 1 >= pc.t1) break;
             loads_arrived();
             __syncthreads();
-            if (kt + 2 < pc.t1) stage(kt + 2, k0buf, v0buf);
-            look_up(min(kt + 3, pc.t1 - 1));
+            if (kt + 2 < pc.t1) stage(kt + 2, entry, k0buf, v0buf);
+            entry = look_up(min(kt + 3, pc.t1 - 1));
             step(kt + 1, k1buf, v1buf);
         }
 
-        const bool whole = pc.starts && pc.ends;
-        const int slot = 2 * block + (pc.starts ? 1 : 0);
-        if (!whole && threadIdx.x == 0)
-            a.rec[slot] = int4{walk.b + 1, pc.head, pc.j, pc.ends ? 1 : 0};
-        float *const po = whole ? nullptr : a.part + slot * slot_floats<G::BM, D>();
+        const bool whole = pc.parts == 1;
+        float *const po = whole ? nullptr : a.part + id * slot_floats<G::BM, D>();
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             const float lt = column_sum(st.l[qb]);
@@ -549,13 +669,13 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
             if (r >= s.rows) continue;
             if (whole) {
                 const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-                uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, walk.b, s, pc.head, r);
+                uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, pc.b, s, pc.head, r);
 #pragma unroll
                 for (int db = 0; db < G::DB; ++db) {
                     const f4 v = st.o[db][qb] * inv;
                     *reinterpret_cast<u2 *>(yr + db * 16 + g * 4) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
                 }
-                if (a.lse && g == 0) a.lse[lse_at(a, walk.b, s, pc.head, r)] = (st.m[qb] + __log2f(lt)) * kLn2;
+                if (a.lse && g == 0) a.lse[lse_at(a, pc.b, s, pc.head, r)] = (st.m[qb] + __log2f(lt)) * kLn2;
             } else {
                 const int tr = r - pc.j * G::BM;
 #pragma unroll
@@ -694,10 +814,15 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
         auto first = [&](int kt) { return (kt * kWaves + w) * G::KW; };
         auto at = [&](int kt, int i) { return min(first(kt) + i, keys - 1); };
         auto look_up = [&](int kt) {
-            if constexpr (PAGED) return page_at(a.src, walk.b, at(min(kt, pc.t1 - 1), lane % G::KW));
+            if constexpr (PAGED) return entry_at(a.src, walk.b, at(min(kt, pc.t1 - 1), lane % G::KW));
             else return int32_t(0);
         };
-        auto stage = [&](int kt, int32_t pages, u4 (&k)[G::KB][G::CH], uint8_t *vb) {
+        auto has = [&](int32_t entry) {
+            if constexpr (PAGED) return is_page(a.src, entry);
+            else return true;
+        };
+        auto stage = [&](int kt, int32_t entry, u4 (&k)[G::KB][G::CH], uint8_t *vb) {
+            const int32_t pages = PAGED && !has(entry) ? -1 : entry;
 #pragma unroll
             for (int e = 0; e < G::RUNS; ++e) {
                 const int row = (e * 1024 + 16 * lane) / G::RB, ch = v_chunk<D>(row, (e * 1024 + 16 * lane) % G::RB / 16);
@@ -802,75 +927,118 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
     }
 }
 
-// Joins the parts of the items that start in block x and end in a later one.  A block takes a row at a time; its
-// wavefronts take every fourth part, eight of them in flight, and their sums are added in order.
-template <class T, int D, bool PAGED, int BM>
+// Joins the parts of the items that start in block (narrow) or slot (wide) x: a wavefront takes RPW rows at once, and
+// 16 accumulator reads are in flight (the time is that of a few dependent reads).  The parts are added in order.
+template <class T, class G, bool PAGED>
 __global__ __launch_bounds__(kThreads) void merge_kernel(Args<PAGED> a, int blocks) {
-    constexpr int E = D / kWave, U = 8;
-    __shared__ float so[kWaves][D], sl[kWaves];
+    constexpr int D = G::CPR * 8, BM = G::BM, E = D / kWave;
+    constexpr bool kThin = BM < 128;
+    constexpr int RPW = kThin ? 1 : 4, U = 16 / RPW;
     const int x = blockIdx.x;
-    const int4 it = a.rec[2 * x + 1];
+    const int4 it = a.rec[kThin ? 2 * x + 1 : 2 * x];
     if (it.x == 0) return;
     const int b = it.x - 1, head = it.y, j = it.z;
     const Seq s = seq_of<PAGED>(a, b);
     const int rows = min(s.rows - j * BM, BM);
-    if (static_cast<int>(blockIdx.y) >= rows) return;
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
-    // the parts: slot 1 of block x, then slot 0 of the blocks after it up to the one that holds the item's end
-    int n = 2;
-    for (int from = x + 1;; from += kWave) {
-        const int at = from + lane;
-        const uint64_t ends = __ballot(at >= blocks - 1 || a.rec[2 * at].w != 0);
-        if (ends) {
-            n = from + __builtin_ctzll(ends) - x + 1;
-            break;
+    const int step = static_cast<int>(gridDim.y) * kWaves * RPW;
+    int r0 = (static_cast<int>(blockIdx.y) * kWaves + w) * RPW;
+    if (r0 >= rows) return;
+    int n = it.w;
+    if constexpr (kThin) {
+        // slot 1 of block x, then slot 0 of the blocks after it up to the one that holds the item's end
+        for (int from = x + 1;; from += kWave) {
+            const int at = from + lane;
+            const uint64_t ends = __ballot(at >= blocks - 1 || a.rec[2 * at].w != 0);
+            if (ends) {
+                n = from + __builtin_ctzll(ends) - x + 1;
+                break;
+            }
         }
     }
-    auto part = [&](int i) { return a.part + (2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
-    for (int r = blockIdx.y; r < rows; r += static_cast<int>(gridDim.y)) {
-        float m = -__builtin_inff();
-        for (int i = lane; i < n; i += kWave) m = fmaxf(m, part(i)[BM * D + r]);
-        for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
-        const float ref = m == -__builtin_inff() ? 0.0f : m;
-        float l = 0.0f, o[E];
+    // The slot of part c + lane; parts past the last take its slot (they are not added).  Wide: the parts of a row tile
+    // lie the chunk's row tiles apart.
+    const int chunk = kThin ? 0 : a.rec[2 * x + 1].x;
+    auto slot_of = [&](int c, int &carry) {
+        if constexpr (kThin) {
+            const int i = min(c + lane, n - 1);
+            return 2 * (x + i) + (i == 0 ? 1 : 0);
+        } else {
+            typedef Deal<PAGED, BM, G::BN> D_;
+            const int i = min(c + lane, n - 1);
+            const int32_t here = c + lane < n - 1 ? D_::reach(a, D_::load(a, s), i, chunk) : 0;
+            const int32_t incl = wave_incl_scan(here);
+            const int at = x + carry + incl - here;
+            carry += __shfl(incl, kWave - 1, kWave);
+            return at;
+        }
+    };
+    auto state = [&](int slot) { return a.part + static_cast<int64_t>(slot) * slot_floats<BM, D>(); };
+    for (; r0 < rows; r0 += step) {
+        float m[RPW], l[RPW], o[RPW][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.0f;
-        for (int i0 = w; i0 < n; i0 += kWaves * U) {
-            float f[U], pl[U], po[U][E];
+        for (int k = 0; k < RPW; ++k) {
+            m[k] = -__builtin_inff();
+            l[k] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < U; ++i) {  // parts past the last read it again, with weight 0
-                const int k = i0 + i * kWaves;
-                const float *p = part(k < n ? k : n - 1);
-                f[i] = k < n ? __builtin_amdgcn_exp2f(p[BM * D + r] - ref) : 0.0f;
-                pl[i] = k < n ? p[BM * (D + 1) + r] : 0.0f;
+            for (int e = 0; e < E; ++e) o[k][e] = 0.0f;
+        }
+        int carry = 0;
+        for (int c = 0; c < n; c += kWave) {
+            const float *p = state(slot_of(c, carry)) + BM * D;
 #pragma unroll
-                for (int e = 0; e < E; ++e) po[i][e] = k < n ? p[r * D + lane * E + e] : 0.0f;
+            for (int k = 0; k < RPW; ++k) m[k] = fmaxf(m[k], p[min(r0 + k, rows - 1)]);
+        }
+#pragma unroll
+        for (int k = 0; k < RPW; ++k) {
+            for (int d = 1; d < kWave; d <<= 1) m[k] = fmaxf(m[k], shfl_xor_f(m[k], d));
+            m[k] = m[k] == -__builtin_inff() ? 0.0f : m[k];
+        }
+        carry = 0;
+        for (int c = 0; c < n; c += kWave) {
+            const int slot = slot_of(c, carry);
+            float f[RPW];
+#pragma unroll
+            for (int k = 0; k < RPW; ++k) {
+                const float *p = state(slot) + BM * D + min(r0 + k, rows - 1);
+                f[k] = c + lane < n ? __builtin_amdgcn_exp2f(p[0] - m[k]) : 0.0f;
+                l[k] += c + lane < n ? f[k] * p[BM] : 0.0f;
             }
+            const int here = min(n - c, kWave);
+            for (int i0 = 0; i0 < here; i0 += U) {
+                float po[U][RPW][E];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                l += f[i] * pl[i];
+                for (int i = 0; i < U; ++i) {
+                    const float *p = state(__shfl(slot, min(i0 + i, kWave - 1), kWave)) + lane * E;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += f[i] * po[i][e];
+                    for (int k = 0; k < RPW; ++k)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) po[i][k][e] = p[min(r0 + k, rows - 1) * D + e];
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    if (i0 + i >= here) break;
+#pragma unroll
+                    for (int k = 0; k < RPW; ++k) {
+                        const float fi = __shfl(f[k], i0 + i, kWave);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) o[k][e] += fi * po[i][k][e];
+                    }
+                }
             }
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) so[w][lane * E + e] = o[e];
-        if (lane == 0) sl[w] = l;
-        __syncthreads();
-        if (w == 0) {
-            l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int d = lane * E + e;
-                o[e] = ((so[0][d] + so[1][d]) + (so[2][d] + so[3][d])) * inv;
-            }
+        for (int k = 0; k < RPW; ++k) {
+            for (int d = 1; d < kWave; d <<= 1) l[k] += shfl_xor_f(l[k], d);
+            const int r = r0 + k;
+            if (r >= rows) break;
+            const float inv = l[k] == 0.0f ? 0.0f : 1.0f / l[k];
             uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + lane * E;
-            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(yr) = T::pack(o[0], o[1]);
-            else *yr = static_cast<uint16_t>(T::pack(o[0], 0.0f));
-            if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
+            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(yr) = T::pack(o[k][0] * inv, o[k][1] * inv);
+            else *yr = static_cast<uint16_t>(T::pack(o[k][0] * inv, 0.0f));
+            if (a.lse && lane == 0)
+                a.lse[lse_at(a, b, s, head, j * BM + r)] = (m[k] + __log2f(l[k])) * kLn2;
         }
-        __syncthreads();
     }
 }
 
@@ -878,21 +1046,28 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(Args<PAGED> a, int bloc
 
 // How a call is laid out, from what the host knows: sizes and upper bounds of the lengths.
 struct Plan {
-    int64_t blocks;
-    bool split;
+    int64_t blocks;  // of the main kernel and (narrow) of the merge
+    int64_t slots;   // partial states, 0: items are not cut
     size_t part_bytes, rec_bytes;
 };
-template <int BM, int BN, int D>
-Plan plan_for(int64_t items, int64_t longest) {
+// items: at most, and at least (where the rows are packed the host knows bounds only)
+template <class G>
+Plan plan_for(int64_t most, int64_t least, int64_t longest) {
     const int64_t resident = 2 * static_cast<int64_t>(device_cus());
-    const int64_t steps = ceil_div(longest < 1 ? 1 : longest, BN);
-    Plan p{items, false, 0, 0};
-    if (steps > 1 && items < 3 * resident) {
-        p.split = true;
-        p.blocks = items * steps < resident ? items * steps : resident;
-        p.part_bytes = sizeof(float) * 2 * p.blocks * slot_floats<BM, D>();
-        p.rec_bytes = sizeof(int4) * 2 * p.blocks;
+    const int64_t steps = ceil_div(longest < 1 ? 1 : longest, G::BN);
+    Plan p{most, 0, 0, 0};
+    if (G::BM < 128) {
+        // narrow: equal runs for the resident blocks, two slots a block; items of one key tile are dealt whole
+        p.blocks = most * steps < resident ? most * steps : resident;
+        if (steps > 1) p.slots = 2 * p.blocks;
+    } else {
+        if (steps > 1 && least <= resident) p.slots = resident;
+        if (p.blocks < p.slots) p.blocks = p.slots;
+        if (p.blocks > (1 << 20)) p.blocks = 1 << 20;
+        p.blocks = (p.blocks + kXcds - 1) / kXcds * kXcds;
     }
+    p.part_bytes = sizeof(float) * p.slots * slot_floats<G::BM, G::CPR * 8>();
+    p.rec_bytes = sizeof(int4) * 2 * p.slots;
     return p;
 }
 
@@ -912,19 +1087,21 @@ bool cross_thin(const tiga_cross &rel) { return rel.num_dst * (rel.heads / rel.k
 template <class G>
 Plan cross_plan(const tiga_cross &rel) {
     const int64_t rows = rel.num_dst * (rel.heads / rel.kv_heads);
-    return plan_for<G::BM, G::BN, G::CPR * 8>(ceil_div(rows, G::BM) * rel.batch * rel.kv_heads, rel.num_src);
+    const int64_t items = ceil_div(rows, G::BM) * rel.batch * rel.kv_heads;
+    return plan_for<G>(items, items, rel.num_src);
 }
 
 // sequences with new tokens, at most
 int64_t some_sequences(const tiga_cache &c, int64_t num_dst) { return num_dst < c.batch ? num_dst : c.batch; }
 bool paged_thin(const tiga_cache &c, int64_t num_dst, int32_t heads) {
+    if (c.page_size < 8) return true;  // the wide tiles load 8 rows of a page at a time
     return num_dst * (heads / c.kv_heads) <= kThinRows * some_sequences(c, num_dst);
 }
 template <class G>
 Plan paged_plan(const tiga_cache &c, int64_t num_dst, int32_t heads) {
     const int64_t rows = num_dst * (heads / c.kv_heads);
-    return plan_for<G::BM, G::BN, G::CPR * 8>((rows / G::BM + some_sequences(c, num_dst)) * c.kv_heads,
-                                              static_cast<int64_t>(c.table_width) * c.page_size);
+    return plan_for<G>((rows / G::BM + some_sequences(c, num_dst)) * c.kv_heads, rows / G::BM * c.kv_heads,
+                       static_cast<int64_t>(c.table_width) * c.page_size);
 }
 
 size_t plan_ws(const Plan &p) {
@@ -937,21 +1114,22 @@ size_t plan_ws(const Plan &p) {
 template <class T, class G, bool PAGED>
 int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
     constexpr int D = G::CPR * 8;
-    if (p.blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "attention: too many row tiles (%lld)", (long long)p.blocks);
-    if (p.split) {
+    if (p.slots) {
         Carve c(ws);
         a.part = reinterpret_cast<float *>(c.take<char>(p.part_bytes));
         a.rec = reinterpret_cast<int4 *>(c.take<char>(p.rec_bytes));
+        a.slots = static_cast<int>(p.slots);
     }
     prof_before(stream);
     const dim3 grid(static_cast<unsigned>(p.blocks));
-    if constexpr (G::BM == 16) hipLaunchKernelGGL((thin_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
+    if constexpr (G::BM < 128) hipLaunchKernelGGL((thin_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL((wide_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
     prof_after(stream);
     if (int rc = check_launch("attention forward")) return rc;
-    if (!p.split) return TIGA_OK;
-    hipLaunchKernelGGL((merge_kernel<T, D, PAGED, G::BM>), dim3(static_cast<unsigned>(p.blocks), G::BM == 16 ? 8 : 32),
-                       dim3(kThreads), 0, stream, a, static_cast<int>(p.blocks));
+    if (!p.slots) return TIGA_OK;
+    const unsigned joins = static_cast<unsigned>(G::BM < 128 ? p.blocks : p.slots);
+    hipLaunchKernelGGL((merge_kernel<T, G, PAGED>), dim3(joins, 4), dim3(kThreads), 0, stream, a,
+                       static_cast<int>(p.blocks));
     return check_launch("attention merge");
 }
 
