@@ -27,7 +27,6 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kMassCap = 4096.0f;  // largest tile mass of a lane (and so weight) that keeps the reference point
-constexpr int kSchedMfma = 0x008, kSchedDsRead = 0x100;  // instruction classes of the scheduler's groups
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -241,6 +240,7 @@ struct Deal {
         int32_t tiles;    // row tiles of a head
         int32_t n0, n1;   // key tiles of the first and the last of them, at least 1
     };
+    static constexpr int32_t kWhole = 0x7fffffff;
     int64_t pieces;
     int32_t chunk;
 
@@ -296,13 +296,13 @@ struct Deal {
     // and read again, are worth.
     __device__ __forceinline__ void begin(const Args<PAGED> &a) {
         const Load first = load(a, lane_id());
-        chunk = 0x7fffffff;
+        chunk = kWhole;
         pieces = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles); });
         if (!a.part || pieces > a.slots) return;
         const int64_t work = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles) * ((l.n0 + l.n1 + 1) / 2); });
         int64_t c = max(int64_t(4), (work + a.slots - 1) / a.slots);
         do {
-            chunk = static_cast<int32_t>(min(c, int64_t(0x7fffffff)));
+            chunk = static_cast<int32_t>(min(c, static_cast<int64_t>(kWhole)));
             pieces = total(a, first, [&](const Load &l) { return count(a, l, chunk); });
             c += max(int64_t(1), c / 16);
         } while (pieces > a.slots);
@@ -346,6 +346,13 @@ struct Deal {
         int64_t rest = p - base - r.head * per;
         r.part = 0;
         for (int32_t here; rest >= (here = reach(a, l, r.part, chunk)); ++r.part) rest -= here;
+        if (PAGED && chunk == kWhole) {
+            // whole causal items differ in their keys: every eighth row tile, then those before them, so that the
+            // eighths of the pieces that the XCDs take weigh alike
+            int32_t k = 0;
+            for (; k < 7 && rest >= (l.tiles - k + 7) / 8; ++k) rest -= (l.tiles - k + 7) / 8;
+            rest = k + 8 * rest;
+        }
         r.j = l.tiles - 1 - static_cast<int32_t>(rest);
         const int32_t n = (keys_of<PAGED>(a, s, min((r.j + 1) * BM, s.rows) - 1) + BN - 1) / BN;
         r.parts = parts(max(1, n), chunk);
@@ -460,24 +467,27 @@ __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<
                                           const int32_t *seen, int32_t k0, int g) {
     using G = Geo<D>;
     f4 s[G::KB][2];
+    // S^T = K Q^T.  The operand reads run kAhead ahead of their products, in this order: the compiler, left to itself,
+    // puts a read next to its use and waits for it.
+    {
+        constexpr int kReads = G::CH * G::KB, kAhead = 4;
+        auto read = [&](int i) {
+            return *reinterpret_cast<const u4 *>(kt + (kr ^ (64 * (i / G::KB))) + i % G::KB * 16 * G::RB);
+        };
+        u4 ka[kAhead];
 #pragma unroll
-    for (int ch = 0; ch < G::CH; ++ch)
+        for (int i = 0; i < kAhead; ++i) ka[i] = read(i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 0; kb < G::KB; ++kb) {
-            const u4 ka = *reinterpret_cast<const u4 *>(kt + (kr ^ (64 * ch)) + kb * 16 * G::RB);
+        for (int i = 0; i < kReads; ++i) {
+            const int ch = i / G::KB, kb = i % G::KB;
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb)
-                s[kb][qb] = T::mma(ka, q[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[kb][qb]);
+                s[kb][qb] = T::mma(ka[i % kAhead], q[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[kb][qb]);
+            if (i + kAhead < kReads) ka[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    // the operand reads run 4 ahead of their products
-    constexpr int kReads = G::CH * G::KB;
-    __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
-#pragma unroll
-    for (int i = 0; i < kReads - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 8, 0);
     if (edge) {
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
@@ -519,25 +529,27 @@ __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<
     st.l[0] += sum[0];
     st.l[1] += sum[1];
     __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-    for (int db = 0; db < G::DB; ++db)
-#pragma unroll
-        for (int kc = 0; kc < G::KC; ++kc) {
-            const uint8_t *const p = vt + (vr ^ (32 * db)) + kc * 32 * G::RB;
+    // O^T += V^T P^T, likewise: an operand is two transposing reads
+    {
+        constexpr int kReads = G::DB * G::KC, kAhead = 3;
+        auto read = [&](int i) {
+            const uint8_t *const p = vt + (vr ^ (32 * (i / G::KC))) + i % G::KC * 32 * G::RB;
             const u2 lo = lds_transposed16(p), hi = lds_transposed16(p + 16 * G::RB);
-            const u4 va{lo.x, lo.y, hi.x, hi.y};
+            return u4{lo.x, lo.y, hi.x, hi.y};
+        };
+        u4 va[kAhead];
 #pragma unroll
-            for (int qb = 0; qb < 2; ++qb) st.o[db][qb] = T::mma(va, pb[kc][qb], st.o[db][qb]);
+        for (int i = 0; i < kAhead; ++i) va[i] = read(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            const int db = i / G::KC, kc = i % G::KC;
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) st.o[db][qb] = T::mma(va[i % kAhead], pb[kc][qb], st.o[db][qb]);
+            if (i + kAhead < kReads) va[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    // the operand reads (two a product pair) run 3 pairs ahead
-    constexpr int kPairs = G::DB * G::KC;
-    __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 6, 0);
-#pragma unroll
-    for (int i = 0; i < kPairs - 3; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 2, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 6, 0);
 }
 
 // Partial state of a slot: o [rows of the tile][D], then m, then l [rows].
@@ -927,109 +939,140 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
     }
 }
 
-// Joins the parts of the items that start in block (narrow) or slot (wide) x: a wavefront takes RPW rows at once, and
-// 16 accumulator reads are in flight (the time is that of a few dependent reads).  The parts are added in order.
-template <class T, class G, bool PAGED>
-__global__ __launch_bounds__(kThreads) void merge_kernel(Args<PAGED> a, int blocks) {
-    constexpr int D = G::CPR * 8, BM = G::BM, E = D / kWave;
-    constexpr bool kThin = BM < 128;
-    constexpr int RPW = kThin ? 1 : 4, U = 16 / RPW;
+// Joins the parts of the narrow item that starts in block x and ends in a later one (slot 1 of x, then slot 0 of the blocks
+// after it up to the one that holds the end): a block a row.  The time is that of a few dependent reads of lines that
+// other XCDs wrote, so 16 bytes a lane of U parts a lane are in flight in every wavefront; the sums are added
+// in a fixed order.
+template <class T, int D, bool PAGED>
+__global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<PAGED> a, int blocks) {
+    constexpr int BM = Thin<D>::BM, L = D / 4, PP = kWave / L, U = 8;  // L lanes a part, PP parts a wavefront's read
+    __shared__ f4 so[kWaves][kWave];
     const int x = blockIdx.x;
-    const int4 it = a.rec[kThin ? 2 * x + 1 : 2 * x];
+    const int4 it = a.rec[2 * x + 1];
     if (it.x == 0) return;
-    const int b = it.x - 1, head = it.y, j = it.z;
+    const int b = it.x - 1, head = it.y, j = it.z, r = blockIdx.y;
     const Seq s = seq_of<PAGED>(a, b);
+    if (r >= s.rows - j * BM) return;
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    int n = 2;
+    for (int from = x + 1;; from += kWave) {
+        const int at = from + lane;
+        const uint64_t ends = __ballot(at >= blocks - 1 || a.rec[2 * at].w != 0);
+        if (ends) {
+            n = from + __builtin_ctzll(ends) - x + 1;
+            break;
+        }
+    }
+    auto state = [&](int i) { return a.part + static_cast<int64_t>(2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
+    float m = -__builtin_inff(), l = 0.0f;
+    for (int i = lane; i < n; i += kWave) m = fmaxf(m, state(i)[BM * D + r]);
+    for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
+    const float ref = m == -__builtin_inff() ? 0.0f : m;
+    f4 o{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = w * PP + lane / L; i0 - lane / L < n; i0 += U * kWaves * PP) {
+        f4 po[U];
+        float pm[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+            const float *p = state(min(i0 + i * kWaves * PP, n - 1));
+            po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
+            pm[i] = p[BM * D + r];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (i0 + i * kWaves * PP < n) o += po[i] * __builtin_amdgcn_exp2f(pm[i] - ref);
+    }
+    so[w][lane] = o;
+    for (int i = lane; i < n; i += kWave) l += __builtin_amdgcn_exp2f(state(i)[BM * D + r] - ref) * state(i)[BM * (D + 1) + r];
+    for (int d = 1; d < kWave; d <<= 1) l += shfl_xor_f(l, d);
+    __syncthreads();
+    if (w != 0 || lane >= L) return;
+    o = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+#pragma unroll
+        for (int k = 0; k < PP; ++k) o += so[i][k * L + lane];
+    o *= l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + 4 * lane;
+    *reinterpret_cast<u2 *>(yr) = u2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+    if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
+}
+
+// Joins the parts of the wide item whose first part is in slot x: a wavefront takes 4 rows at once, 16 reads in
+// flight; the parts (few) are added in order.
+template <class T, class G, bool PAGED>
+__global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<PAGED> a) {
+    constexpr int D = G::CPR * 8, BM = G::BM, E = D / kWave, RPW = 4, U = 4;
+    typedef Deal<PAGED, BM, G::BN> Pieces;
+    const int x = blockIdx.x;
+    const int4 it = a.rec[2 * x];
+    if (it.x == 0) return;
+    const int chunk = a.rec[2 * x + 1].x;
+    const int b = it.x - 1, head = it.y, j = it.z, n = it.w;
+    const Seq s = seq_of<PAGED>(a, b);
+    const typename Pieces::Load load = Pieces::load(a, s);
     const int rows = min(s.rows - j * BM, BM);
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int step = static_cast<int>(gridDim.y) * kWaves * RPW;
-    int r0 = (static_cast<int>(blockIdx.y) * kWaves + w) * RPW;
-    if (r0 >= rows) return;
-    int n = it.w;
-    if constexpr (kThin) {
-        // slot 1 of block x, then slot 0 of the blocks after it up to the one that holds the item's end
-        for (int from = x + 1;; from += kWave) {
-            const int at = from + lane;
-            const uint64_t ends = __ballot(at >= blocks - 1 || a.rec[2 * at].w != 0);
-            if (ends) {
-                n = from + __builtin_ctzll(ends) - x + 1;
-                break;
-            }
-        }
-    }
-    // The slot of part c + lane; parts past the last take its slot (they are not added).  Wide: the parts of a row tile
-    // lie the chunk's row tiles apart.
-    const int chunk = kThin ? 0 : a.rec[2 * x + 1].x;
-    auto slot_of = [&](int c, int &carry) {
-        if constexpr (kThin) {
-            const int i = min(c + lane, n - 1);
-            return 2 * (x + i) + (i == 0 ? 1 : 0);
-        } else {
-            typedef Deal<PAGED, BM, G::BN> D_;
-            const int i = min(c + lane, n - 1);
-            const int32_t here = c + lane < n - 1 ? D_::reach(a, D_::load(a, s), i, chunk) : 0;
-            const int32_t incl = wave_incl_scan(here);
-            const int at = x + carry + incl - here;
-            carry += __shfl(incl, kWave - 1, kWave);
-            return at;
-        }
-    };
-    auto state = [&](int slot) { return a.part + static_cast<int64_t>(slot) * slot_floats<BM, D>(); };
-    for (; r0 < rows; r0 += step) {
+    // the parts of a row tile lie the chunk's row tiles apart
+    auto state = [&](int64_t slot) { return a.part + slot * slot_floats<BM, D>(); };
+    for (int r0 = (static_cast<int>(blockIdx.y) * kWaves + w) * RPW; r0 < rows; r0 += step) {
+        int row[RPW];
         float m[RPW], l[RPW], o[RPW][E];
 #pragma unroll
         for (int k = 0; k < RPW; ++k) {
+            row[k] = min(r0 + k, rows - 1);
             m[k] = -__builtin_inff();
             l[k] = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[k][e] = 0.0f;
         }
-        int carry = 0;
+        // each lane finds the slots of its parts alike
+        int64_t slot = x;
         for (int c = 0; c < n; c += kWave) {
-            const float *p = state(slot_of(c, carry)) + BM * D;
+            int64_t mine = x;
+            for (int i = 0; i < kWave && c + i < n; ++i) {
+                if (i == lane) mine = slot;
+                slot += Pieces::reach(a, load, c + i, chunk);
+            }
+            if (c + lane < n)
 #pragma unroll
-            for (int k = 0; k < RPW; ++k) m[k] = fmaxf(m[k], p[min(r0 + k, rows - 1)]);
+                for (int k = 0; k < RPW; ++k) m[k] = fmaxf(m[k], state(mine)[BM * D + row[k]]);
         }
 #pragma unroll
         for (int k = 0; k < RPW; ++k) {
             for (int d = 1; d < kWave; d <<= 1) m[k] = fmaxf(m[k], shfl_xor_f(m[k], d));
             m[k] = m[k] == -__builtin_inff() ? 0.0f : m[k];
         }
-        carry = 0;
-        for (int c = 0; c < n; c += kWave) {
-            const int slot = slot_of(c, carry);
-            float f[RPW];
+        slot = x;
+        for (int c = 0; c < n; c += U) {
+            float po[U][RPW][E], pm[U][RPW], pl[U][RPW];
 #pragma unroll
-            for (int k = 0; k < RPW; ++k) {
-                const float *p = state(slot) + BM * D + min(r0 + k, rows - 1);
-                f[k] = c + lane < n ? __builtin_amdgcn_exp2f(p[0] - m[k]) : 0.0f;
-                l[k] += c + lane < n ? f[k] * p[BM] : 0.0f;
-            }
-            const int here = min(n - c, kWave);
-            for (int i0 = 0; i0 < here; i0 += U) {
-                float po[U][RPW][E];
+            for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+                const float *p = state(slot);
+                if (c + i < n - 1) slot += Pieces::reach(a, load, c + i, chunk);
 #pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const float *p = state(__shfl(slot, min(i0 + i, kWave - 1), kWave)) + lane * E;
+                for (int k = 0; k < RPW; ++k) {
+                    pm[i][k] = p[BM * D + row[k]];
+                    pl[i][k] = p[BM * (D + 1) + row[k]];
 #pragma unroll
-                    for (int k = 0; k < RPW; ++k)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) po[i][k][e] = p[min(r0 + k, rows - 1) * D + e];
+                    for (int e = 0; e < E; ++e) po[i][k][e] = p[row[k] * D + lane * E + e];
                 }
+            }
 #pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    if (i0 + i >= here) break;
+            for (int i = 0; i < U; ++i) {
+                if (c + i >= n) break;
 #pragma unroll
-                    for (int k = 0; k < RPW; ++k) {
-                        const float fi = __shfl(f[k], i0 + i, kWave);
+                for (int k = 0; k < RPW; ++k) {
+                    const float f = __builtin_amdgcn_exp2f(pm[i][k] - m[k]);
+                    l[k] += f * pl[i][k];
 #pragma unroll
-                        for (int e = 0; e < E; ++e) o[k][e] += fi * po[i][k][e];
-                    }
+                    for (int e = 0; e < E; ++e) o[k][e] += f * po[i][k][e];
                 }
             }
         }
 #pragma unroll
         for (int k = 0; k < RPW; ++k) {
-            for (int d = 1; d < kWave; d <<= 1) l[k] += shfl_xor_f(l[k], d);
             const int r = r0 + k;
             if (r >= rows) break;
             const float inv = l[k] == 0.0f ? 0.0f : 1.0f / l[k];
@@ -1127,9 +1170,12 @@ int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
     prof_after(stream);
     if (int rc = check_launch("attention forward")) return rc;
     if (!p.slots) return TIGA_OK;
-    const unsigned joins = static_cast<unsigned>(G::BM < 128 ? p.blocks : p.slots);
-    hipLaunchKernelGGL((merge_kernel<T, G, PAGED>), dim3(joins, 4), dim3(kThreads), 0, stream, a,
-                       static_cast<int>(p.blocks));
+    if constexpr (G::BM < 128)
+        hipLaunchKernelGGL((thin_merge_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks), G::BM), dim3(kThreads), 0,
+                           stream, a, static_cast<int>(p.blocks));
+    else
+        hipLaunchKernelGGL((wide_merge_kernel<T, G, PAGED>), dim3(static_cast<unsigned>(p.slots), 4), dim3(kThreads), 0,
+                           stream, a);
     return check_launch("attention merge");
 }
 
