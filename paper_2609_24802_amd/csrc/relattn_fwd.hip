@@ -231,8 +231,13 @@ struct Walk {
     }
 };
 
-// Wide tiles: pieces in the order (sequence, source head, chunk of keys, row tile), chunks of `chunk` key tiles.  The row
-// tiles that reach into a chunk are the last ones of a causal sequence, all of a strided one, and they come last first.
+// Wide tiles: what a block works on.
+//  - Items cut into chunks of `chunk` key tiles: pieces in the order (sequence, source head, chunk of keys, row tile), and
+//    an XCD takes an eighth of them that lies together.  The row tiles that reach into a chunk are the last ones of a
+//    causal sequence, all of a strided one, and they come last first.
+//  - Whole items: (sequence, eight heads, row tile, head), dealt to the XCDs in turn, so that an XCD's L2 holds one head of
+//    the eight, the XCDs get alike shares of unequal sequences, and a causal sequence's longest items start first
+//    (blocks start in order: a long one late in the order would end late).
 template <bool PAGED, int BM, int BN>
 struct Deal {
     struct Load {
@@ -342,18 +347,21 @@ struct Deal {
         const int64_t per = count(a, l, chunk);
         Piece r;
         r.b = b;
-        r.head = static_cast<int32_t>((p - base) / per);
-        int64_t rest = p - base - r.head * per;
         r.part = 0;
-        for (int32_t here; rest >= (here = reach(a, l, r.part, chunk)); ++r.part) rest -= here;
-        if (PAGED && chunk == kWhole) {
-            // whole causal items differ in their keys: every eighth row tile, then those before them, so that the
-            // eighths of the pieces that the XCDs take weigh alike
-            int32_t k = 0;
-            for (; k < 7 && rest >= (l.tiles - k + 7) / 8; ++k) rest -= (l.tiles - k + 7) / 8;
-            rest = k + 8 * rest;
+        int64_t rest = p - base;
+        if (chunk == kWhole) {
+            const int32_t heads = a.kv_heads % static_cast<int>(kXcds) == 0 ? static_cast<int>(kXcds) : a.kv_heads;
+            const int64_t band = static_cast<int64_t>(l.tiles) * heads;
+            const int32_t at = static_cast<int32_t>(rest / band);
+            rest -= at * band;
+            r.j = l.tiles - 1 - static_cast<int32_t>(rest / heads);
+            r.head = at * heads + static_cast<int32_t>(rest % heads);
+        } else {
+            r.head = static_cast<int32_t>(rest / per);
+            rest -= r.head * per;
+            for (int32_t here; rest >= (here = reach(a, l, r.part, chunk)); ++r.part) rest -= here;
+            r.j = l.tiles - 1 - static_cast<int32_t>(rest);
         }
-        r.j = l.tiles - 1 - static_cast<int32_t>(rest);
         const int32_t n = (keys_of<PAGED>(a, s, min((r.j + 1) * BM, s.rows) - 1) + BN - 1) / BN;
         r.parts = parts(max(1, n), chunk);
         r.t0 = static_cast<int32_t>(min(static_cast<int64_t>(r.part) * chunk, static_cast<int64_t>(n)));
@@ -577,14 +585,16 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
-    // the blocks of one XCD (every eighth) take neighbouring pieces
     Deal<PAGED, G::BM, G::BN> deal;
     deal.begin(a);
-    const int x = blockIdx.x % kXcds;
-    const int64_t per = deal.pieces / kXcds, rem = deal.pieces % kXcds;
     if (a.part && threadIdx.x == 0 && deal.pieces + blockIdx.x < a.slots) a.rec[2 * (deal.pieces + blockIdx.x)] = int4{0, 0, 0, 0};
-    for (int64_t i = blockIdx.x / kXcds; i < per + (x < rem ? 1 : 0); i += gridDim.x / kXcds) {
-        const int64_t id = x * per + min(static_cast<int64_t>(x), rem) + i;
+    // block b of the grid (a multiple of 8) runs on XCD b % 8
+    const bool whole_items = deal.chunk == deal.kWhole;
+    const int x = blockIdx.x % kXcds;
+    const int64_t per = deal.pieces / kXcds + (x < deal.pieces % kXcds ? 1 : 0);  // pieces of this XCD
+    const int64_t first = whole_items ? x : x * (deal.pieces / kXcds) + min(static_cast<int64_t>(x), deal.pieces % kXcds);
+    for (int64_t i = blockIdx.x / kXcds; i < per; i += gridDim.x / kXcds) {
+        const int64_t id = first + (whole_items ? i * kXcds : i);
         Seq s;
         const typename Deal<PAGED, G::BM, G::BN>::Piece pc = deal.piece(a, id, s);
         if (a.part && threadIdx.x == 0 && id < a.slots) {
