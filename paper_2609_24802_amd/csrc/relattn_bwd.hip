@@ -1,5 +1,24 @@
-// Vector-Jacobian product of cross attention: dq over a destination's sources, dk and dv over a source's
-// destinations (of every head that shares it).  One wavefront a row; the lanes hold the width.
+// Vector-Jacobian product of cross attention.  With p_ij = exp(s_ij - lse_i), delta_i = <dy_i, y_i> and
+// ds_ij = p_ij (<dy_i, v_j> - delta_i):
+//   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij dy_i,
+// i over the destinations of every head that shares source head j's.  Scores and weights are formed again from q, k and
+// lse; nothing of the size of the relation is stored.
+//
+// Three launches: the rows' statistics (lse in the log2 domain, delta), then dq with the rows owned and the keys
+// streamed, and dk, dv with the keys owned and the rows streamed.  The second and third are one kernel: a wavefront owns
+// 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or q) and Y2 (v
+// or dy) through LDS.  Per 32 streamed rows
+//   S = Y1 X1^T, DP = Y2 X2^T   (streamed x owned, 16x16x32 MFMA, fp32)
+//   P = 2^(c S - lse2), DS = P (DP - delta), rounded to the input type as the operands of the next products
+//   acc1 += Y1^T DS (dq or dk),  acc2 += Y2^T P (dv)
+// where the accumulator layout of S is the operand layout of P (each lane's rows of two 16-row blocks fill its 8 slots of
+// a 32-deep product, and the transposing LDS reads of Y^T take the rows in that order).  dk and dv need S and DP once
+// more than a fused pass would, 14 instead of 10 operations a pair and width; the fused pass would have to add dq over
+// blocks of keys, by atomics (an order that varies) or through fp32 partial sums of S / 128 times dq's size.
+//
+// Every sum has a fixed order.  Where the owned tiles do not fill the device, the streamed axis is split, and the parts'
+// fp32 sums go to the workspace and are added by reduce_kernel.
+#include "mfma16.hpp"
 #include "relation.hpp"
 #include "relattn.hpp"
 
@@ -8,130 +27,494 @@ namespace relattn {
 
 namespace {
 
-constexpr int kRows = 4;
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kOwn = 128;  // owned rows or keys of a block: 32 a wavefront
 constexpr float kLog2e = 1.4426950408889634f;
 
-struct F16 {
-    static __device__ __forceinline__ float get(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
-    static __device__ __forceinline__ uint16_t put(float f) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(f)); }
+// n / d for n < 2^31 by a multiplication (round-up method; M holds the low 32 bits of a 33-bit factor).
+struct Divider {
+    uint32_t m, s, d;
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(m, n) + n) >> s; }
 };
-struct BF16 {
-    static __device__ __forceinline__ float get(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
-    static __device__ __forceinline__ uint16_t put(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
-};
-
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int d = 1; d < kWave; d <<= 1) v += shfl_xor_f(v, d);
-    return v;
+Divider divider(uint32_t d) {
+    uint32_t s = 0;
+    while ((uint64_t(1) << s) < d) ++s;
+    return Divider{static_cast<uint32_t>(((uint64_t(1) << 32) * ((uint64_t(1) << s) - d)) / d + 1), s, d};
 }
 
 struct Args {
     Rows q, k, v, y, dy, dq, dk, dv;
     const float *lse;
     const int32_t *len;
-    int64_t num_dst, num_src;
-    int batch, heads, group;
+    float *lse2, *delta;  // [batch * heads * num_dst + 1]: the last is what rows past the end have (no weight)
+    float *part;          // split sums
+    int32_t num_dst, num_src, batch, heads, kv_heads;
+    Divider group;
+    int64_t stats;        // batch * heads * num_dst
+    int32_t rows;         // num_dst * group
+    int32_t splits;
     float scale;
 };
 
-template <class T, int D>
-__device__ __forceinline__ void load(float *r, const uint16_t *p) {
-    for (int e = 0; e < D / 64; ++e) r[e] = T::get(p[e * 64 + lane_id()]);
-}
-template <class T, int D>
-__device__ __forceinline__ void store(const uint16_t *p, const float *r) {
-    for (int e = 0; e < D / 64; ++e) const_cast<uint16_t *>(p)[e * 64 + lane_id()] = T::put(r[e]);
-}
-template <int D>
-__device__ __forceinline__ float dot(const float *a, const float *b) {
-    float s = 0.0f;
-    for (int e = 0; e < D / 64; ++e) s += a[e] * b[e];
-    return wave_sum(s);
-}
-__device__ __forceinline__ int64_t sources(const Args &a, int b) {
+__device__ __forceinline__ int32_t sources(const Args &a, int b) {
     if (!a.len) return a.num_src;
-    return a.len[b] < 0 ? 0 : (a.len[b] > a.num_src ? a.num_src : a.len[b]);
+    const int32_t n = a.len[b];
+    return n < 0 ? 0 : (n > a.num_src ? a.num_src : n);
+}
+// Row r of a source head is token r / group of head r % group of its group.
+__device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int b, int kv, int32_t r) {
+    const int32_t token = static_cast<int32_t>(a.group.div(r)), g = r - token * static_cast<int32_t>(a.group.d);
+    return b * t.batch + static_cast<int64_t>(kv * static_cast<int32_t>(a.group.d) + g) * t.head + token * t.row;
+}
+__device__ __forceinline__ int64_t stat_at(const Args &a, int b, int kv, int32_t r) {
+    const int32_t token = static_cast<int32_t>(a.group.div(r)), g = r - token * static_cast<int32_t>(a.group.d);
+    return (static_cast<int64_t>(b) * a.heads + kv * static_cast<int32_t>(a.group.d) + g) * a.num_dst + token;
 }
 
+// ------------------------------------------------------------------------------------------ statistics
+
+// D / 8 lanes a row, 16 bytes each.
 template <class T, int D>
-__global__ __launch_bounds__(kRows * kWave) void dq_kernel(Args a) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kWave;
-    if (r >= static_cast<int64_t>(a.batch) * a.heads * a.num_dst) return;
-    const int64_t i = r % a.num_dst;
-    const int h = static_cast<int>(r / a.num_dst % a.heads), b = static_cast<int>(r / a.num_dst / a.heads);
-    const int64_t n = sources(a, b);
-    float q[2], y[2], dy[2], k[2], v[2], o[2] = {0.0f, 0.0f};
-    load<T, D>(q, a.q.p + b * a.q.batch + h * a.q.head + i * a.q.row);
-    load<T, D>(y, a.y.p + b * a.y.batch + h * a.y.head + i * a.y.row);
-    load<T, D>(dy, a.dy.p + b * a.dy.batch + h * a.dy.head + i * a.dy.row);
-    const float delta = dot<D>(y, dy), lse = a.lse[r];
-    for (int64_t j = 0; j < n; ++j) {
-        load<T, D>(k, a.k.p + b * a.k.batch + h / a.group * a.k.head + j * a.k.row);
-        load<T, D>(v, a.v.p + b * a.v.batch + h / a.group * a.v.head + j * a.v.row);
-        const float p = __builtin_amdgcn_exp2f((dot<D>(q, k) * a.scale - lse) * kLog2e);
-        const float ds = p * (dot<D>(dy, v) - delta) * a.scale;
-        for (int e = 0; e < D / 64; ++e) o[e] += ds * k[e];
+__global__ __launch_bounds__(kThreads) void stats_kernel(Args a) {
+    constexpr int L = D / 8;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t r = t / L;
+    const int part = static_cast<int>(t % L);
+    if (t == 0) {
+        a.lse2[a.stats] = __builtin_inff();
+        a.delta[a.stats] = 0.0f;
     }
-    store<T, D>(a.dq.p + b * a.dq.batch + h * a.dq.head + i * a.dq.row, o);
+    if (r >= a.stats) return;  // whole rows: the lanes of a row leave together
+    const int64_t i = r % a.num_dst, bh = r / a.num_dst;
+    const int64_t h = bh % a.heads, b = bh / a.heads;
+    const u4 y = *reinterpret_cast<const u4 *>(a.y.p + b * a.y.batch + h * a.y.head + i * a.y.row + 8 * part);
+    const u4 dy = *reinterpret_cast<const u4 *>(a.dy.p + b * a.dy.batch + h * a.dy.head + i * a.dy.row + 8 * part);
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const f2 u = T::unpack(y[e]), v = T::unpack(dy[e]);
+        s += u.x * v.x + u.y * v.y;
+    }
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) s += shfl_xor_f(s, d);
+    if (part == 0) {
+        const float l = a.lse[r];
+        // a row that saw no weight has no gradient
+        a.lse2[r] = l == -__builtin_inff() ? __builtin_inff() : l * kLog2e;
+        a.delta[r] = s;
+    }
 }
 
-template <class T, int D>
-__global__ __launch_bounds__(kRows * kWave) void dkv_kernel(Args a) {
-    const int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kWave;
-    const int kvh = a.heads / a.group;
-    if (r >= static_cast<int64_t>(a.batch) * kvh * a.num_src) return;
-    const int64_t j = r % a.num_src;
-    const int g = static_cast<int>(r / a.num_src % kvh), b = static_cast<int>(r / a.num_src / kvh);
-    float q[2], y[2], dy[2], k[2], v[2], dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    if (j < sources(a, b)) {
-        load<T, D>(k, a.k.p + b * a.k.batch + g * a.k.head + j * a.k.row);
-        load<T, D>(v, a.v.p + b * a.v.batch + g * a.v.head + j * a.v.row);
-        for (int h = g * a.group; h < (g + 1) * a.group; ++h)
-            for (int64_t i = 0; i < a.num_dst; ++i) {
-                load<T, D>(q, a.q.p + b * a.q.batch + h * a.q.head + i * a.q.row);
-                load<T, D>(y, a.y.p + b * a.y.batch + h * a.y.head + i * a.y.row);
-                load<T, D>(dy, a.dy.p + b * a.dy.batch + h * a.dy.head + i * a.dy.row);
-                const float lse = a.lse[(static_cast<int64_t>(b) * a.heads + h) * a.num_dst + i];
-                const float p = __builtin_amdgcn_exp2f((dot<D>(q, k) * a.scale - lse) * kLog2e);
-                const float ds = p * (dot<D>(dy, v) - dot<D>(y, dy)) * a.scale;
-                for (int e = 0; e < D / 64; ++e) {
-                    dk[e] += ds * q[e];
-                    dv[e] += p * dy[e];
-                }
+// ------------------------------------------------------------------------------------------ products
+
+template <int D>
+struct Geo {
+    static constexpr int CPR = D / 8;                 // 16-byte chunks per row
+    static constexpr int RB = 2 * D;                  // bytes per row
+    static constexpr int R = 256 / RB;                // rows per 256-byte bank window
+    static constexpr int CH = D / 32;                 // 32-deep chunks of S and DP
+    static constexpr int DB = D / 16;                 // 16-wide blocks of the sums
+    static constexpr int BN = D == 64 ? 128 : 64;     // streamed rows a tile
+    static constexpr int KC = BN / 32;                // 32-row chunks of a tile
+    static constexpr int TILE = BN * RB;              // 16 KB
+    static constexpr int LPW = TILE / 1024 / kWaves;  // 1-KB direct loads per wavefront, tile and operand
+};
+
+// LDS layout of a streamed tile: 16-byte chunk c of row k sits at chunk c ^ swizzle(k).  The direct reads take 16 rows at
+// one chunk (16 distinct bank groups, as the swizzle is a permutation of 16 rows' windows), the transposing reads 8 rows
+// at one 32-byte block (distinct too, as the swizzle's upper bits are a permutation of 8 neighbouring rows).
+template <int D>
+__device__ __forceinline__ int swizzle(int k) {
+    constexpr int CPR = Geo<D>::CPR;
+    const int y = (k / Geo<D>::R) % CPR;
+    return ((y & (CPR / 2 - 1)) << 1) | (y / (CPR / 2));
+}
+
+template <class T, int D, bool KEYS>
+struct Sums {
+    f4 a1[Geo<D>::DB][2];
+    f4 a2[KEYS ? Geo<D>::DB : 1][2];
+};
+
+// 32 streamed rows from `y1`, `y2` (their first row's LDS address).  dr / tr: this lane's offsets of the direct and of the
+// transposing reads.  Owned statistics (dq) are own[2] and own_delta[2], streamed ones (dk, dv) lie at st / sd.
+template <class T, int D, bool KEYS>
+__device__ __forceinline__ void chunk_step(Sums<T, D, KEYS> &acc, const u4 (&x1)[2][Geo<D>::CH],
+                                           const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
+                                           int tr, float c, const float *own, const float *own_delta, const float *st,
+                                           const float *sd, bool edge, int left, int g) {
+    using G = Geo<D>;
+    f4 s[2][2], dp[2][2];  // [16-row block][column block]
+    {
+        constexpr int kReads = 4 * G::CH, kAhead = 4;
+        auto read = [&](int i) {
+            const uint8_t *const p = (i / 2) % 2 ? y2 : y1;
+            return *reinterpret_cast<const u4 *>(p + (dr ^ (64 * (i / 4))) + i % 2 * 16 * G::RB);
+        };
+        u4 w[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) w[i] = read(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            const int ch = i / 4, e = i % 2;
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                if ((i / 2) % 2 == 0)
+                    s[e][qb] = T::mma(w[i % kAhead], x1[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[e][qb]);
+                else
+                    dp[e][qb] = T::mma(w[i % kAhead], x2[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : dp[e][qb]);
             }
+            if (i + kAhead < kReads) w[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    if (a.dk.p) store<T, D>(a.dk.p + b * a.dk.batch + g * a.dk.head + j * a.dk.row, dk);
-    if (a.dv.p) store<T, D>(a.dv.p + b * a.dv.batch + g * a.dv.head + j * a.dv.row, dv);
+    u4 pb[2], db[2];
+    f4 lse2[2], delta[2];
+    if constexpr (KEYS) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            lse2[e] = *reinterpret_cast<const f4 *>(st + e * 16 + 4 * g);
+            delta[e] = *reinterpret_cast<const f4 *>(sd + e * 16 + 4 * g);
+        }
+    }
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        float p[2][4], ds[2][4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][qb][i], c, KEYS ? -lse2[e][i] : -own[qb]));
+                if (!KEYS && edge) p[e][i] = e * 16 + 4 * g + i < left ? p[e][i] : 0.0f;
+                ds[e][i] = p[e][i] * (dp[e][qb][i] - (KEYS ? delta[e][i] : own_delta[qb]));
+            }
+        if constexpr (KEYS)
+            pb[qb] = u4{T::pack(p[0][0], p[0][1]), T::pack(p[0][2], p[0][3]), T::pack(p[1][0], p[1][1]),
+                        T::pack(p[1][2], p[1][3])};
+        db[qb] = u4{T::pack(ds[0][0], ds[0][1]), T::pack(ds[0][2], ds[0][3]), T::pack(ds[1][0], ds[1][1]),
+                    T::pack(ds[1][2], ds[1][3])};
+    }
+    {
+        constexpr int M = KEYS ? 2 : 1, kReads = M * G::DB, kAhead = 3;
+        auto read = [&](int i) {
+            const uint8_t *const p = (KEYS && i % 2 ? y2 : y1) + (tr ^ (32 * (i / M)));
+            const u2 lo = lds_transposed16(p), hi = lds_transposed16(p + 16 * G::RB);
+            return u4{lo.x, lo.y, hi.x, hi.y};
+        };
+        u4 w[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) w[i] = read(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            const int d = i / M;
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) {
+                if (KEYS && i % 2) acc.a2[KEYS ? d : 0][qb] = T::mma(w[i % kAhead], pb[qb], acc.a2[KEYS ? d : 0][qb]);
+                else acc.a1[d][qb] = T::mma(w[i % kAhead], db[qb], acc.a1[d][qb]);
+            }
+            if (i + kAhead < kReads) w[i % kAhead] = read(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+// KEYS: a block owns 128 keys of a source head and streams its rows, for dk and dv; otherwise it owns 128 rows and streams
+// the keys, for dq.  A block's pieces: (eight heads, tile, split, head), so that an XCD (every eighth block) keeps to
+// one head of the eight and unequal sequences spread over the XCDs.
+template <class T, int D, bool KEYS>
+__global__ __launch_bounds__(kThreads, KEYS ? 1 : 2) void products_kernel(Args a, int tiles) {
+    using G = Geo<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t y1a[G::TILE], y2a[G::TILE], y1b[G::TILE], y2b[G::TILE];
+    __shared__ __attribute__((aligned(256))) float sta[KEYS ? 2 * G::BN : 2], stb[KEYS ? 2 * G::BN : 2];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, g = lane >> 4;
+
+    const int64_t heads = static_cast<int64_t>(a.batch) * a.kv_heads, per = static_cast<int64_t>(tiles) * a.splits;
+    const int64_t band = blockIdx.x / (kXcds * per);
+    const int64_t in = blockIdx.x - band * kXcds * per;
+    const int width = static_cast<int>(min(heads - band * kXcds, static_cast<int64_t>(kXcds)));
+    const int64_t bh = band * kXcds + in % width;
+    const int ts = static_cast<int>(in / width), tile = ts / a.splits, split = ts % a.splits;
+    const int b = static_cast<int>(bh / a.kv_heads), kv = static_cast<int>(bh % a.kv_heads);
+
+    const int32_t n = sources(a, b);
+    const int32_t own_n = KEYS ? n : a.rows, str_n = KEYS ? a.rows : n;
+    const int32_t own0 = tile * kOwn;
+    if (own0 >= own_n && a.splits > 1) return;  // no part of it is read
+    const int32_t steps = own0 < own_n ? (str_n + G::BN - 1) / G::BN : 0;
+    const int32_t t0 = static_cast<int32_t>(static_cast<int64_t>(steps) * split / a.splits);
+    const int32_t t1 = static_cast<int32_t>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
+
+    // owned operands; columns past the end repeat the last (what they sum is not stored)
+    u4 x1[2][G::CH], x2[2][G::CH];
+    float own[2], own_delta[2];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int32_t o = min(own0 + w * 32 + qb * 16 + col, own_n - 1);
+        own[qb] = own_delta[qb] = 0.0f;
+        if (own_n > 0 && own0 < own_n) {
+            const uint16_t *p1, *p2;
+            if constexpr (KEYS) {
+                p1 = a.k.p + b * a.k.batch + kv * a.k.head + o * a.k.row;
+                p2 = a.v.p + b * a.v.batch + kv * a.v.head + o * a.v.row;
+            } else {
+                p1 = a.q.p + row_at(a, a.q, b, kv, o);
+                p2 = a.dy.p + row_at(a, a.dy, b, kv, o);
+                own[qb] = a.lse2[stat_at(a, b, kv, o)];
+                own_delta[qb] = a.delta[stat_at(a, b, kv, o)];
+            }
+#pragma unroll
+            for (int ch = 0; ch < G::CH; ++ch) {
+                x1[qb][ch] = reinterpret_cast<const u4 *>(p1)[ch * 4 + g];
+                x2[qb][ch] = reinterpret_cast<const u4 *>(p2)[ch * 4 + g];
+            }
+        }
+    }
+    Sums<T, D, KEYS> acc;
+#pragma unroll
+    for (int d = 0; d < G::DB; ++d)
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            acc.a1[d][qb] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (KEYS) acc.a2[KEYS ? d : 0][qb] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+
+    // this lane's places in a tile: rows and chunks of its direct loads, offsets of its operand reads
+    int krow[G::LPW], kch[G::LPW];
+#pragma unroll
+    for (int r = 0; r < G::LPW; ++r) {
+        const int byte = (w * G::LPW + r) * 1024 + 16 * lane;
+        krow[r] = byte / G::RB;
+        kch[r] = byte % G::RB / 16 ^ swizzle<D>(krow[r]);
+    }
+    const int dr = col * G::RB + 16 * (g ^ swizzle<D>(col));
+    const int trow = 4 * g + col / 4;
+    const int tr = trow * G::RB + 16 * ((col % 4 / 2) ^ swizzle<D>(trow)) + 8 * (col % 2);
+
+    const uint16_t *const kb = a.k.p + b * a.k.batch + kv * a.k.head, *const vb = a.v.p + b * a.v.batch + kv * a.v.head;
+    auto stage = [&](int kt, uint8_t *b1, uint8_t *b2, float *stats) {
+        const int32_t k0 = kt * G::BN;
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            const int run = (w * G::LPW + r) * 1024;
+            const int32_t i = min(k0 + krow[r], str_n - 1);  // past the end: the last row again, without weight
+            const uint16_t *p1, *p2;
+            if constexpr (KEYS) {
+                p1 = a.q.p + row_at(a, a.q, b, kv, i);
+                p2 = a.dy.p + row_at(a, a.dy, b, kv, i);
+            } else {
+                p1 = kb + i * a.k.row;
+                p2 = vb + i * a.v.row;
+            }
+            load_to_lds16(p1 + 8 * kch[r], b1 + run);
+            load_to_lds16(p2 + 8 * kch[r], b2 + run);
+        }
+        if constexpr (KEYS) {
+            // 64 lanes, 4 bytes each: the first half of the needed wavefronts takes lse2, the other delta
+            constexpr int kNeed = 2 * G::BN / kWave;
+            if (w < kNeed) {
+                const int32_t i = k0 + w % (kNeed / 2) * kWave + lane;
+                const int64_t at = i < str_n ? stat_at(a, b, kv, i) : a.stats;
+                __builtin_amdgcn_global_load_lds((w < kNeed / 2 ? a.lse2 : a.delta) + at,
+                                                 (__attribute__((address_space(3))) void *)(stats + w * kWave), 4, 0, 0);
+            }
+        }
+    };
+    const float c = a.scale * kLog2e;
+    auto step = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *stats) {
+        const bool edge = !KEYS && (kt + 1) * G::BN > str_n;
+#pragma unroll
+        for (int kc = 0; kc < G::KC; ++kc) {
+            const int off = kc * 32 * G::RB;
+            chunk_step<T, D, KEYS>(acc, x1, x2, b1 + off, b2 + off, dr, tr, c, own, own_delta, stats + (KEYS ? kc * 32 : 0),
+                                   stats + (KEYS ? G::BN + kc * 32 : 0), edge, str_n - kt * G::BN - kc * 32, g);
+        }
+    };
+    if (t0 < t1) stage(t0, y1a, y2a, sta);
+    for (int kt = t0; kt < t1; kt += 2) {
+        loads_arrived();
+        __syncthreads();
+        if (kt + 1 < t1) stage(kt + 1, y1b, y2b, stb);
+        step(kt, y1a, y2a, sta);
+        if (kt + 1 >= t1) break;
+        loads_arrived();
+        __syncthreads();
+        if (kt + 2 < t1) stage(kt + 2, y1a, y2a, sta);
+        step(kt + 1, y1b, y2b, stb);
+    }
+
+    const int32_t total = KEYS ? a.num_src : a.rows;
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int32_t o = own0 + w * 32 + qb * 16 + col;
+        if (o >= total) continue;
+        if (a.splits > 1) {
+            float *const p = a.part + ((bh * tiles + tile) * a.splits + split) * (KEYS ? 2 : 1) * kOwn * D + (o - own0) * D;
+#pragma unroll
+            for (int d = 0; d < G::DB; ++d) {
+                *reinterpret_cast<f4 *>(p + d * 16 + g * 4) = acc.a1[d][qb];
+                if (KEYS) *reinterpret_cast<f4 *>(p + kOwn * D + d * 16 + g * 4) = acc.a2[KEYS ? d : 0][qb];
+            }
+            continue;
+        }
+        const bool seen = o < own_n;  // keys past the sequence's length have gradient 0
+        auto put = [&](uint16_t *p, f4 v) {
+            *reinterpret_cast<u2 *>(p) = seen ? u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])} : u2{0u, 0u};
+        };
+        if constexpr (KEYS) {
+            uint16_t *const pk = const_cast<uint16_t *>(a.dk.p) + b * a.dk.batch + kv * a.dk.head + o * a.dk.row;
+            uint16_t *const pv = const_cast<uint16_t *>(a.dv.p) + b * a.dv.batch + kv * a.dv.head + o * a.dv.row;
+#pragma unroll
+            for (int d = 0; d < G::DB; ++d) {
+                if (a.dk.p) put(pk + d * 16 + g * 4, acc.a1[d][qb] * a.scale);
+                if (a.dv.p) put(pv + d * 16 + g * 4, acc.a2[d][qb]);
+            }
+        } else {
+            uint16_t *const pq = const_cast<uint16_t *>(a.dq.p) + row_at(a, a.dq, b, kv, o);
+#pragma unroll
+            for (int d = 0; d < G::DB; ++d) put(pq + d * 16 + g * 4, acc.a1[d][qb] * a.scale);
+        }
+    }
+}
+
+// Adds the splits' sums in order: 4 widths a thread.
+template <class T, int D, bool KEYS>
+__global__ __launch_bounds__(kThreads) void reduce_kernel(Args a, int tiles) {
+    constexpr int L = D / 4, M = KEYS ? 2 : 1;
+    const int32_t total = KEYS ? a.num_src : a.rows;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t item = t / L;
+    const int d = static_cast<int>(t % L) * 4;
+    const int64_t bh = item / total;
+    if (bh >= static_cast<int64_t>(a.batch) * a.kv_heads) return;
+    const int32_t o = static_cast<int32_t>(item - bh * total);
+    const int b = static_cast<int>(bh / a.kv_heads), kv = static_cast<int>(bh % a.kv_heads);
+    const float *const p = a.part + ((bh * tiles + o / kOwn) * a.splits) * M * kOwn * D + o % kOwn * D + d;
+    f4 s1{0.0f, 0.0f, 0.0f, 0.0f}, s2 = s1;
+    if (!KEYS || o < sources(a, b)) {
+#pragma unroll 8
+        for (int i = 0; i < a.splits; ++i) {
+            s1 += *reinterpret_cast<const f4 *>(p + static_cast<int64_t>(i) * M * kOwn * D);
+            if (KEYS) s2 += *reinterpret_cast<const f4 *>(p + (static_cast<int64_t>(i) * M + 1) * kOwn * D);
+        }
+    }
+    auto put = [&](const uint16_t *at, f4 v) {
+        *reinterpret_cast<u2 *>(const_cast<uint16_t *>(at) + d) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+    };
+    s1 *= a.scale;
+    if constexpr (KEYS) {
+        if (a.dk.p) put(a.dk.p + b * a.dk.batch + kv * a.dk.head + o * a.dk.row, s1);
+        if (a.dv.p) put(a.dv.p + b * a.dv.batch + kv * a.dv.head + o * a.dv.row, s2);
+    } else {
+        put(a.dq.p + row_at(a, a.dq, b, kv, o), s1);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launch
+
+struct Plan {
+    int64_t tiles, splits;
+    size_t part_floats;
+};
+// Owned tiles, and how many parts the streamed axis is cut into where they do not fill the device's blocks.
+Plan plan_for(const tiga_cross &rel, bool keys) {
+    const int64_t heads = static_cast<int64_t>(rel.batch) * rel.kv_heads, rows = rel.num_dst * (rel.heads / rel.kv_heads);
+    const int64_t bn = rel.width == 64 ? 128 : 64;
+    const int64_t own = keys ? rel.num_src : rows, streamed = ceil_div(keys ? rows : rel.num_src, bn);
+    const int64_t resident = static_cast<int64_t>(device_cus()) * (keys ? 1 : 2);
+    Plan p{ceil_div(own, kOwn), 1, 0};
+    const int64_t items = p.tiles * heads;
+    if (items > 0 && items * 2 <= resident) p.splits = resident / items;
+    if (p.splits > streamed) p.splits = streamed < 1 ? 1 : streamed;
+    if (p.splits > 1) p.part_floats = static_cast<size_t>(items * p.splits * (keys ? 2 : 1) * kOwn * rel.width);
+    return p;
+}
+
+struct Layout {
+    Plan q, kv;
+    float *lse2, *delta, *part;
+    size_t bytes;
+};
+Layout layout(const tiga_cross &rel, void *ws) {
+    Layout l;
+    l.q = plan_for(rel, false);
+    l.kv = plan_for(rel, true);
+    Carve c(ws);
+    const size_t stats = static_cast<size_t>(rel.batch) * rel.heads * rel.num_dst + 1;
+    l.lse2 = c.take<float>(stats);
+    l.delta = c.take<float>(stats);
+    l.part = c.take<float>(l.q.part_floats > l.kv.part_floats ? l.q.part_floats : l.kv.part_floats);
+    l.bytes = c.bytes();
+    return l;
+}
+
+template <class T, int D, bool KEYS>
+int products(const Plan &p, Args a, hipStream_t stream) {
+    const int64_t heads = static_cast<int64_t>(a.batch) * a.kv_heads, blocks = heads * p.tiles * p.splits;
+    if (blocks == 0) return TIGA_OK;
+    const int64_t sums = ceil_div(heads * (KEYS ? a.num_src : a.rows) * (D / 4), kThreads);
+    if (blocks > 0x7fffffff || sums > 0x7fffffff)
+        return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many tiles (%lld)", (long long)blocks);
+    a.splits = static_cast<int32_t>(p.splits);
+    if (KEYS) prof_before(stream);
+    hipLaunchKernelGGL((products_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
+                       static_cast<int>(p.tiles));
+    if (KEYS) prof_after(stream);
+    if (int rc = check_launch("cross attention backward")) return rc;
+    if (p.splits == 1) return TIGA_OK;
+    hipLaunchKernelGGL((reduce_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(sums)), dim3(kThreads), 0, stream, a,
+                       static_cast<int>(p.tiles));
+    return check_launch("cross attention backward sums");
 }
 
 template <class T, int D>
-int launch(const Args &a, int64_t num_src_rows, hipStream_t stream) {
-    const int64_t rows = a.num_dst * a.heads * a.batch;
-    prof_before(stream);
-    if (a.dq.p && rows)
-        hipLaunchKernelGGL((dq_kernel<T, D>), dim3(static_cast<unsigned>(ceil_div(rows, kRows))), dim3(kRows * kWave), 0,
-                           stream, a);
-    if ((a.dk.p || a.dv.p) && num_src_rows)
-        hipLaunchKernelGGL((dkv_kernel<T, D>), dim3(static_cast<unsigned>(ceil_div(num_src_rows, kRows))),
-                           dim3(kRows * kWave), 0, stream, a);
-    prof_after(stream);
-    return check_launch("cross attention backward");
+int launch(const Layout &l, const Args &a, hipStream_t stream) {
+    const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * (D / 8), kThreads);
+    if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");
+    hipLaunchKernelGGL((stats_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a);
+    if (int rc = check_launch("cross attention statistics")) return rc;
+    if (a.dk.p || a.dv.p)
+        if (int rc = products<T, D, true>(l.kv, a, stream)) return rc;
+    if (a.dq.p) return products<T, D, false>(l.q, a, stream);
+    return TIGA_OK;
 }
 
 }  // namespace
 
-size_t cross_bwd_ws_bytes(const tiga_cross &) { return 256; }
+size_t cross_bwd_ws_bytes(const tiga_cross &rel) { return rel.kv_heads == 0 ? 256 : layout(rel, nullptr).bytes; }
 
 int cross_backward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v,
                    const tiga_view &y, const float *lse, const tiga_view &dy, float scale, const tiga_view &dq,
-                   const tiga_view &dk, const tiga_view &dv, void *, hipStream_t stream) {
-    const Args a{rows_of(q), rows_of(k), rows_of(v), rows_of(y), rows_of(dy), rows_of(dq), rows_of(dk), rows_of(dv), lse,
-                 rel.src_len, rel.num_dst, rel.num_src, rel.batch, rel.heads, rel.heads / rel.kv_heads, scale};
-    const int64_t src_rows = rel.num_src * rel.kv_heads * rel.batch;
-    if (ceil_div(rel.num_dst * rel.heads * rel.batch, kRows) > 0x7fffffff || ceil_div(src_rows, kRows) > 0x7fffffff)
-        return fail(TIGA_EUNSUPPORTED, "cross attention: too many rows");
-    if (rel.dtype == TIGA_DT_F16) return rel.width == 64 ? launch<F16, 64>(a, src_rows, stream) : launch<F16, 128>(a, src_rows, stream);
-    return rel.width == 64 ? launch<BF16, 64>(a, src_rows, stream) : launch<BF16, 128>(a, src_rows, stream);
+                   const tiga_view &dk, const tiga_view &dv, void *ws, hipStream_t stream) {
+    const Layout l = layout(rel, ws);
+    Args a{};
+    a.q = rows_of(q);
+    a.k = rows_of(k);
+    a.v = rows_of(v);
+    a.y = rows_of(y);
+    a.dy = rows_of(dy);
+    a.dq = rows_of(dq);
+    a.dk = rows_of(dk);
+    a.dv = rows_of(dv);
+    a.lse = lse;
+    a.len = rel.src_len;
+    a.lse2 = l.lse2;
+    a.delta = l.delta;
+    a.part = l.part;
+    a.num_dst = static_cast<int32_t>(rel.num_dst);
+    a.num_src = static_cast<int32_t>(rel.num_src);
+    a.batch = rel.batch;
+    a.heads = rel.heads;
+    a.kv_heads = rel.kv_heads;
+    a.group = divider(static_cast<uint32_t>(rel.heads / rel.kv_heads));
+    a.stats = static_cast<int64_t>(rel.batch) * rel.heads * rel.num_dst;
+    a.rows = static_cast<int32_t>(rel.num_dst * (rel.heads / rel.kv_heads));
+    a.scale = scale;
+    if (rel.dtype == TIGA_DT_F16) return rel.width == 64 ? launch<Half16, 64>(l, a, stream) : launch<Half16, 128>(l, a, stream);
+    return rel.width == 64 ? launch<Brain16, 64>(l, a, stream) : launch<Brain16, 128>(l, a, stream);
 }
 
 }  // namespace relattn
