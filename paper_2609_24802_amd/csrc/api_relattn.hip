@@ -164,6 +164,8 @@ int tiga_mp_attention_cross_bwd(const tiga_cross *rel, const tiga_view *q, const
     if (srcs) {
         if (int rc = check_view(what, "k", k, false, 0, 0, 0)) return rc;
         if (int rc = check_view(what, "v", v, false, 0, 0, 0)) return rc;
+        if (int rc = check_rows(what, "k", k)) return rc;
+        if (int rc = check_rows(what, "v", v)) return rc;
         if (dk)
             if (int rc = check_view(what, "dk", dk, true, rel->batch, rel->kv_heads, rel->num_src)) return rc;
         if (dv)

@@ -131,6 +131,10 @@ __device__ __forceinline__ int swizzle(int k) {
     return ((y & (CPR / 2 - 1)) << 1) | (y / (CPR / 2));
 }
 
+// Blocks a compute unit: dk and dv at width 128 take 512 registers a lane (128 of sums, 64 of owned operands).
+template <int D, bool KEYS>
+constexpr int kBlocks = KEYS && D == 128 ? 1 : 2;
+
 template <class T, int D, bool KEYS>
 struct Sums {
     f4 a1[Geo<D>::DB][2];
@@ -225,7 +229,7 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, KEYS> &acc, const u4 (&x1)
 // the keys, for dq.  A block's pieces: (eight heads, tile, split, head), so that an XCD (every eighth block) keeps to
 // one head of the eight and unequal sequences spread over the XCDs.
 template <class T, int D, bool KEYS>
-__global__ __launch_bounds__(kThreads, KEYS ? 1 : 2) void products_kernel(Args a, int tiles) {
+__global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(Args a, int tiles) {
     using G = Geo<D>;
     __shared__ __attribute__((aligned(1024))) uint8_t y1a[G::TILE], y2a[G::TILE], y1b[G::TILE], y2b[G::TILE];
     __shared__ __attribute__((aligned(256))) float sta[KEYS ? 2 * G::BN : 2], stb[KEYS ? 2 * G::BN : 2];
@@ -297,6 +301,7 @@ __global__ __launch_bounds__(kThreads, KEYS ? 1 : 2) void products_kernel(Args a
     const uint16_t *const kb = a.k.p + b * a.k.batch + kv * a.k.head, *const vb = a.v.p + b * a.v.batch + kv * a.v.head;
     auto stage = [&](int kt, uint8_t *b1, uint8_t *b2, float *stats) {
         const int32_t k0 = kt * G::BN;
+        const uint16_t *const kt0 = kb + k0 * a.k.row, *const vt0 = vb + k0 * a.v.row;
 #pragma unroll
         for (int r = 0; r < G::LPW; ++r) {
             const int run = (w * G::LPW + r) * 1024;
@@ -306,8 +311,8 @@ __global__ __launch_bounds__(kThreads, KEYS ? 1 : 2) void products_kernel(Args a
                 p1 = a.q.p + row_at(a, a.q, b, kv, i);
                 p2 = a.dy.p + row_at(a, a.dy, b, kv, i);
             } else {
-                p1 = kb + i * a.k.row;
-                p2 = vb + i * a.v.row;
+                p1 = kt0 + (i - k0) * static_cast<int32_t>(a.k.row);
+                p2 = vt0 + (i - k0) * static_cast<int32_t>(a.v.row);
             }
             load_to_lds16(p1 + 8 * kch[r], b1 + run);
             load_to_lds16(p2 + 8 * kch[r], b2 + run);
@@ -424,7 +429,7 @@ Plan plan_for(const tiga_cross &rel, bool keys) {
     const int64_t heads = static_cast<int64_t>(rel.batch) * rel.kv_heads, rows = rel.num_dst * (rel.heads / rel.kv_heads);
     const int64_t bn = rel.width == 64 ? 128 : 64;
     const int64_t own = keys ? rel.num_src : rows, streamed = ceil_div(keys ? rows : rel.num_src, bn);
-    const int64_t resident = static_cast<int64_t>(device_cus()) * (keys ? 1 : 2);
+    const int64_t resident = static_cast<int64_t>(device_cus()) * (keys && rel.width == 128 ? 1 : 2);
     Plan p{ceil_div(own, kOwn), 1, 0};
     const int64_t items = p.tiles * heads;
     if (items > 0 && items * 2 <= resident) p.splits = resident / items;
