@@ -417,8 +417,8 @@ size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
  * A destination without sources (src_len[b] == 0) finalizes the reducer's
  * identity: y = 0, lse = -inf.  Sources at and past src_len[b] are not read.
  *   q, y: [batch, heads, num_dst, width];  k, v: [batch, kv_heads, num_src, width]
- *         of dtype, 16-byte aligned, strides multiples of 8 (row strides of k and
- *         v below 2^23); y is overwritten.
+ *         of dtype, 16-byte aligned, strides multiples of 8, head and row strides
+ *         below 2^31 (row strides of k and v below 2^23); y is overwritten.
  *   lse:  fp32 [batch, heads, num_dst], contiguous, or NULL.
  * Products of the inputs are exact and summed in fp32; the mass is the fp32 sum
  * of the fp32 weights; the weights enter the value product rounded to dtype.

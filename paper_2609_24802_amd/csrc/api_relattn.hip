@@ -25,6 +25,8 @@ int check_view(const char *what, const char *name, const tiga_view *v, bool outp
     if (!aligned16(v->data)) return fail(TIGA_EINVAL, "%s: %s must be 16-byte aligned", what, name);
     if ((v->batch | v->head | v->row) & 7) return fail(TIGA_EINVAL, "%s: strides of %s must be multiples of 8", what, name);
     if (v->batch < 0 || v->head < 0 || v->row < 0) return fail(TIGA_EINVAL, "%s: negative stride of %s", what, name);
+    if (v->head > 0x7fffffff || v->row > 0x7fffffff)
+        return fail(TIGA_EUNSUPPORTED, "%s: the head and row strides of %s must be below 2^31", what, name);
     if (output && ((batch > 1 && v->batch == 0) || (heads > 1 && v->head == 0) || (rows > 1 && v->row == 0)))
         return fail(TIGA_EINVAL, "%s: the rows of %s overlap (a stride is 0)", what, name);
     return TIGA_OK;

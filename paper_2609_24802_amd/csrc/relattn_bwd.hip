@@ -65,7 +65,9 @@ __device__ __forceinline__ int32_t sources(const Args &a, int b) {
 // Row r of a source head is token r / group of head r % group of its group.
 __device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int b, int kv, int32_t r) {
     const int32_t token = static_cast<int32_t>(a.group.div(r)), g = r - token * static_cast<int32_t>(a.group.d);
-    return b * t.batch + static_cast<int64_t>(kv * static_cast<int32_t>(a.group.d) + g) * t.head + token * t.row;
+    // row and head strides are below 2^31
+    return b * t.batch + static_cast<int64_t>(kv * static_cast<int32_t>(a.group.d) + g) * static_cast<int32_t>(t.head) +
+           static_cast<int64_t>(token) * static_cast<int32_t>(t.row);
 }
 __device__ __forceinline__ int64_t stat_at(const Args &a, int b, int kv, int32_t r) {
     const int32_t token = static_cast<int32_t>(a.group.div(r)), g = r - token * static_cast<int32_t>(a.group.d);
