@@ -541,67 +541,65 @@ _HALF_TYPES = {torch.float16: DT_F16, torch.bfloat16: DT_BF16}
 _ROTARY_TYPES = {torch.float16: DT_F16, torch.bfloat16: DT_BF16, torch.float32: DT_F32}
 
 
-def _on(device, **tensors):
+# positions of the axes batch, heads, rows, width in a tensor of each layout (-1: no batch axis)
+_AXES = {"bhnd": (0, 1, 2, 3), "bnhd": (0, 2, 1, 3), "hnd": (-1, 0, 1, 2), "nhd": (-1, 1, 0, 2)}
+
+
+def _axes(layout, dims):
+    if layout not in _AXES or len(layout) not in dims:
+        raise ValueError(f"unknown layout {layout!r}")
+    return _AXES[layout]
+
+
+def _same_device(device: int, **tensors):
     """The call's tensors lie on one device, and that is the current one (whose stream the work goes to)."""
     for name, t in tensors.items():
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-        if t.device != device:
-            raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {device}, the current device is {torch.cuda.current_device()}")
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} is on {t.device}, expected cuda:{device}")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is {torch.cuda.current_device()}")
 
 
-def _rows(t, name, layout, dtype=None, shape=None, out=False):
-    """t in the axis order [batch, heads, rows, width] (any strides, the width contiguous) and its view.
-
-    layout names t's own axes: "bhnd" or "bnhd", or without a batch "hnd" or "nhd"."""
-    order = {"bhnd": None, "bnhd": (0, 2, 1, 3), "hnd": None, "nhd": (1, 0, 2)}
-    if layout not in order:
-        raise ValueError(f"unknown layout {layout!r}")
+def _rows(t, name, axes, dtype=None, shape=None):
+    """(batch, heads, rows, width) of t and its view: any strides, the width contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != len(layout):
-        raise ValueError(f"{name} must have {len(layout)} dimensions (layout {layout!r})")
-    if order[layout] is not None:
-        t = t.permute(order[layout])
-    if t.dim() == 3:
-        t = t.unsqueeze(0)
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has [batch, heads, rows, width] {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.shape[3] > 1 and t.numel() and t.stride(3) != 1:
+    s, st = t.shape, t.stride()
+    b, h, n, d = axes
+    if len(s) != d + 1:
+        raise ValueError(f"{name} must have {d + 1} dimensions")
+    got = (s[b] if b >= 0 else 1, s[h], s[n], s[d])
+    if shape is not None and got != shape:
+        raise ValueError(f"{name} has (batch, heads, rows, width) {got}, expected {tuple(shape)}")
+    if got[3] > 1 and st[d] != 1 and t.numel():
         raise ValueError(f"{name}: the width must be contiguous")
     # the stride of an axis with one entry is never used; torch leaves anything there
-    st = [t.stride(a) if t.shape[a] > 1 else 0 for a in range(3)]
-    return t, _View(t.data_ptr() if t.numel() else None, *st)
+    return got, _View(t.data_ptr() or None, st[b] if got[0] > 1 else 0, st[h] if got[1] > 1 else 0,
+                      st[n] if got[2] > 1 else 0)
 
 
-def _like(t, layout):
-    """A new contiguous tensor of t's shape and layout, and its view."""
-    y = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-    return y, _rows(y, "output", layout)[1]
+def _like(t, axes):
+    """A new contiguous tensor of t's shape, and its view."""
+    y = t.new_empty(t.shape)
+    return y, _rows(y, "output", axes)[1]
 
 
 def _cross(q, k, v, src_len, layout):
-    if len(layout) != 4:
-        raise ValueError(f"unknown layout {layout!r}")
-    if not isinstance(q, torch.Tensor) or q.dtype not in _HALF_TYPES:
+    axes = _axes(layout, (4,))
+    (B, H, N, D), qv = _rows(q, "q", axes)
+    dt = _HALF_TYPES.get(q.dtype)
+    if dt is None:
         raise TypeError("q must be a float16 or bfloat16 tensor")
-    qt, qv = _rows(q, "q", layout)
-    kt, kv = _rows(k, "k", layout, q.dtype)
-    B, H, N, D = qt.shape
-    Hk, S = kt.shape[1], kt.shape[2]
-    _, kv = _rows(k, "k", layout, q.dtype, (B, Hk, S, D))
-    _, vv = _rows(v, "v", layout, q.dtype, (B, Hk, S, D))
-    _on(q.device, k=k, v=v, src_len=src_len)
+    (Bk, Hk, S, Dk), kv = _rows(k, "k", axes, q.dtype)
+    if Bk != B or Dk != D:
+        raise ValueError(f"k has batch {Bk} and width {Dk}, q has {B} and {D}")
+    _, vv = _rows(v, "v", axes, q.dtype, (B, Hk, S, D))
+    _same_device(q.get_device(), k=k, v=v, src_len=src_len)
     if src_len is not None:
         _dev(src_len, torch.int32, "src_len", (B,))
-    rel = _Cross(N, S, B, H, Hk, D, _HALF_TYPES[q.dtype], src_len.data_ptr() if src_len is not None else None)
-    return rel, qv, kv, vv
+    return _Cross(N, S, B, H, Hk, D, dt, src_len.data_ptr() if src_len is not None else None), qv, kv, vv, axes
 
 
 def tiga_mp_attention_cross_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -615,14 +613,14 @@ def tiga_mp_attention_cross_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     (None: all).  A sequence without sources gives y = 0, lse = -inf.  scale defaults to width ** -0.5.
     Returns y in q's shape (and lse fp32 [batch, heads, num_dst] when want_lse)."""
     lib = load()
-    rel, qv, kv, vv = _cross(q, k, v, src_len, layout)
-    y, yv = _like(q, layout)
-    lse = torch.empty(rel.batch, rel.heads, rel.num_dst, dtype=torch.float32, device=q.device) if want_lse else None
+    rel, qv, kv, vv, axes = _cross(q, k, v, src_len, layout)
+    y, yv = _like(q, axes)
+    lse = q.new_empty((rel.batch, rel.heads, rel.num_dst), dtype=torch.float32) if want_lse else None
     ref = C.byref
     if ws is None:
         ws = _workspace(lib.tiga_mp_attention_cross_fwd_workspace(ref(rel)), q.device)
     _check(lib.tiga_mp_attention_cross_fwd(ref(rel), ref(qv), ref(kv), ref(vv),
-                                           float(rel.width ** -0.5 if scale is None else scale), ref(yv), _ptr(lse),
+                                           rel.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
                                            _ptr(ws), ws.numel(), _stream()))
     return (y, lse) if want_lse else y
 
@@ -632,23 +630,23 @@ def tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy, src_len: torch.Tensor | Non
     """The VJP of tiga_mp_attention_cross_fwd for the cotangent dy, from the forward's y and lse; returns a
     dict of the wanted gradients in the inputs' shapes.  Gradients of sources past src_len are 0."""
     lib = load()
-    rel, qv, kv, vv = _cross(q, k, v, src_len, layout)
+    rel, qv, kv, vv, axes = _cross(q, k, v, src_len, layout)
     shape = (rel.batch, rel.heads, rel.num_dst, rel.width)
-    _, yv = _rows(y, "y", layout, q.dtype, shape)
-    _, dyv = _rows(dy, "dy", layout, q.dtype, shape)
-    _on(q.device, y=y, dy=dy, lse=lse)
+    _, yv = _rows(y, "y", axes, q.dtype, shape)
+    _, dyv = _rows(dy, "dy", axes, q.dtype, shape)
     _dev(lse, torch.float32, "lse", shape[:3])
-    out, views = {}, dict(dq=None, dk=None, dv=None)
-    for name, t in (("dq", q), ("dk", k), ("dv", v)):
-        if name in want:
-            out[name], views[name] = _like(t, layout)
+    _same_device(q.get_device(), y=y, dy=dy, lse=lse)
     ref = C.byref
+    out, refs = {}, [None, None, None]
+    for i, (name, t) in enumerate((("dq", q), ("dk", k), ("dv", v))):
+        if name in want:
+            out[name], view = _like(t, axes)
+            refs[i] = ref(view)
     if ws is None:
         ws = _workspace(lib.tiga_mp_attention_cross_bwd_workspace(ref(rel)), q.device)
-    opt = lambda name: ref(views[name]) if views[name] is not None else None
     _check(lib.tiga_mp_attention_cross_bwd(ref(rel), ref(qv), ref(kv), ref(vv), ref(yv), _ptr(lse), ref(dyv),
-                                           float(rel.width ** -0.5 if scale is None else scale), opt("dq"), opt("dk"),
-                                           opt("dv"), _ptr(ws), ws.numel(), _stream()))
+                                           rel.width ** -0.5 if scale is None else float(scale), *refs, _ptr(ws),
+                                           ws.numel(), _stream()))
     return out
 
 
@@ -685,11 +683,11 @@ class Rotary:
 
 
 def _rotary_call(name, x, pos, rot, layout, out):
-    lib = load()
-    if not isinstance(x, torch.Tensor) or x.dtype not in _ROTARY_TYPES:
+    axes = _axes(layout, (3, 4))
+    (B, H, N, D), xv = _rows(x, "x", axes)
+    dt = _ROTARY_TYPES.get(x.dtype)
+    if dt is None:
         raise TypeError("x must be a float16, bfloat16 or float32 tensor")
-    xt, xv = _rows(x, "x", layout)
-    B, H, N, D = xt.shape
     pos_batch = 0
     if pos is not None:
         if pos.dim() == 2:
@@ -697,13 +695,12 @@ def _rotary_call(name, x, pos, rot, layout, out):
             pos_batch = N
         else:
             _dev(pos, torch.int32, "pos", (N,))
-    _on(x.device, pos=pos, freq=rot.freq, out=out)
     if out is None:
-        out, ov = _like(x, layout)
+        out, ov = _like(x, axes)
     else:
-        _, ov = _rows(out, "out", layout, x.dtype, xt.shape)
-    _check(getattr(lib, name)(B, H, N, D, _ROTARY_TYPES[x.dtype], C.byref(xv), _ptr(pos), pos_batch, rot.ref,
-                              C.byref(ov), _stream()))
+        _, ov = _rows(out, "out", axes, x.dtype, (B, H, N, D))
+    _same_device(x.get_device(), pos=pos, freq=rot.freq, out=out)
+    _check(getattr(load(), name)(B, H, N, D, dt, C.byref(xv), _ptr(pos), pos_batch, rot.ref, C.byref(ov), _stream()))
     return out
 
 
@@ -731,10 +728,10 @@ class KvCache:
     call.  The tensors are the caller's; their contents may change between calls."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
-        if not isinstance(k_pages, torch.Tensor) or k_pages.dtype not in _HALF_TYPES:
+        shape, kv = _rows(k_pages, "k_pages", _AXES["bhnd"])
+        if k_pages.dtype not in _HALF_TYPES:
             raise TypeError("k_pages must be a float16 or bfloat16 tensor")
-        kt, kv = _rows(k_pages, "k_pages", "bhnd")
-        _, vv = _rows(v_pages, "v_pages", "bhnd", k_pages.dtype, kt.shape)
+        _, vv = _rows(v_pages, "v_pages", _AXES["bhnd"], k_pages.dtype, shape)
         self.table = _dev(table, torch.int32, "table")
         if table.dim() != 2:
             raise ValueError("table must be [batch, table_width]")
@@ -743,7 +740,7 @@ class KvCache:
             if t.device != k_pages.device:
                 raise ValueError(f"{name} is on {t.device}, expected {k_pages.device}")
         self.k_pages, self.v_pages = k_pages, v_pages
-        P, H, R, D = kt.shape
+        P, H, R, D = shape
         self.kv_heads, self.width, self.batch = H, D, table.shape[0]
         self._c = _Cache(P, R, H, D, _HALF_TYPES[k_pages.dtype], table.shape[0], table.shape[1], kv, vv,
                          table.data_ptr() if table.numel() else None, length.data_ptr() if length.numel() else None)
@@ -753,21 +750,19 @@ class KvCache:
         return C.byref(self._c)
 
 
-def _new_rows(cache, t, name, layout, heads=None):
-    """A packed tensor of new tokens in the cache's type and width."""
-    if len(layout) != 3:
-        raise ValueError(f"unknown layout {layout!r}")
-    tt, view = _rows(t, name, layout, cache.k_pages.dtype)
-    if tt.shape[3] != cache.width or (heads is not None and tt.shape[1] != heads):
-        raise ValueError(f"{name} has [heads, rows, width] {tuple(tt.shape[1:])}, expected "
-                         f"{heads if heads is not None else 'heads'} heads of width {cache.width}")
-    return tt, view
+def _new_rows(cache, t, name, axes, heads=None, rows=None):
+    """heads, rows and the view of a packed tensor of new tokens in the cache's type and width."""
+    got, view = _rows(t, name, axes, cache.k_pages.dtype)
+    if got[3] != cache.width or heads not in (None, got[1]) or rows not in (None, got[2]):
+        raise ValueError(f"{name} has (heads, rows, width) {got[1:]}, expected "
+                         f"({'heads' if heads is None else heads}, {'rows' if rows is None else rows}, {cache.width})")
+    return got[1], got[2], view
 
 
 def tiga_cache_validate(cache: KvCache, num_dst: int, dst_ptr: torch.Tensor):
     """Raise TigaError (TIGA_EGRAPH) if dst_ptr, the lengths or the pages they need are inconsistent.  Synchronizes."""
     _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
-    _on(cache.k_pages.device, dst_ptr=dst_ptr)
+    _same_device(cache.k_pages.get_device(), dst_ptr=dst_ptr)
     _check(load().tiga_cache_validate(cache.ref, int(num_dst), _ptr(dst_ptr), _stream()))
 
 
@@ -779,29 +774,27 @@ def tiga_mp_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, dst_p
     of all sequences packed: sequence b owns rows dst_ptr[b] to dst_ptr[b + 1] (int32 [batch + 1]), its last
     row at position length[b] - 1.  With q [heads, rows, width] the queries are rotated by the same
     positions in the same launch and returned (q_out may be q)."""
-    lib = load()
-    _, kv = _new_rows(cache, k, "k", layout, cache.kv_heads)
-    kt, vv = _new_rows(cache, v, "v", layout, cache.kv_heads)
-    rows = _rows(k, "k", layout)[0].shape[2]
-    if kt.shape[2] != rows:
-        raise ValueError(f"v has {kt.shape[2]} rows, k has {rows}")
+    axes = _axes(layout, (3,))
+    _, rows, kv = _new_rows(cache, k, "k", axes, cache.kv_heads)
+    _, _, vv = _new_rows(cache, v, "v", axes, cache.kv_heads, rows)
     _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    ref = C.byref
     heads, qv, ov = 0, None, None
     if q is not None:
         if rot is None:
             raise ValueError("q is only taken to be rotated: rot is missing")
-        qt, qv = _new_rows(cache, q, "q", layout)
-        heads = qt.shape[1]
-        if qt.shape[2] != rows:
-            raise ValueError(f"q has {qt.shape[2]} rows, k has {rows}")
+        heads, _, qv = _new_rows(cache, q, "q", axes, None, rows)
         if q_out is None:
-            q_out, ov = _like(q, layout)
+            q_out, ov = _like(q, axes)
         else:
-            _, ov = _rows(q_out, "q_out", layout, q.dtype, qt.shape)
-    _on(cache.k_pages.device, k=k, v=v, dst_ptr=dst_ptr, q=q, q_out=q_out, freq=rot.freq if rot else None)
-    ref = C.byref
-    _check(lib.tiga_mp_cache_append(cache.ref, rows, _ptr(dst_ptr), ref(kv), ref(vv), rot.ref if rot else None, heads,
-                                    ref(qv) if qv else None, ref(ov) if ov else None, _stream()))
+            _, _, ov = _new_rows(cache, q_out, "q_out", axes, heads, rows)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _same_device(cache.k_pages.get_device(), k=k, v=v, dst_ptr=dst_ptr, q=q, q_out=q_out,
+                 freq=rot.freq if rot is not None else None)
+    _check(load().tiga_mp_cache_append(cache.ref, rows, _ptr(dst_ptr), ref(kv), ref(vv),
+                                       rot.ref if rot is not None else None, heads, ref(qv) if qv is not None else None,
+                                       ref(ov) if ov is not None else None, _stream()))
     return q_out
 
 
@@ -813,20 +806,20 @@ def tiga_mp_attention_paged_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.
     multiple of the cache's; the row at position p reads positions 0 to p of its sequence.  Rows behind
     dst_ptr[batch] of y are left as they were.  Returns y in q's shape (and lse fp32 [heads, rows])."""
     lib = load()
-    qt, qv = _new_rows(cache, q, "q", layout)
-    heads, rows = qt.shape[1], qt.shape[2]
+    axes = _axes(layout, (3,))
+    heads, rows, qv = _new_rows(cache, q, "q", axes)
     _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
     if y is None:
-        y, yv = _like(q, layout)
+        y, yv = _like(q, axes)
     else:
-        _, yv = _rows(y, "y", layout, q.dtype, qt.shape)
-    _on(cache.k_pages.device, q=q, y=y, dst_ptr=dst_ptr)
-    lse = torch.empty(heads, rows, dtype=torch.float32, device=q.device) if want_lse else None
+        _, _, yv = _new_rows(cache, y, "y", axes, heads, rows)
+    _same_device(cache.k_pages.get_device(), q=q, y=y, dst_ptr=dst_ptr)
+    lse = q.new_empty((heads, rows), dtype=torch.float32) if want_lse else None
     ref = C.byref
     if ws is None:
         ws = _workspace(lib.tiga_mp_attention_paged_fwd_workspace(cache.ref, rows, heads), q.device)
     _check(lib.tiga_mp_attention_paged_fwd(cache.ref, rows, _ptr(dst_ptr), heads, ref(qv),
-                                           float(cache.width ** -0.5 if scale is None else scale), ref(yv), _ptr(lse),
+                                           cache.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
                                            _ptr(ws), ws.numel(), _stream()))
     return (y, lse) if want_lse else y
 

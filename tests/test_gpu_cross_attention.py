@@ -226,7 +226,7 @@ def test_outputs_are_written_inside_their_rows_only(lib):
     q, k, v, _ = make(2, 2, 2, 37, 50, 64, F16, seed=13)
     buf = torch.full((2, 2, 39, 80), 7.0, dtype=F16, device="cuda")
     L = lib.load()
-    rel, qv, kv, vv = lib._cross(q, k, v, None, "bhnd")
+    rel, qv, kv, vv, _ = lib._cross(q, k, v, None, "bhnd")
     yv = lib._View(buf.data_ptr() + 2 * (80 + 8), *buf.stride()[:3])
     ws = lib._workspace(L.tiga_mp_attention_cross_fwd_workspace(C.byref(rel)), q.device)
     rc = L.tiga_mp_attention_cross_fwd(C.byref(rel), C.byref(qv), C.byref(kv), C.byref(vv), 0.125, C.byref(yv), None,
