@@ -7,6 +7,49 @@
 namespace tiga {
 namespace relattn {
 
+// n / d for n < 2^31 by a multiplication (round-up method; m holds the low 32 bits of a 33-bit factor).
+struct Divider {
+    uint32_t m, s, d;
+    __device__ __forceinline__ int32_t div(int32_t n) const {
+        return static_cast<int32_t>((__umulhi(m, static_cast<uint32_t>(n)) + static_cast<uint32_t>(n)) >> s);
+    }
+};
+inline Divider divider(int32_t d) {
+    uint32_t s = 0;
+    const uint64_t n = static_cast<uint64_t>(d);
+    while ((uint64_t(1) << s) < n) ++s;
+    return Divider{static_cast<uint32_t>(((uint64_t(1) << 32) * ((uint64_t(1) << s) - n)) / n + 1), s, static_cast<uint32_t>(d)};
+}
+
+// a / b for a >= 0, b > 0 (uniform): the 64-bit division is a long subroutine, and these values are small.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
+// Inclusive prefix sum over the wavefront by lane shifts within the vector unit (no LDS round trips): shifts by 1, 2, 4
+// and 8 within rows of 16 lanes, then row 0 and 2 into the next, then the lower half into the upper.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t lanes_shifted(int64_t v) {
+    const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(v >> 32), CTRL, ROWS, 0xf, false);
+    return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo));
+}
+__device__ __forceinline__ int64_t wave_prefix(int64_t v) {
+    v += lanes_shifted<0x111, 0xf>(v);
+    v += lanes_shifted<0x112, 0xf>(v);
+    v += lanes_shifted<0x114, 0xf>(v);
+    v += lanes_shifted<0x118, 0xf>(v);
+    v += lanes_shifted<0x142, 0xa>(v);
+    v += lanes_shifted<0x143, 0xc>(v);
+    return v;
+}
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {  // lane: uniform
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), lane);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(static_cast<uint64_t>(v) >> 32), lane);
+    return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
 // Element strides of a view as the kernels take them.
 struct Rows {
     const uint16_t *p;

@@ -32,17 +32,6 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kOwn = 128;  // owned rows or keys of a block: 32 a wavefront
 constexpr float kLog2e = 1.4426950408889634f;
 
-// n / d for n < 2^31 by a multiplication (round-up method; M holds the low 32 bits of a 33-bit factor).
-struct Divider {
-    uint32_t m, s, d;
-    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(m, n) + n) >> s; }
-};
-Divider divider(uint32_t d) {
-    uint32_t s = 0;
-    while ((uint64_t(1) << s) < d) ++s;
-    return Divider{static_cast<uint32_t>(((uint64_t(1) << 32) * ((uint64_t(1) << s) - d)) / d + 1), s, d};
-}
-
 struct Args {
     Rows q, k, v, y, dy, dq, dk, dv;
     const float *lse;
@@ -64,13 +53,13 @@ __device__ __forceinline__ int32_t sources(const Args &a, int b) {
 }
 // Row r of a source head is token r / group of head r % group of its group.
 __device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int b, int kv, int32_t r) {
-    const int32_t token = static_cast<int32_t>(a.group.div(r)), g = r - token * static_cast<int32_t>(a.group.d);
+    const int32_t token = a.group.div(r), g = r - token * static_cast<int32_t>(a.group.d);
     // row and head strides are below 2^31
     return b * t.batch + static_cast<int64_t>(kv * static_cast<int32_t>(a.group.d) + g) * static_cast<int32_t>(t.head) +
            static_cast<int64_t>(token) * static_cast<int32_t>(t.row);
 }
 __device__ __forceinline__ int64_t stat_at(const Args &a, int b, int kv, int32_t r) {
-    const int32_t token = static_cast<int32_t>(a.group.div(r)), g = r - token * static_cast<int32_t>(a.group.d);
+    const int32_t token = a.group.div(r), g = r - token * static_cast<int32_t>(a.group.d);
     return (static_cast<int64_t>(b) * a.heads + kv * static_cast<int32_t>(a.group.d) + g) * a.num_dst + token;
 }
 
@@ -516,7 +505,7 @@ int cross_backward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k
     a.batch = rel.batch;
     a.heads = rel.heads;
     a.kv_heads = rel.kv_heads;
-    a.group = divider(static_cast<uint32_t>(rel.heads / rel.kv_heads));
+    a.group = divider(rel.heads / rel.kv_heads);
     a.stats = static_cast<int64_t>(rel.batch) * rel.heads * rel.num_dst;
     a.rows = static_cast<int32_t>(rel.num_dst * (rel.heads / rel.kv_heads));
     a.scale = scale;

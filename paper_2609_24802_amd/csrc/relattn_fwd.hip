@@ -51,7 +51,8 @@ struct Args {
     float *lse;
     int64_t lse_batch, lse_head;
     float c;  // scale * log2 e: scores are kept in the log2 domain
-    int kv_heads, group;
+    int kv_heads;
+    Divider group;  // rows to a token
     // partial states and what they are of; NULL: items are not cut
     float *part;
     int4 *rec;
@@ -82,11 +83,11 @@ template <bool PAGED>
 __device__ __forceinline__ Seq seq_of(const Args<PAGED> &a, int b) {
     if constexpr (PAGED) {
         const Chunk ch = chunk_of(a.src, b);
-        return Seq{ch.first, ch.count * a.group, ch.pos0 + 1};
+        return Seq{ch.first, ch.count * static_cast<int32_t>(a.group.d), ch.pos0 + 1};
     } else {
         int32_t n = a.src.num_src;
         if (a.src.len) n = a.src.len[b] < 0 ? 0 : (a.src.len[b] > n ? n : a.src.len[b]);
-        return Seq{0, a.src.num_dst * a.group, n};
+        return Seq{0, a.src.num_dst * static_cast<int32_t>(a.group.d), n};
     }
 }
 // Keys that row r of the sequence sees, at least 0.  A row past the table's end sees one position behind it, which is
@@ -94,7 +95,7 @@ __device__ __forceinline__ Seq seq_of(const Args<PAGED> &a, int b) {
 template <bool PAGED>
 __device__ __forceinline__ int32_t keys_of(const Args<PAGED> &a, const Seq &s, int r) {
     if constexpr (PAGED) {
-        const int64_t n = s.keys0 + r / a.group, most = (static_cast<int64_t>(a.src.table_width) << a.src.shift) + 1;
+        const int64_t n = s.keys0 + a.group.div(r), most = (static_cast<int64_t>(a.src.table_width) << a.src.shift) + 1;
         return static_cast<int32_t>(n < 0 ? 0 : (n > most ? most : n));
     } else {
         return static_cast<int32_t>(s.keys0);
@@ -119,11 +120,12 @@ struct Tiles {
             const int32_t n0 = keys_of<PAGED>(a, s, min(BM, s.rows) - 1), n1 = keys_of<PAGED>(a, s, s.rows - 1);
             const int32_t w1 = max(1, (n1 + BN - 1) / BN);
             t.w0 = max(1, (n0 + BN - 1) / BN);
-            t.slope = static_cast<double>(w1 - static_cast<int32_t>(t.w0)) / (2.0 * t.count);
+            if (w1 != static_cast<int32_t>(t.w0)) t.slope = static_cast<double>(w1 - static_cast<int32_t>(t.w0)) / (2.0 * t.count);
         }
         return t;
     }
     __device__ __forceinline__ int64_t start(int64_t j) const {
+        if (slope == 0.0) return j * w0;
         return j * w0 + static_cast<int64_t>(slope * static_cast<double>(j) * static_cast<double>(j));
     }
     __device__ __forceinline__ int64_t total() const { return start(count); }
@@ -143,63 +145,56 @@ struct Tiles {
 template <bool PAGED, int BM, int BN>
 struct Walk {
     typedef Tiles<BM, BN> T;
-    int64_t u, end;   // position and end of the run
-    int64_t base;     // where sequence b starts
+    int64_t u, end;       // position and end of the run
+    int64_t base, whole;  // where sequence b starts, and a head's weight in it
     int32_t b;
     Seq s;
     T t;
 
-    __device__ __forceinline__ int64_t weight(const Args<PAGED> &a, int e) const {
-        if (e >= batch(a)) return 0;
+    static __device__ __forceinline__ int64_t weight(const Args<PAGED> &a, int e) {
+        if (e >= a.src.batch) return 0;
         return T::template of<PAGED>(a, seq_of<PAGED>(a, e), a.part != nullptr).total() * a.kv_heads;
     }
-    static __device__ __forceinline__ int batch(const Args<PAGED> &a) { return a.src.batch; }
-
+    static __device__ __forceinline__ bool alike(const Args<PAGED> &a) {  // every sequence weighs the same
+        if constexpr (PAGED) return false;
+        else return !a.src.len || !a.part;
+    }
     __device__ __forceinline__ void begin(const Args<PAGED> &a, int w, int blocks) {
-        int64_t all = 0;
-        const int nb = batch(a);
-        const int64_t first = weight(a, lane_id());
-        if constexpr (!PAGED) {
-            if (!a.src.len || !a.part) all = uniform64(first) * nb;  // every sequence alike
-        }
-        if (all == 0)
-            for (int e = 0; e < nb; e += kWave) all += wave_total(e == 0 ? first : weight(a, e + lane_id()));
-        const int64_t per = all / blocks, rem = all % blocks;
+        const int nb = a.src.batch;
+        const int64_t first = weight(a, lane_id()), prefix = wave_prefix(first);
+        int64_t all = lane_value(prefix, kWave - 1);
+        if (alike(a)) all = lane_value(first, 0) * nb;
+        else
+            for (int e = kWave; e < nb; e += kWave) all += lane_value(wave_prefix(weight(a, e + lane_id())), kWave - 1);
+        const int64_t per = quotient(all, blocks), rem = all - per * blocks;
         u = w * per + (w < rem ? w : rem);
         end = u + per + (w < rem ? 1 : 0);
         base = 0;
         b = 0;
         if (u >= end) return;
-        if constexpr (!PAGED) {
-            if (!a.src.len || !a.part) {
-                b = static_cast<int32_t>(u / uniform64(first));
-                base = b * uniform64(first);
-                load(a);
-                return;
+        if (alike(a)) {
+            b = static_cast<int32_t>(quotient(u, lane_value(first, 0)));
+            base = b * lane_value(first, 0);
+        } else {
+            for (int e = 0; e < nb; e += kWave) {
+                const int64_t mine = e == 0 ? first : weight(a, e + lane_id());
+                const int64_t incl = e == 0 ? prefix : wave_prefix(mine);
+                const uint64_t past = __ballot(base + incl > u);
+                if (past) {
+                    const int l = __builtin_ctzll(past);
+                    b = e + l;
+                    base += lane_value(incl - mine, l);
+                    break;
+                }
+                base += lane_value(incl, kWave - 1);
             }
         }
-        for (int e = 0; e < nb; e += kWave) {
-            const int64_t mine = e == 0 ? first : weight(a, e + lane_id());
-            const int64_t incl = wave_incl_scan(mine);
-            const uint64_t past = __ballot(base + incl > u);
-            if (past) {
-                const int l = __builtin_ctzll(past);
-                b = e + l;
-                base += __shfl(incl - mine, l, kWave);
-                break;
-            }
-            base += __shfl(incl, kWave - 1, kWave);
-        }
-        base = uniform64(base);
-        b = uniform(b);
         load(a);
-    }
-    static __device__ __forceinline__ int64_t wave_total(int64_t v) {
-        return uniform64(__shfl(wave_incl_scan(v), kWave - 1, kWave));
     }
     __device__ __forceinline__ void load(const Args<PAGED> &a) {
         s = seq_of<PAGED>(a, b);
         t = T::template of<PAGED>(a, s, a.part != nullptr);
+        whole = t.total();
     }
     // The next part of an item of the run: row tile j of source head `head`, key tiles [t0, t1) of n.  starts / ends:
     // whether it holds the item's first and last share.
@@ -210,20 +205,20 @@ struct Walk {
     };
     __device__ __forceinline__ bool next(const Args<PAGED> &a, Piece &p) {
         if (u >= end) return false;
-        while (u >= base + t.total() * a.kv_heads) {  // the run is not at its end, so a later sequence holds u
-            base += t.total() * a.kv_heads;
+        while (u >= base + whole * a.kv_heads) {  // the run is not at its end, so a later sequence holds u
+            base += whole * a.kv_heads;
             ++b;
             load(a);
         }
         const int64_t in = u - base;
-        p.head = static_cast<int32_t>(in / t.total());
-        const int64_t r = in - p.head * t.total();
+        p.head = static_cast<int32_t>(quotient(in, whole));
+        const int64_t r = in - p.head * whole;
         p.j = t.find(r);
         const int64_t at = t.start(p.j), w = t.start(p.j + 1) - at, off = r - at;
         const int64_t take = min(w - off, end - u);
         p.n = (keys_of<PAGED>(a, s, min((p.j + 1) * BM, s.rows) - 1) + BN - 1) / BN;
-        p.t0 = static_cast<int32_t>(off * p.n / w);
-        p.t1 = static_cast<int32_t>((off + take) * p.n / w);
+        p.t0 = static_cast<int32_t>(w == p.n ? off : quotient(off * p.n, w));
+        p.t1 = static_cast<int32_t>(w == p.n ? off + take : quotient((off + take) * p.n, w));
         p.starts = off == 0;
         p.ends = off + take == w;
         u += take;
@@ -267,21 +262,19 @@ struct Deal {
     // Sum of f(load) over the sequences, times the heads.
     template <class F>
     static __device__ __forceinline__ int64_t total(const Args<PAGED> &a, const Load &first, F f) {
-        if (alike(a)) return uniform64(f(first)) * a.src.batch * a.kv_heads;
-        int64_t all = 0;
-        for (int e = 0; e < a.src.batch; e += kWave) {
-            int64_t v = e == 0 ? f(first) : f(load(a, e + lane_id()));
-            for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d, kWave);
-            all += v;
-        }
-        return uniform64(all) * a.kv_heads;
+        if (alike(a)) return lane_value(f(first), 0) * a.src.batch * a.kv_heads;
+        int64_t all = lane_value(wave_prefix(f(first)), kWave - 1);
+        for (int e = kWave; e < a.src.batch; e += kWave) all += lane_value(wave_prefix(f(load(a, e + lane_id()))), kWave - 1);
+        return all * a.kv_heads;
     }
-    static __device__ __forceinline__ int32_t parts(int32_t n, int32_t chunk) { return static_cast<int32_t>((n + static_cast<int64_t>(chunk) - 1) / chunk); }
+    static __device__ __forceinline__ int32_t parts(int32_t n, int32_t chunk) {  // n >= 1
+        return static_cast<int32_t>(static_cast<uint32_t>(n - 1) / static_cast<uint32_t>(chunk)) + 1;
+    }
     // Row tiles that see keys of chunk c: token t does if keys0 + t > c * chunk * BN.
     static __device__ __forceinline__ int32_t reach(const Args<PAGED> &a, const Load &l, int32_t c, int32_t chunk) {
         if constexpr (PAGED) {
             const int64_t t = static_cast<int64_t>(c) * chunk * BN - l.keys0 + 1;
-            return c == 0 || t <= 0 ? l.tiles : l.tiles - static_cast<int32_t>(t * a.group / BM);
+            return c == 0 || t <= 0 ? l.tiles : l.tiles - static_cast<int32_t>(t * a.group.d / BM);
         } else {
             return l.tiles;
         }
@@ -291,7 +284,7 @@ struct Deal {
         const int32_t n = parts(l.n1, chunk);
         if constexpr (!PAGED) return static_cast<int64_t>(n) * l.tiles;
         // the chunks below the first token's keys are whole
-        const int64_t below = l.keys0 > 0 ? (l.keys0 - 1) / (static_cast<int64_t>(chunk) * BN) + 1 : 1;
+        const int64_t below = l.keys0 > 0 ? static_cast<int64_t>(static_cast<uint32_t>((l.keys0 - 1) / BN) / static_cast<uint32_t>(chunk)) + 1 : 1;
         int64_t all = min(static_cast<int64_t>(n), below) * l.tiles;
         for (int64_t c = below; c < n; ++c) all += reach(a, l, static_cast<int32_t>(c), chunk);
         return all;
@@ -305,7 +298,7 @@ struct Deal {
         pieces = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles); });
         if (!a.part || pieces > a.slots) return;
         const int64_t work = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles) * ((l.n0 + l.n1 + 1) / 2); });
-        int64_t c = max(int64_t(4), (work + a.slots - 1) / a.slots);
+        int64_t c = max(int64_t(4), quotient(work + a.slots - 1, a.slots));
         do {
             chunk = static_cast<int32_t>(min(c, static_cast<int64_t>(kWhole)));
             pieces = total(a, first, [&](const Load &l) { return count(a, l, chunk); });
@@ -323,24 +316,22 @@ struct Deal {
         int b = 0;
         const Load first = load(a, lane_id());
         if (alike(a)) {
-            const int64_t per = uniform64(count(a, first, chunk)) * a.kv_heads;
-            b = static_cast<int>(p / per);
+            const int64_t per = lane_value(count(a, first, chunk), 0) * a.kv_heads;
+            b = static_cast<int>(quotient(p, per));
             base = b * per;
         } else {
             for (int e = 0; e < a.src.batch; e += kWave) {
                 const int64_t mine = count(a, e == 0 ? first : load(a, e + lane_id()), chunk) * a.kv_heads;
-                const int64_t incl = wave_incl_scan(mine);
+                const int64_t incl = wave_prefix(mine);
                 const uint64_t past = __ballot(base + incl > p);
                 if (past) {
                     const int i = __builtin_ctzll(past);
                     b = e + i;
-                    base += __shfl(incl - mine, i, kWave);
+                    base += lane_value(incl - mine, i);
                     break;
                 }
-                base += __shfl(incl, kWave - 1, kWave);
+                base += lane_value(incl, kWave - 1);
             }
-            base = uniform64(base);
-            b = uniform(b);
         }
         s = seq_of<PAGED>(a, b);
         const Load l = load(a, s);
@@ -352,12 +343,13 @@ struct Deal {
         if (chunk == kWhole) {
             const int32_t heads = a.kv_heads % static_cast<int>(kXcds) == 0 ? static_cast<int>(kXcds) : a.kv_heads;
             const int64_t band = static_cast<int64_t>(l.tiles) * heads;
-            const int32_t at = static_cast<int32_t>(rest / band);
+            const int32_t at = static_cast<int32_t>(quotient(rest, band));
             rest -= at * band;
-            r.j = l.tiles - 1 - static_cast<int32_t>(rest / heads);
-            r.head = at * heads + static_cast<int32_t>(rest % heads);
+            const int32_t k = static_cast<int32_t>(quotient(rest, heads));
+            r.j = l.tiles - 1 - k;
+            r.head = at * heads + static_cast<int32_t>(rest - static_cast<int64_t>(k) * heads);
         } else {
-            r.head = static_cast<int32_t>(rest / per);
+            r.head = static_cast<int32_t>(quotient(rest, per));
             rest -= r.head * per;
             for (int32_t here; rest >= (here = reach(a, l, r.part, chunk)); ++r.part) rest -= here;
             r.j = l.tiles - 1 - static_cast<int32_t>(rest);
@@ -407,13 +399,13 @@ struct Source {
 // Start of row r's width in a [heads, rows, width] tensor of destinations, for source head `head`.
 template <bool PAGED>
 __device__ __forceinline__ int64_t row_at(const Args<PAGED> &a, const Rows &t, int b, const Seq &s, int head, int r) {
-    const int token = r / a.group, g = r - token * a.group;
-    return b * t.batch + static_cast<int64_t>(head * a.group + g) * t.head + static_cast<int64_t>(s.first + token) * t.row;
+    const int d = static_cast<int>(a.group.d), token = a.group.div(r), g = r - token * d;
+    return b * t.batch + static_cast<int64_t>(head * d + g) * t.head + static_cast<int64_t>(s.first + token) * t.row;
 }
 template <bool PAGED>
 __device__ __forceinline__ int64_t lse_at(const Args<PAGED> &a, int b, const Seq &s, int head, int r) {
-    const int token = r / a.group, g = r - token * a.group;
-    return b * a.lse_batch + (head * a.group + g) * a.lse_head + s.first + token;
+    const int d = static_cast<int>(a.group.d), token = a.group.div(r), g = r - token * d;
+    return b * a.lse_batch + (head * d + g) * a.lse_head + s.first + token;
 }
 
 // ------------------------------------------------------------------------------------------ wide tiles
@@ -1211,7 +1203,7 @@ int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k,
     a.lse_batch = rel.num_dst * rel.heads;
     a.c = scale * kLog2e;
     a.kv_heads = rel.kv_heads;
-    a.group = rel.heads / rel.kv_heads;
+    a.group = divider(rel.heads / rel.kv_heads);
     a.src = Strided{rows_of(k), rows_of(v), rel.src_len, static_cast<int32_t>(rel.num_dst),
                     static_cast<int32_t>(rel.num_src), rel.batch};
     return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto t, auto g) {
@@ -1228,7 +1220,7 @@ int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_p
     a.lse_head = num_dst;
     a.c = scale * kLog2e;
     a.kv_heads = cache.kv_heads;
-    a.group = heads / cache.kv_heads;
+    a.group = divider(heads / cache.kv_heads);
     a.src = pages_of(cache, num_dst, dst_ptr);
     return by_type(cache.dtype, cache.width, paged_thin(cache, num_dst, heads), [&](auto t, auto g) {
         return run<decltype(t), decltype(g), true>(paged_plan<decltype(g)>(cache, num_dst, heads), a, ws, stream);
