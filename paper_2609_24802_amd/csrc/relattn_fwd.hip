@@ -15,6 +15,8 @@
 //    of the same keys are neighbours (Deal), so that the row tiles of a head read them from one XCD's L2 at one time.
 // Both are found from the lengths on the device, so a captured call follows lengths that change between replays, and
 // the result depends on the sizes and lengths alone.
+#include <type_traits>
+
 #include "mfma16.hpp"
 #include "relation.hpp"
 #include "relattn.hpp"
@@ -943,12 +945,13 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
 
 // Joins the parts of the narrow item that starts in block x and ends in a later one (slot 1 of x, then slot 0 of the blocks
 // after it up to the one that holds the end): a block a row.  The time is that of a few dependent reads of lines that
-// other XCDs wrote, so 16 bytes a lane of U parts a lane are in flight in every wavefront; the sums are added
-// in a fixed order.
+// other XCDs wrote, so 16 bytes a lane of 4 or (many parts) 16 parts a lane are in flight in every wavefront; the sums
+// are added in a fixed order.
 template <class T, int D, bool PAGED>
 __global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<PAGED> a, int blocks) {
-    constexpr int BM = Thin<D>::BM, L = D / 4, PP = kWave / L, U = 8;  // L lanes a part, PP parts a wavefront's read
+    constexpr int BM = Thin<D>::BM, L = D / 4, PP = kWave / L;  // L lanes a part, PP parts a wavefront's read
     __shared__ f4 so[kWaves][kWave];
+    __shared__ float sl[kWaves][kWave];
     const int x = blockIdx.x;
     const int4 it = a.rec[2 * x + 1];
     if (it.x == 0) return;
@@ -956,44 +959,69 @@ __global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<PAGED> a, int
     const Seq s = seq_of<PAGED>(a, b);
     if (r >= s.rows - j * BM) return;
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    // 4 reads a lane in flight: the parts of up to 256 blocks at a time
     int n = 2;
-    for (int from = x + 1;; from += kWave) {
-        const int at = from + lane;
-        const uint64_t ends = __ballot(at >= blocks - 1 || a.rec[2 * at].w != 0);
-        if (ends) {
-            n = from + __builtin_ctzll(ends) - x + 1;
+    for (int from = x + 1;; from += 4 * kWave) {
+        uint64_t ends[4];
+        bool hit[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hit[i] = from + i * kWave + lane >= blocks - 1 || a.rec[2 * (from + i * kWave + lane)].w != 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ends[i] = __ballot(hit[i]);
+        int i = 0;
+        while (i < 4 && !ends[i]) ++i;
+        if (i < 4) {
+            n = from + i * kWave + __builtin_ctzll(ends[i]) - x + 1;
             break;
         }
     }
     auto state = [&](int i) { return a.part + static_cast<int64_t>(2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
     float m = -__builtin_inff(), l = 0.0f;
-    for (int i = lane; i < n; i += kWave) m = fmaxf(m, state(i)[BM * D + r]);
+    for (int i0 = lane; i0 - lane < n; i0 += 4 * kWave) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i0 + i * kWave < n ? state(i0 + i * kWave)[BM * D + r] : -__builtin_inff();
+        m = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+    }
     for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
     const float ref = m == -__builtin_inff() ? 0.0f : m;
     f4 o{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i0 = w * PP + lane / L; i0 - lane / L < n; i0 += U * kWaves * PP) {
-        f4 po[U];
-        float pm[U];
+    auto add = [&](auto u) {
+        constexpr int U = decltype(u)::value;
+        for (int i0 = w * PP + lane / L; i0 - lane / L < n; i0 += U * kWaves * PP) {
+            f4 po[U];
+            float pm[U], pl[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
-            const float *p = state(min(i0 + i * kWaves * PP, n - 1));
-            po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
-            pm[i] = p[BM * D + r];
+            for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+                const float *p = state(min(i0 + i * kWaves * PP, n - 1));
+                po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
+                pm[i] = p[BM * D + r];
+                pl[i] = p[BM * (D + 1) + r];
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (i0 + i * kWaves * PP < n) {
+                    const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
+                    o += po[i] * f;
+                    l += pl[i] * f;
+                }
         }
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-            if (i0 + i * kWaves * PP < n) o += po[i] * __builtin_amdgcn_exp2f(pm[i] - ref);
-    }
+    };
+    if (n <= 4 * kWaves * PP) add(std::integral_constant<int, 4>{});
+    else add(std::integral_constant<int, 16>{});
+    sl[w][lane] = l;
     so[w][lane] = o;
-    for (int i = lane; i < n; i += kWave) l += __builtin_amdgcn_exp2f(state(i)[BM * D + r] - ref) * state(i)[BM * (D + 1) + r];
-    for (int d = 1; d < kWave; d <<= 1) l += shfl_xor_f(l, d);
     __syncthreads();
     if (w != 0 || lane >= L) return;
     o = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    l = 0.0f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i)
 #pragma unroll
-        for (int k = 0; k < PP; ++k) o += so[i][k * L + lane];
+        for (int k = 0; k < PP; ++k) {
+            o += so[i][k * L + lane];
+            l += sl[i][k * L + lane];
+        }
     o *= l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + 4 * lane;
     *reinterpret_cast<u2 *>(yr) = u2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};

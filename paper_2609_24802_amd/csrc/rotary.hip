@@ -253,24 +253,34 @@ __device__ __forceinline__ int sequence_of(const Pages &cache, int row) {
     return b;
 }
 
-// A block a new token: slots of its keys and queries (turned) and values (copied).  The rows' loads do not wait for the
-// token's place.
+// A block takes per_block (at most 4) new tokens: slots of their keys and queries (turned) and values (copied).  A
+// wavefront finds each token's place while the slots' loads are in flight.
 template <class T>
 __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view k, tiga_view v, tiga_rotary rot, int heads,
-                                                          int kv_heads, tiga_view q, tiga_view qo, Slots sl, Slots whole) {
+                                                          int kv_heads, tiga_view q, tiga_view qo, int per_block, Slots sl,
+                                                          Slots whole, Divider per_token) {
     typedef typename T::raw raw;
+    struct Place {
+        int64_t pos;
+        int32_t page;  // -1: keys and values are not stored
+        bool own;      // the row is a sequence's
+    };
     __shared__ float c[kMaxPairs], s[kMaxPairs];
-    const int row = blockIdx.x, pairs = rot.rot / 2;
-    const int nk = kv_heads * sl.all, nv = kv_heads * whole.all, items = nk + nv + heads * sl.all;
+    __shared__ Place places[4];
+    const int row0 = blockIdx.x * per_block, here = min(per_block, cache.num_dst - row0), pairs = rot.rot / 2;
+    const int nk = kv_heads * sl.all, nv = kv_heads * whole.all, each = nk + nv + heads * sl.all, items = here * each;
     const tiga_rotary plain{nullptr, 0, TIGA_PAIRS_ADJACENT, 1.0f};
     Move<T> m[kSteps];
-    int kind[kSteps];  // 0 keys, 1 values, 2 queries
+    int kind[kSteps], token[kSteps];  // 0 keys, 1 values, 2 queries
     int64_t off[kSteps];
     auto fetch_all = [&](int i0) {
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-            const int i = i0 + j * kThreads;
             m[j].slot = -1;
+            if (i0 + j * kThreads >= items) continue;
+            token[j] = per_token.div(i0 + j * kThreads);
+            const int i = i0 + j * kThreads - token[j] * each;
+            const int64_t row = row0 + token[j];
             if (i < nk) {
                 const int h = sl.div.div(i);
                 kind[j] = 0;
@@ -282,42 +292,56 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view
                 off[j] = h * cache.v.head;
                 fetch<T>(m[j], static_cast<const raw *>(v.data) + row * v.row + h * v.head, nullptr, plain, whole,
                          i - nk - h * whole.all);
-            } else if (i < items) {
+            } else {
                 const int h = sl.div.div(i - nk - nv);
                 kind[j] = 2;
-                off[j] = h * qo.head;
+                off[j] = h * qo.head + row * qo.row;
                 fetch<T>(m[j], static_cast<const raw *>(q.data) + row * q.row + h * q.head, nullptr, rot, sl,
                          i - nk - nv - h * sl.all);
             }
         }
     };
     fetch_all(threadIdx.x);
-    const int b = sequence_of(cache, row);
-    if (b >= cache.batch) return;
-    const Chunk ch = chunk_of(cache, b);
-    if (row < ch.first || row >= ch.first + ch.count) return;
-    const int64_t pos = ch.pos0 + (row - ch.first);
-    const int32_t page = pos < 0 ? -1 : page_at(cache, b, pos);
-    const int64_t slot = pos & ((1 << cache.shift) - 1);
-    const bool turn = rot.freq && pos >= 0;
-    if (turn)
-        for (int i = threadIdx.x; i < pairs; i += kThreads) {
-            const Angle a = angle_of(pos, rot.freq[i], rot.amplitude, 1.0f);
+    const int w = static_cast<int>(threadIdx.x) / kWave;
+    if (w < here) {
+        const int row = row0 + w, b = sequence_of(cache, row);
+        Place p{-1, -1, false};
+        if (b < cache.batch) {
+            const Chunk ch = chunk_of(cache, b);
+            p.own = row >= ch.first && row < ch.first + ch.count;
+            p.pos = ch.pos0 + (row - ch.first);
+            if (p.own && p.pos >= 0) p.page = page_at(cache, b, p.pos);
+        }
+        if (lane_id() == 0) places[w] = p;
+    }
+    __syncthreads();
+    if (rot.freq)
+        for (int i = threadIdx.x; i < here * pairs; i += kThreads) {
+            const int t = i / pairs;
+            const Angle a = angle_of(places[t].pos, rot.freq[i - t * pairs], rot.amplitude, 1.0f);
             c[i] = a.c;
             s[i] = a.s;
         }
-    raw *const kp = const_cast<raw *>(cache.k.p) + page * cache.k.batch + slot * cache.k.row;
-    raw *const vp = const_cast<raw *>(cache.v.p) + page * cache.v.batch + slot * cache.v.row;
-    raw *const qp = static_cast<raw *>(qo.data) + row * qo.row;
     __syncthreads();
     for (int i0 = threadIdx.x;;) {
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-            if (m[j].slot < 0 || (kind[j] < 2 && page < 0)) continue;
-            const int e = kind[j] == 1 ? start_of(plain, whole, m[j].slot, Run<T>::N) : start_of(rot, sl, m[j].slot, Run<T>::N);
-            m[j].y = (kind[j] == 0 ? kp : kind[j] == 1 ? vp : qp) + off[j] + e;
-            if (kind[j] == 1) settle<T>(m[j], plain, whole, c, s, false);
-            else settle<T>(m[j], rot, sl, c, s, turn);
+            if (m[j].slot < 0) continue;
+            const Place p = places[token[j]];
+            if (!p.own || (kind[j] < 2 && p.page < 0)) continue;
+            if (kind[j] == 2) {
+                m[j].y = static_cast<raw *>(qo.data) + off[j];
+            } else {
+                const relattn::Rows &to = kind[j] == 0 ? cache.k : cache.v;
+                m[j].y = const_cast<raw *>(to.p) + off[j] + p.page * to.batch + (p.pos & ((1 << cache.shift) - 1)) * to.row;
+            }
+            if (kind[j] == 1) {
+                m[j].y += start_of(plain, whole, m[j].slot, Run<T>::N);
+                settle<T>(m[j], plain, whole, c, s, false);
+            } else {
+                m[j].y += start_of(rot, sl, m[j].slot, Run<T>::N);
+                settle<T>(m[j], rot, sl, c + token[j] * pairs, s + token[j] * pairs, rot.freq && p.pos >= 0);
+            }
         }
         i0 += kThreads * kSteps;
         if (i0 - static_cast<int>(threadIdx.x) >= items) break;
@@ -420,6 +444,7 @@ int rotate(int32_t batch, int32_t heads, int64_t rows, int32_t width, int dtype,
     // heads a block: all of them, fewer where the rows alone do not fill the device
     int64_t group = blocks >= wanted ? heads : ceil_div(static_cast<int64_t>(heads) * blocks, wanted);
     if (ceil_div(heads, group) > 65535) group = ceil_div(heads, 65535);
+    if (runs && group * sl.all * per_block > 0x3fffffff) group = 0x3fffffff / (sl.all * per_block);  // 32-bit slot numbers
     if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "rotary: too many rows");
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(ceil_div(heads, group)));
     auto go = [&](auto by_runs, auto by_pairs) {
@@ -445,13 +470,21 @@ int append(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, con
     const tiga_rotary none{nullptr, 0, TIGA_PAIRS_ADJACENT, 1.0f};
     const Slots sl = slots_of(rot, cache.width, 8), whole = slots_of(none, cache.width, 8);
     const bool runs = slots_fit(rot, cache.width, 8);
-    const dim3 grid(static_cast<unsigned>(num_dst));
     const int32_t q_heads = q.data ? heads : 0;
+    // tokens a block: as many as give its threads kSteps slots each, while the blocks last
+    const int64_t each = static_cast<int64_t>(cache.kv_heads) * (sl.all + whole.all) + static_cast<int64_t>(q_heads) * sl.all;
+    int64_t per_block = runs ? num_dst / (4 * static_cast<int64_t>(device_cus())) : 1;
+    if (per_block > kThreads * kSteps / each) per_block = kThreads * kSteps / each;
+    if (per_block > 4) per_block = 4;
+    if (per_block < 1) per_block = 1;
+    if (each * per_block > 0x3fffffff) return fail(TIGA_EUNSUPPORTED, "cache append: too many heads");
+    const dim3 grid(static_cast<unsigned>(ceil_div(num_dst, per_block)));
     auto go = [&](auto by_runs, auto by_pairs) {
         prof_before(stream);
         if (runs)
             hipLaunchKernelGGL(by_runs, grid, dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
-                               cache.kv_heads, q, q_out, sl, whole);
+                               cache.kv_heads, q, q_out, static_cast<int>(per_block), sl, whole,
+                               divider(static_cast<int32_t>(each)));
         else
             hipLaunchKernelGGL(by_pairs, grid, dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
                                cache.kv_heads, q, q_out, cache.width);
