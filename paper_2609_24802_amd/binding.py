@@ -921,6 +921,7 @@ class CrossAttention(torch.autograd.Function):
         return y
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         q, k, v, src_len, y, lse = ctx.saved_tensors
         want = [n for n, need in zip(("dq", "dk", "dv"), ctx.needs_input_grad) if need]
@@ -938,7 +939,11 @@ def _unreadable(t):
 
 
 def cross_attention(q, k, v, src_len: torch.Tensor | None = None, scale: float | None = None, layout: str = "bhnd"):
-    """Differentiable cross attention; see tiga_mp_attention_cross_fwd."""
+    """Differentiable cross attention; see tiga_mp_attention_cross_fwd.  Gradients once, not of gradients.
+
+    Forward and backward can be captured in a graph.  As with every differentiable function of torch, a backward
+    pass that accumulates into leaves (loss.backward()) must not be captured while an eager graph of the same leaves
+    is alive; torch.autograd.grad inside the capture has no such condition."""
     return CrossAttention.apply(q, k, v, src_len, scale, layout)
 
 
@@ -952,6 +957,7 @@ class RotaryPositions(torch.autograd.Function):
         return tiga_mp_rotary_fwd(x, pos, rot, layout)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         (pos,) = ctx.saved_tensors
         if dy.stride(-1) != 1:
@@ -960,5 +966,5 @@ class RotaryPositions(torch.autograd.Function):
 
 
 def rotary(x: torch.Tensor, pos: torch.Tensor | None, rot: Rotary, layout: str = "bhnd") -> torch.Tensor:
-    """Differentiable rotary positions; see tiga_mp_rotary_fwd."""
+    """Differentiable rotary positions; see tiga_mp_rotary_fwd.  Gradients once, not of gradients."""
     return RotaryPositions.apply(x, pos, rot, layout)
