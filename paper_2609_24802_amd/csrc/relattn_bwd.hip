@@ -4,8 +4,8 @@
 // i over the destinations of every head that shares source head j's.  Scores and weights are formed again from q, k and
 // lse; nothing of the size of the relation is stored.
 //
-// Three launches: the rows' statistics (lse in the log2 domain, delta), then dq with the rows owned and the keys
-// streamed, and dk, dv with the keys owned and the rows streamed.  The second and third are one kernel: a wavefront owns
+// Three launches: the rows' statistics (lse in the log2 domain, delta), then dk, dv with the keys owned and the rows
+// streamed, and dq with the rows owned and the keys streamed.  The second and third are one kernel: a wavefront owns
 // 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or q) and Y2 (v
 // or dy) through LDS.  Per 32 streamed rows
 //   S = Y1 X1^T, DP = Y2 X2^T   (streamed x owned, 16x16x32 MFMA, fp32)
@@ -15,6 +15,11 @@
 // a 32-deep product, and the transposing LDS reads of Y^T take the rows in that order).  dk and dv need S and DP once
 // more than a fused pass would, 14 instead of 10 operations a pair and width; the fused pass would have to add dq over
 // blocks of keys, by atomics (an order that varies) or through fp32 partial sums of S / 128 times dq's size.
+//
+// delta is taken from the forward's y, whose rounding (of itself and of the weights in it) makes an error of u |dy| |y|.
+// Over many sources that is small against ds; over a few it is not (twice the error of dq and dk at 2 to 5 sources),
+// so where the sources fit one streamed tile, delta is formed as sum_j p_ij <dy_i, v_j> in fp32 instead, by the products
+// S and DP of that tile.
 //
 // Every sum has a fixed order.  Where the owned tiles do not fill the device, the streamed axis is split, and the parts'
 // fp32 sums go to the workspace and are added by reduce_kernel.
@@ -65,6 +70,13 @@ __device__ __forceinline__ int64_t stat_at(const Args &a, int b, int kv, int32_t
 
 // ------------------------------------------------------------------------------------------ statistics
 
+// A row that saw no weight has no gradient: its weights are formed as 0.
+__device__ __forceinline__ float log2_of(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
+__device__ __forceinline__ void close_stats(const Args &a) {
+    a.lse2[a.stats] = __builtin_inff();
+    a.delta[a.stats] = 0.0f;
+}
+
 // D / 8 lanes a row, 16 bytes each.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void stats_kernel(Args a) {
@@ -72,10 +84,7 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Args a) {
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     const int64_t r = t / L;
     const int part = static_cast<int>(t % L);
-    if (t == 0) {
-        a.lse2[a.stats] = __builtin_inff();
-        a.delta[a.stats] = 0.0f;
-    }
+    if (t == 0) close_stats(a);
     if (r >= a.stats) return;  // whole rows: the lanes of a row leave together
     const int64_t i = r % a.num_dst, bh = r / a.num_dst;
     const int64_t h = bh % a.heads, b = bh / a.heads;
@@ -90,9 +99,7 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Args a) {
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) s += shfl_xor_f(s, d);
     if (part == 0) {
-        const float l = a.lse[r];
-        // a row that saw no weight has no gradient
-        a.lse2[r] = l == -__builtin_inff() ? __builtin_inff() : l * kLog2e;
+        a.lse2[r] = log2_of(a.lse[r]);
         a.delta[r] = s;
     }
 }
@@ -126,20 +133,25 @@ __device__ __forceinline__ int swizzle(int k) {
 template <int D, bool KEYS>
 constexpr int kBlocks = KEYS && D == 128 ? 1 : 2;
 
-template <class T, int D, bool KEYS>
+// What the products are formed for: dq (rows owned), dk and dv (keys owned), or delta (rows owned).
+enum Mode { kQuery, kKeys, kDelta };
+
+template <class T, int D, Mode MODE>
 struct Sums {
-    f4 a1[Geo<D>::DB][2];
-    f4 a2[KEYS ? Geo<D>::DB : 1][2];
+    f4 a1[MODE == kDelta ? 1 : Geo<D>::DB][2];
+    f4 a2[MODE == kKeys ? Geo<D>::DB : 1][2];
+    float delta[2];
 };
 
 // 32 streamed rows from `y1`, `y2` (their first row's LDS address).  dr / tr: this lane's offsets of the direct and of the
 // transposing reads.  Owned statistics (dq) are own[2] and own_delta[2], streamed ones (dk, dv) lie at st / sd.
-template <class T, int D, bool KEYS>
-__device__ __forceinline__ void chunk_step(Sums<T, D, KEYS> &acc, const u4 (&x1)[2][Geo<D>::CH],
+template <class T, int D, Mode MODE>
+__device__ __forceinline__ void chunk_step(Sums<T, D, MODE> &acc, const u4 (&x1)[2][Geo<D>::CH],
                                            const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
                                            int tr, float c, const float *own, const float *own_delta, const float *st,
                                            const float *sd, bool edge, int left, int g) {
     using G = Geo<D>;
+    constexpr bool KEYS = MODE == kKeys;
     f4 s[2][2], dp[2][2];  // [16-row block][column block]
     {
         constexpr int kReads = 4 * G::CH, kAhead = 4;
@@ -183,6 +195,7 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, KEYS> &acc, const u4 (&x1)
             for (int i = 0; i < 4; ++i) {
                 p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][qb][i], c, KEYS ? -lse2[e][i] : -own[qb]));
                 if (!KEYS && edge) p[e][i] = e * 16 + 4 * g + i < left ? p[e][i] : 0.0f;
+                if (MODE == kDelta) acc.delta[qb] += p[e][i] * dp[e][qb][i];
                 ds[e][i] = p[e][i] * (dp[e][qb][i] - (KEYS ? delta[e][i] : own_delta[qb]));
             }
         if constexpr (KEYS)
@@ -191,7 +204,7 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, KEYS> &acc, const u4 (&x1)
         db[qb] = u4{T::pack(ds[0][0], ds[0][1]), T::pack(ds[0][2], ds[0][3]), T::pack(ds[1][0], ds[1][1]),
                     T::pack(ds[1][2], ds[1][3])};
     }
-    {
+    if constexpr (MODE != kDelta) {
         constexpr int M = KEYS ? 2 : 1, kReads = M * G::DB, kAhead = 3;
         auto read = [&](int i) {
             const uint8_t *const p = (KEYS && i % 2 ? y2 : y1) + (tr ^ (32 * (i / M)));
@@ -216,12 +229,13 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, KEYS> &acc, const u4 (&x1)
     }
 }
 
-// KEYS: a block owns 128 keys of a source head and streams its rows, for dk and dv; otherwise it owns 128 rows and streams
-// the keys, for dq.  A block's pieces: (eight heads, tile, split, head), so that an XCD (every eighth block) keeps to
+// kKeys: a block owns 128 keys of a source head and streams its rows; otherwise it owns 128 rows and streams the keys.
+// A block's pieces: (eight heads, tile, split, head), so that an XCD (every eighth block) keeps to
 // one head of the eight and unequal sequences spread over the XCDs.
-template <class T, int D, bool KEYS>
-__global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(Args a, int tiles) {
+template <class T, int D, Mode MODE>
+__global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void products_kernel(Args a, int tiles) {
     using G = Geo<D>;
+    constexpr bool KEYS = MODE == kKeys;
     __shared__ __attribute__((aligned(1024))) uint8_t y1a[G::TILE], y2a[G::TILE], y1b[G::TILE], y2b[G::TILE];
     __shared__ __attribute__((aligned(256))) float sta[KEYS ? 2 * G::BN : 2], stb[KEYS ? 2 * G::BN : 2];
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
@@ -258,8 +272,13 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(
             } else {
                 p1 = a.q.p + row_at(a, a.q, b, kv, o);
                 p2 = a.dy.p + row_at(a, a.dy, b, kv, o);
-                own[qb] = a.lse2[stat_at(a, b, kv, o)];
-                own_delta[qb] = a.delta[stat_at(a, b, kv, o)];
+                const int64_t at = stat_at(a, b, kv, o);
+                if constexpr (MODE == kDelta) {
+                    own[qb] = log2_of(a.lse[at]);
+                } else {
+                    own[qb] = a.lse2[at];
+                    own_delta[qb] = a.delta[at];
+                }
             }
 #pragma unroll
             for (int ch = 0; ch < G::CH; ++ch) {
@@ -268,9 +287,10 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(
             }
         }
     }
-    Sums<T, D, KEYS> acc;
+    Sums<T, D, MODE> acc;
+    acc.delta[0] = acc.delta[1] = 0.0f;
 #pragma unroll
-    for (int d = 0; d < G::DB; ++d)
+    for (int d = 0; d < (MODE == kDelta ? 1 : G::DB); ++d)
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             acc.a1[d][qb] = f4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -325,7 +345,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(
 #pragma unroll
         for (int kc = 0; kc < G::KC; ++kc) {
             const int off = kc * 32 * G::RB;
-            chunk_step<T, D, KEYS>(acc, x1, x2, b1 + off, b2 + off, dr, tr, c, own, own_delta, stats + (KEYS ? kc * 32 : 0),
+            chunk_step<T, D, MODE>(acc, x1, x2, b1 + off, b2 + off, dr, tr, c, own, own_delta, stats + (KEYS ? kc * 32 : 0),
                                    stats + (KEYS ? G::BN + kc * 32 : 0), edge, str_n - kt * G::BN - kc * 32, g);
         }
     };
@@ -342,6 +362,19 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(
         step(kt + 1, y1b, y2b, stb);
     }
 
+    if constexpr (MODE == kDelta) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) close_stats(a);
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const float delta = column_sum(acc.delta[qb]);
+            const int32_t o = own0 + w * 32 + qb * 16 + col;
+            if (o < own_n && g == 0) {
+                a.lse2[stat_at(a, b, kv, o)] = own[qb];
+                a.delta[stat_at(a, b, kv, o)] = delta;
+            }
+        }
+        return;
+    }
     const int32_t total = KEYS ? a.num_src : a.rows;
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -351,7 +384,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(
             float *const p = a.part + ((bh * tiles + tile) * a.splits + split) * (KEYS ? 2 : 1) * kOwn * D + (o - own0) * D;
 #pragma unroll
             for (int d = 0; d < G::DB; ++d) {
-                *reinterpret_cast<f4 *>(p + d * 16 + g * 4) = acc.a1[d][qb];
+                *reinterpret_cast<f4 *>(p + d * 16 + g * 4) = acc.a1[MODE == kDelta ? 0 : d][qb];
                 if (KEYS) *reinterpret_cast<f4 *>(p + kOwn * D + d * 16 + g * 4) = acc.a2[KEYS ? d : 0][qb];
             }
             continue;
@@ -365,13 +398,13 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, KEYS>)) void products_kernel(
             uint16_t *const pv = const_cast<uint16_t *>(a.dv.p) + b * a.dv.batch + kv * a.dv.head + o * a.dv.row;
 #pragma unroll
             for (int d = 0; d < G::DB; ++d) {
-                if (a.dk.p) put(pk + d * 16 + g * 4, acc.a1[d][qb] * a.scale);
-                if (a.dv.p) put(pv + d * 16 + g * 4, acc.a2[d][qb]);
+                if (a.dk.p) put(pk + d * 16 + g * 4, acc.a1[MODE == kDelta ? 0 : d][qb] * a.scale);
+                if (a.dv.p) put(pv + d * 16 + g * 4, acc.a2[KEYS ? d : 0][qb]);
             }
         } else {
             uint16_t *const pq = const_cast<uint16_t *>(a.dq.p) + row_at(a, a.dq, b, kv, o);
 #pragma unroll
-            for (int d = 0; d < G::DB; ++d) put(pq + d * 16 + g * 4, acc.a1[d][qb] * a.scale);
+            for (int d = 0; d < G::DB; ++d) put(pq + d * 16 + g * 4, acc.a1[MODE == kDelta ? 0 : d][qb] * a.scale);
         }
     }
 }
@@ -447,8 +480,9 @@ Layout layout(const tiga_cross &rel, void *ws) {
     return l;
 }
 
-template <class T, int D, bool KEYS>
+template <class T, int D, Mode MODE>
 int products(const Plan &p, Args a, hipStream_t stream) {
+    constexpr bool KEYS = MODE == kKeys;
     const int64_t heads = static_cast<int64_t>(a.batch) * a.kv_heads, blocks = heads * p.tiles * p.splits;
     if (blocks == 0) return TIGA_OK;
     const int64_t sums = ceil_div(heads * (KEYS ? a.num_src : a.rows) * (D / 4), kThreads);
@@ -456,7 +490,7 @@ int products(const Plan &p, Args a, hipStream_t stream) {
         return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many tiles (%lld)", (long long)blocks);
     a.splits = static_cast<int32_t>(p.splits);
     if (KEYS) prof_before(stream);
-    hipLaunchKernelGGL((products_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
+    hipLaunchKernelGGL((products_kernel<T, D, MODE>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
                        static_cast<int>(p.tiles));
     if (KEYS) prof_after(stream);
     if (int rc = check_launch("cross attention backward")) return rc;
@@ -468,13 +502,17 @@ int products(const Plan &p, Args a, hipStream_t stream) {
 
 template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
-    const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * (D / 8), kThreads);
-    if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");
-    hipLaunchKernelGGL((stats_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a);
-    if (int rc = check_launch("cross attention statistics")) return rc;
+    if (a.num_src <= Geo<D>::BN && a.stats > 0) {
+        if (int rc = products<T, D, kDelta>(Plan{l.q.tiles, 1, 0}, a, stream)) return rc;
+    } else {
+        const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * (D / 8), kThreads);
+        if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");
+        hipLaunchKernelGGL((stats_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a);
+        if (int rc = check_launch("cross attention statistics")) return rc;
+    }
     if (a.dk.p || a.dv.p)
-        if (int rc = products<T, D, true>(l.kv, a, stream)) return rc;
-    if (a.dq.p) return products<T, D, false>(l.q, a, stream);
+        if (int rc = products<T, D, kKeys>(l.kv, a, stream)) return rc;
+    if (a.dq.p) return products<T, D, kQuery>(l.q, a, stream);
     return TIGA_OK;
 }
 
