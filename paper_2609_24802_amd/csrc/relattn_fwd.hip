@@ -92,6 +92,10 @@ __device__ __forceinline__ Seq seq_of(const Args<PAGED> &a, int b) {
         return Seq{0, a.src.num_dst * static_cast<int32_t>(a.group.d), n};
     }
 }
+// Sequence `lane` (uniform) of those that the lanes hold.
+__device__ __forceinline__ Seq lane_seq(const Seq &s, int lane) {
+    return Seq{__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.rows, lane), lane_value(s.keys0, lane)};
+}
 // Keys that row r of the sequence sees, at least 0.  A row past the table's end sees one position behind it, which is
 // no page: it needs no more of them to become NaN.
 template <bool PAGED>
@@ -152,10 +156,13 @@ struct Walk {
     int32_t b;
     Seq s;
     T t;
+    Seq mine;  // the lane's of the first 64 sequences
 
-    static __device__ __forceinline__ int64_t weight(const Args<PAGED> &a, int e) {
-        if (e >= a.src.batch) return 0;
-        return T::template of<PAGED>(a, seq_of<PAGED>(a, e), a.part != nullptr).total() * a.kv_heads;
+    static __device__ __forceinline__ Seq fetch(const Args<PAGED> &a, int e) {
+        return e < a.src.batch ? seq_of<PAGED>(a, e) : Seq{0, 0, 0};
+    }
+    static __device__ __forceinline__ int64_t weight(const Args<PAGED> &a, const Seq &q) {
+        return T::template of<PAGED>(a, q, a.part != nullptr).total() * a.kv_heads;
     }
     static __device__ __forceinline__ bool alike(const Args<PAGED> &a) {  // every sequence weighs the same
         if constexpr (PAGED) return false;
@@ -163,11 +170,12 @@ struct Walk {
     }
     __device__ __forceinline__ void begin(const Args<PAGED> &a, int w, int blocks) {
         const int nb = a.src.batch;
-        const int64_t first = weight(a, lane_id()), prefix = wave_prefix(first);
+        mine = fetch(a, lane_id());
+        const int64_t first = weight(a, mine), prefix = wave_prefix(first);
         int64_t all = lane_value(prefix, kWave - 1);
         if (alike(a)) all = lane_value(first, 0) * nb;
         else
-            for (int e = kWave; e < nb; e += kWave) all += lane_value(wave_prefix(weight(a, e + lane_id())), kWave - 1);
+            for (int e = kWave; e < nb; e += kWave) all += lane_value(wave_prefix(weight(a, fetch(a, e + lane_id()))), kWave - 1);
         const int64_t per = quotient(all, blocks), rem = all - per * blocks;
         u = w * per + (w < rem ? w : rem);
         end = u + per + (w < rem ? 1 : 0);
@@ -179,13 +187,13 @@ struct Walk {
             base = b * lane_value(first, 0);
         } else {
             for (int e = 0; e < nb; e += kWave) {
-                const int64_t mine = e == 0 ? first : weight(a, e + lane_id());
-                const int64_t incl = e == 0 ? prefix : wave_prefix(mine);
+                const int64_t here = e == 0 ? first : weight(a, fetch(a, e + lane_id()));
+                const int64_t incl = e == 0 ? prefix : wave_prefix(here);
                 const uint64_t past = __ballot(base + incl > u);
                 if (past) {
                     const int l = __builtin_ctzll(past);
                     b = e + l;
-                    base += lane_value(incl - mine, l);
+                    base += lane_value(incl - here, l);
                     break;
                 }
                 base += lane_value(incl, kWave - 1);
@@ -194,7 +202,7 @@ struct Walk {
         load(a);
     }
     __device__ __forceinline__ void load(const Args<PAGED> &a) {
-        s = seq_of<PAGED>(a, b);
+        s = b < kWave ? lane_seq(mine, b) : seq_of<PAGED>(a, b);
         t = T::template of<PAGED>(a, s, a.part != nullptr);
         whole = t.total();
     }
@@ -238,7 +246,7 @@ struct Walk {
 template <bool PAGED, int BM, int BN>
 struct Deal {
     struct Load {
-        int64_t keys0;
+        Seq s;
         int32_t tiles;    // row tiles of a head
         int32_t n0, n1;   // key tiles of the first and the last of them, at least 1
     };
@@ -247,7 +255,7 @@ struct Deal {
     int32_t chunk;
 
     static __device__ __forceinline__ Load load(const Args<PAGED> &a, const Seq &s) {
-        Load l{s.keys0, (s.rows + BM - 1) / BM, 1, 1};
+        Load l{s, (s.rows + BM - 1) / BM, 1, 1};
         if (s.rows > 0) {
             l.n0 = max(1, (keys_of<PAGED>(a, s, min(BM, s.rows) - 1) + BN - 1) / BN);
             l.n1 = max(1, (keys_of<PAGED>(a, s, s.rows - 1) + BN - 1) / BN);
@@ -255,7 +263,7 @@ struct Deal {
         return l;
     }
     static __device__ __forceinline__ Load load(const Args<PAGED> &a, int e) {
-        return e < a.src.batch ? load(a, seq_of<PAGED>(a, e)) : Load{0, 0, 1, 1};
+        return load(a, e < a.src.batch ? seq_of<PAGED>(a, e) : Seq{0, 0, 0});
     }
     static __device__ __forceinline__ bool alike(const Args<PAGED> &a) {
         if constexpr (PAGED) return false;
@@ -275,7 +283,7 @@ struct Deal {
     // Row tiles that see keys of chunk c: token t does if keys0 + t > c * chunk * BN.
     static __device__ __forceinline__ int32_t reach(const Args<PAGED> &a, const Load &l, int32_t c, int32_t chunk) {
         if constexpr (PAGED) {
-            const int64_t t = static_cast<int64_t>(c) * chunk * BN - l.keys0 + 1;
+            const int64_t t = static_cast<int64_t>(c) * chunk * BN - l.s.keys0 + 1;
             return c == 0 || t <= 0 ? l.tiles : l.tiles - static_cast<int32_t>(t * a.group.d / BM);
         } else {
             return l.tiles;
@@ -286,7 +294,7 @@ struct Deal {
         const int32_t n = parts(l.n1, chunk);
         if constexpr (!PAGED) return static_cast<int64_t>(n) * l.tiles;
         // the chunks below the first token's keys are whole
-        const int64_t below = l.keys0 > 0 ? static_cast<int64_t>(static_cast<uint32_t>((l.keys0 - 1) / BN) / static_cast<uint32_t>(chunk)) + 1 : 1;
+        const int64_t below = l.s.keys0 > 0 ? static_cast<int64_t>(static_cast<uint32_t>((l.s.keys0 - 1) / BN) / static_cast<uint32_t>(chunk)) + 1 : 1;
         int64_t all = min(static_cast<int64_t>(n), below) * l.tiles;
         for (int64_t c = below; c < n; ++c) all += reach(a, l, static_cast<int32_t>(c), chunk);
         return all;
@@ -294,11 +302,12 @@ struct Deal {
 
     // Chunks as small as lets all pieces run at once, but not below 4 tiles, whose work a part's 64 KB of state, written
     // and read again, are worth.
-    __device__ __forceinline__ void begin(const Args<PAGED> &a) {
+    // Returns the loads that the lanes took of the first 64 sequences.
+    __device__ __forceinline__ Load begin(const Args<PAGED> &a) {
         const Load first = load(a, lane_id());
         chunk = kWhole;
         pieces = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles); });
-        if (!a.part || pieces > a.slots) return;
+        if (!a.part || pieces > a.slots) return first;
         const int64_t work = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles) * ((l.n0 + l.n1 + 1) / 2); });
         int64_t c = max(int64_t(4), quotient(work + a.slots - 1, a.slots));
         do {
@@ -306,6 +315,7 @@ struct Deal {
             pieces = total(a, first, [&](const Load &l) { return count(a, l, chunk); });
             c += max(int64_t(1), c / 16);
         } while (pieces > a.slots);
+        return first;
     }
 
     struct Piece {
@@ -313,10 +323,9 @@ struct Deal {
         int32_t t0, t1;        // key tiles
         int32_t part, parts;   // of the item
     };
-    __device__ __forceinline__ Piece piece(const Args<PAGED> &a, int64_t p, Seq &s) const {
+    __device__ __forceinline__ Piece piece(const Args<PAGED> &a, const Load &first, int64_t p, Seq &s) const {
         int64_t base = 0;
         int b = 0;
-        const Load first = load(a, lane_id());
         if (alike(a)) {
             const int64_t per = lane_value(count(a, first, chunk), 0) * a.kv_heads;
             b = static_cast<int>(quotient(p, per));
@@ -335,7 +344,7 @@ struct Deal {
                 base += lane_value(incl, kWave - 1);
             }
         }
-        s = seq_of<PAGED>(a, b);
+        s = b < kWave ? lane_seq(first.s, b) : seq_of<PAGED>(a, b);
         const Load l = load(a, s);
         const int64_t per = count(a, l, chunk);
         Piece r;
@@ -580,7 +589,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
     Deal<PAGED, G::BM, G::BN> deal;
-    deal.begin(a);
+    typename Deal<PAGED, G::BM, G::BN>::Load lanes = deal.begin(a);
     if (a.part && threadIdx.x == 0 && deal.pieces + blockIdx.x < a.slots) a.rec[2 * (deal.pieces + blockIdx.x)] = int4{0, 0, 0, 0};
     // block b of the grid (a multiple of 8) runs on XCD b % 8
     const bool whole_items = deal.chunk == deal.kWhole;
@@ -590,7 +599,8 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
     for (int64_t i = blockIdx.x / kXcds; i < per; i += gridDim.x / kXcds) {
         const int64_t id = first + (whole_items ? i * kXcds : i);
         Seq s;
-        const typename Deal<PAGED, G::BM, G::BN>::Piece pc = deal.piece(a, id, s);
+        if (i >= gridDim.x / kXcds) lanes = deal.load(a, lane_id());  // not kept over a piece's work
+        const typename Deal<PAGED, G::BM, G::BN>::Piece pc = deal.piece(a, lanes, id, s);
         if (a.part && threadIdx.x == 0 && id < a.slots) {
             a.rec[2 * id] = pc.part == 0 && pc.parts > 1 ? int4{pc.b + 1, pc.head, pc.j, pc.parts} : int4{0, 0, 0, 0};
             a.rec[2 * id + 1] = int4{deal.chunk, 0, 0, 0};
