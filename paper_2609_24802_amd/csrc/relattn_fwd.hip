@@ -1038,11 +1038,11 @@ __global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<PAGED> a, int
     if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
 }
 
-// Joins the parts of the wide item whose first part is in slot x: a wavefront takes 4 rows at once, 16 reads in
-// flight; the parts (few) are added in order.
+// Joins the parts of the wide item whose first part is in slot x: a wavefront takes 4 rows, 16 bytes a lane, the parts in
+// order and 16 reads of accumulators in flight, rescaling into the common maximum as it goes.
 template <class T, class G, bool PAGED>
 __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<PAGED> a) {
-    constexpr int D = G::CPR * 8, BM = G::BM, E = D / kWave, RPW = 4, U = 4;
+    constexpr int D = G::CPR * 8, BM = G::BM, L = D / 4, AT = kWave / L, N = 4 / AT, U = 16 / N;
     typedef Deal<PAGED, BM, G::BN> Pieces;
     const int x = blockIdx.x;
     const int4 it = a.rec[2 * x];
@@ -1053,75 +1053,59 @@ __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<PAGED> a) {
     const typename Pieces::Load load = Pieces::load(a, s);
     const int rows = min(s.rows - j * BM, BM);
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
-    const int step = static_cast<int>(gridDim.y) * kWaves * RPW;
-    // the parts of a row tile lie the chunk's row tiles apart
-    auto state = [&](int64_t slot) { return a.part + slot * slot_floats<BM, D>(); };
-    for (int r0 = (static_cast<int>(blockIdx.y) * kWaves + w) * RPW; r0 < rows; r0 += step) {
-        int row[RPW];
-        float m[RPW], l[RPW], o[RPW][E];
+    const int r0 = (static_cast<int>(blockIdx.y) * kWaves + w) * 4;
+    if (r0 >= rows) return;
+    int row[N];  // rows r0 + 0..3: AT of them at a time
+    float m[N], l[N];
+    f4 o[N];
 #pragma unroll
-        for (int k = 0; k < RPW; ++k) {
-            row[k] = min(r0 + k, rows - 1);
-            m[k] = -__builtin_inff();
-            l[k] = 0.0f;
+    for (int k = 0; k < N; ++k) {
+        row[k] = min(r0 + k * AT + lane / L, rows - 1);
+        m[k] = -__builtin_inff();
+        l[k] = 0.0f;
+        o[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    int64_t slot = x;  // the parts of a row tile lie the chunk's row tiles apart
+    for (int c = 0; c < n; c += U) {
+        f4 po[U][N];
+        float pm[U][N], pl[U][N];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[k][e] = 0.0f;
-        }
-        // each lane finds the slots of its parts alike
-        int64_t slot = x;
-        for (int c = 0; c < n; c += kWave) {
-            int64_t mine = x;
-            for (int i = 0; i < kWave && c + i < n; ++i) {
-                if (i == lane) mine = slot;
-                slot += Pieces::reach(a, load, c + i, chunk);
+        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+            const float *p = a.part + slot * slot_floats<BM, D>();
+            if (c + i < n - 1) slot += Pieces::reach(a, load, c + i, chunk);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                pm[i][k] = p[BM * D + row[k]];
+                pl[i][k] = p[BM * (D + 1) + row[k]];
+                po[i][k] = *reinterpret_cast<const f4 *>(p + row[k] * D + 4 * (lane % L));
             }
-            if (c + lane < n)
-#pragma unroll
-                for (int k = 0; k < RPW; ++k) m[k] = fmaxf(m[k], state(mine)[BM * D + row[k]]);
         }
 #pragma unroll
-        for (int k = 0; k < RPW; ++k) {
-            for (int d = 1; d < kWave; d <<= 1) m[k] = fmaxf(m[k], shfl_xor_f(m[k], d));
-            m[k] = m[k] == -__builtin_inff() ? 0.0f : m[k];
-        }
-        slot = x;
-        for (int c = 0; c < n; c += U) {
-            float po[U][RPW][E], pm[U][RPW], pl[U][RPW];
+        for (int k = 0; k < N; ++k) {
+            float top = m[k];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
-                const float *p = state(slot);
-                if (c + i < n - 1) slot += Pieces::reach(a, load, c + i, chunk);
-#pragma unroll
-                for (int k = 0; k < RPW; ++k) {
-                    pm[i][k] = p[BM * D + row[k]];
-                    pl[i][k] = p[BM * (D + 1) + row[k]];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) po[i][k][e] = p[row[k] * D + lane * E + e];
-                }
-            }
+            for (int i = 0; i < U; ++i) top = fmaxf(top, pm[i][k]);
+            const float ref = top == -__builtin_inff() ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m[k] - ref);
+            m[k] = top;
+            l[k] *= alpha;
+            o[k] *= alpha;
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 if (c + i >= n) break;
-#pragma unroll
-                for (int k = 0; k < RPW; ++k) {
-                    const float f = __builtin_amdgcn_exp2f(pm[i][k] - m[k]);
-                    l[k] += f * pl[i][k];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[k][e] += f * po[i][k][e];
-                }
+                const float f = __builtin_amdgcn_exp2f(pm[i][k] - ref);
+                l[k] += f * pl[i][k];
+                o[k] += f * po[i][k];
             }
         }
+    }
 #pragma unroll
-        for (int k = 0; k < RPW; ++k) {
-            const int r = r0 + k;
-            if (r >= rows) break;
-            const float inv = l[k] == 0.0f ? 0.0f : 1.0f / l[k];
-            uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + lane * E;
-            if constexpr (E == 2) *reinterpret_cast<uint32_t *>(yr) = T::pack(o[k][0] * inv, o[k][1] * inv);
-            else *yr = static_cast<uint16_t>(T::pack(o[k][0] * inv, 0.0f));
-            if (a.lse && lane == 0)
-                a.lse[lse_at(a, b, s, head, j * BM + r)] = (m[k] + __log2f(l[k])) * kLn2;
-        }
+    for (int k = 0; k < N; ++k) {
+        const int r = r0 + k * AT + lane / L;
+        if (r >= rows) continue;
+        const f4 v = o[k] * (l[k] == 0.0f ? 0.0f : 1.0f / l[k]);
+        uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + 4 * (lane % L);
+        *reinterpret_cast<u2 *>(yr) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+        if (a.lse && lane % L == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (m[k] + __log2f(l[k])) * kLn2;
     }
 }
 
@@ -1214,7 +1198,7 @@ int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
         hipLaunchKernelGGL((thin_merge_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks), G::BM), dim3(kThreads), 0,
                            stream, a, static_cast<int>(p.blocks));
     else
-        hipLaunchKernelGGL((wide_merge_kernel<T, G, PAGED>), dim3(static_cast<unsigned>(p.slots), 4), dim3(kThreads), 0,
+        hipLaunchKernelGGL((wide_merge_kernel<T, G, PAGED>), dim3(static_cast<unsigned>(p.slots), G::BM / 16), dim3(kThreads), 0,
                            stream, a);
     return check_launch("attention merge");
 }
