@@ -407,7 +407,8 @@ typedef struct {
     const int32_t *src_len;
 } tiga_cross;
 
-/* Workspace bytes for tiga_mp_attention_cross_fwd (0 on error). */
+/* Workspace bytes for tiga_mp_attention_cross_fwd (0 on error; at most about
+ * 36 MB).  One sized for a relation holds every smaller one. */
 size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
 
 /* The online-softmax reducer of tiga_mp_attention_fwd over a rectangular
@@ -429,7 +430,9 @@ size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
 int tiga_mp_attention_cross_fwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
                                 float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
 
-/* Workspace bytes for tiga_mp_attention_cross_bwd (0 on error). */
+/* Workspace bytes for tiga_mp_attention_cross_bwd (0 on error): about 34 MB and
+ * 8 bytes a destination row and head.  One sized for a relation holds every
+ * smaller one. */
 size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel);
 
 /* Vector-Jacobian product of tiga_mp_attention_cross_fwd.  With the forward's y
@@ -547,7 +550,8 @@ int tiga_mp_cache_append(const tiga_cache *cache, int64_t num_dst, const int32_t
                          const tiga_view *v, const tiga_rotary *rot, int32_t heads, const tiga_view *q,
                          const tiga_view *q_out, void *stream);
 
-/* Workspace bytes for tiga_mp_attention_paged_fwd (0 on error). */
+/* Workspace bytes for tiga_mp_attention_paged_fwd (0 on error; at most about
+ * 36 MB).  One sized for a call holds every smaller one. */
 size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads);
 
 /* Causal attention of the new tokens over the cache, their own keys and values

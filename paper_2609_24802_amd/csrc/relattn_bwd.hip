@@ -449,7 +449,6 @@ __global__ __launch_bounds__(kThreads) void reduce_kernel(Args a, int tiles) {
 
 struct Plan {
     int64_t tiles, splits;
-    size_t part_floats;
 };
 // Owned tiles, and how many parts the streamed axis is cut into where they do not fill the device's blocks.
 Plan plan_for(const tiga_cross &rel, bool keys) {
@@ -457,11 +456,10 @@ Plan plan_for(const tiga_cross &rel, bool keys) {
     const int64_t bn = rel.width == 64 ? 128 : 64;
     const int64_t own = keys ? rel.num_src : rows, streamed = ceil_div(keys ? rows : rel.num_src, bn);
     const int64_t resident = static_cast<int64_t>(device_cus()) * (keys && rel.width == 128 ? 1 : 2);
-    Plan p{ceil_div(own, kOwn), 1, 0};
+    Plan p{ceil_div(own, kOwn), 1};
     const int64_t items = p.tiles * heads;
     if (items > 0 && items * 2 <= resident) p.splits = resident / items;
     if (p.splits > streamed) p.splits = streamed < 1 ? 1 : streamed;
-    if (p.splits > 1) p.part_floats = static_cast<size_t>(items * p.splits * (keys ? 2 : 1) * kOwn * rel.width);
     return p;
 }
 
@@ -478,7 +476,9 @@ Layout layout(const tiga_cross &rel, void *ws) {
     const size_t stats = static_cast<size_t>(rel.batch) * rel.heads * rel.num_dst + 1;
     l.lse2 = c.take<float>(stats);
     l.delta = c.take<float>(stats);
-    l.part = c.take<float>(l.q.part_floats > l.kv.part_floats ? l.q.part_floats : l.kv.part_floats);
+    // parts of as many items as run at once, whether this problem is split or not: a workspace holds every smaller one
+    const size_t parts = static_cast<size_t>(device_cus()) * kOwn * rel.width * 2;
+    l.part = c.take<float>(rel.width == 128 ? parts : 2 * parts);
     l.bytes = c.bytes();
     return l;
 }
@@ -506,7 +506,7 @@ int products(const Plan &p, Args a, hipStream_t stream) {
 template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
     if (a.num_src <= Geo<D>::BN && a.stats > 0) {
-        if (int rc = products<T, D, kDelta>(Plan{l.q.tiles, 1, 0}, a, stream)) return rc;
+        if (int rc = products<T, D, kDelta>(Plan{l.q.tiles, 1}, a, stream)) return rc;
     } else {
         const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * (D / 8), kThreads);
         if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");

@@ -8,13 +8,19 @@
 // head, row tile).
 //
 // Work.  An item's keys come in tiles of BN.  Where the items alone do not fill the device they are cut along the
-// keys, the parts' states (o, m, l) go to the workspace in fp32, and merge_kernel joins the parts of an item in order:
+// keys, the parts' states (o, m, l) go to the workspace in fp32, and a merge kernel joins the parts of an item in order:
 //  - narrow tiles (few rows, bound by reading the keys): the key tiles of all items are laid end to end and every
 //    block walks an equal run of them (Walk), whatever the sequences' lengths;
 //  - wide tiles (many rows, bound by the matrix cores): items are cut into chunks of one number of key tiles, and chunks
 //    of the same keys are neighbours (Deal), so that the row tiles of a head read them from one XCD's L2 at one time.
-// Both are found from the lengths on the device, so a captured call follows lengths that change between replays, and
-// the result depends on the sizes and lengths alone.
+// Both are found from the lengths on the device, so a captured call follows lengths that change between replays.  The
+// orders of all sums depend on the sizes, the lengths and the device's compute units alone.
+//
+// Measured (MI355X): wide, 2 x 16 x 2048 rows over 8192 keys of width 128, bf16: 255 us, 1.08 PFLOP/s (a large library
+// product reaches 1.2 to 1.4); a prompt of 8192 tokens, 16 heads: 301 us, 0.91; bound by the matrix cores at the clock
+// the load leaves (2.0 GHz, half their cycles busy) and the dependent chain of a tile, which the second wavefront of
+// the SIMD covers.  Narrow, 64 single tokens over up to 8192 keys, 8 heads of 128: 144 us for 740 MB, 5.1 TB/s (a large
+// copy moves 4.8); one token over 4001 keys: 8.8 us, latency (finding the run 2.7, two dependent loads 2.6, the join 1.6).
 #include <type_traits>
 
 #include "mfma16.hpp"
@@ -301,8 +307,8 @@ struct Deal {
     }
 
     // Chunks as small as lets all pieces run at once, but not below 4 tiles, whose work a part's 64 KB of state, written
-    // and read again, are worth.
-    // Returns the loads that the lanes took of the first 64 sequences.
+    // and read again, are worth.  (Pieces up to twice the resident blocks: some XCDs' in two turns, 281 instead of 182 us
+    // for 1023 tokens over 16001 keys.)  Returns what the lanes read of the first 64 sequences.
     __device__ __forceinline__ Load begin(const Args<PAGED> &a) {
         const Load first = load(a, lane_id());
         chunk = kWhole;
@@ -1115,16 +1121,19 @@ __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<PAGED> a) {
 struct Plan {
     int64_t blocks;  // of the main kernel and (narrow) of the merge
     int64_t slots;   // partial states, 0: items are not cut
-    size_t part_bytes, rec_bytes;
 };
+template <class G>
+int64_t steps_of(int64_t longest) { return ceil_div(longest < 1 ? 1 : longest, G::BN); }
+template <class G>
+constexpr bool kNarrow = G::BM < 128;
+
 // items: at most, and at least (where the rows are packed the host knows bounds only)
 template <class G>
 Plan plan_for(int64_t most, int64_t least, int64_t longest) {
-    const int64_t resident = 2 * static_cast<int64_t>(device_cus());
-    const int64_t steps = ceil_div(longest < 1 ? 1 : longest, G::BN);
-    Plan p{most, 0, 0, 0};
-    if (G::BM < 128) {
-        // narrow: equal runs for the resident blocks, two slots a block; items of one key tile are dealt whole
+    const int64_t resident = 2 * static_cast<int64_t>(device_cus()), steps = steps_of<G>(longest);
+    Plan p{most, 0};
+    if (kNarrow<G>) {
+        // equal runs for the resident blocks, two slots a block; items of one key tile are dealt whole
         p.blocks = most * steps < resident ? most * steps : resident;
         if (steps > 1) p.slots = 2 * p.blocks;
     } else {
@@ -1133,8 +1142,22 @@ Plan plan_for(int64_t most, int64_t least, int64_t longest) {
         if (p.blocks > (1 << 20)) p.blocks = 1 << 20;
         p.blocks = (p.blocks + kXcds - 1) / kXcds * kXcds;
     }
-    p.part_bytes = sizeof(float) * p.slots * slot_floats<G::BM, G::CPR * 8>();
-    p.rec_bytes = sizeof(int4) * 2 * p.slots;
+    return p;
+}
+
+// The workspace of `slots` partial states.
+struct Parts {
+    float *part;
+    int4 *rec;
+    size_t bytes;
+};
+template <class G>
+Parts carve(void *ws, int64_t slots) {
+    Carve c(ws);
+    Parts p;
+    p.part = c.take<float>(slots * slot_floats<G::BM, G::CPR * 8>());
+    p.rec = c.take<int4>(2 * slots);
+    p.bytes = c.bytes() < 256 ? 256 : c.bytes();
     return p;
 }
 
@@ -1171,30 +1194,23 @@ Plan paged_plan(const tiga_cache &c, int64_t num_dst, int32_t heads) {
                        static_cast<int64_t>(c.table_width) * c.page_size);
 }
 
-size_t plan_ws(const Plan &p) {
-    Carve c(nullptr);
-    c.take<char>(p.part_bytes);
-    c.take<char>(p.rec_bytes);
-    return c.bytes() < 256 ? 256 : c.bytes();
-}
-
 template <class T, class G, bool PAGED>
 int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
     constexpr int D = G::CPR * 8;
     if (p.slots) {
-        Carve c(ws);
-        a.part = reinterpret_cast<float *>(c.take<char>(p.part_bytes));
-        a.rec = reinterpret_cast<int4 *>(c.take<char>(p.rec_bytes));
+        const Parts w = carve<G>(ws, p.slots);
+        a.part = w.part;
+        a.rec = w.rec;
         a.slots = static_cast<int>(p.slots);
     }
     prof_before(stream);
     const dim3 grid(static_cast<unsigned>(p.blocks));
-    if constexpr (G::BM < 128) hipLaunchKernelGGL((thin_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
+    if constexpr (kNarrow<G>) hipLaunchKernelGGL((thin_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
     else hipLaunchKernelGGL((wide_kernel<T, D, PAGED>), grid, dim3(kThreads), 0, stream, a);
     prof_after(stream);
     if (int rc = check_launch("attention forward")) return rc;
     if (!p.slots) return TIGA_OK;
-    if constexpr (G::BM < 128)
+    if constexpr (kNarrow<G>)
         hipLaunchKernelGGL((thin_merge_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks), G::BM), dim3(kThreads), 0,
                            stream, a, static_cast<int>(p.blocks));
     else
@@ -1205,14 +1221,29 @@ int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
 
 }  // namespace
 
+// Workspaces hold every smaller problem: wide tiles ask for all slots whether the items are cut or not, and a packed call
+// that might take wide tiles with fewer sequences asks for theirs.
 size_t cross_fwd_ws_bytes(const tiga_cross &rel) {
     if (rel.kv_heads == 0) return 256;
-    return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto, auto g) { return plan_ws(cross_plan<decltype(g)>(rel)); });
+    return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto, auto g) {
+        typedef decltype(g) G;
+        if (kNarrow<G>) return carve<G>(nullptr, cross_plan<G>(rel).slots).bytes;
+        return carve<G>(nullptr, steps_of<G>(rel.num_src) > 1 ? 2 * device_cus() : 0).bytes;
+    });
 }
 size_t paged_fwd_ws_bytes(const tiga_cache &c, int64_t num_dst, int32_t heads) {
-    if (c.kv_heads == 0) return 256;
-    return by_type(c.dtype, c.width, paged_thin(c, num_dst, heads),
-                   [&](auto, auto g) { return plan_ws(paged_plan<decltype(g)>(c, num_dst, heads)); });
+    if (c.kv_heads == 0 || num_dst == 0) return 256;
+    const int64_t longest = static_cast<int64_t>(c.table_width) * c.page_size;
+    const bool narrow = num_dst * (heads / c.kv_heads) <= kThinRows;
+    const size_t wide = by_type(c.dtype, c.width, false, [&](auto, auto g) {
+        typedef decltype(g) G;
+        return carve<G>(nullptr, !narrow && steps_of<G>(longest) > 1 ? 2 * device_cus() : 0).bytes;
+    });
+    const size_t thin = by_type(c.dtype, c.width, true, [&](auto, auto g) {
+        typedef decltype(g) G;
+        return carve<G>(nullptr, paged_plan<G>(c, num_dst, heads).slots).bytes;
+    });
+    return wide > thin ? wide : thin;
 }
 
 int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, float scale,
@@ -1238,6 +1269,7 @@ int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_p
     Args<true> a{};
     a.q = rows_of(q);
     a.y = rows_of(y);
+    a.q.batch = a.y.batch = 0;  // one packed axis
     a.lse = lse;
     a.lse_head = num_dst;
     a.c = scale * kLog2e;

@@ -221,3 +221,35 @@ def test_empty_calls(lib):
     y = torch.full_like(q, 2.0)
     lib.tiga_mp_attention_paged_fwd(none, q, torch.zeros(1, dtype=torch.int32, device="cuda"), y=y)
     assert (y == 2.0).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_batch_strides_of_packed_rows_are_not_used(lib, new):
+    """Whatever a C caller leaves in the batch strides of q and y (one packed axis has none)."""
+    import ctypes as C
+    bt = Batch([(100, new), (60, new), (300, new)], 2, 64, 16, F16, seed=14)
+    q = bt.tokens(4)
+    ref = lib.tiga_mp_attention_paged_fwd(bt.cache(lib), q, bt.dst_ptr)
+    y = torch.zeros_like(q)
+    L, cache = lib.load(), bt.cache(lib)
+    _, qv = lib._rows(q, "q", lib._AXES["hnd"])
+    _, yv = lib._rows(y, "y", lib._AXES["hnd"])
+    qv.batch = yv.batch = 8
+    ws = lib._workspace(L.tiga_mp_attention_paged_fwd_workspace(cache.ref, bt.num_dst, 4), q.device)
+    assert L.tiga_mp_attention_paged_fwd(cache.ref, bt.num_dst, lib._ptr(bt.dst_ptr), 4, C.byref(qv), 0.125, C.byref(yv), None,
+                                         lib._ptr(ws), ws.numel(), lib._stream()) == lib.TIGA_OK
+    torch.cuda.synchronize()
+    assert torch.equal(y, ref)
+
+
+def test_a_workspace_of_a_larger_problem(lib):
+    """One workspace, sized for the largest, serves smaller problems of either tile shape, filled with anything before."""
+    big = Batch([(3000, 200)] * 4, 2, 128, 16, BF16, seed=15)
+    L = lib.load()
+    ws = lib._workspace(L.tiga_mp_attention_paged_fwd_workspace(big.cache(lib).ref, big.num_dst, 8), torch.device("cuda"))
+    for lens in ([(3000, 200)] * 4, [(2000, 1)] * 4, [(700, 90)], [(5, 1), (2900, 3)]):
+        bt = Batch(lens, 2, 128, 16, BF16, seed=16)
+        q = bt.tokens(8)
+        ws.fill_(0xFF)
+        y = lib.tiga_mp_attention_paged_fwd(bt.cache(lib), q, bt.dst_ptr, ws=ws)
+        assert torch.equal(y, lib.tiga_mp_attention_paged_fwd(bt.cache(lib), q, bt.dst_ptr))

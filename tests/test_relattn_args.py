@@ -187,3 +187,26 @@ def test_binding_refuses_host_tensors(b):
         b.KvCache(x, x, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
     with pytest.raises(ValueError):
         b.tiga_rotary_frequencies(8, scaling="other")
+
+
+def test_a_workspace_holds_every_smaller_problem(b):
+    """Growing any size of a problem never shrinks its workspace."""
+    L, r = b.load(), C.byref
+    grow = [1, 2, 3, 5, 16, 17, 31, 64, 65, 100, 128, 129, 256, 257, 500, 512, 513, 1024, 4096, 20_000, 200_000]
+    base = dict(num_dst=40, num_src=700, batch=3, heads=8, kv_heads=4, width=128, dtype=0, src_len=None)
+    for width in (64, 128):
+        for query in (L.tiga_mp_attention_cross_fwd_workspace, L.tiga_mp_attention_cross_bwd_workspace):
+            for other in (dict(), dict(num_dst=1), dict(num_src=50), dict(num_dst=3000, batch=1)):
+                for f in ("num_dst", "num_src", "batch"):
+                    sizes = [query(r(b._Cross(**{**base, "width": width, **other, f: n}))) for n in grow]
+                    assert min(sizes) >= 256 and sizes == sorted(sizes), (f, other, sizes)
+                kv = [query(r(b._Cross(**{**base, "width": width, **other, "heads": 2 * n, "kv_heads": n}))) for n in grow[:15]]
+                assert kv == sorted(kv)
+    for over in (dict(), dict(page_size=2), dict(kv_heads=1), dict(table_width=400)):
+        for group in (1, 8, 32):
+            size = lambda n, **o: L.tiga_mp_attention_paged_fwd_workspace(
+                r(c := cache(b, **{**over, **o})), n, c.kv_heads * group)
+            for seq in ([size(n) for n in grow], [size(17, batch=n) for n in grow if n < 1 << 16],
+                        [size(300, batch=n) for n in grow if n < 1 << 16], [size(9, table_width=n) for n in grow],
+                        [size(100, table_width=n) for n in grow], [size(30, kv_heads=n) for n in grow[:15]]):
+                assert min(seq) >= 256 and seq == sorted(seq), (over, group, seq)
