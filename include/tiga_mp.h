@@ -15,6 +15,11 @@
  *   - the dense all-pairs relation, which needs no edge array (Section 1).
  * Reverse mode (Section 5, vector-Jacobian products) is provided for the CSR
  * and radius relations.
+ * The online-softmax reducer (Section 5.2) also runs over the triangular and
+ * the dense relation of a sequence with itself, over the rectangular relation
+ * to another sequence (cross attention, with its vector-Jacobian product), and
+ * over a sequence's pages in a cache; rotary positions and the append to a
+ * cache feed it.
  *
  * Conventions shared by every entry point
  *   - Arrays are DEVICE pointers unless a comment says otherwise.  The caller

@@ -960,79 +960,83 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
 }
 
 // Joins the parts of the narrow item that starts in block x and ends in a later one (slot 1 of x, then slot 0 of the blocks
-// after it up to the one that holds the end): a block a row.  The time is that of a few dependent reads of lines that
-// other XCDs wrote, so 16 bytes a lane of 4 or (many parts) 16 parts a lane are in flight in every wavefront; the sums
-// are added in a fixed order.
+// after it up to the one that holds the end).  Its rows are spread over 4 blocks, a block's rows over its wavefronts (one,
+// two or four a row).  The time is that of a few dependent reads of lines that other XCDs wrote, so 16 bytes a
+// lane of 4 or (many parts) 16 parts a lane are in flight in every wavefront; the sums are added in a fixed order.
 template <class T, int D, bool PAGED>
 __global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<PAGED> a, int blocks) {
     constexpr int BM = Thin<D>::BM, L = D / 4, PP = kWave / L;  // L lanes a part, PP parts a wavefront's read
     __shared__ f4 so[kWaves][kWave];
     __shared__ float sl[kWaves][kWave];
-    const int x = blockIdx.x;
+    const int x = static_cast<int>(xcd_block());  // items start every few blocks: in every eighth, one XCD would join all
     const int4 it = a.rec[2 * x + 1];
     if (it.x == 0) return;
-    const int b = it.x - 1, head = it.y, j = it.z, r = blockIdx.y;
+    const int b = it.x - 1, head = it.y, j = it.z;
     const Seq s = seq_of<PAGED>(a, b);
-    if (r >= s.rows - j * BM) return;
+    const int rows = min(s.rows - j * BM, BM), per_block = (rows + kWaves - 1) / kWaves;
+    if (static_cast<int>(blockIdx.y) * per_block >= rows) return;
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
-    // 4 reads a lane in flight: the parts of up to 256 blocks at a time
-    int n = 2;
-    for (int from = x + 1;; from += 4 * kWave) {
-        uint64_t ends[4];
-        bool hit[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) hit[i] = from + i * kWave + lane >= blocks - 1 || a.rec[2 * (from + i * kWave + lane)].w != 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ends[i] = __ballot(hit[i]);
-        int i = 0;
-        while (i < 4 && !ends[i]) ++i;
-        if (i < 4) {
-            n = from + i * kWave + __builtin_ctzll(ends[i]) - x + 1;
-            break;
-        }
-    }
-    auto state = [&](int i) { return a.part + static_cast<int64_t>(2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
-    float m = -__builtin_inff(), l = 0.0f;
-    for (int i0 = lane; i0 - lane < n; i0 += 4 * kWave) {
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i0 + i * kWave < n ? state(i0 + i * kWave)[BM * D + r] : -__builtin_inff();
-        m = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
-    }
-    for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
-    const float ref = m == -__builtin_inff() ? 0.0f : m;
+    const int share = per_block == 1 ? 4 : (per_block == 2 ? 2 : 1);  // wavefronts a row
+    const int r = static_cast<int>(blockIdx.y) * per_block + w / share, turn = w % share;
+    const bool busy = w / share < per_block && r < rows;
+    float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
     f4 o{0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](auto u) {
-        constexpr int U = decltype(u)::value;
-        for (int i0 = w * PP + lane / L; i0 - lane / L < n; i0 += U * kWaves * PP) {
-            f4 po[U];
-            float pm[U], pl[U];
+    if (busy) {
+        // 64 records at a time, then (many parts) 256
+        auto ends_at = [&](int at) { return at >= blocks - 1 || a.rec[2 * at].w != 0; };
+        int n = 0;
+        uint64_t ends = __ballot(ends_at(x + 1 + lane));
+        if (ends) n = __builtin_ctzll(ends) + 2;
+        for (int from = x + 1 + kWave; n == 0; from += 4 * kWave) {
+            bool hit[4];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
-                const float *p = state(min(i0 + i * kWaves * PP, n - 1));
-                po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
-                pm[i] = p[BM * D + r];
-                pl[i] = p[BM * (D + 1) + r];
+            for (int i = 0; i < 4; ++i) hit[i] = ends_at(from + i * kWave + lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                ends = __ballot(hit[i]);
+                if (n == 0 && ends) n = from + i * kWave + __builtin_ctzll(ends) - x + 1;
             }
-#pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (i0 + i * kWaves * PP < n) {
-                    const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
-                    o += po[i] * f;
-                    l += pl[i] * f;
-                }
         }
-    };
-    if (n <= 4 * kWaves * PP) add(std::integral_constant<int, 4>{});
-    else add(std::integral_constant<int, 16>{});
-    sl[w][lane] = l;
+        auto state = [&](int i) { return a.part + static_cast<int64_t>(2 * (x + i) + (i == 0 ? 1 : 0)) * slot_floats<BM, D>(); };
+        for (int i0 = lane; i0 - lane < n; i0 += 4 * kWave) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = i0 + i * kWave < n ? state(i0 + i * kWave)[BM * D + r] : -__builtin_inff();
+            m = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+        }
+        for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, shfl_xor_f(m, d));
+        ref = m == -__builtin_inff() ? 0.0f : m;
+        auto add = [&](auto u) {
+            constexpr int U = decltype(u)::value;
+            for (int i0 = turn * PP + lane / L; i0 - lane / L < n; i0 += U * share * PP) {
+                f4 po[U];
+                float pm[U], pl[U];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+                    const float *p = state(min(i0 + i * share * PP, n - 1));
+                    po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
+                    pm[i] = p[BM * D + r];
+                    pl[i] = p[BM * (D + 1) + r];
+                }
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+                    if (i0 + i * share * PP < n) {
+                        const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
+                        o += po[i] * f;
+                        l += pl[i] * f;
+                    }
+            }
+        };
+        if (n <= 4 * share * PP) add(std::integral_constant<int, 4>{});
+        else add(std::integral_constant<int, 16>{});
+    }
     so[w][lane] = o;
+    sl[w][lane] = l;
     __syncthreads();
-    if (w != 0 || lane >= L) return;
+    if (!busy || turn != 0 || lane >= L) return;
     o = f4{0.0f, 0.0f, 0.0f, 0.0f};
     l = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i)
+    for (int i = w; i < w + share; ++i)
 #pragma unroll
         for (int k = 0; k < PP; ++k) {
             o += so[i][k * L + lane];
@@ -1211,7 +1215,7 @@ int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
     if (int rc = check_launch("attention forward")) return rc;
     if (!p.slots) return TIGA_OK;
     if constexpr (kNarrow<G>)
-        hipLaunchKernelGGL((thin_merge_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks), G::BM), dim3(kThreads), 0,
+        hipLaunchKernelGGL((thin_merge_kernel<T, D, PAGED>), dim3(static_cast<unsigned>(p.blocks), kWaves), dim3(kThreads), 0,
                            stream, a, static_cast<int>(p.blocks));
     else
         hipLaunchKernelGGL((wide_merge_kernel<T, G, PAGED>), dim3(static_cast<unsigned>(p.slots), G::BM / 16), dim3(kThreads), 0,
