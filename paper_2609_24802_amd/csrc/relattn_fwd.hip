@@ -35,6 +35,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kMassCap = 4096.0f;  // largest tile mass of a lane (and so weight) that keeps the reference point
+constexpr int kLeastChunk = 4;       // key tiles of a part of a wide item, at least
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -306,7 +307,7 @@ struct Deal {
         return all;
     }
 
-    // Chunks as small as lets all pieces run at once, but not below 4 tiles, whose work a part's 64 KB of state, written
+    // Chunks as small as lets all pieces run at once, but not below kLeastChunk tiles, whose work a part's 64 KB of state, written
     // and read again, are worth.  (Pieces up to twice the resident blocks: some XCDs' in two turns, 281 instead of 182 us
     // for 1023 tokens over 16001 keys.)  Returns what the lanes read of the first 64 sequences.
     __device__ __forceinline__ Load begin(const Args<PAGED> &a) {
@@ -315,7 +316,7 @@ struct Deal {
         pieces = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles); });
         if (!a.part || pieces > a.slots) return first;
         const int64_t work = total(a, first, [](const Load &l) { return static_cast<int64_t>(l.tiles) * ((l.n0 + l.n1 + 1) / 2); });
-        int64_t c = max(int64_t(4), quotient(work + a.slots - 1, a.slots));
+        int64_t c = max(int64_t(kLeastChunk), quotient(work + a.slots - 1, a.slots));
         do {
             chunk = static_cast<int32_t>(min(c, static_cast<int64_t>(kWhole)));
             pieces = total(a, first, [&](const Load &l) { return count(a, l, chunk); });
@@ -1131,9 +1132,9 @@ int64_t steps_of(int64_t longest) { return ceil_div(longest < 1 ? 1 : longest, G
 template <class G>
 constexpr bool kNarrow = G::BM < 128;
 
-// items: at most, and at least (where the rows are packed the host knows bounds only)
+// items: at most, and at least (where the rows are packed the host knows bounds only); alike: all of `longest` keys
 template <class G>
-Plan plan_for(int64_t most, int64_t least, int64_t longest) {
+Plan plan_for(int64_t most, int64_t least, int64_t longest, bool alike) {
     const int64_t resident = 2 * static_cast<int64_t>(device_cus()), steps = steps_of<G>(longest);
     Plan p{most, 0};
     if (kNarrow<G>) {
@@ -1141,7 +1142,8 @@ Plan plan_for(int64_t most, int64_t least, int64_t longest) {
         p.blocks = most * steps < resident ? most * steps : resident;
         if (steps > 1) p.slots = 2 * p.blocks;
     } else {
-        if (steps > 1 && least <= resident) p.slots = resident;
+        // cut where there are fewer items than blocks, of more than one chunk (alike: where two parts of all fit)
+        if (steps > kLeastChunk && least <= resident && !(alike && 2 * most > resident)) p.slots = resident;
         if (p.blocks < p.slots) p.blocks = p.slots;
         if (p.blocks > (1 << 20)) p.blocks = 1 << 20;
         p.blocks = (p.blocks + kXcds - 1) / kXcds * kXcds;
@@ -1165,7 +1167,10 @@ Parts carve(void *ws, int64_t slots) {
     return p;
 }
 
-// The tile shape: narrow tiles where a sequence has few rows for a source head.
+// The tile shape: narrow where a sequence has at most 16 rows for a source head (on average, where the host does not know
+// more).  Narrow against wide in us, width 128, 4 source heads: at 16 rows 35 and 34 (16 x 4096 keys), 91 and 98 (2 x
+// 100,000), 15 and 20 (1 x 4001); at 24 rows 42 and 37, 138 and 99, 16 and 20, where a narrow tile reads the keys twice.
+// Unequal sequences that fill the device uncut (64 of up to 8192 keys, 8 heads): 156 and 235 at 4 rows.
 constexpr int64_t kThinRows = 16;
 
 template <class F>
@@ -1182,7 +1187,7 @@ template <class G>
 Plan cross_plan(const tiga_cross &rel) {
     const int64_t rows = rel.num_dst * (rel.heads / rel.kv_heads);
     const int64_t items = ceil_div(rows, G::BM) * rel.batch * rel.kv_heads;
-    return plan_for<G>(items, items, rel.num_src);
+    return plan_for<G>(items, items, rel.num_src, rel.src_len == nullptr);
 }
 
 // sequences with new tokens, at most
@@ -1195,7 +1200,7 @@ template <class G>
 Plan paged_plan(const tiga_cache &c, int64_t num_dst, int32_t heads) {
     const int64_t rows = num_dst * (heads / c.kv_heads);
     return plan_for<G>((rows / G::BM + some_sequences(c, num_dst)) * c.kv_heads, rows / G::BM * c.kv_heads,
-                       static_cast<int64_t>(c.table_width) * c.page_size);
+                       static_cast<int64_t>(c.table_width) * c.page_size, false);
 }
 
 template <class T, class G, bool PAGED>
