@@ -564,7 +564,7 @@ size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t nu
  * N(b, p) = {0, ..., p}, otherwise as tiga_mp_attention_cross_fwd.  One token a
  * sequence (generation), chunks of prompts, or both mixed.
  *   q, y: [1, heads, num_dst, width] (the views' batch strides are not used);
- *   lse: fp32 [heads, num_dst] or NULL.
+ *   y may be q (same strides).  lse: fp32 [heads, num_dst] or NULL.
  * A row with a negative position gives y = 0, lse = -inf.  A row that needs a
  * position past the table or a page outside [0, num_pages) gives NaN (nothing
  * is read there).  Rows behind dst_ptr[batch] are left as they were.  A value

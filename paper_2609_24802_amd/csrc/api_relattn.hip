@@ -113,7 +113,7 @@ int check_packed(const char *what, int64_t num_dst, int32_t heads) {
 extern "C" {
 
 size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel) {
-    EntryScope scope;
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
     return check_cross(rel) ? 0 : relattn::cross_fwd_ws_bytes(*rel);
 }
 
@@ -140,7 +140,7 @@ int tiga_mp_attention_cross_fwd(const tiga_cross *rel, const tiga_view *q, const
 }
 
 size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel) {
-    EntryScope scope;
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
     return check_cross(rel) ? 0 : relattn::cross_bwd_ws_bytes(*rel);
 }
 
@@ -223,7 +223,7 @@ int tiga_cache_validate(const tiga_cache *cache, int64_t num_dst, const int32_t 
 }
 
 size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads) {
-    EntryScope scope;
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
     const char *what = "paged attention";
     if (check_cache(what, cache) || check_heads(what, heads, cache->kv_heads, cache->width, cache->dtype) ||
         check_packed(what, num_dst, heads))

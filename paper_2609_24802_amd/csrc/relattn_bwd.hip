@@ -497,10 +497,10 @@ int products(const Plan &p, Args a, hipStream_t stream) {
     if (blocks > 0x7fffffff || sums > 0x7fffffff)
         return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many tiles (%lld)", (long long)blocks);
     a.splits = static_cast<int32_t>(p.splits);
-    if (KEYS) prof_before(stream);
+    if (MODE != kDelta) prof_before(stream);  // the first of the two that is launched takes the armed events
     hipLaunchKernelGGL((products_kernel<T, D, MODE>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
                        static_cast<int>(p.tiles));
-    if (KEYS) prof_after(stream);
+    if (MODE != kDelta) prof_after(stream);
     if (int rc = check_launch("cross attention backward")) return rc;
     if (p.splits == 1) return TIGA_OK;
     hipLaunchKernelGGL((reduce_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(sums)), dim3(kThreads), 0, stream, a,

@@ -123,3 +123,43 @@ def test_captured_training_step(lib):
         ref = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, ref))
+
+
+@pytest.mark.parametrize("lens", [[(700, 1), (33, 1)], [(900, 300), (40, 2)], [(2500, 900)] * 9])
+def test_output_in_the_place_of_the_queries(lib, lens):
+    bt = Batch(lens, 2, 64, 16, F16, seed=48)
+    q = bt.tokens(8)
+    ref = lib.tiga_mp_attention_paged_fwd(bt.cache(lib), q, bt.dst_ptr)
+    assert lib.tiga_mp_attention_paged_fwd(bt.cache(lib), q, bt.dst_ptr, y=q) is q
+    torch.cuda.synchronize()
+    assert torch.equal(q, ref)
+
+
+def test_kernel_events(lib):
+    """An armed pair of events is recorded around one kernel of every entry point, and by that call alone."""
+    q, k, v, dy = make(2, 4, 2, 100, 300, 64, F16, seed=49)
+    y, lse = lib.tiga_mp_attention_cross_fwd(q, k, v, want_lse=True)
+    bt = Batch([(300, 1), (90, 5)], 2, 64, 16, F16, seed=50)
+    rot = lib.Rotary(lib.tiga_rotary_frequencies(64).cuda())
+    few = make(1, 2, 2, 50, 20, 64, F16, seed=51)
+    fy, fl = lib.tiga_mp_attention_cross_fwd(*few[:3], want_lse=True)
+    calls = [lambda: lib.tiga_mp_attention_cross_fwd(q, k, v), lambda: lib.tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy),
+             lambda: lib.tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy, want=("dq",)),
+             lambda: lib.tiga_mp_attention_cross_bwd(*few[:3], fy, fl, few[3], want=("dq",)),
+             lambda: lib.tiga_mp_attention_paged_fwd(bt.cache(lib), bt.tokens(4), bt.dst_ptr),
+             lambda: lib.tiga_mp_rotary_fwd(q, None, rot), lambda: lib.tiga_mp_rotary_bwd(q, None, rot),
+             lambda: lib.tiga_mp_cache_append(bt.cache(lib), bt.tokens(2), bt.tokens(2), bt.dst_ptr, rot)]
+    for call in calls:
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        stop.record()
+        torch.cuda.synchronize()
+        before = start.elapsed_time(stop)
+        lib.tiga_mp_set_kernel_events(start, stop)
+        call()
+        torch.cuda.synchronize()
+        took = start.elapsed_time(stop)
+        assert took > 0 and took != before
+        call()
+        torch.cuda.synchronize()
+        assert start.elapsed_time(stop) == took
