@@ -21,8 +21,8 @@
 // so where the sources fit one streamed tile, delta is formed as sum_j p_ij <dy_i, v_j> in fp32 instead, by the products
 // S and DP of that tile.
 //
-// Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 566 us (0.97 PFLOP/s), dq
-// 416 us (0.99), statistics 8; 4 x 16 x 4096 x 4096 x 64: 507 us (1.08) and 436 us (0.95).  A large library product
+// Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 571 us (0.96 PFLOP/s), dq
+// 333 us (1.24), statistics 8; 4 x 16 x 4096 x 4096 x 64: 507 us (1.08) and 399 us (1.03).  A large library product
 // reaches 1.2 to 1.4.  Bound by the matrix cores at the clock the load leaves and by LDS reads: each operand read feeds
 // two products, 128 bytes a cycle and compute unit at full matrix rate, which is all that LDS delivers.
 //
@@ -200,9 +200,21 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, MODE> &acc, const u4 (&x1)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i)
                 p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][qb][i], c, KEYS ? -lse2[e][i] : -own[qb]));
-                if (!KEYS && edge) p[e][i] = e * 16 + 4 * g + i < left ? p[e][i] : 0.0f;
+        if (!KEYS && edge) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[e][i] = e * 16 + 4 * g + i < left ? p[e][i] : 0.0f;
+                    __asm__ volatile("" : "+v"(p[e][i]));  // a branch: selects in every tile take a tenth of the time
+                }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
                 if (MODE == kDelta) acc.delta[qb] += p[e][i] * dp[e][qb][i];
                 ds[e][i] = p[e][i] * (dp[e][qb][i] - (KEYS ? delta[e][i] : own_delta[qb]));
             }
@@ -320,21 +332,23 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
     const uint16_t *const kb = a.k.p + b * a.k.batch + kv * a.k.head, *const vb = a.v.p + b * a.v.batch + kv * a.v.head;
     auto stage = [&](int kt, uint8_t *b1, uint8_t *b2, float *stats) {
         const int32_t k0 = kt * G::BN;
-        const uint16_t *const kt0 = kb + k0 * a.k.row, *const vt0 = vb + k0 * a.v.row;
+        const uint8_t *const kt0 = reinterpret_cast<const uint8_t *>(kb + k0 * a.k.row);
+        const uint8_t *const vt0 = reinterpret_cast<const uint8_t *>(vb + k0 * a.v.row);
 #pragma unroll
         for (int r = 0; r < G::LPW; ++r) {
             const int run = (w * G::LPW + r) * 1024;
             const int32_t i = min(k0 + krow[r], str_n - 1);  // past the end: the last row again, without weight
-            const uint16_t *p1, *p2;
+            const uint8_t *p1, *p2;
             if constexpr (KEYS) {
-                p1 = a.q.p + row_at(a, a.q, b, kv, i);
-                p2 = a.dy.p + row_at(a, a.dy, b, kv, i);
+                p1 = reinterpret_cast<const uint8_t *>(a.q.p + row_at(a, a.q, b, kv, i) + 8 * kch[r]);
+                p2 = reinterpret_cast<const uint8_t *>(a.dy.p + row_at(a, a.dy, b, kv, i) + 8 * kch[r]);
             } else {
-                p1 = kt0 + (i - k0) * static_cast<int32_t>(a.k.row);
-                p2 = vt0 + (i - k0) * static_cast<int32_t>(a.v.row);
+                // a uniform base and 32-bit offsets in bytes (row strides are below 2^23): 64-bit ones a lane spill
+                p1 = kt0 + (2u * static_cast<uint32_t>(i - k0) * static_cast<uint32_t>(a.k.row) + 16u * kch[r]);
+                p2 = vt0 + (2u * static_cast<uint32_t>(i - k0) * static_cast<uint32_t>(a.v.row) + 16u * kch[r]);
             }
-            load_to_lds16(p1 + 8 * kch[r], b1 + run);
-            load_to_lds16(p2 + 8 * kch[r], b2 + run);
+            load_to_lds16(p1, b1 + run);
+            load_to_lds16(p2, b2 + run);
         }
         if constexpr (KEYS) {
             // 64 lanes, 4 bytes each: the first half of the needed wavefronts takes lse2, the other delta
@@ -358,16 +372,22 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
         }
     };
     if (t0 < t1) stage(t0, y1a, y2a, sta);
-    for (int kt = t0; kt < t1; kt += 2) {
+    int kt = t0;
+    // one exit, after a whole turn of both buffers: with another between them the sums are moved and spill
+    for (; MODE != kDelta && kt + 1 < t1; kt += 2) {  // delta: one tile
         loads_arrived();
         __syncthreads();
-        if (kt + 1 < t1) stage(kt + 1, y1b, y2b, stb);
+        stage(kt + 1, y1b, y2b, stb);
         step(kt, y1a, y2a, sta);
-        if (kt + 1 >= t1) break;
         loads_arrived();
         __syncthreads();
         if (kt + 2 < t1) stage(kt + 2, y1a, y2a, sta);
         step(kt + 1, y1b, y2b, stb);
+    }
+    if (kt < t1) {
+        loads_arrived();
+        __syncthreads();
+        step(kt, y1a, y2a, sta);
     }
 
     if constexpr (MODE == kDelta) {
