@@ -21,8 +21,8 @@
 // so where the sources fit one streamed tile, delta is formed as sum_j p_ij <dy_i, v_j> in fp32 instead, by the products
 // S and DP of that tile.
 //
-// Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 571 us (0.96 PFLOP/s), dq
-// 333 us (1.24), statistics 8; 4 x 16 x 4096 x 4096 x 64: 507 us (1.08) and 399 us (1.03).  A large library product
+// Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 494 us (1.11 PFLOP/s), dq
+// 333 us (1.24), statistics 8; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 400 us (1.03).  A large library product
 // reaches 1.2 to 1.4.  Bound by the matrix cores at the clock the load leaves and by LDS reads: each operand read feeds
 // two products, 128 bytes a cycle and compute unit at full matrix rate, which is all that LDS delivers.
 //
@@ -151,21 +151,20 @@ struct Sums {
     float delta[2];
 };
 
-// 32 streamed rows from `y1`, `y2` (their first row's LDS address).  dr / tr: this lane's offsets of the direct and of the
-// transposing reads.  Owned statistics (dq) are own[2] and own_delta[2], streamed ones (dk, dv) lie at st / sd.
-template <class T, int D, Mode MODE>
-__device__ __forceinline__ void chunk_step(Sums<T, D, MODE> &acc, const u4 (&x1)[2][Geo<D>::CH],
-                                           const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
-                                           int tr, float c, const float *own, const float *own_delta, const float *st,
-                                           const float *sd, bool edge, int left, int g) {
-    using G = Geo<D>;
-    constexpr bool KEYS = MODE == kKeys;
-    f4 s[2][2], dp[2][2];  // [16-row block][column block]
-    {
-        constexpr int kReads = 4 * G::CH, kAhead = 4;
+// The 32 streamed rows at `y1`, `y2` (their first row's LDS address) against the owned columns: S and DP as
+// [16-row block][column block].  dr: this lane's offset of the direct reads, which run kAhead ahead of their products.
+// between(i) is what the vector unit does under the products of read i.
+template <class T, int D>
+struct Scores {
+    static constexpr int kReads = 4 * Geo<D>::CH;
+    f4 s[2][2], dp[2][2];
+    template <class Between>
+    __device__ __forceinline__ void form(const u4 (&x1)[2][Geo<D>::CH], const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1,
+                                         const uint8_t *y2, int dr, Between between) {
+        constexpr int kAhead = 4;
         auto read = [&](int i) {
             const uint8_t *const p = (i / 2) % 2 ? y2 : y1;
-            return *reinterpret_cast<const u4 *>(p + (dr ^ (64 * (i / 4))) + i % 2 * 16 * G::RB);
+            return *reinterpret_cast<const u4 *>(p + (dr ^ (64 * (i / 4))) + i % 2 * 16 * Geo<D>::RB);
         };
         u4 w[kAhead];
 #pragma unroll
@@ -182,27 +181,60 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, MODE> &acc, const u4 (&x1)
                     dp[e][qb] = T::mma(w[i % kAhead], x2[qb][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : dp[e][qb]);
             }
             if (i + kAhead < kReads) w[i % kAhead] = read(i + kAhead);
+            between(i);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    u4 pb[2], db[2];
-    f4 lse2[2], delta[2];
-    if constexpr (KEYS) {
+};
+
+// acc1 += Y1^T DS, acc2 += Y2^T P (dk, dv only) of 32 streamed rows.  tr: this lane's offset of the transposing reads.
+template <class T, int D, Mode MODE>
+constexpr int kSumReads = (MODE == kKeys ? 2 : 1) * Geo<D>::DB;
+template <class T, int D, Mode MODE, class Between>
+__device__ __forceinline__ void add_products(Sums<T, D, MODE> &acc, const u4 (&pb)[2], const u4 (&db)[2], const uint8_t *y1,
+                                             const uint8_t *y2, int tr, Between between) {
+    constexpr bool KEYS = MODE == kKeys;
+    constexpr int M = KEYS ? 2 : 1, kReads = kSumReads<T, D, MODE>, kAhead = 3;
+    auto read = [&](int i) {
+        const uint8_t *const p = (KEYS && i % 2 ? y2 : y1) + (tr ^ (32 * (i / M)));
+        const u2 lo = lds_transposed16(p), hi = lds_transposed16(p + 16 * Geo<D>::RB);
+        return u4{lo.x, lo.y, hi.x, hi.y};
+    };
+    u4 w[kAhead];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            lse2[e] = *reinterpret_cast<const f4 *>(st + e * 16 + 4 * g);
-            delta[e] = *reinterpret_cast<const f4 *>(sd + e * 16 + 4 * g);
+    for (int i = 0; i < kAhead; ++i) w[i] = read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) {
+        const int d = i / M;
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            if (KEYS && i % 2) acc.a2[KEYS ? d : 0][qb] = T::mma(w[i % kAhead], pb[qb], acc.a2[KEYS ? d : 0][qb]);
+            else acc.a1[d][qb] = T::mma(w[i % kAhead], db[qb], acc.a1[d][qb]);
         }
+        if (i + kAhead < kReads) w[i % kAhead] = read(i + kAhead);
+        between(i);
+        __builtin_amdgcn_sched_barrier(0);
     }
+}
+
+// dq and delta, 32 streamed keys, with the rows' statistics own, own_delta.  `left` keys exist where `edge` is set.
+template <class T, int D, Mode MODE>
+__device__ __forceinline__ void keys_step(Sums<T, D, MODE> &acc, const u4 (&x1)[2][Geo<D>::CH],
+                                          const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
+                                          int tr, float c, const float *own, const float *own_delta, bool edge, int left,
+                                          int g) {
+    Scores<T, D> f;
+    f.form(x1, x2, y1, y2, dr, [](int) {});
+    u4 db[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         float p[2][4], ds[2][4];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e][qb][i], c, KEYS ? -lse2[e][i] : -own[qb]));
-        if (!KEYS && edge) {
+            for (int i = 0; i < 4; ++i) p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -own[qb]));
+        if (edge) {
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -215,38 +247,65 @@ __device__ __forceinline__ void chunk_step(Sums<T, D, MODE> &acc, const u4 (&x1)
         for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (MODE == kDelta) acc.delta[qb] += p[e][i] * dp[e][qb][i];
-                ds[e][i] = p[e][i] * (dp[e][qb][i] - (KEYS ? delta[e][i] : own_delta[qb]));
+                if (MODE == kDelta) acc.delta[qb] += p[e][i] * f.dp[e][qb][i];
+                ds[e][i] = p[e][i] * (f.dp[e][qb][i] - own_delta[qb]);
             }
-        if constexpr (KEYS)
-            pb[qb] = u4{T::pack(p[0][0], p[0][1]), T::pack(p[0][2], p[0][3]), T::pack(p[1][0], p[1][1]),
-                        T::pack(p[1][2], p[1][3])};
         db[qb] = u4{T::pack(ds[0][0], ds[0][1]), T::pack(ds[0][2], ds[0][3]), T::pack(ds[1][0], ds[1][1]),
                     T::pack(ds[1][2], ds[1][3])};
     }
-    if constexpr (MODE != kDelta) {
-        constexpr int M = KEYS ? 2 : 1, kReads = M * G::DB, kAhead = 3;
-        auto read = [&](int i) {
-            const uint8_t *const p = (KEYS && i % 2 ? y2 : y1) + (tr ^ (32 * (i / M)));
-            const u2 lo = lds_transposed16(p), hi = lds_transposed16(p + 16 * G::RB);
-            return u4{lo.x, lo.y, hi.x, hi.y};
-        };
-        u4 w[kAhead];
+    if constexpr (MODE != kDelta) add_products<T, D, MODE>(acc, db, db, y1, y2, tr, [](int) {});
+}
+
+// Weights P and DS of 32 streamed rows, whose statistics lie at st, sd in LDS, one of 16 elements a lane at a time.
+template <class T, int D>
+struct Weights {
+    f4 lse2[2], delta[2];
+    float p[16], ds[16];
+    uint32_t pw[8], dw[8];
+    __device__ __forceinline__ void load(const float *st, const float *sd, int g) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) w[i] = read(i);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < kReads; ++i) {
-            const int d = i / M;
-#pragma unroll
-            for (int qb = 0; qb < 2; ++qb) {
-                if (KEYS && i % 2) acc.a2[KEYS ? d : 0][qb] = T::mma(w[i % kAhead], pb[qb], acc.a2[KEYS ? d : 0][qb]);
-                else acc.a1[d][qb] = T::mma(w[i % kAhead], db[qb], acc.a1[d][qb]);
-            }
-            if (i + kAhead < kReads) w[i % kAhead] = read(i + kAhead);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < 2; ++e) {
+            lse2[e] = *reinterpret_cast<const f4 *>(st + e * 16 + 4 * g);
+            delta[e] = *reinterpret_cast<const f4 *>(sd + e * 16 + 4 * g);
         }
     }
+    __device__ __forceinline__ void form(const Scores<T, D> &f, float c, int n) {
+        const int qb = n / 8, e = n / 4 % 2, i = n % 4;
+        p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[e][i]));
+        ds[n] = p[n] * (f.dp[e][qb][i] - delta[e][i]);
+        if (n % 2) {
+            pw[n / 2] = T::pack(p[n - 1], p[n]);
+            dw[n / 2] = T::pack(ds[n - 1], ds[n]);
+        }
+    }
+};
+
+// dk and dv, 64 streamed rows as two halves.  The first half's weights are formed under the products for the second's
+// scores, the second's under the first half's sums: at width 128 a SIMD has one wavefront, and nothing else fills its
+// matrix unit meanwhile (527 us without, 494).  At width 64 two wavefronts share a SIMD: 8 x 449 rows over 1500 ragged 54.8
+// and 52.7 us, 4 x 4096 over 77 23.4 and 21.0, 4 x 4096 over 4096 507 and 525.
+template <class T, int D>
+__device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)[2][Geo<D>::CH],
+                                          const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
+                                          int tr, float c, const float *st, const float *sd, int g) {
+    constexpr int kHalf = 32 * Geo<D>::RB, kScore = 16 / Scores<T, D>::kReads, kSum = 16 / kSumReads<T, D, kKeys>;
+    Scores<T, D> f0, f1;
+    Weights<T, D> w0, w1;
+    w0.load(st, sd, g);
+    f0.form(x1, x2, y1, y2, dr, [](int) {});
+    f1.form(x1, x2, y1 + kHalf, y2 + kHalf, dr, [&](int i) {
+#pragma unroll
+        for (int n = 0; n < kScore; ++n) w0.form(f0, c, i * kScore + n);
+    });
+    w1.load(st + 32, sd + 32, g);
+    auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
+    const u4 p0[2] = {operand(w0.pw, 0), operand(w0.pw, 1)}, d0[2] = {operand(w0.dw, 0), operand(w0.dw, 1)};
+    add_products<T, D, kKeys>(acc, p0, d0, y1, y2, tr, [&](int i) {
+#pragma unroll
+        for (int n = 0; n < kSum; ++n) w1.form(f1, c, i * kSum + n);
+    });
+    const u4 p1[2] = {operand(w1.pw, 0), operand(w1.pw, 1)}, d1[2] = {operand(w1.dw, 0), operand(w1.dw, 1)};
+    add_products<T, D, kKeys>(acc, p1, d1, y1 + kHalf, y2 + kHalf, tr, [](int) {});
 }
 
 // kKeys: a block owns 128 keys of a source head and streams its rows; otherwise it owns 128 rows and streams the keys.
@@ -363,12 +422,17 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
     };
     const float c = a.scale * kLog2e;
     auto step = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *stats) {
-        const bool edge = !KEYS && (kt + 1) * G::BN > str_n;
+        const bool edge = (kt + 1) * G::BN > str_n;
+        if constexpr (KEYS) {
 #pragma unroll
-        for (int kc = 0; kc < G::KC; ++kc) {
-            const int off = kc * 32 * G::RB;
-            chunk_step<T, D, MODE>(acc, x1, x2, b1 + off, b2 + off, dr, tr, c, own, own_delta, stats + (KEYS ? kc * 32 : 0),
-                                   stats + (KEYS ? G::BN + kc * 32 : 0), edge, str_n - kt * G::BN - kc * 32, g);
+            for (int kc = 0; kc < G::KC; kc += 2)
+                rows_step<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, dr, tr, c, stats + kc * 32,
+                                stats + G::BN + kc * 32, g);
+        } else {
+#pragma unroll
+            for (int kc = 0; kc < G::KC; ++kc)
+                keys_step<T, D, MODE>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, dr, tr, c, own, own_delta,
+                                      edge, str_n - kt * G::BN - kc * 32, g);
         }
     };
     if (t0 < t1) stage(t0, y1a, y2a, sta);
