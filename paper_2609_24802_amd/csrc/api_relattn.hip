@@ -184,6 +184,7 @@ int tiga_cache_validate(const tiga_cache *cache, int64_t num_dst, const int32_t 
     const char *what = "cache validation";
     if (int rc = check_cache(what, cache)) return rc;
     if (int rc = check_packed(what, num_dst, 1)) return rc;
+    if (cache->batch == 0 || cache->kv_heads == 0) return TIGA_OK;  // as the calls, which read nothing then
     if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
     const size_t nb = cache->batch, cells = nb * cache->table_width;
     std::vector<int32_t> ptr, len, table;
@@ -353,6 +354,7 @@ int tiga_mp_cache_append(const tiga_cache *cache, int64_t num_dst, const int32_t
     if (rot)
         if (int rc = check_rotary(what, rot, cache->width)) return rc;
     if (with_q && !rot) return fail(TIGA_EINVAL, "%s: q is only taken to be rotated", what);
+    if (with_q && heads > 0 && cache->kv_heads == 0) return fail(TIGA_EINVAL, "%s: q for a cache without heads", what);
     if (cache->batch == 0 || cache->kv_heads == 0 || num_dst == 0) return TIGA_OK;
     if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
     if (int rc = check_view(what, "k", k, false, 0, 0, 0)) return rc;

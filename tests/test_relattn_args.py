@@ -176,6 +176,17 @@ def test_rotary_arguments(b):
     assert freq(kind=3, trained=0.0) == E and freq(kind=1, factor=float("nan")) == E
 
 
+def test_empty_caches(b):
+    """Without sequences or heads nothing is read, so nothing is asked for; queries of no cache are refused."""
+    L, r, none = b.load(), C.byref, b._View(None, 0, 0, 0)
+    for over in (dict(batch=0), dict(kv_heads=0), dict(batch=0, num_pages=0)):
+        c = cache(b, **{**over, "k": none, "v": none, "table": None, "length": None})
+        assert L.tiga_cache_validate(r(c), 5, None, None) == b.TIGA_OK
+        assert L.tiga_mp_cache_append(r(c), 5, None, None, None, None, 0, None, None, None) == b.TIGA_OK
+    c, v, rot = cache(b, kv_heads=0), view(b), b._Rotary(FAKE, 64, 0, 1.0)
+    assert L.tiga_mp_cache_append(r(c), 5, C.c_void_p(FAKE), r(v), r(v), r(rot), 4, r(v), r(v), None) == b.TIGA_EINVAL
+
+
 def test_binding_refuses_host_tensors(b):
     import torch
     x = torch.zeros(1, 1, 4, 64, dtype=torch.float16)
