@@ -20,7 +20,7 @@
 // product reaches 1.2 to 1.4); a prompt of 8192 tokens, 16 heads: 301 us, 0.91; bound by the matrix cores at the clock
 // the load leaves (2.0 GHz, half their cycles busy) and the dependent chain of a tile, which the second wavefront of
 // the SIMD covers.  Narrow, 64 single tokens over up to 8192 keys, 8 heads of 128: 144 us for 740 MB, 5.1 TB/s (a large
-// copy moves 4.8); one token over 4001 keys: 8.8 us, latency (finding the run 2.7, two dependent loads 2.6, the join 1.6).
+// copy moves 4.8); one token over 4001 keys: 8.2 us, latency (finding the run 2.7, two dependent loads 2.6, the join 1).
 #include <type_traits>
 
 #include "mfma16.hpp"
@@ -913,7 +913,8 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
         __syncthreads();
         float *const mine = reinterpret_cast<float *>(v0);
 #pragma unroll
-        for (int db = 0; db < G::DB; ++db) *reinterpret_cast<f4 *>(mine + col * D + db * 16 + g * 4) = st.o[db];
+        for (int db = 0; db < G::DB; ++db)  // chunk c of row r at c ^ r (16 rows in one bank cost 0.8 us)
+            *reinterpret_cast<f4 *>(mine + col * D + 4 * ((db * 4 + g) ^ col)) = st.o[db];
         if (g == 0) {
             ml[0][w][col] = st.m;
             ml[1][w][col] = lt;
@@ -935,9 +936,9 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
             for (int i = 0; i < kWaves; ++i) {
                 const float f = __builtin_amdgcn_exp2f(ml[0][i][tr] - ref);
                 l += f * ml[1][i][tr];
-                const float *p = reinterpret_cast<const float *>(v0buf + i * WAVE) + tr * D + d0;
+                const float *const p = reinterpret_cast<const float *>(v0buf + i * WAVE) + tr * D;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += f * p[e];
+                for (int e = 0; e < E; ++e) o[e] += f * p[4 * ((d0 + e) / 4 ^ tr) + e % 4];
             }
             if (whole) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
