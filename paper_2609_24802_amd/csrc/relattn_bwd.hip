@@ -19,7 +19,7 @@
 // delta is taken from the forward's y, whose rounding (of itself and of the weights in it) makes an error of u |dy| |y|.
 // Over many sources that is small against ds; over a few it is not (twice the error of dq and dk at 2 to 5 sources),
 // so where the sources fit one streamed tile, delta is formed as sum_j p_ij <dy_i, v_j> in fp32 instead, by the products
-// S and DP of that tile.
+// S and DP of that tile, in one launch with dq, which takes the same products (and comes first then).
 //
 // Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 494 us (1.11 PFLOP/s), dq
 // 333 us (1.24), statistics 8; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 400 us (1.03).  A large library product
@@ -141,14 +141,13 @@ __device__ __forceinline__ int swizzle(int k) {
 template <int D, bool KEYS>
 constexpr int kBlocks = KEYS && D == 128 ? 1 : 2;
 
-// What the products are formed for: dq (rows owned), dk and dv (keys owned), or delta (rows owned).
-enum Mode { kQuery, kKeys, kDelta };
+// What the products are formed for: dq (rows owned), dk and dv (keys owned), or delta and dq over one tile of keys.
+enum Mode { kQuery, kKeys, kFew };
 
 template <class T, int D, Mode MODE>
 struct Sums {
-    f4 a1[MODE == kDelta ? 1 : Geo<D>::DB][2];
+    f4 a1[Geo<D>::DB][2];
     f4 a2[MODE == kKeys ? Geo<D>::DB : 1][2];
-    float delta[2];
 };
 
 // The 32 streamed rows at `y1`, `y2` (their first row's LDS address) against the owned columns: S and DP as
@@ -218,42 +217,43 @@ __device__ __forceinline__ void add_products(Sums<T, D, MODE> &acc, const u4 (&p
     }
 }
 
-// dq and delta, 32 streamed keys, with the rows' statistics own, own_delta.  `left` keys exist where `edge` is set.
-template <class T, int D, Mode MODE>
-__device__ __forceinline__ void keys_step(Sums<T, D, MODE> &acc, const u4 (&x1)[2][Geo<D>::CH],
-                                          const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
-                                          int tr, float c, const float *own, const float *own_delta, bool edge, int left,
-                                          int g) {
-    Scores<T, D> f;
-    f.form(x1, x2, y1, y2, dr, [](int) {});
-    u4 db[2];
+// P of 32 streamed keys in the place of their scores; `left` keys exist where `edge` is set.
+template <class T, int D>
+__device__ __forceinline__ void weigh(Scores<T, D> &f, float c, const float *lse2, bool edge, int left, int g) {
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-        float p[2][4], ds[2][4];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[e][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -own[qb]));
+            for (int i = 0; i < 4; ++i) f.s[e][qb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[qb]));
         if (edge) {
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[e][i] = e * 16 + 4 * g + i < left ? p[e][i] : 0.0f;
-                    __asm__ volatile("" : "+v"(p[e][i]));  // a branch: selects in every tile take a tenth of the time
+                    float p = e * 16 + 4 * g + i < left ? f.s[e][qb][i] : 0.0f;
+                    __asm__ volatile("" : "+v"(p));  // a branch: selects in every tile take a tenth of the time
+                    f.s[e][qb][i] = p;
                 }
         }
+    }
+}
+// dq += K^T DS of 32 streamed keys with weights f.s.
+template <class T, int D, Mode MODE>
+__device__ __forceinline__ void add_keys(Sums<T, D, MODE> &acc, const Scores<T, D> &f, const float *delta, const uint8_t *y1,
+                                         int tr) {
+    u4 db[2];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        float ds[2][4];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (MODE == kDelta) acc.delta[qb] += p[e][i] * f.dp[e][qb][i];
-                ds[e][i] = p[e][i] * (f.dp[e][qb][i] - own_delta[qb]);
-            }
+            for (int i = 0; i < 4; ++i) ds[e][i] = f.s[e][qb][i] * (f.dp[e][qb][i] - delta[qb]);
         db[qb] = u4{T::pack(ds[0][0], ds[0][1]), T::pack(ds[0][2], ds[0][3]), T::pack(ds[1][0], ds[1][1]),
                     T::pack(ds[1][2], ds[1][3])};
     }
-    if constexpr (MODE != kDelta) add_products<T, D, MODE>(acc, db, db, y1, y2, tr, [](int) {});
+    add_products<T, D, MODE>(acc, db, db, y1, y1, tr, [](int) {});
 }
 
 // Weights P and DS of 32 streamed rows, whose statistics lie at st, sd in LDS, one of 16 elements a lane at a time.
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
                 p1 = a.q.p + row_at(a, a.q, b, kv, o);
                 p2 = a.dy.p + row_at(a, a.dy, b, kv, o);
                 const int64_t at = stat_at(a, b, kv, o);
-                if constexpr (MODE == kDelta) {
+                if constexpr (MODE == kFew) {
                     own[qb] = log2_of(a.lse[at]);
                 } else {
                     own[qb] = a.lse2[at];
@@ -367,9 +367,8 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
         }
     }
     Sums<T, D, MODE> acc;
-    acc.delta[0] = acc.delta[1] = 0.0f;
 #pragma unroll
-    for (int d = 0; d < (MODE == kDelta ? 1 : G::DB); ++d)
+    for (int d = 0; d < G::DB; ++d)
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             acc.a1[d][qb] = f4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -430,42 +429,63 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
                                 stats + G::BN + kc * 32, g);
         } else {
 #pragma unroll
-            for (int kc = 0; kc < G::KC; ++kc)
-                keys_step<T, D, MODE>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, dr, tr, c, own, own_delta,
-                                      edge, str_n - kt * G::BN - kc * 32, g);
+            for (int kc = 0; kc < G::KC; ++kc) {
+                Scores<T, D> f;
+                f.form(x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, dr, [](int) {});
+                weigh<T, D>(f, c, own, edge, str_n - kt * G::BN - kc * 32, g);
+                add_keys<T, D, MODE>(acc, f, own_delta, b1 + kc * 32 * G::RB, tr);
+            }
         }
     };
     if (t0 < t1) stage(t0, y1a, y2a, sta);
-    int kt = t0;
-    // one exit, after a whole turn of both buffers: with another between them the sums are moved and spill
-    for (; MODE != kDelta && kt + 1 < t1; kt += 2) {  // delta: one tile
-        loads_arrived();
-        __syncthreads();
-        stage(kt + 1, y1b, y2b, stb);
-        step(kt, y1a, y2a, sta);
-        loads_arrived();
-        __syncthreads();
-        if (kt + 2 < t1) stage(kt + 2, y1a, y2a, sta);
-        step(kt + 1, y1b, y2b, stb);
-    }
-    if (kt < t1) {
-        loads_arrived();
-        __syncthreads();
-        step(kt, y1a, y2a, sta);
-    }
-
-    if constexpr (MODE == kDelta) {
+    if constexpr (MODE == kFew) {
+        if (t0 < t1) {
+            Scores<T, D> f[G::KC];
+            loads_arrived();
+            __syncthreads();
+#pragma unroll
+            for (int kc = 0; kc < G::KC; ++kc) {
+                f[kc].form(x1, x2, y1a + kc * 32 * G::RB, y2a + kc * 32 * G::RB, dr, [](int) {});
+                weigh<T, D>(f[kc], c, own, G::BN > str_n, str_n - kc * 32, g);
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) own_delta[qb] += f[kc].s[i / 4][qb][i % 4] * f[kc].dp[i / 4][qb][i % 4];
+            }
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb) own_delta[qb] = column_sum(own_delta[qb]);
+            if (a.dq.p)
+#pragma unroll
+                for (int kc = 0; kc < G::KC; ++kc) add_keys<T, D, MODE>(acc, f[kc], own_delta, y1a + kc * 32 * G::RB, tr);
+        }
         if (blockIdx.x == 0 && threadIdx.x == 0) close_stats(a);
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
-            const float delta = column_sum(acc.delta[qb]);
             const int32_t o = own0 + w * 32 + qb * 16 + col;
             if (o < own_n && g == 0) {
                 a.lse2[stat_at(a, b, kv, o)] = own[qb];
-                a.delta[stat_at(a, b, kv, o)] = delta;
+                a.delta[stat_at(a, b, kv, o)] = own_delta[qb];
             }
         }
-        return;
+        if (!a.dq.p) return;
+    } else {
+        int kt = t0;
+        // one exit, after a whole turn of both buffers: with another between them the sums are moved and spill
+        for (; kt + 1 < t1; kt += 2) {
+            loads_arrived();
+            __syncthreads();
+            stage(kt + 1, y1b, y2b, stb);
+            step(kt, y1a, y2a, sta);
+            loads_arrived();
+            __syncthreads();
+            if (kt + 2 < t1) stage(kt + 2, y1a, y2a, sta);
+            step(kt + 1, y1b, y2b, stb);
+        }
+        if (kt < t1) {
+            loads_arrived();
+            __syncthreads();
+            step(kt, y1a, y2a, sta);
+        }
     }
     const int32_t total = KEYS ? a.num_src : a.rows;
 #pragma unroll
@@ -476,7 +496,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
             float *const p = a.part + ((bh * tiles + tile) * a.splits + split) * (KEYS ? 2 : 1) * kOwn * D + (o - own0) * D;
 #pragma unroll
             for (int d = 0; d < G::DB; ++d) {
-                *reinterpret_cast<f4 *>(p + d * 16 + g * 4) = acc.a1[MODE == kDelta ? 0 : d][qb];
+                *reinterpret_cast<f4 *>(p + d * 16 + g * 4) = acc.a1[d][qb];
                 if (KEYS) *reinterpret_cast<f4 *>(p + kOwn * D + d * 16 + g * 4) = acc.a2[KEYS ? d : 0][qb];
             }
             continue;
@@ -490,13 +510,13 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
             uint16_t *const pv = const_cast<uint16_t *>(a.dv.p) + b * a.dv.batch + kv * a.dv.head + o * a.dv.row;
 #pragma unroll
             for (int d = 0; d < G::DB; ++d) {
-                if (a.dk.p) put(pk + d * 16 + g * 4, acc.a1[MODE == kDelta ? 0 : d][qb] * a.scale);
+                if (a.dk.p) put(pk + d * 16 + g * 4, acc.a1[d][qb] * a.scale);
                 if (a.dv.p) put(pv + d * 16 + g * 4, acc.a2[KEYS ? d : 0][qb]);
             }
         } else {
             uint16_t *const pq = const_cast<uint16_t *>(a.dq.p) + row_at(a, a.dq, b, kv, o);
 #pragma unroll
-            for (int d = 0; d < G::DB; ++d) put(pq + d * 16 + g * 4, acc.a1[MODE == kDelta ? 0 : d][qb] * a.scale);
+            for (int d = 0; d < G::DB; ++d) put(pq + d * 16 + g * 4, acc.a1[d][qb] * a.scale);
         }
     }
 }
@@ -581,10 +601,10 @@ int products(const Plan &p, Args a, hipStream_t stream) {
     if (blocks > 0x7fffffff || sums > 0x7fffffff)
         return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many tiles (%lld)", (long long)blocks);
     a.splits = static_cast<int32_t>(p.splits);
-    if (MODE != kDelta) prof_before(stream);  // the first of the two that is launched takes the armed events
+    prof_before(stream);  // the first that is launched takes the armed events
     hipLaunchKernelGGL((products_kernel<T, D, MODE>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
                        static_cast<int>(p.tiles));
-    if (MODE != kDelta) prof_after(stream);
+    prof_after(stream);
     if (int rc = check_launch("cross attention backward")) return rc;
     if (p.splits == 1) return TIGA_OK;
     hipLaunchKernelGGL((reduce_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(sums)), dim3(kThreads), 0, stream, a,
@@ -594,8 +614,9 @@ int products(const Plan &p, Args a, hipStream_t stream) {
 
 template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
-    if (a.num_src <= Geo<D>::BN && a.stats > 0) {
-        if (int rc = products<T, D, kDelta>(Plan{l.q.tiles, 1}, a, stream)) return rc;
+    const bool few = a.num_src <= Geo<D>::BN && a.stats > 0;
+    if (few) {
+        if (int rc = products<T, D, kFew>(l.q, a, stream)) return rc;  // of one tile of keys: not split
     } else {
         const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * (D / 8), kThreads);
         if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");
@@ -604,7 +625,7 @@ int launch(const Layout &l, const Args &a, hipStream_t stream) {
     }
     if (a.dk.p || a.dv.p)
         if (int rc = products<T, D, kKeys>(l.kv, a, stream)) return rc;
-    if (a.dq.p) return products<T, D, kQuery>(l.q, a, stream);
+    if (a.dq.p && !few) return products<T, D, kQuery>(l.q, a, stream);
     return TIGA_OK;
 }
 
