@@ -163,3 +163,22 @@ def test_kernel_events(lib):
         call()
         torch.cuda.synchronize()
         assert start.elapsed_time(stop) == took
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("D,S", [(64, 3), (64, 127), (64, 128), (64, 129), (128, 2), (128, 63), (128, 64), (128, 65)])
+def test_gradients_around_one_tile_of_sources(lib, D, S, dt):
+    """Up to one tile of sources delta comes with dq, from them; unequal lengths, padding never seen, any choice of gradients."""
+    q, k, v, dy = make(4, 6, 2, 75, S, D, dt, seed=60 + S)
+    lens = torch.tensor([S, 0, 1, S - 1], dtype=torch.int32, device="cuda")
+    kc, vc = k.clone(), v.clone()
+    for b, n in enumerate(lens.tolist()):
+        kc[b, :, n:], vc[b, :, n:] = 0, 0
+        k[b, :, n:], v[b, :, n:] = float("nan"), float("inf")
+    got = both(lib, q, k, v, dy, lens)
+    ref, bound = R.cross(q, kc, vc, lens, D ** -0.5, dy)
+    for name in ("lse", "y", "dv", "dq", "dk"):
+        R.assert_within(got[name], ref[name], bound[name], name)
+    for want in (("dq",), ("dk",), ("dv",), ("dq", "dv")):
+        some = lib.tiga_mp_attention_cross_bwd(q, k, v, got["y"], got["lse"], dy, lens, want=want)
+        assert list(some) == list(want) and all(torch.equal(some[n], got[n]) for n in want)
