@@ -23,8 +23,9 @@
 //
 // Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 494 us (1.11 PFLOP/s), dq
 // 333 us (1.24), statistics 8; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 400 us (1.03); 4 x 8 x 4096 rows over
-// 77 of 64: delta and dq 21 us (apart 15 and 19), dk and dv 17 and their sums 5.  A large library product reaches 1.2 to 1.4.  Bound by the matrix cores at the clock the load leaves and by LDS reads: each operand read feeds
-// two products, 128 bytes a cycle and compute unit at full matrix rate, which is all that LDS delivers.
+// 77 of 64: delta and dq 21 us (apart 15 and 19), dk and dv 17 and their sums 5.  A large library product reaches 1.2 to
+// 1.4.  Bound by the matrix cores at the clock the load leaves and by LDS reads: each operand read feeds two products,
+// 128 bytes a cycle and compute unit at full matrix rate, which is all that LDS delivers.
 //
 // Every sum has a fixed order.  Where the owned tiles do not fill the device, the streamed axis is split, and the parts'
 // fp32 sums go to the workspace and are added by reduce_kernel.
