@@ -4,9 +4,9 @@
 // i over the destinations of every head that shares source head j's.  Scores and weights are formed again from q, k and
 // lse; nothing of the size of the relation is stored.
 //
-// Three launches: the rows' statistics (lse in the log2 domain, delta), then dk, dv with the keys owned and the rows
-// streamed, and dq with the rows owned and the keys streamed.  The second and third are one kernel: a wavefront owns
-// 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or q) and Y2 (v
+// Two launches of one kernel: dq with the rows owned and the keys streamed, which also leaves the rows' statistics (lse in
+// the log2 domain, delta; a kernel of its own forms them where dq is not wanted), then dk, dv with the keys owned and the
+// rows streamed.  A wavefront owns 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or q) and Y2 (v
 // or dy) through LDS.  Per 32 streamed rows
 //   S = Y1 X1^T, DP = Y2 X2^T   (streamed x owned, 16x16x32 MFMA, fp32)
 //   P = 2^(c S - lse2), DS = P (DP - delta), rounded to the input type as the operands of the next products
@@ -22,7 +22,7 @@
 // S and DP of that tile, in one launch with dq, which takes the same products (and comes first then).
 //
 // Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 494 us (1.11 PFLOP/s), dq
-// 333 us (1.24), statistics 8; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 400 us (1.03); 4 x 8 x 4096 rows over
+// 333 us (1.24), 836 together; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 392 us (1.05); 4 x 8 x 4096 rows over
 // 77 of 64: delta and dq 21 us (apart 15 and 19), dk and dv 17 and their sums 5.  A large library product reaches 1.2 to
 // 1.4.  Bound by the matrix cores at the clock the load leaves and by LDS reads: each operand read feeds two products,
 // 128 bytes a cycle and compute unit at full matrix rate, which is all that LDS delivers.
@@ -83,28 +83,41 @@ __device__ __forceinline__ void close_stats(const Args &a) {
     a.delta[a.stats] = 0.0f;
 }
 
-// D / 8 lanes a row, 16 bytes each.
+// <dy, y> of a row, lane g of its four: 16-byte chunks g, g + 4, ...; the four lanes' sums are added g ^ 1 first, then g ^ 2.
+template <class T, int CH>
+__device__ __forceinline__ float row_product(const u4 (&dy)[CH], const uint16_t *y, int g) {
+    float s = 0.0f;
+#pragma unroll
+    for (int ch = 0; ch < CH; ++ch) {
+        const u4 x = reinterpret_cast<const u4 *>(y)[ch * 4 + g];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f2 u = T::unpack(x[e]), v = T::unpack(dy[ch][e]);
+            s = __builtin_fmaf(u.y, v.y, __builtin_fmaf(u.x, v.x, s));
+        }
+    }
+    return s;
+}
+
+// Four lanes a row.  The same bits as where dq is formed: dk and dv do not depend on whether it is.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void stats_kernel(Args a) {
-    constexpr int L = D / 8;
+    constexpr int CH = D / 32;
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t r = t / L;
-    const int part = static_cast<int>(t % L);
+    const int64_t r = t / 4;
+    const int g = static_cast<int>(t % 4);
     if (t == 0) close_stats(a);
     if (r >= a.stats) return;  // whole rows: the lanes of a row leave together
     const int64_t i = r % a.num_dst, bh = r / a.num_dst;
     const int64_t h = bh % a.heads, b = bh / a.heads;
-    const u4 y = *reinterpret_cast<const u4 *>(a.y.p + b * a.y.batch + h * a.y.head + i * a.y.row + 8 * part);
-    const u4 dy = *reinterpret_cast<const u4 *>(a.dy.p + b * a.dy.batch + h * a.dy.head + i * a.dy.row + 8 * part);
-    float s = 0.0f;
+    const u4 *const p = reinterpret_cast<const u4 *>(a.dy.p + b * a.dy.batch + h * a.dy.head + i * a.dy.row);
+    u4 dy[CH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const f2 u = T::unpack(y[e]), v = T::unpack(dy[e]);
-        s += u.x * v.x + u.y * v.y;
-    }
-#pragma unroll
-    for (int d = 1; d < L; d <<= 1) s += shfl_xor_f(s, d);
-    if (part == 0) {
+    for (int ch = 0; ch < CH; ++ch) dy[ch] = p[ch * 4 + g];
+    float s = row_product<T>(dy, a.y.p + b * a.y.batch + h * a.y.head + i * a.y.row, g);
+    s += shfl_xor_f(s, 1);
+    s += shfl_xor_f(s, 2);
+    if (g == 0) {
         a.lse2[r] = log2_of(a.lse[r]);
         a.delta[r] = s;
     }
@@ -352,21 +365,30 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
             } else {
                 p1 = a.q.p + row_at(a, a.q, b, kv, o);
                 p2 = a.dy.p + row_at(a, a.dy, b, kv, o);
-                const int64_t at = stat_at(a, b, kv, o);
-                if constexpr (MODE == kFew) {
-                    own[qb] = log2_of(a.lse[at]);
-                } else {
-                    own[qb] = a.lse2[at];
-                    own_delta[qb] = a.delta[at];
-                }
+                own[qb] = log2_of(a.lse[stat_at(a, b, kv, o)]);
             }
 #pragma unroll
             for (int ch = 0; ch < G::CH; ++ch) {
                 x1[qb][ch] = reinterpret_cast<const u4 *>(p1)[ch * 4 + g];
                 x2[qb][ch] = reinterpret_cast<const u4 *>(p2)[ch * 4 + g];
             }
+            if constexpr (MODE == kQuery)
+                own_delta[qb] = column_sum(row_product<T>(x2[qb], a.y.p + row_at(a, a.y, b, kv, o), g));
         }
     }
+    // The owned rows' statistics, for dk and dv: delta is there.
+    auto leave_stats = [&] {
+        if (blockIdx.x == 0 && threadIdx.x == 0) close_stats(a);
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const int32_t o = own0 + w * 32 + qb * 16 + col;
+            if (o < own_n && g == 0 && split == 0) {
+                a.lse2[stat_at(a, b, kv, o)] = own[qb];
+                a.delta[stat_at(a, b, kv, o)] = own_delta[qb];
+            }
+        }
+    };
+    if constexpr (MODE == kQuery) leave_stats();
     Sums<T, D, MODE> acc;
 #pragma unroll
     for (int d = 0; d < G::DB; ++d)
@@ -459,15 +481,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
 #pragma unroll
                 for (int kc = 0; kc < G::KC; ++kc) add_keys<T, D, MODE>(acc, f[kc], own_delta, y1a + kc * 32 * G::RB, tr);
         }
-        if (blockIdx.x == 0 && threadIdx.x == 0) close_stats(a);
-#pragma unroll
-        for (int qb = 0; qb < 2; ++qb) {
-            const int32_t o = own0 + w * 32 + qb * 16 + col;
-            if (o < own_n && g == 0) {
-                a.lse2[stat_at(a, b, kv, o)] = own[qb];
-                a.delta[stat_at(a, b, kv, o)] = own_delta[qb];
-            }
-        }
+        leave_stats();
         if (!a.dq.p) return;
     } else {
         int kt = t0;
@@ -594,7 +608,7 @@ Layout layout(const tiga_cross &rel, void *ws) {
 }
 
 template <class T, int D, Mode MODE>
-int products(const Plan &p, Args a, hipStream_t stream) {
+int products(const Plan &p, Args a, bool timed, hipStream_t stream) {
     constexpr bool KEYS = MODE == kKeys;
     const int64_t heads = static_cast<int64_t>(a.batch) * a.kv_heads, blocks = heads * p.tiles * p.splits;
     if (blocks == 0) return TIGA_OK;
@@ -602,10 +616,10 @@ int products(const Plan &p, Args a, hipStream_t stream) {
     if (blocks > 0x7fffffff || sums > 0x7fffffff)
         return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many tiles (%lld)", (long long)blocks);
     a.splits = static_cast<int32_t>(p.splits);
-    prof_before(stream);  // the first that is launched takes the armed events
+    if (timed) prof_before(stream);
     hipLaunchKernelGGL((products_kernel<T, D, MODE>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
                        static_cast<int>(p.tiles));
-    prof_after(stream);
+    if (timed) prof_after(stream);
     if (int rc = check_launch("cross attention backward")) return rc;
     if (p.splits == 1) return TIGA_OK;
     hipLaunchKernelGGL((reduce_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(sums)), dim3(kThreads), 0, stream, a,
@@ -615,19 +629,18 @@ int products(const Plan &p, Args a, hipStream_t stream) {
 
 template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
-    const bool few = a.num_src <= Geo<D>::BN && a.stats > 0;
-    if (few) {
-        if (int rc = products<T, D, kFew>(l.q, a, stream)) return rc;  // of one tile of keys: not split
+    const bool keys = a.dk.p || a.dv.p;
+    if (a.num_src <= Geo<D>::BN && a.stats > 0) {
+        if (int rc = products<T, D, kFew>(l.q, a, !keys, stream)) return rc;  // of one tile of keys: not split
+    } else if (a.dq.p) {
+        if (int rc = products<T, D, kQuery>(l.q, a, !keys, stream)) return rc;
     } else {
-        const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * (D / 8), kThreads);
+        const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * 4, kThreads);
         if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");
         hipLaunchKernelGGL((stats_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a);
         if (int rc = check_launch("cross attention statistics")) return rc;
     }
-    if (a.dk.p || a.dv.p)
-        if (int rc = products<T, D, kKeys>(l.kv, a, stream)) return rc;
-    if (a.dq.p && !few) return products<T, D, kQuery>(l.q, a, stream);
-    return TIGA_OK;
+    return keys ? products<T, D, kKeys>(l.kv, a, true, stream) : TIGA_OK;
 }
 
 }  // namespace
