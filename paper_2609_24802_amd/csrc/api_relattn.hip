@@ -245,6 +245,8 @@ int tiga_mp_attention_paged_fwd(const tiga_cache *cache, int64_t num_dst, const 
     if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
     if (int rc = check_view(what, "q", q, false, 0, 0, 0)) return rc;
     if (int rc = check_view(what, "y", y, true, 1, heads, num_dst)) return rc;
+    if (q->data == y->data && ((heads > 1 && q->head != y->head) || (num_dst > 1 && q->row != y->row)))
+        return fail(TIGA_EINVAL, "%s: y in the place of q needs its strides", what);
     if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(TIGA_EINVAL, "%s: lse misaligned", what);
     if (int rc = check_ws(what, ws, ws_bytes, relattn::paged_fwd_ws_bytes(*cache, num_dst, heads))) return rc;
     return relattn::paged_forward(*cache, num_dst, dst_ptr, heads, *q, scale, *y, lse, ws,
