@@ -1231,29 +1231,31 @@ int run(const Plan &p, Args<PAGED> a, void *ws, hipStream_t stream) {
 
 }  // namespace
 
-// Workspaces hold every smaller problem: wide tiles ask for all slots whether the items are cut or not, and a packed call
-// that might take wide tiles with fewer sequences asks for theirs.
-size_t cross_fwd_ws_bytes(const tiga_cross &rel) {
-    if (rel.kv_heads == 0) return 256;
-    return by_type(rel.dtype, rel.width, cross_thin(rel), [&](auto, auto g) {
-        typedef decltype(g) G;
-        if (kNarrow<G>) return carve<G>(nullptr, cross_plan<G>(rel).slots).bytes;
-        return carve<G>(nullptr, steps_of<G>(rel.num_src) > 1 ? 2 * device_cus() : 0).bytes;
-    });
-}
-size_t paged_fwd_ws_bytes(const tiga_cache &c, int64_t num_dst, int32_t heads) {
-    if (c.kv_heads == 0 || num_dst == 0) return 256;
-    const int64_t longest = static_cast<int64_t>(c.table_width) * c.page_size;
-    const bool narrow = num_dst * (heads / c.kv_heads) <= kThinRows;
-    const size_t wide = by_type(c.dtype, c.width, false, [&](auto, auto g) {
+// Workspaces hold every smaller problem. Fewer source heads at the same heads turn narrow tiles wide, and so do fewer sequences
+// of packed rows: unless all heads' rows together are few, the wide tiles' slots are asked for, whether the items are
+// cut or not.
+template <class F>
+size_t ws_bytes(int dtype, int width, int64_t rows, int64_t longest, F thin_slots) {
+    const bool narrow = rows <= kThinRows;  // of one source head if it has all heads
+    const size_t wide = by_type(dtype, width, false, [&](auto, auto g) {
         typedef decltype(g) G;
         return carve<G>(nullptr, !narrow && steps_of<G>(longest) > 1 ? 2 * device_cus() : 0).bytes;
     });
-    const size_t thin = by_type(c.dtype, c.width, true, [&](auto, auto g) {
+    const size_t thin = by_type(dtype, width, true, [&](auto, auto g) {
         typedef decltype(g) G;
-        return carve<G>(nullptr, paged_plan<G>(c, num_dst, heads).slots).bytes;
+        return carve<G>(nullptr, thin_slots(g)).bytes;
     });
     return wide > thin ? wide : thin;
+}
+size_t cross_fwd_ws_bytes(const tiga_cross &rel) {
+    if (rel.kv_heads == 0) return 256;
+    return ws_bytes(rel.dtype, rel.width, rel.num_dst * rel.heads, rel.num_src,
+                    [&](auto g) { return cross_plan<decltype(g)>(rel).slots; });
+}
+size_t paged_fwd_ws_bytes(const tiga_cache &c, int64_t num_dst, int32_t heads) {
+    if (c.kv_heads == 0 || num_dst == 0) return 256;
+    return ws_bytes(c.dtype, c.width, num_dst * heads, static_cast<int64_t>(c.table_width) * c.page_size,
+                    [&](auto g) { return paged_plan<decltype(g)>(c, num_dst, heads).slots; });
 }
 
 int cross_forward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, float scale,
