@@ -144,14 +144,20 @@ size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel) {
     return check_cross(rel) ? 0 : relattn::cross_bwd_ws_bytes(*rel);
 }
 
-int tiga_mp_attention_cross_bwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+int tiga_mp_attention_cross_bwd(const tiga_cross *given, const tiga_view *q, const tiga_view *k, const tiga_view *v,
                                 const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
                                 const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,
                                 size_t ws_bytes, void *stream) {
     EntryScope scope;
     const char *what = "cross attention backward";
-    if (int rc = check_cross(rel)) return rc;
+    if (int rc = check_cross(given)) return rc;
     if (int rc = check_scale(what, scale)) return rc;
+    tiga_cross some = *given;
+    if (some.heads == 0) {  // source heads that nothing reads: gradients of 0, as without destinations
+        some.heads = some.kv_heads;
+        some.num_dst = 0;
+    }
+    const tiga_cross *const rel = &some;
     const bool rows = rel->num_dst > 0, srcs = rel->num_src > 0;
     if (rel->batch == 0 || rel->heads == 0 || (!rows && !srcs)) return TIGA_OK;
     const tiga_view none{};
