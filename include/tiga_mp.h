@@ -545,10 +545,11 @@ int tiga_cache_validate(const tiga_cache *cache, int64_t num_dst, const int32_t 
  * q_out may be q).
  *   k, v: [1, kv_heads, num_dst, width]; q, q_out: [1, heads, num_dst, width] of
  *   the cache's dtype (the views' batch strides are not used).
- * Rows outside every sequence, and rows whose position is negative or past the
+ * Rows before dst_ptr[0], and rows whose position is negative or past the
  * table, or whose page is not in [0, num_pages), store nothing; their q is
- * copied unrotated if the row has no position and rotated otherwise.  Rows
- * behind dst_ptr[batch] are left as they were.
+ * rotated by the position where there is one, and copied unrotated where there
+ * is none (before dst_ptr[0], negative).  Rows behind dst_ptr[batch] store
+ * nothing, and their q_out is left as it was.
  * No two rows of one call may fall on the same place of a page.
  * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EDEVICE. */
 int tiga_mp_cache_append(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, const tiga_view *k,
@@ -567,7 +568,8 @@ size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t nu
  *   y may be q (same strides).  lse: fp32 [heads, num_dst] or NULL.
  * A row with a negative position gives y = 0, lse = -inf.  A row that needs a
  * position past the table or a page outside [0, num_pages) gives NaN (nothing
- * is read there).  Rows behind dst_ptr[batch] are left as they were.  A value
+ * is read there).  Rows before dst_ptr[0] and behind dst_ptr[batch] are left as
+ * they were.  A value
  * row that is not finite reaches every row of its sequence's new tokens that
  * it shares a tile with: new tokens' values must be finite.
  * Requires heads a multiple of kv_heads, width 64 or 128, num_dst * heads <

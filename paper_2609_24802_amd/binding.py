@@ -773,7 +773,8 @@ def tiga_mp_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, dst_p
     k, v: [kv_heads, rows, width] (layout "hnd"; "nhd" has rows first) of the cache's type, the new tokens
     of all sequences packed: sequence b owns rows dst_ptr[b] to dst_ptr[b + 1] (int32 [batch + 1]), its last
     row at position length[b] - 1.  With q [heads, rows, width] the queries are rotated by the same
-    positions in the same launch and returned (q_out may be q)."""
+    positions in the same launch and returned (q_out may be q).  Rows before dst_ptr[0] are returned
+    unrotated; rows behind dst_ptr[batch] are left as q_out has them (uninitialized without q_out)."""
     axes = _axes(layout, (3,))
     _, rows, kv = _new_rows(cache, k, "k", axes, cache.kv_heads)
     _, _, vv = _new_rows(cache, v, "v", axes, cache.kv_heads, rows)
@@ -803,8 +804,8 @@ def tiga_mp_attention_paged_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.
     """Causal attention of new tokens over a paged cache that already holds their own keys and values.
 
     q: [heads, rows, width] (layout "hnd"; "nhd" has rows first) packed as in tiga_mp_cache_append, heads a
-    multiple of the cache's; the row at position p reads positions 0 to p of its sequence.  Rows behind
-    dst_ptr[batch] of y are left as they were.  Returns y in q's shape (and lse fp32 [heads, rows])."""
+    multiple of the cache's; the row at position p reads positions 0 to p of its sequence.  Rows before
+    dst_ptr[0] and behind dst_ptr[batch] are left as y has them (uninitialized without y).  Returns y in q's shape (and lse fp32 [heads, rows])."""
     lib = load()
     axes = _axes(layout, (3,))
     heads, rows, qv = _new_rows(cache, q, "q", axes)

@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view
     struct Place {
         int64_t pos;
         int32_t page;  // -1: keys and values are not stored
-        bool own;      // the row is a sequence's
+        bool behind;   // the last sequence: nothing is written
     };
     __shared__ float c[kMaxPairs], s[kMaxPairs];
     __shared__ Place places[4];
@@ -307,12 +307,11 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view
     const int w = static_cast<int>(threadIdx.x) / kWave;
     if (w < here) {
         const int row = row0 + w, b = sequence_of(cache, row);
-        Place p{-1, -1, false};
-        if (b < cache.batch) {
+        Place p{-1, -1, b >= cache.batch};
+        if (!p.behind) {
             const Chunk ch = chunk_of(cache, b);
-            p.own = row >= ch.first && row < ch.first + ch.count;
-            p.pos = ch.pos0 + (row - ch.first);
-            if (p.own && p.pos >= 0) p.page = page_at(cache, b, p.pos);
+            if (row >= ch.first && row < ch.first + ch.count) p.pos = ch.pos0 + (row - ch.first);
+            if (p.pos >= 0) p.page = page_at(cache, b, p.pos);
         }
         if (lane_id() == 0) places[w] = p;
     }
@@ -330,7 +329,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view
         for (int j = 0; j < kSteps; ++j) {
             if (m[j].slot < 0) continue;
             const Place p = places[token[j]];
-            if (!p.own || (kind[j] < 2 && p.page < 0)) continue;
+            if (p.behind || (kind[j] < 2 && p.page < 0)) continue;
             if (kind[j] == 2) {
                 m[j].y = static_cast<raw *>(qo.data) + off[j];
             } else {
@@ -392,8 +391,8 @@ __global__ __launch_bounds__(kThreads) void append_pairs_kernel(Pages cache, tig
     const int b = sequence_of(cache, row);
     if (b >= cache.batch) return;
     const Chunk ch = chunk_of(cache, b);
-    if (row < ch.first || row >= ch.first + ch.count) return;
-    const int64_t pos = ch.pos0 + (row - ch.first);
+    const bool own = row >= ch.first && row < ch.first + ch.count;  // a row before the first sequence has no position
+    const int64_t pos = own ? ch.pos0 + (row - ch.first) : -1;
     const int32_t page = pos < 0 ? -1 : page_at(cache, b, pos);
     const int64_t slot = pos & ((1 << cache.shift) - 1);
     for (int i = threadIdx.x; i < width / 2; i += kThreads) {
