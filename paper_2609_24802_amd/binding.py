@@ -954,13 +954,13 @@ class RotaryPositions(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, pos, rot, layout):
         ctx.rot, ctx.layout = rot, layout
-        ctx.save_for_backward(pos)
+        ctx.save_for_backward(pos, rot.freq)  # freq too: torch then refuses a backward after a change in place
         return tiga_mp_rotary_fwd(x, pos, rot, layout)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        (pos,) = ctx.saved_tensors
+        pos, _ = ctx.saved_tensors
         if dy.stride(-1) != 1:
             dy = dy.contiguous()
         return tiga_mp_rotary_bwd(dy, pos, ctx.rot, ctx.layout), None, None, None
