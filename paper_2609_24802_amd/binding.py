@@ -666,9 +666,26 @@ def tiga_rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "pla
     return freq
 
 
+def _bound(name):
+    """A tensor whose address a handle holds: written into freely, but not replaced (the handle would keep reading the
+    old one, freed or not).  `handle.name += 1` writes in place and is fine."""
+
+    def get(self):
+        return self.__dict__[name]
+
+    def put(self, value):
+        if value is not self.__dict__.setdefault(name, value):
+            raise AttributeError(f"{name} of a {type(self).__name__} cannot be replaced: write into it, or make another")
+
+    return property(get, put)
+
+
 class Rotary:
     """A rotation by positions: freq float64 [rot / 2] on the device (radians a position), the pairs (i, i + rot / 2)
-    or (interleaved) (2 i, 2 i + 1), and an amplitude that multiplies the rotated elements."""
+    or (interleaved) (2 i, 2 i + 1), and an amplitude that multiplies the rotated elements.  freq's contents may
+    change; another tensor in its place needs another Rotary."""
+
+    freq = _bound("freq")
 
     def __init__(self, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0):
         self.freq = _dev(freq, torch.float64, "freq")
@@ -725,7 +742,10 @@ class KvCache:
     multiples of 8 elements with a contiguous width (pages stored rows first are passed permuted);
     table: int32 [batch, table_width], position p of sequence b is row p % page_size of page
     table[b, p // page_size]; length: int32 [batch], positions of each sequence with the new ones of a
-    call.  The tensors are the caller's; their contents may change between calls."""
+    call.  The tensors are the caller's; their contents may change between calls, other tensors in their
+    places need another KvCache."""
+
+    k_pages, v_pages, table, length = _bound("k_pages"), _bound("v_pages"), _bound("table"), _bound("length")
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
         shape, kv = _rows(k_pages, "k_pages", _AXES["bhnd"])
