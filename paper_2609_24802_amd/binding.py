@@ -580,6 +580,19 @@ def _rows(t, name, axes, dtype=None, shape=None):
                       st[n] if got[2] > 1 else 0)
 
 
+def _given_or_new(ws, query, *args, device):
+    """The workspace of a call on `device`: the caller's, or one of the size that query(*args) tells."""
+    if ws is None:
+        return _workspace(query(*args), device)
+    if not isinstance(ws, torch.Tensor) or not ws.is_cuda:
+        raise TypeError("ws must be a CUDA (HIP) tensor")
+    if ws.device != device:
+        raise ValueError(f"ws is on {ws.device}, expected {device}")
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws
+
+
 def _like(t, axes):
     """A new contiguous tensor of t's shape, and its view."""
     y = t.new_empty(t.shape)
@@ -617,11 +630,10 @@ def tiga_mp_attention_cross_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     y, yv = _like(q, axes)
     lse = q.new_empty((rel.batch, rel.heads, rel.num_dst), dtype=torch.float32) if want_lse else None
     ref = C.byref
-    if ws is None:
-        ws = _workspace(lib.tiga_mp_attention_cross_fwd_workspace(ref(rel)), q.device)
+    ws = _given_or_new(ws, lib.tiga_mp_attention_cross_fwd_workspace, ref(rel), device=q.device)
     _check(lib.tiga_mp_attention_cross_fwd(ref(rel), ref(qv), ref(kv), ref(vv),
                                            rel.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
-                                           _ptr(ws), ws.numel(), _stream()))
+                                           _ptr(ws), ws.nbytes, _stream()))
     return (y, lse) if want_lse else y
 
 
@@ -642,11 +654,10 @@ def tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy, src_len: torch.Tensor | Non
         if name in want:
             out[name], view = _like(t, axes)
             refs[i] = ref(view)
-    if ws is None:
-        ws = _workspace(lib.tiga_mp_attention_cross_bwd_workspace(ref(rel)), q.device)
+    ws = _given_or_new(ws, lib.tiga_mp_attention_cross_bwd_workspace, ref(rel), device=q.device)
     _check(lib.tiga_mp_attention_cross_bwd(ref(rel), ref(qv), ref(kv), ref(vv), ref(yv), _ptr(lse), ref(dyv),
                                            rel.width ** -0.5 if scale is None else float(scale), *refs, _ptr(ws),
-                                           ws.numel(), _stream()))
+                                           ws.nbytes, _stream()))
     return out
 
 
@@ -837,11 +848,10 @@ def tiga_mp_attention_paged_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.
     _same_device(cache.k_pages.get_device(), q=q, y=y, dst_ptr=dst_ptr)
     lse = q.new_empty((heads, rows), dtype=torch.float32) if want_lse else None
     ref = C.byref
-    if ws is None:
-        ws = _workspace(lib.tiga_mp_attention_paged_fwd_workspace(cache.ref, rows, heads), q.device)
+    ws = _given_or_new(ws, lib.tiga_mp_attention_paged_fwd_workspace, cache.ref, rows, heads, device=q.device)
     _check(lib.tiga_mp_attention_paged_fwd(cache.ref, rows, _ptr(dst_ptr), heads, ref(qv),
                                            cache.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
-                                           _ptr(ws), ws.numel(), _stream()))
+                                           _ptr(ws), ws.nbytes, _stream()))
     return (y, lse) if want_lse else y
 
 
