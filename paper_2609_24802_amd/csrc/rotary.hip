@@ -189,15 +189,15 @@ __device__ __forceinline__ void settle(const Move<T> &m, const tiga_rotary &rot,
     if (m.slot < sl.turned && half) *reinterpret_cast<u4 *>(m.y + rot.rot / 2) = b;
 }
 
-// Block (x, y): rows [x * per_block, ...) of batch * rows, heads [y * group, ...).
+// Block (x, y): rows [(block0 + x) * per_block, ...) of batch * rows, heads [y * group, ...).
 template <class T>
 __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(tiga_view x, tiga_view y, const int32_t *__restrict__ pos,
                                                                int64_t pos_batch, int64_t rows, int64_t total,
                                                                int per_block, int heads, int group, tiga_rotary rot,
-                                                               Slots sl, Divider heads_div, float sign) {
+                                                               Slots sl, Divider heads_div, float sign, int64_t block0) {
     typedef typename T::raw raw;
     __shared__ float c[kMaxPairs], s[kMaxPairs];
-    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * per_block;
+    const int64_t row0 = (block0 + blockIdx.x) * per_block;
     const int here = static_cast<int>(min(static_cast<int64_t>(per_block), total - row0));
     const int h0 = blockIdx.y * group, nh = min(group, heads - h0), pairs = rot.rot / 2;
     for (int i = threadIdx.x; i < here * pairs; i += kThreads) {
@@ -260,7 +260,7 @@ __device__ __forceinline__ int sequence_of(const Pages &cache, int row) {
 template <class T>
 __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view k, tiga_view v, tiga_rotary rot, int heads,
                                                           int kv_heads, tiga_view q, tiga_view qo, int per_block, Slots sl,
-                                                          Slots whole, Divider per_token) {
+                                                          Slots whole, Divider per_token, int block0) {
     typedef typename T::raw raw;
     struct Place {
         int64_t pos;
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view
     };
     __shared__ float c[kMaxPairs], s[kMaxPairs];
     __shared__ Place places[4];
-    const int row0 = blockIdx.x * per_block, here = min(per_block, cache.num_dst - row0), pairs = rot.rot / 2;
+    const int row0 = (block0 + static_cast<int>(blockIdx.x)) * per_block, here = min(per_block, cache.num_dst - row0), pairs = rot.rot / 2;
     const int nk = kv_heads * sl.all, nv = kv_heads * whole.all, each = nk + nv + heads * sl.all, items = here * each;
     const tiga_rotary plain{nullptr, 0, TIGA_PAIRS_ADJACENT, 1.0f};
     Move<T> m[kSteps];
@@ -369,9 +369,10 @@ __device__ __forceinline__ void turn_heads(const typename T::raw *x, int64_t xh,
 template <class T>
 __global__ __launch_bounds__(kThreads) void rotate_pairs_kernel(tiga_view x, tiga_view y, const int32_t *__restrict__ pos,
                                                                 int64_t pos_batch, int64_t rows, int64_t total, int heads,
-                                                                int group, int width, tiga_rotary rot, float sign) {
+                                                                int group, int width, tiga_rotary rot, float sign,
+                                                                int64_t block0) {
     const int units = (width + 1) / 2, h0 = blockIdx.y * group;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t t = (block0 + blockIdx.x) * kThreads + threadIdx.x;
     if (t >= total) return;
     const int64_t line = quotient(t, units), b = quotient(line, rows), r = line - b * rows;
     const int i = static_cast<int>(t - line * units);
@@ -385,9 +386,9 @@ __global__ __launch_bounds__(kThreads) void rotate_pairs_kernel(tiga_view x, tig
 // A block a new token.
 template <class T>
 __global__ __launch_bounds__(kThreads) void append_pairs_kernel(Pages cache, tiga_view k, tiga_view v, tiga_rotary rot, int heads,
-                                                          int kv_heads, tiga_view q, tiga_view qo, int width) {
+                                                          int kv_heads, tiga_view q, tiga_view qo, int width, int block0) {
     typedef typename T::raw raw;
-    const int row = blockIdx.x;
+    const int row = block0 + static_cast<int>(blockIdx.x);
     const int b = sequence_of(cache, row);
     if (b >= cache.batch) return;
     const Chunk ch = chunk_of(cache, b);
@@ -412,6 +413,20 @@ __global__ __launch_bounds__(kThreads) void append_pairs_kernel(Pages cache, tig
             turn_heads<T>(static_cast<const raw *>(q.data) + row * q.row, q.head, static_cast<raw *>(qo.data) + row * qo.row,
                           qo.head, heads, i, width, rr, a);
     }
+}
+
+// launch(first block, blocks) until all are launched: a grid counts its threads in 32 bits, and a larger one would wrap
+// around without an error.
+constexpr int64_t kMostBlocks = int64_t(1) << 23;
+template <class F>
+int in_grids(int64_t blocks, const char *what, hipStream_t stream, F launch) {
+    prof_before(stream);
+    for (int64_t at = 0; at < blocks; at += kMostBlocks) {
+        launch(at, static_cast<unsigned>(blocks - at < kMostBlocks ? blocks - at : kMostBlocks));
+        if (int rc = check_launch(what)) return rc;
+    }
+    prof_after(stream);
+    return TIGA_OK;
 }
 
 // Whether the rows of a view consist of aligned 16-byte runs that the rotation's slots are made of.
@@ -446,18 +461,16 @@ int rotate(int32_t batch, int32_t heads, int64_t rows, int32_t width, int dtype,
     int64_t group = blocks >= wanted ? heads : ceil_div(static_cast<int64_t>(heads) * blocks, wanted);
     if (ceil_div(heads, group) > 65535) group = ceil_div(heads, 65535);
     if (runs && group * sl.all * per_block > 0x3fffffff) group = 0x3fffffff / (sl.all * per_block);  // 32-bit slot numbers
-    if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "rotary: too many rows");
-    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(ceil_div(heads, group)));
+    const unsigned parts = static_cast<unsigned>(ceil_div(heads, group));
     auto go = [&](auto by_runs, auto by_pairs) {
-        prof_before(stream);
-        if (runs)
-            hipLaunchKernelGGL(by_runs, grid, dim3(kThreads), 0, stream, x, y, pos, pos_batch, rows, lines,
-                               static_cast<int>(per_block), heads, static_cast<int>(group), rot, sl, divider(heads), sign);
-        else
-            hipLaunchKernelGGL(by_pairs, grid, dim3(kThreads), 0, stream, x, y, pos, pos_batch, rows, total, heads,
-                               static_cast<int>(group), width, rot, sign);
-        prof_after(stream);
-        return check_launch("rotary");
+        return in_grids(blocks, "rotary", stream, [&](int64_t at, unsigned n) {
+            if (runs)
+                hipLaunchKernelGGL(by_runs, dim3(n, parts), dim3(kThreads), 0, stream, x, y, pos, pos_batch, rows, lines,
+                                   static_cast<int>(per_block), heads, static_cast<int>(group), rot, sl, divider(heads), sign, at);
+            else
+                hipLaunchKernelGGL(by_pairs, dim3(n, parts), dim3(kThreads), 0, stream, x, y, pos, pos_batch, rows, total,
+                                   heads, static_cast<int>(group), width, rot, sign, at);
+        });
     };
     if (dtype == TIGA_DT_F32) return go(rotate_rows_kernel<F32>, rotate_pairs_kernel<F32>);
     return dtype == TIGA_DT_F16 ? go(rotate_rows_kernel<F16>, rotate_pairs_kernel<F16>)
@@ -479,18 +492,16 @@ int append(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, con
     if (per_block > 4) per_block = 4;
     if (per_block < 1) per_block = 1;
     if (each * per_block > 0x3fffffff) return fail(TIGA_EUNSUPPORTED, "cache append: too many heads");
-    const dim3 grid(static_cast<unsigned>(ceil_div(num_dst, per_block)));
     auto go = [&](auto by_runs, auto by_pairs) {
-        prof_before(stream);
-        if (runs)
-            hipLaunchKernelGGL(by_runs, grid, dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
-                               cache.kv_heads, q, q_out, static_cast<int>(per_block), sl, whole,
-                               divider(static_cast<int32_t>(each)));
-        else
-            hipLaunchKernelGGL(by_pairs, grid, dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
-                               cache.kv_heads, q, q_out, cache.width);
-        prof_after(stream);
-        return check_launch("cache append");
+        return in_grids(ceil_div(num_dst, per_block), "cache append", stream, [&](int64_t at, unsigned n) {
+            if (runs)
+                hipLaunchKernelGGL(by_runs, dim3(n), dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
+                                   cache.kv_heads, q, q_out, static_cast<int>(per_block), sl, whole,
+                                   divider(static_cast<int32_t>(each)), static_cast<int>(at));
+            else
+                hipLaunchKernelGGL(by_pairs, dim3(n), dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
+                                   cache.kv_heads, q, q_out, cache.width, static_cast<int>(at));
+        });
     };
     return cache.dtype == TIGA_DT_F16 ? go(append_kernel<F16>, append_pairs_kernel<F16>)
                                       : go(append_kernel<BF16>, append_pairs_kernel<BF16>);
