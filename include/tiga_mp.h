@@ -448,7 +448,9 @@ size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel);
  * Gradients of sources at and past src_len[b] are 0.
  *   dy: as y; dq as q, dk and dv as k and v, of dtype, overwritten; each may be
  *   NULL (skipped).  p and ds enter the products rounded to dtype; sums in fp32.
- * Deterministic (no atomics).  Requirements and errors as the forward. */
+ * Deterministic (no atomics).  Requirements and errors as the forward; besides,
+ * batch * heads * num_dst <= 2^30 - 64, and at most 2^24 - 1 tiles of 128 sources
+ * (batch * kv_heads * ceil(num_src / 128)), TIGA_EUNSUPPORTED otherwise. */
 int tiga_mp_attention_cross_bwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
                                 const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
                                 const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,

@@ -587,6 +587,10 @@ Plan plan_for(const tiga_cross &rel, bool keys) {
     return p;
 }
 
+// A grid counts its threads in 32 bits (and wraps around without an error).  The grids are of tiles, of the rows' statistics
+// (4 threads a row) and of the sums of split items, which are at most as many as run at once.
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
+
 struct Layout {
     Plan q, kv;
     float *lse2, *delta, *part;
@@ -613,8 +617,6 @@ int products(const Plan &p, Args a, bool timed, hipStream_t stream) {
     const int64_t heads = static_cast<int64_t>(a.batch) * a.kv_heads, blocks = heads * p.tiles * p.splits;
     if (blocks == 0) return TIGA_OK;
     const int64_t sums = ceil_div(heads * (KEYS ? a.num_src : a.rows) * (D / 4), kThreads);
-    if (blocks > 0x7fffffff || sums > 0x7fffffff)
-        return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many tiles (%lld)", (long long)blocks);
     a.splits = static_cast<int32_t>(p.splits);
     if (timed) prof_before(stream);
     hipLaunchKernelGGL((products_kernel<T, D, MODE>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a,
@@ -636,7 +638,6 @@ int launch(const Layout &l, const Args &a, hipStream_t stream) {
         if (int rc = products<T, D, kQuery>(l.q, a, !keys, stream)) return rc;
     } else {
         const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * 4, kThreads);
-        if (blocks > 0x7fffffff) return fail(TIGA_EUNSUPPORTED, "cross attention backward: too many rows");
         hipLaunchKernelGGL((stats_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a);
         if (int rc = check_launch("cross attention statistics")) return rc;
     }
@@ -651,6 +652,10 @@ int cross_backward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k
                    const tiga_view &y, const float *lse, const tiga_view &dy, float scale, const tiga_view &dq,
                    const tiga_view &dk, const tiga_view &dv, void *ws, hipStream_t stream) {
     const Layout l = layout(rel, ws);
+    const int64_t heads = static_cast<int64_t>(rel.batch) * rel.kv_heads;
+    if (heads * l.q.tiles * l.q.splits > kMostBlocks || heads * l.kv.tiles * l.kv.splits > kMostBlocks ||
+        ceil_div(static_cast<int64_t>(rel.batch) * rel.heads * rel.num_dst, kThreads / 4) > kMostBlocks)
+        return fail(TIGA_EUNSUPPORTED, "cross attention backward: at most 2^30 - 64 rows, and 2^24 - 1 tiles of 128 rows or sources");
     Args a{};
     a.q = rows_of(q);
     a.k = rows_of(k);
