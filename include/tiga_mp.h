@@ -441,16 +441,18 @@ int tiga_mp_attention_cross_fwd(const tiga_cross *rel, const tiga_view *q, const
 size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel);
 
 /* Vector-Jacobian product of tiga_mp_attention_cross_fwd.  With the forward's y
- * and lse, p_ij = exp(s_ij - lse_i) and delta_i = <dy_i, y_i>:
+ * and lse, p_ij = exp(s_ij - lse_i) and delta_i = <dy_i, y_i> (formed as
+ * sum_j p_ij <dy_i, v_j> where a sequence's sources fit a tile, at most 128 of
+ * width 64 or 64 of width 128, over which y's rounding would matter):
  *   ds_ij = p_ij (<dy_i, v_j> - delta_i)
  *   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dy_i
  * where the sums over i also run over the heads that share source head j's.
  * Gradients of sources at and past src_len[b] are 0.
  *   dy: as y; dq as q, dk and dv as k and v, of dtype, overwritten; each may be
  *   NULL (skipped).  p and ds enter the products rounded to dtype; sums in fp32.
- * Deterministic (no atomics).  Requirements and errors as the forward; besides,
- * batch * heads * num_dst <= 2^30 - 64, and at most 2^24 - 1 tiles of 128 sources
- * (batch * kv_heads * ceil(num_src / 128)), TIGA_EUNSUPPORTED otherwise. */
+ * Deterministic (no atomics).  Requirements and errors as the forward; besides, at
+ * most 2^24 - 1 tiles of 128 sources, or rows of a source head, over all batch *
+ * kv_heads, TIGA_EUNSUPPORTED otherwise. */
 int tiga_mp_attention_cross_bwd(const tiga_cross *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
                                 const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
                                 const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,

@@ -5,9 +5,9 @@
 // lse; nothing of the size of the relation is stored.
 //
 // Two launches of one kernel: dq with the rows owned and the keys streamed, which also leaves the rows' statistics (lse in
-// the log2 domain, delta; a kernel of its own forms them where dq is not wanted), then dk, dv with the keys owned and the
-// rows streamed.  A wavefront owns 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or q) and Y2 (v
-// or dy) through LDS.  Per 32 streamed rows
+// the log2 domain, delta; these alone where dq is not wanted), then dk, dv with the keys owned and the rows streamed.  A
+// wavefront owns 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or
+// q) and Y2 (v or dy) through LDS.  Per 32 streamed rows
 //   S = Y1 X1^T, DP = Y2 X2^T   (streamed x owned, 16x16x32 MFMA, fp32)
 //   P = 2^(c S - lse2), DS = P (DP - delta), rounded to the input type as the operands of the next products
 //   acc1 += Y1^T DS (dq or dk),  acc2 += Y2^T P (dv)
@@ -18,8 +18,9 @@
 //
 // delta is taken from the forward's y, whose rounding (of itself and of the weights in it) makes an error of u |dy| |y|.
 // Over many sources that is small against ds; over a few it is not (twice the error of dq and dk at 2 to 5 sources),
-// so where the sources fit one streamed tile, delta is formed as sum_j p_ij <dy_i, v_j> in fp32 instead, by the products
-// S and DP of that tile, in one launch with dq, which takes the same products (and comes first then).
+// so where a sequence's sources fit one streamed tile, delta is formed as sum_j p_ij <dy_i, v_j> in fp32 instead, by the
+// products S and DP of that tile, in one launch with dq, which takes the same products (and comes first then).  That goes
+// by the sequence's own sources: its gradients do not depend on what else is in the batch.
 //
 // Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 494 us (1.11 PFLOP/s), dq
 // 333 us (1.24), 836 together; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 392 us (1.05); 4 x 8 x 4096 rows over
@@ -78,10 +79,6 @@ __device__ __forceinline__ int64_t stat_at(const Args &a, int b, int kv, int32_t
 
 // A row that saw no weight has no gradient: its weights are formed as 0.
 __device__ __forceinline__ float log2_of(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
-__device__ __forceinline__ void close_stats(const Args &a) {
-    a.lse2[a.stats] = __builtin_inff();
-    a.delta[a.stats] = 0.0f;
-}
 
 // <dy, y> of a row, lane g of its four: 16-byte chunks g, g + 4, ...; the four lanes' sums are added g ^ 1 first, then g ^ 2.
 template <class T, int CH>
@@ -97,30 +94,6 @@ __device__ __forceinline__ float row_product(const u4 (&dy)[CH], const uint16_t 
         }
     }
     return s;
-}
-
-// Four lanes a row.  The same bits as where dq is formed: dk and dv do not depend on whether it is.
-template <class T, int D>
-__global__ __launch_bounds__(kThreads) void stats_kernel(Args a) {
-    constexpr int CH = D / 32;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t r = t / 4;
-    const int g = static_cast<int>(t % 4);
-    if (t == 0) close_stats(a);
-    if (r >= a.stats) return;  // whole rows: the lanes of a row leave together
-    const int64_t i = r % a.num_dst, bh = r / a.num_dst;
-    const int64_t h = bh % a.heads, b = bh / a.heads;
-    const u4 *const p = reinterpret_cast<const u4 *>(a.dy.p + b * a.dy.batch + h * a.dy.head + i * a.dy.row);
-    u4 dy[CH];
-#pragma unroll
-    for (int ch = 0; ch < CH; ++ch) dy[ch] = p[ch * 4 + g];
-    float s = row_product<T>(dy, a.y.p + b * a.y.batch + h * a.y.head + i * a.y.row, g);
-    s += shfl_xor_f(s, 1);
-    s += shfl_xor_f(s, 2);
-    if (g == 0) {
-        a.lse2[r] = log2_of(a.lse[r]);
-        a.delta[r] = s;
-    }
 }
 
 // ------------------------------------------------------------------------------------------ products
@@ -155,7 +128,8 @@ __device__ __forceinline__ int swizzle(int k) {
 template <int D, bool KEYS>
 constexpr int kBlocks = KEYS && D == 128 ? 1 : 2;
 
-// What the products are formed for: dq (rows owned), dk and dv (keys owned), or delta and dq over one tile of keys.
+// What the products are formed for: dq (rows owned), dk and dv (keys owned), or delta and dq where no sequence has more than
+// one tile of keys (as kQuery would, in half the LDS).
 enum Mode { kQuery, kKeys, kFew };
 
 template <class T, int D, Mode MODE>
@@ -350,6 +324,9 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
     const int32_t t0 = static_cast<int32_t>(static_cast<int64_t>(steps) * split / a.splits);
     const int32_t t1 = static_cast<int32_t>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
 
+    // the sequence's sources fit one tile: delta comes from the tile's products
+    const bool few = MODE == kFew || (MODE == kQuery && n <= G::BN);
+
     // owned operands; columns past the end repeat the last (what they sum is not stored)
     u4 x1[2][G::CH], x2[2][G::CH];
     float own[2], own_delta[2];
@@ -372,23 +349,29 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
                 x1[qb][ch] = reinterpret_cast<const u4 *>(p1)[ch * 4 + g];
                 x2[qb][ch] = reinterpret_cast<const u4 *>(p2)[ch * 4 + g];
             }
-            if constexpr (MODE == kQuery)
+            if (MODE == kQuery && !few)
                 own_delta[qb] = column_sum(row_product<T>(x2[qb], a.y.p + row_at(a, a.y, b, kv, o), g));
         }
     }
+    if (!KEYS && blockIdx.x == 0 && threadIdx.x == 0) {  // what rows past the end have
+        a.lse2[a.stats] = __builtin_inff();
+        a.delta[a.stats] = 0.0f;
+    }
     // The owned rows' statistics, for dk and dv: delta is there.
     auto leave_stats = [&] {
-        if (blockIdx.x == 0 && threadIdx.x == 0) close_stats(a);
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             const int32_t o = own0 + w * 32 + qb * 16 + col;
-            if (o < own_n && g == 0 && split == 0) {
+            if (o < own_n && g == 0) {
                 a.lse2[stat_at(a, b, kv, o)] = own[qb];
                 a.delta[stat_at(a, b, kv, o)] = own_delta[qb];
             }
         }
     };
-    if constexpr (MODE == kQuery) leave_stats();
+    if (MODE == kQuery && !few) {
+        if (split == 0) leave_stats();
+        if (!a.dq.p) return;
+    }
     Sums<T, D, MODE> acc;
 #pragma unroll
     for (int d = 0; d < G::DB; ++d)
@@ -461,42 +444,46 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
         }
     };
     if (t0 < t1) stage(t0, y1a, y2a, sta);
-    if constexpr (MODE == kFew) {
-        if (t0 < t1) {
-            Scores<T, D> f[G::KC];
-            loads_arrived();
-            __syncthreads();
+    if constexpr (!KEYS) {
+        if (few) {
+            if (t0 < t1) {
+                Scores<T, D> f[G::KC];
+                loads_arrived();
+                __syncthreads();
 #pragma unroll
-            for (int kc = 0; kc < G::KC; ++kc) {
-                f[kc].form(x1, x2, y1a + kc * 32 * G::RB, y2a + kc * 32 * G::RB, dr, [](int) {});
-                weigh<T, D>(f[kc], c, own, G::BN > str_n, str_n - kc * 32, g);
+                for (int kc = 0; kc < G::KC; ++kc) {
+                    f[kc].form(x1, x2, y1a + kc * 32 * G::RB, y2a + kc * 32 * G::RB, dr, [](int) {});
+                    weigh<T, D>(f[kc], c, own, G::BN > str_n, str_n - kc * 32, g);
 #pragma unroll
-                for (int qb = 0; qb < 2; ++qb)
+                    for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) own_delta[qb] += f[kc].s[i / 4][qb][i % 4] * f[kc].dp[i / 4][qb][i % 4];
+                        for (int i = 0; i < 8; ++i) own_delta[qb] += f[kc].s[i / 4][qb][i % 4] * f[kc].dp[i / 4][qb][i % 4];
+                }
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb) own_delta[qb] = column_sum(own_delta[qb]);
+                if (a.dq.p)
+#pragma unroll
+                    for (int kc = 0; kc < G::KC; ++kc) add_keys<T, D, MODE>(acc, f[kc], own_delta, y1a + kc * 32 * G::RB, tr);
             }
-#pragma unroll
-            for (int qb = 0; qb < 2; ++qb) own_delta[qb] = column_sum(own_delta[qb]);
-            if (a.dq.p)
-#pragma unroll
-                for (int kc = 0; kc < G::KC; ++kc) add_keys<T, D, MODE>(acc, f[kc], own_delta, y1a + kc * 32 * G::RB, tr);
+            if (split == a.splits - 1) leave_stats();  // the split that has the tile, if there is one
+            if (!a.dq.p) return;
         }
-        leave_stats();
-        if (!a.dq.p) return;
-    } else {
+    }
+    if constexpr (MODE != kFew) {
+        const int32_t end = few ? t0 : t1;
         int kt = t0;
         // one exit, after a whole turn of both buffers: with another between them the sums are moved and spill
-        for (; kt + 1 < t1; kt += 2) {
+        for (; kt + 1 < end; kt += 2) {
             loads_arrived();
             __syncthreads();
             stage(kt + 1, y1b, y2b, stb);
             step(kt, y1a, y2a, sta);
             loads_arrived();
             __syncthreads();
-            if (kt + 2 < t1) stage(kt + 2, y1a, y2a, sta);
+            if (kt + 2 < end) stage(kt + 2, y1a, y2a, sta);
             step(kt + 1, y1b, y2b, stb);
         }
-        if (kt < t1) {
+        if (kt < end) {
             loads_arrived();
             __syncthreads();
             step(kt, y1a, y2a, sta);
@@ -587,8 +574,8 @@ Plan plan_for(const tiga_cross &rel, bool keys) {
     return p;
 }
 
-// A grid counts its threads in 32 bits (and wraps around without an error).  The grids are of tiles, of the rows' statistics
-// (4 threads a row) and of the sums of split items, which are at most as many as run at once.
+// A grid counts its threads in 32 bits (and wraps around without an error).  The grids are of tiles, and of the sums of
+// split items, which are at most as many as run at once.
 constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
 
 struct Layout {
@@ -632,14 +619,12 @@ int products(const Plan &p, Args a, bool timed, hipStream_t stream) {
 template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
     const bool keys = a.dk.p || a.dv.p;
-    if (a.num_src <= Geo<D>::BN && a.stats > 0) {
-        if (int rc = products<T, D, kFew>(l.q, a, !keys, stream)) return rc;  // of one tile of keys: not split
-    } else if (a.dq.p) {
-        if (int rc = products<T, D, kQuery>(l.q, a, !keys, stream)) return rc;
-    } else {
-        const int64_t blocks = ceil_div((a.stats > 0 ? a.stats : 1) * 4, kThreads);
-        hipLaunchKernelGGL((stats_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, a);
-        if (int rc = check_launch("cross attention statistics")) return rc;
+    if (a.stats > 0) {
+        Plan p = l.q;
+        if (!a.dq.p) p.splits = 1;  // the rows' statistics alone
+        const int rc = a.num_src <= Geo<D>::BN ? products<T, D, kFew>(p, a, !keys, stream)  // of one tile of keys: not split
+                                               : products<T, D, kQuery>(p, a, !keys, stream);
+        if (rc) return rc;
     }
     return keys ? products<T, D, kKeys>(l.kv, a, true, stream) : TIGA_OK;
 }
@@ -653,9 +638,8 @@ int cross_backward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k
                    const tiga_view &dk, const tiga_view &dv, void *ws, hipStream_t stream) {
     const Layout l = layout(rel, ws);
     const int64_t heads = static_cast<int64_t>(rel.batch) * rel.kv_heads;
-    if (heads * l.q.tiles * l.q.splits > kMostBlocks || heads * l.kv.tiles * l.kv.splits > kMostBlocks ||
-        ceil_div(static_cast<int64_t>(rel.batch) * rel.heads * rel.num_dst, kThreads / 4) > kMostBlocks)
-        return fail(TIGA_EUNSUPPORTED, "cross attention backward: at most 2^30 - 64 rows, and 2^24 - 1 tiles of 128 rows or sources");
+    if (heads * l.q.tiles * l.q.splits > kMostBlocks || heads * l.kv.tiles * l.kv.splits > kMostBlocks)
+        return fail(TIGA_EUNSUPPORTED, "cross attention backward: at most 2^24 - 1 tiles of 128 rows or sources");
     Args a{};
     a.q = rows_of(q);
     a.k = rows_of(k);

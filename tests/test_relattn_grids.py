@@ -6,8 +6,8 @@ import pytest
 from tests.test_relattn_args import FAKE, b, view  # noqa: F401  (b: the fixture)
 
 
-@pytest.mark.parametrize("over", [dict(num_dst=1 << 20, batch=1 << 10, num_src=5), dict(num_dst=1 << 20, batch=1 << 12, num_src=500),
-                                  dict(num_dst=3, batch=1 << 12, num_src=1 << 20), dict(num_dst=1 << 28, heads=5, batch=1, num_src=9)])
+@pytest.mark.parametrize("over", [dict(num_dst=1 << 20, batch=1 << 11, num_src=5), dict(num_dst=1 << 20, batch=1 << 12, num_src=500),
+                                  dict(num_dst=3, batch=1 << 12, num_src=1 << 20)])
 @pytest.mark.parametrize("want", [(1, 0, 0), (0, 1, 1), (1, 1, 1)])
 def test_backward(b, over, want):  # noqa: F811
     rel = b._Cross(**{**dict(heads=1, kv_heads=1, width=64, dtype=0, src_len=None), **over})
