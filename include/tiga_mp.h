@@ -449,7 +449,9 @@ size_t tiga_mp_attention_cross_bwd_workspace(const tiga_cross *rel);
  * where the sums over i also run over the heads that share source head j's.
  * Gradients of sources at and past src_len[b] are 0.
  *   dy: as y; dq as q, dk and dv as k and v, of dtype, overwritten; each may be
- *   NULL (skipped).  p and ds enter the products rounded to dtype; sums in fp32.
+ *   NULL (skipped).  p and ds enter the products rounded to dtype (binary16: as
+ *   scaled by powers of two that bring the largest ones near its largest number,
+ *   which a pass over v and dy finds); sums in fp32.
  * Deterministic (no atomics).  Requirements and errors as the forward; besides, at
  * most 2^24 - 1 tiles of 128 sources, or rows of a source head, over all batch *
  * kv_heads, TIGA_EUNSUPPORTED otherwise. */

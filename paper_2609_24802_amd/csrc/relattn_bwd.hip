@@ -9,7 +9,8 @@
 // wavefront owns 32 columns, whose operands X1 (q or k) and X2 (dy or v) stay in registers, and streams tiles of Y1 (k or
 // q) and Y2 (v or dy) through LDS.  Per 32 streamed rows
 //   S = Y1 X1^T, DP = Y2 X2^T   (streamed x owned, 16x16x32 MFMA, fp32)
-//   P = 2^(c S - lse2), DS = P (DP - delta), rounded to the input type as the operands of the next products
+//   P = 2^(c S - lse2), DS = P (DP - delta), rounded to the input type as the operands of the next products (binary16:
+//   scaled into its range first)
 //   acc1 += Y1^T DS (dq or dk),  acc2 += Y2^T P (dv)
 // where the accumulator layout of S is the operand layout of P (each lane's rows of two 16-row blocks fill its 8 slots of
 // a 32-deep product, and the transposing LDS reads of Y^T take the rows in that order).  dk and dv need S and DP once
@@ -30,6 +31,8 @@
 //
 // Every sum has a fixed order.  Where the owned tiles do not fill the device, the streamed axis is split, and the parts'
 // fp32 sums go to the workspace and are added by reduce_kernel.
+#include <type_traits>
+
 #include "mfma16.hpp"
 #include "relation.hpp"
 #include "relattn.hpp"
@@ -50,6 +53,8 @@ struct Args {
     const int32_t *len;
     float *lse2, *delta;  // [batch * heads * num_dst + 1]: the last is what rows past the end have (no weight)
     float *part;          // split sums
+    f2 *peak;             // [batch * kv_heads][peaks]: of a share of a source head's values and cotangents (binary16)
+    int32_t peaks;
     int32_t num_dst, num_src, batch, heads, kv_heads;
     Divider group;
     int64_t stats;        // batch * heads * num_dst
@@ -94,6 +99,93 @@ __device__ __forceinline__ float row_product(const u4 (&dy)[CH], const uint16_t 
         }
     }
     return s;
+}
+
+// ------------------------------------------------------------------------------------------ range of binary16
+
+// P and DS enter the products in the input type.  P is of order 1 / S and DS of that times the cotangents, and binary16 has
+// no normal numbers below 2^-14, so there they are scaled by powers of two, which the fp32 sums are rid of again:
+//  - P by 2^kUp: at most 1 (and what lse's rounding adds), so it stays below 2^16;
+//  - DS by 2^up(M), M >= |<dy_i, v_j>|, and so |DS| <= 2 M: below 2^15.  M = |dy_i|_1 max |v| of the row for dq, whose sums
+//    are the row's own, and of the source head's largest row for dk, whose sums run over its rows.
+// What is then rounded to a multiple of 2^-24 is 2^-38 of those bounds.  (Unscaled, over 8192 sources at cotangents of
+// 1e-3: dq and dk 1.1e-2 off, at 1e-4 0.1.)  bfloat16 has the range of fp32.
+template <class T>
+constexpr bool kScaled = std::is_same<T, Half16>::value;
+constexpr int kUp = 14;
+// M < 2^(its binary exponent).  0, infinities and NaN, where any factor does, have exponent 0.
+__device__ __forceinline__ int up(float m) { return kUp - __builtin_amdgcn_frexp_expf(m); }
+__device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
+
+template <class T>
+__device__ __forceinline__ float sum_abs(u4 x) {
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const f2 u = T::unpack(x[e]);
+        s += __builtin_fabsf(u.x) + __builtin_fabsf(u.y);
+    }
+    return s;
+}
+
+// max |v| and max |dy|_1 of a share of a source head's sources and rows; what is not a number is passed over (its results
+// are none either).
+// Bound by reading v and dy once: 2 x 16 x 2048 rows and 4 x 8192 sources of 128, 34 MB
+// in 8 us, of 884; 8 x 449 ragged rows over 1500 of 64, 23 MB in 8 us, of 95.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void peak_kernel(Args a) {
+    constexpr int L = D / 8, ROWS = kThreads / L;  // 16 bytes a lane
+    __shared__ f2 of_wave[kWaves];
+    const int64_t bh = blockIdx.x / a.peaks;
+    const int part = static_cast<int>(blockIdx.x - bh * a.peaks);
+    const int b = static_cast<int>(bh / a.kv_heads), kv = static_cast<int>(bh % a.kv_heads);
+    const int first = static_cast<int>(threadIdx.x) / L, c = static_cast<int>(threadIdx.x) % L;
+    auto from = [&](int64_t n, int i) { return static_cast<int32_t>(n * i / a.peaks); };
+    f2 top{0.0f, 0.0f};
+    const int32_t n = sources(a, b);
+    const u4 *const v = reinterpret_cast<const u4 *>(a.v.p + b * a.v.batch + kv * a.v.head) + c;
+    const int32_t v1 = from(n, part + 1);
+#pragma unroll 4
+    for (int32_t j = from(n, part) + first; j < v1; j += ROWS) {
+        const u4 x = v[j * (a.v.row / 8)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f2 u = T::unpack(x[e]);
+            top.x = fmaxf(top.x, fmaxf(__builtin_fabsf(u.x), __builtin_fabsf(u.y)));
+        }
+    }
+    const int32_t r1 = from(a.rows, part + 1);
+#pragma unroll 4
+    for (int32_t r = from(a.rows, part) + first; r < r1; r += ROWS) {
+        float l1 = sum_abs<T>(reinterpret_cast<const u4 *>(a.dy.p + row_at(a, a.dy, b, kv, r))[c]);
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) l1 += shfl_xor_f(l1, d);  // whole rows: the lanes of a row leave together
+        top.y = fmaxf(top.y, l1);
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        top.x = fmaxf(top.x, shfl_xor_f(top.x, d));
+        top.y = fmaxf(top.y, shfl_xor_f(top.y, d));
+    }
+    if (lane_id() == 0) of_wave[threadIdx.x / kWave] = top;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < kWaves; ++w) top = f2{fmaxf(top.x, of_wave[w].x), fmaxf(top.y, of_wave[w].y)};
+    a.peak[blockIdx.x] = top;
+}
+// Of the whole source head.
+__device__ __forceinline__ f2 peak_of(const Args &a, int64_t bh) {
+    f2 top{0.0f, 0.0f};
+    for (int i = lane_id(); i < a.peaks; i += kWave) {
+        const f2 x = a.peak[bh * a.peaks + i];
+        top = f2{fmaxf(top.x, x.x), fmaxf(top.y, x.y)};
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        top.x = fmaxf(top.x, shfl_xor_f(top.x, d));
+        top.y = fmaxf(top.y, shfl_xor_f(top.y, d));
+    }
+    return f2{__uint_as_float(uniform(__float_as_uint(top.x))), __uint_as_float(uniform(__float_as_uint(top.y)))};
 }
 
 // ------------------------------------------------------------------------------------------ products
@@ -244,7 +336,8 @@ __device__ __forceinline__ void add_keys(Sums<T, D, MODE> &acc, const Scores<T, 
     add_products<T, D, MODE>(acc, db, db, y1, y1, tr, [](int) {});
 }
 
-// Weights P and DS of 32 streamed rows, whose statistics lie at st, sd in LDS, one of 16 elements a lane at a time.
+// Weights P and DS of 32 streamed rows, whose statistics lie at st, sd in LDS, one of 16 elements a lane at a time.  In
+// binary16 the statistics are of scaled ones, and h is the factor from DP to the statistics' delta.
 template <class T, int D>
 struct Weights {
     f4 lse2[2], delta[2];
@@ -257,10 +350,10 @@ struct Weights {
             delta[e] = *reinterpret_cast<const f4 *>(sd + e * 16 + 4 * g);
         }
     }
-    __device__ __forceinline__ void form(const Scores<T, D> &f, float c, int n) {
+    __device__ __forceinline__ void form(const Scores<T, D> &f, float c, float h, int n) {
         const int qb = n / 8, e = n / 4 % 2, i = n % 4;
         p[n] = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[e][i]));
-        ds[n] = p[n] * (f.dp[e][qb][i] - delta[e][i]);
+        ds[n] = p[n] * (kScaled<T> ? __builtin_fmaf(f.dp[e][qb][i], h, -delta[e][i]) : f.dp[e][qb][i] - delta[e][i]);
         if (n % 2) {
             pw[n / 2] = T::pack(p[n - 1], p[n]);
             dw[n / 2] = T::pack(ds[n - 1], ds[n]);
@@ -275,7 +368,7 @@ struct Weights {
 template <class T, int D>
 __device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)[2][Geo<D>::CH],
                                           const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
-                                          int tr, float c, const float *st, const float *sd, int g) {
+                                          int tr, float c, float h, const float *st, const float *sd, int g) {
     constexpr int kHalf = 32 * Geo<D>::RB, kScore = 16 / Scores<T, D>::kReads, kSum = 16 / kSumReads<T, D, kKeys>;
     Scores<T, D> f0, f1;
     Weights<T, D> w0, w1;
@@ -283,14 +376,14 @@ __device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)
     f0.form(x1, x2, y1, y2, dr, [](int) {});
     f1.form(x1, x2, y1 + kHalf, y2 + kHalf, dr, [&](int i) {
 #pragma unroll
-        for (int n = 0; n < kScore; ++n) w0.form(f0, c, i * kScore + n);
+        for (int n = 0; n < kScore; ++n) w0.form(f0, c, h, i * kScore + n);
     });
     w1.load(st + 32, sd + 32, g);
     auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
     const u4 p0[2] = {operand(w0.pw, 0), operand(w0.pw, 1)}, d0[2] = {operand(w0.dw, 0), operand(w0.dw, 1)};
     add_products<T, D, kKeys>(acc, p0, d0, y1, y2, tr, [&](int i) {
 #pragma unroll
-        for (int n = 0; n < kSum; ++n) w1.form(f1, c, i * kSum + n);
+        for (int n = 0; n < kSum; ++n) w1.form(f1, c, h, i * kSum + n);
     });
     const u4 p1[2] = {operand(w1.pw, 0), operand(w1.pw, 1)}, d1[2] = {operand(w1.dw, 0), operand(w1.dw, 1)};
     add_products<T, D, kKeys>(acc, p1, d1, y1 + kHalf, y2 + kHalf, tr, [](int) {});
@@ -329,7 +422,12 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
 
     // owned operands; columns past the end repeat the last (what they sum is not stored)
     u4 x1[2][G::CH], x2[2][G::CH];
+    f2 peak{0.0f, 0.0f};
+    if constexpr (kScaled<T>) peak = peak_of(a, bh);
+    const int keys_up = kScaled<T> ? up(peak.x * peak.y) : 0;               // the exponent of DS in dk
+    const float h = kScaled<T> ? two_to(keys_up - kUp) : 1.0f;              // P has kUp of it
     float own[2], own_delta[2];
+    int own_up[2] = {0, 0};  // the exponent of DS
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         const int32_t o = min(own0 + w * 32 + qb * 16 + col, own_n - 1);
@@ -349,6 +447,13 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
                 x1[qb][ch] = reinterpret_cast<const u4 *>(p1)[ch * 4 + g];
                 x2[qb][ch] = reinterpret_cast<const u4 *>(p2)[ch * 4 + g];
             }
+            if (!KEYS && kScaled<T>) {
+                float l1 = 0.0f;
+#pragma unroll
+                for (int ch = 0; ch < G::CH; ++ch) l1 += sum_abs<T>(x2[qb][ch]);
+                own_up[qb] = up(column_sum(l1) * peak.x);
+                own[qb] -= static_cast<float>(own_up[qb]);
+            }
             if (MODE == kQuery && !few)
                 own_delta[qb] = column_sum(row_product<T>(x2[qb], a.y.p + row_at(a, a.y, b, kv, o), g));
         }
@@ -363,8 +468,9 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
         for (int qb = 0; qb < 2; ++qb) {
             const int32_t o = own0 + w * 32 + qb * 16 + col;
             if (o < own_n && g == 0) {
-                a.lse2[stat_at(a, b, kv, o)] = own[qb];
-                a.delta[stat_at(a, b, kv, o)] = own_delta[qb];
+                const int64_t at = stat_at(a, b, kv, o);
+                a.lse2[at] = kScaled<T> ? log2_of(a.lse[at]) - kUp : own[qb];
+                a.delta[at] = own_delta[qb] * h;
             }
         }
     };
@@ -431,7 +537,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
         if constexpr (KEYS) {
 #pragma unroll
             for (int kc = 0; kc < G::KC; kc += 2)
-                rows_step<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, dr, tr, c, stats + kc * 32,
+                rows_step<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, dr, tr, c, h, stats + kc * 32,
                                 stats + G::BN + kc * 32, g);
         } else {
 #pragma unroll
@@ -460,7 +566,10 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
                         for (int i = 0; i < 8; ++i) own_delta[qb] += f[kc].s[i / 4][qb][i % 4] * f[kc].dp[i / 4][qb][i % 4];
                 }
 #pragma unroll
-                for (int qb = 0; qb < 2; ++qb) own_delta[qb] = column_sum(own_delta[qb]);
+                for (int qb = 0; qb < 2; ++qb) {
+                    own_delta[qb] = column_sum(own_delta[qb]);
+                    if (kScaled<T>) own_delta[qb] *= two_to(-own_up[qb]);
+                }
                 if (a.dq.p)
 #pragma unroll
                     for (int kc = 0; kc < G::KC; ++kc) add_keys<T, D, MODE>(acc, f[kc], own_delta, y1a + kc * 32 * G::RB, tr);
@@ -494,6 +603,13 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, MODE == kKeys>)) void product
     for (int qb = 0; qb < 2; ++qb) {
         const int32_t o = own0 + w * 32 + qb * 16 + col;
         if (o >= total) continue;
+        if constexpr (kScaled<T>) {
+#pragma unroll
+            for (int d = 0; d < G::DB; ++d) {
+                acc.a1[d][qb] *= two_to(KEYS ? -keys_up : -own_up[qb]);
+                if (KEYS) acc.a2[KEYS ? d : 0][qb] *= two_to(-kUp);
+            }
+        }
         if (a.splits > 1) {
             float *const p = a.part + ((bh * tiles + tile) * a.splits + split) * (KEYS ? 2 : 1) * kOwn * D + (o - own0) * D;
 #pragma unroll
@@ -581,8 +697,12 @@ constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
 struct Layout {
     Plan q, kv;
     float *lse2, *delta, *part;
+    f2 *peak;
+    int64_t peaks;
     size_t bytes;
 };
+// Shares of a source head's peaks: blocks enough to read v and dy at the memory's rate, of 128 rows at least.
+constexpr int64_t kPeakBlocks = 1024, kMostPeaks = 256;
 Layout layout(const tiga_cross &rel, void *ws) {
     Layout l;
     l.q = plan_for(rel, false);
@@ -594,6 +714,12 @@ Layout layout(const tiga_cross &rel, void *ws) {
     // parts of as many items as run at once, whether this problem is split or not: a workspace holds every smaller one
     const size_t parts = static_cast<size_t>(device_cus()) * kOwn * rel.width * 2;
     l.part = c.take<float>(rel.width == 128 ? parts : 2 * parts);
+    const int64_t heads = static_cast<int64_t>(rel.batch) * rel.kv_heads;
+    l.peaks = ceil_div(rel.num_dst * (rel.heads / rel.kv_heads) + rel.num_src, 128);
+    if (heads > 0 && l.peaks > kPeakBlocks / heads) l.peaks = kPeakBlocks / heads;
+    if (l.peaks > kMostPeaks) l.peaks = kMostPeaks;
+    if (l.peaks < 1) l.peaks = 1;
+    l.peak = c.take<f2>(kPeakBlocks + heads);  // not less for a larger problem
     l.bytes = c.bytes();
     return l;
 }
@@ -619,6 +745,10 @@ int products(const Plan &p, Args a, bool timed, hipStream_t stream) {
 template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
     const bool keys = a.dk.p || a.dv.p;
+    if constexpr (kScaled<T>) {
+        hipLaunchKernelGGL((peak_kernel<T, D>), dim3(static_cast<unsigned>(a.batch * a.kv_heads * a.peaks)), dim3(kThreads), 0, stream, a);
+        if (int rc = check_launch("cross attention backward peaks")) return rc;
+    }
     if (a.stats > 0) {
         Plan p = l.q;
         if (!a.dq.p) p.splits = 1;  // the rows' statistics alone
@@ -654,6 +784,8 @@ int cross_backward(const tiga_cross &rel, const tiga_view &q, const tiga_view &k
     a.lse2 = l.lse2;
     a.delta = l.delta;
     a.part = l.part;
+    a.peak = l.peak;
+    a.peaks = static_cast<int32_t>(l.peaks);
     a.num_dst = static_cast<int32_t>(rel.num_dst);
     a.num_src = static_cast<int32_t>(rel.num_src);
     a.batch = rel.batch;

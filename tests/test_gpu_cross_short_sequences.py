@@ -25,7 +25,7 @@ def run(lib, q, k, v, dy, lens=None, want=("dq", "dk", "dv")):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("dt", [BF16])
+@pytest.mark.parametrize("dt", [F16, BF16])
 @pytest.mark.parametrize("N", [1, 40, 300])
 def test_padded_batch(lib, N, D, dt):
     """Peaked weights: where one source has nearly all of a row's weight, ds is small against delta's terms."""
