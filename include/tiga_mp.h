@@ -426,6 +426,7 @@ size_t tiga_mp_attention_cross_fwd_workspace(const tiga_cross *rel);
  *         of dtype, 16-byte aligned, strides multiples of 8, head and row strides
  *         below 2^31 (row strides of k and v below 2^23); y is overwritten.
  *   lse:  fp32 [batch, heads, num_dst], contiguous, or NULL.
+ * A value that is not finite reaches the rows that see it, as an infinity or NaN.
  * Products of the inputs are exact and summed in fp32; the mass is the fp32 sum
  * of the fp32 weights; the weights enter the value product rounded to dtype.
  * Deterministic.  Requires width 64 or 128 (TIGA_EUNSUPPORTED otherwise), heads

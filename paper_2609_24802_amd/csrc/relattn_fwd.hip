@@ -638,8 +638,9 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
 
         // A load's 1 KB are 4 or 8 rows from a multiple of as many, so in pages of 8 rows or more they lie in one page.
         // Lane r looks load r's page up, a tile ahead of the rows; the entry is read and checked when they are loaded.
-        // Positions past the item's last key read that key (its scores there are masked); a page that the cache does
-        // not have is read from the constant rows.
+        // Positions past the item's last key read that key (its scores there are masked, its value there is cleared
+        // once it has arrived: a weight of 0 times an infinity would be NaN); a page that the cache does not have is
+        // read from the constant rows.
         auto look_up = [&](int kt) -> int32_t {
             if constexpr (PAGED) {
                 const int group = (w * G::LPW + lane % G::LPW) * (1024 / G::RB);
@@ -669,6 +670,13 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
                 load_to_lds16(vp + vo + 8 * vch[r], vb + run);
             }
         };
+        auto clear_past = [&](int kt, uint8_t *vb) {  // of this wavefront's rows of the tile
+            const int32_t left = keys - kt * G::BN;
+            if (left >= G::BN) return;
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r)
+                if (krow[r] >= left) *reinterpret_cast<u4 *>(vb + (w * G::LPW + r) * 1024 + 16 * lane) = u4{0u, 0u, 0u, 0u};
+        };
         auto step = [&](int kt, const uint8_t *kb, const uint8_t *vb) {
             const int32_t k0 = kt * G::BN;
             if (any && k0 < most) tile_step<T, D>(st, q, kb, vb, kr, vr, a.c, k0 + G::BN > least, seen, k0, g);
@@ -681,12 +689,14 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
         }
         for (int kt = pc.t0; kt < pc.t1; kt += 2) {
             loads_arrived();
+            clear_past(kt, v0buf);
             __syncthreads();
             if (kt + 1 < pc.t1) stage(kt + 1, entry, k1buf, v1buf);
             entry = look_up(min(kt + 2, pc.t1 - 1));
             step(kt, k0buf, v0buf);
             if (kt + 1 >= pc.t1) break;
             loads_arrived();
+            clear_past(kt + 1, v1buf);
             __syncthreads();
             if (kt + 2 < pc.t1) stage(kt + 2, entry, k0buf, v0buf);
             entry = look_up(min(kt + 3, pc.t1 - 1));
@@ -843,7 +853,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
         st.m = -__builtin_inff();
         st.l = 0.0f;
 
-        // the step's first key; positions past the last key read that key (masked)
+        // the step's first key; positions past the last key read that key (masked, and its value cleared)
         auto first = [&](int kt) { return (kt * kWaves + w) * G::KW; };
         auto at = [&](int kt, int i) { return min(first(kt) + i, keys - 1); };
         auto look_up = [&](int kt) {
@@ -880,8 +890,13 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
             else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
         };
         auto reads_done = [] { __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
-        auto step = [&](int kt, const u4 (&k)[G::KB][G::CH], const uint8_t *vb) {
+        auto step = [&](int kt, const u4 (&k)[G::KB][G::CH], uint8_t *vb) {
             const int32_t k0 = first(kt);
+            if (k0 < keys && k0 + G::KW > keys) {
+#pragma unroll
+                for (int e = 0; e < G::RUNS; ++e)
+                    if ((e * 1024 + 16 * lane) / G::RB >= keys - k0) *reinterpret_cast<u4 *>(vb + e * 1024 + 16 * lane) = u4{0u, 0u, 0u, 0u};
+            }
             if (k0 < keys) thin_step<T, D>(st, q, k, vb, vr, a.c, k0 + G::KW > least, seen - k0, g);
         };
         u4 ka[G::KB][G::CH], kb[G::KB][G::CH];
