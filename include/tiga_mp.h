@@ -576,9 +576,7 @@ size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t nu
  * A row with a negative position gives y = 0, lse = -inf.  A row that needs a
  * position past the table or a page outside [0, num_pages) gives NaN (nothing
  * is read there).  Rows before dst_ptr[0] and behind dst_ptr[batch] are left as
- * they were.  A value
- * row that is not finite reaches every row of its sequence's new tokens that
- * it shares a tile with: new tokens' values must be finite.
+ * they were.
  * Requires heads a multiple of kv_heads, width 64 or 128, num_dst * heads <
  * 2^31 - 1024, table_width * page_size < 2^31 - 1024,
  * batch < 2^16, scale finite and > 0.
