@@ -34,7 +34,15 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr float kMassCap = 4096.0f;  // largest tile mass of a lane (and so weight) that keeps the reference point
+// Weights are formed against a reference point 2^kLift below the row's largest, and enter the value product in the input
+// type.  binary16 has no normal numbers below 2^-14: a lift of 10 of its 15 bits above 1 keeps weights down to 2^-24 of the
+// largest exact to u, which long contexts need beside a token that nearly all weight goes to and whose value says little.
+// (Without it, a weight of e^-17 becomes 2^-24, 44% more.  Times are the same.)  kMassCap: the largest tile mass of a lane, and so weight,
+// that keeps the point; alike weights at the lift make 32 of it.
+template <class T>
+constexpr float kLift = std::is_same<T, Half16>::value ? 10.0f : 0.0f;
+template <class T>
+constexpr float kMassCap = std::is_same<T, Half16>::value ? 49152.0f : 4096.0f;
 constexpr int kLeastChunk = 4;       // key tiles of a part of a wide item, at least
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -559,7 +567,7 @@ __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<
     for (int qb = 0; qb < 2; ++qb) sum[qb] = weights<T, G::KB>(s, qb, c, st.m[qb], pb);
     // Against the current reference point every weight is at most the lane's sum; up to the cap they stay inside
     // every 16-bit type's range.  A larger sum, or NaN (the first tile, where m = -inf, always), moves the point.
-    if (!__all(sum[0] <= kMassCap && sum[1] <= kMassCap)) {
+    if (!__all(sum[0] <= kMassCap<T> && sum[1] <= kMassCap<T>)) {
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             float mt = s[0][qb][0];
@@ -567,7 +575,7 @@ __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<
             for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[kb][qb][i]);
-            mt = column_max(mt) * c;
+            mt = column_max(mt) * c - kLift<T>;
             if (mt > st.m[qb]) {
                 // nothing seen so far: o is 0, or what add_wild put there
                 const float alpha = st.m[qb] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(st.m[qb] - mt);
@@ -853,7 +861,7 @@ __device__ __forceinline__ void thin_step(ThinState<T, D> &st, const u4 *q, cons
 #pragma unroll
         for (int db = 0; db < G::DB; ++db) st.o[db] *= alpha;
     }
-    const float ref = st.m == -__builtin_inff() ? 0.0f : st.m;  // nothing seen so far: weights of 0
+    const float ref = st.m == -__builtin_inff() ? 0.0f : st.m - kLift<T>;  // nothing seen so far: weights of 0
     u4 pb[G::KC];
 #pragma unroll
     for (int kc = 0; kc < G::KC; ++kc) {
@@ -1018,7 +1026,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
         for (int db = 0; db < G::DB; ++db)  // chunk c of row r at c ^ r (16 rows in one bank cost 0.8 us)
             *reinterpret_cast<f4 *>(mine + col * D + 4 * ((db * 4 + g) ^ col)) = st.o[db];
         if (g == 0) {
-            ml[0][w][col] = st.m;
+            ml[0][w][col] = st.m - kLift<T>;
             ml[1][w][col] = lt;
         }
         __syncthreads();
