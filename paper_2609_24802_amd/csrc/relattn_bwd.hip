@@ -677,7 +677,12 @@ __global__ __launch_bounds__(kThreads) void reduce_kernel(Args a, int tiles) {
 struct Plan {
     int64_t tiles, splits;
 };
-// Owned tiles, and how many parts the streamed axis is cut into where they do not fill the device's blocks.
+// Owned tiles, and how many parts the streamed axis is cut into where they do not fill the device's blocks: as many as run
+// at once, so none above half of those blocks.  Uncut against 2 and 3 parts in us (4096 streamed rows; 512 blocks run at once
+// of width 64, of width 128 512 of dq and 256 of dk and dv): dk and dv of 64 at 256 items 82, 80, 86, at 300 118, 109, 101, at
+// 384 121, 116, 126, at 448 127, 144, 154, at 512 132, 154, 165; of 128 at 128 items 125, 84, 108, at 160 127, 147, 114, at
+// 192 127, 148, 155, at 256 131, 154, 171; dq of 64 at 256 items 76, 64, 69, at 300 97, 93, 83, at 384 98, 94, 102, at 448
+// 102, 113, 116.
 Plan plan_for(const tiga_cross &rel, bool keys) {
     const int64_t heads = static_cast<int64_t>(rel.batch) * rel.kv_heads, rows = rel.num_dst * (rel.heads / rel.kv_heads);
     const int64_t bn = rel.width == 64 ? 128 : 64;

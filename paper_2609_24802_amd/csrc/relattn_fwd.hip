@@ -439,33 +439,32 @@ __device__ __forceinline__ int64_t lse_at(const Args<PAGED> &a, int b, const Seq
 // A row must not take anything from a value that it does not see, but its weight of 0 times an infinity would be NaN.  A
 // tile that some rows of an item see less of than others (the last ones of a causal chunk) is looked through for values
 // that are not finite; where there are any, the rows that see them are given them one by one, and the product gets 0 in their
-// places.  (8 x 64 new tokens over up to 4000, f16: 37.3 us without, 38.1 with; a prompt of 8192 tokens 298 both.)
+// places.  (8 x 64 new tokens over up to 4000, f16: 37.1 us without, 37.4 with; a prompt of 8192 tokens 292 and 294.  By
+// masks and selects: branches on each half held exec masks that spilled, 0.3 us of a single token's 8.2.)
+// Bit 15 of each half that is not finite: adding 0x8000 less the exponent's bits carries into it.
 template <class T>
-__device__ __forceinline__ bool any_wild(u4 x) {
-    bool r = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        constexpr uint32_t E = T::kExponent, H = E << 16;
-        r = r || (x[e] & E) == E || (x[e] & H) == H;
-    }
-    return r;
+__device__ __forceinline__ uint32_t wild(uint32_t x) {
+    return ((x & 0x7fff7fffu) + (0x8000u - T::kExponent) * 0x10001u) & 0x80008000u;
+}
+template <class T>
+__device__ __forceinline__ uint32_t any_wild(u4 x) {
+    return (wild<T>(x[0]) | wild<T>(x[1])) | (wild<T>(x[2]) | wild<T>(x[3]));
 }
 template <class T>
 __device__ __forceinline__ u4 without_wild(u4 x) {
-    constexpr uint32_t E = T::kExponent, H = E << 16;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] &= ((x[e] & E) == E ? 0u : 0xffffu) | ((x[e] & H) == H ? 0u : 0xffff0000u);
+    for (int e = 0; e < 4; ++e) x[e] &= ~((wild<T>(x[e]) >> 15) * 0xffffu);
     return x;
 }
-// o += the values (4 widths) that are not finite.
+// o += the values (4 widths) that are not finite, for a row that sees them.
 template <class T>
-__device__ __forceinline__ void add_wild(f4 &o, u2 x) {
+__device__ __forceinline__ void add_wild(f4 &o, u2 x, bool sees) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        constexpr uint32_t E = T::kExponent, H = E << 16;
+        const uint32_t m = sees ? wild<T>(x[e]) : 0u;
         const f2 v = T::unpack(x[e]);
-        if ((x[e] & E) == E) o[2 * e] += v.x;
-        if ((x[e] & H) == H) o[2 * e + 1] += v.y;
+        o[2 * e] += m & 0x8000u ? v.x : 0.0f;
+        o[2 * e + 1] += m >> 16 ? v.y : 0.0f;
     }
 }
 
@@ -723,14 +722,14 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
         auto tidy = [&](int kt, uint8_t *vb, int *found) {
             if (kt < edge) return;
             const int32_t left = keys - kt * G::BN;
-            bool bad = false;
+            uint32_t bad = 0;
 #pragma unroll
             for (int r = 0; r < G::LPW; ++r) {
                 if (krow[r] >= left) *own_rows(vb, r) = u4{0u, 0u, 0u, 0u};
-                else if (PAGED) bad = bad || any_wild<T>(*own_rows(vb, r));
+                if (PAGED) bad |= any_wild<T>(*own_rows(vb, r));
             }
             if (PAGED) {
-                const bool here = __any(bad);
+                const bool here = __any(bad != 0);
                 if (lane == 0) found[w] = here;
             }
         };
@@ -743,7 +742,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<PAGED> a) {
                     const u2 x = *reinterpret_cast<const u2 *>(vb + k * G::RB + 16 * v_chunk<D>(k, 2 * db + g / 2) + 8 * (g % 2));
 #pragma unroll
                     for (int qb = 0; qb < 2; ++qb)
-                        if (kt * G::BN + k < seen[qb]) add_wild<T>(st.o[db][qb], x);
+                        add_wild<T>(st.o[db][qb], x, kt * G::BN + k < seen[qb]);
                 }
             __syncthreads();
 #pragma unroll
@@ -958,8 +957,8 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
                 for (int ch = 0; ch < G::CH; ++ch) k[kb][ch] = reinterpret_cast<const u4 *>(p)[ch * 4 + g];
             }
         };
-        // Loads of the step before the one just issued have arrived (the issued ones, and a paged call's look-up before
-        // them, may be in flight), and this wavefront's LDS reads are done, so its other buffer may be filled.
+        // Loads of the step before the one just issued have arrived.  The issued ones may be in flight; a paged call's look-up
+        // was issued before them, so it has arrived too.
         auto arrived = [&](bool more) {
             if (more) __asm__ volatile("s_waitcnt vmcnt(%0)" ::"i"(G::LOADS) : "memory");
             else __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -974,15 +973,15 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<PAGED> a) {
             }
             if constexpr (PAGED) {
                 if (least < keys && k0 < keys && k0 + G::KW > least) {
-                    bool bad = false;
+                    uint32_t bad = 0;
 #pragma unroll
-                    for (int e = 0; e < G::RUNS; ++e) bad = bad || any_wild<T>(*reinterpret_cast<const u4 *>(vb + e * 1024 + 16 * lane));
-                    if (__any(bad)) {
+                    for (int e = 0; e < G::RUNS; ++e) bad |= any_wild<T>(*reinterpret_cast<const u4 *>(vb + e * 1024 + 16 * lane));
+                    if (__any(bad != 0)) {
                         for (int i = 0; i < G::KW; ++i)
 #pragma unroll
                             for (int db = 0; db < G::DB; ++db) {
                                 const u2 x = *reinterpret_cast<const u2 *>(vb + i * G::RB + 16 * v_chunk<D>(i, 2 * db + g / 2) + 8 * (g % 2));
-                                if (k0 + i < seen) add_wild<T>(st.o[db], x);
+                                add_wild<T>(st.o[db], x, k0 + i < seen);
                             }
 #pragma unroll
                         for (int e = 0; e < G::RUNS; ++e) {
@@ -1281,7 +1280,10 @@ Parts carve(void *ws, int64_t slots) {
 // The tile shape: narrow where a sequence has at most 16 rows for a source head (on average, where the host does not know
 // more).  Narrow against wide in us, width 128, 4 source heads: at 16 rows 35 and 34 (16 x 4096 keys), 91 and 98 (2 x
 // 100,000), 15 and 20 (1 x 4001); at 24 rows 42 and 37, 138 and 99, 16 and 20, where a narrow tile reads the keys twice.
-// Unequal sequences that fill the device uncut (64 of up to 8192 keys, 8 heads): 156 and 235 at 4 rows.
+// Unequal sequences that fill the device uncut (64 of up to 8192 keys, 8 heads): 156 and 235 at 4 rows; cut ones (63 of up to
+// 4096 keys, 4 heads) 71 and 67.  The mean is no good guide where a chunk stands beside single tokens: 63 of them and a chunk
+// of 190, 4 rows to a token, up to 4096 keys 110 (narrow, mean 16) and 81, up to 16,384 keys 364 and 247; a chunk of 260,
+// which the mean makes wide, 119 and 91.
 constexpr int64_t kThinRows = 16;
 
 template <class F>
