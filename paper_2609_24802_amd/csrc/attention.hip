@@ -37,6 +37,7 @@
 //  - Causal blocks are scheduled heaviest first, and each XCD takes a contiguous range of
 //    (head, query tile) tasks, so the K/V tiles of a head are shared in that XCD's L2.
 #include "attention.hpp"
+#include "mfma16.hpp"
 
 namespace tiga {
 namespace attention {
@@ -51,34 +52,11 @@ constexpr float kMassCap = 4096.0f;    // largest tile mass (and so weight) of t
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef float f4 __attribute__((ext_vector_type(4)));
-typedef float f2 __attribute__((ext_vector_type(2)));
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-
-// The 16-bit input type: MFMA and the packed fp32 -> 16-bit conversion (round to nearest even).
-struct F16 {
-    static __device__ __forceinline__ f4 mma(u4 a, u4 b, f4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ uint32_t pack(float a, float b) {
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), h2));
-    }
+// The 16-bit input types, with the all-ones operand that sums weights.
+struct F16 : Half16 {
     static __device__ __forceinline__ u4 ones() { return u4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}; }
 };
-struct BF16 {
-    static __device__ __forceinline__ f4 mma(u4 a, u4 b, f4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ uint32_t pack(float a, float b) {
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));
-    }
+struct BF16 : Brain16 {
     static __device__ __forceinline__ u4 ones() { return u4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}; }
 };
 
@@ -99,16 +77,6 @@ struct Geo {
     static constexpr int LDS = 4 * TILE;                 // two buffers of (K, V)
 };
 
-// Maximum over the four lanes l, l^16, l^32, l^48 (the lanes that share a query column), with
-// the gfx950 lane swaps (VALU, no LDS round trip): each swap returns, per lane, its own value and
-// its partner's.
-__device__ __forceinline__ float max_over_column(float v) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
 // LDS layouts (no padding; XOR swizzles keep the operand reads free of bank conflicts):
 //  - K tile, row-major (key, width): the 16-byte chunk c of key row k sits at chunk
 //    c ^ ((k / R) % CPR).  The score product reads 16 consecutive keys at one chunk, which then
@@ -124,12 +92,6 @@ template <int D>
 __device__ __forceinline__ int v_chunk(int k, int pc) {
     using G = Geo<D>;
     return (((pc >> 1) ^ ((k / G::R) % G::NB)) << 1) | (pc & 1);
-}
-
-// 16 bytes per lane from global memory straight into LDS: lane t writes bytes [16 t, 16 t + 16)
-// of the 1-KB run at `run` (a wavefront-uniform LDS address).
-__device__ __forceinline__ void lds_load16(const void *src, uint8_t *run) {
-    __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)run, 16, 0, 0);
 }
 
 // gfx950 transposing LDS read of 16-bit data: within each group of 16 lanes, lane i receives, in
@@ -183,8 +145,8 @@ __device__ __forceinline__ void stage_kv(const u4 *__restrict__ kh, const u4 *__
 #pragma unroll
         for (int r = 0; r < G::LPW; ++r) {
             const int run = (w * G::LPW + r) * 1024;
-            lds_load16(kt + ko[r], kl + run);
-            lds_load16(vt + vo[r], vl + run);
+            load_to_lds16(kt + ko[r], kl + run);
+            load_to_lds16(vt + vo[r], vl + run);
         }
     } else {
         // keys past n read the last row instead: their scores are masked to -inf, so their
@@ -196,8 +158,8 @@ __device__ __forceinline__ void stage_kv(const u4 *__restrict__ kh, const u4 *__
             const int k = (run + 16 * lane) / G::RB;
             const int pc = ((run + 16 * lane) % G::RB) / 16;
             const int key = k < last ? k : last;
-            lds_load16(kt + key * G::CPR + k_chunk<D>(k, pc), kl + run);
-            lds_load16(vt + key * G::CPR + v_chunk<D>(k, pc), vl + run);
+            load_to_lds16(kt + key * G::CPR + k_chunk<D>(k, pc), kl + run);
+            load_to_lds16(vt + key * G::CPR + v_chunk<D>(k, pc), vl + run);
         }
     }
 }
@@ -342,7 +304,7 @@ __device__ __forceinline__ void softmax_of(State<T, D> &st, const f4 (*s)[2], u4
             for (int kb = 0; kb < G::KB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[kb][qb][i]);
-            mt = max_over_column(mt) * c;
+            mt = column_max(mt) * c;
             if (mt > st.m[qb]) {
                 const float alpha = __builtin_amdgcn_exp2f(st.m[qb] - mt);
                 st.m[qb] = mt;

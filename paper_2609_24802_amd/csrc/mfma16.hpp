@@ -10,9 +10,9 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 
-// A 16-bit type (kExponent: its exponent's bits, all set where a number is not finite): MFMA 16x16x32 with fp32 accumulation (A: 16 rows x 32, lane l holds row l % 16, elements
-// 8 (l / 16) + 0..7; B: 32 x 16, column l % 16 likewise; C: rows 4 (l / 16) + 0..3 of column l % 16), and
-// the packed fp32 -> 16-bit conversion (round to nearest even).
+// A 16-bit type: MFMA 16x16x32 with fp32 accumulation (A: 16 rows x 32, lane l holds row l % 16, elements
+// 8 (l / 16) + 0..7; B: 32 x 16, column l % 16 likewise; C: rows 4 (l / 16) + 0..3 of column l % 16), the packed
+// fp32 -> 16-bit conversion (round to nearest even) and back, and the exponent's bits, all set where a number is not finite.
 struct Half16 {
     static constexpr uint32_t kExponent = 0x7c00u;
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
