@@ -836,7 +836,7 @@ def tiga_mp_attention_paged_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.
 
     q: [heads, rows, width] (layout "hnd"; "nhd" has rows first) packed as in tiga_mp_cache_append, heads a
     multiple of the cache's; the row at position p reads positions 0 to p of its sequence.  Rows before
-    dst_ptr[0] and behind dst_ptr[batch] are left as y has them (uninitialized without y).  Returns y in q's shape (and lse fp32 [heads, rows])."""
+    dst_ptr[0] and behind dst_ptr[batch] are left as y has them (uninitialized without y, and in lse).  Returns y in q's shape (and lse fp32 [heads, rows])."""
     lib = load()
     axes = _axes(layout, (3,))
     heads, rows, qv = _new_rows(cache, q, "q", axes)
@@ -997,5 +997,6 @@ class RotaryPositions(torch.autograd.Function):
 
 
 def rotary(x: torch.Tensor, pos: torch.Tensor | None, rot: Rotary, layout: str = "bhnd") -> torch.Tensor:
-    """Differentiable rotary positions; see tiga_mp_rotary_fwd.  Gradients once, not of gradients."""
+    """Differentiable rotary positions; see tiga_mp_rotary_fwd.  Gradients once, not of gradients.  What cross_attention says
+    of graphs holds here too."""
     return RotaryPositions.apply(x, pos, rot, layout)

@@ -23,11 +23,13 @@
 // products S and DP of that tile, in one launch with dq, which takes the same products (and comes first then).  That goes
 // by the sequence's own sources: its gradients do not depend on what else is in the batch.
 //
-// Measured (MI355X), 2 x 16 x 2048 rows, 4 source heads of 8192 keys, width 128, bf16: dk and dv 494 us (1.11 PFLOP/s), dq
-// 333 us (1.24), 836 together; 4 x 16 x 4096 x 4096 x 64: 525 us (1.05) and 392 us (1.05); 4 x 8 x 4096 rows over
-// 77 of 64: delta and dq 21 us (apart 15 and 19), dk and dv 17 and their sums 5.  A large library product reaches 1.2 to
-// 1.4.  Bound by the matrix cores at the clock the load leaves and by LDS reads: each operand read feeds two products,
-// 128 bytes a cycle and compute unit at full matrix rate, which is all that LDS delivers.
+// Measured (MI355X; ranges are of several runs, the first of calls repeated while hot), 2 x 16 x 2048 rows, 4 source heads of
+// 8192 keys, width 128, bf16: dk and dv 487 to 574 us (0.96 to 1.13 PFLOP/s), dq 318 to 356 (1.16 to 1.30), 818 to 930
+// together; binary16 884, with 8 for its range; 4 x 16 x 4096 x 4096 x 64 f16: 512 to 527 us (1.04 to 1.07) and 377 to 389
+// (1.06 to 1.09), 15 for the range; 4 x 8 x 4096 rows over 77 of 64: delta and dq 21 to 22 us (apart 15 and 19), dk and dv 17
+// and their sums 5.  A large library product reaches 1.2 to 1.4.  Bound by the matrix cores at the clock the load leaves and by
+// LDS reads: each operand read feeds two products, 128 bytes a cycle and compute unit at full matrix rate, which is all that
+// LDS delivers.
 //
 // Every sum has a fixed order.  Where the owned tiles do not fill the device, the streamed axis is split, and the parts'
 // fp32 sums go to the workspace and are added by reduce_kernel.
@@ -129,9 +131,8 @@ __device__ __forceinline__ float sum_abs(u4 x) {
 }
 
 // max |v| and max |dy|_1 of a share of a source head's sources and rows; what is not a number is passed over (its results
-// are none either).
-// Bound by reading v and dy once: 2 x 16 x 2048 rows and 4 x 8192 sources of 128, 34 MB
-// in 8 us, of 884; 8 x 449 ragged rows over 1500 of 64, 23 MB in 8 us, of 95.
+// are none either).  Bound by reading v and dy once: 2 x 16 x 2048 rows and 4 x 8192 sources of 128, 34 MB in 8 us, of 884;
+// 8 x 449 ragged rows over 1500 of 64, 23 MB in 8 us, of 95.
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void peak_kernel(Args a) {
     constexpr int L = D / 8, ROWS = kThreads / L;  // 16 bytes a lane
@@ -751,7 +752,8 @@ template <class T, int D>
 int launch(const Layout &l, const Args &a, hipStream_t stream) {
     const bool keys = a.dk.p || a.dv.p;
     if constexpr (kScaled<T>) {
-        hipLaunchKernelGGL((peak_kernel<T, D>), dim3(static_cast<unsigned>(a.batch * a.kv_heads * a.peaks)), dim3(kThreads), 0, stream, a);
+        const dim3 grid(static_cast<unsigned>(a.batch * a.kv_heads * a.peaks));
+        hipLaunchKernelGGL((peak_kernel<T, D>), grid, dim3(kThreads), 0, stream, a);
         if (int rc = check_launch("cross attention backward peaks")) return rc;
     }
     if (a.stats > 0) {

@@ -16,11 +16,12 @@
 // Both are found from the lengths on the device, so a captured call follows lengths that change between replays.  The
 // orders of all sums depend on the sizes, the lengths and the device's compute units alone.
 //
-// Measured (MI355X): wide, 2 x 16 x 2048 rows over 8192 keys of width 128, bf16: 255 us, 1.08 PFLOP/s (a large library
-// product reaches 1.2 to 1.4); a prompt of 8192 tokens, 16 heads: 301 us, 0.91; bound by the matrix cores at the clock
-// the load leaves (2.0 GHz, half their cycles busy) and the dependent chain of a tile, which the second wavefront of
-// the SIMD covers.  Narrow, 64 single tokens over up to 8192 keys, 8 heads of 128: 144 us for 740 MB, 5.1 TB/s (a large
-// copy moves 4.8); one token over 4001 keys: 8.2 us, latency (finding the run 2.7, two dependent loads 2.6, the join 1).
+// Measured (MI355X; ranges are of several runs): wide, 2 x 16 x 2048 rows over 8192 keys of width 128, bf16: 250 to 266 us,
+// 1.03 to 1.10 PFLOP/s (a large library product reaches 1.2 to 1.4); a prompt of 8192 tokens, 16 heads: 292 to 303 us, 0.91
+// to 0.94; bound by the matrix cores at the clock the load leaves (2.0 GHz, half their cycles busy) and the dependent chain
+// of a tile, which the second wavefront of the SIMD covers.  Narrow, 64 single tokens over up to 8192 keys, 8 heads of 128:
+// 142 to 145 us for 740 MB, 5.1 to 5.2 TB/s (a large copy moves 4.8); one token over 4001 keys: 8.2 to 8.8 us, latency
+// (finding the run 2.7, two dependent loads 2.6, the join 1).
 #include <type_traits>
 
 #include "mfma16.hpp"

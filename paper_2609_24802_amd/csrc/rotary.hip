@@ -8,9 +8,9 @@
 // into LDS, and then move 16 bytes a thread and step (a slot: the two 16-byte runs whose elements pair up, or one run
 // of adjacent pairs, or one run behind the rotated part), four steps' loads in flight.  Where there are few rows their
 // heads are spread over more blocks.  Measured (MI355X): 4 x 4096 rows of 40 heads x 128, bf16, 69 us, 4.85 TB/s (a large
-// copy moves 4.84); 61 rows of 36 heads 3.7 us; the append of 64 tokens 5.0 us (a chain of four dependent loads), of 8189
-// tokens 26 us, 3.8 TB/s (element by element and a token a block: 51 us).  Rows that are not 16-byte aligned, or do not divide into such slots, go
-// element by element (a thread a pair).
+// copy moves 4.84); 61 rows of 36 heads 3.6 to 4.2 us; the append of 64 tokens 4.8 to 5.0 us (a chain of four dependent
+// loads), of 8189 tokens 26 us, 3.8 TB/s (element by element and a token a block: 51 us).  Rows that are not 16-byte aligned,
+// or do not divide into such slots, go element by element (a thread a pair).
 #include "mfma16.hpp"
 #include "relation.hpp"
 #include "rotary.hpp"
@@ -269,7 +269,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Pages cache, tiga_view
     };
     __shared__ float c[kMaxPairs], s[kMaxPairs];
     __shared__ Place places[4];
-    const int row0 = (block0 + static_cast<int>(blockIdx.x)) * per_block, here = min(per_block, cache.num_dst - row0), pairs = rot.rot / 2;
+    const int row0 = (block0 + static_cast<int>(blockIdx.x)) * per_block, here = min(per_block, cache.num_dst - row0);
+    const int pairs = rot.rot / 2;
     const int nk = kv_heads * sl.all, nv = kv_heads * whole.all, each = nk + nv + heads * sl.all, items = here * each;
     const tiga_rotary plain{nullptr, 0, TIGA_PAIRS_ADJACENT, 1.0f};
     Move<T> m[kSteps];
@@ -466,7 +467,8 @@ int rotate(int32_t batch, int32_t heads, int64_t rows, int32_t width, int dtype,
         return in_grids(blocks, "rotary", stream, [&](int64_t at, unsigned n) {
             if (runs)
                 hipLaunchKernelGGL(by_runs, dim3(n, parts), dim3(kThreads), 0, stream, x, y, pos, pos_batch, rows, lines,
-                                   static_cast<int>(per_block), heads, static_cast<int>(group), rot, sl, divider(heads), sign, at);
+                                   static_cast<int>(per_block), heads, static_cast<int>(group), rot, sl, divider(heads), sign,
+                                   at);
             else
                 hipLaunchKernelGGL(by_pairs, dim3(n, parts), dim3(kThreads), 0, stream, x, y, pos, pos_batch, rows, total,
                                    heads, static_cast<int>(group), width, rot, sign, at);
@@ -495,12 +497,12 @@ int append(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, con
     auto go = [&](auto by_runs, auto by_pairs) {
         return in_grids(ceil_div(num_dst, per_block), "cache append", stream, [&](int64_t at, unsigned n) {
             if (runs)
-                hipLaunchKernelGGL(by_runs, dim3(n), dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
-                                   cache.kv_heads, q, q_out, static_cast<int>(per_block), sl, whole,
+                hipLaunchKernelGGL(by_runs, dim3(n), dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot,
+                                   q_heads, cache.kv_heads, q, q_out, static_cast<int>(per_block), sl, whole,
                                    divider(static_cast<int32_t>(each)), static_cast<int>(at));
             else
-                hipLaunchKernelGGL(by_pairs, dim3(n), dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot, q_heads,
-                                   cache.kv_heads, q, q_out, cache.width, static_cast<int>(at));
+                hipLaunchKernelGGL(by_pairs, dim3(n), dim3(kThreads), 0, stream, pages_of(cache, num_dst, dst_ptr), k, v, rot,
+                                   q_heads, cache.kv_heads, q, q_out, cache.width, static_cast<int>(at));
         });
     };
     return cache.dtype == TIGA_DT_F16 ? go(append_kernel<F16>, append_pairs_kernel<F16>)
