@@ -115,3 +115,20 @@ def test_captured(lib):
         ref = call()
         torch.cuda.synchronize()
         assert all(torch.equal(out[n], ref[n]) for n in out), i
+
+
+@pytest.mark.parametrize("dt", [F16, torch.bfloat16])
+@pytest.mark.parametrize("S", [60, 900])
+@pytest.mark.parametrize("x", [float("inf"), float("nan")])
+def test_a_cotangent_that_is_not_finite(lib, x, S, dt):
+    """It stays in its row of dq and in its source head's dk and dv, where it shows (a loss scale's overflow is looked for)."""
+    q, k, v, dy = make(1, 4, 2, 100, S, 64, dt, seed=8)
+    _, _, a = run(lib, q, k, v, dy)
+    dy[0, 1, 37, 11] = x
+    _, _, b = run(lib, q, k, v, dy)
+    keep = torch.ones(4, 100, dtype=torch.bool, device="cuda")
+    keep[1, 37] = False
+    assert torch.equal(b["dq"][0][keep], a["dq"][0][keep]) and not bool(torch.isfinite(b["dq"][0, 1, 37]).any())
+    for name in ("dk", "dv"):
+        assert torch.equal(b[name][0, 1], a[name][0, 1])
+    assert not bool(torch.isfinite(b["dk"][0, 0]).any()) and not bool(torch.isfinite(b["dv"][0, 0, :, 11]).any())
