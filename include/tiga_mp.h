@@ -461,6 +461,57 @@ int tiga_mp_attention_cross_bwd(const tiga_cross *rel, const tiga_view *q, const
                                 const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,
                                 size_t ws_bytes, void *stream);
 
+/* --------------------------------------- causal attention of packed sequences */
+
+/* Sequences of different lengths packed along one axis of num_rows rows (tokens):
+ * sequence b is rows [ptr[b], ptr[b + 1]), ptr device int32 [batch + 1],
+ * non-decreasing, within [0, num_rows] (a value outside is taken as the nearer
+ * bound).  Row i reads its sequence's rows up to itself, N(i) = {ptr[b], ..., i};
+ * head h of the queries reads head h / (heads / kv_heads) of the keys and values.
+ * The struct lives in HOST memory. */
+typedef struct {
+    int64_t num_rows;
+    int32_t batch, heads, kv_heads, width;
+    int32_t dtype; /* TIGA_DT_F16 or TIGA_DT_BF16 */
+    const int32_t *ptr;
+} tiga_packed;
+
+/* Workspace bytes for tiga_mp_attention_packed_fwd (0 on error; at most about
+ * 36 MB).  One sized for a call holds every smaller one. */
+size_t tiga_mp_attention_packed_fwd_workspace(const tiga_packed *rel);
+
+/* The online-softmax reducer over the triangular relation of every packed
+ * sequence with itself, otherwise as tiga_mp_attention_cross_fwd.
+ *   q, y: [1, heads, num_rows, width];  k, v: [1, kv_heads, num_rows, width] (the
+ *         views' batch strides are not used), requirements as there; y is
+ *         overwritten and must not overlap the inputs.
+ *   lse:  fp32 [heads, num_rows], contiguous, or NULL.
+ * Rows of no sequence (before ptr[0], behind ptr[batch]) see nothing: y = 0,
+ * lse = -inf; what they hold is not read.  A row takes nothing from rows after it
+ * or of other sequences, whatever they hold.  Deterministic.
+ * Requires width 64 or 128, heads a multiple of kv_heads, num_rows * heads <
+ * 2^31 - 1024, batch < 2^20, scale finite and > 0.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
+int tiga_mp_attention_packed_fwd(const tiga_packed *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+                                 float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes for tiga_mp_attention_packed_bwd (0 on error): about 8 bytes a
+ * row and head.  One sized for a call holds every smaller one. */
+size_t tiga_mp_attention_packed_bwd_workspace(const tiga_packed *rel);
+
+/* Vector-Jacobian product of tiga_mp_attention_packed_fwd, from its y and lse;
+ * formulas, arguments and roundings as tiga_mp_attention_cross_bwd (delta formed
+ * as sum_j p_ij <dy_i, v_j> for the rows of a tile of 128 whose last row sees at
+ * most 128 tokens).  Gradients of rows of no sequence are 0.  What row i holds
+ * reaches the gradients of rows up to i alone, in its own sequence (through its
+ * key and value: of rows from i on).
+ * Deterministic (no atomics).  Requirements and errors as the forward; besides, at
+ * most 2^24 - 1 tiles of 128 rows of a source head. */
+int tiga_mp_attention_packed_bwd(const tiga_packed *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+                                 const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
+                                 const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,
+                                 size_t ws_bytes, void *stream);
+
 /* ----------------------------------------------------------- rotary positions */
 
 /* How the elements of a row pair up (rot elements from the front take part). */

@@ -53,6 +53,11 @@ class _Cross(C.Structure):
                 ("kv_heads", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32), ("src_len", C.c_void_p)]
 
 
+class _Packed(C.Structure):
+    _fields_ = [("num_rows", C.c_int64), ("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("width", C.c_int32), ("dtype", C.c_int32), ("ptr", C.c_void_p)]
+
+
 class _Rotary(C.Structure):
     _fields_ = [("freq", C.c_void_p), ("rot", C.c_int32), ("pairs", C.c_int32), ("amplitude", C.c_float)]
 
@@ -114,6 +119,12 @@ _SIGS = {
     "tiga_mp_attention_cross_bwd_workspace": (C.c_size_t, [C.c_void_p]),
     "tiga_mp_attention_cross_bwd": (C.c_int, [C.c_void_p] * 7 + [C.c_float] + [C.c_void_p] * 4 +
                                     [C.c_size_t, C.c_void_p]),
+    "tiga_mp_attention_packed_fwd_workspace": (C.c_size_t, [C.c_void_p]),
+    "tiga_mp_attention_packed_fwd": (C.c_int, [C.c_void_p] * 4 + [C.c_float] + [C.c_void_p] * 3 +
+                                     [C.c_size_t, C.c_void_p]),
+    "tiga_mp_attention_packed_bwd_workspace": (C.c_size_t, [C.c_void_p]),
+    "tiga_mp_attention_packed_bwd": (C.c_int, [C.c_void_p] * 7 + [C.c_float] + [C.c_void_p] * 4 +
+                                     [C.c_size_t, C.c_void_p]),
     "tiga_rotary_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double,
                                           C.c_double, C.c_void_p]),
     "tiga_mp_rotary_fwd": (C.c_int, [C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int, C.c_void_p, C.c_void_p,
@@ -661,6 +672,68 @@ def tiga_mp_attention_cross_bwd(q, k, v, y, lse, dy, src_len: torch.Tensor | Non
     return out
 
 
+def _packed(q, k, v, ptr, layout):
+    axes = _axes(layout, (3,))
+    (_, H, N, D), qv = _rows(q, "q", axes)
+    dt = _HALF_TYPES.get(q.dtype)
+    if dt is None:
+        raise TypeError("q must be a float16 or bfloat16 tensor")
+    (_, Hk, Nk, Dk), kv = _rows(k, "k", axes, q.dtype)
+    if Nk != N or Dk != D:
+        raise ValueError(f"k has {Nk} rows of width {Dk}, q has {N} of {D}")
+    _, vv = _rows(v, "v", axes, q.dtype, (1, Hk, N, D))
+    _dev(ptr, torch.int32, "ptr")
+    if ptr.dim() != 1 or ptr.numel() < 1:
+        raise ValueError("ptr must be [batch + 1]")
+    _same_device(q.get_device(), k=k, v=v, ptr=ptr)
+    return _Packed(N, ptr.numel() - 1, H, Hk, D, dt, ptr.data_ptr()), qv, kv, vv, axes
+
+
+def tiga_mp_attention_packed_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ptr: torch.Tensor,
+                                 scale: float | None = None, want_lse: bool = False, layout: str = "hnd", ws=None):
+    """Causal attention within packed sequences: whole prompts of different lengths, or training documents.
+
+    q: float16 or bfloat16 [heads, rows, width] (layout "hnd"; "nhd" has rows first); k, v: [kv_heads, rows, width],
+    heads a multiple of kv_heads.  Any strides that are multiples of 8 elements, the width contiguous.  ptr: int32
+    [batch + 1] on the device, sequence b is rows ptr[b] to ptr[b + 1], and a row reads its sequence's rows up to
+    itself.  Rows of no sequence give y = 0, lse = -inf.  scale defaults to width ** -0.5.
+    Returns y in q's shape (and lse fp32 [heads, rows] when want_lse)."""
+    lib = load()
+    rel, qv, kv, vv, axes = _packed(q, k, v, ptr, layout)
+    y, yv = _like(q, axes)
+    lse = q.new_empty((rel.heads, rel.num_rows), dtype=torch.float32) if want_lse else None
+    ref = C.byref
+    ws = _given_or_new(ws, lib.tiga_mp_attention_packed_fwd_workspace, ref(rel), device=q.device)
+    _check(lib.tiga_mp_attention_packed_fwd(ref(rel), ref(qv), ref(kv), ref(vv),
+                                            rel.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
+                                            _ptr(ws), ws.nbytes, _stream()))
+    return (y, lse) if want_lse else y
+
+
+def tiga_mp_attention_packed_bwd(q, k, v, y, lse, dy, ptr: torch.Tensor, scale: float | None = None,
+                                 want=("dq", "dk", "dv"), layout: str = "hnd", ws=None):
+    """The VJP of tiga_mp_attention_packed_fwd for the cotangent dy, from the forward's y and lse; returns a dict of
+    the wanted gradients in the inputs' shapes.  Gradients of rows of no sequence are 0."""
+    lib = load()
+    rel, qv, kv, vv, axes = _packed(q, k, v, ptr, layout)
+    shape = (1, rel.heads, rel.num_rows, rel.width)
+    _, yv = _rows(y, "y", axes, q.dtype, shape)
+    _, dyv = _rows(dy, "dy", axes, q.dtype, shape)
+    _dev(lse, torch.float32, "lse", shape[1:3])
+    _same_device(q.get_device(), y=y, dy=dy, lse=lse)
+    ref = C.byref
+    out, refs = {}, [None, None, None]
+    for i, (name, t) in enumerate((("dq", q), ("dk", k), ("dv", v))):
+        if name in want:
+            out[name], view = _like(t, axes)
+            refs[i] = ref(view)
+    ws = _given_or_new(ws, lib.tiga_mp_attention_packed_bwd_workspace, ref(rel), device=q.device)
+    _check(lib.tiga_mp_attention_packed_bwd(ref(rel), ref(qv), ref(kv), ref(vv), ref(yv), _ptr(lse), ref(dyv),
+                                            rel.width ** -0.5 if scale is None else float(scale), *refs, _ptr(ws),
+                                            ws.nbytes, _stream()))
+    return out
+
+
 def tiga_rotary_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
                             trained: float = 0.0, low: float = 1.0, high: float = 4.0) -> torch.Tensor:
     """Radians a position of each of the rot / 2 pairs: float64 on the host.
@@ -976,6 +1049,35 @@ def cross_attention(q, k, v, src_len: torch.Tensor | None = None, scale: float |
     pass that accumulates into leaves (loss.backward()) must not be captured while an eager graph of the same leaves
     is alive; torch.autograd.grad inside the capture has no such condition."""
     return CrossAttention.apply(q, k, v, src_len, scale, layout)
+
+
+class PackedAttention(torch.autograd.Function):
+    """y_i = sum_{j <= i} softmax_j(scale <q_i, k_j>) v_j within packed sequences (their bounds not differentiated)."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, ptr, scale, layout):
+        y, lse = tiga_mp_attention_packed_fwd(q, k, v, ptr, scale, want_lse=True, layout=layout)
+        ctx.scale, ctx.layout = scale, layout
+        ctx.save_for_backward(q, k, v, ptr, y, lse)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        q, k, v, ptr, y, lse = ctx.saved_tensors
+        want = [n for n, need in zip(("dq", "dk", "dv"), ctx.needs_input_grad) if need]
+        if not want:
+            return None, None, None, None, None, None
+        if _unreadable(dy):
+            dy = dy.clone(memory_format=torch.contiguous_format)
+        g = tiga_mp_attention_packed_bwd(q, k, v, y, lse, dy, ptr, ctx.scale, want=want, layout=ctx.layout)
+        return g.get("dq"), g.get("dk"), g.get("dv"), None, None, None
+
+
+def packed_attention(q, k, v, ptr: torch.Tensor, scale: float | None = None, layout: str = "hnd"):
+    """Differentiable causal attention of packed sequences; see tiga_mp_attention_packed_fwd.  Gradients once, not of
+    gradients.  What cross_attention says of graphs holds here too."""
+    return PackedAttention.apply(q, k, v, ptr, scale, layout)
 
 
 class RotaryPositions(torch.autograd.Function):

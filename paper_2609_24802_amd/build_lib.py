@@ -27,7 +27,7 @@ FLAGS = [
 # per source: results of matrix products in the registers that the vector unit reads, the long-lived sums alone in the
 # others (without it every score of a kernel of more than 256 registers is moved twice: 536 -> 493 us of dk and dv at
 # 2 x 16 x 2048 x 8192 x 128)
-SOURCE_FLAGS = {"relattn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+SOURCE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("relattn_bwd.hip", "relattn_packed_bwd.hip")}
 
 
 def _compile(src: str) -> str:

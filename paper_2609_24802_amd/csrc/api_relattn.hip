@@ -72,6 +72,18 @@ int check_cross(const tiga_cross *rel) {
     return TIGA_OK;
 }
 
+int check_sequences(const char *what, const tiga_packed *rel) {
+    if (!rel) return fail(TIGA_EINVAL, "%s: the relation is required", what);
+    if (rel->num_rows < 0 || rel->batch < 0) return fail(TIGA_EINVAL, "%s: negative size", what);
+    if (int rc = check_heads(what, rel->heads, rel->kv_heads, rel->width, rel->dtype)) return rc;
+    if (rel->num_rows >= kMaxRows || rel->num_rows * rel->heads >= kMaxRows || rel->num_rows * rel->kv_heads >= kMaxRows)
+        return fail(TIGA_EUNSUPPORTED, "%s: num_rows * heads must be < 2^31 - 1024", what);
+    if (rel->batch >= (1 << 20)) return fail(TIGA_EUNSUPPORTED, "%s: batch must be < 2^20", what);
+    if (rel->batch > 0 && (!rel->ptr || (reinterpret_cast<uintptr_t>(rel->ptr) & 3u)))
+        return fail(TIGA_EINVAL, "%s: ptr missing or misaligned", what);
+    return TIGA_OK;
+}
+
 int check_cache(const char *what, const tiga_cache *c) {
     if (!c) return fail(TIGA_EINVAL, "%s: the cache is required", what);
     if (c->num_pages < 0 || c->batch < 0 || c->table_width < 0) return fail(TIGA_EINVAL, "%s: negative size", what);
@@ -183,6 +195,73 @@ int tiga_mp_attention_cross_bwd(const tiga_cross *given, const tiga_view *q, con
     return relattn::cross_backward(*rel, rows ? *q : none, srcs ? *k : none, srcs ? *v : none, rows ? *y : none, lse,
                                    rows ? *dy : none, scale, rows && dq ? *dq : none, srcs && dk ? *dk : none,
                                    srcs && dv ? *dv : none, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t tiga_mp_attention_packed_fwd_workspace(const tiga_packed *rel) {
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
+    return check_sequences("packed attention", rel) ? 0 : relattn::packed_fwd_ws_bytes(*rel);
+}
+
+int tiga_mp_attention_packed_fwd(const tiga_packed *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+                                 float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    EntryScope scope;
+    const char *what = "packed attention";
+    if (int rc = check_sequences(what, rel)) return rc;
+    if (int rc = check_scale(what, scale)) return rc;
+    if (rel->heads == 0 || rel->num_rows == 0) return TIGA_OK;
+    if (int rc = check_view(what, "q", q, false, 0, 0, 0)) return rc;
+    if (int rc = check_view(what, "k", k, false, 0, 0, 0)) return rc;
+    if (int rc = check_view(what, "v", v, false, 0, 0, 0)) return rc;
+    if (int rc = check_rows(what, "k", k)) return rc;
+    if (int rc = check_rows(what, "v", v)) return rc;
+    if (int rc = check_view(what, "y", y, true, 1, rel->heads, rel->num_rows)) return rc;
+    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(TIGA_EINVAL, "%s: lse misaligned", what);
+    if (int rc = check_ws(what, ws, ws_bytes, relattn::packed_fwd_ws_bytes(*rel))) return rc;
+    return relattn::packed_forward(*rel, *q, *k, *v, scale, *y, lse, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t tiga_mp_attention_packed_bwd_workspace(const tiga_packed *rel) {
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
+    return check_sequences("packed attention backward", rel) ? 0 : relattn::packed_bwd_ws_bytes(*rel);
+}
+
+int tiga_mp_attention_packed_bwd(const tiga_packed *given, const tiga_view *q, const tiga_view *k, const tiga_view *v,
+                                 const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
+                                 const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,
+                                 size_t ws_bytes, void *stream) {
+    EntryScope scope;
+    const char *what = "packed attention backward";
+    if (int rc = check_sequences(what, given)) return rc;
+    if (int rc = check_scale(what, scale)) return rc;
+    tiga_packed some = *given;
+    const bool unread = some.heads == 0;  // source heads that nothing reads: gradients of 0, as of rows of no sequence
+    if (unread) {
+        some.heads = some.kv_heads;
+        some.batch = 0;
+    }
+    const tiga_packed *const rel = &some;
+    if (rel->heads == 0 || rel->num_rows == 0) return TIGA_OK;
+    const tiga_view none{};
+    if (!unread) {
+        if (int rc = check_view(what, "q", q, false, 0, 0, 0)) return rc;
+        if (int rc = check_view(what, "y", y, false, 0, 0, 0)) return rc;
+        if (int rc = check_view(what, "dy", dy, false, 0, 0, 0)) return rc;
+        if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3u)) return fail(TIGA_EINVAL, "%s: lse missing or misaligned", what);
+        if (dq)
+            if (int rc = check_view(what, "dq", dq, true, 1, rel->heads, rel->num_rows)) return rc;
+    }
+    if (int rc = check_view(what, "k", k, false, 0, 0, 0)) return rc;
+    if (int rc = check_view(what, "v", v, false, 0, 0, 0)) return rc;
+    if (int rc = check_rows(what, "k", k)) return rc;
+    if (int rc = check_rows(what, "v", v)) return rc;
+    if (dk)
+        if (int rc = check_view(what, "dk", dk, true, 1, rel->kv_heads, rel->num_rows)) return rc;
+    if (dv)
+        if (int rc = check_view(what, "dv", dv, true, 1, rel->kv_heads, rel->num_rows)) return rc;
+    if (int rc = check_ws(what, ws, ws_bytes, relattn::packed_bwd_ws_bytes(*rel))) return rc;
+    return relattn::packed_backward(*rel, unread ? none : *q, *k, *v, unread ? none : *y, lse, unread ? none : *dy, scale,
+                                    !unread && dq ? *dq : none, dk ? *dk : none, dv ? *dv : none, ws,
+                                    static_cast<hipStream_t>(stream));
 }
 
 int tiga_cache_validate(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, void *stream) {

@@ -57,6 +57,33 @@ __device__ __forceinline__ float column_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Bit 15 of each half that is not finite: adding 0x8000 less the exponent's bits carries into it.
+template <class T>
+__device__ __forceinline__ uint32_t wild(uint32_t x) {
+    return ((x & 0x7fff7fffu) + (0x8000u - T::kExponent) * 0x10001u) & 0x80008000u;
+}
+template <class T>
+__device__ __forceinline__ uint32_t any_wild(u4 x) {
+    return (wild<T>(x[0]) | wild<T>(x[1])) | (wild<T>(x[2]) | wild<T>(x[3]));
+}
+template <class T>
+__device__ __forceinline__ u4 without_wild(u4 x) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] &= ~((wild<T>(x[e]) >> 15) * 0xffffu);
+    return x;
+}
+// o += the values (4 widths) that are not finite, for a row that sees them.
+template <class T>
+__device__ __forceinline__ void add_wild(f4 &o, u2 x, bool sees) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t m = sees ? wild<T>(x[e]) : 0u;
+        const f2 v = T::unpack(x[e]);
+        o[2 * e] += m & 0x8000u ? v.x : 0.0f;
+        o[2 * e + 1] += m >> 16 ? v.y : 0.0f;
+    }
+}
+
 // 16 bytes per lane from global memory straight into LDS: lane t writes bytes [16 t, 16 t + 16) of the 1-KB
 // run at `run` (a wavefront-uniform LDS address).  Buffers that are read while a load into another is in
 // flight are separate __shared__ arrays, so that the compiler sees that the read need not wait.

@@ -87,6 +87,25 @@ __device__ __forceinline__ Chunk chunk_of(const Pages &c, int b) {
     return Chunk{s, e - s, static_cast<int64_t>(c.length[b]) - (e - s)};
 }
 
+// Sequences packed along the rows' axis: sequence b is rows [ptr[b], ptr[b + 1]).
+struct Packed {
+    Rows k, v;
+    const int32_t *ptr;
+    int32_t batch, num_rows;
+};
+// Rows [first, first + count) of sequence b.  Pointers that run backwards or past num_rows give an empty or a shortened
+// range, never one outside the tensors.
+struct Run {
+    int32_t first, count;
+};
+__device__ __forceinline__ Run run_between(const int32_t *ptr, int b0, int b1, int32_t num_rows) {
+    int32_t s = ptr[b0], e = ptr[b1];
+    s = s < 0 ? 0 : (s > num_rows ? num_rows : s);
+    e = e < s ? s : (e > num_rows ? num_rows : e);
+    return Run{s, e - s};
+}
+__device__ __forceinline__ Run run_of(const Packed &p, int b) { return run_between(p.ptr, b, b + 1, p.num_rows); }
+
 // The table's entry for position pos (>= 0) of sequence b, -1 where the table does not reach.  Only an entry that
 // is_page() accepts names a page; the check is apart so that a look-up ahead of its use need not wait for the load.
 __device__ __forceinline__ int32_t entry_at(const Pages &c, int b, int64_t pos) {

@@ -1,0 +1,686 @@
+// Vector-Jacobian product of causal attention within packed sequences.  With p_ij = exp(s_ij - lse_i) for j <= i, 0 after,
+// delta_i = <dy_i, y_i> and ds_ij = p_ij (<dy_i, v_j> - delta_i):
+//   dq_i = scale sum_{j <= i} ds_ij k_j,   dk_j = scale sum_{i >= j} ds_ij q_i,   dv_j = sum_{i >= j} p_ij dy_i,
+// i over the tokens of every head that shares source head j's.  The products are those of the rectangular relation
+// (relattn_bwd.hpp): dq with 128 rows owned and the keys up to the diagonal streamed, then dk, dv with 128 keys owned and
+// the rows from the last token back to the diagonal streamed, so that tiles of one source head that run together read the
+// same rows.  Only tiles that the diagonal cuts are masked.
+//
+// An item is one owned tile of a sequence and source head.  Its work grows linearly along a sequence, so items start in the
+// order of their remaining tiles, the longest of 64 sequences first.
+#include "relation.hpp"
+#include "relattn.hpp"
+#include "relattn_bwd.hpp"
+
+namespace tiga {
+namespace relattn {
+
+namespace {
+
+struct Args {
+    Rows q, k, v, y, dy, dq, dk, dv;  // one packed axis: the batch strides are not used
+    const float *lse;
+    const int32_t *ptr;
+    float *lse2, *delta;  // [heads * num_rows + 1]: the last is what rows past the end have (no weight)
+    f2 *peak;             // [kv_heads][slots]: of 128 tokens' values and cotangents (binary16)
+    int32_t slots;
+    int32_t num_rows, batch, kv_heads;
+    Divider group;
+    int64_t stats;        // heads * num_rows
+    float scale;
+};
+
+// Row r of a sequence's source head is token r / group of head r % group of its group.
+__device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int32_t first, int kv, int32_t r) {
+    const int32_t d = static_cast<int32_t>(a.group.d), token = a.group.div(r), g = r - token * d;
+    // row and head strides are below 2^31
+    return static_cast<int64_t>(kv * d + g) * static_cast<int32_t>(t.head) +
+           static_cast<int64_t>(first + token) * static_cast<int32_t>(t.row);
+}
+__device__ __forceinline__ int64_t stat_at(const Args &a, int32_t first, int kv, int32_t r) {
+    const int32_t d = static_cast<int32_t>(a.group.d), token = a.group.div(r), g = r - token * d;
+    return static_cast<int64_t>(kv * d + g) * a.num_rows + first + token;
+}
+
+// ------------------------------------------------------------------------------------------ items
+
+// An owned tile of a sequence: `level` is how many tiles of the sequence it has to go with itself, of `tiles`.
+struct Item {
+    Run run;
+    int32_t b, kv, level, tiles;  // level 0: there is no such item
+};
+// Item `id` of tiles of 128 / mult tokens.  Sequences are taken 64 at a time, which start at or behind what the sequences
+// before them need at most; of 64, the tiles with the most levels come first: F(L) = sum of max(0, tiles - L) have more
+// than L, so the level of the n-th is the smallest L with F(L) <= n.
+__device__ __forceinline__ Item item_of(const Args &a, int32_t mult, int32_t id) {
+    const int lane = lane_id();
+    Item it{Run{0, 0}, 0, id % a.kv_heads, 0, 0};
+    int32_t n = id / a.kv_heads;
+    if (a.batch == 0) return it;
+    auto start = [&](int chunk) {
+        int32_t s = a.ptr[chunk * kWave];
+        s = s < 0 ? 0 : (s > a.num_rows ? a.num_rows : s);
+        return static_cast<int32_t>(static_cast<int64_t>(s) * mult / kOwn) + chunk * kWave;
+    };
+    int lo = 0, hi = (a.batch - 1) / kWave;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (start(mid) <= n) lo = mid;
+        else hi = mid - 1;
+    }
+    const int base = lo * kWave;
+    n -= start(lo);
+    if (n < 0) return it;
+    const Run mine = base + lane < a.batch ? run_between(a.ptr, base + lane, base + lane + 1, a.num_rows) : Run{0, 0};
+    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(mine.count) * mult + kOwn - 1) / kOwn);
+    auto above = [&](int32_t level) { return lane_value(wave_prefix(tiles > level ? tiles - level : 0), kWave - 1); };
+    int32_t from = 0, to = static_cast<int32_t>((static_cast<int64_t>(a.num_rows) * mult + kOwn - 1) / kOwn);
+    while (from < to) {
+        const int32_t mid = from + (to - from) / 2;
+        if (above(mid) <= n) to = mid;
+        else from = mid + 1;
+    }
+    if (from == 0) return it;
+    const int32_t k = n - static_cast<int32_t>(above(from));
+    const uint64_t some = __ballot(tiles >= from);
+    const int before = __popcll(some & ((uint64_t(1) << lane) - 1));
+    const uint64_t hit = __ballot(tiles >= from && before == k);
+    if (hit == 0) return it;
+    const int l = __builtin_ctzll(hit);
+    it.run = Run{__builtin_amdgcn_readlane(mine.first, l), __builtin_amdgcn_readlane(mine.count, l)};
+    it.tiles = __builtin_amdgcn_readlane(tiles, l);
+    it.b = base + l;
+    it.level = from;
+    return it;
+}
+
+// Gradients of rows of no sequence: before ptr[0] and behind ptr[batch].
+template <int D>
+__device__ __forceinline__ void clear_outside(const Args &a, const Rows &t, int64_t heads) {
+    if (!t.p) return;
+    const Run inside = a.batch > 0 ? run_between(a.ptr, 0, a.batch, a.num_rows) : Run{0, 0};
+    const int32_t outside = a.num_rows - inside.count;
+    if (outside == 0) return;
+    const int64_t all = outside * heads * (D / 8);
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+        const int64_t head = i / (D / 8) % heads;
+        int64_t row = i / (D / 8) / heads;
+        if (row >= inside.first) row += inside.count;
+        reinterpret_cast<u4 *>(const_cast<uint16_t *>(t.p) + head * t.head + row * t.row)[i % (D / 8)] = u4{0u, 0u, 0u, 0u};
+    }
+}
+
+// ------------------------------------------------------------------------------------------ range of binary16
+
+// Where the peaks of 128 tokens lie: the runs of tiles of all sequences, each from at or behind the end of the one before.
+__device__ __forceinline__ int32_t slot_of(const Item &it, int32_t tile) { return it.run.first / kOwn + it.b + tile; }
+
+// max |v| and max |dy|_1 of 128 tokens of a source head.  What is not finite is passed over: the results that it reaches are
+// not finite, and it must not change the scale of the others.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void packed_peak_kernel(Args a) {
+    constexpr int L = D / 8, ROWS = kThreads / L;  // 16 bytes a lane
+    __shared__ f2 of_wave[kWaves];
+    const Item it = item_of(a, 1, static_cast<int32_t>(blockIdx.x));
+    if (it.level == 0) return;
+    const int32_t t0 = (it.tiles - it.level) * kOwn, t1 = min(t0 + kOwn, it.run.count);
+    const int first = static_cast<int>(threadIdx.x) / L, c = static_cast<int>(threadIdx.x) % L;
+    auto finite = [](float x) { return x < __builtin_inff() ? x : 0.0f; };  // of an absolute value; NaN too
+    f2 top{0.0f, 0.0f};
+    const u4 *const v = reinterpret_cast<const u4 *>(a.v.p + it.kv * a.v.head + it.run.first * a.v.row) + c;
+    for (int32_t j = t0 + first; j < t1; j += ROWS) {
+        const u4 x = v[j * (a.v.row / 8)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f2 u = T::unpack(x[e]);
+            top.x = fmaxf(top.x, fmaxf(finite(__builtin_fabsf(u.x)), finite(__builtin_fabsf(u.y))));
+        }
+    }
+    const int32_t d = static_cast<int32_t>(a.group.d);
+#pragma unroll 4
+    for (int32_t r = t0 * d + first; r < t1 * d; r += ROWS) {
+        float l1 = sum_abs<T>(reinterpret_cast<const u4 *>(a.dy.p + row_at(a, a.dy, it.run.first, it.kv, r))[c]);
+#pragma unroll
+        for (int s = 1; s < L; s <<= 1) l1 += shfl_xor_f(l1, s);  // whole rows: the lanes of a row leave together
+        top.y = fmaxf(top.y, finite(l1));
+    }
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+        top.x = fmaxf(top.x, shfl_xor_f(top.x, s));
+        top.y = fmaxf(top.y, shfl_xor_f(top.y, s));
+    }
+    if (lane_id() == 0) of_wave[threadIdx.x / kWave] = top;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < kWaves; ++w) top = f2{fmaxf(top.x, of_wave[w].x), fmaxf(top.y, of_wave[w].y)};
+    a.peak[static_cast<int64_t>(it.kv) * a.slots + slot_of(it, it.tiles - it.level)] = top;
+}
+// Of the whole sequence and source head.
+__device__ __forceinline__ f2 peak_of(const Args &a, const Item &it) {
+    const f2 *const p = a.peak + static_cast<int64_t>(it.kv) * a.slots + slot_of(it, 0);
+    f2 top{0.0f, 0.0f};
+    for (int i = lane_id(); i < (it.run.count + kOwn - 1) / kOwn; i += kWave) top = f2{fmaxf(top.x, p[i].x), fmaxf(top.y, p[i].y)};
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        top.x = fmaxf(top.x, shfl_xor_f(top.x, d));
+        top.y = fmaxf(top.y, shfl_xor_f(top.y, d));
+    }
+    return f2{__uint_as_float(uniform(__float_as_uint(top.x))), __uint_as_float(uniform(__float_as_uint(top.y)))};
+}
+
+// ------------------------------------------------------------------------------------------ tiles in LDS
+
+// This lane's places in a streamed tile: rows and chunks of its direct loads, offsets of its operand reads.
+template <int D>
+struct Places {
+    using G = Geo<D>;
+    int krow[G::LPW], kch[G::LPW], dr, tr;
+    __device__ __forceinline__ Places(int lane, int w) {
+        const int col = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            const int byte = (w * G::LPW + r) * 1024 + 16 * lane;
+            krow[r] = byte / G::RB;
+            kch[r] = byte % G::RB / 16 ^ swizzle<D>(krow[r]);
+        }
+        dr = col * G::RB + 16 * (g ^ swizzle<D>(col));
+        const int trow = 4 * g + col / 4;
+        tr = trow * G::RB + 16 * ((col % 4 / 2) ^ swizzle<D>(trow)) + 8 * (col % 2);
+    }
+};
+// This lane's 16 bytes of its wavefront's load r of a tile.
+template <int D>
+__device__ __forceinline__ u4 *own_rows(uint8_t *tile, int w, int r) {
+    return reinterpret_cast<u4 *>(tile + (w * Geo<D>::LPW + r) * 1024 + 16 * lane_id());
+}
+
+// Tiles that the diagonal cuts hold keys that some rows do not see, and a weight of 0 times an infinity would be NaN.  They
+// are looked through for values that are not finite before the barrier that makes them readable; where there are any, those
+// are replaced by 0 in LDS, and the rows or keys that see them are given NaN, or the value itself, apart.
+// Leaves in *found whether this wavefront's rows of the tile (or two of them) hold one.
+template <class T, int D>
+__device__ __forceinline__ void look_through(uint8_t *t1, uint8_t *t2, int w, int *found) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int r = 0; r < Geo<D>::LPW; ++r) {
+        bad |= any_wild<T>(*own_rows<D>(t1, w, r));
+        if (t2) bad |= any_wild<T>(*own_rows<D>(t2, w, r));
+    }
+    const bool here = __any(bad != 0);
+    if (lane_id() == 0) found[w] = here;
+}
+__device__ __forceinline__ bool any_found(const int *found) { return uniform(found[0] | found[1] | found[2] | found[3]) != 0; }
+
+// ------------------------------------------------------------------------------------------ dq
+
+// P (in the place of the scores) and DP of 32 streamed keys where the diagonal cuts: this lane's rows see the first
+// rel[qb] of the keys from its own 4 g on.  taint (or NULL): 0, or NaN for a key that was not finite.
+template <class T, int D>
+__device__ __forceinline__ void weigh_causal(Scores<T, D> &f, float c, const float *lse2, const int32_t *rel, const float *taint,
+                                             int g) {
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[qb]));
+                if (taint) p += taint[e * 16 + 4 * g + i];
+                const bool sees = e * 16 + i < rel[qb];
+                f.s[e][qb][i] = sees ? p : 0.0f;
+                f.dp[e][qb][i] = sees ? f.dp[e][qb][i] : 0.0f;
+            }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
+    using G = Geo<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t y1a[G::TILE], y2a[G::TILE], y1b[G::TILE], y2b[G::TILE];
+    __shared__ float taint[2][G::BN];
+    __shared__ int found[2][kWaves];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, g = lane >> 4;
+    const int32_t d = static_cast<int32_t>(a.group.d);
+
+    if (blockIdx.x == 0 && threadIdx.x == 0) {  // what rows past the end have
+        a.lse2[a.stats] = __builtin_inff();
+        a.delta[a.stats] = 0.0f;
+    }
+    clear_outside<D>(a, a.dq, static_cast<int64_t>(a.kv_heads) * d);
+    const Item it = item_of(a, d, static_cast<int32_t>(blockIdx.x));
+    if (it.level == 0) return;
+    const int32_t rows = it.run.count * d, own0 = (it.level - 1) * kOwn;
+    const int32_t keys = a.group.div(min(own0 + kOwn, rows) - 1) + 1;  // that the tile's last row sees
+    const int32_t steps = (keys + G::BN - 1) / G::BN;
+    // The rounding of y (of itself and of the weights in it) makes an error of u |dy| |y| of delta, which matters over few
+    // sources: where the tile's keys are few, delta is formed as sum_j p_ij <dy_i, v_j> in fp32, by the tiles' products.
+    const bool few = keys <= kOwn;
+
+    // owned operands; columns past the end repeat the last (what they sum is not stored)
+    u4 x1[2][G::CH], x2[2][G::CH];
+    f2 peak{0.0f, 0.0f};
+    if constexpr (kScaled<T>) peak = peak_of(a, it);
+    const float h = kScaled<T> ? two_to(up(peak.x * peak.y) - kUp) : 1.0f;
+    float own[2], own_delta[2];
+    int own_up[2] = {0, 0};  // the exponent of DS
+    int32_t sees[2];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int32_t o = min(own0 + w * 32 + qb * 16 + col, rows - 1);
+        sees[qb] = a.group.div(o) + 1;
+        own[qb] = log2_of(a.lse[stat_at(a, it.run.first, it.kv, o)]);
+        own_delta[qb] = 0.0f;
+        const uint16_t *const p1 = a.q.p + row_at(a, a.q, it.run.first, it.kv, o);
+        const uint16_t *const p2 = a.dy.p + row_at(a, a.dy, it.run.first, it.kv, o);
+#pragma unroll
+        for (int ch = 0; ch < G::CH; ++ch) {
+            x1[qb][ch] = reinterpret_cast<const u4 *>(p1)[ch * 4 + g];
+            x2[qb][ch] = reinterpret_cast<const u4 *>(p2)[ch * 4 + g];
+        }
+        if constexpr (kScaled<T>) {
+            float l1 = 0.0f;
+#pragma unroll
+            for (int ch = 0; ch < G::CH; ++ch) l1 += sum_abs<T>(x2[qb][ch]);
+            own_up[qb] = up(column_sum(l1) * peak.x);
+            own[qb] -= static_cast<float>(own_up[qb]);
+        }
+        if (!few) own_delta[qb] = column_sum(row_product<T>(x2[qb], a.y.p + row_at(a, a.y, it.run.first, it.kv, o), g));
+    }
+    // The owned rows' statistics, for dk and dv: delta is there.
+    auto leave_stats = [&] {
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const int32_t o = own0 + w * 32 + qb * 16 + col;
+            if (o < rows && g == 0) {
+                const int64_t at = stat_at(a, it.run.first, it.kv, o);
+                a.lse2[at] = kScaled<T> ? log2_of(a.lse[at]) - kUp : own[qb];
+                a.delta[at] = own_delta[qb] * h;
+            }
+        }
+    };
+    if (!few) {
+        leave_stats();
+        if (!a.dq.p) return;
+    }
+    Sums<T, D, kQuery> acc;
+#pragma unroll
+    for (int db = 0; db < G::DB; ++db) acc.a1[db][0] = acc.a1[db][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const Places<D> at(lane, w);
+    const uint16_t *const kb = a.k.p + it.kv * a.k.head + it.run.first * a.k.row;
+    const uint16_t *const vb = a.v.p + it.kv * a.v.head + it.run.first * a.v.row;
+    auto stage = [&](int kt, uint8_t *b1, uint8_t *b2) {
+        const int32_t k0 = kt * G::BN;
+        const uint8_t *const kt0 = reinterpret_cast<const uint8_t *>(kb + k0 * a.k.row);
+        const uint8_t *const vt0 = reinterpret_cast<const uint8_t *>(vb + k0 * a.v.row);
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            const int run = (w * G::LPW + r) * 1024;
+            const uint32_t i = min(at.krow[r], keys - 1 - k0);  // past the end: the last key again, without weight
+            load_to_lds16(kt0 + (2u * i * static_cast<uint32_t>(a.k.row) + 16u * at.kch[r]), b1 + run);
+            load_to_lds16(vt0 + (2u * i * static_cast<uint32_t>(a.v.row) + 16u * at.kch[r]), b2 + run);
+        }
+    };
+    const float c = a.scale * kLog2e;
+    const int32_t least = a.group.div(own0) + 1;                                                  // the tile's first row sees
+    const int32_t my_least = a.group.div(min(own0 + w * 32, rows - 1)) + 1;                       // the wavefront's first row
+    const int32_t my_most = own0 + w * 32 < rows ? a.group.div(min(own0 + w * 32 + 31, rows - 1)) + 1 : 0;
+    auto cut = [&](int kt) { return (kt + 1) * G::BN > least; };
+    // Before and after the barrier that makes a tile readable.
+    auto tidy = [&](int kt, uint8_t *b1, int n) {
+        if (cut(kt)) look_through<T, D>(b1, nullptr, w, found[n]);
+    };
+    auto mend = [&](int kt, uint8_t *b1, int n) -> const float * {
+        if (!cut(kt) || !any_found(found[n])) return nullptr;
+        if (threadIdx.x < G::BN) taint[n][threadIdx.x] = 0.0f;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            u4 *const p = own_rows<D>(b1, w, r);
+            if (any_wild<T>(*p)) {
+                taint[n][at.krow[r]] = __builtin_nanf("");
+                *p = without_wild<T>(*p);
+            }
+        }
+        __syncthreads();
+        return taint[n];
+    };
+    auto form = [&](Scores<T, D> &f, int kt, int kc, const uint8_t *b1, const uint8_t *b2, const float *bad) {
+        f.form(x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, [](int) {});
+        const int32_t k0 = kt * G::BN + kc * 32;
+        if (k0 + 32 > my_least || bad) {
+            const int32_t rel[2] = {sees[0] - k0 - 4 * g, sees[1] - k0 - 4 * g};
+            weigh_causal<T, D>(f, c, own, rel, bad ? bad + kc * 32 : nullptr, g);
+        } else {
+            weigh<T, D>(f, c, own, false, 0, g);
+        }
+    };
+    auto step = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *bad) {
+#pragma unroll
+        for (int kc = 0; kc < G::KC; ++kc) {
+            if (kt * G::BN + kc * 32 >= my_most) continue;
+            Scores<T, D> f;
+            form(f, kt, kc, b1, b2, bad);
+            add_keys<T, D, kQuery>(acc, f, own_delta, b1 + kc * 32 * G::RB, at.tr);
+        }
+    };
+    auto deltas = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *bad) {
+#pragma unroll
+        for (int kc = 0; kc < G::KC; ++kc) {
+            if (kt * G::BN + kc * 32 >= my_most) continue;
+            Scores<T, D> f;
+            form(f, kt, kc, b1, b2, bad);
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) own_delta[qb] += f.s[i / 4][qb][i % 4] * f.dp[i / 4][qb][i % 4];
+        }
+    };
+    stage(0, y1a, y2a);
+    if (few) {  // at most two tiles, both in LDS
+        if (steps > 1) stage(1, y1b, y2b);
+        loads_arrived();
+        tidy(0, y1a, 0);
+        if (steps > 1) tidy(1, y1b, 1);
+        __syncthreads();
+        const float *const bad0 = mend(0, y1a, 0), *const bad1 = steps > 1 ? mend(1, y1b, 1) : nullptr;
+        deltas(0, y1a, y2a, bad0);
+        if (steps > 1) deltas(1, y1b, y2b, bad1);
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            own_delta[qb] = column_sum(own_delta[qb]);
+            if (kScaled<T>) own_delta[qb] *= two_to(-own_up[qb]);
+        }
+        leave_stats();
+        if (!a.dq.p) return;
+        step(0, y1a, y2a, bad0);
+        if (steps > 1) step(1, y1b, y2b, bad1);
+    } else {
+        int kt = 0;
+        // one exit, after a whole turn of both buffers: with another between them the sums are moved and spill
+        for (; kt + 1 < steps; kt += 2) {
+            loads_arrived();
+            tidy(kt, y1a, 0);
+            __syncthreads();
+            stage(kt + 1, y1b, y2b);
+            step(kt, y1a, y2a, mend(kt, y1a, 0));
+            loads_arrived();
+            tidy(kt + 1, y1b, 1);
+            __syncthreads();
+            if (kt + 2 < steps) stage(kt + 2, y1a, y2a);
+            step(kt + 1, y1b, y2b, mend(kt + 1, y1b, 1));
+        }
+        if (kt < steps) {
+            loads_arrived();
+            tidy(kt, y1a, 0);
+            __syncthreads();
+            step(kt, y1a, y2a, mend(kt, y1a, 0));
+        }
+    }
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        const int32_t o = own0 + w * 32 + qb * 16 + col;
+        if (o >= rows) continue;
+        const float f = kScaled<T> ? a.scale * two_to(-own_up[qb]) : a.scale;
+        uint16_t *const p = const_cast<uint16_t *>(a.dq.p) + row_at(a, a.dq, it.run.first, it.kv, o);
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) {
+            const f4 v = acc.a1[db][qb] * f;
+            *reinterpret_cast<u2 *>(p + db * 16 + g * 4) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ dk, dv
+
+// 32 streamed rows that the diagonal cuts: row `r0` and the 31 after it, of which this lane's columns are keys key[qb].
+template <class T, int D>
+__device__ __forceinline__ void rows_cut(Sums<T, D, kKeys> &acc, const u4 (&x1)[2][Geo<D>::CH], const u4 (&x2)[2][Geo<D>::CH],
+                                         const uint8_t *y1, const uint8_t *y2, int dr, int tr, float c, float h,
+                                         const float *st, const float *sd, int g, const Divider &group, int32_t r0,
+                                         const int32_t *key) {
+    Scores<T, D> f;
+    Weights<T, D> w;
+    w.load(st, sd, g);
+    f.form(x1, x2, y1, y2, dr, [](int) {});
+    int32_t token[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) token[i] = group.div(r0 + i / 4 * 16 + 4 * g + i % 4);
+#pragma unroll
+    for (int n = 0; n < 16; ++n) w.form_if(f, c, h, n, key[n / 8] <= token[n % 8]);
+    auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
+    const u4 p[2] = {operand(w.pw, 0), operand(w.pw, 1)}, ds[2] = {operand(w.dw, 0), operand(w.dw, 1)};
+    add_products<T, D, kKeys>(acc, p, ds, y1, y2, tr, [](int) {});
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kernel(Args a) {
+    using G = Geo<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t y1a[G::TILE], y2a[G::TILE], y1b[G::TILE], y2b[G::TILE];
+    __shared__ __attribute__((aligned(256))) float sta[2 * G::BN], stb[2 * G::BN];
+    __shared__ int found[2][kWaves];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, g = lane >> 4;
+    const int32_t d = static_cast<int32_t>(a.group.d);
+
+    clear_outside<D>(a, a.dk, a.kv_heads);
+    clear_outside<D>(a, a.dv, a.kv_heads);
+    const Item it = item_of(a, 1, static_cast<int32_t>(blockIdx.x));
+    if (it.level == 0) return;
+    const int32_t own_n = it.run.count, own0 = (it.tiles - it.level) * kOwn, rows = own_n * d;
+    // row tiles from the last one back to that of the first owned key (128 tokens are whole tiles)
+    const int32_t end = (rows + G::BN - 1) / G::BN, steps = end - own0 / G::BN * d;
+
+    // owned operands; columns past the end repeat the last (what they sum is not stored)
+    u4 x1[2][G::CH], x2[2][G::CH];
+    f2 peak{0.0f, 0.0f};
+    if constexpr (kScaled<T>) peak = peak_of(a, it);
+    const int keys_up = kScaled<T> ? up(peak.x * peak.y) : 0;               // the exponent of DS
+    const float h = kScaled<T> ? two_to(keys_up - kUp) : 1.0f;              // P has kUp of it
+    int32_t key[2];
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        key[qb] = own0 + w * 32 + qb * 16 + col;
+        const int32_t o = it.run.first + min(key[qb], own_n - 1);
+        const uint16_t *const p1 = a.k.p + it.kv * a.k.head + o * a.k.row, *const p2 = a.v.p + it.kv * a.v.head + o * a.v.row;
+#pragma unroll
+        for (int ch = 0; ch < G::CH; ++ch) {
+            x1[qb][ch] = reinterpret_cast<const u4 *>(p1)[ch * 4 + g];
+            x2[qb][ch] = reinterpret_cast<const u4 *>(p2)[ch * 4 + g];
+        }
+    }
+    Sums<T, D, kKeys> acc;
+#pragma unroll
+    for (int db = 0; db < G::DB; ++db)
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) acc.a1[db][qb] = acc.a2[db][qb] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const Places<D> at(lane, w);
+    auto stage = [&](int n, uint8_t *b1, uint8_t *b2, float *stats) {
+        const int32_t k0 = (end - 1 - n) * G::BN;
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            const int run = (w * G::LPW + r) * 1024;
+            const int32_t i = min(k0 + at.krow[r], rows - 1);  // past the end: the last row again, without weight
+            load_to_lds16(a.q.p + row_at(a, a.q, it.run.first, it.kv, i) + 8 * at.kch[r], b1 + run);
+            load_to_lds16(a.dy.p + row_at(a, a.dy, it.run.first, it.kv, i) + 8 * at.kch[r], b2 + run);
+        }
+        // 64 lanes, 4 bytes each: the first half of the needed wavefronts takes lse2, the other delta
+        constexpr int kNeed = 2 * G::BN / kWave;
+        if (w < kNeed) {
+            const int32_t i = k0 + w % (kNeed / 2) * kWave + lane;
+            const int64_t s = i < rows ? stat_at(a, it.run.first, it.kv, i) : a.stats;
+            __builtin_amdgcn_global_load_lds((w < kNeed / 2 ? a.lse2 : a.delta) + s,
+                                             (__attribute__((address_space(3))) void *)(stats + w * kWave), 4, 0, 0);
+        }
+    };
+    const float c = a.scale * kLog2e;
+    // tiles whose first row does not see the last owned key
+    auto cut = [&](int n) { return static_cast<int64_t>(end - 1 - n) * G::BN < static_cast<int64_t>(own0 + kOwn - 1) * d; };
+    auto tidy = [&](int n, uint8_t *b1, uint8_t *b2, int which) {
+        if (cut(n)) look_through<T, D>(b1, b2, w, found[which]);
+    };
+    // A query that is not finite makes its row's weights NaN, a cotangent its ds; dv takes the cotangent itself.
+    auto mend = [&](int n, uint8_t *b1, uint8_t *b2, float *stats, int which) {
+        if (!cut(n) || !any_found(found[which])) return;
+        const int32_t k0 = (end - 1 - n) * G::BN;
+        for (int k = 0; k < G::BN && k0 + k < rows; ++k) {
+            const int32_t token = a.group.div(k0 + k);
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db) {
+                const u2 x = *reinterpret_cast<const u2 *>(b2 + k * G::RB + 16 * ((2 * db + g / 2) ^ swizzle<D>(k)) + 8 * (g % 2));
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb) add_wild<T>(acc.a2[db][qb], x, key[qb] <= token);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            u4 *const p1 = own_rows<D>(b1, w, r), *const p2 = own_rows<D>(b2, w, r);
+            if (any_wild<T>(*p1)) stats[at.krow[r]] = __builtin_nanf("");
+            if (any_wild<T>(*p2)) stats[G::BN + at.krow[r]] = __builtin_nanf("");
+            *p1 = without_wild<T>(*p1);
+            *p2 = without_wild<T>(*p2);
+        }
+        __syncthreads();
+    };
+    auto step = [&](int n, const uint8_t *b1, const uint8_t *b2, const float *stats) {
+        if (cut(n)) {
+            const int32_t k0 = (end - 1 - n) * G::BN;
+#pragma unroll 1
+            for (int kc = 0; kc < G::KC; ++kc)
+                rows_cut<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
+                               stats + G::BN + kc * 32, g, a.group, k0 + kc * 32, key);
+        } else {
+#pragma unroll
+            for (int kc = 0; kc < G::KC; kc += 2)
+                rows_step<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
+                                stats + G::BN + kc * 32, g);
+        }
+    };
+    stage(0, y1a, y2a, sta);
+    int n = 0;
+    for (; n + 1 < steps; n += 2) {
+        loads_arrived();
+        tidy(n, y1a, y2a, 0);
+        __syncthreads();
+        stage(n + 1, y1b, y2b, stb);
+        mend(n, y1a, y2a, sta, 0);
+        step(n, y1a, y2a, sta);
+        loads_arrived();
+        tidy(n + 1, y1b, y2b, 1);
+        __syncthreads();
+        if (n + 2 < steps) stage(n + 2, y1a, y2a, sta);
+        mend(n + 1, y1b, y2b, stb, 1);
+        step(n + 1, y1b, y2b, stb);
+    }
+    if (n < steps) {
+        loads_arrived();
+        tidy(n, y1a, y2a, 0);
+        __syncthreads();
+        mend(n, y1a, y2a, sta, 0);
+        step(n, y1a, y2a, sta);
+    }
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+        if (key[qb] >= own_n) continue;
+        const int32_t o = it.run.first + key[qb];
+        const float f1 = kScaled<T> ? a.scale * two_to(-keys_up) : a.scale, f2 = kScaled<T> ? two_to(-kUp) : 1.0f;
+        uint16_t *const pk = const_cast<uint16_t *>(a.dk.p) + it.kv * a.dk.head + o * a.dk.row;
+        uint16_t *const pv = const_cast<uint16_t *>(a.dv.p) + it.kv * a.dv.head + o * a.dv.row;
+        auto put = [&](uint16_t *p, f4 v) { *reinterpret_cast<u2 *>(p) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])}; };
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) {
+            if (a.dk.p) put(pk + db * 16 + g * 4, acc.a1[db][qb] * f1);
+            if (a.dv.p) put(pv + db * 16 + g * 4, acc.a2[db][qb] * f2);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launch
+
+// A grid counts its threads in 32 bits (and wraps around without an error).
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
+
+// Items of tiles of 128 / mult tokens, at most.
+int64_t most_items(const tiga_packed &rel, int64_t mult) {
+    const int64_t some = rel.num_rows < rel.batch ? rel.num_rows : rel.batch;
+    return (rel.num_rows * mult / kOwn + (rel.batch > kWave ? rel.batch : some)) * rel.kv_heads;
+}
+
+struct Layout {
+    float *lse2, *delta;
+    f2 *peak;
+    int64_t slots;
+    size_t bytes;
+};
+Layout layout(const tiga_packed &rel, void *ws) {
+    Layout l;
+    Carve c(ws);
+    const size_t stats = static_cast<size_t>(rel.heads) * rel.num_rows + 1;
+    l.lse2 = c.take<float>(stats);
+    l.delta = c.take<float>(stats);
+    l.slots = rel.num_rows / kOwn + rel.batch + 1;
+    l.peak = c.take<f2>(l.slots * rel.kv_heads);
+    l.bytes = c.bytes();
+    return l;
+}
+
+template <class T, int D>
+int launch(const tiga_packed &rel, const Args &a, hipStream_t stream) {
+    const int64_t by_keys = most_items(rel, 1), by_rows = most_items(rel, a.group.d);
+    const dim3 keys(static_cast<unsigned>(by_keys < 1 ? 1 : by_keys)), rows(static_cast<unsigned>(by_rows < 1 ? 1 : by_rows));
+    const bool want_keys = a.dk.p || a.dv.p;
+    if constexpr (kScaled<T>) {
+        hipLaunchKernelGGL((packed_peak_kernel<T, D>), keys, dim3(kThreads), 0, stream, a);
+        if (int rc = check_launch("packed attention backward peaks")) return rc;
+    }
+    if (!want_keys) prof_before(stream);
+    hipLaunchKernelGGL((packed_query_kernel<T, D>), rows, dim3(kThreads), 0, stream, a);
+    if (!want_keys) prof_after(stream);
+    if (int rc = check_launch("packed attention backward, dq")) return rc;
+    if (!want_keys) return TIGA_OK;
+    prof_before(stream);
+    hipLaunchKernelGGL((packed_keys_kernel<T, D>), keys, dim3(kThreads), 0, stream, a);
+    prof_after(stream);
+    return check_launch("packed attention backward, dk and dv");
+}
+
+}  // namespace
+
+size_t packed_bwd_ws_bytes(const tiga_packed &rel) { return rel.kv_heads == 0 ? 256 : layout(rel, nullptr).bytes; }
+
+int packed_backward(const tiga_packed &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, const tiga_view &y,
+                    const float *lse, const tiga_view &dy, float scale, const tiga_view &dq, const tiga_view &dk,
+                    const tiga_view &dv, void *ws, hipStream_t stream) {
+    const int32_t group = rel.heads / rel.kv_heads;
+    if (most_items(rel, group) > kMostBlocks || most_items(rel, 1) > kMostBlocks)
+        return fail(TIGA_EUNSUPPORTED, "packed attention backward: at most 2^24 - 1 tiles of 128 rows or sources");
+    const Layout l = layout(rel, ws);
+    Args a{};
+    a.q = rows_of(q);
+    a.k = rows_of(k);
+    a.v = rows_of(v);
+    a.y = rows_of(y);
+    a.dy = rows_of(dy);
+    a.dq = rows_of(dq);
+    a.dk = rows_of(dk);
+    a.dv = rows_of(dv);
+    a.lse = lse;
+    a.ptr = rel.ptr;
+    a.lse2 = l.lse2;
+    a.delta = l.delta;
+    a.peak = l.peak;
+    a.slots = static_cast<int32_t>(l.slots);
+    a.num_rows = static_cast<int32_t>(rel.num_rows);
+    a.batch = rel.batch;
+    a.kv_heads = rel.kv_heads;
+    a.group = divider(group);
+    a.stats = static_cast<int64_t>(rel.heads) * rel.num_rows;
+    a.scale = scale;
+    if (rel.dtype == TIGA_DT_F16) return rel.width == 64 ? launch<Half16, 64>(rel, a, stream) : launch<Half16, 128>(rel, a, stream);
+    return rel.width == 64 ? launch<Brain16, 64>(rel, a, stream) : launch<Brain16, 128>(rel, a, stream);
+}
+
+}  // namespace relattn
+}  // namespace tiga

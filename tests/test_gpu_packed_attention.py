@@ -1,0 +1,234 @@
+"""Causal attention of packed sequences against 64 bits on the CPU; the bounds are derived in relattn_ref."""
+import pytest
+import torch
+
+from tests import relattn_ref as R
+from tests.packed_ref import Packed, check, reference
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+# lengths, heads, source heads, width, type
+CASES = [
+    ([1], 1, 1, 64, F16),
+    ([2], 2, 1, 128, BF16),
+    ([1, 1, 1, 1, 1], 4, 2, 64, BF16),
+    ([5, 17, 16, 33], 4, 2, 128, F16),
+    ([0, 40, 0, 129, 0], 3, 3, 64, F16),
+    ([128], 1, 1, 128, BF16),
+    ([127, 129], 2, 2, 64, F16),
+    ([64, 65, 63], 8, 1, 128, BF16),
+    ([256, 1, 31], 2, 1, 128, F16),
+    ([300, 7], 6, 2, 64, BF16),
+    ([513], 5, 1, 64, F16),
+    ([700, 3, 130], 3, 1, 128, BF16),
+    ([1300], 1, 1, 128, F16),
+    ([1100, 90], 2, 1, 64, BF16),
+    ([1 + 7 * (i % 11) for i in range(70)], 2, 2, 64, F16),
+    ([3 + (i * 37) % 50 for i in range(150)], 1, 1, 128, BF16),
+    ([257] * 3, 32, 2, 64, F16),
+    ([140, 20], 16, 16, 128, BF16),
+]
+
+
+@pytest.mark.parametrize("lens,H,Hk,D,dt", CASES)
+def test_against_64_bits(lib, lens, H, Hk, D, dt):
+    check(lib, Packed(lens, H, Hk, D, dt, seed=len(lens) + D), f"{(len(lens), lens[0], H, Hk, D)}")
+
+
+@pytest.mark.parametrize("D,dt", [(64, F16), (128, BF16)])
+@pytest.mark.parametrize("scale", [0.02, 0.9])
+def test_scales(lib, D, dt, scale):
+    check(lib, Packed([200, 70], 2, 1, D, dt, seed=3), "scale", scale=scale)
+
+
+@pytest.mark.parametrize("lens", [[90, 200], [5, 9], []])
+@pytest.mark.parametrize("H,Hk,D,dt", [(4, 2, 64, F16), (2, 2, 128, BF16)])
+def test_rows_of_no_sequence(lib, lens, H, Hk, D, dt):
+    """They may hold anything, and give 0."""
+    s = Packed(lens, H, Hk, D, dt, seed=5, lead=13, tail=150)
+    ref = reference(s, D ** -0.5)
+    out = s.outside().cuda()
+    for t, bad in ((s.q, float("nan")), (s.k, float("inf")), (s.v, float("nan")), (s.dy, float("-inf"))):
+        t[:, out] = bad
+    check(lib, s, "outside", ref=ref)
+
+
+@pytest.mark.parametrize("H,Hk", [(4, 2), (6, 1)])
+def test_layouts_and_strides(lib, H, Hk):
+    """Rows first, all three side by side: the same bits as from tensors of their own."""
+    s = Packed([150, 33], H, Hk, 64, BF16, seed=6)
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+    g = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)
+    qkv = torch.cat([s.q, s.k, s.v]).permute(1, 0, 2).contiguous()
+    q, k, v = qkv[:, :H], qkv[:, H:H + Hk], qkv[:, H + Hk:]
+    y2, lse2 = lib.tiga_mp_attention_packed_fwd(q, k, v, s.ptr_t, want_lse=True, layout="nhd")
+    dy = s.dy.permute(1, 0, 2).contiguous()
+    g2 = lib.tiga_mp_attention_packed_bwd(q, k, v, y2, lse2, dy, s.ptr_t, layout="nhd")
+    torch.cuda.synchronize()
+    assert torch.equal(y2.permute(1, 0, 2), y) and torch.equal(lse, lse2)
+    for n in g:
+        assert torch.equal(g2[n].permute(1, 0, 2), g[n]), n
+
+
+def test_each_gradient_alone(lib):
+    s = Packed([150, 300], 4, 2, 64, F16, seed=7)
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+    every = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)
+    for want in (("dq",), ("dk",), ("dv",), ("dq", "dv"), ("dk", "dv"), ()):
+        g = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t, want=want)
+        torch.cuda.synchronize()
+        assert set(g) == set(want) and all(torch.equal(g[n], every[n]) for n in want), want
+
+
+def test_a_sequence_does_not_depend_on_the_batch(lib):
+    """Alone or among others: the same bits, where no part is split otherwise."""
+    s = Packed([90, 400, 33], 2, 2, 64, F16, seed=8)
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+    g = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)
+    one = slice(s.ptr[1], s.ptr[2])
+    q, k, v, dy, y1 = (t[:, one].contiguous() for t in (s.q, s.k, s.v, s.dy, y))
+    ptr = torch.tensor([0, 400], dtype=torch.int32, device="cuda")
+    g1 = lib.tiga_mp_attention_packed_bwd(q, k, v, y1, lse[:, one].contiguous(), dy, ptr)
+    torch.cuda.synchronize()
+    for n in g:
+        assert torch.equal(g[n][:, one], g1[n]), n
+
+
+BAD = [float("inf"), float("-inf"), float("nan")]
+
+
+@pytest.mark.parametrize("bad", BAD)
+@pytest.mark.parametrize("at", [0, 40, 200, 299])
+@pytest.mark.parametrize("D,H,Hk,dt", [(64, 2, 1, F16), (128, 1, 1, BF16)])
+def test_what_is_not_finite_reaches_nothing_before_it(lib, bad, at, D, H, Hk, dt):
+    """Row `at` of the second sequence: forward results before it, and gradients that do not depend on it, are those without
+    it (within the bounds: rows that share a wavefront share the steps of their weights' reference points, so a row that is
+    NaN may round its neighbours' weights against another point)."""
+    s = Packed([20, 300, 40], H, Hk, D, dt, seed=9)
+    out, bound = reference(s, D ** -0.5)
+    row = s.ptr[1] + at
+    before = list(range(s.ptr[1])) + list(range(s.ptr[2], s.N))
+    clean = before + list(range(s.ptr[1], row))          # rows that do not see row `at`
+    after = before + list(range(row + 1, s.ptr[2]))      # keys that row `at` does not see
+    other = before + [r for r in range(s.ptr[1], s.ptr[2]) if r != row]
+    for name in ("q", "k", "v", "dy"):
+        t = getattr(s, name)
+        kept = t[:, row].clone()
+        t[0, row, 5] = bad
+        y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+        g = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)
+        torch.cuda.synchronize()
+        t[:, row] = kept
+
+        def right(n, got, rows):
+            R.assert_within(got[:, rows], out[n][:, rows], bound[n][:, rows], f"{name}: {n}")
+
+        right("y", y, clean)
+        right("lse", lse, clean)
+        if name in ("q", "dy"):  # its own row alone, and the keys that it sees
+            right("dq", g["dq"], other)
+            right("dk", g["dk"], after)
+            right("dv", g["dv"], after)
+            if name == "dy":
+                assert not torch.isfinite(g["dv"][0, s.ptr[1]:row + 1, 5]).any()
+            assert not torch.isfinite(g["dk"][0, s.ptr[1]:row + 1, 5]).any(), name
+        else:  # the rows from it on
+            right("dq", g["dq"], clean)
+            # an infinite key may have a score of -inf, and so a weight of 0: then only ds * k is not finite, in element 5
+            assert not torch.isfinite(g["dq"][0, row:s.ptr[2], 5]).any(), name
+
+
+def autograd_in_64_bits(s, scale):
+    leaves = [t.detach().double().cpu().requires_grad_(True) for t in (s.q, s.k, s.v)]
+    g = s.H // s.Hk
+    ys = []
+    for a, e in zip(s.ptr, s.ptr[1:]):
+        q, k, v = (t[:, a:e] for t in leaves)
+        k, v = k.repeat_interleave(g, 0), v.repeat_interleave(g, 0)
+        sc = (q @ k.transpose(1, 2) * scale).masked_fill(torch.ones(e - a, e - a, dtype=torch.bool).triu(1), -torch.inf)
+        ys.append(torch.softmax(sc, -1) @ v)
+    return torch.autograd.grad(torch.cat(ys, 1), leaves, s.dy.double().cpu())
+
+
+def test_autograd_and_differences(lib):
+    """The differentiable function gives the VJP's bits, those agree with automatic differentiation in 64 bits, and that
+    with central differences of the definition."""
+    s = Packed([33, 70], 4, 2, 64, F16, seed=11)
+    scale = 64 ** -0.5
+    y0, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+    g0 = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y0, lse, s.dy, s.ptr_t)
+    leaves = [t.clone().requires_grad_(True) for t in (s.q, s.k, s.v)]
+    y = lib.packed_attention(*leaves, s.ptr_t)
+    g = torch.autograd.grad(y, leaves, s.dy)
+    torch.cuda.synchronize()
+    assert torch.equal(y, y0)
+    out, bound = reference(s, scale)
+    for n, a, e in zip(("dq", "dk", "dv"), g, autograd_in_64_bits(s, scale)):
+        assert torch.equal(a, g0[n]), n
+        R.assert_within(a, e, bound[n], n)
+        R.assert_within(out[n], e, 1e-9 * (1 + e.abs()), "the formula's " + n)
+
+    def loss(q, k, v):
+        t = Packed.__new__(Packed)
+        t.__dict__.update(s.__dict__, q=q, k=k, v=v)
+        return (reference(t, scale, False)[0]["y"] * s.dy.double().cpu()).sum()
+
+    base = [t.double().cpu() for t in (s.q, s.k, s.v)]
+    for i, n in enumerate(("dq", "dk", "dv")):
+        step = torch.zeros_like(base[i])
+        step[1, 40, 7], step[0, 2, 3], step[1, 33, 1] = 1.0, -0.5, 2.0
+        eps = 1e-4
+        moved = [[b + (sign * eps * step if j == i else 0) for j, b in enumerate(base)] for sign in (1, -1)]
+        rate = (loss(*moved[0]) - loss(*moved[1])) / (2 * eps)
+        assert abs(float(rate) - float((out[n] * step).sum())) < 1e-6 * (1 + abs(float(rate))), n
+
+
+def test_needs_and_strided_cotangents(lib):
+    s = Packed([60, 9], 2, 1, 64, BF16, seed=12)
+    q, k, v = s.q.clone().requires_grad_(True), s.k, s.v.clone().requires_grad_(True)
+    y = lib.packed_attention(q, k, v, s.ptr_t)
+    (y.float().transpose(1, 2) * 2.0).sum().backward()    # an expanded cotangent
+    assert q.grad is not None and v.grad is not None and torch.isfinite(q.grad.float()).all()
+
+
+def test_captured(lib):
+    """Lengths that change between replays; eager work in between."""
+    s = Packed([100, 300, 50], 4, 2, 64, BF16, seed=13)
+    sides = [s.ptr, [0, 7, 7, 450], [0, 1, 450, 450]]
+    run = lambda: (lambda y, lse: (y, lse, lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)))(
+        *lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True))
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, lse, g = run()
+    for p in sides + sides[::-1]:
+        s.ptr_t.copy_(torch.tensor(p, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        y2, lse2, g2 = run()
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2) and torch.equal(lse, lse2) and all(torch.equal(g[n], g2[n]) for n in g)
+
+
+def test_on_another_stream(lib):
+    s = Packed([100, 300], 4, 2, 128, BF16, seed=14)
+    y = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y2 = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t)
+    side.synchronize()
+    assert torch.equal(y, y2)
+
+
+def test_pointers_that_run_backwards_stay_inside(lib):
+    """Nothing is promised about such a call but that it stays within the tensors and ends."""
+    s = Packed([100, 60, 40], 2, 1, 64, F16, seed=15)
+    for p in ([0, 160, 100, 200], [-5, 100, 50, 1 << 30], [200, 100, 50, 0], [1 << 30, -1, 1 << 30, 3]):
+        s.ptr_t.copy_(torch.tensor(p, dtype=torch.int32))
+        y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+        lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)
+        torch.cuda.synchronize()
