@@ -29,8 +29,8 @@
  *   - Work is enqueued on `stream` (a hipStream_t passed as void*; NULL is the
  *     null stream).  Calls return before the work completes; a device fault
  *     surfaces at the caller's next synchronization.  Only
- *     tiga_csr_validate(level 2), tiga_radius_neighbors and
- *     tiga_cache_validate synchronize.
+ *     tiga_csr_validate(level 2), tiga_radius_neighbors, tiga_cache_validate and
+ *     tiga_prefix_validate synchronize.
  *   - Outputs are overwritten, never accumulated into.
  *   - fp32 features are row-major [rows, feat], of any width.  Rows need only
  *     the alignment of floats; some paths are faster where feat % 4 == 0 and
@@ -635,6 +635,41 @@ size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t nu
 int tiga_mp_attention_paged_fwd(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,
                                 const tiga_view *q, float scale, const tiga_view *y, float *lse, void *ws,
                                 size_t ws_bytes, void *stream);
+
+/* Groups of neighbouring sequences of a cache whose first positions hold the same
+ * keys and values (a system prompt, a document): sequences [ptr[g], ptr[g + 1])
+ * share their positions below len[g].
+ *   ptr, len: device int32 [groups + 1] (non-decreasing, within [0, batch]; a value
+ *   outside is taken as the nearer bound) and [groups].  Sequences of no group
+ *   share nothing.
+ * Whether the sequences' tables name the same pages or copies does not matter: the
+ * shared positions are read from the pages of a group's first sequence (rounded
+ * down to a multiple of the page size and of 128; the rest, and groups of one
+ * sequence, from each sequence's own).  The struct lives in HOST memory. */
+typedef struct {
+    int32_t groups;
+    const int32_t *ptr;
+    const int32_t *len;
+} tiga_prefix;
+
+/* tiga_cache_validate, and that ptr and len are in range and no sequence with new
+ * tokens has its first one among the shared positions (TIGA_EGRAPH).  That the
+ * shared positions hold the same is not looked at.  Synchronizes `stream`. */
+int tiga_prefix_validate(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst, const int32_t *dst_ptr,
+                         void *stream);
+
+/* Workspace bytes for tiga_mp_attention_prefix_fwd (0 on error): about 36 MB and 4
+ * (width + 1) bytes a row and head.  One sized for a call holds every smaller one. */
+size_t tiga_mp_attention_prefix_fwd_workspace(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst,
+                                              int32_t heads);
+
+/* tiga_mp_attention_paged_fwd with the shared positions of each group read once for
+ * all of its rows.  The results are those of the paged call but for the order of
+ * the sums; a sequence whose first new token is among its shared positions gives
+ * NaN.  Arguments, requirements and errors as there. */
+int tiga_mp_attention_prefix_fwd(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst,
+                                 const int32_t *dst_ptr, int32_t heads, const tiga_view *q, float scale,
+                                 const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------- profiling */
 

@@ -68,6 +68,10 @@ class _Cache(C.Structure):
                 ("table", C.c_void_p), ("length", C.c_void_p)]
 
 
+class _Prefix(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("ptr", C.c_void_p), ("len", C.c_void_p)]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -137,6 +141,10 @@ _SIGS = {
     "tiga_mp_attention_paged_fwd_workspace": (C.c_size_t, [C.c_void_p, C.c_int64, C.c_int32]),
     "tiga_mp_attention_paged_fwd": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_float,
                                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tiga_prefix_validate": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "tiga_mp_attention_prefix_fwd_workspace": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32]),
+    "tiga_mp_attention_prefix_fwd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
+                                               C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tiga_mp_set_kernel_events": (C.c_int, [C.c_void_p, C.c_void_p]),
 }
 
@@ -925,6 +933,53 @@ def tiga_mp_attention_paged_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.
     _check(lib.tiga_mp_attention_paged_fwd(cache.ref, rows, _ptr(dst_ptr), heads, ref(qv),
                                            cache.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
                                            _ptr(ws), ws.nbytes, _stream()))
+    return (y, lse) if want_lse else y
+
+
+def _prefix(cache, group_ptr, group_len):
+    _dev(group_ptr, torch.int32, "group_ptr")
+    if group_ptr.dim() != 1 or group_ptr.numel() < 1:
+        raise ValueError("group_ptr must be [groups + 1]")
+    _dev(group_len, torch.int32, "group_len", (group_ptr.numel() - 1,))
+    _same_device(cache.k_pages.get_device(), group_ptr=group_ptr, group_len=group_len)
+    return _Prefix(group_ptr.numel() - 1, group_ptr.data_ptr(), group_len.data_ptr() if group_len.numel() else None)
+
+
+def tiga_prefix_validate(cache: KvCache, num_dst: int, dst_ptr: torch.Tensor, group_ptr: torch.Tensor,
+                         group_len: torch.Tensor):
+    """tiga_cache_validate, and raise TigaError (TIGA_EGRAPH) if the groups are inconsistent or a sequence's first new
+    token is among its shared positions.  Synchronizes."""
+    _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    _same_device(cache.k_pages.get_device(), dst_ptr=dst_ptr)
+    _check(load().tiga_prefix_validate(cache.ref, C.byref(_prefix(cache, group_ptr, group_len)), int(num_dst),
+                                       _ptr(dst_ptr), _stream()))
+
+
+def tiga_mp_attention_prefix_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch.Tensor, group_ptr: torch.Tensor,
+                                 group_len: torch.Tensor, scale: float | None = None, want_lse: bool = False,
+                                 layout: str = "hnd", y=None, ws=None):
+    """tiga_mp_attention_paged_fwd for sequences of which groups share their first positions (a system prompt, a document):
+    their keys and values are read once a group, for all of its rows.
+
+    Group g is sequences group_ptr[g] to group_ptr[g + 1] (int32 [groups + 1] on the device), whose positions below
+    group_len[g] (int32 [groups]) hold the same, in the same pages or in copies.  New tokens lie behind them (NaN
+    otherwise).  Other arguments and results as tiga_mp_attention_paged_fwd."""
+    lib = load()
+    axes = _axes(layout, (3,))
+    heads, rows, qv = _new_rows(cache, q, "q", axes)
+    _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    if y is None:
+        y, yv = _like(q, axes)
+    else:
+        _, _, yv = _new_rows(cache, y, "y", axes, heads, rows)
+    prefix = _prefix(cache, group_ptr, group_len)
+    _same_device(cache.k_pages.get_device(), q=q, y=y, dst_ptr=dst_ptr)
+    lse = q.new_empty((heads, rows), dtype=torch.float32) if want_lse else None
+    ref = C.byref
+    ws = _given_or_new(ws, lib.tiga_mp_attention_prefix_fwd_workspace, cache.ref, ref(prefix), rows, heads, device=q.device)
+    _check(lib.tiga_mp_attention_prefix_fwd(cache.ref, ref(prefix), rows, _ptr(dst_ptr), heads, ref(qv),
+                                            cache.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
+                                            _ptr(ws), ws.nbytes, _stream()))
     return (y, lse) if want_lse else y
 
 

@@ -120,6 +120,90 @@ int check_packed(const char *what, int64_t num_dst, int32_t heads) {
     return TIGA_OK;
 }
 
+// Sizes of attention over a cache, and its arrays, for a call with rows to work on.
+int check_paged(const char *what, const tiga_cache *cache, int64_t num_dst, int32_t heads) {
+    if (int rc = check_cache(what, cache)) return rc;
+    if (int rc = check_heads(what, heads, cache->kv_heads, cache->width, cache->dtype)) return rc;
+    return check_packed(what, num_dst, heads);
+}
+int check_paged_data(const char *what, const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,
+                     const tiga_view *q, const tiga_view *y, const float *lse) {
+    if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
+    if (int rc = check_view(what, "q", q, false, 0, 0, 0)) return rc;
+    if (int rc = check_view(what, "y", y, true, 1, heads, num_dst)) return rc;
+    if (q->data == y->data && ((heads > 1 && q->head != y->head) || (num_dst > 1 && q->row != y->row)))
+        return fail(TIGA_EINVAL, "%s: y in the place of q needs its strides", what);
+    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(TIGA_EINVAL, "%s: lse misaligned", what);
+    return TIGA_OK;
+}
+
+int check_prefix(const char *what, const tiga_prefix *p) {
+    if (!p) return fail(TIGA_EINVAL, "%s: the groups are required", what);
+    if (p->groups < 0) return fail(TIGA_EINVAL, "%s: negative number of groups", what);
+    if (p->groups >= (1 << 16)) return fail(TIGA_EUNSUPPORTED, "%s: groups must be < 2^16", what);
+    if (p->groups > 0 && (!p->ptr || !p->len || ((reinterpret_cast<uintptr_t>(p->ptr) | reinterpret_cast<uintptr_t>(p->len)) & 3u)))
+        return fail(TIGA_EINVAL, "%s: the groups' ptr or len missing or misaligned", what);
+    return TIGA_OK;
+}
+
+// A cache's call, and the groups that share positions (prefix, or NULL), on the host.
+int validate(const char *what, const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst, const int32_t *dst_ptr,
+             hipStream_t s) {
+    if (int rc = check_cache(what, cache)) return rc;
+    if (int rc = check_packed(what, num_dst, 1)) return rc;
+    if (cache->batch == 0 || cache->kv_heads == 0) return TIGA_OK;  // as the calls, which read nothing then
+    if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
+    const size_t nb = cache->batch, cells = nb * cache->table_width;
+    const size_t groups = prefix ? prefix->groups : 0;
+    std::vector<int32_t> ptr, len, table, group_ptr, group_len;
+    try {
+        ptr.resize(nb + 1);
+        len.resize(nb);
+        table.resize(cells);
+        group_ptr.resize(groups + 1);
+        group_len.resize(groups);
+    } catch (const std::bad_alloc &) {
+        return fail(TIGA_EDEVICE, "%s: no host memory for %zu table entries", what, cells);
+    }
+    int rc = check_hip(hipMemcpyAsync(ptr.data(), dst_ptr, 4 * (nb + 1), hipMemcpyDeviceToHost, s), what);
+    if (!rc && nb) rc = check_hip(hipMemcpyAsync(len.data(), cache->length, 4 * nb, hipMemcpyDeviceToHost, s), what);
+    if (!rc && cells) rc = check_hip(hipMemcpyAsync(table.data(), cache->table, 4 * cells, hipMemcpyDeviceToHost, s), what);
+    if (!rc && groups) rc = check_hip(hipMemcpyAsync(group_ptr.data(), prefix->ptr, 4 * (groups + 1), hipMemcpyDeviceToHost, s), what);
+    if (!rc && groups) rc = check_hip(hipMemcpyAsync(group_len.data(), prefix->len, 4 * groups, hipMemcpyDeviceToHost, s), what);
+    // also after a failed copy: the ones before it write into the vectors
+    const int rs = check_hip(hipStreamSynchronize(s), what);
+    if (rc || rs) return rc ? rc : rs;
+    if (ptr[0] < 0) return fail(TIGA_EGRAPH, "dst_ptr[0] = %d is negative", ptr[0]);
+    for (size_t b = 0; b < nb; ++b) {
+        if (ptr[b + 1] < ptr[b]) return fail(TIGA_EGRAPH, "dst_ptr decreases at sequence %zu", b);
+        if (ptr[b + 1] > num_dst)
+            return fail(TIGA_EGRAPH, "dst_ptr[%zu] = %d passes num_dst = %lld", b + 1, ptr[b + 1], (long long)num_dst);
+        if (len[b] < ptr[b + 1] - ptr[b])
+            return fail(TIGA_EGRAPH, "sequence %zu of length %d has %d new tokens", b, len[b], ptr[b + 1] - ptr[b]);
+        const int64_t need = ceil_div(len[b], cache->page_size);
+        if (need > cache->table_width)
+            return fail(TIGA_EGRAPH, "sequence %zu of length %d needs %lld pages, the table holds %d", b, len[b],
+                        (long long)need, cache->table_width);
+        for (int64_t e = 0; e < need; ++e) {
+            const int32_t id = table[b * cache->table_width + e];
+            if (id < 0 || id >= cache->num_pages)
+                return fail(TIGA_EGRAPH, "page %lld of sequence %zu is %d, outside [0, %lld)", (long long)e, b, id,
+                            (long long)cache->num_pages);
+        }
+    }
+    for (size_t g = 0; g < groups; ++g) {
+        const int32_t g0 = group_ptr[g], g1 = group_ptr[g + 1];
+        if (g0 < 0 || g1 < g0 || g1 > cache->batch)
+            return fail(TIGA_EGRAPH, "group %zu is sequences [%d, %d) of %zu", g, g0, g1, nb);
+        if (group_len[g] < 0) return fail(TIGA_EGRAPH, "group %zu shares %d positions", g, group_len[g]);
+        for (int32_t b = g0; b < g1; ++b)
+            if (ptr[b + 1] > ptr[b] && len[b] - (ptr[b + 1] - ptr[b]) < group_len[g])
+                return fail(TIGA_EGRAPH, "sequence %d has its first new token at %d, among the %d that group %zu shares", b,
+                            len[b] - (ptr[b + 1] - ptr[b]), group_len[g], g);
+    }
+    return TIGA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -266,54 +350,21 @@ int tiga_mp_attention_packed_bwd(const tiga_packed *given, const tiga_view *q, c
 
 int tiga_cache_validate(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, void *stream) {
     EntryScope scope;
-    const char *what = "cache validation";
-    if (int rc = check_cache(what, cache)) return rc;
-    if (int rc = check_packed(what, num_dst, 1)) return rc;
-    if (cache->batch == 0 || cache->kv_heads == 0) return TIGA_OK;  // as the calls, which read nothing then
-    if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
-    const size_t nb = cache->batch, cells = nb * cache->table_width;
-    std::vector<int32_t> ptr, len, table;
-    try {
-        ptr.resize(nb + 1);
-        len.resize(nb);
-        table.resize(cells);
-    } catch (const std::bad_alloc &) {
-        return fail(TIGA_EDEVICE, "%s: no host memory for %zu table entries", what, cells);
-    }
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    int rc = check_hip(hipMemcpyAsync(ptr.data(), dst_ptr, 4 * (nb + 1), hipMemcpyDeviceToHost, s), what);
-    if (!rc && nb) rc = check_hip(hipMemcpyAsync(len.data(), cache->length, 4 * nb, hipMemcpyDeviceToHost, s), what);
-    if (!rc && cells) rc = check_hip(hipMemcpyAsync(table.data(), cache->table, 4 * cells, hipMemcpyDeviceToHost, s), what);
-    // also after a failed copy: the ones before it write into the vectors
-    const int rs = check_hip(hipStreamSynchronize(s), what);
-    if (rc || rs) return rc ? rc : rs;
-    if (ptr[0] < 0) return fail(TIGA_EGRAPH, "dst_ptr[0] = %d is negative", ptr[0]);
-    for (size_t b = 0; b < nb; ++b) {
-        if (ptr[b + 1] < ptr[b]) return fail(TIGA_EGRAPH, "dst_ptr decreases at sequence %zu", b);
-        if (ptr[b + 1] > num_dst)
-            return fail(TIGA_EGRAPH, "dst_ptr[%zu] = %d passes num_dst = %lld", b + 1, ptr[b + 1], (long long)num_dst);
-        if (len[b] < ptr[b + 1] - ptr[b])
-            return fail(TIGA_EGRAPH, "sequence %zu of length %d has %d new tokens", b, len[b], ptr[b + 1] - ptr[b]);
-        const int64_t need = ceil_div(len[b], cache->page_size);
-        if (need > cache->table_width)
-            return fail(TIGA_EGRAPH, "sequence %zu of length %d needs %lld pages, the table holds %d", b, len[b],
-                        (long long)need, cache->table_width);
-        for (int64_t e = 0; e < need; ++e) {
-            const int32_t id = table[b * cache->table_width + e];
-            if (id < 0 || id >= cache->num_pages)
-                return fail(TIGA_EGRAPH, "page %lld of sequence %zu is %d, outside [0, %lld)", (long long)e, b, id,
-                            (long long)cache->num_pages);
-        }
-    }
-    return TIGA_OK;
+    return validate("cache validation", cache, nullptr, num_dst, dst_ptr, static_cast<hipStream_t>(stream));
+}
+
+int tiga_prefix_validate(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst, const int32_t *dst_ptr,
+                         void *stream) {
+    EntryScope scope;
+    const char *what = "prefix validation";
+    if (int rc = check_prefix(what, prefix)) return rc;
+    return validate(what, cache, prefix, num_dst, dst_ptr, static_cast<hipStream_t>(stream));
 }
 
 size_t tiga_mp_attention_paged_fwd_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads) {
     clear_error();  // no EntryScope: armed kernel events are for the call that follows
     const char *what = "paged attention";
-    if (check_cache(what, cache) || check_heads(what, heads, cache->kv_heads, cache->width, cache->dtype) ||
-        check_packed(what, num_dst, heads))
-        return 0;
+    if (check_paged(what, cache, num_dst, heads)) return 0;
     return relattn::paged_fwd_ws_bytes(*cache, num_dst, heads);
 }
 
@@ -322,20 +373,36 @@ int tiga_mp_attention_paged_fwd(const tiga_cache *cache, int64_t num_dst, const 
                                 size_t ws_bytes, void *stream) {
     EntryScope scope;
     const char *what = "paged attention";
-    if (int rc = check_cache(what, cache)) return rc;
-    if (int rc = check_heads(what, heads, cache->kv_heads, cache->width, cache->dtype)) return rc;
-    if (int rc = check_packed(what, num_dst, heads)) return rc;
+    if (int rc = check_paged(what, cache, num_dst, heads)) return rc;
     if (int rc = check_scale(what, scale)) return rc;
     if (cache->batch == 0 || heads == 0 || num_dst == 0) return TIGA_OK;
-    if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
-    if (int rc = check_view(what, "q", q, false, 0, 0, 0)) return rc;
-    if (int rc = check_view(what, "y", y, true, 1, heads, num_dst)) return rc;
-    if (q->data == y->data && ((heads > 1 && q->head != y->head) || (num_dst > 1 && q->row != y->row)))
-        return fail(TIGA_EINVAL, "%s: y in the place of q needs its strides", what);
-    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(TIGA_EINVAL, "%s: lse misaligned", what);
+    if (int rc = check_paged_data(what, cache, num_dst, dst_ptr, heads, q, y, lse)) return rc;
     if (int rc = check_ws(what, ws, ws_bytes, relattn::paged_fwd_ws_bytes(*cache, num_dst, heads))) return rc;
     return relattn::paged_forward(*cache, num_dst, dst_ptr, heads, *q, scale, *y, lse, ws,
                                   static_cast<hipStream_t>(stream));
+}
+
+size_t tiga_mp_attention_prefix_fwd_workspace(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst,
+                                              int32_t heads) {
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
+    const char *what = "prefix attention";
+    if (check_paged(what, cache, num_dst, heads) || check_prefix(what, prefix)) return 0;
+    return relattn::prefix_fwd_ws_bytes(*cache, *prefix, num_dst, heads);
+}
+
+int tiga_mp_attention_prefix_fwd(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst,
+                                 const int32_t *dst_ptr, int32_t heads, const tiga_view *q, float scale,
+                                 const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    EntryScope scope;
+    const char *what = "prefix attention";
+    if (int rc = check_paged(what, cache, num_dst, heads)) return rc;
+    if (int rc = check_prefix(what, prefix)) return rc;
+    if (int rc = check_scale(what, scale)) return rc;
+    if (cache->batch == 0 || heads == 0 || num_dst == 0) return TIGA_OK;
+    if (int rc = check_paged_data(what, cache, num_dst, dst_ptr, heads, q, y, lse)) return rc;
+    if (int rc = check_ws(what, ws, ws_bytes, relattn::prefix_fwd_ws_bytes(*cache, *prefix, num_dst, heads))) return rc;
+    return relattn::prefix_forward(*cache, *prefix, num_dst, dst_ptr, heads, *q, scale, *y, lse, ws,
+                                   static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -106,6 +106,46 @@ __device__ __forceinline__ Run run_between(const int32_t *ptr, int b0, int b1, i
 }
 __device__ __forceinline__ Run run_of(const Packed &p, int b) { return run_between(p.ptr, b, b + 1, p.num_rows); }
 
+// Groups of neighbouring sequences whose first positions hold the same keys and values: group g is sequences
+// [group_ptr[g], group_ptr[g + 1]), which share group_len[g] positions.  Of those, whole pages and whole multiples of 128 are
+// read once, from the first sequence's pages, so that what lies behind them starts at a tile and a page; a group of one
+// sequence shares nothing.
+struct Shared : Pages {  // batch: the groups
+    const int32_t *group_ptr, *group_len;
+    int32_t sequences;   // of the cache
+    int32_t whole;       // log2 of what is shared whole
+    int32_t *skip;       // [sequences]: shared positions of each
+    float *state, *lse2; // [heads, num_dst, width], [heads, num_dst]: what the rows have of the shared positions
+};
+struct Behind : Pages {
+    const int32_t *skip;
+    const float *state, *lse2;
+};
+struct Group {
+    int32_t first, end;  // sequences
+    int32_t shared;      // positions
+};
+__device__ __forceinline__ Group group_of(const Shared &c, int g) {
+    const Run run = run_between(c.group_ptr, g, g + 1, c.sequences);
+    const int64_t most = static_cast<int64_t>(c.table_width) << c.shift;
+    int64_t n = c.group_len[g];
+    n = n < 0 || run.count < 2 ? 0 : (n > most ? most : n);
+    return Group{run.first, run.first + run.count, static_cast<int32_t>(n >> c.whole << c.whole)};
+}
+// Shared positions of every sequence, for the pass over what lies behind them.
+__device__ __forceinline__ void leave_skips(const Shared &c) {
+    for (int b = blockIdx.x * blockDim.x + threadIdx.x; b < c.sequences; b += gridDim.x * blockDim.x) {
+        int lo = 0, hi = c.batch - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (c.group_ptr[mid] <= b) lo = mid;
+            else hi = mid - 1;
+        }
+        const Group g = group_of(c, lo);
+        c.skip[b] = g.first <= b && b < g.end ? g.shared : 0;
+    }
+}
+
 // The table's entry for position pos (>= 0) of sequence b, -1 where the table does not reach.  Only an entry that
 // is_page() accepts names a page; the check is apart so that a look-up ahead of its use need not wait for the load.
 __device__ __forceinline__ int32_t entry_at(const Pages &c, int b, int64_t pos) {

@@ -33,5 +33,9 @@ size_t paged_fwd_ws_bytes(const tiga_cache &cache, int64_t num_dst, int32_t head
 int paged_forward(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads, const tiga_view &q,
                   float scale, const tiga_view &y, float *lse, void *ws, hipStream_t stream);
 
+size_t prefix_fwd_ws_bytes(const tiga_cache &cache, const tiga_prefix &prefix, int64_t num_dst, int32_t heads);
+int prefix_forward(const tiga_cache &cache, const tiga_prefix &prefix, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,
+                   const tiga_view &q, float scale, const tiga_view &y, float *lse, void *ws, hipStream_t stream);
+
 }  // namespace relattn
 }  // namespace tiga

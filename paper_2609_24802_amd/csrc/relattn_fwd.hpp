@@ -56,13 +56,14 @@ struct Strided {
     const int32_t *len;
     int32_t num_dst, num_src, batch;
 };
-// What a call's rows read: a padded batch of other sequences, a cache's pages up to the row's position, or their own
-// sequence's rows of packed sequences up to themselves.
-enum Relation { kStrided, kPaged, kPacked };
+// What a call's rows read: a padded batch of other sequences, a cache's pages up to the row's position, their own
+// sequence's rows of packed sequences up to themselves; and for sequences of which groups share their first positions, those
+// (the rows of all of a group's sequences are one item's) and the pages behind them, from the state that those left.
+enum Relation { kStrided, kPaged, kPacked, kShared, kBehind };
 template <Relation REL>
-constexpr bool kPages = REL == kPaged;
+constexpr bool kPages = REL == kPaged || REL == kShared || REL == kBehind;
 template <Relation REL>
-constexpr bool kCausal = REL != kStrided;
+constexpr bool kCausal = REL == kPaged || REL == kPacked || REL == kBehind;
 template <Relation REL>
 struct SourceArgs {
     typedef Strided type;
@@ -74,6 +75,14 @@ struct SourceArgs<kPaged> {
 template <>
 struct SourceArgs<kPacked> {
     typedef Packed type;
+};
+template <>
+struct SourceArgs<kShared> {
+    typedef Shared type;
+};
+template <>
+struct SourceArgs<kBehind> {
+    typedef Behind type;
 };
 template <Relation REL>
 struct Args {
@@ -118,6 +127,13 @@ __device__ __forceinline__ Seq seq_of(const Args<REL> &a, int b) {
     } else if constexpr (REL == kPacked) {
         const Run run = run_of(a.src, b);
         return Seq{run.first, run.count * static_cast<int32_t>(a.group.d), 1};
+    } else if constexpr (REL == kShared) {
+        const Group g = group_of(a.src, b);
+        const Run run = run_between(a.src.dst_ptr, g.first, g.end, a.src.num_dst);
+        return Seq{run.first, g.shared > 0 ? run.count * static_cast<int32_t>(a.group.d) : 0, g.shared};
+    } else if constexpr (REL == kBehind) {
+        const Chunk ch = chunk_of(a.src, b);
+        return Seq{ch.first, ch.count * static_cast<int32_t>(a.group.d), ch.pos0 + 1 - a.src.skip[b]};
     } else {
         int32_t n = a.src.num_src;
         if (a.src.len) n = a.src.len[b] < 0 ? 0 : (a.src.len[b] > n ? n : a.src.len[b]);
@@ -134,7 +150,7 @@ template <Relation REL>
 __device__ __forceinline__ int32_t keys_of(const Args<REL> &a, const Seq &s, int r) {
     if constexpr (REL == kPacked) {
         return 1 + a.group.div(r);
-    } else if constexpr (REL == kPaged) {
+    } else if constexpr (kCausal<REL>) {
         const int64_t n = s.keys0 + a.group.div(r), most = (static_cast<int64_t>(a.src.table_width) << a.src.shift) + 1;
         return static_cast<int32_t>(n < 0 ? 0 : (n > most ? most : n));
     } else {
@@ -199,7 +215,7 @@ struct Walk {
         return T::template of<REL>(a, q, a.part != nullptr).total() * a.kv_heads;
     }
     static __device__ __forceinline__ bool alike(const Args<REL> &a) {  // every sequence weighs the same
-        if constexpr (kCausal<REL>) return false;
+        if constexpr (REL != kStrided) return false;
         else return !a.src.len || !a.part;
     }
     __device__ __forceinline__ void begin(const Args<REL> &a, int w, int blocks) {
@@ -300,7 +316,7 @@ struct Deal {
         return load(a, e < a.src.batch ? seq_of<REL>(a, e) : Seq{0, 0, 0});
     }
     static __device__ __forceinline__ bool alike(const Args<REL> &a) {
-        if constexpr (kCausal<REL>) return false;
+        if constexpr (REL != kStrided) return false;
         else return a.src.len == nullptr;
     }
     // Sum of f(load) over the sequences, times the heads.
@@ -443,6 +459,21 @@ struct Source {
     }
 };
 
+// The table's entry for an item's position.
+template <Relation REL>
+struct Cells {
+    int32_t row;   // of the table
+    int32_t skip;  // positions of the sequence before position 0 of the item
+    __device__ __forceinline__ Cells(const Args<REL> &a, int b) : row(b), skip(0) {
+        if constexpr (REL == kShared) row = group_of(a.src, b).first;
+        if constexpr (REL == kBehind) skip = a.src.skip[b];
+    }
+    __device__ __forceinline__ int32_t entry(const Args<REL> &a, int32_t pos) const {
+        if constexpr (REL == kBehind) return entry_at(a.src, row, static_cast<int64_t>(pos) + skip);
+        else return entry_at(a.src, row, pos);
+    }
+};
+
 // Start of row r's width in a [heads, rows, width] tensor of destinations, for source head `head`.
 template <Relation REL>
 __device__ __forceinline__ int64_t row_at(const Args<REL> &a, const Rows &t, int b, const Seq &s, int head, int r) {
@@ -454,6 +485,40 @@ __device__ __forceinline__ int64_t lse_at(const Args<REL> &a, int b, const Seq &
     const int d = static_cast<int>(a.group.d), token = a.group.div(r), g = r - token * d;
     return b * a.lse_batch + (head * d + g) * a.lse_head + s.first + token;
 }
+
+// Where row r's results go, 4 widths at a time: y in the input type, or the fp32 state of shared positions; and lse, there in the
+// log2 domain.
+template <int D, Relation REL>
+__device__ __forceinline__ auto out_row(const Args<REL> &a, int b, const Seq &s, int head, int r) {
+    if constexpr (REL == kShared) return a.src.state + lse_at(a, b, s, head, r) * D;
+    else return const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, r);
+}
+template <class T>
+__device__ __forceinline__ void put(uint16_t *p, f4 v) { *reinterpret_cast<u2 *>(p) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])}; }
+template <class T>
+__device__ __forceinline__ void put(float *p, f4 v) { *reinterpret_cast<f4 *>(p) = v; }
+template <Relation REL>
+__device__ __forceinline__ void put_lse(const Args<REL> &a, int b, const Seq &s, int head, int r, float lse2) {
+    if constexpr (REL == kShared) a.src.lse2[lse_at(a, b, s, head, r)] = lse2;
+    else if (a.lse) a.lse[lse_at(a, b, s, head, r)] = lse2 * kLn2;
+}
+
+// The state that row r's item starts from, behind shared positions: their results, as a mass of 1 at their lse.  NaN where
+// the sequence's first new token is among the shared positions, of which it would see too many.
+template <int D>
+struct Before {
+    const float *o;
+    float m, l;  // l = 0: nothing before
+    __device__ __forceinline__ Before(const Args<kBehind> &a, const Cells<kBehind> &cells, int b, const Seq &s, int head, int r) {
+        const int64_t at = lse_at(a, b, s, head, r);
+        o = a.src.state + at * D;
+        m = -__builtin_inff();
+        l = 0.0f;
+        if (cells.skip == 0) return;
+        m = s.keys0 > 0 ? a.src.lse2[at] : __builtin_nanf("");
+        l = m == -__builtin_inff() ? 0.0f : (m != m ? m : 1.0f);
+    }
+};
 
 // Rows of no sequence of a packed call: before ptr[0] and behind ptr[batch].  They see nothing: y = 0, lse = -inf.
 template <int D, Relation REL>
@@ -653,6 +718,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
+    if constexpr (REL == kShared) leave_skips(a.src);
     Deal<REL, G::BM, G::BN> deal;
     typename Deal<REL, G::BM, G::BN>::Load lanes = deal.begin(a);
     if (a.part && threadIdx.x == 0 && deal.pieces + blockIdx.x < a.slots) a.rec[2 * (deal.pieces + blockIdx.x)] = int4{0, 0, 0, 0};
@@ -674,6 +740,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
         Source<REL> ks, vs;
         ks.set(a, a.src.k, pc.b, s, pc.head);
         vs.set(a, a.src.v, pc.b, s, pc.head);
+        const Cells<REL> cells(a, pc.b);
         const int32_t keys = keys_of<REL>(a, s, min((pc.j + 1) * G::BM, s.rows) - 1);  // of the tile's last row
         u4 q[2][G::CH];
         int32_t seen[2];
@@ -693,6 +760,20 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
         for (int db = 0; db < G::DB; ++db) st.o[db][0] = st.o[db][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         st.m[0] = st.m[1] = -__builtin_inff();
         st.l[0] = st.l[1] = 0.0f;
+        if constexpr (REL == kBehind) {
+            if (pc.part == 0 && cells.skip > 0) {
+                const float lift = __builtin_exp2f(kLift<T>);
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb) {
+                    const Before<D> x(a, cells, pc.b, s, pc.head, min(r0 + qb * 16 + col, s.rows - 1));
+                    st.m[qb] = x.m - kLift<T>;
+                    st.l[qb] = g == 0 ? x.l * lift : 0.0f;
+#pragma unroll
+                    for (int db = 0; db < G::DB; ++db)
+                        st.o[db][qb] = x.l == 0.0f ? f4{0.0f, 0.0f, 0.0f, 0.0f} : *reinterpret_cast<const f4 *>(x.o + db * 16 + g * 4) * (x.l * lift);
+                }
+            }
+        }
 
         // A load's 1 KB are 4 or 8 rows from a multiple of as many, so in pages of 8 rows or more they lie in one page.
         // Lane r looks load r's page up, a tile ahead of the rows; the entry is read and checked when they are loaded.
@@ -702,7 +783,7 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
         auto look_up = [&](int kt) -> int32_t {
             if constexpr (kPages<REL>) {
                 const int group = (w * G::LPW + lane % G::LPW) * (1024 / G::RB);
-                return entry_at(a.src, pc.b, min(kt * G::BN + group, keys - 1));
+                return cells.entry(a, min(kt * G::BN + group, keys - 1));
             } else {
                 return 0;
             }
@@ -800,13 +881,10 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
             if (r >= s.rows) continue;
             if (whole) {
                 const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-                uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, pc.b, s, pc.head, r);
+                auto *const yr = out_row<D, REL>(a, pc.b, s, pc.head, r);
 #pragma unroll
-                for (int db = 0; db < G::DB; ++db) {
-                    const f4 v = st.o[db][qb] * inv;
-                    *reinterpret_cast<u2 *>(yr + db * 16 + g * 4) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
-                }
-                if (a.lse && g == 0) a.lse[lse_at(a, pc.b, s, pc.head, r)] = (st.m[qb] + __log2f(lt)) * kLn2;
+                for (int db = 0; db < G::DB; ++db) put<T>(yr + db * 16 + g * 4, st.o[db][qb] * inv);
+                if (g == 0) put_lse(a, pc.b, s, pc.head, r, st.m[qb] + __log2f(lt));
             } else {
                 const int tr = r - pc.j * G::BM;
 #pragma unroll
@@ -913,6 +991,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
+    if constexpr (REL == kShared) leave_skips(a.src);
     Walk<REL, G::BM, G::BN> walk;
     walk.begin(a, block, static_cast<int>(gridDim.x));
     if (a.part && threadIdx.x == 0) {
@@ -926,6 +1005,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
         Source<REL> ks, vs;
         ks.set(a, a.src.k, walk.b, s, pc.head);
         vs.set(a, a.src.v, walk.b, s, pc.head);
+        const Cells<REL> cells(a, walk.b);
         const int32_t keys = keys_of<REL>(a, s, min(r0 + G::BM, s.rows) - 1);
         const int32_t least = keys_of<REL>(a, s, r0);
         const int r = min(r0 + col, s.rows - 1);
@@ -941,12 +1021,23 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
         for (int db = 0; db < G::DB; ++db) st.o[db] = f4{0.0f, 0.0f, 0.0f, 0.0f};
         st.m = -__builtin_inff();
         st.l = 0.0f;
+        if constexpr (REL == kBehind) {
+            if (pc.starts && w == 0 && cells.skip > 0) {
+                const float lift = __builtin_exp2f(kLift<T>);
+                const Before<D> x(a, cells, walk.b, s, pc.head, r);
+                st.m = x.m;
+                st.l = g == 0 ? x.l * lift : 0.0f;
+#pragma unroll
+                for (int db = 0; db < G::DB; ++db)
+                    st.o[db] = x.l == 0.0f ? f4{0.0f, 0.0f, 0.0f, 0.0f} : *reinterpret_cast<const f4 *>(x.o + db * 16 + g * 4) * (x.l * lift);
+            }
+        }
 
         // the step's first key; positions past the last key read that key (masked, and its value cleared)
         auto first = [&](int kt) { return (kt * kWaves + w) * G::KW; };
         auto at = [&](int kt, int i) { return min(first(kt) + i, keys - 1); };
         auto look_up = [&](int kt) {
-            if constexpr (kPages<REL>) return entry_at(a.src, walk.b, at(min(kt, pc.t1 - 1), lane % G::KW));
+            if constexpr (kPages<REL>) return cells.entry(a, at(min(kt, pc.t1 - 1), lane % G::KW));
             else return int32_t(0);
         };
         auto has = [&](int32_t entry) {
@@ -1066,11 +1157,10 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
             }
             if (whole) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, walk.b, s, pc.head, r0 + tr) + d0;
+                auto *const yr = out_row<D, REL>(a, walk.b, s, pc.head, r0 + tr) + d0;
 #pragma unroll
-                for (int e = 0; e < E; e += 4)
-                    *reinterpret_cast<u2 *>(yr + e) = u2{T::pack(o[e] * inv, o[e + 1] * inv), T::pack(o[e + 2] * inv, o[e + 3] * inv)};
-                if (a.lse && d0 == 0) a.lse[lse_at(a, walk.b, s, pc.head, r0 + tr)] = (ref + __log2f(l)) * kLn2;
+                for (int e = 0; e < E; e += 4) put<T>(yr + e, f4{o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv});
+                if (d0 == 0) put_lse(a, walk.b, s, pc.head, r0 + tr, ref + __log2f(l));
             } else {
                 float *const po = a.part + slot * slot_floats<G::BM, D>();
 #pragma unroll
@@ -1170,9 +1260,8 @@ __global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<REL> a, int b
             l += sl[i][k * L + lane];
         }
     o *= l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + 4 * lane;
-    *reinterpret_cast<u2 *>(yr) = u2{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
-    if (a.lse && lane == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (ref + __log2f(l)) * kLn2;
+    put<T>(out_row<D, REL>(a, b, s, head, j * BM + r) + 4 * lane, o);
+    if (lane == 0) put_lse(a, b, s, head, j * BM + r, ref + __log2f(l));
 }
 
 // Joins the parts of the wide item whose first part is in slot x: a wavefront takes 4 rows, 16 bytes a lane, the parts in
@@ -1240,9 +1329,8 @@ __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
         const int r = r0 + k * AT + lane / L;
         if (r >= rows) continue;
         const f4 v = o[k] * (l[k] == 0.0f ? 0.0f : 1.0f / l[k]);
-        uint16_t *yr = const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, j * BM + r) + 4 * (lane % L);
-        *reinterpret_cast<u2 *>(yr) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
-        if (a.lse && lane % L == 0) a.lse[lse_at(a, b, s, head, j * BM + r)] = (m[k] + __log2f(l[k])) * kLn2;
+        put<T>(out_row<D, REL>(a, b, s, head, j * BM + r) + 4 * (lane % L), v);
+        if (lane % L == 0) put_lse(a, b, s, head, j * BM + r, m[k] + __log2f(l[k]));
     }
 }
 
