@@ -671,6 +671,59 @@ int tiga_mp_attention_prefix_fwd(const tiga_cache *cache, const tiga_prefix *pre
                                  const int32_t *dst_ptr, int32_t heads, const tiga_view *q, float scale,
                                  const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
 
+/* --------------------------------------------- which positions of a cache stay */
+
+/* Workspace bytes for tiga_mp_cache_weights (0 on error).  One sized for a call
+ * holds every smaller one. */
+size_t tiga_mp_cache_weights_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads);
+
+/* Add the attention weights that a call's new tokens give to the positions of the
+ * cache, from the queries and the lse of tiga_mp_attention_paged_fwd (or _prefix_
+ * _fwd): with s_ij = scale <q_i, k_j>, for every sequence, source head and position
+ * j below the sequence's length,
+ *   out_j = decay * weights_j + sum_i exp(s_ij - lse_i)
+ * over the new tokens i that see j, of every head that shares the source head;
+ * weights_j counts as 0 at the new tokens' own positions, whatever lies there.
+ *   q:   as for tiga_mp_attention_paged_fwd;  lse: fp32 [heads, num_dst].
+ *   weights, out: fp32 [num_pages, kv_heads, page_size], contiguous, the cells of
+ *   the cache's pages; out may be weights.  Cells of no position are left as they
+ *   were.  No two sequences may share a page.
+ * A row with lse = -inf gives nothing.  Positions past the table or without a page
+ * have no cell.  Sums in fp32 in a fixed order; deterministic.  Requires decay
+ * finite and >= 0; otherwise as tiga_mp_attention_paged_fwd.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
+int tiga_mp_cache_weights(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,
+                          const tiga_view *q, const float *lse, float scale, float decay, const float *weights,
+                          float *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes for tiga_mp_cache_evict (0 on error): little; in place (to is
+ * cache) the rows that stay.  One sized for a call holds every smaller one. */
+size_t tiga_mp_cache_evict_workspace(const tiga_cache *cache, const tiga_cache *to, int32_t keep);
+
+/* Keep the `keep` positions of each sequence and source head with the largest
+ * weights: the last `recent` positions, and of the others those of the largest
+ * weights, of equal ones the first.  They move, in order, to the first positions of
+ * the same sequence and head of `to`: keys, values, weights, and lengths.
+ *   weights:    fp32 [num_pages, kv_heads, page_size] of cache; NaN counts as more
+ *               than everything, a position without a page as less.
+ *   to:         a cache of the same batch, kv_heads, width and dtype, whose length
+ *               array is not read; its pages are none that cache's tables name, or
+ *               it is cache itself (the same table and k.data): in place.
+ *   to_weights: fp32 [to->num_pages, kv_heads, to->page_size] or NULL; in place it
+ *               may be weights.
+ *   to_length:  int32 [batch], min(length, keep); may be cache's length array.
+ *   kept:       int32 [batch, kv_heads, keep], the positions that stayed, in order,
+ *               -1 past them.
+ * Keys that were rotated keep the rotation of the position they had.  Positions past
+ * cache's table are none; rows whose new position has no page in `to`, or whose old
+ * one had none, are not stored.  Nothing else is written.  No two sequences may
+ * share a page of `to`.  Deterministic.
+ * Requires 1 <= keep, 0 <= recent <= keep, batch * kv_heads < 2^20.
+ * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
+int tiga_mp_cache_evict(const tiga_cache *cache, const float *weights, int32_t keep, int32_t recent,
+                        const tiga_cache *to, float *to_weights, int32_t *to_length, int32_t *kept, void *ws,
+                        size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------- profiling */
 
 /* Profiling aid.  Arms the calling thread so that its next entry-point call

@@ -145,6 +145,12 @@ _SIGS = {
     "tiga_mp_attention_prefix_fwd_workspace": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32]),
     "tiga_mp_attention_prefix_fwd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
                                                C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tiga_mp_cache_weights_workspace": (C.c_size_t, [C.c_void_p, C.c_int64, C.c_int32]),
+    "tiga_mp_cache_weights": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float,
+                                        C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tiga_mp_cache_evict_workspace": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int32]),
+    "tiga_mp_cache_evict": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "tiga_mp_set_kernel_events": (C.c_int, [C.c_void_p, C.c_void_p]),
 }
 
@@ -981,6 +987,62 @@ def tiga_mp_attention_prefix_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch
                                             cache.width ** -0.5 if scale is None else float(scale), ref(yv), _ptr(lse),
                                             _ptr(ws), ws.nbytes, _stream()))
     return (y, lse) if want_lse else y
+
+
+def _cells(cache, t, name):
+    P, H, R = cache.k_pages.shape[:3]
+    return _dev(t, torch.float32, name, (P, H, R))
+
+
+def tiga_mp_cache_weights(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, dst_ptr: torch.Tensor,
+                          weights: torch.Tensor, out: torch.Tensor | None = None, decay: float = 1.0,
+                          scale: float | None = None, layout: str = "hnd", ws=None):
+    """Add the attention weights that new tokens give to the cached positions: decay * weights + sum exp(s - lse).
+
+    q, dst_ptr, scale as for tiga_mp_attention_paged_fwd, lse fp32 [heads, rows] from it.  weights: fp32
+    [num_pages, kv_heads, page_size], one for each row of the cache's pages, summed over the heads that share it; the
+    new tokens' own count as 0 before.  out: where the sums go (None: weights, in place).  Pages are no two sequences'.
+    Returns out."""
+    lib = load()
+    axes = _axes(layout, (3,))
+    heads, rows, qv = _new_rows(cache, q, "q", axes)
+    _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
+    _dev(lse, torch.float32, "lse", (heads, rows))
+    _cells(cache, weights, "weights")
+    out = weights if out is None else _cells(cache, out, "out")
+    _same_device(cache.k_pages.get_device(), q=q, lse=lse, dst_ptr=dst_ptr, weights=weights, out=out)
+    ws = _given_or_new(ws, lib.tiga_mp_cache_weights_workspace, cache.ref, rows, heads, device=q.device)
+    _check(lib.tiga_mp_cache_weights(cache.ref, rows, _ptr(dst_ptr), heads, C.byref(qv), _ptr(lse),
+                                     cache.width ** -0.5 if scale is None else float(scale), float(decay), _ptr(weights),
+                                     _ptr(out), _ptr(ws), ws.nbytes, _stream()))
+    return out
+
+
+def tiga_mp_cache_evict(cache: KvCache, weights: torch.Tensor, to: KvCache | None = None,
+                        to_weights: torch.Tensor | None = None, *, keep: int, recent: int = 0, kept=None, ws=None):
+    """Keep `keep` positions of each sequence and source head: the last `recent`, and those of the largest weights.
+
+    weights: fp32 [num_pages, kv_heads, page_size].  They move in order to the first positions of `to` (keys, values, and
+    weights to to_weights if given), whose pages are none of the cache's sequences' own; to.length is set to
+    min(length, keep).  Without `to` the cache is evicted from in place, weights and length too.  Keys keep the rotation
+    of their old positions: rotate later tokens by their true positions (tiga_mp_rotary_fwd) and append them unrotated.
+    Returns kept: int32 [batch, kv_heads, keep], the positions that stayed, -1 past them."""
+    lib = load()
+    _cells(cache, weights, "weights")
+    if to is None:
+        to, to_weights = cache, weights if to_weights is None else to_weights
+    if to_weights is not None:
+        _cells(to, to_weights, "to_weights")
+    shape = (cache.batch, cache.kv_heads, int(keep))
+    if int(keep) < 1:
+        raise ValueError("keep must be at least 1")
+    kept = weights.new_empty(shape, dtype=torch.int32) if kept is None else _dev(kept, torch.int32, "kept", shape)
+    _same_device(cache.k_pages.get_device(), weights=weights, to=to.k_pages, to_weights=to_weights, kept=kept)
+    ref = cache.ref, to.ref
+    ws = _given_or_new(ws, lib.tiga_mp_cache_evict_workspace, *ref, int(keep), device=weights.device)
+    _check(lib.tiga_mp_cache_evict(ref[0], _ptr(weights), int(keep), int(recent), ref[1], _ptr(to_weights), _ptr(to.length),
+                                   _ptr(kept), _ptr(ws), ws.nbytes, _stream()))
+    return kept
 
 
 # ------------------------------------------------------------ autograd wrappers

@@ -4,6 +4,7 @@
 #include <vector>
 
 #include "relattn.hpp"
+#include "retention.hpp"
 #include "rotary.hpp"
 
 using namespace tiga;
@@ -522,6 +523,90 @@ int tiga_mp_cache_append(const tiga_cache *cache, int64_t num_dst, const int32_t
     }
     return rotary::append(*cache, num_dst, dst_ptr, *k, *v, rot ? *rot : tiga_rotary{}, heads, with_q ? *q : none,
                           with_q ? *q_out : none, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------- which positions of a cache stay
+
+namespace {
+
+// Cells of a cache's pages.
+int check_cells(const char *what, const char *name, const float *p) {
+    if (!p || (reinterpret_cast<uintptr_t>(p) & 15u)) return fail(TIGA_EINVAL, "%s: %s missing or not 16-byte aligned", what, name);
+    return TIGA_OK;
+}
+
+bool in_place(const tiga_cache *cache, const tiga_cache *to) {
+    return to->table == cache->table && to->k.data == cache->k.data;
+}
+
+int check_evict(const char *what, const tiga_cache *cache, const tiga_cache *to, int32_t keep) {
+    if (int rc = check_cache(what, cache)) return rc;
+    if (int rc = check_cache(what, to)) return rc;
+    if (to->batch != cache->batch || to->kv_heads != cache->kv_heads || to->width != cache->width || to->dtype != cache->dtype)
+        return fail(TIGA_EINVAL, "%s: the caches differ in batch, heads, width or dtype", what);
+    if (keep < 1) return fail(TIGA_EINVAL, "%s: keep must be at least 1", what);
+    if (static_cast<int64_t>(cache->batch) * cache->kv_heads >= (1 << 20))
+        return fail(TIGA_EUNSUPPORTED, "%s: batch * kv_heads must be < 2^20", what);
+    return TIGA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tiga_mp_cache_weights_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads) {
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
+    return check_paged("cache weights", cache, num_dst, heads) ? 0 : retention::weights_ws_bytes(*cache, num_dst, heads);
+}
+
+int tiga_mp_cache_weights(const tiga_cache *cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads,
+                          const tiga_view *q, const float *lse, float scale, float decay, const float *weights,
+                          float *out, void *ws, size_t ws_bytes, void *stream) {
+    EntryScope scope;
+    const char *what = "cache weights";
+    if (int rc = check_paged(what, cache, num_dst, heads)) return rc;
+    if (int rc = check_scale(what, scale)) return rc;
+    if (!(decay >= 0.0f) || bad_float(decay)) return fail(TIGA_EINVAL, "%s: decay must be finite and >= 0", what);
+    if (cache->batch == 0 || cache->kv_heads == 0 || cache->table_width == 0) return TIGA_OK;
+    if (heads == 0) return fail(TIGA_EINVAL, "%s: no heads", what);
+    if (int rc = check_cache_data(what, cache, dst_ptr)) return rc;
+    if (num_dst > 0) {
+        if (int rc = check_view(what, "q", q, false, 0, 0, 0)) return rc;
+        if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3u)) return fail(TIGA_EINVAL, "%s: lse missing or misaligned", what);
+    }
+    if (int rc = check_cells(what, "weights", weights)) return rc;
+    if (int rc = check_cells(what, "out", out)) return rc;
+    if (int rc = check_ws(what, ws, ws_bytes, retention::weights_ws_bytes(*cache, num_dst, heads))) return rc;
+    return retention::accumulate(*cache, num_dst, dst_ptr, heads, num_dst > 0 ? *q : tiga_view{}, lse, scale, decay, weights, out,
+                                 ws, static_cast<hipStream_t>(stream));
+}
+
+size_t tiga_mp_cache_evict_workspace(const tiga_cache *cache, const tiga_cache *to, int32_t keep) {
+    clear_error();  // no EntryScope: armed kernel events are for the call that follows
+    return check_evict("cache eviction", cache, to, keep) ? 0 : retention::evict_ws_bytes(*cache, keep, in_place(cache, to));
+}
+
+int tiga_mp_cache_evict(const tiga_cache *cache, const float *weights, int32_t keep, int32_t recent,
+                        const tiga_cache *to, float *to_weights, int32_t *to_length, int32_t *kept, void *ws,
+                        size_t ws_bytes, void *stream) {
+    EntryScope scope;
+    const char *what = "cache eviction";
+    if (int rc = check_evict(what, cache, to, keep)) return rc;
+    if (recent < 0 || recent > keep) return fail(TIGA_EINVAL, "%s: recent = %d must be in [0, keep]", what, recent);
+    if (cache->batch == 0 || cache->kv_heads == 0) return TIGA_OK;
+    if (int rc = check_cache_data(what, cache, cache->length)) return rc;
+    if (int rc = check_cache_data(what, to, to_length)) return rc;
+    if (int rc = check_cells(what, "weights", weights)) return rc;
+    if (to_weights)
+        if (int rc = check_cells(what, "to_weights", to_weights)) return rc;
+    if (!to_length || !kept || ((reinterpret_cast<uintptr_t>(to_length) | reinterpret_cast<uintptr_t>(kept)) & 3u))
+        return fail(TIGA_EINVAL, "%s: to_length or kept missing or misaligned", what);
+    const bool staged = in_place(cache, to);
+    if (int rc = check_ws(what, ws, ws_bytes, retention::evict_ws_bytes(*cache, keep, staged))) return rc;
+    return retention::evict(*cache, weights, keep, recent, *to, to_weights, to_length, kept, staged, ws,
+                            static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
