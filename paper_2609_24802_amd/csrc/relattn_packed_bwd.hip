@@ -364,6 +364,15 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
             add_keys<T, D, kQuery>(acc, f, own_delta, b1 + kc * 32 * G::RB, at.tr);
         }
     };
+    auto plain = [&](const uint8_t *b1, const uint8_t *b2) {
+#pragma unroll
+        for (int kc = 0; kc < G::KC; ++kc) {
+            Scores<T, D> f;
+            f.form(x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, [](int) {});
+            weigh<T, D>(f, c, own, false, 0, g);
+            add_keys<T, D, kQuery>(acc, f, own_delta, b1 + kc * 32 * G::RB, at.tr);
+        }
+    };
     auto deltas = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *bad) {
 #pragma unroll
         for (int kc = 0; kc < G::KC; ++kc) {
@@ -397,6 +406,17 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
         if (steps > 1) step(1, y1b, y2b, bad1);
     } else {
         int kt = 0;
+        // tiles that all rows see whole, in pairs
+        for (const int whole = least / G::BN & ~1; kt < whole; kt += 2) {
+            loads_arrived();
+            __syncthreads();
+            stage(kt + 1, y1b, y2b);
+            plain(y1a, y2a);
+            loads_arrived();
+            __syncthreads();
+            if (kt + 2 < steps) stage(kt + 2, y1a, y2a);
+            plain(y1b, y2b);
+        }
         // one exit, after a whole turn of both buffers: with another between them the sums are moved and spill
         for (; kt + 1 < steps; kt += 2) {
             loads_arrived();
@@ -544,22 +564,33 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
         }
         __syncthreads();
     };
-    auto step = [&](int n, const uint8_t *b1, const uint8_t *b2, const float *stats) {
-        if (cut(n)) {
-            const int32_t k0 = (end - 1 - n) * G::BN;
-#pragma unroll 1
-            for (int kc = 0; kc < G::KC; ++kc)
-                rows_cut<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
-                               stats + G::BN + kc * 32, g, a.group, k0 + kc * 32, key);
-        } else {
+    auto plain = [&](const uint8_t *b1, const uint8_t *b2, const float *stats) {
 #pragma unroll
-            for (int kc = 0; kc < G::KC; kc += 2)
-                rows_step<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
-                                stats + G::BN + kc * 32, g);
-        }
+        for (int kc = 0; kc < G::KC; kc += 2)
+            rows_step<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
+                            stats + G::BN + kc * 32, g);
+    };
+    auto step = [&](int n, const uint8_t *b1, const uint8_t *b2, const float *stats) {
+        const int32_t k0 = (end - 1 - n) * G::BN;
+#pragma unroll 1
+        for (int kc = 0; kc < G::KC; ++kc)
+            rows_cut<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
+                           stats + G::BN + kc * 32, g, a.group, k0 + kc * 32, key);
     };
     stage(0, y1a, y2a, sta);
     int n = 0;
+    // tiles whose rows all see every owned key, in pairs
+    const int64_t from = (static_cast<int64_t>(own0 + kOwn - 1) * d + G::BN - 1) / G::BN;
+    for (const int whole = from < end ? static_cast<int>(end - from) & ~1 : 0; n < whole; n += 2) {
+        loads_arrived();
+        __syncthreads();
+        stage(n + 1, y1b, y2b, stb);
+        plain(y1a, y2a, sta);
+        loads_arrived();
+        __syncthreads();
+        if (n + 2 < steps) stage(n + 2, y1a, y2a, sta);
+        plain(y1b, y2b, stb);
+    }
     for (; n + 1 < steps; n += 2) {
         loads_arrived();
         tidy(n, y1a, y2a, 0);
