@@ -235,13 +235,12 @@ struct Weights {
             dw[n / 2] = T::pack(ds[n - 1], ds[n]);
         }
     }
-    // Where the pair does not exist both are 0, whatever its operands hold.
-    __device__ __forceinline__ void form_if(const Scores<T, D> &f, float c, float h, int n, bool exists) {
+    // bit n of `exists`: whether the pair does
+    __device__ __forceinline__ void form_if(const Scores<T, D> &f, float c, float h, int n, uint32_t exists) {
         const int qb = n / 8, e = n / 4 % 2, i = n % 4;
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[e][i]));
-        const float y = x * (kScaled<T> ? __builtin_fmaf(f.dp[e][qb][i], h, -delta[e][i]) : f.dp[e][qb][i] - delta[e][i]);
-        p[n] = exists ? x : 0.0f;
-        ds[n] = exists ? y : 0.0f;
+        p[n] = __uint_as_float(__float_as_uint(x) & static_cast<uint32_t>(__builtin_amdgcn_sbfe(exists, n, 1)));
+        ds[n] = p[n] * (kScaled<T> ? __builtin_fmaf(f.dp[e][qb][i], h, -delta[e][i]) : f.dp[e][qb][i] - delta[e][i]);
         if (n % 2) {
             pw[n / 2] = T::pack(p[n - 1], p[n]);
             dw[n / 2] = T::pack(ds[n - 1], ds[n]);
@@ -253,10 +252,12 @@ struct Weights {
 // scores, the second's under the first half's sums: at width 128 a SIMD has one wavefront, and nothing else fills its
 // matrix unit meanwhile (527 us without, 494).  At width 64 two wavefronts share a SIMD: 8 x 449 rows over 1500 ragged 54.8
 // and 52.7 us, 4 x 4096 over 77 23.4 and 21.0, 4 x 4096 over 4096 507 and 525.
-template <class T, int D>
+// CUT: bit n of exists[half] says whether pair n of the half does; otherwise all do.
+template <class T, int D, bool CUT = false>
 __device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)[2][Geo<D>::CH],
                                           const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
-                                          int tr, float c, float h, const float *st, const float *sd, int g) {
+                                          int tr, float c, float h, const float *st, const float *sd, int g,
+                                          const uint32_t *exists = nullptr) {
     constexpr int kHalf = 32 * Geo<D>::RB, kScore = 16 / Scores<T, D>::kReads, kSum = 16 / kSumReads<T, D, kKeys>;
     Scores<T, D> f0, f1;
     Weights<T, D> w0, w1;
@@ -264,14 +265,20 @@ __device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)
     f0.form(x1, x2, y1, y2, dr, [](int) {});
     f1.form(x1, x2, y1 + kHalf, y2 + kHalf, dr, [&](int i) {
 #pragma unroll
-        for (int n = 0; n < kScore; ++n) w0.form(f0, c, h, i * kScore + n);
+        for (int n = 0; n < kScore; ++n) {
+            if constexpr (CUT) w0.form_if(f0, c, h, i * kScore + n, exists[0]);
+            else w0.form(f0, c, h, i * kScore + n);
+        }
     });
     w1.load(st + 32, sd + 32, g);
     auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
     const u4 p0[2] = {operand(w0.pw, 0), operand(w0.pw, 1)}, d0[2] = {operand(w0.dw, 0), operand(w0.dw, 1)};
     add_products<T, D, kKeys>(acc, p0, d0, y1, y2, tr, [&](int i) {
 #pragma unroll
-        for (int n = 0; n < kSum; ++n) w1.form(f1, c, h, i * kSum + n);
+        for (int n = 0; n < kSum; ++n) {
+            if constexpr (CUT) w1.form_if(f1, c, h, i * kSum + n, exists[1]);
+            else w1.form(f1, c, h, i * kSum + n);
+        }
     });
     const u4 p1[2] = {operand(w1.pw, 0), operand(w1.pw, 1)}, d1[2] = {operand(w1.dw, 0), operand(w1.dw, 1)};
     add_products<T, D, kKeys>(acc, p1, d1, y1 + kHalf, y2 + kHalf, tr, [](int) {});

@@ -453,24 +453,17 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
 
 // ------------------------------------------------------------------------------------------ dk, dv
 
-// 32 streamed rows that the diagonal cuts: row `r0` and the 31 after it, of which this lane's columns are keys key[qb].
-template <class T, int D>
-__device__ __forceinline__ void rows_cut(Sums<T, D, kKeys> &acc, const u4 (&x1)[2][Geo<D>::CH], const u4 (&x2)[2][Geo<D>::CH],
-                                         const uint8_t *y1, const uint8_t *y2, int dr, int tr, float c, float h,
-                                         const float *st, const float *sd, int g, const Divider &group, int32_t r0,
-                                         const int32_t *key) {
-    Scores<T, D> f;
-    Weights<T, D> w;
-    w.load(st, sd, g);
-    f.form(x1, x2, y1, y2, dr, [](int) {});
-    int32_t token[8];
+// Which of this lane's 16 pairs of 32 streamed rows from `r0` on exist, as Weights numbers them: key[qb] is at or before the
+// row's token.
+__device__ __forceinline__ uint32_t pairs_of(const Divider &group, int32_t r0, int g, const int32_t *key) {
+    uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) token[i] = group.div(r0 + i / 4 * 16 + 4 * g + i % 4);
+    for (int i = 0; i < 8; ++i) {
+        const int32_t token = group.div(r0 + i / 4 * 16 + 4 * g + i % 4);
 #pragma unroll
-    for (int n = 0; n < 16; ++n) w.form_if(f, c, h, n, key[n / 8] <= token[n % 8]);
-    auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
-    const u4 p[2] = {operand(w.pw, 0), operand(w.pw, 1)}, ds[2] = {operand(w.dw, 0), operand(w.dw, 1)};
-    add_products<T, D, kKeys>(acc, p, ds, y1, y2, tr, [](int) {});
+        for (int qb = 0; qb < 2; ++qb) bits |= key[qb] <= token ? 1u << (8 * qb + i) : 0u;
+    }
+    return bits;
 }
 
 template <class T, int D>
@@ -540,25 +533,38 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     auto tidy = [&](int n, uint8_t *b1, uint8_t *b2, int which) {
         if (cut(n)) look_through<T, D>(b1, b2, w, found[which]);
     };
-    // A query that is not finite makes its row's weights NaN, a cotangent its ds; dv takes the cotangent itself.
+    // A row whose query is not finite has NaN for weights, one whose cotangent is not finite for ds: the sums of the keys that
+    // see it get those apart, and dv the cotangent itself; without them the row has no weight, or none in ds.
     auto mend = [&](int n, uint8_t *b1, uint8_t *b2, float *stats, int which) {
         if (!cut(n) || !any_found(found[which])) return;
         const int32_t k0 = (end - 1 - n) * G::BN;
         for (int k = 0; k < G::BN && k0 + k < rows; ++k) {
             const int32_t token = a.group.div(k0 + k);
+            uint32_t bad1 = 0, bad2 = 0;
+#pragma unroll 1
+            for (int i = 0; i < G::CPR; ++i) {
+                bad1 |= any_wild<T>(reinterpret_cast<const u4 *>(b1 + k * G::RB)[i]);
+                bad2 |= any_wild<T>(reinterpret_cast<const u4 *>(b2 + k * G::RB)[i]);
+            }
+            if (uniform(bad1 | bad2) == 0) continue;
+            const float nan = __builtin_nanf(""), in_dv = uniform(bad1) ? nan : 0.0f;
 #pragma unroll
             for (int db = 0; db < G::DB; ++db) {
                 const u2 x = *reinterpret_cast<const u2 *>(b2 + k * G::RB + 16 * ((2 * db + g / 2) ^ swizzle<D>(k)) + 8 * (g % 2));
 #pragma unroll
-                for (int qb = 0; qb < 2; ++qb) add_wild<T>(acc.a2[db][qb], x, key[qb] <= token);
+                for (int qb = 0; qb < 2; ++qb) {
+                    add_wild<T>(acc.a2[db][qb], x, key[qb] <= token);
+                    acc.a1[db][qb] += key[qb] <= token ? nan : 0.0f;
+                    acc.a2[db][qb] += key[qb] <= token ? in_dv : 0.0f;
+                }
             }
         }
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < G::LPW; ++r) {
             u4 *const p1 = own_rows<D>(b1, w, r), *const p2 = own_rows<D>(b2, w, r);
-            if (any_wild<T>(*p1)) stats[at.krow[r]] = __builtin_nanf("");
-            if (any_wild<T>(*p2)) stats[G::BN + at.krow[r]] = __builtin_nanf("");
+            if (any_wild<T>(*p1)) stats[at.krow[r]] = __builtin_inff();
+            if (any_wild<T>(*p1) || any_wild<T>(*p2)) stats[G::BN + at.krow[r]] = 0.0f;
             *p1 = without_wild<T>(*p1);
             *p2 = without_wild<T>(*p2);
         }
@@ -572,10 +578,12 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     };
     auto step = [&](int n, const uint8_t *b1, const uint8_t *b2, const float *stats) {
         const int32_t k0 = (end - 1 - n) * G::BN;
-#pragma unroll 1
-        for (int kc = 0; kc < G::KC; ++kc)
-            rows_cut<T, D>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
-                           stats + G::BN + kc * 32, g, a.group, k0 + kc * 32, key);
+#pragma unroll
+        for (int kc = 0; kc < G::KC; kc += 2) {
+            const uint32_t exists[2] = {pairs_of(a.group, k0 + kc * 32, g, key), pairs_of(a.group, k0 + kc * 32 + 32, g, key)};
+            rows_step<T, D, true>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
+                                  stats + G::BN + kc * 32, g, exists);
+        }
     };
     stage(0, y1a, y2a, sta);
     int n = 0;
