@@ -7,7 +7,9 @@
 // same rows.  Only tiles that the diagonal cuts are masked.
 //
 // An item is one owned tile of a sequence and source head.  Its work grows linearly along a sequence, so items start in the
-// order of their remaining tiles, the longest of 64 sequences first.
+// order of their remaining tiles, the longest of 64 sequences first.  Items longer than a block's share of all work (one long
+// sequence, few heads) are cut along the streamed axis into parts of at most that, whose fp32 sums go to the workspace and are
+// added in order by packed_reduce_kernel.
 #include "relation.hpp"
 #include "relattn.hpp"
 #include "relattn_bwd.hpp"
@@ -28,7 +30,11 @@ struct Args {
     Divider group;
     int64_t stats;        // heads * num_rows
     float scale;
+    float *part;          // sums of parts
+    int32_t resident;     // blocks that run at once
+    int32_t least;        // levels of a part, at least (kNoCut: nothing is cut)
 };
+constexpr int32_t kNoCut = 1 << 30;
 
 // Row r of a sequence's source head is token r / group of head r % group of its group.
 __device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int32_t first, int kv, int32_t r) {
@@ -48,13 +54,21 @@ __device__ __forceinline__ int64_t stat_at(const Args &a, int32_t first, int kv,
 struct Item {
     Run run;
     int32_t b, kv, level, tiles;  // level 0: there is no such item
+    int32_t part, parts;
 };
-// Item `id` of tiles of 128 / mult tokens.  Sequences are taken 64 at a time, which start at or behind what the sequences
-// before them need at most; of 64, the tiles with the most levels come first: F(L) = sum of max(0, tiles - L) have more
-// than L, so the level of the n-th is the smallest L with F(L) <= n.
+// Items are cut into parts of at most `cut` levels.  How many pieces the items of the first m levels make:
+__device__ __forceinline__ int64_t pieces_upto(int32_t m, int32_t cut) {
+    if (m <= cut) return m;
+    const uint32_t q = static_cast<uint32_t>(m) / static_cast<uint32_t>(cut), r = static_cast<uint32_t>(m) - q * cut;
+    return static_cast<int64_t>(q) * (q + 1) / 2 * cut + static_cast<int64_t>(r) * (q + 1);
+}
+// Piece `id` of tiles of 128 / mult tokens.  Sequences are taken 64 at a time, which start at or behind what the sequences
+// before them need at most; of 64, the tiles with the most levels come first: F(L) = sum of pieces_upto(tiles) - pieces_upto(L)
+// are of more than L, so the level of the n-th is the smallest L with F(L) <= n.  Only the first 64 sequences are cut, of
+// batches that have no more.
 __device__ __forceinline__ Item item_of(const Args &a, int32_t mult, int32_t id) {
     const int lane = lane_id();
-    Item it{Run{0, 0}, 0, id % a.kv_heads, 0, 0};
+    Item it{Run{0, 0}, 0, id % a.kv_heads, 0, 0, 0, 1};
     int32_t n = id / a.kv_heads;
     if (a.batch == 0) return it;
     auto start = [&](int chunk) {
@@ -69,11 +83,23 @@ __device__ __forceinline__ Item item_of(const Args &a, int32_t mult, int32_t id)
         else hi = mid - 1;
     }
     const int base = lo * kWave;
-    n -= start(lo);
+    if (a.batch > kWave) n -= start(lo);
     if (n < 0) return it;
     const Run mine = base + lane < a.batch ? run_between(a.ptr, base + lane, base + lane + 1, a.num_rows) : Run{0, 0};
     const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(mine.count) * mult + kOwn - 1) / kOwn);
-    auto above = [&](int32_t level) { return lane_value(wave_prefix(tiles > level ? tiles - level : 0), kWave - 1); };
+    auto all = [&](int64_t x) { return lane_value(wave_prefix(x), kWave - 1); };
+    int32_t cut = kNoCut;
+    if (a.least < kNoCut) {
+        // Parts of half a block's share of all levels, or of as much more as makes at most two pieces a block, up to the whole
+        // share, which makes at most twice as many parts as blocks run at once.  (dk and dv of 10,000 tokens, 4 heads over one
+        // of 128: 264 us by a simulation of this order, 407 with whole shares, 269 with one piece a block, 1329 uncut.)
+        const int64_t levels = all(static_cast<int64_t>(tiles) * (tiles + 1) / 2) * a.kv_heads;
+        const int64_t share = min(static_cast<int64_t>(kNoCut) - 1, max(static_cast<int64_t>(a.least), quotient(levels + a.resident - 1, a.resident)));
+        int64_t c = max(static_cast<int64_t>(a.least), (share + 1) / 2);
+        while (c < share && all(pieces_upto(tiles, static_cast<int32_t>(c))) * a.kv_heads > 2 * a.resident) c += c / 16 + 1;
+        cut = static_cast<int32_t>(min(c, share));
+    }
+    auto above = [&](int32_t level) { return all(tiles > level ? pieces_upto(tiles, cut) - pieces_upto(level, cut) : 0); };
     int32_t from = 0, to = static_cast<int32_t>((static_cast<int64_t>(a.num_rows) * mult + kOwn - 1) / kOwn);
     while (from < to) {
         const int32_t mid = from + (to - from) / 2;
@@ -81,7 +107,8 @@ __device__ __forceinline__ Item item_of(const Args &a, int32_t mult, int32_t id)
         else from = mid + 1;
     }
     if (from == 0) return it;
-    const int32_t k = n - static_cast<int32_t>(above(from));
+    const int32_t parts = from <= cut ? 1 : (from + cut - 1) / cut;
+    const int32_t rest = n - static_cast<int32_t>(above(from)), k = rest / parts;
     const uint64_t some = __ballot(tiles >= from);
     const int before = __popcll(some & ((uint64_t(1) << lane) - 1));
     const uint64_t hit = __ballot(tiles >= from && before == k);
@@ -91,8 +118,17 @@ __device__ __forceinline__ Item item_of(const Args &a, int32_t mult, int32_t id)
     it.tiles = __builtin_amdgcn_readlane(tiles, l);
     it.b = base + l;
     it.level = from;
+    it.part = rest - k * parts;
+    it.parts = parts;
     return it;
 }
+// The streamed steps of a part.
+__device__ __forceinline__ int32_t part_start(int32_t steps, int32_t part, int32_t parts) {
+    return static_cast<int32_t>(static_cast<int64_t>(steps) * part / parts);
+}
+// Sums [operand][owned][D] of a part: cut items come first, so that a piece's number is its place.
+template <int D, int M>
+__device__ __forceinline__ float *part_at(const Args &a, int32_t id) { return a.part + static_cast<int64_t>(id) * M * kOwn * D; }
 
 // Gradients of rows of no sequence: before ptr[0] and behind ptr[batch].
 template <int D>
@@ -251,7 +287,8 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
     if (it.level == 0) return;
     const int32_t rows = it.run.count * d, own0 = (it.level - 1) * kOwn;
     const int32_t keys = a.group.div(min(own0 + kOwn, rows) - 1) + 1;  // that the tile's last row sees
-    const int32_t steps = (keys + G::BN - 1) / G::BN;
+    const int32_t all_steps = (keys + G::BN - 1) / G::BN;
+    const int32_t first_step = part_start(all_steps, it.part, it.parts), steps = part_start(all_steps, it.part + 1, it.parts);
     // The rounding of y (of itself and of the weights in it) makes an error of u |dy| |y| of delta, which matters over few
     // sources: where the tile's keys are few, delta is formed as sum_j p_ij <dy_i, v_j> in fp32, by the tiles' products.
     const bool few = keys <= kOwn;
@@ -299,7 +336,7 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
         }
     };
     if (!few) {
-        leave_stats();
+        if (it.part == 0) leave_stats();
         if (!a.dq.p) return;
     }
     Sums<T, D, kQuery> acc;
@@ -385,8 +422,8 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
                 for (int i = 0; i < 8; ++i) own_delta[qb] += f.s[i / 4][qb][i % 4] * f.dp[i / 4][qb][i % 4];
         }
     };
-    stage(0, y1a, y2a);
-    if (few) {  // at most two tiles, both in LDS
+    stage(first_step, y1a, y2a);
+    if (few) {  // at most two tiles, both in LDS (and never cut)
         if (steps > 1) stage(1, y1b, y2b);
         loads_arrived();
         tidy(0, y1a, 0);
@@ -405,9 +442,10 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
         step(0, y1a, y2a, bad0);
         if (steps > 1) step(1, y1b, y2b, bad1);
     } else {
-        int kt = 0;
+        int kt = first_step;
         // tiles that all rows see whole, in pairs
-        for (const int whole = least / G::BN & ~1; kt < whole; kt += 2) {
+        const int seen = min(least / G::BN, steps);
+        for (const int whole = seen > kt ? kt + (seen - kt & ~1) : kt; kt < whole; kt += 2) {
             loads_arrived();
             __syncthreads();
             stage(kt + 1, y1b, y2b);
@@ -441,6 +479,13 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
     for (int qb = 0; qb < 2; ++qb) {
         const int32_t o = own0 + w * 32 + qb * 16 + col;
         if (o >= rows) continue;
+        if (it.parts > 1) {
+            float *const p = part_at<D, 1>(a, static_cast<int32_t>(blockIdx.x)) + (o - own0) * D;
+            const float f = kScaled<T> ? two_to(-own_up[qb]) : 1.0f;
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db) *reinterpret_cast<f4 *>(p + db * 16 + g * 4) = acc.a1[db][qb] * f;
+            continue;
+        }
         const float f = kScaled<T> ? a.scale * two_to(-own_up[qb]) : a.scale;
         uint16_t *const p = const_cast<uint16_t *>(a.dq.p) + row_at(a, a.dq, it.run.first, it.kv, o);
 #pragma unroll
@@ -482,7 +527,8 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     if (it.level == 0) return;
     const int32_t own_n = it.run.count, own0 = (it.tiles - it.level) * kOwn, rows = own_n * d;
     // row tiles from the last one back to that of the first owned key (128 tokens are whole tiles)
-    const int32_t end = (rows + G::BN - 1) / G::BN, steps = end - own0 / G::BN * d;
+    const int32_t end = (rows + G::BN - 1) / G::BN, all_steps = end - own0 / G::BN * d;
+    const int32_t first_step = part_start(all_steps, it.part, it.parts), steps = part_start(all_steps, it.part + 1, it.parts);
 
     // owned operands; columns past the end repeat the last (what they sum is not stored)
     u4 x1[2][G::CH], x2[2][G::CH];
@@ -585,11 +631,12 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
                                   stats + G::BN + kc * 32, g, exists);
         }
     };
-    stage(0, y1a, y2a, sta);
-    int n = 0;
+    stage(first_step, y1a, y2a, sta);
+    int n = first_step;
     // tiles whose rows all see every owned key, in pairs
     const int64_t from = (static_cast<int64_t>(own0 + kOwn - 1) * d + G::BN - 1) / G::BN;
-    for (const int whole = from < end ? static_cast<int>(end - from) & ~1 : 0; n < whole; n += 2) {
+    const int seen = from < end ? min(static_cast<int>(end - from), steps) : 0;
+    for (const int whole = seen > n ? n + (seen - n & ~1) : n; n < whole; n += 2) {
         loads_arrived();
         __syncthreads();
         stage(n + 1, y1b, y2b, stb);
@@ -624,6 +671,16 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     for (int qb = 0; qb < 2; ++qb) {
         if (key[qb] >= own_n) continue;
         const int32_t o = it.run.first + key[qb];
+        if (it.parts > 1) {
+            float *const p = part_at<D, 2>(a, static_cast<int32_t>(blockIdx.x)) + (key[qb] - own0) * D;
+            const float f1 = kScaled<T> ? two_to(-keys_up) : 1.0f, f2 = kScaled<T> ? two_to(-kUp) : 1.0f;
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db) {
+                *reinterpret_cast<f4 *>(p + db * 16 + g * 4) = acc.a1[db][qb] * f1;
+                *reinterpret_cast<f4 *>(p + kOwn * D + db * 16 + g * 4) = acc.a2[db][qb] * f2;
+            }
+            continue;
+        }
         const float f1 = kScaled<T> ? a.scale * two_to(-keys_up) : a.scale, f2 = kScaled<T> ? two_to(-kUp) : 1.0f;
         uint16_t *const pk = const_cast<uint16_t *>(a.dk.p) + it.kv * a.dk.head + o * a.dk.row;
         uint16_t *const pv = const_cast<uint16_t *>(a.dv.p) + it.kv * a.dv.head + o * a.dv.row;
@@ -636,19 +693,69 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     }
 }
 
+// Adds the parts of the item whose first part is piece blockIdx.x, in order: 4 widths a thread.
+template <class T, int D, bool KEYS>
+__global__ __launch_bounds__(kThreads) void packed_reduce_kernel(Args a) {
+    constexpr int L = D / 4, M = KEYS ? 2 : 1;
+    const int32_t d = KEYS ? 1 : static_cast<int32_t>(a.group.d), id = static_cast<int32_t>(blockIdx.x);
+    const Item it = item_of(a, d, id);
+    if (it.level == 0 || it.part != 0 || it.parts == 1) return;
+    const int32_t own0 = (KEYS ? it.tiles - it.level : it.level - 1) * kOwn, rows = min(it.run.count * d - own0, kOwn);
+    for (int32_t i = static_cast<int32_t>(blockIdx.y) * kThreads + threadIdx.x; i < rows * L; i += static_cast<int32_t>(gridDim.y) * kThreads) {
+        const int32_t o = i / L, w = i % L * 4;
+        const float *p = part_at<D, M>(a, id) + o * D + w;
+        f4 s1{0.0f, 0.0f, 0.0f, 0.0f}, s2 = s1;
+#pragma unroll 4
+        for (int e = 0; e < it.parts; ++e) {  // the parts of an item are kv_heads pieces apart
+            s1 += *reinterpret_cast<const f4 *>(p);
+            if (KEYS) s2 += *reinterpret_cast<const f4 *>(p + kOwn * D);
+            p += static_cast<int64_t>(a.kv_heads) * M * kOwn * D;
+        }
+        auto put = [&](const uint16_t *at, f4 v) {
+            *reinterpret_cast<u2 *>(const_cast<uint16_t *>(at) + w) = u2{T::pack(v[0], v[1]), T::pack(v[2], v[3])};
+        };
+        s1 *= a.scale;
+        if constexpr (KEYS) {
+            const int32_t row = it.run.first + own0 + o;
+            if (a.dk.p) put(a.dk.p + it.kv * a.dk.head + row * a.dk.row, s1);
+            if (a.dv.p) put(a.dv.p + it.kv * a.dv.head + row * a.dv.row, s2);
+        } else {
+            put(a.dq.p + row_at(a, a.dq, it.run.first, it.kv, own0 + o), s1);
+        }
+    }
+}
+
 // ------------------------------------------------------------------------------------------ launch
 
 // A grid counts its threads in 32 bits (and wraps around without an error).
 constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;
 
-// Items of tiles of 128 / mult tokens, at most.
+// Items of tiles of 128 / mult tokens, at most, not cut.
 int64_t most_items(const tiga_packed &rel, int64_t mult) {
     const int64_t some = rel.num_rows < rel.batch ? rel.num_rows : rel.batch;
     return (rel.num_rows * mult / kOwn + (rel.batch > kWave ? rel.batch : some)) * rel.kv_heads;
 }
+// Which items are cut: batches of up to 64 sequences, whose longest might have more than the least levels of a part, of
+// kLeastSteps streamed tiles.  A part's sums (64 or 128 KB at width 128) are worth that many.
+constexpr int64_t kLeastSteps = 16;
+struct Cut {
+    int32_t resident, least;  // as in Args
+    int64_t pieces;           // of cut items, at most
+};
+Cut cut_for(const tiga_packed &rel, bool keys) {
+    const int64_t group = rel.heads / rel.kv_heads, bn = rel.width == 64 ? 128 : 64;
+    Cut c;
+    c.resident = device_cus() * (keys && rel.width == 128 ? 1 : 2);
+    const int64_t least = ceil_div(kLeastSteps * bn * (keys ? 1 : group), kOwn * (keys ? group : 1));
+    const int64_t most = ceil_div(rel.num_rows * (keys ? 1 : group), kOwn);
+    const bool some = rel.batch <= kWave && most > least;
+    c.least = some ? static_cast<int32_t>(least) : kNoCut;
+    c.pieces = some ? 2 * static_cast<int64_t>(c.resident) + rel.kv_heads : 0;
+    return c;
+}
 
 struct Layout {
-    float *lse2, *delta;
+    float *lse2, *delta, *part;
     f2 *peak;
     int64_t slots;
     size_t bytes;
@@ -661,28 +768,42 @@ Layout layout(const tiga_packed &rel, void *ws) {
     l.delta = c.take<float>(stats);
     l.slots = rel.num_rows / kOwn + rel.batch + 1;
     l.peak = c.take<f2>(l.slots * rel.kv_heads);
+    // whether this call's items are cut or not: a workspace holds every smaller call
+    const size_t pieces = 2 * static_cast<size_t>(device_cus()) * (rel.width == 128 ? 1 : 2) + rel.kv_heads;
+    l.part = c.take<float>((rel.num_rows > kOwn ? pieces : 0) * 2 * kOwn * rel.width);
     l.bytes = c.bytes();
     return l;
 }
 
+template <class T, int D, bool KEYS>
+int products(const tiga_packed &rel, Args a, bool timed, hipStream_t stream) {
+    const Cut cut = cut_for(rel, KEYS);
+    a.resident = cut.resident;
+    a.least = cut.least;
+    const int64_t items = most_items(rel, KEYS ? 1 : a.group.d) + cut.pieces;
+    const dim3 grid(static_cast<unsigned>(items < 1 ? 1 : items));
+    if (timed) prof_before(stream);
+    if constexpr (KEYS) hipLaunchKernelGGL((packed_keys_kernel<T, D>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((packed_query_kernel<T, D>), grid, dim3(kThreads), 0, stream, a);
+    if (timed) prof_after(stream);
+    if (int rc = check_launch("packed attention backward")) return rc;
+    if (cut.pieces == 0 || (!KEYS && !a.dq.p)) return TIGA_OK;
+    hipLaunchKernelGGL((packed_reduce_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(cut.pieces), 4), dim3(kThreads), 0, stream, a);
+    return check_launch("packed attention backward sums");
+}
+
 template <class T, int D>
 int launch(const tiga_packed &rel, const Args &a, hipStream_t stream) {
-    const int64_t by_keys = most_items(rel, 1), by_rows = most_items(rel, a.group.d);
-    const dim3 keys(static_cast<unsigned>(by_keys < 1 ? 1 : by_keys)), rows(static_cast<unsigned>(by_rows < 1 ? 1 : by_rows));
-    const bool want_keys = a.dk.p || a.dv.p;
+    const int64_t tiles = most_items(rel, 1);
+    const bool keys = a.dk.p || a.dv.p;
     if constexpr (kScaled<T>) {
-        hipLaunchKernelGGL((packed_peak_kernel<T, D>), keys, dim3(kThreads), 0, stream, a);
+        Args p = a;
+        p.least = kNoCut;
+        hipLaunchKernelGGL((packed_peak_kernel<T, D>), dim3(static_cast<unsigned>(tiles < 1 ? 1 : tiles)), dim3(kThreads), 0, stream, p);
         if (int rc = check_launch("packed attention backward peaks")) return rc;
     }
-    if (!want_keys) prof_before(stream);
-    hipLaunchKernelGGL((packed_query_kernel<T, D>), rows, dim3(kThreads), 0, stream, a);
-    if (!want_keys) prof_after(stream);
-    if (int rc = check_launch("packed attention backward, dq")) return rc;
-    if (!want_keys) return TIGA_OK;
-    prof_before(stream);
-    hipLaunchKernelGGL((packed_keys_kernel<T, D>), keys, dim3(kThreads), 0, stream, a);
-    prof_after(stream);
-    return check_launch("packed attention backward, dk and dv");
+    if (int rc = products<T, D, false>(rel, a, !keys, stream)) return rc;
+    return keys ? products<T, D, true>(rel, a, true, stream) : TIGA_OK;
 }
 
 }  // namespace
@@ -693,7 +814,7 @@ int packed_backward(const tiga_packed &rel, const tiga_view &q, const tiga_view 
                     const float *lse, const tiga_view &dy, float scale, const tiga_view &dq, const tiga_view &dk,
                     const tiga_view &dv, void *ws, hipStream_t stream) {
     const int32_t group = rel.heads / rel.kv_heads;
-    if (most_items(rel, group) > kMostBlocks || most_items(rel, 1) > kMostBlocks)
+    if (most_items(rel, group) + cut_for(rel, false).pieces > kMostBlocks || most_items(rel, 1) + cut_for(rel, true).pieces > kMostBlocks)
         return fail(TIGA_EUNSUPPORTED, "packed attention backward: at most 2^24 - 1 tiles of 128 rows or sources");
     const Layout l = layout(rel, ws);
     Args a{};
@@ -710,6 +831,7 @@ int packed_backward(const tiga_packed &rel, const tiga_view &q, const tiga_view 
     a.lse2 = l.lse2;
     a.delta = l.delta;
     a.peak = l.peak;
+    a.part = l.part;
     a.slots = static_cast<int32_t>(l.slots);
     a.num_rows = static_cast<int32_t>(rel.num_rows);
     a.batch = rel.batch;

@@ -29,6 +29,11 @@ CASES = [
     ([3 + (i * 37) % 50 for i in range(150)], 1, 1, 128, BF16),
     ([257] * 3, 32, 2, 64, F16),
     ([140, 20], 16, 16, 128, BF16),
+    # long sequences of few heads, whose backward is cut into parts
+    ([1500, 300], 2, 1, 128, BF16),
+    ([40, 3000], 1, 1, 64, F16),
+    ([2600], 4, 1, 64, BF16),
+    ([700, 1, 2200], 3, 3, 128, F16),
 ]
 
 
@@ -195,8 +200,8 @@ def test_needs_and_strided_cotangents(lib):
 
 def test_captured(lib):
     """Lengths that change between replays; eager work in between."""
-    s = Packed([100, 300, 50], 4, 2, 64, BF16, seed=13)
-    sides = [s.ptr, [0, 7, 7, 450], [0, 1, 450, 450]]
+    s = Packed([900, 2300, 50], 4, 2, 64, BF16, seed=13)
+    sides = [s.ptr, [0, 7, 7, 3250], [0, 1, 3250, 3250], [0, 1000, 2000, 3000], [100, 200, 3000, 3100]]
     run = lambda: (lambda y, lse: (y, lse, lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)))(
         *lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True))
     run()
