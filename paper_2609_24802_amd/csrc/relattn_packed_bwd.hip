@@ -30,11 +30,9 @@ struct Args {
     Divider group;
     int64_t stats;        // heads * num_rows
     float scale;
-    float *part;          // sums of parts
-    int32_t resident;     // blocks that run at once
-    int32_t least;        // levels of a part, at least (kNoCut: nothing is cut)
+    const int4 *rows_table, *keys_table;  // the pieces of dq, and of dk and dv
+    float *rows_part, *keys_part;         // sums of parts
 };
-constexpr int32_t kNoCut = 1 << 30;
 
 // Row r of a sequence's source head is token r / group of head r % group of its group.
 __device__ __forceinline__ int64_t row_at(const Args &a, const Rows &t, int32_t first, int kv, int32_t r) {
@@ -56,71 +54,99 @@ struct Item {
     int32_t b, kv, level, tiles;  // level 0: there is no such item
     int32_t part, parts;
 };
+// The pieces of one kind of owned tiles, of 128 / mult tokens: every source head has those of the table.
+struct Pieces {
+    int4 *table;       // [places][2]: first, count, b, level; part, parts
+    int32_t places, mult;
+    int32_t resident;  // blocks that run at once
+    int32_t least;     // levels of a part, at least (kNoCut: nothing is cut)
+};
+constexpr int32_t kNoCut = 1 << 30;
 // Items are cut into parts of at most `cut` levels.  How many pieces the items of the first m levels make:
 __device__ __forceinline__ int64_t pieces_upto(int32_t m, int32_t cut) {
     if (m <= cut) return m;
     const uint32_t q = static_cast<uint32_t>(m) / static_cast<uint32_t>(cut), r = static_cast<uint32_t>(m) - q * cut;
     return static_cast<int64_t>(q) * (q + 1) / 2 * cut + static_cast<int64_t>(r) * (q + 1);
 }
-// Piece `id` of tiles of 128 / mult tokens.  Sequences are taken 64 at a time, which start at or behind what the sequences
-// before them need at most; of 64, the tiles with the most levels come first: F(L) = sum of pieces_upto(tiles) - pieces_upto(L)
-// are of more than L, so the level of the n-th is the smallest L with F(L) <= n.  Only the first 64 sequences are cut, of
-// batches that have no more.
-__device__ __forceinline__ Item item_of(const Args &a, int32_t mult, int32_t id) {
-    const int lane = lane_id();
-    Item it{Run{0, 0}, 0, id % a.kv_heads, 0, 0, 0, 1};
-    int32_t n = id / a.kv_heads;
-    if (a.batch == 0) return it;
+// Writes the tables.  Sequences are taken 64 at a time (blockIdx.x), whose places start at or behind what the sequences before
+// them need at most.  Of 64, the tiles with the most levels come first: a piece of level L stands behind the sum of
+// pieces_upto(tiles) - pieces_upto(L) of those with more.  Batches of more than 64 are not cut.  (Every block finding its own
+// piece so took 12 us of each kernel's 49 to 65 for 100 short sequences of 16 heads.)
+__global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int32_t *ptr, int32_t num_rows, int32_t batch, int32_t kv_heads,
+                                                               Pieces by_rows, Pieces by_keys) {
+    const Pieces p = blockIdx.z == 0 ? by_rows : by_keys;
+    const int lane = lane_id(), base = static_cast<int>(blockIdx.x) * kWave;
+    __shared__ int32_t tiles_of[kWave], before[kWave + 1], first_of[kWave], count_of[kWave];
+    __shared__ int64_t pieces_of[kWave];
     auto start = [&](int chunk) {
-        int32_t s = a.ptr[chunk * kWave];
-        s = s < 0 ? 0 : (s > a.num_rows ? a.num_rows : s);
-        return static_cast<int32_t>(static_cast<int64_t>(s) * mult / kOwn) + chunk * kWave;
+        if (chunk == 0) return 0;
+        if (chunk * kWave >= batch) return p.places;
+        int32_t s = ptr[chunk * kWave];
+        s = s < 0 ? 0 : (s > num_rows ? num_rows : s);
+        return min(static_cast<int32_t>(static_cast<int64_t>(s) * p.mult / kOwn) + chunk * kWave, p.places);
     };
-    int lo = 0, hi = (a.batch - 1) / kWave;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (start(mid) <= n) lo = mid;
-        else hi = mid - 1;
-    }
-    const int base = lo * kWave;
-    if (a.batch > kWave) n -= start(lo);
-    if (n < 0) return it;
-    const Run mine = base + lane < a.batch ? run_between(a.ptr, base + lane, base + lane + 1, a.num_rows) : Run{0, 0};
-    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(mine.count) * mult + kOwn - 1) / kOwn);
+    const int32_t s0 = start(static_cast<int>(blockIdx.x)), s1 = start(static_cast<int>(blockIdx.x) + 1);
+    const Run mine = base + lane < batch ? run_between(ptr, base + lane, base + lane + 1, num_rows) : Run{0, 0};
+    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(mine.count) * p.mult + kOwn - 1) / kOwn);
     auto all = [&](int64_t x) { return lane_value(wave_prefix(x), kWave - 1); };
     int32_t cut = kNoCut;
-    if (a.least < kNoCut) {
+    if (p.least < kNoCut) {
         // Parts of half a block's share of all levels, or of as much more as makes at most two pieces a block, up to the whole
         // share, which makes at most twice as many parts as blocks run at once.  (dk and dv of 10,000 tokens, 4 heads over one
-        // of 128: 264 us by a simulation of this order, 407 with whole shares, 269 with one piece a block, 1329 uncut.)
-        const int64_t levels = all(static_cast<int64_t>(tiles) * (tiles + 1) / 2) * a.kv_heads;
-        const int64_t share = min(static_cast<int64_t>(kNoCut) - 1, max(static_cast<int64_t>(a.least), quotient(levels + a.resident - 1, a.resident)));
-        int64_t c = max(static_cast<int64_t>(a.least), (share + 1) / 2);
-        while (c < share && all(pieces_upto(tiles, static_cast<int32_t>(c))) * a.kv_heads > 2 * a.resident) c += c / 16 + 1;
+        // of 128: 272 us, 387 with whole shares; 1.3 ms uncut.)
+        const int64_t levels = all(static_cast<int64_t>(tiles) * (tiles + 1) / 2) * kv_heads;
+        const int64_t share = min(static_cast<int64_t>(kNoCut) - 1, max(static_cast<int64_t>(p.least), quotient(levels + p.resident - 1, p.resident)));
+        int64_t c = max(static_cast<int64_t>(p.least), (share + 1) / 2);
+        while (c < share && all(pieces_upto(tiles, static_cast<int32_t>(c))) * kv_heads > 2 * p.resident) c += c / 16 + 1;
         cut = static_cast<int32_t>(min(c, share));
     }
-    auto above = [&](int32_t level) { return all(tiles > level ? pieces_upto(tiles, cut) - pieces_upto(level, cut) : 0); };
-    int32_t from = 0, to = static_cast<int32_t>((static_cast<int64_t>(a.num_rows) * mult + kOwn - 1) / kOwn);
-    while (from < to) {
-        const int32_t mid = from + (to - from) / 2;
-        if (above(mid) <= n) to = mid;
-        else from = mid + 1;
+    const int64_t pieces = pieces_upto(tiles, cut);
+    int64_t total = all(pieces);
+    if (total > s1 - s0) total = 0;  // pointers that run backwards: nothing is done
+    const int64_t incl = wave_prefix(tiles);
+    if (threadIdx.x < kWave) {
+        tiles_of[lane] = tiles;
+        pieces_of[lane] = pieces;
+        before[lane + 1] = static_cast<int32_t>(incl);
+        if (lane == 0) before[0] = 0;
+        first_of[lane] = mine.first;
+        count_of[lane] = mine.count;
     }
-    if (from == 0) return it;
-    const int32_t parts = from <= cut ? 1 : (from + cut - 1) / cut;
-    const int32_t rest = n - static_cast<int32_t>(above(from)), k = rest / parts;
-    const uint64_t some = __ballot(tiles >= from);
-    const int before = __popcll(some & ((uint64_t(1) << lane) - 1));
-    const uint64_t hit = __ballot(tiles >= from && before == k);
-    if (hit == 0) return it;
-    const int l = __builtin_ctzll(hit);
-    it.run = Run{__builtin_amdgcn_readlane(mine.first, l), __builtin_amdgcn_readlane(mine.count, l)};
-    it.tiles = __builtin_amdgcn_readlane(tiles, l);
-    it.b = base + l;
-    it.level = from;
-    it.part = rest - k * parts;
-    it.parts = parts;
-    return it;
+    __syncthreads();
+    for (int32_t s = s0 + static_cast<int32_t>(blockIdx.y) * kThreads + threadIdx.x; s < s1; s += static_cast<int32_t>(gridDim.y) * kThreads) {
+        const int32_t r = s - s0;
+        if (r >= total) {
+            p.table[2 * s] = int4{0, 0, 0, 0};
+            continue;
+        }
+        if (r >= before[kWave]) continue;
+        int lo = 0, hi = kWave - 1;  // the r-th tile's sequence
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (before[mid] <= r) lo = mid;
+            else hi = mid - 1;
+        }
+        const int32_t level = r - before[lo] + 1, parts = level <= cut ? 1 : (level + cut - 1) / cut;
+        const int64_t upto = pieces_upto(level, cut);
+        int64_t place = 0;
+#pragma unroll 8
+        for (int i = 0; i < kWave; ++i) {
+            if (tiles_of[i] > level) place += pieces_of[i] - upto;
+            if (i < lo && tiles_of[i] >= level) place += parts;
+        }
+        for (int32_t e = 0; e < parts; ++e) {
+            const int64_t at = s0 + place + e;
+            p.table[2 * at] = int4{first_of[lo], count_of[lo], base + lo, level};
+            p.table[2 * at + 1] = int4{e, parts, 0, 0};
+        }
+    }
+}
+// mult: 128 / tokens of a tile, as in the table's Pieces.
+__device__ __forceinline__ Item item_of(const Args &a, const int4 *table, int32_t mult, int32_t id) {
+    const int32_t n = id / a.kv_heads;
+    const int4 x = table[2 * n], y = table[2 * n + 1];
+    const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(x.y) * mult + kOwn - 1) / kOwn);
+    return Item{Run{x.x, x.y}, x.z, id - n * a.kv_heads, x.w > tiles ? 0 : x.w, tiles, y.x, y.y};
 }
 // The streamed steps of a part.
 __device__ __forceinline__ int32_t part_start(int32_t steps, int32_t part, int32_t parts) {
@@ -128,7 +154,9 @@ __device__ __forceinline__ int32_t part_start(int32_t steps, int32_t part, int32
 }
 // Sums [operand][owned][D] of a part: cut items come first, so that a piece's number is its place.
 template <int D, int M>
-__device__ __forceinline__ float *part_at(const Args &a, int32_t id) { return a.part + static_cast<int64_t>(id) * M * kOwn * D; }
+__device__ __forceinline__ float *part_at(const Args &a, int32_t id) {
+    return (M == 1 ? a.rows_part : a.keys_part) + static_cast<int64_t>(id) * M * kOwn * D;
+}
 
 // Gradients of rows of no sequence: before ptr[0] and behind ptr[batch].
 template <int D>
@@ -157,8 +185,8 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads) void packed_peak_kernel(Args a) {
     constexpr int L = D / 8, ROWS = kThreads / L;  // 16 bytes a lane
     __shared__ f2 of_wave[kWaves];
-    const Item it = item_of(a, 1, static_cast<int32_t>(blockIdx.x));
-    if (it.level == 0) return;
+    const Item it = item_of(a, a.keys_table, 1, static_cast<int32_t>(blockIdx.x));
+    if (it.level == 0 || it.part != 0) return;
     const int32_t t0 = (it.tiles - it.level) * kOwn, t1 = min(t0 + kOwn, it.run.count);
     const int first = static_cast<int>(threadIdx.x) / L, c = static_cast<int>(threadIdx.x) % L;
     auto finite = [](float x) { return x < __builtin_inff() ? x : 0.0f; };  // of an absolute value; NaN too
@@ -250,18 +278,16 @@ __device__ __forceinline__ bool any_found(const int *found) { return uniform(fou
 // ------------------------------------------------------------------------------------------ dq
 
 // P (in the place of the scores) and DP of 32 streamed keys where the diagonal cuts: this lane's rows see the first
-// rel[qb] of the keys from its own 4 g on.  taint (or NULL): 0, or NaN for a key that was not finite.
+// rel[qb] of the keys from its own 4 g on.
 template <class T, int D>
-__device__ __forceinline__ void weigh_causal(Scores<T, D> &f, float c, const float *lse2, const int32_t *rel, const float *taint,
-                                             int g) {
+__device__ __forceinline__ void weigh_causal(Scores<T, D> &f, float c, const float *lse2, const int32_t *rel) {
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[qb]));
-                if (taint) p += taint[e * 16 + 4 * g + i];
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[qb]));
                 const bool sees = e * 16 + i < rel[qb];
                 f.s[e][qb][i] = sees ? p : 0.0f;
                 f.dp[e][qb][i] = sees ? f.dp[e][qb][i] : 0.0f;
@@ -272,7 +298,6 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
     using G = Geo<D>;
     __shared__ __attribute__((aligned(1024))) uint8_t y1a[G::TILE], y2a[G::TILE], y1b[G::TILE], y2b[G::TILE];
-    __shared__ float taint[2][G::BN];
     __shared__ int found[2][kWaves];
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, g = lane >> 4;
@@ -283,7 +308,7 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
         a.delta[a.stats] = 0.0f;
     }
     clear_outside<D>(a, a.dq, static_cast<int64_t>(a.kv_heads) * d);
-    const Item it = item_of(a, d, static_cast<int32_t>(blockIdx.x));
+    const Item it = item_of(a, a.rows_table, d, static_cast<int32_t>(blockIdx.x));
     if (it.level == 0) return;
     const int32_t rows = it.run.count * d, own0 = (it.level - 1) * kOwn;
     const int32_t keys = a.group.div(min(own0 + kOwn, rows) - 1) + 1;  // that the tile's last row sees
@@ -360,44 +385,45 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
     };
     const float c = a.scale * kLog2e;
     const int32_t least = a.group.div(own0) + 1;                                                  // the tile's first row sees
-    const int32_t my_least = a.group.div(min(own0 + w * 32, rows - 1)) + 1;                       // the wavefront's first row
     const int32_t my_most = own0 + w * 32 < rows ? a.group.div(min(own0 + w * 32 + 31, rows - 1)) + 1 : 0;
     auto cut = [&](int kt) { return (kt + 1) * G::BN > least; };
     // Before and after the barrier that makes a tile readable.
     auto tidy = [&](int kt, uint8_t *b1, int n) {
         if (cut(kt)) look_through<T, D>(b1, nullptr, w, found[n]);
     };
-    auto mend = [&](int kt, uint8_t *b1, int n) -> const float * {
-        if (!cut(kt) || !any_found(found[n])) return nullptr;
-        if (threadIdx.x < G::BN) taint[n][threadIdx.x] = 0.0f;
-        __syncthreads();
+    // A key that is not finite makes the sums of the rows that see it NaN, and counts as 0 without it.
+    auto mend = [&](int kt, uint8_t *b1, int n) {
+        if (!cut(kt) || !any_found(found[n])) return;
+        for (int k = 0; k < G::BN && kt * G::BN + k < keys; ++k) {
+            uint32_t bad = 0;
+#pragma unroll 1
+            for (int i = 0; i < G::CPR; ++i) bad |= any_wild<T>(reinterpret_cast<const u4 *>(b1 + k * G::RB)[i]);
+            if (uniform(bad) == 0) continue;
 #pragma unroll
-        for (int r = 0; r < G::LPW; ++r) {
-            u4 *const p = own_rows<D>(b1, w, r);
-            if (any_wild<T>(*p)) {
-                taint[n][at.krow[r]] = __builtin_nanf("");
-                *p = without_wild<T>(*p);
+            for (int qb = 0; qb < 2; ++qb) {
+                const float nan = kt * G::BN + k < sees[qb] ? __builtin_nanf("") : 0.0f;
+                own_delta[qb] += nan;
+#pragma unroll
+                for (int db = 0; db < G::DB; ++db) acc.a1[db][qb] += nan;
             }
         }
         __syncthreads();
-        return taint[n];
-    };
-    auto form = [&](Scores<T, D> &f, int kt, int kc, const uint8_t *b1, const uint8_t *b2, const float *bad) {
-        f.form(x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, [](int) {});
-        const int32_t k0 = kt * G::BN + kc * 32;
-        if (k0 + 32 > my_least || bad) {
-            const int32_t rel[2] = {sees[0] - k0 - 4 * g, sees[1] - k0 - 4 * g};
-            weigh_causal<T, D>(f, c, own, rel, bad ? bad + kc * 32 : nullptr, g);
-        } else {
-            weigh<T, D>(f, c, own, false, 0, g);
-        }
-    };
-    auto step = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *bad) {
 #pragma unroll
+        for (int r = 0; r < G::LPW; ++r) *own_rows<D>(b1, w, r) = without_wild<T>(*own_rows<D>(b1, w, r));
+        __syncthreads();
+    };
+    // 32 keys of a tile that the diagonal may cut
+    auto form = [&](Scores<T, D> &f, int kt, int kc, const uint8_t *b1, const uint8_t *b2) {
+        f.form(x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, [](int) {});
+        const int32_t k0 = kt * G::BN + kc * 32, rel[2] = {sees[0] - k0 - 4 * g, sees[1] - k0 - 4 * g};
+        weigh_causal<T, D>(f, c, own, rel);
+    };
+    auto step = [&](int kt, const uint8_t *b1, const uint8_t *b2) {
+#pragma unroll 1
         for (int kc = 0; kc < G::KC; ++kc) {
-            if (kt * G::BN + kc * 32 >= my_most) continue;
+            if (kt * G::BN + kc * 32 >= my_most) break;
             Scores<T, D> f;
-            form(f, kt, kc, b1, b2, bad);
+            form(f, kt, kc, b1, b2);
             add_keys<T, D, kQuery>(acc, f, own_delta, b1 + kc * 32 * G::RB, at.tr);
         }
     };
@@ -410,12 +436,12 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
             add_keys<T, D, kQuery>(acc, f, own_delta, b1 + kc * 32 * G::RB, at.tr);
         }
     };
-    auto deltas = [&](int kt, const uint8_t *b1, const uint8_t *b2, const float *bad) {
-#pragma unroll
+    auto deltas = [&](int kt, const uint8_t *b1, const uint8_t *b2) {
+#pragma unroll 1
         for (int kc = 0; kc < G::KC; ++kc) {
-            if (kt * G::BN + kc * 32 >= my_most) continue;
+            if (kt * G::BN + kc * 32 >= my_most) break;
             Scores<T, D> f;
-            form(f, kt, kc, b1, b2, bad);
+            form(f, kt, kc, b1, b2);
 #pragma unroll
             for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
@@ -429,9 +455,10 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
         tidy(0, y1a, 0);
         if (steps > 1) tidy(1, y1b, 1);
         __syncthreads();
-        const float *const bad0 = mend(0, y1a, 0), *const bad1 = steps > 1 ? mend(1, y1b, 1) : nullptr;
-        deltas(0, y1a, y2a, bad0);
-        if (steps > 1) deltas(1, y1b, y2b, bad1);
+        mend(0, y1a, 0);
+        if (steps > 1) mend(1, y1b, 1);
+        deltas(0, y1a, y2a);
+        if (steps > 1) deltas(1, y1b, y2b);
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             own_delta[qb] = column_sum(own_delta[qb]);
@@ -439,8 +466,8 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
         }
         leave_stats();
         if (!a.dq.p) return;
-        step(0, y1a, y2a, bad0);
-        if (steps > 1) step(1, y1b, y2b, bad1);
+        step(0, y1a, y2a);
+        if (steps > 1) step(1, y1b, y2b);
     } else {
         int kt = first_step;
         // tiles that all rows see whole, in pairs
@@ -461,18 +488,21 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
             tidy(kt, y1a, 0);
             __syncthreads();
             stage(kt + 1, y1b, y2b);
-            step(kt, y1a, y2a, mend(kt, y1a, 0));
+            mend(kt, y1a, 0);
+            step(kt, y1a, y2a);
             loads_arrived();
             tidy(kt + 1, y1b, 1);
             __syncthreads();
             if (kt + 2 < steps) stage(kt + 2, y1a, y2a);
-            step(kt + 1, y1b, y2b, mend(kt + 1, y1b, 1));
+            mend(kt + 1, y1b, 1);
+            step(kt + 1, y1b, y2b);
         }
         if (kt < steps) {
             loads_arrived();
             tidy(kt, y1a, 0);
             __syncthreads();
-            step(kt, y1a, y2a, mend(kt, y1a, 0));
+            mend(kt, y1a, 0);
+            step(kt, y1a, y2a);
         }
     }
 #pragma unroll
@@ -523,7 +553,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
 
     clear_outside<D>(a, a.dk, a.kv_heads);
     clear_outside<D>(a, a.dv, a.kv_heads);
-    const Item it = item_of(a, 1, static_cast<int32_t>(blockIdx.x));
+    const Item it = item_of(a, a.keys_table, 1, static_cast<int32_t>(blockIdx.x));
     if (it.level == 0) return;
     const int32_t own_n = it.run.count, own0 = (it.tiles - it.level) * kOwn, rows = own_n * d;
     // row tiles from the last one back to that of the first owned key (128 tokens are whole tiles)
@@ -624,7 +654,7 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     };
     auto step = [&](int n, const uint8_t *b1, const uint8_t *b2, const float *stats) {
         const int32_t k0 = (end - 1 - n) * G::BN;
-#pragma unroll
+#pragma unroll 1
         for (int kc = 0; kc < G::KC; kc += 2) {
             const uint32_t exists[2] = {pairs_of(a.group, k0 + kc * 32, g, key), pairs_of(a.group, k0 + kc * 32 + 32, g, key)};
             rows_step<T, D, true>(acc, x1, x2, b1 + kc * 32 * G::RB, b2 + kc * 32 * G::RB, at.dr, at.tr, c, h, stats + kc * 32,
@@ -693,12 +723,12 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     }
 }
 
-// Adds the parts of the item whose first part is piece blockIdx.x, in order: 4 widths a thread.
+// Adds the parts of the item whose first part is piece `id`, in order: 4 widths a thread.
 template <class T, int D, bool KEYS>
-__global__ __launch_bounds__(kThreads) void packed_reduce_kernel(Args a) {
+__device__ __forceinline__ void add_parts(const Args &a, int32_t id) {
     constexpr int L = D / 4, M = KEYS ? 2 : 1;
-    const int32_t d = KEYS ? 1 : static_cast<int32_t>(a.group.d), id = static_cast<int32_t>(blockIdx.x);
-    const Item it = item_of(a, d, id);
+    const int32_t d = KEYS ? 1 : static_cast<int32_t>(a.group.d);
+    const Item it = item_of(a, KEYS ? a.keys_table : a.rows_table, d, id);
     if (it.level == 0 || it.part != 0 || it.parts == 1) return;
     const int32_t own0 = (KEYS ? it.tiles - it.level : it.level - 1) * kOwn, rows = min(it.run.count * d - own0, kOwn);
     for (int32_t i = static_cast<int32_t>(blockIdx.y) * kThreads + threadIdx.x; i < rows * L; i += static_cast<int32_t>(gridDim.y) * kThreads) {
@@ -724,6 +754,13 @@ __global__ __launch_bounds__(kThreads) void packed_reduce_kernel(Args a) {
         }
     }
 }
+// The parts of dq (pieces below by_rows), then those of dk and dv.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void packed_reduce_kernel(Args a, int32_t by_rows) {
+    const int32_t id = static_cast<int32_t>(blockIdx.x);
+    if (id < by_rows) add_parts<T, D, false>(a, id);
+    else add_parts<T, D, true>(a, id - by_rows);
+}
 
 // ------------------------------------------------------------------------------------------ launch
 
@@ -738,72 +775,87 @@ int64_t most_items(const tiga_packed &rel, int64_t mult) {
 // Which items are cut: batches of up to 64 sequences, whose longest might have more than the least levels of a part, of
 // kLeastSteps streamed tiles.  A part's sums (64 or 128 KB at width 128) are worth that many.
 constexpr int64_t kLeastSteps = 16;
-struct Cut {
-    int32_t resident, least;  // as in Args
-    int64_t pieces;           // of cut items, at most
+struct Plan {
+    int32_t resident, least;  // as in Pieces
+    int64_t cut;              // pieces of cut items, at most
+    int64_t places;           // of the table: a source head's pieces, at most
 };
-Cut cut_for(const tiga_packed &rel, bool keys) {
+Plan plan_for(const tiga_packed &rel, bool keys) {
     const int64_t group = rel.heads / rel.kv_heads, bn = rel.width == 64 ? 128 : 64;
-    Cut c;
-    c.resident = device_cus() * (keys && rel.width == 128 ? 1 : 2);
+    Plan p;
+    p.resident = device_cus() * (keys && rel.width == 128 ? 1 : 2);
     const int64_t least = ceil_div(kLeastSteps * bn * (keys ? 1 : group), kOwn * (keys ? group : 1));
     const int64_t most = ceil_div(rel.num_rows * (keys ? 1 : group), kOwn);
     const bool some = rel.batch <= kWave && most > least;
-    c.least = some ? static_cast<int32_t>(least) : kNoCut;
-    c.pieces = some ? 2 * static_cast<int64_t>(c.resident) + rel.kv_heads : 0;
-    return c;
+    p.least = some ? static_cast<int32_t>(least) : kNoCut;
+    p.cut = some ? 2 * static_cast<int64_t>(p.resident) : 0;
+    p.places = most_items(rel, keys ? 1 : group) / rel.kv_heads + ceil_div(p.cut, rel.kv_heads);
+    return p;
 }
 
 struct Layout {
-    float *lse2, *delta, *part;
+    Plan rows, keys;
+    int4 *rows_table, *keys_table;
+    float *lse2, *delta, *rows_part, *keys_part;
     f2 *peak;
     int64_t slots;
     size_t bytes;
 };
 Layout layout(const tiga_packed &rel, void *ws) {
     Layout l;
+    l.rows = plan_for(rel, false);
+    l.keys = plan_for(rel, true);
     Carve c(ws);
     const size_t stats = static_cast<size_t>(rel.heads) * rel.num_rows + 1;
     l.lse2 = c.take<float>(stats);
     l.delta = c.take<float>(stats);
     l.slots = rel.num_rows / kOwn + rel.batch + 1;
     l.peak = c.take<f2>(l.slots * rel.kv_heads);
-    // whether this call's items are cut or not: a workspace holds every smaller call
-    const size_t pieces = 2 * static_cast<size_t>(device_cus()) * (rel.width == 128 ? 1 : 2) + rel.kv_heads;
-    l.part = c.take<float>((rel.num_rows > kOwn ? pieces : 0) * 2 * kOwn * rel.width);
+    // for any number of heads, and whether this call's items are cut or not: a workspace holds every smaller call
+    const size_t cus = device_cus(), some = rel.num_rows > kOwn ? 1 : 0;
+    const size_t places = static_cast<size_t>(rel.num_rows) / kOwn + rel.batch + 4 * cus + 1;
+    l.rows_table = c.take<int4>(2 * (places + static_cast<size_t>(rel.num_rows) * rel.heads / kOwn));
+    l.keys_table = c.take<int4>(2 * places);
+    l.rows_part = c.take<float>(some * (4 * cus + rel.heads) * kOwn * rel.width);
+    l.keys_part = c.take<float>(some * ((rel.width == 128 ? 2 : 4) * cus + rel.heads) * 2 * kOwn * rel.width);
     l.bytes = c.bytes();
     return l;
 }
 
-template <class T, int D, bool KEYS>
-int products(const tiga_packed &rel, Args a, bool timed, hipStream_t stream) {
-    const Cut cut = cut_for(rel, KEYS);
-    a.resident = cut.resident;
-    a.least = cut.least;
-    const int64_t items = most_items(rel, KEYS ? 1 : a.group.d) + cut.pieces;
-    const dim3 grid(static_cast<unsigned>(items < 1 ? 1 : items));
-    if (timed) prof_before(stream);
-    if constexpr (KEYS) hipLaunchKernelGGL((packed_keys_kernel<T, D>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((packed_query_kernel<T, D>), grid, dim3(kThreads), 0, stream, a);
-    if (timed) prof_after(stream);
-    if (int rc = check_launch("packed attention backward")) return rc;
-    if (cut.pieces == 0 || (!KEYS && !a.dq.p)) return TIGA_OK;
-    hipLaunchKernelGGL((packed_reduce_kernel<T, D, KEYS>), dim3(static_cast<unsigned>(cut.pieces), 4), dim3(kThreads), 0, stream, a);
-    return check_launch("packed attention backward sums");
-}
-
 template <class T, int D>
-int launch(const tiga_packed &rel, const Args &a, hipStream_t stream) {
-    const int64_t tiles = most_items(rel, 1);
+int launch(const Layout &l, const tiga_packed &rel, const Args &a, hipStream_t stream) {
+    const int64_t chunks = ceil_div(rel.batch, kWave);
+    const int64_t most = l.rows.places > l.keys.places ? l.rows.places : l.keys.places;
+    int64_t turns = rel.batch <= kWave ? ceil_div(most, kThreads) : 4;
+    if (turns > 256) turns = 256;
     const bool keys = a.dk.p || a.dv.p;
+    const Pieces by_rows{l.rows_table, static_cast<int32_t>(l.rows.places), static_cast<int32_t>(a.group.d), l.rows.resident, l.rows.least};
+    const Pieces by_keys{l.keys_table, static_cast<int32_t>(l.keys.places), 1, l.keys.resident, l.keys.least};
+    hipLaunchKernelGGL(packed_plan_kernel, dim3(static_cast<unsigned>(chunks < 1 ? 1 : chunks), static_cast<unsigned>(turns < 1 ? 1 : turns), 2),
+                       dim3(kThreads), 0, stream, rel.ptr, a.num_rows, a.batch, a.kv_heads, by_rows, by_keys);
+    if (int rc = check_launch("packed attention backward, plan")) return rc;
+    const dim3 row_blocks(static_cast<unsigned>(l.rows.places * rel.kv_heads)), key_blocks(static_cast<unsigned>(l.keys.places * rel.kv_heads));
     if constexpr (kScaled<T>) {
-        Args p = a;
-        p.least = kNoCut;
-        hipLaunchKernelGGL((packed_peak_kernel<T, D>), dim3(static_cast<unsigned>(tiles < 1 ? 1 : tiles)), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL((packed_peak_kernel<T, D>), key_blocks, dim3(kThreads), 0, stream, a);
         if (int rc = check_launch("packed attention backward peaks")) return rc;
     }
-    if (int rc = products<T, D, false>(rel, a, !keys, stream)) return rc;
-    return keys ? products<T, D, true>(rel, a, true, stream) : TIGA_OK;
+    if (!keys) prof_before(stream);
+    hipLaunchKernelGGL((packed_query_kernel<T, D>), row_blocks, dim3(kThreads), 0, stream, a);
+    if (!keys) prof_after(stream);
+    if (int rc = check_launch("packed attention backward, dq")) return rc;
+    if (keys) {
+        prof_before(stream);
+        hipLaunchKernelGGL((packed_keys_kernel<T, D>), key_blocks, dim3(kThreads), 0, stream, a);
+        prof_after(stream);
+        if (int rc = check_launch("packed attention backward, dk and dv")) return rc;
+    }
+    // whole places, so that parts of every head are seen
+    const int64_t row_parts = a.dq.p && l.rows.cut ? ceil_div(l.rows.cut, rel.kv_heads) * rel.kv_heads : 0;
+    const int64_t key_parts = keys && l.keys.cut ? ceil_div(l.keys.cut, rel.kv_heads) * rel.kv_heads : 0;
+    if (row_parts + key_parts == 0) return TIGA_OK;
+    hipLaunchKernelGGL((packed_reduce_kernel<T, D>), dim3(static_cast<unsigned>(row_parts + key_parts), 4), dim3(kThreads), 0, stream, a,
+                       static_cast<int32_t>(row_parts));
+    return check_launch("packed attention backward sums");
 }
 
 }  // namespace
@@ -814,9 +866,9 @@ int packed_backward(const tiga_packed &rel, const tiga_view &q, const tiga_view 
                     const float *lse, const tiga_view &dy, float scale, const tiga_view &dq, const tiga_view &dk,
                     const tiga_view &dv, void *ws, hipStream_t stream) {
     const int32_t group = rel.heads / rel.kv_heads;
-    if (most_items(rel, group) + cut_for(rel, false).pieces > kMostBlocks || most_items(rel, 1) + cut_for(rel, true).pieces > kMostBlocks)
-        return fail(TIGA_EUNSUPPORTED, "packed attention backward: at most 2^24 - 1 tiles of 128 rows or sources");
     const Layout l = layout(rel, ws);
+    if (l.rows.places * rel.kv_heads > kMostBlocks || l.keys.places * rel.kv_heads > kMostBlocks)
+        return fail(TIGA_EUNSUPPORTED, "packed attention backward: at most 2^24 - 1 tiles of 128 rows or sources");
     Args a{};
     a.q = rows_of(q);
     a.k = rows_of(k);
@@ -831,7 +883,10 @@ int packed_backward(const tiga_packed &rel, const tiga_view &q, const tiga_view 
     a.lse2 = l.lse2;
     a.delta = l.delta;
     a.peak = l.peak;
-    a.part = l.part;
+    a.rows_table = l.rows_table;
+    a.keys_table = l.keys_table;
+    a.rows_part = l.rows_part;
+    a.keys_part = l.keys_part;
     a.slots = static_cast<int32_t>(l.slots);
     a.num_rows = static_cast<int32_t>(rel.num_rows);
     a.batch = rel.batch;
@@ -839,8 +894,8 @@ int packed_backward(const tiga_packed &rel, const tiga_view &q, const tiga_view 
     a.group = divider(group);
     a.stats = static_cast<int64_t>(rel.heads) * rel.num_rows;
     a.scale = scale;
-    if (rel.dtype == TIGA_DT_F16) return rel.width == 64 ? launch<Half16, 64>(rel, a, stream) : launch<Half16, 128>(rel, a, stream);
-    return rel.width == 64 ? launch<Brain16, 64>(rel, a, stream) : launch<Brain16, 128>(rel, a, stream);
+    if (rel.dtype == TIGA_DT_F16) return rel.width == 64 ? launch<Half16, 64>(l, rel, a, stream) : launch<Half16, 128>(l, rel, a, stream);
+    return rel.width == 64 ? launch<Brain16, 64>(l, rel, a, stream) : launch<Brain16, 128>(l, rel, a, stream);
 }
 
 }  // namespace relattn

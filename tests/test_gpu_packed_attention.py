@@ -232,8 +232,15 @@ def test_on_another_stream(lib):
 def test_pointers_that_run_backwards_stay_inside(lib):
     """Nothing is promised about such a call but that it stays within the tensors and ends."""
     s = Packed([100, 60, 40], 2, 1, 64, F16, seed=15)
-    for p in ([0, 160, 100, 200], [-5, 100, 50, 1 << 30], [200, 100, 50, 0], [1 << 30, -1, 1 << 30, 3]):
-        s.ptr_t.copy_(torch.tensor(p, dtype=torch.int32))
-        y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
-        lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t)
+    many = [(i * 7919) % 211 for i in range(200)]
+    for p in ([0, 160, 100, 200], [-5, 100, 50, 1 << 30], [200, 100, 50, 0], [1 << 30, -1, 1 << 30, 3], [0, 200] * 30, many,
+              [0, 200] * 100):
+        ptr = torch.tensor(p, dtype=torch.int32, device="cuda")
+        y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, ptr, want_lse=True)
+        lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, ptr)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("lead", [1, 700])
+def test_many_sequences_behind_rows_of_none(lib, lead):
+    check(lib, Packed([1 + (i * 29) % 40 for i in range(130)], 2, 1, 64, BF16, seed=16, lead=lead, tail=3), "many")
