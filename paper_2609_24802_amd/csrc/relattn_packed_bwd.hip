@@ -113,6 +113,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int32_t *pt
         count_of[lane] = mine.count;
     }
     __syncthreads();
+    const int here = min(batch - base, kWave);
     for (int32_t s = s0 + static_cast<int32_t>(blockIdx.y) * kThreads + threadIdx.x; s < s1; s += static_cast<int32_t>(gridDim.y) * kThreads) {
         const int32_t r = s - s0;
         if (r >= total) {
@@ -129,8 +130,8 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int32_t *pt
         const int32_t level = r - before[lo] + 1, parts = level <= cut ? 1 : (level + cut - 1) / cut;
         const int64_t upto = pieces_upto(level, cut);
         int64_t place = 0;
-#pragma unroll 8
-        for (int i = 0; i < kWave; ++i) {
+#pragma unroll 4
+        for (int i = 0; i < here; ++i) {
             if (tiles_of[i] > level) place += pieces_of[i] - upto;
             if (i < lo && tiles_of[i] >= level) place += parts;
         }
