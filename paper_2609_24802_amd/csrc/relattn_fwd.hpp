@@ -1334,12 +1334,102 @@ __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
     }
 }
 
+// The slot of the n-th item that has parts, or -1.
+template <Relation REL>
+__device__ __forceinline__ int nth_item(const Args<REL> &a, int n) {
+    constexpr int U = 8;
+    for (int e = 0; e < a.slots; e += U * kWave) {
+        int mine[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) mine[i] = e + i * kWave + lane_id() < a.slots ? a.rec[2 * (e + i * kWave + lane_id())].x : 0;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const uint64_t starts = __ballot(mine[i] != 0);
+            const int here = __popcll(starts);
+            if (n < here) {
+                const int before = __popcll(starts & ((uint64_t(1) << lane_id()) - 1));
+                return e + i * kWave + __builtin_ctzll(__ballot(mine[i] != 0 && before == n));
+            }
+            n -= here;
+        }
+    }
+    return -1;
+}
+
+// Joins the parts of the n-th wide item of shared positions: there are few items (the rows of a group are one tile or two a
+// head) of many parts, so a block takes the rows that a wavefront reads at once, and each wavefront a quarter of the parts;
+// the quarters are joined in order.
+template <class T, class G>
+__global__ __launch_bounds__(kThreads) void shared_merge_kernel(Args<kShared> a) {
+    constexpr int D = G::CPR * 8, BM = G::BM, L = D / 4, AT = kWave / L, U = 8;
+    typedef Deal<kShared, BM, G::BN> Pieces;
+    __shared__ f4 so[kWaves][kWave];
+    __shared__ float sm[kWaves][AT], sl[kWaves][AT];
+    const int x = nth_item(a, static_cast<int>(blockIdx.x));
+    if (x < 0) return;
+    const int4 it = a.rec[2 * x];
+    const int b = it.x - 1, head = it.y, j = it.z, n = it.w;
+    const Seq s = seq_of<kShared>(a, b);
+    const int rows = min(s.rows - j * BM, BM), r0 = static_cast<int>(blockIdx.y) * AT;
+    if (r0 >= rows) return;
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int row = min(r0 + lane / L, rows - 1), tiles = Pieces::load(a, s).tiles;  // the parts of a row tile lie `tiles` apart
+    float m = -__builtin_inff(), l = 0.0f;
+    f4 o{0.0f, 0.0f, 0.0f, 0.0f};
+    const int last = n * (w + 1) / kWaves;
+    for (int c = n * w / kWaves; c < last; c += U) {
+        f4 po[U];
+        float pm[U], pl[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+            const float *const p = a.part + (x + static_cast<int64_t>(min(c + i, last - 1)) * tiles) * slot_floats<BM, D>();
+            pm[i] = p[BM * D + row];
+            pl[i] = p[BM * (D + 1) + row];
+            po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < U; ++i) top = fmaxf(top, pm[i]);
+        const float ref = top == -__builtin_inff() ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+        m = top;
+        l *= alpha;
+        o *= alpha;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (c + i >= last) break;
+            const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
+            l += f * pl[i];
+            o += f * po[i];
+        }
+    }
+    so[w][lane] = o;
+    if (lane % L == 0) {
+        sm[w][lane / L] = m;
+        sl[w][lane / L] = l;
+    }
+    __syncthreads();
+    if (w != 0 || r0 + lane / L >= rows) return;
+    for (int i = 1; i < kWaves; ++i) m = fmaxf(m, sm[i][lane / L]);
+    const float ref = m == -__builtin_inff() ? 0.0f : m;
+    l = 0.0f;
+    o = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        const float f = __builtin_amdgcn_exp2f(sm[i][lane / L] - ref);
+        l += f * sl[i][lane / L];
+        o += so[i][lane] * f;
+    }
+    put<T>(out_row<D, kShared>(a, b, s, head, j * BM + row) + 4 * (lane % L), o * (l == 0.0f ? 0.0f : 1.0f / l));
+    if (lane % L == 0) put_lse(a, b, s, head, j * BM + row, m + __log2f(l));
+}
+
 // ------------------------------------------------------------------------------------------ launch
 
 // How a call is laid out, from what the host knows: sizes and upper bounds of the lengths.
 struct Plan {
     int64_t blocks;  // of the main kernel and (narrow) of the merge
     int64_t slots;   // partial states, 0: items are not cut
+    int64_t items;   // at most
 };
 template <class G>
 int64_t steps_of(int64_t longest) { return ceil_div(longest < 1 ? 1 : longest, G::BN); }
@@ -1350,7 +1440,7 @@ constexpr bool kNarrow = G::BM < 128;
 template <class G>
 Plan plan_for(int64_t most, int64_t least, int64_t longest, bool alike) {
     const int64_t resident = 2 * static_cast<int64_t>(device_cus()), steps = steps_of<G>(longest);
-    Plan p{most, 0};
+    Plan p{most, 0, most};
     if (kNarrow<G>) {
         // equal runs for the resident blocks, two slots a block; items of one key tile are dealt whole
         p.blocks = most * steps < resident ? most * steps : resident;
@@ -1418,6 +1508,9 @@ int run(const Plan &p, Args<REL> a, void *ws, hipStream_t stream) {
     if constexpr (kNarrow<G>)
         hipLaunchKernelGGL((thin_merge_kernel<T, D, REL>), dim3(static_cast<unsigned>(p.blocks), kWaves), dim3(kThreads), 0,
                            stream, a, static_cast<int>(p.blocks));
+    else if constexpr (REL == kShared)  // items that have parts are fewer than slots
+        hipLaunchKernelGGL((shared_merge_kernel<T, G>), dim3(static_cast<unsigned>(p.items < p.slots ? p.items : p.slots), G::BM * (D / 4) / kWave),
+                           dim3(kThreads), 0, stream, a);
     else
         hipLaunchKernelGGL((wide_merge_kernel<T, G, REL>), dim3(static_cast<unsigned>(p.slots), G::BM / 16), dim3(kThreads), 0,
                            stream, a);
