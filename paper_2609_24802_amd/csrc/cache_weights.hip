@@ -6,6 +6,13 @@
 // to end and every block walks an equal run of them.  A wavefront takes 32 or 64 keys a step, a step ahead in registers in
 // the matrix operand's layout, with the queries as the other operand: a result's column is a key, and the sum over the rows
 // is one over four registers and four lanes.
+//
+// Many rows (chunks of prompts): bound by the exponentials (4 quarter-rate and 8 full-rate instructions for 256 pairs, where
+// their products take two thirds of that on the matrix cores at width 128).  A block owns 128 keys, 32 a wavefront as operands
+// in registers, and streams the rows through LDS.  Where there are few keys the rows are cut into parts, whose sums (512
+// bytes) go to the workspace and are added in order by a second launch.
+#include <type_traits>
+
 #include "mfma16.hpp"
 #include "relation.hpp"
 #include "retention.hpp"
@@ -30,6 +37,8 @@ struct Args {
     float c, decay;    // c = scale * log2 e
     int kv_heads;
     Divider group;
+    int32_t few;       // rows of the sequences that the narrow kernel takes, at most; the others are the wide one's
+    float *part;       // [kMostParts][kOwn]
 };
 
 // Positions of a sequence: none past the table.
@@ -37,6 +46,10 @@ __device__ __forceinline__ int32_t positions(const Pages &c, int b) {
     const int64_t n = c.length[b], most = static_cast<int64_t>(c.table_width) << c.shift;
     return static_cast<int32_t>(n < 0 ? 0 : (n > most ? most : n));
 }
+
+__device__ __forceinline__ int32_t new_rows(const Args &a, int b) { return chunk_of(a.src, b).count * static_cast<int32_t>(a.group.d); }
+// Positions of a sequence that the narrow kernel takes.
+__device__ __forceinline__ int32_t narrow_positions(const Args &a, int b) { return new_rows(a, b) <= a.few ? positions(a.src, b) : 0; }
 
 // The tiles of BN keys of all sequences and heads end to end, and a block's run of them.
 template <int BN>
@@ -49,7 +62,7 @@ struct Run1 {
     static __device__ __forceinline__ int32_t tiles(int32_t n) { return (n + BN - 1) / BN; }
     __device__ __forceinline__ void begin(const Args &a, int w, int blocks) {
         const int nb = a.src.batch;
-        auto fetch = [&](int e) { return e < nb ? positions(a.src, e) : 0; };
+        auto fetch = [&](int e) { return e < nb ? narrow_positions(a, e) : 0; };
         mine = fetch(lane_id());
         int64_t all = 0;
         for (int e = 0; e < nb; e += kWave)
@@ -73,7 +86,7 @@ struct Run1 {
             }
             base += lane_value(incl, kWave - 1);
         }
-        n = b < kWave ? __builtin_amdgcn_readlane(mine, b) : positions(a.src, b);
+        n = b < kWave ? __builtin_amdgcn_readlane(mine, b) : narrow_positions(a, b);
     }
     struct Tile {
         int32_t b, head, n, k0;  // k0: its first key
@@ -83,7 +96,7 @@ struct Run1 {
         while (u >= base + static_cast<int64_t>(tiles(n)) * a.kv_heads) {  // a later sequence holds u
             base += static_cast<int64_t>(tiles(n)) * a.kv_heads;
             ++b;
-            n = b < kWave ? __builtin_amdgcn_readlane(mine, b) : positions(a.src, b);
+            n = b < kWave ? __builtin_amdgcn_readlane(mine, b) : narrow_positions(a, b);
         }
         const int64_t in = u - base, head = quotient(in, tiles(n));
         t = Tile{b, static_cast<int32_t>(head), n, static_cast<int32_t>(in - head * tiles(n)) * BN};
@@ -204,15 +217,249 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(Args a) {
     }
 }
 
+// ------------------------------------------------------------------------------------------ many rows
+
+constexpr int kOwn = 128;          // keys of a block
+constexpr int kLeastSteps = 4;     // row tiles of a part, at least
+
+template <int D>
+struct Wide {
+    static constexpr int RB = 2 * D, CPR = D / 8, R = 256 / RB, CH = D / 32;
+    static constexpr int BN = D == 64 ? 128 : 64;     // rows a tile
+    static constexpr int TILE = BN * RB;              // 16 KB
+    static constexpr int LPW = TILE / 1024 / kWaves;  // 1-KB direct loads per wavefront and tile
+};
+// 16-byte chunk c of row k lies at chunk c ^ swizzle(k): the 16 rows of a read fall into 16 bank groups.
+template <int D>
+__device__ __forceinline__ int swizzle(int k) { return (k / Wide<D>::R) % Wide<D>::CPR; }
+
+// A sequence with many rows: `tiles` of its positions, `steps` of its rows, cut into `parts`.
+struct Load {
+    int32_t tiles, steps;
+    __device__ __forceinline__ int32_t parts(int32_t most) const { return (steps + most - 1) / most; }
+};
+template <int D>
+__device__ __forceinline__ Load load_of(const Args &a, int b) {
+    if (b >= a.src.batch) return Load{0, 0};
+    const int32_t rows = new_rows(a, b);
+    if (rows <= a.few) return Load{0, 0};
+    return Load{(positions(a.src, b) + kOwn - 1) / kOwn, (rows + Wide<D>::BN - 1) / Wide<D>::BN};
+}
+// How the sequences are cut: into parts of at most `most` steps, such that there are about `blocks` pieces of cut sequences.
+// Pieces are in the order (sequence, head, part, tile): neighbours read the same rows.  A cut sequence's pieces are counted
+// apart, which gives their places in the workspace: fewer than work / most + one for each cut item, so under 2 blocks.
+template <int D>
+struct Cut {
+    Load first;       // of the lane's of the first 64 sequences
+    int32_t most;
+    int64_t pieces;   // of a head
+    static __device__ __forceinline__ int64_t all(int64_t x) { return lane_value(wave_prefix(x), kWave - 1); }
+    template <class F>
+    __device__ __forceinline__ int64_t sum(const Args &a, F f) const {
+        int64_t n = all(f(first));
+        for (int e = kWave; e < a.src.batch; e += kWave) n += all(f(load_of<D>(a, e + lane_id())));
+        return n;
+    }
+    __device__ __forceinline__ Cut(const Args &a, int blocks) : first(load_of<D>(a, lane_id())) {
+        const int64_t work = sum(a, [](const Load &l) { return static_cast<int64_t>(l.tiles) * l.steps; }) * a.kv_heads;
+        most = static_cast<int32_t>(min(static_cast<int64_t>(0x7fffffff), max(static_cast<int64_t>(kLeastSteps), quotient(work + blocks - 1, blocks))));
+        pieces = sum(a, [&](const Load &l) { return static_cast<int64_t>(l.tiles) * l.parts(most); }) * a.kv_heads;
+    }
+    struct Piece {
+        int32_t b, head, part, parts, tile;
+        int64_t place;  // among the pieces of cut sequences
+        Load load;
+    };
+    // Piece id of all (or, CUT_ITEMS, item id of the cut sequences: part 0).
+    template <bool CUT_ITEMS>
+    __device__ __forceinline__ bool find(const Args &a, int64_t id, Piece &p) const {
+        int64_t base = 0, cut_base = 0;
+        for (int e = 0; e < a.src.batch; e += kWave) {
+            const Load l = e == 0 ? first : load_of<D>(a, e + lane_id());
+            const int32_t parts = l.parts(most);
+            const int64_t own = static_cast<int64_t>(l.tiles) * a.kv_heads, cut = parts > 1 ? own * parts : 0;
+            const int64_t mine = CUT_ITEMS ? (parts > 1 ? own : 0) : own * parts;
+            const int64_t incl = wave_prefix(mine), cut_incl = wave_prefix(cut);
+            const uint64_t past = __ballot(base + incl > id);
+            if (past) {
+                const int i = __builtin_ctzll(past);
+                p.b = e + i;
+                p.load = Load{__builtin_amdgcn_readlane(l.tiles, i), __builtin_amdgcn_readlane(l.steps, i)};
+                p.parts = p.load.parts(most);
+                int64_t rest = id - (base + lane_value(incl - mine, i));
+                const int64_t per = static_cast<int64_t>(p.load.tiles) * (CUT_ITEMS ? 1 : p.parts);
+                p.head = static_cast<int32_t>(quotient(rest, per));
+                rest -= p.head * per;
+                p.part = static_cast<int32_t>(quotient(rest, p.load.tiles));
+                p.tile = static_cast<int32_t>(rest - static_cast<int64_t>(p.part) * p.load.tiles);
+                p.place = cut_base + lane_value(cut_incl - cut, i) + (static_cast<int64_t>(p.head) * p.parts + p.part) * p.load.tiles + p.tile;
+                return true;
+            }
+            base += lane_value(incl, kWave - 1);
+            cut_base += lane_value(cut_incl, kWave - 1);
+        }
+        return false;
+    }
+};
+__device__ __forceinline__ int64_t cell_of(const Args &a, int32_t page, int head, int32_t at) {
+    return ((static_cast<int64_t>(page) * a.kv_heads + head) << a.src.shift) + (at & ((1 << a.src.shift) - 1));
+}
+// The weight of a position: what the rows give it, and what is left of the old one.
+__device__ __forceinline__ void put_weight(const Args &a, int b, int head, int64_t pos0, int32_t at, float given) {
+    const int32_t page = page_at(a.src, b, at);
+    if (page < 0) return;
+    const int64_t cell = cell_of(a, page, head, at);
+    a.out[cell] = given + (at < pos0 ? a.decay * a.in[cell] : 0.0f);
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 4) void wide_weights_kernel(Args a, int blocks) {
+    using G = Wide<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t qa[G::TILE], qb[G::TILE];
+    __shared__ __attribute__((aligned(256))) float sta[G::BN], stb[G::BN];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
+    const int col = lane & 15, g = lane >> 4;
+    const int32_t d = static_cast<int32_t>(a.group.d);
+    int krow[G::LPW], kch[G::LPW];
+#pragma unroll
+    for (int r = 0; r < G::LPW; ++r) {
+        const int byte = (w * G::LPW + r) * 1024 + 16 * lane;
+        krow[r] = byte / G::RB;
+        kch[r] = byte % G::RB / 16 ^ swizzle<D>(krow[r]);
+    }
+    const int dr = col * G::RB + 16 * (g ^ swizzle<D>(col));
+    const Cut<D> cut(a, blocks);
+    for (int64_t id = xcd_block(); id < cut.pieces; id += gridDim.x) {
+        typename Cut<D>::Piece pc;
+        if (!cut.template find<false>(a, id, pc)) break;
+        const Chunk chunk = chunk_of(a.src, pc.b);
+        const int32_t n = positions(a.src, pc.b), rows = chunk.count * d, k0 = pc.tile * kOwn;
+        // the steps of the part that see a key of the tile
+        const int64_t from = static_cast<int64_t>(k0) - chunk.pos0 > 0 ? (static_cast<int64_t>(k0) - chunk.pos0) * d / G::BN : 0;
+        const int32_t t0 = static_cast<int32_t>(max(from, static_cast<int64_t>(pc.load.steps) * pc.part / pc.parts));
+        const int32_t t1 = static_cast<int32_t>(static_cast<int64_t>(pc.load.steps) * (pc.part + 1) / pc.parts);
+        auto at = [&](int32_t r, int64_t head_stride, int64_t row_stride) {
+            const int32_t token = a.group.div(r);
+            return static_cast<int64_t>(pc.head * d + r - token * d) * head_stride + (chunk.first + token) * row_stride;
+        };
+        float lse = 0.0f;  // of row threadIdx.x of the staged tile
+        auto stage = [&](int kt, uint8_t *buf) {
+            const int32_t r0 = kt * G::BN;
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r)  // past the end: the last row again, without weight
+                load_to_lds16(a.q.p + at(min(r0 + krow[r], rows - 1), a.q.head, a.q.row) + 8 * kch[r], buf + (w * G::LPW + r) * 1024);
+            const int32_t r = r0 + static_cast<int32_t>(threadIdx.x);
+            if (threadIdx.x < G::BN) lse = r < rows ? a.lse[at(r, a.src.num_dst, 1)] : -__builtin_inff();
+        };
+        __syncthreads();  // the previous piece's tiles are read
+        if (t0 < t1) stage(t0, qa);
+        u4 k[2][G::CH];
+        int32_t key[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            key[x] = k0 + w * 32 + x * 16 + col;
+            const int32_t pos = min(key[x], n - 1), entry = entry_at(a.src, pc.b, pos);
+            const int32_t page = is_page(a.src, entry) ? entry : 0;  // a key of some page, whose weight is not stored
+            const uint16_t *const p = a.src.k.p + page * a.src.k.batch + pc.head * a.src.k.head +
+                                      static_cast<int64_t>(pos & ((1 << a.src.shift) - 1)) * a.src.k.row;
+#pragma unroll
+            for (int ch = 0; ch < G::CH; ++ch) k[x][ch] = reinterpret_cast<const u4 *>(p)[ch * 4 + g];
+        }
+        f4 sum[2] = {f4{0.0f, 0.0f, 0.0f, 0.0f}, f4{0.0f, 0.0f, 0.0f, 0.0f}};
+        const int64_t last = static_cast<int64_t>(min(k0 + kOwn, n)) - 1 - chunk.pos0;  // the first token that sees all keys
+        auto step = [&](int kt, const uint8_t *buf, const float *st) {
+            const int32_t r0 = kt * G::BN;
+            const bool edge = a.group.div(r0) < last;
+#pragma unroll 2
+            for (int rb = 0; rb < G::BN / 16; ++rb) {
+                f4 s[2];
+#pragma unroll
+                for (int ch = 0; ch < G::CH; ++ch) {
+                    const u4 q = *reinterpret_cast<const u4 *>(buf + (dr ^ (64 * ch)) + rb * 16 * G::RB);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) s[x] = T::mma(q, k[x][ch], ch == 0 ? f4{0.0f, 0.0f, 0.0f, 0.0f} : s[x]);
+                }
+                const f4 lse2 = *reinterpret_cast<const f4 *>(st + rb * 16 + 4 * g);
+                if (edge) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t pos = chunk.pos0 + a.group.div(r0 + rb * 16 + 4 * g + i);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], a.c, -lse2[i]));
+                            sum[x][i] += key[x] <= pos ? p : 0.0f;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[x][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], a.c, -lse2[i]));
+                }
+            }
+        };
+        auto arrive = [&](float *st) {
+            loads_arrived();
+            if (threadIdx.x < G::BN) st[threadIdx.x] = log2_of(lse);
+            __syncthreads();
+        };
+        for (int kt = t0; kt < t1; kt += 2) {
+            arrive(sta);
+            if (kt + 1 < t1) stage(kt + 1, qb);
+            step(kt, qa, sta);
+            if (kt + 1 >= t1) break;
+            arrive(stb);
+            if (kt + 2 < t1) stage(kt + 2, qa);
+            step(kt + 1, qb, stb);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float all = column_sum((sum[x][0] + sum[x][1]) + (sum[x][2] + sum[x][3]));
+            if (g != 0 || key[x] >= n) continue;
+            if (pc.parts > 1) a.part[pc.place * kOwn + key[x] - k0] = all;
+            else put_weight(a, pc.b, pc.head, chunk.pos0, key[x], all);
+        }
+    }
+}
+
+// The parts of the cut sequences' sums, in order: a key a thread, an item a block.
+template <int D>
+__global__ __launch_bounds__(kOwn) void add_weights_kernel(Args a, int blocks) {
+    const Cut<D> cut(a, blocks);
+    for (int64_t id = blockIdx.x;; id += gridDim.x) {
+        typename Cut<D>::Piece pc;
+        if (!cut.template find<true>(a, id, pc)) return;
+        const int32_t key = pc.tile * kOwn + static_cast<int32_t>(threadIdx.x);
+        if (key >= positions(a.src, pc.b)) continue;
+        float sum = 0.0f;
+        const float *p = a.part + pc.place * kOwn + threadIdx.x;
+#pragma unroll 8
+        for (int e = 0; e < pc.parts; ++e) sum += p[static_cast<int64_t>(e) * pc.load.tiles * kOwn];
+        put_weight(a, pc.b, pc.head, chunk_of(a.src, pc.b).pos0, key, sum);
+    }
+}
+
+// Narrow for all sequences where they have at most 16 rows on average; otherwise for those that have, and the wide kernel for
+// the others.
+constexpr int64_t kFewRows = 16;
+bool all_narrow(const tiga_cache &c, int64_t num_dst, int32_t heads) {
+    const int64_t some = num_dst < c.batch ? num_dst : c.batch;
+    return num_dst * (heads / c.kv_heads) <= kFewRows * some;
+}
+int64_t wide_blocks() { return 4 * static_cast<int64_t>(device_cus()); }
+
 }  // namespace
 
-size_t weights_ws_bytes(const tiga_cache &, int64_t, int32_t) { return 256; }
+size_t weights_ws_bytes(const tiga_cache &, int64_t num_dst, int32_t heads) {
+    // of any number of source heads and sequences
+    return num_dst * heads <= kFewRows ? 256 : 2 * wide_blocks() * kOwn * sizeof(float);
+}
 
 int accumulate(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads, const tiga_view &q,
-               const float *lse, float scale, float decay, const float *weights, float *out, void *, hipStream_t stream) {
+               const float *lse, float scale, float decay, const float *weights, float *out, void *ws, hipStream_t stream) {
     Args a{};
     a.src = pages_of(cache, num_dst, dst_ptr);
-    a.q = rows_of(q);
+    a.q = relattn::rows_of(q);
     a.lse = lse;
     a.in = weights;
     a.out = out;
@@ -220,20 +467,34 @@ int accumulate(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr,
     a.decay = decay;
     a.kv_heads = cache.kv_heads;
     a.group = divider(heads / cache.kv_heads);
-    const int64_t tiles = ceil_div(static_cast<int64_t>(cache.table_width) * cache.page_size, 4 * 4096 / cache.width) *
-                          cache.batch * cache.kv_heads;
-    const int64_t most = 2 * static_cast<int64_t>(device_cus());
-    const dim3 grid(static_cast<unsigned>(tiles < most ? (tiles < 1 ? 1 : tiles) : most));
-    prof_before(stream);
-    auto go = [&](auto t) {
-        typedef decltype(t) T;
-        if (cache.width == 64) hipLaunchKernelGGL((weights_kernel<T, 64>), grid, dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((weights_kernel<T, 128>), grid, dim3(kThreads), 0, stream, a);
+    a.part = static_cast<float *>(ws);
+    const bool narrow = all_narrow(cache, num_dst, heads);
+    a.few = narrow ? 0x7fffffff : static_cast<int32_t>(kFewRows);
+    const int64_t positions = static_cast<int64_t>(cache.table_width) * cache.page_size;
+    auto blocks_for = [&](int64_t keys, int64_t most) {
+        const int64_t tiles = ceil_div(positions, keys) * cache.batch * cache.kv_heads;
+        return dim3(static_cast<unsigned>(tiles < most ? (tiles < 1 ? 1 : tiles) : most));
     };
-    if (cache.dtype == TIGA_DT_F16) go(Half16{});
-    else go(Brain16{});
-    prof_after(stream);
-    return check_launch("cache weights");
+    const int blocks = static_cast<int>(wide_blocks());
+    auto go = [&](auto t, auto width) -> int {
+        typedef decltype(t) T;
+        constexpr int D = decltype(width)::value;
+        if (narrow) prof_before(stream);
+        hipLaunchKernelGGL((weights_kernel<T, D>), blocks_for(Step<T, D>::BN, 2 * device_cus()), dim3(kThreads), 0, stream, a);
+        if (narrow) prof_after(stream);
+        if (int rc = check_launch("cache weights")) return rc;
+        if (narrow) return TIGA_OK;
+        prof_before(stream);
+        hipLaunchKernelGGL((wide_weights_kernel<T, D>), dim3(blocks), dim3(kThreads), 0, stream, a, blocks);
+        prof_after(stream);
+        if (int rc = check_launch("cache weights of many rows")) return rc;
+        hipLaunchKernelGGL((add_weights_kernel<D>), blocks_for(kOwn, blocks), dim3(kOwn), 0, stream, a, blocks);
+        return check_launch("cache weights, sums");
+    };
+    auto by_width = [&](auto t) {
+        return cache.width == 64 ? go(t, std::integral_constant<int, 64>{}) : go(t, std::integral_constant<int, 128>{});
+    };
+    return cache.dtype == TIGA_DT_F16 ? by_width(Half16{}) : by_width(Brain16{});
 }
 
 }  // namespace retention

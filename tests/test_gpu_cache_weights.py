@@ -82,6 +82,10 @@ CASES = [
     ([(257, 1)] * 3, 12, 12, 128, 256, BF16),
     ([(1500, 900), (300, 300)], 2, 1, 128, 2, BF16),
     ([(700, 257), (128, 128), (64, 17)], 16, 2, 64, 32, F16),
+    # long chunks over few keys, whose rows are cut; beside next tokens
+    ([(2100, 2000), (900, 1), (70, 5), (1300, 1200)], 8, 1, 128, 16, BF16),
+    ([(3000, 2900)], 4, 1, 64, 64, F16),
+    ([(130 + i, 20 + i) for i in range(70)], 2, 1, 64, 16, BF16),
 ]
 
 
