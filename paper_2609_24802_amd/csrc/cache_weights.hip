@@ -9,8 +9,9 @@
 //
 // Many rows (chunks of prompts): bound by the exponentials (4 quarter-rate and 8 full-rate instructions for 256 pairs, where
 // their products take two thirds of that on the matrix cores at width 128).  A block owns 128 keys, 32 a wavefront as operands
-// in registers, and streams the rows through LDS.  Where there are few keys the rows are cut into parts, whose sums (512
-// bytes) go to the workspace and are added in order by a second launch.
+// in registers, and streams the rows through LDS.  The row tiles of all items (128 keys of a head) are laid end to end and
+// every block takes an equal run of them; the sums of an item's parts (512 bytes) go to the workspace and are added in order
+// by a second launch.
 #include <type_traits>
 
 #include "mfma16.hpp"
@@ -38,7 +39,8 @@ struct Args {
     int kv_heads;
     Divider group;
     int32_t few;       // rows of the sequences that the narrow kernel takes, at most; the others are the wide one's
-    float *part;       // [kMostParts][kOwn]
+    float *part;       // [2 * blocks][kOwn]: a block's first and last item may be parts
+    int4 *rec;         // [2 * blocks]: b + 1, head, tile, whether the item ends here
 };
 
 // Positions of a sequence: none past the table.
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(Args a) {
 // ------------------------------------------------------------------------------------------ many rows
 
 constexpr int kOwn = 128;          // keys of a block
-constexpr int kLeastSteps = 4;     // row tiles of a part, at least
+constexpr int kLeastSteps = 4;     // row tiles of a block's run, at least
 
 template <int D>
 struct Wide {
@@ -233,10 +235,10 @@ struct Wide {
 template <int D>
 __device__ __forceinline__ int swizzle(int k) { return (k / Wide<D>::R) % Wide<D>::CPR; }
 
-// A sequence with many rows: `tiles` of its positions, `steps` of its rows, cut into `parts`.
+// A sequence with many rows: `tiles` of its positions, `steps` of its rows.
 struct Load {
     int32_t tiles, steps;
-    __device__ __forceinline__ int32_t parts(int32_t most) const { return (steps + most - 1) / most; }
+    __device__ __forceinline__ int64_t work() const { return static_cast<int64_t>(tiles) * steps; }
 };
 template <int D>
 __device__ __forceinline__ Load load_of(const Args &a, int b) {
@@ -245,60 +247,59 @@ __device__ __forceinline__ Load load_of(const Args &a, int b) {
     if (rows <= a.few) return Load{0, 0};
     return Load{(positions(a.src, b) + kOwn - 1) / kOwn, (rows + Wide<D>::BN - 1) / Wide<D>::BN};
 }
-// How the sequences are cut: into parts of at most `most` steps, such that there are about `blocks` pieces of cut sequences.
-// Pieces are in the order (sequence, head, part, tile): neighbours read the same rows.  A cut sequence's pieces are counted
-// apart, which gives their places in the workspace: fewer than work / most + one for each cut item, so under 2 blocks.
+// A block's run of the steps of all items, in the order (sequence, head, tile).
 template <int D>
-struct Cut {
-    Load first;       // of the lane's of the first 64 sequences
-    int32_t most;
-    int64_t pieces;   // of a head
-    static __device__ __forceinline__ int64_t all(int64_t x) { return lane_value(wave_prefix(x), kWave - 1); }
-    template <class F>
-    __device__ __forceinline__ int64_t sum(const Args &a, F f) const {
-        int64_t n = all(f(first));
-        for (int e = kWave; e < a.src.batch; e += kWave) n += all(f(load_of<D>(a, e + lane_id())));
-        return n;
-    }
-    __device__ __forceinline__ Cut(const Args &a, int blocks) : first(load_of<D>(a, lane_id())) {
-        const int64_t work = sum(a, [](const Load &l) { return static_cast<int64_t>(l.tiles) * l.steps; }) * a.kv_heads;
-        most = static_cast<int32_t>(min(static_cast<int64_t>(0x7fffffff), max(static_cast<int64_t>(kLeastSteps), quotient(work + blocks - 1, blocks))));
-        pieces = sum(a, [&](const Load &l) { return static_cast<int64_t>(l.tiles) * l.parts(most); }) * a.kv_heads;
-    }
-    struct Piece {
-        int32_t b, head, part, parts, tile;
-        int64_t place;  // among the pieces of cut sequences
-        Load load;
-    };
-    // Piece id of all (or, CUT_ITEMS, item id of the cut sequences: part 0).
-    template <bool CUT_ITEMS>
-    __device__ __forceinline__ bool find(const Args &a, int64_t id, Piece &p) const {
-        int64_t base = 0, cut_base = 0;
+struct Run2 {
+    int64_t u, end, base;  // base: where sequence b starts
+    int32_t b;
+    Load load, mine;       // of sequence b, and of the lane's of the first 64
+    __device__ __forceinline__ void begin(const Args &a, int w, int blocks) {
+        mine = load_of<D>(a, lane_id());
+        auto work_of = [&](int e) { return (e == 0 ? mine : load_of<D>(a, e + lane_id())).work() * a.kv_heads; };
+        int64_t all = 0;
+        for (int e = 0; e < a.src.batch; e += kWave) all += lane_value(wave_prefix(work_of(e)), kWave - 1);
+        const int64_t per = max(static_cast<int64_t>(kLeastSteps), quotient(all + blocks - 1, blocks));
+        u = w * per;
+        end = min(all, u + per);
+        base = 0;
+        b = 0;
+        if (u >= end) return;
         for (int e = 0; e < a.src.batch; e += kWave) {
-            const Load l = e == 0 ? first : load_of<D>(a, e + lane_id());
-            const int32_t parts = l.parts(most);
-            const int64_t own = static_cast<int64_t>(l.tiles) * a.kv_heads, cut = parts > 1 ? own * parts : 0;
-            const int64_t mine = CUT_ITEMS ? (parts > 1 ? own : 0) : own * parts;
-            const int64_t incl = wave_prefix(mine), cut_incl = wave_prefix(cut);
-            const uint64_t past = __ballot(base + incl > id);
+            const int64_t here = work_of(e), incl = wave_prefix(here);
+            const uint64_t past = __ballot(base + incl > u);
             if (past) {
-                const int i = __builtin_ctzll(past);
-                p.b = e + i;
-                p.load = Load{__builtin_amdgcn_readlane(l.tiles, i), __builtin_amdgcn_readlane(l.steps, i)};
-                p.parts = p.load.parts(most);
-                int64_t rest = id - (base + lane_value(incl - mine, i));
-                const int64_t per = static_cast<int64_t>(p.load.tiles) * (CUT_ITEMS ? 1 : p.parts);
-                p.head = static_cast<int32_t>(quotient(rest, per));
-                rest -= p.head * per;
-                p.part = static_cast<int32_t>(quotient(rest, p.load.tiles));
-                p.tile = static_cast<int32_t>(rest - static_cast<int64_t>(p.part) * p.load.tiles);
-                p.place = cut_base + lane_value(cut_incl - cut, i) + (static_cast<int64_t>(p.head) * p.parts + p.part) * p.load.tiles + p.tile;
-                return true;
+                const int l = __builtin_ctzll(past);
+                b = e + l;
+                base += lane_value(incl - here, l);
+                break;
             }
             base += lane_value(incl, kWave - 1);
-            cut_base += lane_value(cut_incl, kWave - 1);
         }
-        return false;
+        fetch(a);
+    }
+    __device__ __forceinline__ void fetch(const Args &a) {
+        load = b < kWave ? Load{__builtin_amdgcn_readlane(mine.tiles, b), __builtin_amdgcn_readlane(mine.steps, b)} : load_of<D>(a, b);
+    }
+    struct Piece {
+        int32_t head, tile, t0, t1;  // steps [t0, t1) of the item
+        bool starts, ends;
+    };
+    __device__ __forceinline__ bool next(const Args &a, Piece &p) {
+        if (u >= end) return false;
+        while (u >= base + load.work() * a.kv_heads) {  // a later sequence holds u
+            base += load.work() * a.kv_heads;
+            ++b;
+            fetch(a);
+        }
+        const int64_t in = u - base, head = quotient(in, load.work()), rest = in - head * load.work();
+        p.head = static_cast<int32_t>(head);
+        p.tile = static_cast<int32_t>(quotient(rest, load.steps));
+        p.t0 = static_cast<int32_t>(rest - static_cast<int64_t>(p.tile) * load.steps);
+        p.t1 = static_cast<int32_t>(min(static_cast<int64_t>(load.steps), p.t0 + end - u));
+        p.starts = p.t0 == 0;
+        p.ends = p.t1 == load.steps;
+        u += p.t1 - p.t0;
+        return true;
     }
 };
 __device__ __forceinline__ int64_t cell_of(const Args &a, int32_t page, int head, int32_t at) {
@@ -313,7 +314,7 @@ __device__ __forceinline__ void put_weight(const Args &a, int b, int head, int64
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 4) void wide_weights_kernel(Args a, int blocks) {
+__global__ __launch_bounds__(kThreads, 3) void wide_weights_kernel(Args a, int blocks) {
     using G = Wide<D>;
     __shared__ __attribute__((aligned(1024))) uint8_t qa[G::TILE], qb[G::TILE];
     __shared__ __attribute__((aligned(256))) float sta[G::BN], stb[G::BN];
@@ -328,26 +329,46 @@ __global__ __launch_bounds__(kThreads, 4) void wide_weights_kernel(Args a, int b
         kch[r] = byte % G::RB / 16 ^ swizzle<D>(krow[r]);
     }
     const int dr = col * G::RB + 16 * (g ^ swizzle<D>(col));
-    const Cut<D> cut(a, blocks);
-    for (int64_t id = xcd_block(); id < cut.pieces; id += gridDim.x) {
-        typename Cut<D>::Piece pc;
-        if (!cut.template find<false>(a, id, pc)) break;
-        const Chunk chunk = chunk_of(a.src, pc.b);
-        const int32_t n = positions(a.src, pc.b), rows = chunk.count * d, k0 = pc.tile * kOwn;
+    const int block = static_cast<int>(xcd_block());
+    Run2<D> run;
+    run.begin(a, block, blocks);
+    if (threadIdx.x == 0) a.rec[2 * block] = a.rec[2 * block + 1] = int4{0, 0, 0, 0};
+    typename Run2<D>::Piece pc;
+    while (run.next(a, pc)) {
+        const Chunk chunk = chunk_of(a.src, run.b);
+        const int32_t n = positions(a.src, run.b), rows = chunk.count * d, k0 = pc.tile * kOwn;
         // the steps of the part that see a key of the tile
         const int64_t from = static_cast<int64_t>(k0) - chunk.pos0 > 0 ? (static_cast<int64_t>(k0) - chunk.pos0) * d / G::BN : 0;
-        const int32_t t0 = static_cast<int32_t>(max(from, static_cast<int64_t>(pc.load.steps) * pc.part / pc.parts));
-        const int32_t t1 = static_cast<int32_t>(static_cast<int64_t>(pc.load.steps) * (pc.part + 1) / pc.parts);
-        auto at = [&](int32_t r, int64_t head_stride, int64_t row_stride) {
+        const int32_t t0 = static_cast<int32_t>(max(from, static_cast<int64_t>(pc.t0))), t1 = pc.t1;
+        // head and row strides are below 2^31
+        auto at = [&](int32_t r, int32_t head_stride, int32_t row_stride) {
             const int32_t token = a.group.div(r);
-            return static_cast<int64_t>(pc.head * d + r - token * d) * head_stride + (chunk.first + token) * row_stride;
+            return static_cast<int64_t>(pc.head * d + r - token * d) * head_stride + static_cast<int64_t>(chunk.first + token) * row_stride;
         };
+        const int32_t head_stride = static_cast<int32_t>(a.q.head), row_stride = static_cast<int32_t>(a.q.row);
+        // Where tiles start at whole tokens a lane's places in a tile are the same in all of them but the last (as products of
+        // 64 bits in every step: 87 us for 1023 tokens over 9000 positions).
+        const bool regular = G::BN % d == 0;
+        int64_t place[G::LPW], lse_place = 0;
+        if (regular) {
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r) place[r] = at(krow[r], head_stride, row_stride) + 8 * kch[r];
+            lse_place = at(static_cast<int32_t>(threadIdx.x) % G::BN, a.src.num_dst, 1);
+        }
         float lse = 0.0f;  // of row threadIdx.x of the staged tile
         auto stage = [&](int kt, uint8_t *buf) {
             const int32_t r0 = kt * G::BN;
+            if (regular && r0 + G::BN <= rows) {
+                const int64_t token = kt * (G::BN / d);
+                const uint16_t *const base = a.q.p + token * row_stride;
+#pragma unroll
+                for (int r = 0; r < G::LPW; ++r) load_to_lds16(base + place[r], buf + (w * G::LPW + r) * 1024);
+                if (threadIdx.x < G::BN) lse = a.lse[lse_place + token];
+                return;
+            }
 #pragma unroll
             for (int r = 0; r < G::LPW; ++r)  // past the end: the last row again, without weight
-                load_to_lds16(a.q.p + at(min(r0 + krow[r], rows - 1), a.q.head, a.q.row) + 8 * kch[r], buf + (w * G::LPW + r) * 1024);
+                load_to_lds16(a.q.p + at(min(r0 + krow[r], rows - 1), head_stride, row_stride) + 8 * kch[r], buf + (w * G::LPW + r) * 1024);
             const int32_t r = r0 + static_cast<int32_t>(threadIdx.x);
             if (threadIdx.x < G::BN) lse = r < rows ? a.lse[at(r, a.src.num_dst, 1)] : -__builtin_inff();
         };
@@ -358,7 +379,7 @@ __global__ __launch_bounds__(kThreads, 4) void wide_weights_kernel(Args a, int b
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             key[x] = k0 + w * 32 + x * 16 + col;
-            const int32_t pos = min(key[x], n - 1), entry = entry_at(a.src, pc.b, pos);
+            const int32_t pos = min(key[x], n - 1), entry = entry_at(a.src, run.b, pos);
             const int32_t page = is_page(a.src, entry) ? entry : 0;  // a key of some page, whose weight is not stored
             const uint16_t *const p = a.src.k.p + page * a.src.k.batch + pc.head * a.src.k.head +
                                       static_cast<int64_t>(pos & ((1 << a.src.shift) - 1)) * a.src.k.row;
@@ -416,27 +437,27 @@ __global__ __launch_bounds__(kThreads, 4) void wide_weights_kernel(Args a, int b
         for (int x = 0; x < 2; ++x) {
             const float all = column_sum((sum[x][0] + sum[x][1]) + (sum[x][2] + sum[x][3]));
             if (g != 0 || key[x] >= n) continue;
-            if (pc.parts > 1) a.part[pc.place * kOwn + key[x] - k0] = all;
-            else put_weight(a, pc.b, pc.head, chunk.pos0, key[x], all);
+            if (pc.starts && pc.ends) put_weight(a, run.b, pc.head, chunk.pos0, key[x], all);
+            else a.part[(2 * block + (pc.starts ? 1 : 0)) * kOwn + key[x] - k0] = all;
         }
+        if (!(pc.starts && pc.ends) && threadIdx.x == 0) a.rec[2 * block + (pc.starts ? 1 : 0)] = int4{run.b + 1, pc.head, pc.tile, pc.ends ? 1 : 0};
     }
 }
 
-// The parts of the cut sequences' sums, in order: a key a thread, an item a block.
-template <int D>
+// The sums of the item that starts in block x and ends in a later one (slot 1 of x, then slot 0 of the blocks after it up to
+// the one that holds the end), in order: a key a thread.
 __global__ __launch_bounds__(kOwn) void add_weights_kernel(Args a, int blocks) {
-    const Cut<D> cut(a, blocks);
-    for (int64_t id = blockIdx.x;; id += gridDim.x) {
-        typename Cut<D>::Piece pc;
-        if (!cut.template find<true>(a, id, pc)) return;
-        const int32_t key = pc.tile * kOwn + static_cast<int32_t>(threadIdx.x);
-        if (key >= positions(a.src, pc.b)) continue;
-        float sum = 0.0f;
-        const float *p = a.part + pc.place * kOwn + threadIdx.x;
-#pragma unroll 8
-        for (int e = 0; e < pc.parts; ++e) sum += p[static_cast<int64_t>(e) * pc.load.tiles * kOwn];
-        put_weight(a, pc.b, pc.head, chunk_of(a.src, pc.b).pos0, key, sum);
+    const int x = static_cast<int>(blockIdx.x);
+    const int4 it = a.rec[2 * x + 1];
+    if (it.x == 0) return;
+    const int b = it.x - 1;
+    float sum = a.part[(2 * x + 1) * kOwn + threadIdx.x];
+    for (int y = x + 1; y < blocks; ++y) {
+        sum += a.part[2 * y * kOwn + threadIdx.x];
+        if (a.rec[2 * y].w != 0) break;
     }
+    const int32_t key = it.z * kOwn + static_cast<int32_t>(threadIdx.x);
+    if (key < positions(a.src, b)) put_weight(a, b, it.y, chunk_of(a.src, b).pos0, key, sum);
 }
 
 // Narrow for all sequences where they have at most 16 rows on average; otherwise for those that have, and the wide kernel for
@@ -446,13 +467,13 @@ bool all_narrow(const tiga_cache &c, int64_t num_dst, int32_t heads) {
     const int64_t some = num_dst < c.batch ? num_dst : c.batch;
     return num_dst * (heads / c.kv_heads) <= kFewRows * some;
 }
-int64_t wide_blocks() { return 4 * static_cast<int64_t>(device_cus()); }
+int64_t wide_blocks() { return 3 * static_cast<int64_t>(device_cus()); }
 
 }  // namespace
 
 size_t weights_ws_bytes(const tiga_cache &, int64_t num_dst, int32_t heads) {
     // of any number of source heads and sequences
-    return num_dst * heads <= kFewRows ? 256 : 2 * wide_blocks() * kOwn * sizeof(float);
+    return num_dst * heads <= kFewRows ? 256 : 2 * wide_blocks() * (kOwn * sizeof(float) + sizeof(int4));
 }
 
 int accumulate(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr, int32_t heads, const tiga_view &q,
@@ -468,6 +489,7 @@ int accumulate(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr,
     a.kv_heads = cache.kv_heads;
     a.group = divider(heads / cache.kv_heads);
     a.part = static_cast<float *>(ws);
+    a.rec = reinterpret_cast<int4 *>(a.part + 2 * wide_blocks() * kOwn);
     const bool narrow = all_narrow(cache, num_dst, heads);
     a.few = narrow ? 0x7fffffff : static_cast<int32_t>(kFewRows);
     const int64_t positions = static_cast<int64_t>(cache.table_width) * cache.page_size;
@@ -488,7 +510,7 @@ int accumulate(const tiga_cache &cache, int64_t num_dst, const int32_t *dst_ptr,
         hipLaunchKernelGGL((wide_weights_kernel<T, D>), dim3(blocks), dim3(kThreads), 0, stream, a, blocks);
         prof_after(stream);
         if (int rc = check_launch("cache weights of many rows")) return rc;
-        hipLaunchKernelGGL((add_weights_kernel<D>), blocks_for(kOwn, blocks), dim3(kOwn), 0, stream, a, blocks);
+        hipLaunchKernelGGL(add_weights_kernel, dim3(blocks), dim3(kOwn), 0, stream, a, blocks);
         return check_launch("cache weights, sums");
     };
     auto by_width = [&](auto t) {
