@@ -7,8 +7,9 @@
 // the matrix operand's layout, with the queries as the other operand: a result's column is a key, and the sum over the rows
 // is one over four registers and four lanes.
 //
-// Many rows (chunks of prompts): bound by the exponentials (4 quarter-rate and 8 full-rate instructions for 256 pairs, where
-// their products take two thirds of that on the matrix cores at width 128).  A block owns 128 keys, 32 a wavefront as operands
+// Many rows (chunks of prompts): bound by the vector unit, 4 quarter-rate and 8 full-rate instructions for 256 pairs (96 cycles),
+// and the matrix cores, whose products take 64 at width 128 and hardly overlap with them: 256 keys a block, and the weights
+// of 16 rows formed under the products of the next, took the same 74 us as 128 keys and three blocks a compute unit, 72.  A block owns 128 keys, 32 a wavefront as operands
 // in registers, and streams the rows through LDS.  The row tiles of all items (128 keys of a head) are laid end to end and
 // every block takes an equal run of them; the sums of an item's parts (512 bytes) go to the workspace and are added in order
 // by a second launch.
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(kThreads, 3) void wide_weights_kernel(Args a, int b
         auto step = [&](int kt, const uint8_t *buf, const float *st) {
             const int32_t r0 = kt * G::BN;
             const bool edge = a.group.div(r0) < last;
-#pragma unroll 2
+#pragma unroll
             for (int rb = 0; rb < G::BN / 16; ++rb) {
                 f4 s[2];
 #pragma unroll
