@@ -71,6 +71,12 @@ CASES = [
     ([90, 33], 1, 128, 2, BF16, 32, 5, "few"),
     ([33_000, 100], 1, 64, 64, F16, 1000, 10, "few"),
     ([70_001], 1, 64, 16, BF16, 65_000, 1, "wild"),
+    ([50_000, 8192, 8193, 400, 0], 2, 64, 32, F16, 8000, 4000, "spread"),
+    ([40_000, 33_000], 1, 64, 64, BF16, 500, 500, "near"),
+    ([60_000], 3, 64, 16, F16, 20_000, 100, "near"),
+    ([40_000, 9_000], 1, 64, 128, F16, 12_000, 7, "equal"),
+    ([35_000], 1, 64, 1, F16, 30_000, 9, "wild"),
+    ([34_000 - 100 * (i % 300) for i in range(300)], 1, 64, 64, F16, 900, 10, "few"),   # more lists than compute units
     ([20 + 5 * (i % 30) for i in range(70)], 3, 64, 16, F16, 90, 9, "spread"),
 ]
 
