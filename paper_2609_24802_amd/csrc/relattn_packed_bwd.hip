@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(const int32_t *pt
     const int32_t tiles = static_cast<int32_t>((static_cast<int64_t>(mine.count) * p.mult + kOwn - 1) / kOwn);
     auto all = [&](int64_t x) { return lane_value(wave_prefix(x), kWave - 1); };
     int32_t cut = kNoCut;
-    if (p.least < kNoCut) {
+    if (p.least < kNoCut && __any(tiles > p.least)) {
         // Parts of half a block's share of all levels, or of as much more as makes at most two pieces a block, up to the whole
         // share, which makes at most twice as many parts as blocks run at once.  (dk and dv of 10,000 tokens, 4 heads over one
         // of 128: 272 us, 387 with whole shares; 1.3 ms uncut.)
@@ -319,6 +319,23 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
     // sources: where the tile's keys are few, delta is formed as sum_j p_ij <dy_i, v_j> in fp32, by the tiles' products.
     const bool few = keys <= kOwn;
 
+    const Places<D> at(lane, w);
+    const uint16_t *const kb = a.k.p + it.kv * a.k.head + it.run.first * a.k.row;
+    const uint16_t *const vb = a.v.p + it.kv * a.v.head + it.run.first * a.v.row;
+    auto stage = [&](int kt, uint8_t *b1, uint8_t *b2) {
+        const int32_t k0 = kt * G::BN;
+        const uint8_t *const kt0 = reinterpret_cast<const uint8_t *>(kb + k0 * a.k.row);
+        const uint8_t *const vt0 = reinterpret_cast<const uint8_t *>(vb + k0 * a.v.row);
+#pragma unroll
+        for (int r = 0; r < G::LPW; ++r) {
+            const int run = (w * G::LPW + r) * 1024;
+            const uint32_t i = min(at.krow[r], keys - 1 - k0);  // past the end: the last key again, without weight
+            load_to_lds16(kt0 + (2u * i * static_cast<uint32_t>(a.k.row) + 16u * at.kch[r]), b1 + run);
+            load_to_lds16(vt0 + (2u * i * static_cast<uint32_t>(a.v.row) + 16u * at.kch[r]), b2 + run);
+        }
+    };
+    if (few || a.dq.p) stage(first_step, y1a, y2a);  // under way while the owned operands arrive
+
     // owned operands; columns past the end repeat the last (what they sum is not stored)
     u4 x1[2][G::CH], x2[2][G::CH];
     f2 peak{0.0f, 0.0f};
@@ -369,21 +386,6 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
 #pragma unroll
     for (int db = 0; db < G::DB; ++db) acc.a1[db][0] = acc.a1[db][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const Places<D> at(lane, w);
-    const uint16_t *const kb = a.k.p + it.kv * a.k.head + it.run.first * a.k.row;
-    const uint16_t *const vb = a.v.p + it.kv * a.v.head + it.run.first * a.v.row;
-    auto stage = [&](int kt, uint8_t *b1, uint8_t *b2) {
-        const int32_t k0 = kt * G::BN;
-        const uint8_t *const kt0 = reinterpret_cast<const uint8_t *>(kb + k0 * a.k.row);
-        const uint8_t *const vt0 = reinterpret_cast<const uint8_t *>(vb + k0 * a.v.row);
-#pragma unroll
-        for (int r = 0; r < G::LPW; ++r) {
-            const int run = (w * G::LPW + r) * 1024;
-            const uint32_t i = min(at.krow[r], keys - 1 - k0);  // past the end: the last key again, without weight
-            load_to_lds16(kt0 + (2u * i * static_cast<uint32_t>(a.k.row) + 16u * at.kch[r]), b1 + run);
-            load_to_lds16(vt0 + (2u * i * static_cast<uint32_t>(a.v.row) + 16u * at.kch[r]), b2 + run);
-        }
-    };
     const float c = a.scale * kLog2e;
     const int32_t least = a.group.div(own0) + 1;                                                  // the tile's first row sees
     const int32_t my_most = own0 + w * 32 < rows ? a.group.div(min(own0 + w * 32 + 31, rows - 1)) + 1 : 0;
@@ -449,7 +451,6 @@ __global__ __launch_bounds__(kThreads, 2) void packed_query_kernel(Args a) {
                 for (int i = 0; i < 8; ++i) own_delta[qb] += f.s[i / 4][qb][i % 4] * f.dp[i / 4][qb][i % 4];
         }
     };
-    stage(first_step, y1a, y2a);
     if (few) {  // at most two tiles, both in LDS (and never cut)
         if (steps > 1) stage(1, y1b, y2b);
         loads_arrived();
@@ -561,6 +562,49 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
     const int32_t end = (rows + G::BN - 1) / G::BN, all_steps = end - own0 / G::BN * d;
     const int32_t first_step = part_start(all_steps, it.part, it.parts), steps = part_start(all_steps, it.part + 1, it.parts);
 
+    const Places<D> at(lane, w);
+    // Where tiles start at whole tokens a lane's places in a tile are the same in all of them but the sequence's last (dk and dv
+    // of 16,384 ragged tokens, 16 heads over 4 of 128: 1733 us without, 1677 with; at width 64 the registers are not there).
+    const int64_t reach = static_cast<int64_t>(d - 1) * max(a.q.head, a.dy.head) + static_cast<int64_t>(G::BN / d) * max(a.q.row, a.dy.row);
+    const bool regular = D == 128 && G::BN % d == 0 && reach < (int64_t(1) << 30);
+    uint32_t q_place[G::LPW], dy_place[G::LPW];  // bytes
+#pragma unroll
+    for (int r = 0; r < G::LPW; ++r) {
+        const uint32_t token = a.group.div(at.krow[r]), head = at.krow[r] - token * d;
+        q_place[r] = 2u * (head * static_cast<uint32_t>(a.q.head) + token * static_cast<uint32_t>(a.q.row) + 8u * at.kch[r]);
+        dy_place[r] = 2u * (head * static_cast<uint32_t>(a.dy.head) + token * static_cast<uint32_t>(a.dy.row) + 8u * at.kch[r]);
+    }
+    auto stage = [&](int n, uint8_t *b1, uint8_t *b2, float *stats) {
+        const int32_t k0 = (end - 1 - n) * G::BN;
+        if (regular && n > 0) {
+            const int64_t token = it.run.first + (end - 1 - n) * (G::BN / d), head = static_cast<int64_t>(it.kv) * d;
+            const uint8_t *const q0 = reinterpret_cast<const uint8_t *>(a.q.p + head * a.q.head + token * a.q.row);
+            const uint8_t *const dy0 = reinterpret_cast<const uint8_t *>(a.dy.p + head * a.dy.head + token * a.dy.row);
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r) {
+                load_to_lds16(q0 + q_place[r], b1 + (w * G::LPW + r) * 1024);
+                load_to_lds16(dy0 + dy_place[r], b2 + (w * G::LPW + r) * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < G::LPW; ++r) {
+                const int run = (w * G::LPW + r) * 1024;
+                const int32_t i = min(k0 + at.krow[r], rows - 1);  // past the end: the last row again, without weight
+                load_to_lds16(a.q.p + row_at(a, a.q, it.run.first, it.kv, i) + 8 * at.kch[r], b1 + run);
+                load_to_lds16(a.dy.p + row_at(a, a.dy, it.run.first, it.kv, i) + 8 * at.kch[r], b2 + run);
+            }
+        }
+        // 64 lanes, 4 bytes each: the first half of the needed wavefronts takes lse2, the other delta
+        constexpr int kNeed = 2 * G::BN / kWave;
+        if (w < kNeed) {
+            const int32_t i = k0 + w % (kNeed / 2) * kWave + lane;
+            const int64_t s = i < rows ? stat_at(a, it.run.first, it.kv, i) : a.stats;
+            __builtin_amdgcn_global_load_lds((w < kNeed / 2 ? a.lse2 : a.delta) + s,
+                                             (__attribute__((address_space(3))) void *)(stats + w * kWave), 4, 0, 0);
+        }
+    };
+    stage(first_step, y1a, y2a, sta);  // under way while the owned operands arrive
+
     // owned operands; columns past the end repeat the last (what they sum is not stored)
     u4 x1[2][G::CH], x2[2][G::CH];
     f2 peak{0.0f, 0.0f};
@@ -585,25 +629,6 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) acc.a1[db][qb] = acc.a2[db][qb] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const Places<D> at(lane, w);
-    auto stage = [&](int n, uint8_t *b1, uint8_t *b2, float *stats) {
-        const int32_t k0 = (end - 1 - n) * G::BN;
-#pragma unroll
-        for (int r = 0; r < G::LPW; ++r) {
-            const int run = (w * G::LPW + r) * 1024;
-            const int32_t i = min(k0 + at.krow[r], rows - 1);  // past the end: the last row again, without weight
-            load_to_lds16(a.q.p + row_at(a, a.q, it.run.first, it.kv, i) + 8 * at.kch[r], b1 + run);
-            load_to_lds16(a.dy.p + row_at(a, a.dy, it.run.first, it.kv, i) + 8 * at.kch[r], b2 + run);
-        }
-        // 64 lanes, 4 bytes each: the first half of the needed wavefronts takes lse2, the other delta
-        constexpr int kNeed = 2 * G::BN / kWave;
-        if (w < kNeed) {
-            const int32_t i = k0 + w % (kNeed / 2) * kWave + lane;
-            const int64_t s = i < rows ? stat_at(a, it.run.first, it.kv, i) : a.stats;
-            __builtin_amdgcn_global_load_lds((w < kNeed / 2 ? a.lse2 : a.delta) + s,
-                                             (__attribute__((address_space(3))) void *)(stats + w * kWave), 4, 0, 0);
-        }
-    };
     const float c = a.scale * kLog2e;
     // tiles whose first row does not see the last owned key
     auto cut = [&](int n) { return static_cast<int64_t>(end - 1 - n) * G::BN < static_cast<int64_t>(own0 + kOwn - 1) * d; };
@@ -662,7 +687,6 @@ __global__ __launch_bounds__(kThreads, (kBlocks<D, true>)) void packed_keys_kern
                                   stats + G::BN + kc * 32, g, exists);
         }
     };
-    stage(first_step, y1a, y2a, sta);
     int n = first_step;
     // tiles whose rows all see every owned key, in pairs
     const int64_t from = (static_cast<int64_t>(own0 + kOwn - 1) * d + G::BN - 1) / G::BN;
