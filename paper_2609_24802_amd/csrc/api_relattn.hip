@@ -85,6 +85,15 @@ int check_sequences(const char *what, const tiga_packed *rel) {
     return TIGA_OK;
 }
 
+// Source heads that nothing reads get gradients of 0, as rows of no sequence do.
+tiga_packed with_readers(tiga_packed rel) {
+    if (rel.heads == 0) {
+        rel.heads = rel.kv_heads;
+        rel.batch = 0;
+    }
+    return rel;
+}
+
 int check_cache(const char *what, const tiga_cache *c) {
     if (!c) return fail(TIGA_EINVAL, "%s: the cache is required", what);
     if (c->num_pages < 0 || c->batch < 0 || c->table_width < 0) return fail(TIGA_EINVAL, "%s: negative size", what);
@@ -307,7 +316,7 @@ int tiga_mp_attention_packed_fwd(const tiga_packed *rel, const tiga_view *q, con
 
 size_t tiga_mp_attention_packed_bwd_workspace(const tiga_packed *rel) {
     clear_error();  // no EntryScope: armed kernel events are for the call that follows
-    return check_sequences("packed attention backward", rel) ? 0 : relattn::packed_bwd_ws_bytes(*rel);
+    return check_sequences("packed attention backward", rel) ? 0 : relattn::packed_bwd_ws_bytes(with_readers(*rel));
 }
 
 int tiga_mp_attention_packed_bwd(const tiga_packed *given, const tiga_view *q, const tiga_view *k, const tiga_view *v,
@@ -318,13 +327,9 @@ int tiga_mp_attention_packed_bwd(const tiga_packed *given, const tiga_view *q, c
     const char *what = "packed attention backward";
     if (int rc = check_sequences(what, given)) return rc;
     if (int rc = check_scale(what, scale)) return rc;
-    tiga_packed some = *given;
-    const bool unread = some.heads == 0;  // source heads that nothing reads: gradients of 0, as of rows of no sequence
-    if (unread) {
-        some.heads = some.kv_heads;
-        some.batch = 0;
-    }
+    const tiga_packed some = with_readers(*given);
     const tiga_packed *const rel = &some;
+    const bool unread = given->heads == 0;
     if (rel->heads == 0 || rel->num_rows == 0) return TIGA_OK;
     const tiga_view none{};
     if (!unread) {

@@ -815,6 +815,7 @@ Plan plan_for(const tiga_packed &rel, bool keys) {
     p.least = some ? static_cast<int32_t>(least) : kNoCut;
     p.cut = some ? 2 * static_cast<int64_t>(p.resident) : 0;
     p.places = most_items(rel, keys ? 1 : group) / rel.kv_heads + ceil_div(p.cut, rel.kv_heads);
+    if (p.places < 1) p.places = 1;  // no sequences: all rows are cleared
     return p;
 }
 

@@ -244,3 +244,60 @@ def test_pointers_that_run_backwards_stay_inside(lib):
 @pytest.mark.parametrize("lead", [1, 700])
 def test_many_sequences_behind_rows_of_none(lib, lead):
     check(lib, Packed([1 + (i * 29) % 40 for i in range(130)], 2, 1, 64, BF16, seed=16, lead=lead, tail=3), "many")
+
+
+@pytest.mark.parametrize("Hk", [1, 3])
+def test_no_heads(lib, Hk):
+    """Source heads without query heads get gradients of 0; no rows and no sequences give empty results and zeros."""
+    s = Packed([40, 60], Hk, Hk, 64, F16, seed=17)
+    none = s.q[:0]
+    y, lse = lib.tiga_mp_attention_packed_fwd(none, s.k, s.v, s.ptr_t, want_lse=True)
+    g = lib.tiga_mp_attention_packed_bwd(none, s.k, s.v, y, lse, s.dy[:0], s.ptr_t)
+    torch.cuda.synchronize()
+    assert y.shape == (0, 100, 64) and g["dq"].shape == (0, 100, 64)
+    assert (g["dk"] == 0).all() and (g["dv"] == 0).all()
+    empty = [t[:, :0] for t in (s.q, s.k, s.v)]
+    y, lse = lib.tiga_mp_attention_packed_fwd(*empty, s.ptr_t[:1] * 0, want_lse=True)
+    g = lib.tiga_mp_attention_packed_bwd(*empty, y, lse, empty[0], s.ptr_t[:1] * 0)
+    torch.cuda.synchronize()
+    assert y.shape == (Hk, 0, 64) and g["dk"].shape == (Hk, 0, 64)
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t[:1], want_lse=True)      # a batch of none
+    g = lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t[:1])
+    torch.cuda.synchronize()
+    assert (y == 0).all() and torch.isneginf(lse).all() and all((t == 0).all() for t in g.values())
+
+
+def test_two_graphs_share_a_workspace(lib):
+    """Replayed in turn on one stream."""
+    one, two = Packed([300, 900], 4, 2, 64, F16, seed=18), Packed([1200], 4, 2, 64, F16, seed=19)
+    ref = lib.C.byref
+    size = max(lib.load().tiga_mp_attention_packed_fwd_workspace(ref(lib._packed(s.q, s.k, s.v, s.ptr_t, "hnd")[0])) for s in (one, two))
+    size = max(size, *(lib.load().tiga_mp_attention_packed_bwd_workspace(ref(lib._packed(s.q, s.k, s.v, s.ptr_t, "hnd")[0])) for s in (one, two)))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def call(s, ws=None):
+        y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True, ws=ws)
+        return y, lse, lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t, ws=ws)
+
+    want = [call(s) for s in (one, two)]
+    torch.cuda.synchronize()
+    graphs, got = [], []
+    for s in (one, two):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got.append(call(s, ws))
+        graphs.append(graph)
+    for i in (0, 1, 1, 0, 1):
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got[i][:2], want[i][:2]):
+            assert torch.equal(a, b)
+        assert all(torch.equal(got[i][2][n], want[i][2][n]) for n in want[i][2])
+
+
+def test_given_workspaces_are_checked(lib):
+    s = Packed([30], 2, 1, 64, F16, seed=20)
+    for bad, err in ((torch.empty(16, dtype=torch.uint8, device="cuda"), lib.TigaError), (torch.empty(1 << 20), TypeError),
+                     (torch.empty(1 << 20, 2, dtype=torch.uint8, device="cuda")[:, 0], ValueError)):
+        with pytest.raises(err):
+            lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, ws=bad)

@@ -72,6 +72,9 @@ def test_arguments(b):  # noqa: F811
     for over in (dict(num_rows=0), dict(heads=0, kv_heads=0)):
         assert fwd(b, q=None, k=None, v=None, y=None, ws=0, n=0, **over) == 0
         assert bwd(b, over=over, q=None, k=None, v=None, y=None, dy=None, dq=None, dk=None, dv=None, lse=0, ws=0, n=0) == 0
+    for which in ("fwd", "bwd"):  # source heads that nothing reads
+        for over in (dict(heads=0), dict(heads=0, kv_heads=0), dict(num_rows=0), dict(batch=0), dict(batch=0, ptr=None)):
+            assert getattr(b.load(), f"tiga_mp_attention_packed_{which}_workspace")(C.byref(b._Packed(**{**PACKED, **over}))) > 0
     # more tiles than one grid of threads counts
     many = dict(num_rows=(1 << 31) - 2048, heads=1, kv_heads=1, batch=(1 << 20) - 1)
     assert bwd(b, over=many) == b.TIGA_EUNSUPPORTED and b"tiles" in b.load().tiga_last_error()
