@@ -110,40 +110,42 @@ __device__ __forceinline__ Run run_of(const Packed &p, int b) { return run_betwe
 // [group_ptr[g], group_ptr[g + 1]), which share group_len[g] positions.  Of those, whole pages and whole multiples of 128 are
 // read once, from the first sequence's pages, so that what lies behind them starts at a tile and a page; a group of one
 // sequence shares nothing.
-struct Shared : Pages {  // batch: the groups
-    const int32_t *group_ptr, *group_len;
+struct Groups {
+    const int32_t *ptr, *len;
+    int32_t count;
     int32_t sequences;   // of the cache
     int32_t whole;       // log2 of what is shared whole
-    int32_t *skip;       // [sequences]: shared positions of each
+};
+struct Shared : Pages {  // batch: the groups
+    Groups groups;
     float *state, *lse2; // [heads, num_dst, width], [heads, num_dst]: what the rows have of the shared positions
 };
 struct Behind : Pages {
-    const int32_t *skip;
-    const float *state, *lse2;
+    Groups groups;
+    float *state, *lse2; // of the positions behind
+    float *shared_lse2;
 };
 struct Group {
     int32_t first, end;  // sequences
     int32_t shared;      // positions
 };
-__device__ __forceinline__ Group group_of(const Shared &c, int g) {
-    const Run run = run_between(c.group_ptr, g, g + 1, c.sequences);
+__device__ __forceinline__ Group group_of(const Pages &c, const Groups &groups, int g) {
+    const Run run = run_between(groups.ptr, g, g + 1, groups.sequences);
     const int64_t most = static_cast<int64_t>(c.table_width) << c.shift;
-    int64_t n = c.group_len[g];
+    int64_t n = groups.len[g];
     n = n < 0 || run.count < 2 ? 0 : (n > most ? most : n);
-    return Group{run.first, run.first + run.count, static_cast<int32_t>(n >> c.whole << c.whole)};
+    return Group{run.first, run.first + run.count, static_cast<int32_t>(n >> groups.whole << groups.whole)};
 }
-// Shared positions of every sequence, for the pass over what lies behind them.
-__device__ __forceinline__ void leave_skips(const Shared &c) {
-    for (int b = blockIdx.x * blockDim.x + threadIdx.x; b < c.sequences; b += gridDim.x * blockDim.x) {
-        int lo = 0, hi = c.batch - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (c.group_ptr[mid] <= b) lo = mid;
-            else hi = mid - 1;
-        }
-        const Group g = group_of(c, lo);
-        c.skip[b] = g.first <= b && b < g.end ? g.shared : 0;
+// The shared positions of sequence b.  (By the lanes of a wavefront for up to 64 groups, the kernels spill.)
+__device__ __forceinline__ int32_t skip_of(const Behind &c, int b) {
+    int lo = 0, hi = c.groups.count - 1;  // the last group that starts at or before b
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (c.groups.ptr[mid] <= b) lo = mid;
+        else hi = mid - 1;
     }
+    const Group g = group_of(c, c.groups, lo);
+    return g.first <= b && b < g.end ? g.shared : 0;
 }
 
 // The table's entry for position pos (>= 0) of sequence b, -1 where the table does not reach.  Only an entry that

@@ -58,10 +58,12 @@ struct Strided {
 };
 // What a call's rows read: a padded batch of other sequences, a cache's pages up to the row's position, their own
 // sequence's rows of packed sequences up to themselves; and for sequences of which groups share their first positions, those
-// (the rows of all of a group's sequences are one item's) and the pages behind them, from the state that those left.
+// (the rows of all of a group's sequences are one item's) and the pages behind them, whose results are joined afterwards.
 enum Relation { kStrided, kPaged, kPacked, kShared, kBehind };
 template <Relation REL>
 constexpr bool kPages = REL == kPaged || REL == kShared || REL == kBehind;
+template <Relation REL>
+constexpr bool kHalf = REL == kShared || REL == kBehind;  // results are fp32 states
 template <Relation REL>
 constexpr bool kCausal = REL == kPaged || REL == kPacked || REL == kBehind;
 template <Relation REL>
@@ -128,12 +130,12 @@ __device__ __forceinline__ Seq seq_of(const Args<REL> &a, int b) {
         const Run run = run_of(a.src, b);
         return Seq{run.first, run.count * static_cast<int32_t>(a.group.d), 1};
     } else if constexpr (REL == kShared) {
-        const Group g = group_of(a.src, b);
+        const Group g = group_of(a.src, a.src.groups, b);
         const Run run = run_between(a.src.dst_ptr, g.first, g.end, a.src.num_dst);
         return Seq{run.first, g.shared > 0 ? run.count * static_cast<int32_t>(a.group.d) : 0, g.shared};
     } else if constexpr (REL == kBehind) {
         const Chunk ch = chunk_of(a.src, b);
-        return Seq{ch.first, ch.count * static_cast<int32_t>(a.group.d), ch.pos0 + 1 - a.src.skip[b]};
+        return Seq{ch.first, ch.count * static_cast<int32_t>(a.group.d), ch.pos0 + 1 - skip_of(a.src, b)};
     } else {
         int32_t n = a.src.num_src;
         if (a.src.len) n = a.src.len[b] < 0 ? 0 : (a.src.len[b] > n ? n : a.src.len[b]);
@@ -468,8 +470,8 @@ struct Cells {
     int32_t row;   // of the table
     int32_t skip;  // positions of the sequence before position 0 of the item
     __device__ __forceinline__ Cells(const Args<REL> &a, int b) : row(b), skip(0) {
-        if constexpr (REL == kShared) row = group_of(a.src, b).first;
-        if constexpr (REL == kBehind) skip = a.src.skip[b];
+        if constexpr (REL == kShared) row = group_of(a.src, a.src.groups, b).first;
+        if constexpr (REL == kBehind) skip = skip_of(a.src, b);
     }
     __device__ __forceinline__ int32_t entry(const Args<REL> &a, int32_t pos) const {
         if constexpr (REL == kBehind) return entry_at(a.src, row, static_cast<int64_t>(pos) + skip);
@@ -489,11 +491,11 @@ __device__ __forceinline__ int64_t lse_at(const Args<REL> &a, int b, const Seq &
     return b * a.lse_batch + (head * d + g) * a.lse_head + s.first + token;
 }
 
-// Where row r's results go, 4 widths at a time: y in the input type, or the fp32 state of shared positions; and lse, there in the
-// log2 domain.
+// Where row r's results go, 4 widths at a time: y in the input type, or an fp32 state (normalized) to be joined; and lse, there
+// in the log2 domain.
 template <int D, Relation REL>
 __device__ __forceinline__ auto out_row(const Args<REL> &a, int b, const Seq &s, int head, int r) {
-    if constexpr (REL == kShared) return a.src.state + lse_at(a, b, s, head, r) * D;
+    if constexpr (kHalf<REL>) return a.src.state + lse_at(a, b, s, head, r) * D;
     else return const_cast<uint16_t *>(a.y.p) + row_at(a, a.y, b, s, head, r);
 }
 template <class T>
@@ -502,26 +504,17 @@ template <class T>
 __device__ __forceinline__ void put(float *p, f4 v) { *reinterpret_cast<f4 *>(p) = v; }
 template <Relation REL>
 __device__ __forceinline__ void put_lse(const Args<REL> &a, int b, const Seq &s, int head, int r, float lse2) {
-    if constexpr (REL == kShared) a.src.lse2[lse_at(a, b, s, head, r)] = lse2;
+    if constexpr (kHalf<REL>) a.src.lse2[lse_at(a, b, s, head, r)] = lse2;
     else if (a.lse) a.lse[lse_at(a, b, s, head, r)] = lse2 * kLn2;
 }
 
-// The state that row r's item starts from, behind shared positions: their results, as a mass of 1 at their lse.  NaN where
-// the sequence's first new token is among the shared positions, of which it would see too many.
-template <int D>
-struct Before {
-    const float *o;
-    float m, l;  // l = 0: nothing before
-    __device__ __forceinline__ Before(const Args<kBehind> &a, const Cells<kBehind> &cells, int b, const Seq &s, int head, int r) {
-        const int64_t at = lse_at(a, b, s, head, r);
-        o = a.src.state + at * D;
-        m = -__builtin_inff();
-        l = 0.0f;
-        if (cells.skip == 0) return;
-        m = s.keys0 > 0 ? a.src.lse2[at] : __builtin_nanf("");
-        l = m == -__builtin_inff() ? 0.0f : (m != m ? m : 1.0f);
-    }
-};
+// Row r of an item behind shared positions, once: its share of mass to start with, NaN where the sequence's first new token is
+// among the shared positions, of which it would see too many.  A row that shares nothing says so in the place of the state
+// that it does not have.
+__device__ __forceinline__ float open_row(const Args<kBehind> &a, const Cells<kBehind> &cells, int b, const Seq &s, int head, int r) {
+    if (cells.skip == 0) a.src.shared_lse2[lse_at(a, b, s, head, r)] = -__builtin_inff();
+    return cells.skip > 0 && s.keys0 <= 0 ? __builtin_nanf("") : 0.0f;
+}
 
 // Rows of no sequence of a packed call: before ptr[0] and behind ptr[batch].  They see nothing: y = 0, lse = -inf.
 template <int D, Relation REL>
@@ -699,11 +692,12 @@ __device__ __forceinline__ void tile_step(State<T, D> &st, const u4 (&q)[2][Geo<
 template <int BM, int D>
 constexpr int64_t slot_floats() { return BM * (D + 2); }
 
+// What block `block` of `blocks` (a multiple of 8) works on.  The buffers are separate arrays; wild: of the tiles in v0buf and
+// v1buf, by wavefront.
 template <class T, int D, Relation REL>
-__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
+__device__ __forceinline__ void wide_pieces(const Args<REL> &a, unsigned block, unsigned blocks, uint8_t *k0buf, uint8_t *v0buf,
+                                            uint8_t *k1buf, uint8_t *v1buf, int (*wild)[kWaves]) {
     using G = Geo<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t k0buf[G::TILE], v0buf[G::TILE], k1buf[G::TILE], v1buf[G::TILE];
-    __shared__ int wild[2][kWaves];  // of the tiles in v0buf and v1buf, by wavefront
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, g = lane >> 4;
 
@@ -721,23 +715,22 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
-    if constexpr (REL == kShared) leave_skips(a.src);
     Deal<REL, G::BM, G::BN> deal;
     typename Deal<REL, G::BM, G::BN>::Load lanes = deal.begin(a);
-    if (a.part && threadIdx.x == 0 && deal.pieces + blockIdx.x < a.slots) a.rec[2 * (deal.pieces + blockIdx.x)] = int4{0, 0, 0, 0};
+    if (a.part && threadIdx.x == 0 && deal.pieces + block < a.slots) a.rec[2 * (deal.pieces + block)] = int4{0, 0, 0, 0};
     // block b of the grid (a multiple of 8) runs on XCD b % 8
     const bool whole_items = deal.chunk == deal.kWhole;
-    const int x = blockIdx.x % kXcds;
+    const int x = block % kXcds;
     const int64_t per = deal.pieces / kXcds + (x < deal.pieces % kXcds ? 1 : 0);  // pieces of this XCD
     const int64_t first = whole_items ? x : x * (deal.pieces / kXcds) + min(static_cast<int64_t>(x), deal.pieces % kXcds);
-    for (int64_t i = blockIdx.x / kXcds; i < per; i += gridDim.x / kXcds) {
+    for (int64_t i = block / kXcds; i < per; i += blocks / kXcds) {
         const int64_t id = first + (whole_items ? i * kXcds : i);
         Seq s;
-        if (i >= gridDim.x / kXcds) lanes = deal.load(a, lane_id());  // not kept over a piece's work
+        if (i >= blocks / kXcds) lanes = deal.load(a, lane_id());  // not kept over a piece's work
         const typename Deal<REL, G::BM, G::BN>::Piece pc = deal.piece(a, lanes, id, s);
         if (a.part && threadIdx.x == 0 && id < a.slots) {
             a.rec[2 * id] = pc.part == 0 && pc.parts > 1 ? int4{pc.b + 1, pc.head, pc.j, pc.parts} : int4{0, 0, 0, 0};
-            a.rec[2 * id + 1] = int4{deal.chunk, 0, 0, 0};
+            a.rec[2 * id + 1] = REL == kShared ? int4{deal.chunk, s.first, s.rows, 0} : int4{deal.chunk, 0, 0, 0};
         }
         const int r0 = pc.j * G::BM + w * 32;
         Source<REL> ks, vs;
@@ -764,18 +757,10 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
         st.m[0] = st.m[1] = -__builtin_inff();
         st.l[0] = st.l[1] = 0.0f;
         if constexpr (REL == kBehind) {
-            if (pc.part == 0 && cells.skip > 0) {
-                const float lift = __builtin_exp2f(kLift<T>);
+            if (pc.part == 0 && g == 0)
 #pragma unroll
-                for (int qb = 0; qb < 2; ++qb) {
-                    const Before<D> x(a, cells, pc.b, s, pc.head, min(r0 + qb * 16 + col, s.rows - 1));
-                    st.m[qb] = x.m - kLift<T>;
-                    st.l[qb] = g == 0 ? x.l * lift : 0.0f;
-#pragma unroll
-                    for (int db = 0; db < G::DB; ++db)
-                        st.o[db][qb] = x.l == 0.0f ? f4{0.0f, 0.0f, 0.0f, 0.0f} : *reinterpret_cast<const f4 *>(x.o + db * 16 + g * 4) * (x.l * lift);
-                }
-            }
+                for (int qb = 0; qb < 2; ++qb)
+                    if (r0 + qb * 16 + col < s.rows) st.l[qb] = open_row(a, cells, pc.b, s, pc.head, r0 + qb * 16 + col);
         }
 
         // A load's 1 KB are 4 or 8 rows from a multiple of as many, so in pages of 8 rows or more they lie in one page.
@@ -899,6 +884,14 @@ __global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
             }
         }
     }
+}
+
+template <class T, int D, Relation REL>
+__global__ __launch_bounds__(kThreads, 2) void wide_kernel(Args<REL> a) {
+    constexpr int TILE = Geo<D>::TILE;
+    __shared__ __attribute__((aligned(1024))) uint8_t k0buf[TILE], v0buf[TILE], k1buf[TILE], v1buf[TILE];
+    __shared__ int wild[2][kWaves];
+    wide_pieces<T, D, REL>(a, blockIdx.x, gridDim.x, k0buf, v0buf, k1buf, v1buf, wild);
     clear_outside<D, REL>(a);
 }
 
@@ -979,24 +972,23 @@ __device__ __forceinline__ void thin_step(ThinState<T, D> &st, const u4 *q, cons
         }
 }
 
-template <class T, int D, Relation REL>
-__global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
+// What block `block` of `blocks` works on.  v0of(i), v1of(i): wavefront i's buffers, in separate arrays.
+template <int D>
+constexpr int kThinWave = Thin<D>::KW *Thin<D>::RB;  // bytes of a wavefront's step of values: 8 KB, also 16 rows of fp32 states or more
+template <class T, int D, Relation REL, class Buffer0, class Buffer1>
+__device__ __forceinline__ void thin_pieces(const Args<REL> &a, int block, int blocks, Buffer0 v0of, Buffer1 v1of,
+                                            float (*ml)[kWaves][Thin<D>::BM]) {
     using G = Thin<D>;
-    constexpr int WAVE = G::KW * G::RB;  // bytes of a wavefront's step of values: 8 KB, also 16 rows of fp32 states or more
-    static_assert(WAVE >= G::BM * D * 4, "a wavefront's state fits its buffer");
-    __shared__ __attribute__((aligned(1024))) uint8_t v0buf[kWaves * WAVE], v1buf[kWaves * WAVE];
-    __shared__ float ml[2][kWaves][G::BM];
+    static_assert(kThinWave<D> >= G::BM * D * 4, "a wavefront's state fits its buffer");
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, g = lane >> 4;
-    const int block = static_cast<int>(xcd_block());
-    uint8_t *const v0 = v0buf + w * WAVE, *const v1 = v1buf + w * WAVE;
+    uint8_t *const v0 = v0of(w), *const v1 = v1of(w);
 
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
-    if constexpr (REL == kShared) leave_skips(a.src);
     Walk<REL, G::BM, G::BN> walk;
-    walk.begin(a, block, static_cast<int>(gridDim.x));
+    walk.begin(a, block, blocks);
     if (a.part && threadIdx.x == 0) {
         a.rec[2 * block] = int4{0, 0, 0, 0};
         a.rec[2 * block + 1] = int4{0, 0, 0, 0};
@@ -1025,15 +1017,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
         st.m = -__builtin_inff();
         st.l = 0.0f;
         if constexpr (REL == kBehind) {
-            if (pc.starts && w == 0 && cells.skip > 0) {
-                const float lift = __builtin_exp2f(kLift<T>);
-                const Before<D> x(a, cells, walk.b, s, pc.head, r);
-                st.m = x.m;
-                st.l = g == 0 ? x.l * lift : 0.0f;
-#pragma unroll
-                for (int db = 0; db < G::DB; ++db)
-                    st.o[db] = x.l == 0.0f ? f4{0.0f, 0.0f, 0.0f, 0.0f} : *reinterpret_cast<const f4 *>(x.o + db * 16 + g * 4) * (x.l * lift);
-            }
+            if (pc.starts && w == 0 && g == 0 && r0 + col < s.rows) st.l = open_row(a, cells, walk.b, s, pc.head, r0 + col);
         }
 
         // the step's first key; positions past the last key read that key (masked, and its value cleared)
@@ -1154,7 +1138,7 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
             for (int i = 0; i < kWaves; ++i) {
                 const float f = __builtin_amdgcn_exp2f(ml[0][i][tr] - ref);
                 l += f * ml[1][i][tr];
-                const float *const p = reinterpret_cast<const float *>(v0buf + i * WAVE) + tr * D;
+                const float *const p = reinterpret_cast<const float *>(v0of(i)) + tr * D;
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[e] += f * p[4 * ((d0 + e) / 4 ^ tr) + e % 4];
             }
@@ -1176,6 +1160,15 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
         }
         __syncthreads();  // the states are read before the next item's values arrive
     }
+}
+
+template <class T, int D, Relation REL>
+__global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
+    constexpr int WAVE = kThinWave<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t v0buf[kWaves * WAVE], v1buf[kWaves * WAVE];
+    __shared__ float ml[2][kWaves][Thin<D>::BM];
+    thin_pieces<T, D, REL>(a, static_cast<int>(xcd_block()), static_cast<int>(gridDim.x), [&](int i) { return v0buf + i * WAVE; },
+                           [&](int i) { return v1buf + i * WAVE; }, ml);
     clear_outside<D, REL>(a);
 }
 
@@ -1184,20 +1177,17 @@ __global__ __launch_bounds__(kThreads, 2) void thin_kernel(Args<REL> a) {
 // two or four a row).  The time is that of a few dependent reads of lines that other XCDs wrote, so 16 bytes a
 // lane of 4 or (many parts) 16 parts a lane are in flight in every wavefront; the sums are added in a fixed order.
 template <class T, int D, Relation REL>
-__global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<REL> a, int blocks) {
+__device__ __forceinline__ void thin_merge(const Args<REL> &a, int x, int y, int blocks, f4 (*so)[kWave], float (*sl)[kWave]) {
     constexpr int BM = Thin<D>::BM, L = D / 4, PP = kWave / L;  // L lanes a part, PP parts a wavefront's read
-    __shared__ f4 so[kWaves][kWave];
-    __shared__ float sl[kWaves][kWave];
-    const int x = static_cast<int>(xcd_block());  // items start every few blocks: in every eighth, one XCD would join all
     const int4 it = a.rec[2 * x + 1];
     if (it.x == 0) return;
     const int b = it.x - 1, head = it.y, j = it.z;
     const Seq s = seq_of<REL>(a, b);
     const int rows = min(s.rows - j * BM, BM), per_block = (rows + kWaves - 1) / kWaves;
-    if (static_cast<int>(blockIdx.y) * per_block >= rows) return;
+    if (y * per_block >= rows) return;
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int share = per_block == 1 ? 4 : (per_block == 2 ? 2 : 1);  // wavefronts a row
-    const int r = static_cast<int>(blockIdx.y) * per_block + w / share, turn = w % share;
+    const int r = y * per_block + w / share, turn = w % share;
     const bool busy = w / share < per_block && r < rows;
     float m = -__builtin_inff(), l = 0.0f, ref = 0.0f;
     f4 o{0.0f, 0.0f, 0.0f, 0.0f};
@@ -1267,13 +1257,20 @@ __global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<REL> a, int b
     if (lane == 0) put_lse(a, b, s, head, j * BM + r, ref + __log2f(l));
 }
 
+template <class T, int D, Relation REL>
+__global__ __launch_bounds__(kThreads) void thin_merge_kernel(Args<REL> a, int blocks) {
+    __shared__ f4 so[kWaves][kWave];
+    __shared__ float sl[kWaves][kWave];
+    // items start every few blocks: in every eighth, one XCD would join all
+    thin_merge<T, D, REL>(a, static_cast<int>(xcd_block()), static_cast<int>(blockIdx.y), blocks, so, sl);
+}
+
 // Joins the parts of the wide item whose first part is in slot x: a wavefront takes 4 rows, 16 bytes a lane, the parts in
 // order and 16 reads of accumulators in flight, rescaling into the common maximum as it goes.
 template <class T, class G, Relation REL>
-__global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
+__device__ __forceinline__ void wide_merge(const Args<REL> &a, int x, int y) {
     constexpr int D = G::CPR * 8, BM = G::BM, L = D / 4, AT = kWave / L, N = 4 / AT, U = 16 / N;
     typedef Deal<REL, BM, G::BN> Pieces;
-    const int x = blockIdx.x;
     const int4 it = a.rec[2 * x];
     if (it.x == 0) return;
     const int chunk = a.rec[2 * x + 1].x;
@@ -1282,7 +1279,7 @@ __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
     const typename Pieces::Load load = Pieces::load(a, s);
     const int rows = min(s.rows - j * BM, BM);
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
-    const int r0 = (static_cast<int>(blockIdx.y) * kWaves + w) * 4;
+    const int r0 = (y * kWaves + w) * 4;
     if (r0 >= rows) return;
     int row[N];  // rows r0 + 0..3: AT of them at a time
     float m[N], l[N];
@@ -1337,6 +1334,11 @@ __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
     }
 }
 
+template <class T, class G, Relation REL>
+__global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
+    wide_merge<T, G, REL>(a, static_cast<int>(blockIdx.x), static_cast<int>(blockIdx.y));
+}
+
 // The slot of the n-th item that has parts, or -1.
 template <Relation REL>
 __device__ __forceinline__ int nth_item(const Args<REL> &a, int n) {
@@ -1360,33 +1362,33 @@ __device__ __forceinline__ int nth_item(const Args<REL> &a, int n) {
 }
 
 // Joins the parts of the n-th wide item of shared positions: there are few items (the rows of a group are one tile or two a
-// head) of many parts, so a block takes the rows that a wavefront reads at once, and each wavefront a quarter of the parts;
-// the quarters are joined in order.
+// head) of many parts, so a block takes twice the rows that a wavefront reads at once, and each wavefront half of the parts of
+// one of them; the halves are joined in order.
+template <class G>
+constexpr int kSharedRows = 2 * kWave / (G::CPR * 2);  // of a block
 template <class T, class G>
-__global__ __launch_bounds__(kThreads) void shared_merge_kernel(Args<kShared> a) {
-    constexpr int D = G::CPR * 8, BM = G::BM, L = D / 4, AT = kWave / L, U = 8;
-    typedef Deal<kShared, BM, G::BN> Pieces;
-    __shared__ f4 so[kWaves][kWave];
-    __shared__ float sm[kWaves][AT], sl[kWaves][AT];
+__device__ __forceinline__ void shared_merge(const Args<kShared> &a, int nth, int y, f4 (*so)[kWave], float (*sl)[kWave]) {
+    constexpr int D = G::CPR * 8, BM = G::BM, L = D / 4, AT = kWave / L, U = 8, H = 2;
+    static_assert(kSharedRows<G> == AT * (kWaves / H), "a block's rows");
+    __shared__ float sm[kWaves][AT];
     __shared__ int slot;
     if (threadIdx.x < kWave) {
-        const int mine = nth_item(a, static_cast<int>(blockIdx.x));
+        const int mine = nth_item(a, nth);
         if (threadIdx.x == 0) slot = mine;
     }
     __syncthreads();
     const int x = uniform(slot);
     if (x < 0) return;
-    const int4 it = a.rec[2 * x];
+    const int4 it = a.rec[2 * x], of = a.rec[2 * x + 1];
     const int b = it.x - 1, head = it.y, j = it.z, n = it.w;
-    const Seq s = seq_of<kShared>(a, b);
-    const int rows = min(s.rows - j * BM, BM), r0 = static_cast<int>(blockIdx.y) * AT;
-    if (r0 >= rows) return;
-    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
-    const int row = min(r0 + lane / L, rows - 1), tiles = Pieces::load(a, s).tiles;  // the parts of a row tile lie `tiles` apart
+    const Seq s{of.y, of.z, 0};
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave), half = w % H;
+    const int rows = min(s.rows - j * BM, BM), r = (y * (kWaves / H) + w / H) * AT + lane / L;
+    const int row = min(r, rows - 1), tiles = (s.rows + BM - 1) / BM;  // the parts of a row tile lie `tiles` apart
     float m = -__builtin_inff(), l = 0.0f;
     f4 o{0.0f, 0.0f, 0.0f, 0.0f};
-    const int last = n * (w + 1) / kWaves;
-    for (int c = n * w / kWaves; c < last; c += U) {
+    const int last = n * (half + 1) / H;
+    for (int c = n * half / H; c < last; c += U) {
         f4 po[U];
         float pm[U], pl[U];
 #pragma unroll
@@ -1417,16 +1419,16 @@ __global__ __launch_bounds__(kThreads) void shared_merge_kernel(Args<kShared> a)
         sl[w][lane / L] = l;
     }
     __syncthreads();
-    if (w != 0 || r0 + lane / L >= rows) return;
-    for (int i = 1; i < kWaves; ++i) m = fmaxf(m, sm[i][lane / L]);
+    if (half != 0 || r >= rows) return;
+    for (int i = 1; i < H; ++i) m = fmaxf(m, sm[w + i][lane / L]);
     const float ref = m == -__builtin_inff() ? 0.0f : m;
     l = 0.0f;
     o = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        const float f = __builtin_amdgcn_exp2f(sm[i][lane / L] - ref);
-        l += f * sl[i][lane / L];
-        o += so[i][lane] * f;
+    for (int i = 0; i < H; ++i) {
+        const float f = __builtin_amdgcn_exp2f(sm[w + i][lane / L] - ref);
+        l += f * sl[w + i][lane / L];
+        o += so[w + i][lane] * f;
     }
     put<T>(out_row<D, kShared>(a, b, s, head, j * BM + row) + 4 * (lane % L), o * (l == 0.0f ? 0.0f : 1.0f / l));
     if (lane % L == 0) put_lse(a, b, s, head, j * BM + row, m + __log2f(l));
@@ -1517,9 +1519,6 @@ int run(const Plan &p, Args<REL> a, void *ws, hipStream_t stream) {
     if constexpr (kNarrow<G>)
         hipLaunchKernelGGL((thin_merge_kernel<T, D, REL>), dim3(static_cast<unsigned>(p.blocks), kWaves), dim3(kThreads), 0,
                            stream, a, static_cast<int>(p.blocks));
-    else if constexpr (REL == kShared)  // items that have parts are fewer than slots
-        hipLaunchKernelGGL((shared_merge_kernel<T, G>), dim3(static_cast<unsigned>(p.items < p.slots ? p.items : p.slots), G::BM * (D / 4) / kWave),
-                           dim3(kThreads), 0, stream, a);
     else
         hipLaunchKernelGGL((wide_merge_kernel<T, G, REL>), dim3(static_cast<unsigned>(p.slots), G::BM / 16), dim3(kThreads), 0,
                            stream, a);
