@@ -93,6 +93,9 @@ struct Packed {
     const int32_t *ptr;
     int32_t batch, num_rows;
 };
+struct Planned : Packed {
+    const int4 *table;  // packed_plan.hpp
+};
 // Rows [first, first + count) of sequence b.  Pointers that run backwards or past num_rows give an empty or a shortened
 // range, never one outside the tensors.
 struct Run {

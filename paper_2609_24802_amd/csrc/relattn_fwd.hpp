@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "mfma16.hpp"
+#include "packed_plan.hpp"
 #include "relation.hpp"
 #include "relattn.hpp"
 
@@ -59,13 +60,16 @@ struct Strided {
 // What a call's rows read: a padded batch of other sequences, a cache's pages up to the row's position, their own
 // sequence's rows of packed sequences up to themselves; and for sequences of which groups share their first positions, those
 // (the rows of all of a group's sequences are one item's) and the pages behind them, whose results are joined afterwards.
-enum Relation { kStrided, kPaged, kPacked, kShared, kBehind };
+// kPlanned: packed, the pieces in the order of a table.
+enum Relation { kStrided, kPaged, kPacked, kShared, kBehind, kPlanned };
+template <Relation REL>
+constexpr bool kOwnRows = REL == kPacked || REL == kPlanned;
 template <Relation REL>
 constexpr bool kPages = REL == kPaged || REL == kShared || REL == kBehind;
 template <Relation REL>
 constexpr bool kHalf = REL == kShared || REL == kBehind;  // results are fp32 states
 template <Relation REL>
-constexpr bool kCausal = REL == kPaged || REL == kPacked || REL == kBehind;
+constexpr bool kCausal = REL == kPaged || REL == kBehind || kOwnRows<REL>;
 template <Relation REL>
 struct SourceArgs {
     typedef Strided type;
@@ -77,6 +81,10 @@ struct SourceArgs<kPaged> {
 template <>
 struct SourceArgs<kPacked> {
     typedef Packed type;
+};
+template <>
+struct SourceArgs<kPlanned> {
+    typedef Planned type;
 };
 template <>
 struct SourceArgs<kShared> {
@@ -126,7 +134,7 @@ __device__ __forceinline__ Seq seq_of(const Args<REL> &a, int b) {
     if constexpr (REL == kPaged) {
         const Chunk ch = chunk_of(a.src, b);
         return Seq{ch.first, ch.count * static_cast<int32_t>(a.group.d), ch.pos0 + 1};
-    } else if constexpr (REL == kPacked) {
+    } else if constexpr (kOwnRows<REL>) {
         const Run run = run_of(a.src, b);
         return Seq{run.first, run.count * static_cast<int32_t>(a.group.d), 1};
     } else if constexpr (REL == kShared) {
@@ -150,7 +158,7 @@ __device__ __forceinline__ Seq lane_seq(const Seq &s, int lane) {
 // no page: it needs no more of them to become NaN.
 template <Relation REL>
 __device__ __forceinline__ int32_t keys_of(const Args<REL> &a, const Seq &s, int r) {
-    if constexpr (REL == kPacked) {
+    if constexpr (kOwnRows<REL>) {
         return 1 + a.group.div(r);
     } else if constexpr (kCausal<REL>) {
         const int64_t n = s.keys0 + a.group.div(r), most = (static_cast<int64_t>(a.src.table_width) << a.src.shift) + 1;
@@ -440,7 +448,7 @@ struct Source {
     __device__ __forceinline__ void set(const Args<REL> &a, const Rows &t, int b, const Seq &s, int head) {
         p = t.p + head * t.head;
         row = t.row;
-        if constexpr (REL == kPacked) {
+        if constexpr (kOwnRows<REL>) {
             p += s.first * row;
         } else if constexpr (kPages<REL>) {
             page_stride = t.batch;
@@ -519,7 +527,7 @@ __device__ __forceinline__ float open_row(const Args<kBehind> &a, const Cells<kB
 // Rows of no sequence of a packed call: before ptr[0] and behind ptr[batch].  They see nothing: y = 0, lse = -inf.
 template <int D, Relation REL>
 __device__ __forceinline__ void clear_outside(const Args<REL> &a) {
-    if constexpr (REL == kPacked) {
+    if constexpr (kOwnRows<REL>) {
         const Run inside = a.src.batch > 0 ? run_between(a.src.ptr, 0, a.src.batch, a.src.num_rows) : Run{0, 0};
         const int32_t outside = a.src.num_rows - inside.count;
         if (outside == 0) return;
@@ -715,22 +723,40 @@ __device__ __forceinline__ void wide_pieces(const Args<REL> &a, unsigned block, 
     const int vrow = 4 * g + col / 4;
     const int vr = vrow * G::RB + 32 * ((vrow / G::R) % G::DB) + 8 * (col % 4);
 
-    Deal<REL, G::BM, G::BN> deal;
-    typename Deal<REL, G::BM, G::BN>::Load lanes = deal.begin(a);
-    if (a.part && threadIdx.x == 0 && deal.pieces + block < a.slots) a.rec[2 * (deal.pieces + block)] = int4{0, 0, 0, 0};
-    // block b of the grid (a multiple of 8) runs on XCD b % 8
-    const bool whole_items = deal.chunk == deal.kWhole;
-    const int x = block % kXcds;
-    const int64_t per = deal.pieces / kXcds + (x < deal.pieces % kXcds ? 1 : 0);  // pieces of this XCD
-    const int64_t first = whole_items ? x : x * (deal.pieces / kXcds) + min(static_cast<int64_t>(x), deal.pieces % kXcds);
-    for (int64_t i = block / kXcds; i < per; i += blocks / kXcds) {
-        const int64_t id = first + (whole_items ? i * kXcds : i);
+    typedef Deal<REL, G::BM, G::BN> Pieces;
+    Pieces deal;
+    typename Pieces::Load lanes;
+    bool whole_items = false;
+    int64_t per = 1, first = 0;  // pieces of this block (planned), or of its XCD: block b of the grid (a multiple of 8) runs on XCD b % 8
+    if constexpr (REL != kPlanned) {
+        lanes = deal.begin(a);
+        if (a.part && threadIdx.x == 0 && deal.pieces + block < a.slots) a.rec[2 * (deal.pieces + block)] = int4{0, 0, 0, 0};
+        whole_items = deal.chunk == deal.kWhole;
+        const int x = block % kXcds;
+        per = deal.pieces / kXcds + (x < deal.pieces % kXcds ? 1 : 0);
+        first = whole_items ? x : x * (deal.pieces / kXcds) + min(static_cast<int64_t>(x), deal.pieces % kXcds);
+    }
+    for (int64_t i = REL == kPlanned ? 0 : block / kXcds; i < per; i += REL == kPlanned ? 1 : blocks / kXcds) {
+        int64_t id;
         Seq s;
-        if (i >= blocks / kXcds) lanes = deal.load(a, lane_id());  // not kept over a piece's work
-        const typename Deal<REL, G::BM, G::BN>::Piece pc = deal.piece(a, lanes, id, s);
-        if (a.part && threadIdx.x == 0 && id < a.slots) {
-            a.rec[2 * id] = pc.part == 0 && pc.parts > 1 ? int4{pc.b + 1, pc.head, pc.j, pc.parts} : int4{0, 0, 0, 0};
-            a.rec[2 * id + 1] = REL == kShared ? int4{deal.chunk, s.first, s.rows, 0} : int4{deal.chunk, 0, 0, 0};
+        typename Pieces::Piece pc;
+        if constexpr (REL == kPlanned) {
+            id = block;
+            const Item it = item_of(a.src.table, a.kv_heads, static_cast<int32_t>(a.group.d), static_cast<int32_t>(block));
+            if (it.level == 0) break;
+            s = Seq{it.run.first, it.run.count * static_cast<int32_t>(a.group.d), 1};
+            pc = typename Pieces::Piece{it.b, it.kv, it.level - 1, 0, 0, it.part, it.parts};
+            const int32_t n = (keys_of<REL>(a, s, min((pc.j + 1) * G::BM, s.rows) - 1) + G::BN - 1) / G::BN;
+            pc.t0 = part_start(n, it.part, it.parts);
+            pc.t1 = part_start(n, it.part + 1, it.parts);
+        } else {
+            id = first + (whole_items ? i * kXcds : i);
+            if (i >= blocks / kXcds) lanes = deal.load(a, lane_id());  // not kept over a piece's work
+            pc = deal.piece(a, lanes, id, s);
+            if (a.part && threadIdx.x == 0 && id < a.slots) {
+                a.rec[2 * id] = pc.part == 0 && pc.parts > 1 ? int4{pc.b + 1, pc.head, pc.j, pc.parts} : int4{0, 0, 0, 0};
+                a.rec[2 * id + 1] = REL == kShared ? int4{deal.chunk, s.first, s.rows, 0} : int4{deal.chunk, 0, 0, 0};
+            }
         }
         const int r0 = pc.j * G::BM + w * 32;
         Source<REL> ks, vs;
@@ -1337,6 +1363,48 @@ __device__ __forceinline__ void wide_merge(const Args<REL> &a, int x, int y) {
 template <class T, class G, Relation REL>
 __global__ __launch_bounds__(kThreads) void wide_merge_kernel(Args<REL> a) {
     wide_merge<T, G, REL>(a, static_cast<int>(blockIdx.x), static_cast<int>(blockIdx.y));
+}
+
+// Joins the parts of the planned item whose first part is piece x, kv_heads pieces apart: a wavefront takes the rows that it reads
+// at once, the parts in order.
+template <class T, class G>
+__global__ __launch_bounds__(kThreads) void planned_merge_kernel(Args<kPlanned> a) {
+    constexpr int D = G::CPR * 8, BM = G::BM, L = D / 4, AT = kWave / L, U = 8;
+    const Item it = item_of(a.src.table, a.kv_heads, static_cast<int32_t>(a.group.d), static_cast<int32_t>(blockIdx.x));
+    if (it.level == 0 || it.part != 0 || it.parts == 1) return;
+    const Seq s{it.run.first, it.run.count * static_cast<int32_t>(a.group.d), 1};
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave), j = it.level - 1;
+    const int rows = min(s.rows - j * BM, BM), r = (static_cast<int>(blockIdx.y) * kWaves + w) * AT + lane / L, row = min(r, rows - 1);
+    float m = -__builtin_inff(), l = 0.0f;
+    f4 o{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < it.parts; c += U) {
+        f4 po[U];
+        float pm[U], pl[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
+            const float *const p = a.part + (blockIdx.x + static_cast<int64_t>(min(c + i, it.parts - 1)) * a.kv_heads) * slot_floats<BM, D>();
+            pm[i] = p[BM * D + row];
+            pl[i] = p[BM * (D + 1) + row];
+            po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < U; ++i) top = fmaxf(top, pm[i]);
+        const float ref = top == -__builtin_inff() ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+        m = top;
+        l *= alpha;
+        o *= alpha;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (c + i >= it.parts) break;
+            const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
+            l += f * pl[i];
+            o += f * po[i];
+        }
+    }
+    if (r >= rows) return;
+    put<T>(out_row<D, kPlanned>(a, it.b, s, it.kv, j * BM + row) + 4 * (lane % L), o * (l == 0.0f ? 0.0f : 1.0f / l));
+    if (lane % L == 0) put_lse(a, it.b, s, it.kv, j * BM + row, m + __log2f(l));
 }
 
 // The slot of the n-th item that has parts, or -1.

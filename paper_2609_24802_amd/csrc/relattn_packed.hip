@@ -18,12 +18,79 @@ Plan packed_plan(const tiga_packed &rel) {
     return p;
 }
 
+// Sequences of 512 tokens or more on average are worked on in a planned order, longest items first and cut where they are long,
+// as long as the order matters: causal items take from nothing to twice the mean, and with few rounds of them on the device the
+// last round is left to the long ones.  The launch that plans takes 7 us and the join 3.  us dealt (as other relations are) and
+// planned, width 128: 16 heads over 2 source heads, 4000 tokens 120 and 105; 8 over 8, 8000 tokens 192 and 164; 16, 8 x 2000
+// tokens 179 and 160.  Below one tile to a CU items are cut when they are dealt, too (8 heads, 4000 tokens 66 and 70, at width
+// 64 with 2000 tokens 46 and 30); of one or two sequences many tiles fill the device however they come (32 over 4, 4000 tokens
+// 138 and 150).
+constexpr int64_t kPlannedMean = 512, kPlannedTiles = 8;  // key tiles of a part, at least
+constexpr int64_t kPlannedFew = 3, kPlannedMost = 8;      // tiles to a CU: of up to three sequences, and of more
+bool planned(const tiga_packed &rel) {
+    const int64_t work = rel.num_rows * rel.heads, cu = static_cast<int64_t>(device_cus()) * kTileRows;
+    return rel.batch <= kWave && rel.num_rows >= kPlannedMean * rel.batch && (rel.width == 64 || work > cu) &&
+           work <= (rel.batch < 4 ? kPlannedFew : kPlannedMost) * cu;
+}
+struct Planning {
+    Pieces by_rows;
+    float *part;
+    int64_t cut;  // pieces of cut items, at most
+    size_t bytes;
+};
+template <int D>
+Planning planning(const tiga_packed &rel, void *ws) {
+    const int64_t group = rel.kv_heads ? rel.heads / rel.kv_heads : 1;
+    Planning p;
+    const int resident = 2 * device_cus();
+    p.cut = 2 * static_cast<int64_t>(resident);
+    p.by_rows.resident = resident;
+    p.by_rows.mult = static_cast<int32_t>(group < 1 ? 1 : group);
+    p.by_rows.least = static_cast<int32_t>(ceil_div(kPlannedTiles * Geo<D>::BN * group, kTileRows));
+    p.by_rows.places = static_cast<int32_t>(most_items(rel, group) / rel.kv_heads + ceil_div(p.cut, rel.kv_heads));
+    Carve c(ws);
+    // for any number of source heads, and whether this call is planned or not: a workspace holds every smaller call
+    const size_t some = rel.num_rows >= kPlannedMean ? 1 : 0;
+    const size_t rows = static_cast<size_t>(rel.num_rows) * rel.heads, most = static_cast<size_t>(kPlannedMost) * device_cus() * kTileRows;
+    p.by_rows.table = c.take<int4>(some * 2 * ((rows < most ? rows : most) / kTileRows + kWave + p.cut + 1));
+    p.part = c.take<float>(some * (p.cut + rel.heads) * slot_floats<kTileRows, D>());
+    p.bytes = c.bytes();
+    return p;
+}
+
+template <class T, int D>
+int run_planned(const tiga_packed &rel, const Args<kPacked> &given, void *ws, hipStream_t stream) {
+    const Planning p = planning<D>(rel, ws);
+    if (int rc = plan_pieces(rel, p.by_rows, p.by_rows, 1, stream)) return rc;
+    Args<kPlanned> a{};
+    static_cast<Packed &>(a.src) = given.src;
+    a.src.table = p.by_rows.table;
+    a.q = given.q;
+    a.y = given.y;
+    a.lse = given.lse;
+    a.lse_head = given.lse_head;
+    a.c = given.c;
+    a.kv_heads = given.kv_heads;
+    a.group = given.group;
+    a.part = p.part;
+    prof_before(stream);
+    hipLaunchKernelGGL((wide_kernel<T, D, kPlanned>), dim3(static_cast<unsigned>(p.by_rows.places * rel.kv_heads)), dim3(kThreads), 0, stream, a);
+    prof_after(stream);
+    if (int rc = check_launch("packed attention")) return rc;
+    const int64_t cut = ceil_div(p.cut, rel.kv_heads) * rel.kv_heads;  // whole places, so that parts of every head are seen
+    hipLaunchKernelGGL((planned_merge_kernel<T, Geo<D>>), dim3(static_cast<unsigned>(cut), kTileRows * (D / 4) / kThreads), dim3(kThreads), 0,
+                       stream, a);
+    return check_launch("packed attention merge");
+}
+
 }  // namespace
 
 size_t packed_fwd_ws_bytes(const tiga_packed &rel) {
-    if (rel.kv_heads == 0 || rel.num_rows == 0) return 256;
-    return ws_bytes(rel.dtype, rel.width, rel.num_rows * rel.heads, rel.num_rows,
-                    [&](auto g) { return packed_plan<decltype(g)>(rel).slots; });
+    if (rel.kv_heads == 0 || rel.num_rows == 0 || rel.heads == 0) return 256;
+    const size_t dealt = ws_bytes(rel.dtype, rel.width, rel.num_rows * rel.heads, rel.num_rows,
+                                  [&](auto g) { return packed_plan<decltype(g)>(rel).slots; });
+    const size_t in_order = rel.width == 64 ? planning<64>(rel, nullptr).bytes : planning<128>(rel, nullptr).bytes;
+    return dealt > in_order ? dealt : in_order;
 }
 
 int packed_forward(const tiga_packed &rel, const tiga_view &q, const tiga_view &k, const tiga_view &v, float scale,
@@ -38,8 +105,13 @@ int packed_forward(const tiga_packed &rel, const tiga_view &q, const tiga_view &
     a.kv_heads = rel.kv_heads;
     a.group = divider(rel.heads / rel.kv_heads);
     a.src = Packed{rows_of(k), rows_of(v), rel.ptr, rel.batch, static_cast<int32_t>(rel.num_rows)};
-    return by_type(rel.dtype, rel.width, packed_thin(rel), [&](auto t, auto g) {
-        return run<decltype(t), decltype(g), kPacked>(packed_plan<decltype(g)>(rel), a, ws, stream);
+    const bool thin = packed_thin(rel);
+    return by_type(rel.dtype, rel.width, thin, [&](auto t, auto g) {
+        typedef decltype(t) T;
+        typedef decltype(g) G;
+        if constexpr (!kNarrow<G>)
+            if (planned(rel)) return run_planned<T, G::CPR * 8>(rel, a, ws, stream);
+        return run<T, G, kPacked>(packed_plan<G>(rel), a, ws, stream);
     });
 }
 

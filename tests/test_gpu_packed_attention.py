@@ -301,3 +301,49 @@ def test_given_workspaces_are_checked(lib):
                      (torch.empty(1 << 20, 2, dtype=torch.uint8, device="cuda")[:, 0], ValueError)):
         with pytest.raises(err):
             lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, ws=bad)
+
+
+# enough tiles of long sequences that they are worked on in a planned order, cut into parts or not
+PLANNED = [
+    ([2300], 16, 2, 128, BF16, 0, 0),
+    ([2100], 16, 16, 128, F16, 13, 150),
+    ([1400, 1, 700, 0, 900], 16, 4, 128, BF16, 1, 2),
+    ([600] * 4, 32, 4, 64, F16, 0, 0),
+    ([520], 1, 1, 64, BF16, 0, 0),
+    ([130, 4000], 6, 3, 64, F16, 5, 0),
+    ([2200], 18, 3, 128, BF16, 0, 7),
+]
+
+
+@pytest.mark.parametrize("lens,H,Hk,D,dt,lead,tail", PLANNED)
+def test_long_sequences(lib, lens, H, Hk, D, dt, lead, tail):
+    check(lib, Packed(lens, H, Hk, D, dt, seed=21, lead=lead, tail=tail), f"{(lens, H, Hk, D)}")
+
+
+@pytest.mark.parametrize("bad", BAD)
+def test_what_is_not_finite_in_a_long_sequence(lib, bad):
+    """Rows before it are as without it, in whichever part of their keys it lies."""
+    s = Packed([2300], 16, 2, 128, BF16, seed=22)
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+    for row in (0, 1027, 2298):
+        for t in (s.k, s.v):
+            kept = t[1, row].clone()
+            t[1, row, 5] = bad
+            y2, lse2 = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+            torch.cuda.synchronize()
+            t[1, row] = kept
+            assert torch.equal(y2[:8], y[:8]) and torch.equal(lse2[:8], lse[:8])        # of the other source head
+            assert torch.isfinite(y2[:, :row]).all() and torch.isfinite(lse2[:, :row]).all()
+            # the last rounding and the weights' may differ where a neighbour moved the point that weights are relative to
+            torch.testing.assert_close(y2[:, :row].float(), y[:, :row].float(), rtol=2 ** -7, atol=2 ** -6)
+            if t is s.v:
+                assert not torch.isfinite(y2[8:, row:, 5]).any()
+
+
+def test_pointers_that_run_backwards_in_a_long_batch(lib):
+    """Nothing is promised about such a call but that it stays within the tensors and ends."""
+    s = Packed([2200], 16, 2, 128, F16, seed=23)
+    for p in ([2200, 0], [0, 2200, 0, 2200], [1 << 30, -1, 1 << 30, 3], [-5, 1 << 30], [2200, 100, 2200, 0, 2200]):
+        ptr = torch.tensor(p, dtype=torch.int32, device="cuda")
+        lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, ptr, want_lse=True)
+        torch.cuda.synchronize()
