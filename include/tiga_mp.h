@@ -477,7 +477,7 @@ typedef struct {
 } tiga_packed;
 
 /* Workspace bytes for tiga_mp_attention_packed_fwd (0 on error; at most about
- * 36 MB).  One sized for a call holds every smaller one. */
+ * 75 MB).  One sized for a call holds every smaller one. */
 size_t tiga_mp_attention_packed_fwd_workspace(const tiga_packed *rel);
 
 /* The online-softmax reducer over the triangular relation of every packed
@@ -496,15 +496,17 @@ int tiga_mp_attention_packed_fwd(const tiga_packed *rel, const tiga_view *q, con
                                  float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* Workspace bytes for tiga_mp_attention_packed_bwd (0 on error): about 8 bytes a
- * row and head.  One sized for a call holds every smaller one. */
+ * row and head, and from some hundred rows on up to about 140 MB for parts of long
+ * sequences.  One sized for a call holds every smaller one. */
 size_t tiga_mp_attention_packed_bwd_workspace(const tiga_packed *rel);
 
 /* Vector-Jacobian product of tiga_mp_attention_packed_fwd, from its y and lse;
  * formulas, arguments and roundings as tiga_mp_attention_cross_bwd (delta formed
  * as sum_j p_ij <dy_i, v_j> for the rows of a tile of 128 whose last row sees at
- * most 128 tokens).  Gradients of rows of no sequence are 0.  What row i holds
- * reaches the gradients of rows up to i alone, in its own sequence (through its
- * key and value: of rows from i on).
+ * most 128 tokens).  Gradients of rows of no sequence are 0.  Nothing reaches other
+ * sequences.  A query or cotangent that is not finite reaches its own dq and the dk,
+ * dv of the tokens that it sees; a key or value the dq of the rows that see it, and
+ * by way of those rows the dk, dv of what they see.
  * Deterministic (no atomics).  Requirements and errors as the forward; besides, at
  * most 2^24 - 1 tiles of 128 rows of a source head. */
 int tiga_mp_attention_packed_bwd(const tiga_packed *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
@@ -658,8 +660,9 @@ typedef struct {
 int tiga_prefix_validate(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst, const int32_t *dst_ptr,
                          void *stream);
 
-/* Workspace bytes for tiga_mp_attention_prefix_fwd (0 on error): about 36 MB and 4
- * (width + 1) bytes a row and head.  One sized for a call holds every smaller one. */
+/* Workspace bytes for tiga_mp_attention_prefix_fwd (0 on error): at most about 72 MB
+ * and 8 (width + 1) bytes a row and head.  One sized for a call holds every smaller
+ * one. */
 size_t tiga_mp_attention_prefix_fwd_workspace(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst,
                                               int32_t heads);
 
@@ -696,8 +699,10 @@ int tiga_mp_cache_weights(const tiga_cache *cache, int64_t num_dst, const int32_
                           const tiga_view *q, const float *lse, float scale, float decay, const float *weights,
                           float *out, void *ws, size_t ws_bytes, void *stream);
 
-/* Workspace bytes for tiga_mp_cache_evict (0 on error): little; in place (to is
- * cache) the rows that stay.  One sized for a call holds every smaller one. */
+/* Workspace bytes for tiga_mp_cache_evict (0 on error): little; for tables of more
+ * than 32,768 positions 10 KB to 8192 positions of at most 256 sequences and heads;
+ * in place (to is cache) the rows that stay.  One sized for a call holds every
+ * smaller one. */
 size_t tiga_mp_cache_evict_workspace(const tiga_cache *cache, const tiga_cache *to, int32_t keep);
 
 /* Keep the `keep` positions of each sequence and source head with the largest
