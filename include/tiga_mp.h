@@ -645,9 +645,10 @@ int tiga_mp_attention_paged_fwd(const tiga_cache *cache, int64_t num_dst, const 
  *   outside is taken as the nearer bound) and [groups].  Sequences of no group
  *   share nothing.
  * Whether the sequences' tables name the same pages or copies does not matter: the
- * shared positions are read from the pages of a group's first sequence (rounded
- * down to a multiple of the page size and of 128; the rest, and groups of one
- * sequence, from each sequence's own).  The struct lives in HOST memory. */
+ * shared positions are read from the pages of a group's first sequence, with or
+ * without new tokens (as many as it has, rounded down to a multiple of the page size
+ * and of 128; the rest, and groups of one sequence, from each sequence's own).  The
+ * struct lives in HOST memory. */
 typedef struct {
     int32_t groups;
     const int32_t *ptr;

@@ -134,9 +134,11 @@ struct Group {
 };
 __device__ __forceinline__ Group group_of(const Pages &c, const Groups &groups, int g) {
     const Run run = run_between(groups.ptr, g, g + 1, groups.sequences);
-    const int64_t most = static_cast<int64_t>(c.table_width) << c.shift;
+    // no more than the sequence has whose pages are read: it may have ended, and its pages be another's
+    const int64_t held = run.count < 2 ? 0 : c.length[run.first], most = min(held, static_cast<int64_t>(c.table_width) << c.shift);
     int64_t n = groups.len[g];
-    n = n < 0 || run.count < 2 ? 0 : (n > most ? most : n);
+    n = n > most ? most : n;
+    if (n < 0) n = 0;
     return Group{run.first, run.first + run.count, static_cast<int32_t>(n >> groups.whole << groups.whole)};
 }
 // The shared positions of sequence b.  (By the lanes of a wavefront for up to 64 groups, the kernels spill.)

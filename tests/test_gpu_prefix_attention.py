@@ -201,3 +201,14 @@ def test_captured(lib):
         z, lse2 = call()
         torch.cuda.synchronize()
         assert torch.equal(y, z) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("left", [0, 1, 300, 511])
+@pytest.mark.parametrize("new", [1, 30])
+def test_a_first_sequence_that_has_ended(lib, left, new):
+    """What it no longer has is read from the others' own pages."""
+    bt = Grouped([(600, 0), (700, new), (650, new), (900, new)], [(4, 512)], 2, 64, 16, F16, copies=True, seed=31)
+    bt.length[0] = left
+    bt.table[0, -(-left // 16):] = -1
+    lib.tiga_prefix_validate(bt.cache(lib), bt.num_dst, bt.dst_ptr, bt.group_ptr, bt.group_len)
+    compare(lib, bt, 4, f"ended at {left}")
