@@ -1248,11 +1248,17 @@ __device__ __forceinline__ void thin_merge(const Args<REL> &a, int x, int y, int
                 f4 po[U];
                 float pm[U], pl[U];
 #pragma unroll
-                for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
-                    const float *p = state(min(i0 + i * share * PP, n - 1));
-                    po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
-                    pm[i] = p[BM * D + r];
-                    pl[i] = p[BM * (D + 1) + r];
+                for (int i = 0; i < U; ++i) {
+                    po[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                    pm[i] = -__builtin_inff();
+                    pl[i] = 0.0f;
+                    const int part = i0 + i * share * PP;
+                    if (part < n) {
+                        const float *p = state(part);
+                        po[i] = *reinterpret_cast<const f4 *>(p + r * D + 4 * (lane % L));
+                        pm[i] = p[BM * D + r];
+                        pl[i] = p[BM * (D + 1) + r];
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < U; ++i)
@@ -1381,11 +1387,16 @@ __global__ __launch_bounds__(kThreads) void planned_merge_kernel(Args<kPlanned> 
         f4 po[U];
         float pm[U], pl[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
-            const float *const p = a.part + (blockIdx.x + static_cast<int64_t>(min(c + i, it.parts - 1)) * a.kv_heads) * slot_floats<BM, D>();
-            pm[i] = p[BM * D + row];
-            pl[i] = p[BM * (D + 1) + row];
-            po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+        for (int i = 0; i < U; ++i) {
+            pm[i] = -__builtin_inff();
+            pl[i] = 0.0f;
+            po[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (c + i < it.parts) {
+                const float *const p = a.part + (blockIdx.x + static_cast<int64_t>(c + i) * a.kv_heads) * slot_floats<BM, D>();
+                pm[i] = p[BM * D + row];
+                pl[i] = p[BM * (D + 1) + row];
+                po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+            }
         }
         float top = m;
 #pragma unroll
@@ -1396,7 +1407,6 @@ __global__ __launch_bounds__(kThreads) void planned_merge_kernel(Args<kPlanned> 
         o *= alpha;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            if (c + i >= it.parts) break;
             const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
             l += f * pl[i];
             o += f * po[i];
@@ -1460,11 +1470,16 @@ __device__ __forceinline__ void shared_merge(const Args<kShared> &a, int nth, in
         f4 po[U];
         float pm[U], pl[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {  // past the last part: read again, not added
-            const float *const p = a.part + (x + static_cast<int64_t>(min(c + i, last - 1)) * tiles) * slot_floats<BM, D>();
-            pm[i] = p[BM * D + row];
-            pl[i] = p[BM * (D + 1) + row];
-            po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+        for (int i = 0; i < U; ++i) {
+            pm[i] = -__builtin_inff();
+            pl[i] = 0.0f;
+            po[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (c + i < last) {
+                const float *const p = a.part + (x + static_cast<int64_t>(c + i) * tiles) * slot_floats<BM, D>();
+                pm[i] = p[BM * D + row];
+                pl[i] = p[BM * (D + 1) + row];
+                po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+            }
         }
         float top = m;
 #pragma unroll
@@ -1475,7 +1490,6 @@ __device__ __forceinline__ void shared_merge(const Args<kShared> &a, int nth, in
         o *= alpha;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            if (c + i >= last) break;
             const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
             l += f * pl[i];
             o += f * po[i];
