@@ -8,9 +8,10 @@
 // 8 (width + 1) bytes a row and head written and read.
 //
 // Measured (MI355X), kernel + merge + join in us: 64 single tokens behind 8192 shared positions and up to 1000 of their own, 32
-// heads over 8 of width 128, bf16: 45 + 13.8 + 5.1, 64 to 67 a pass, where reading what there is (121 MB) takes 25; each of the
-// two parts by itself takes 23 to 30 and a join.  5 drafted tokens each of 24 sequences over four documents of up to 40,000
-// positions, 16 heads over 2 of width 128, f16: 48.9 + 15.9 + 4.6 for 101 MB and 17 GFLOP (21); 4 single tokens behind 500
+// heads over 8 of width 128, bf16: 45 + 11.2 + 5.1, where reading what there is (121 MB) takes 25; each of the two parts by itself
+// takes 26 to 27, of which 10 to start, find its pieces and end.  (Half of the blocks for either part, so that both run side by
+// side from the start: 49 + 9.)  5 drafted tokens each of 24 sequences over four documents of up to 40,000
+// positions, 16 heads over 2 of width 128, f16: 48.9 + 10.4 + 4.6 for 101 MB and 17 GFLOP (21); 4 single tokens behind 500
 // positions, 16 heads over 4 of width 64: 8.1 + 4.4 + 2.2, latency.  What is above the floors is the time to fill and drain the
 // device three times and, in the merge, dependent loads of the records of the parts (20 to 60 of an item) before their states.
 #include "relattn_fwd.hpp"
