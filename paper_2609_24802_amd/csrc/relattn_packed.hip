@@ -28,13 +28,17 @@ Plan packed_plan(const tiga_packed &rel) {
 // planned, width 128: 16 heads over 2 source heads, 4000 tokens 120 and 105; 8 over 8, 8000 tokens 192 and 164; 16, 8 x 2000
 // tokens 179 and 160.  Below one tile to a CU items are cut when they are dealt, too (8 heads, 4000 tokens 66 and 70, at width
 // 64 with 2000 tokens 46 and 30); of one or two sequences many tiles fill the device however they come (32 over 4, 4000 tokens
-// 138 and 150).
+// 138 and 150), of more the order still evens out some (32 heads over 8 of width 128, 60 sequences of 1 to 1400 tokens: 284 and
+// 260; 17 of 16,384 in all 320 and 314), but at width 64 (16 heads, the 60: 424 and 435).
 constexpr int64_t kPlannedMean = 512, kPlannedTiles = 8;  // key tiles of a part, at least
-constexpr int64_t kPlannedFew = 3, kPlannedMost = 8;      // tiles to a CU: of up to three sequences, and of more
+// tiles to a CU: of up to three sequences, and of more
+constexpr int64_t kPlannedFew = 3;
+template <int D>
+constexpr int64_t kPlannedMost = D == 64 ? 8 : 32;
 bool planned(const tiga_packed &rel) {
     const int64_t work = rel.num_rows * rel.heads, cu = static_cast<int64_t>(device_cus()) * kTileRows;
     return rel.batch <= kWave && rel.num_rows >= kPlannedMean * rel.batch && (rel.width == 64 || work > cu) &&
-           work <= (rel.batch < 4 ? kPlannedFew : kPlannedMost) * cu;
+           work <= (rel.batch < 4 ? kPlannedFew : rel.width == 64 ? kPlannedMost<64> : kPlannedMost<128>) * cu;
 }
 struct Planning {
     Pieces by_rows;
@@ -55,7 +59,7 @@ Planning planning(const tiga_packed &rel, void *ws) {
     Carve c(ws);
     // for any number of source heads, and whether this call is planned or not: a workspace holds every smaller call
     const size_t some = rel.num_rows >= kPlannedMean ? 1 : 0;
-    const size_t rows = static_cast<size_t>(rel.num_rows) * rel.heads, most = static_cast<size_t>(kPlannedMost) * device_cus() * kTileRows;
+    const size_t rows = static_cast<size_t>(rel.num_rows) * rel.heads, most = static_cast<size_t>(kPlannedMost<D>) * device_cus() * kTileRows;
     p.by_rows.table = c.take<int4>(some * 2 * ((rows < most ? rows : most) / kTileRows + kWave + p.cut + 1));
     p.part = c.take<float>(some * (p.cut + rel.heads) * slot_floats<kTileRows, D>());
     p.bytes = c.bytes();
