@@ -25,6 +25,7 @@ struct Pieces {
     int32_t places, mult;
     int32_t resident;  // blocks that run at once
     int32_t least;     // levels of a part, at least (kNoCut: nothing is cut)
+    int32_t quarters;  // of a block's share of all levels, that a part has
 };
 constexpr int32_t kNoCut = 1 << 30;
 // Items are cut into parts of at most `cut` levels.  How many pieces the items of the first m levels make:
@@ -58,12 +59,15 @@ __global__ __launch_bounds__(kPlanThreads) void packed_plan_kernel(const int32_t
     if (p.least < kNoCut && __any(tiles > p.least)) {
         // Parts of half a block's share of all levels, or of as much more as makes at most two pieces a block, up to the whole
         // share, which makes at most twice as many parts as blocks run at once.  (dk and dv of 10,000 tokens, 4 heads over one
-        // of 128: 272 us, 387 with whole shares; 1.3 ms uncut.)
+        // of 128: 272 us, 387 with whole shares; 1.3 ms uncut.)  The forward, whose parts are joined at more cost, takes 5/4:
+        // 4000 tokens, 16 heads over 2, 90 us and 18 to join with halves, 90 + 16 with 5/4, 91 + 12 with 3/2; 8000, 8 over 8, 164 + 18,
+        // 162 + 14, 169 + 11; 10,000, 4 over one, 123 + 20, 129 + 13, 141 + 13.
         const int64_t levels = all(static_cast<int64_t>(tiles) * (tiles + 1) / 2) * kv_heads;
         const int64_t share = min(static_cast<int64_t>(kNoCut) - 1, max(static_cast<int64_t>(p.least), quotient(levels + p.resident - 1, p.resident)));
-        int64_t c = max(static_cast<int64_t>(p.least), (share + 1) / 2);
+        const int64_t most = share * max(p.quarters, 4) / 4;
+        int64_t c = max(static_cast<int64_t>(p.least), (share * p.quarters + 3) / 4);
         while (c < share && all(pieces_upto(tiles, static_cast<int32_t>(c))) * kv_heads > 2 * p.resident) c += c / 16 + 1;
-        cut = static_cast<int32_t>(min(c, share));
+        cut = static_cast<int32_t>(min(c, most));
     }
     const int64_t pieces = pieces_upto(tiles, cut);
     int64_t total = all(pieces);

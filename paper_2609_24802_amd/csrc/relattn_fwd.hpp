@@ -1379,42 +1379,44 @@ __global__ __launch_bounds__(kThreads) void planned_merge_kernel(Args<kPlanned> 
     const Item it = item_of(a.src.table, a.kv_heads, static_cast<int32_t>(a.group.d), static_cast<int32_t>(blockIdx.x));
     if (it.level == 0 || it.part != 0 || it.parts == 1) return;
     const Seq s{it.run.first, it.run.count * static_cast<int32_t>(a.group.d), 1};
-    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave), j = it.level - 1;
-    const int rows = min(s.rows - j * BM, BM), r = (static_cast<int>(blockIdx.y) * kWaves + w) * AT + lane / L, row = min(r, rows - 1);
-    float m = -__builtin_inff(), l = 0.0f;
-    f4 o{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int c = 0; c < it.parts; c += U) {
-        f4 po[U];
-        float pm[U], pl[U];
+    const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave), j = it.level - 1, rows = min(s.rows - j * BM, BM);
+    for (int r0 = static_cast<int>(blockIdx.y) * kWaves + w; r0 * AT < rows; r0 += static_cast<int>(gridDim.y) * kWaves) {
+        const int r = r0 * AT + lane / L, row = min(r, rows - 1);
+        float m = -__builtin_inff(), l = 0.0f;
+        f4 o{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int c = 0; c < it.parts; c += U) {
+            f4 po[U];
+            float pm[U], pl[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            pm[i] = -__builtin_inff();
-            pl[i] = 0.0f;
-            po[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (c + i < it.parts) {
-                const float *const p = a.part + (blockIdx.x + static_cast<int64_t>(c + i) * a.kv_heads) * slot_floats<BM, D>();
-                pm[i] = p[BM * D + row];
-                pl[i] = p[BM * (D + 1) + row];
-                po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+            for (int i = 0; i < U; ++i) {
+                pm[i] = -__builtin_inff();
+                pl[i] = 0.0f;
+                po[i] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (c + i < it.parts) {
+                    const float *const p = a.part + (blockIdx.x + static_cast<int64_t>(c + i) * a.kv_heads) * slot_floats<BM, D>();
+                    pm[i] = p[BM * D + row];
+                    pl[i] = p[BM * (D + 1) + row];
+                    po[i] = *reinterpret_cast<const f4 *>(p + row * D + 4 * (lane % L));
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < U; ++i) top = fmaxf(top, pm[i]);
+            const float ref = top == -__builtin_inff() ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+            m = top;
+            l *= alpha;
+            o *= alpha;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
+                l += f * pl[i];
+                o += f * po[i];
             }
         }
-        float top = m;
-#pragma unroll
-        for (int i = 0; i < U; ++i) top = fmaxf(top, pm[i]);
-        const float ref = top == -__builtin_inff() ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
-        m = top;
-        l *= alpha;
-        o *= alpha;
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const float f = __builtin_amdgcn_exp2f(pm[i] - ref);
-            l += f * pl[i];
-            o += f * po[i];
-        }
+        if (r >= rows) continue;
+        put<T>(out_row<D, kPlanned>(a, it.b, s, it.kv, j * BM + row) + 4 * (lane % L), o * (l == 0.0f ? 0.0f : 1.0f / l));
+        if (lane % L == 0) put_lse(a, it.b, s, it.kv, j * BM + row, m + __log2f(l));
     }
-    if (r >= rows) return;
-    put<T>(out_row<D, kPlanned>(a, it.b, s, it.kv, j * BM + row) + 4 * (lane % L), o * (l == 0.0f ? 0.0f : 1.0f / l));
-    if (lane % L == 0) put_lse(a, it.b, s, it.kv, j * BM + row, m + __log2f(l));
 }
 
 // The slot of the n-th item that has parts, or -1.

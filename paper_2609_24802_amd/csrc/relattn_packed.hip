@@ -24,21 +24,19 @@ Plan packed_plan(const tiga_packed &rel) {
 
 // Sequences of 512 tokens or more on average are worked on in a planned order, longest items first and cut where they are long,
 // as long as the order matters: causal items take from nothing to twice the mean, and with few rounds of them on the device the
-// last round is left to the long ones.  The launch that plans takes 7 us and the join 3.  us dealt (as other relations are) and
-// planned, width 128: 16 heads over 2 source heads, 4000 tokens 120 and 105; 8 over 8, 8000 tokens 192 and 164; 16, 8 x 2000
-// tokens 179 and 160.  Below one tile to a CU items are cut when they are dealt, too (8 heads, 4000 tokens 66 and 70, at width
-// 64 with 2000 tokens 46 and 30); of one or two sequences many tiles fill the device however they come (32 over 4, 4000 tokens
-// 138 and 150), of more the order still evens out some (32 heads over 8 of width 128, 60 sequences of 1 to 1400 tokens: 284 and
-// 260; 17 of 16,384 in all 320 and 314), but at width 64 (16 heads, the 60: 424 and 435).
+// last round is left to the long ones.  The launch that plans takes 5 us and the join 5 to 15.  us dealt (as other relations are)
+// and planned, width 128: 16 heads over 2 source heads, 4000 tokens 118 and 103; 8 over 8, 8000 tokens 190 and 163; 16, 8 x
+// 2000 tokens 175 and 154; 32 over 8, 17 prompts of 16,384 in all 307 and 298; width 64, 8 over 2, 2000 tokens 47 and 32.  Many
+// tiles of one sequence fill the device however they come (32 over 4, 4000 tokens 134 and 140; 16 over 4, 16,000 899 and 911), and
+// so do very many at width 64.
 constexpr int64_t kPlannedMean = 512, kPlannedTiles = 8;  // key tiles of a part, at least
-// tiles to a CU: of up to three sequences, and of more
-constexpr int64_t kPlannedFew = 3;
+constexpr int64_t kPlannedOne = 3;                        // tiles to a CU: of one sequence, and of more
 template <int D>
 constexpr int64_t kPlannedMost = D == 64 ? 8 : 32;
 bool planned(const tiga_packed &rel) {
-    const int64_t work = rel.num_rows * rel.heads, cu = static_cast<int64_t>(device_cus()) * kTileRows;
-    return rel.batch <= kWave && rel.num_rows >= kPlannedMean * rel.batch && (rel.width == 64 || work > cu) &&
-           work <= (rel.batch < 4 ? kPlannedFew : rel.width == 64 ? kPlannedMost<64> : kPlannedMost<128>) * cu;
+    const int64_t most = rel.batch < 2 ? kPlannedOne : rel.width == 64 ? kPlannedMost<64> : kPlannedMost<128>;
+    return rel.batch <= kWave && rel.num_rows >= kPlannedMean * rel.batch &&
+           rel.num_rows * rel.heads <= most * device_cus() * kTileRows;
 }
 struct Planning {
     Pieces by_rows;
@@ -53,6 +51,7 @@ Planning planning(const tiga_packed &rel, void *ws) {
     const int resident = 2 * device_cus();
     p.cut = 2 * static_cast<int64_t>(resident);
     p.by_rows.resident = resident;
+    p.by_rows.quarters = 5;
     p.by_rows.mult = static_cast<int32_t>(group < 1 ? 1 : group);
     p.by_rows.least = static_cast<int32_t>(ceil_div(kPlannedTiles * Geo<D>::BN * group, kTileRows));
     p.by_rows.places = static_cast<int32_t>(most_items(rel, group) / rel.kv_heads + ceil_div(p.cut, rel.kv_heads));
@@ -86,7 +85,7 @@ int run_planned(const tiga_packed &rel, const Args<kPacked> &given, void *ws, hi
     prof_after(stream);
     if (int rc = check_launch("packed attention")) return rc;
     const int64_t cut = ceil_div(p.cut, rel.kv_heads) * rel.kv_heads;  // whole places, so that parts of every head are seen
-    hipLaunchKernelGGL((planned_merge_kernel<T, Geo<D>>), dim3(static_cast<unsigned>(cut), kTileRows * (D / 4) / kThreads), dim3(kThreads), 0,
+    hipLaunchKernelGGL((planned_merge_kernel<T, Geo<D>>), dim3(static_cast<unsigned>(cut), 4), dim3(kThreads), 0,
                        stream, a);
     return check_launch("packed attention merge");
 }

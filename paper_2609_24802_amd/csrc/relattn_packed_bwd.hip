@@ -748,8 +748,8 @@ Layout layout(const tiga_packed &rel, void *ws) {
 template <class T, int D>
 int launch(const Layout &l, const tiga_packed &rel, const Args &a, hipStream_t stream) {
     const bool keys = a.dk.p || a.dv.p;
-    const Pieces by_rows{l.rows_table, static_cast<int32_t>(l.rows.places), static_cast<int32_t>(a.group.d), l.rows.resident, l.rows.least};
-    const Pieces by_keys{l.keys_table, static_cast<int32_t>(l.keys.places), 1, l.keys.resident, l.keys.least};
+    const Pieces by_rows{l.rows_table, static_cast<int32_t>(l.rows.places), static_cast<int32_t>(a.group.d), l.rows.resident, l.rows.least, 2};
+    const Pieces by_keys{l.keys_table, static_cast<int32_t>(l.keys.places), 1, l.keys.resident, l.keys.least, 2};
     if (int rc = plan_pieces(rel, by_rows, by_keys, 2, stream)) return rc;
     const dim3 row_blocks(static_cast<unsigned>(l.rows.places * rel.kv_heads)), key_blocks(static_cast<unsigned>(l.keys.places * rel.kv_heads));
     if constexpr (kScaled<T>) {
