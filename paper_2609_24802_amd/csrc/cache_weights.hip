@@ -10,9 +10,9 @@
 // Many rows (chunks of prompts): bound by the vector unit, 4 quarter-rate and 8 full-rate instructions for 256 pairs (96 cycles),
 // and the matrix cores, whose products take 64 at width 128 and hardly overlap with them: 256 keys a block, and the weights
 // of 16 rows formed under the products of the next, took the same 74 us as 128 keys and three blocks a compute unit, 72.  A
-// block owns 128 keys, 32 a wavefront as operands in registers, and streams the rows through LDS.  The row tiles of all items (128 keys of a head) are laid end to end and
-// every block takes an equal run of them; the sums of an item's parts (512 bytes) go to the workspace and are added in order
-// by a second launch.
+// block owns 128 keys, 32 a wavefront as operands in registers, and streams the rows through LDS.  The row tiles of all items
+// (128 keys of a head) are laid end to end and every block takes an equal run of them; the sums of an item's parts (512 bytes)
+// go to the workspace and are added in order by a second launch.
 //
 // Measured (MI355X), width 128: 64 single tokens over up to 8192 positions, 32 heads over 8, bf16: 83 us for 381 MB, 4.6 TB/s (a
 // large copy moves 4.8).  Two chunks of 1023 tokens and three single ones over up to 9000 positions, 16 heads over 4, f16: 5.8

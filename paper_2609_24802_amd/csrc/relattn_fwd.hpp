@@ -1,6 +1,6 @@
 // Online-softmax reducer over rectangular relations, forward: the kernels of cross attention over strided sources, of causal
-// attention of new tokens over a paged cache, and of causal attention within packed sequences.  With the reducer state of Section 5.2 (running maximum m, mass l,
-// accumulator o; states combine by rescaling into the common maximum):
+// attention of new tokens over a paged cache, and of causal attention within packed sequences.  With the reducer state of Section
+// 5.2 (running maximum m, mass l, accumulator o; states combine by rescaling into the common maximum):
 //   s_ij = scale * <q_i, k_j>,  y_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij),  lse_i = log sum_j exp(s_ij).
 //
 // Rows.  The heads that share a source head are rows over the same keys, so a sequence's rows for one source head are

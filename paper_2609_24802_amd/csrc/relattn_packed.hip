@@ -35,7 +35,7 @@ template <int D>
 constexpr int64_t kPlannedMost = D == 64 ? 8 : 32;
 bool planned(const tiga_packed &rel) {
     const int64_t most = rel.batch < 2 ? kPlannedOne : rel.width == 64 ? kPlannedMost<64> : kPlannedMost<128>;
-    return rel.batch <= kWave && rel.num_rows >= kPlannedMean * rel.batch &&
+    return rel.batch > 0 && rel.batch <= kWave && rel.num_rows >= kPlannedMean * rel.batch &&
            rel.num_rows * rel.heads <= most * device_cus() * kTileRows;
 }
 struct Planning {

@@ -347,3 +347,27 @@ def test_pointers_that_run_backwards_in_a_long_batch(lib):
         ptr = torch.tensor(p, dtype=torch.int32, device="cuda")
         lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, ptr, want_lse=True)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("lens,H,Hk,D,dt,lead,tail", PLANNED + [
+    ([], 2, 1, 64, F16, 100, 0),          # a batch of none
+    ([], 3, 3, 128, BF16, 700, 0),
+    ([0] * 5, 2, 2, 128, F16, 5, 600),
+    ([511], 4, 1, 128, BF16, 0, 0),
+    ([17], 1, 1, 64, F16, 0, 0),
+    ([300] * 65, 2, 1, 128, F16, 0, 0),
+])
+def test_nothing_is_written_behind_a_workspace(lib, lens, H, Hk, D, dt, lead, tail):
+    s = Packed(lens, H, Hk, D, dt, seed=24, lead=lead, tail=tail)
+    ref = lib.C.byref(lib._packed(s.q, s.k, s.v, s.ptr_t, "hnd")[0])
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True)
+    want = y, lse, *lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t).values()
+    sizes = [getattr(lib.load(), f"tiga_mp_attention_packed_{n}_workspace")(ref) for n in ("fwd", "bwd")]
+    whole = [torch.full((n + (1 << 20),), 0xa5, dtype=torch.uint8, device="cuda") for n in sizes]
+    y, lse = lib.tiga_mp_attention_packed_fwd(s.q, s.k, s.v, s.ptr_t, want_lse=True, ws=whole[0][:sizes[0]])
+    got = y, lse, *lib.tiga_mp_attention_packed_bwd(s.q, s.k, s.v, y, lse, s.dy, s.ptr_t, ws=whole[1][:sizes[1]]).values()
+    torch.cuda.synchronize()
+    for t, n in zip(whole, sizes):
+        assert (t[n:] == 0xa5).all()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
