@@ -28,7 +28,7 @@ Plan packed_plan(const tiga_packed &rel) {
 // and planned, width 128: 16 heads over 2 source heads, 4000 tokens 118 and 103; 8 over 8, 8000 tokens 190 and 163; 16, 8 x
 // 2000 tokens 175 and 154; 32 over 8, 17 prompts of 16,384 in all 307 and 298; width 64, 8 over 2, 2000 tokens 47 and 32.  Many
 // tiles of one sequence fill the device however they come (32 over 4, 4000 tokens 134 and 140; 16 over 4, 16,000 899 and 911), and
-// so do very many at width 64.
+// so do very many at width 64; items of shorter sequences are too alike for an order to pay (64 x 256 tokens, 16 heads 64 and 72).
 constexpr int64_t kPlannedMean = 512, kPlannedTiles = 8;  // key tiles of a part, at least
 constexpr int64_t kPlannedOne = 3;                        // tiles to a CU: of one sequence, and of more
 template <int D>
