@@ -27,11 +27,16 @@ bool thin_for(const tiga_cache &c, int64_t num_dst, int32_t heads, int64_t seque
     if (c.page_size < 8) return true;  // the wide tiles load 8 rows of a page at a time
     return num_dst * (heads / c.kv_heads) <= kThinRows * sequences;
 }
+// Blocks are multiples of 8, so that both passes' blocks know their XCD.  A narrow pass has two slots for each of them, not for
+// each that the lengths leave work: a length past the table, or pointers that overlap, make more work than the host can know of.
 template <class G>
 Plan pass_plan(const tiga_cache &c, int64_t num_dst, int32_t heads, int64_t sequences) {
     const int64_t rows = num_dst * (heads / c.kv_heads);
-    return plan_for<G>((rows / G::BM + sequences) * c.kv_heads, rows / G::BM * c.kv_heads,
-                       static_cast<int64_t>(c.table_width) * c.page_size, false);
+    Plan p = plan_for<G>((rows / G::BM + sequences) * c.kv_heads, rows / G::BM * c.kv_heads,
+                         static_cast<int64_t>(c.table_width) * c.page_size, false);
+    p.blocks = ceil_div(p.blocks, kXcds) * kXcds;
+    if (kNarrow<G> && p.slots) p.slots = 2 * p.blocks;
+    return p;
 }
 int64_t some_groups(const tiga_prefix &p, int64_t num_dst) { return num_dst < p.groups ? num_dst : p.groups; }
 
@@ -149,9 +154,7 @@ int launch(const Plan &ps, const Plan &pb, Args<kShared> s, Args<kBehind> b, con
     };
     if (ps.slots) parts(s, carve<GS>(l.shared_parts, ps.slots), ps.slots);
     if (pb.slots) parts(b, carve<GB>(l.behind_parts, pb.slots), pb.slots);
-    // of 8 each, so that both parts' blocks know their XCD (the narrow kernel's runs are equal, whatever their number)
-    auto octets = [](int64_t blocks) { return static_cast<unsigned>(ceil_div(blocks, kXcds) * kXcds); };
-    const unsigned shared = octets(ps.blocks), behind = octets(pb.blocks);
+    const unsigned shared = static_cast<unsigned>(ps.blocks), behind = static_cast<unsigned>(pb.blocks);
     prof_before(stream);
     hipLaunchKernelGGL((prefix_kernel<T, D, ST, BT>), dim3(shared + behind), dim3(kThreads), 0, stream, s, b, shared, behind);
     prof_after(stream);
