@@ -102,22 +102,25 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads) void prefix_join_kernel(Args<kBehind> a, States st, Rows y, float *lse) {
     constexpr int L = D / 4;
     const Run rows = run_between(a.src.dst_ptr, 0, a.src.batch, a.src.num_dst);
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
     const int heads = a.kv_heads * static_cast<int>(a.group.d), w = static_cast<int>(threadIdx.x) % L * 4;
-    const int64_t token = i / heads;
-    if (token >= rows.count) return;
-    const int head = static_cast<int>(i - token * heads);
-    const int64_t row = rows.first + token, at = head * static_cast<int64_t>(a.src.num_dst) + row;
-    const float l1 = st.shared_lse2[at], l2 = st.behind_lse2[at];
-    f4 o1{0.0f, 0.0f, 0.0f, 0.0f};
-    if (l1 != -__builtin_inff()) o1 = *reinterpret_cast<const f4 *>(st.shared + at * D + w);  // there may be none
-    const f4 o2 = *reinterpret_cast<const f4 *>(st.behind + at * D + w);
-    const float m = fmaxf(l1, l2), ref = m == -__builtin_inff() ? 0.0f : m;
-    const float f1 = __builtin_amdgcn_exp2f(l1 - ref), f2 = __builtin_amdgcn_exp2f(l2 - ref), mass = f1 + f2;
-    const f4 v = (o1 * f1 + o2 * f2) * (mass == 0.0f ? 0.0f : 1.0f / mass);
-    put<T>(const_cast<uint16_t *>(y.p) + head * y.head + row * y.row + w, v);
-    if (lse && w == 0) lse[at] = (ref + __log2f(mass)) * kLn2;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kThreads / L) + threadIdx.x / L;; i += static_cast<int64_t>(gridDim.x) * (kThreads / L)) {
+        const int64_t token = i / heads;
+        if (token >= rows.count) return;
+        const int head = static_cast<int>(i - token * heads);
+        const int64_t row = rows.first + token, at = head * static_cast<int64_t>(a.src.num_dst) + row;
+        const float l1 = st.shared_lse2[at], l2 = st.behind_lse2[at];
+        f4 o1{0.0f, 0.0f, 0.0f, 0.0f};
+        if (l1 != -__builtin_inff()) o1 = *reinterpret_cast<const f4 *>(st.shared + at * D + w);  // there may be none
+        const f4 o2 = *reinterpret_cast<const f4 *>(st.behind + at * D + w);
+        const float m = fmaxf(l1, l2), ref = m == -__builtin_inff() ? 0.0f : m;
+        const float f1 = __builtin_amdgcn_exp2f(l1 - ref), f2 = __builtin_amdgcn_exp2f(l2 - ref), mass = f1 + f2;
+        const f4 v = (o1 * f1 + o2 * f2) * (mass == 0.0f ? 0.0f : 1.0f / mass);
+        put<T>(const_cast<uint16_t *>(y.p) + head * y.head + row * y.row + w, v);
+        if (lse && w == 0) lse[at] = (ref + __log2f(mass)) * kLn2;
+    }
 }
+
+constexpr int64_t kMostJoins = 1 << 20;  // blocks
 
 struct Layout {
     States states;
@@ -167,9 +170,10 @@ int launch(const Plan &ps, const Plan &pb, Args<kShared> s, Args<kBehind> b, con
         hipLaunchKernelGGL((prefix_merge_kernel<T, D, ST, BT>), dim3(ms + mb), dim3(kThreads), 0, stream, s, b, ms, shared, behind);
         if (int rc = check_launch("prefix attention merge")) return rc;
     }
-    const int64_t rows = static_cast<int64_t>(b.src.num_dst) * b.kv_heads * b.group.d;
-    hipLaunchKernelGGL((prefix_join_kernel<T, D>), dim3(static_cast<unsigned>(ceil_div(rows, kThreads / (D / 4)))), dim3(kThreads), 0, stream,
-                       b, l.states, rows_of(y), lse);
+    // a grid counts its threads in 32 bits (and wraps around without an error): more rows than that go in turns
+    const int64_t rows = static_cast<int64_t>(b.src.num_dst) * b.kv_heads * b.group.d, joins = ceil_div(rows, kThreads / (D / 4));
+    hipLaunchKernelGGL((prefix_join_kernel<T, D>), dim3(static_cast<unsigned>(joins < kMostJoins ? joins : kMostJoins)), dim3(kThreads), 0,
+                       stream, b, l.states, rows_of(y), lse);
     return check_launch("prefix attention join");
 }
 
