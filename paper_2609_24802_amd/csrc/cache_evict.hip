@@ -172,10 +172,11 @@ struct Held {
 };
 
 // The whole list of a sequence that has no more positions than stay, and what is behind a list: this thread's share of them.
+// (In 64 bits: lists may be as long as 32 bits count, and the step past their end is longer.)
 __device__ __forceinline__ bool list_all(const Args &a, const Span &s, int32_t *kept, int32_t thread, int32_t threads) {
-    for (int32_t i = s.stay + thread; i < a.keep; i += threads) kept[i] = -1;
+    for (int64_t i = static_cast<int64_t>(s.stay) + thread; i < a.keep; i += threads) kept[i] = -1;
     if (s.n > a.keep) return false;
-    for (int32_t i = thread; i < s.n; i += threads) kept[i] = i;
+    for (int64_t i = thread; i < s.n; i += threads) kept[i] = static_cast<int32_t>(i);
     return true;
 }
 
