@@ -190,7 +190,8 @@ __global__ __launch_bounds__(kThreads) void select_kernel(Args a) {
     const Span span(a, b);
     int32_t *const kept = a.kept + static_cast<int64_t>(blockIdx.x) * a.keep;
     if (list_all(a, span, kept, static_cast<int32_t>(threadIdx.x), kThreads)) return;
-    const int32_t per = (span.n + kWaves * 256 - 1) / (kWaves * 256);
+    // at most 2^19, so that positions up to the end of the last group are below 2^31 (n + 4095 need not be)
+    const int32_t per = (span.n - 1) / (kWaves * 256) + 1;
     const Held<PER> held(a, span, b, head, w * per * 256, per);
 
     // the least weight that stays, from its digits, and how many equal ones stay
