@@ -235,15 +235,27 @@ struct Weights {
             dw[n / 2] = T::pack(ds[n - 1], ds[n]);
         }
     }
-    // bit n of `exists`: whether the pair does
+    // bit n of `exists`: whether the pair does.  In bfloat16, whose products may pass fp32's range, a pair that does not has no DS
+    // also where its product or the row's statistics are not finite (0 times which would be NaN): both P and DS are cleared, two
+    // in a register.  (Each by itself takes 1.5 % of dk and dv of 16,384 tokens, 16 heads over 4 of 128.)
     __device__ __forceinline__ void form_if(const Scores<T, D> &f, float c, float h, int n, uint32_t exists) {
-        const int qb = n / 8, e = n / 4 % 2, i = n % 4;
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[e][i]));
-        p[n] = __uint_as_float(__float_as_uint(x) & static_cast<uint32_t>(__builtin_amdgcn_sbfe(exists, n, 1)));
-        ds[n] = p[n] * (kScaled<T> ? __builtin_fmaf(f.dp[e][qb][i], h, -delta[e][i]) : f.dp[e][qb][i] - delta[e][i]);
-        if (n % 2) {
-            pw[n / 2] = T::pack(p[n - 1], p[n]);
-            dw[n / 2] = T::pack(ds[n - 1], ds[n]);
+        const uint32_t mask = static_cast<uint32_t>(__builtin_amdgcn_sbfe(exists, n, 1));
+        if constexpr (kScaled<T>) {
+            const int qb = n / 8, e = n / 4 % 2, i = n % 4;
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(f.s[e][qb][i], c, -lse2[e][i]));
+            p[n] = __uint_as_float(__float_as_uint(x) & mask);
+            ds[n] = p[n] * __builtin_fmaf(f.dp[e][qb][i], h, -delta[e][i]);
+            if (n % 2) {
+                pw[n / 2] = T::pack(p[n - 1], p[n]);
+                dw[n / 2] = T::pack(ds[n - 1], ds[n]);
+            }
+        } else {
+            form(f, c, h, n);
+            if (n % 2) {
+                const uint32_t both = __builtin_amdgcn_perm(mask, static_cast<uint32_t>(__builtin_amdgcn_sbfe(exists, n - 1, 1)), 0x07060100u);
+                pw[n / 2] &= both;
+                dw[n / 2] &= both;
+            }
         }
     }
 };
@@ -252,13 +264,30 @@ struct Weights {
 // scores, the second's under the first half's sums: at width 128 a SIMD has one wavefront, and nothing else fills its
 // matrix unit meanwhile (527 us without, 494).  At width 64 two wavefronts share a SIMD: 8 x 449 rows over 1500 ragged 54.8
 // and 52.7 us, 4 x 4096 over 77 23.4 and 21.0, 4 x 4096 over 4096 507 and 525.
-// CUT: bit n of exists[half] says whether pair n of the half does; otherwise all do.
+// CUT: bit n of exists[half] says whether pair n of the half does; otherwise all do.  At width 64 in bfloat16 the halves of a cut
+// tile are taken one after the other: side by side the masks spill 21 registers, in all tiles (61 sequences of 131 tokens, 16
+// heads: 60 us of dk and dv, so 51).
 template <class T, int D, bool CUT = false>
 __device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)[2][Geo<D>::CH],
                                           const u4 (&x2)[2][Geo<D>::CH], const uint8_t *y1, const uint8_t *y2, int dr,
                                           int tr, float c, float h, const float *st, const float *sd, int g,
                                           const uint32_t *exists = nullptr) {
     constexpr int kHalf = 32 * Geo<D>::RB, kScore = 16 / Scores<T, D>::kReads, kSum = 16 / kSumReads<T, D, kKeys>;
+    auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
+    if constexpr (CUT && D == 64 && !kScaled<T>) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            Scores<T, D> f;
+            Weights<T, D> w;
+            w.load(st + 32 * half, sd + 32 * half, g);
+            f.form(x1, x2, y1 + half * kHalf, y2 + half * kHalf, dr, [](int) {});
+#pragma unroll
+            for (int n = 0; n < 16; ++n) w.form_if(f, c, h, n, exists[half]);
+            const u4 p[2] = {operand(w.pw, 0), operand(w.pw, 1)}, d[2] = {operand(w.dw, 0), operand(w.dw, 1)};
+            add_products<T, D, kKeys>(acc, p, d, y1 + half * kHalf, y2 + half * kHalf, tr, [](int) {});
+        }
+        return;
+    }
     Scores<T, D> f0, f1;
     Weights<T, D> w0, w1;
     w0.load(st, sd, g);
@@ -271,7 +300,6 @@ __device__ __forceinline__ void rows_step(Sums<T, D, kKeys> &acc, const u4 (&x1)
         }
     });
     w1.load(st + 32, sd + 32, g);
-    auto operand = [](const uint32_t *x, int qb) { return u4{x[4 * qb], x[4 * qb + 1], x[4 * qb + 2], x[4 * qb + 3]}; };
     const u4 p0[2] = {operand(w0.pw, 0), operand(w0.pw, 1)}, d0[2] = {operand(w0.dw, 0), operand(w0.dw, 1)};
     add_products<T, D, kKeys>(acc, p0, d0, y1, y2, tr, [&](int i) {
 #pragma unroll
