@@ -112,7 +112,7 @@ struct Run1 {
     }
 };
 
-// A row that saw nothing gives no weight.
+// A row that saw nothing gives no weight, whatever its query holds (a score that is not finite less infinity may be NaN).
 __device__ __forceinline__ float log2_of(float lse) { return lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e; }
 
 template <class T, int D>
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(Args a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int32_t r = r0 + 4 * g + i;
-                    const bool sees = r < rows && at <= chunk.pos0 + a.group.div(r);
+                    const bool sees = r < rows && at <= chunk.pos0 + a.group.div(r) && lse2[i] != __builtin_inff();
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -lse2[i]));
                     sum[kb] += sees ? p : 0.0f;
                 }
@@ -336,6 +336,7 @@ __global__ __launch_bounds__(kThreads, 3) void wide_weights_kernel(Args a, int b
     using G = Wide<D>;
     __shared__ __attribute__((aligned(1024))) uint8_t qa[G::TILE], qb[G::TILE];
     __shared__ __attribute__((aligned(256))) float sta[G::BN], stb[G::BN];
+    __shared__ int nonea[kWaves], noneb[kWaves];  // whether a wavefront's rows of the tile hold one that gives no weight
     const int lane = lane_id(), w = uniform(static_cast<int>(threadIdx.x) / kWave);
     const int col = lane & 15, g = lane >> 4;
     const int32_t d = static_cast<int32_t>(a.group.d);
@@ -437,17 +438,27 @@ __global__ __launch_bounds__(kThreads, 3) void wide_weights_kernel(Args a, int b
                 }
             }
         };
-        auto arrive = [&](float *st) {
+        // Queries of rows that give no weight are replaced by 0 in LDS (a select for each weight: 73 -> 81 us for 1023 tokens over
+        // 9000 positions).
+        static_assert(G::BN <= 2 * kWave, "two wavefronts look at a tile's lse");
+        auto arrive = [&](uint8_t *buf, float *st, int *none) {
             loads_arrived();
             if (threadIdx.x < G::BN) st[threadIdx.x] = log2_of(lse);
+            const bool some = __any(threadIdx.x < G::BN && lse == -__builtin_inff());
+            if (lane == 0) none[w] = some;
+            __syncthreads();
+            if (uniform(none[0] | none[1]) == 0) return;
+#pragma unroll 1
+            for (int i = static_cast<int>(threadIdx.x); i < G::BN * G::CPR; i += kThreads)
+                if (st[i / G::CPR] == __builtin_inff()) reinterpret_cast<u4 *>(buf)[i] = u4{0u, 0u, 0u, 0u};
             __syncthreads();
         };
         for (int kt = t0; kt < t1; kt += 2) {
-            arrive(sta);
+            arrive(qa, sta, nonea);
             if (kt + 1 < t1) stage(kt + 1, qb);
             step(kt, qa, sta);
             if (kt + 1 >= t1) break;
-            arrive(stb);
+            arrive(qb, stb, noneb);
             if (kt + 2 < t1) stage(kt + 2, qa);
             step(kt + 1, qb, stb);
         }
