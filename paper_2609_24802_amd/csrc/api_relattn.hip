@@ -602,7 +602,9 @@ int tiga_mp_cache_evict(const tiga_cache *cache, const float *weights, int32_t k
     if (recent < 0 || recent > keep) return fail(TIGA_EINVAL, "%s: recent = %d must be in [0, keep]", what, recent);
     if (cache->batch == 0 || cache->kv_heads == 0) return TIGA_OK;
     if (int rc = check_cache_data(what, cache, cache->length)) return rc;
-    if (int rc = check_cache_data(what, to, to_length)) return rc;
+    tiga_cache target = *to;
+    target.length = to_length;  // its own is not read
+    if (int rc = check_cache_data(what, &target, to_length)) return rc;
     if (int rc = check_cells(what, "weights", weights)) return rc;
     if (to_weights)
         if (int rc = check_cells(what, "to_weights", to_weights)) return rc;
