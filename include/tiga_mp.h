@@ -29,8 +29,8 @@
  *   - Work is enqueued on `stream` (a hipStream_t passed as void*; NULL is the
  *     null stream).  Calls return before the work completes; a device fault
  *     surfaces at the caller's next synchronization.  Only
- *     tiga_csr_validate(level 2), tiga_radius_neighbors, tiga_cache_validate and
- *     tiga_prefix_validate synchronize.
+ *     tiga_csr_validate(level 2), tiga_radius_neighbors, tiga_cache_validate,
+ *     tiga_prefix_validate and tiga_retention_validate synchronize.
  *   - Outputs are overwritten, never accumulated into.
  *   - fp32 features are row-major [rows, feat], of any width.  Rows need only
  *     the alignment of floats; some paths are faster where feat % 4 == 0 and
@@ -677,6 +677,16 @@ int tiga_mp_attention_prefix_fwd(const tiga_cache *cache, const tiga_prefix *pre
 
 /* --------------------------------------------- which positions of a cache stay */
 
+/* A weight belongs to a cell of a page and rows move from page to page, so here every
+ * page is one sequence's, and named once: sequences that begin alike have the shared
+ * positions in copies (which tiga_mp_attention_prefix_fwd reads once a group all the
+ * same).  With a page that two name, their sums overwrite each other, and an
+ * eviction in place moves one's rows over the other's.  The calls do not look; this
+ * one does, on the host, at the pages of every sequence's positions (entries that
+ * are no page are passed over): TIGA_EGRAPH names a page and two that name it.
+ * Synchronizes `stream`. */
+int tiga_retention_validate(const tiga_cache *cache, void *stream);
+
 /* Workspace bytes for tiga_mp_cache_weights (0 on error).  One sized for a call
  * holds every smaller one. */
 size_t tiga_mp_cache_weights_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads);
@@ -691,7 +701,7 @@ size_t tiga_mp_cache_weights_workspace(const tiga_cache *cache, int64_t num_dst,
  *   q:   as for tiga_mp_attention_paged_fwd;  lse: fp32 [heads, num_dst].
  *   weights, out: fp32 [num_pages, kv_heads, page_size], contiguous, the cells of
  *   the cache's pages; out may be weights.  Cells of no position are left as they
- *   were.  No two sequences may share a page.
+ *   were.  No page may be named twice (tiga_retention_validate).
  * A row with lse = -inf gives nothing.  Positions past the table or without a page
  * have no cell.  Sums in fp32 in a fixed order; deterministic.  Requires decay
  * finite and >= 0; otherwise as tiga_mp_attention_paged_fwd.
@@ -722,8 +732,9 @@ size_t tiga_mp_cache_evict_workspace(const tiga_cache *cache, const tiga_cache *
  *               -1 past them.
  * Keys that were rotated keep the rotation of the position they had.  Positions past
  * cache's table are none; rows whose new position has no page in `to`, or whose old
- * one had none, are not stored.  Nothing else is written.  No two sequences may
- * share a page of `to`.  Deterministic.
+ * one had none, are not stored.  Nothing else is written.  No page of `to` may be
+ * named twice (tiga_retention_validate), in place none of the cache; another cache's
+ * may be read by several.  Deterministic.
  * Requires 1 <= keep, 0 <= recent <= keep, batch * kv_heads < 2^20.
  * Errors: TIGA_EINVAL, TIGA_EUNSUPPORTED, TIGA_EWORKSPACE, TIGA_EDEVICE. */
 int tiga_mp_cache_evict(const tiga_cache *cache, const float *weights, int32_t keep, int32_t recent,

@@ -145,6 +145,7 @@ _SIGS = {
     "tiga_mp_attention_prefix_fwd_workspace": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32]),
     "tiga_mp_attention_prefix_fwd": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
                                                C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "tiga_retention_validate": (C.c_int, [C.c_void_p, C.c_void_p]),
     "tiga_mp_cache_weights_workspace": (C.c_size_t, [C.c_void_p, C.c_int64, C.c_int32]),
     "tiga_mp_cache_weights": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float,
                                         C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -989,6 +990,12 @@ def tiga_mp_attention_prefix_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch
     return (y, lse) if want_lse else y
 
 
+def tiga_retention_validate(cache: KvCache):
+    """Raise TigaError (TIGA_EGRAPH) if two sequences' positions lie in one page, or one's twice: tiga_mp_cache_weights and the
+    cache that tiga_mp_cache_evict moves to need pages of each sequence's own.  Synchronizes."""
+    _check(load().tiga_retention_validate(cache.ref, _stream()))
+
+
 def _cells(cache, t, name):
     P, H, R = cache.k_pages.shape[:3]
     return _dev(t, torch.float32, name, (P, H, R))
@@ -1001,8 +1008,8 @@ def tiga_mp_cache_weights(cache: KvCache, q: torch.Tensor, lse: torch.Tensor, ds
 
     q, dst_ptr, scale as for tiga_mp_attention_paged_fwd, lse fp32 [heads, rows] from it.  weights: fp32
     [num_pages, kv_heads, page_size], one for each row of the cache's pages, summed over the heads that share it; the
-    new tokens' own count as 0 before.  out: where the sums go (None: weights, in place).  Pages are no two sequences'.
-    Returns out."""
+    new tokens' own count as 0 before.  out: where the sums go (None: weights, in place).  No page may be two sequences'
+    (tiga_retention_validate): a prefix that several share lies in copies here.  Returns out."""
     lib = load()
     axes = _axes(layout, (3,))
     heads, rows, qv = _new_rows(cache, q, "q", axes)
@@ -1024,8 +1031,9 @@ def tiga_mp_cache_evict(cache: KvCache, weights: torch.Tensor, to: KvCache | Non
 
     weights: fp32 [num_pages, kv_heads, page_size].  They move in order to the first positions of `to` (keys, values, and
     weights to to_weights if given), whose pages are none of the cache's sequences' own; to.length is set to
-    min(length, keep).  Without `to` the cache is evicted from in place, weights and length too.  Keys keep the rotation
-    of their old positions: rotate later tokens by their true positions (tiga_mp_rotary_fwd) and append them unrotated.
+    min(length, keep).  Without `to` the cache is evicted from in place, weights and length too.  No page that rows move to
+    may be two sequences' (tiga_retention_validate), in place none of the cache.  Keys keep the rotation of their old
+    positions: rotate later tokens by their true positions (tiga_mp_rotary_fwd) and append them unrotated.
     Returns kept: int32 [batch, kv_heads, keep], the positions that stayed, -1 past them."""
     lib = load()
     _cells(cache, weights, "weights")

@@ -1,6 +1,8 @@
 // C entry points of attention over rectangular relations: cross attention and the paged cache.
+#include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "relattn.hpp"
@@ -560,6 +562,42 @@ int check_evict(const char *what, const tiga_cache *cache, const tiga_cache *to,
 }  // namespace
 
 extern "C" {
+
+int tiga_retention_validate(const tiga_cache *cache, void *stream) {
+    EntryScope scope;
+    const char *what = "retention validation";
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = check_cache(what, cache)) return rc;
+    if (cache->batch == 0 || cache->kv_heads == 0) return TIGA_OK;
+    if (int rc = check_cache_data(what, cache, cache->length)) return rc;
+    const size_t nb = cache->batch, width = cache->table_width;
+    std::vector<int32_t> len, table;
+    std::vector<std::pair<int32_t, int32_t>> named;  // page, sequence
+    try {
+        len.resize(nb);
+        table.resize(nb * width);
+        named.reserve(nb * width);
+    } catch (const std::bad_alloc &) {
+        return fail(TIGA_EDEVICE, "%s: no host memory for %zu table entries", what, nb * width);
+    }
+    int rc = check_hip(hipMemcpyAsync(len.data(), cache->length, 4 * nb, hipMemcpyDeviceToHost, s), what);
+    if (!rc && width) rc = check_hip(hipMemcpyAsync(table.data(), cache->table, 4 * nb * width, hipMemcpyDeviceToHost, s), what);
+    // also after a failed copy: the one before it writes into its vector
+    const int rs = check_hip(hipStreamSynchronize(s), what);
+    if (rc || rs) return rc ? rc : rs;
+    for (size_t b = 0; b < nb; ++b) {
+        const int64_t pages = ceil_div(len[b] < 0 ? 0 : len[b], cache->page_size);
+        for (int64_t e = 0; e < pages && e < cache->table_width; ++e) {
+            const int32_t id = table[b * width + e];
+            if (id >= 0 && id < cache->num_pages) named.push_back({id, static_cast<int32_t>(b)});
+        }
+    }
+    std::sort(named.begin(), named.end());
+    for (size_t i = 1; i < named.size(); ++i)
+        if (named[i].first == named[i - 1].first)
+            return fail(TIGA_EGRAPH, "page %d is named by sequence %d and by sequence %d", named[i].first, named[i - 1].second, named[i].second);
+    return TIGA_OK;
+}
 
 size_t tiga_mp_cache_weights_workspace(const tiga_cache *cache, int64_t num_dst, int32_t heads) {
     clear_error();  // no EntryScope: armed kernel events are for the call that follows
