@@ -656,8 +656,10 @@ typedef struct {
 } tiga_prefix;
 
 /* tiga_cache_validate, and that ptr and len are in range and no sequence with new
- * tokens has its first one among the shared positions (TIGA_EGRAPH).  That the
- * shared positions hold the same is not looked at.  Synchronizes `stream`. */
+ * tokens has its first one below its group's len (TIGA_EGRAPH), also where the call
+ * would read no position once or fewer than len (groups of one; rounding), whose
+ * results are right.  That the shared positions hold the same is not looked at.
+ * Synchronizes `stream`. */
 int tiga_prefix_validate(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst, const int32_t *dst_ptr,
                          void *stream);
 
@@ -669,8 +671,9 @@ size_t tiga_mp_attention_prefix_fwd_workspace(const tiga_cache *cache, const tig
 
 /* tiga_mp_attention_paged_fwd with the shared positions of each group read once for
  * all of its rows.  The results are those of the paged call but for the order of
- * the sums; a sequence whose first new token is among its shared positions gives
- * NaN.  Arguments, requirements and errors as there. */
+ * the sums; a sequence whose first new token is among the positions that are read
+ * once (as above: rounded down, none of a group of one) gives NaN.  Arguments,
+ * requirements and errors as there. */
 int tiga_mp_attention_prefix_fwd(const tiga_cache *cache, const tiga_prefix *prefix, int64_t num_dst,
                                  const int32_t *dst_ptr, int32_t heads, const tiga_view *q, float scale,
                                  const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);

@@ -955,7 +955,7 @@ def _prefix(cache, group_ptr, group_len):
 def tiga_prefix_validate(cache: KvCache, num_dst: int, dst_ptr: torch.Tensor, group_ptr: torch.Tensor,
                          group_len: torch.Tensor):
     """tiga_cache_validate, and raise TigaError (TIGA_EGRAPH) if the groups are inconsistent or a sequence's first new
-    token is among its shared positions.  Synchronizes."""
+    token lies below its group's length, whether or not so much would be read once.  Synchronizes."""
     _dev(dst_ptr, torch.int32, "dst_ptr", (cache.batch + 1,))
     _same_device(cache.k_pages.get_device(), dst_ptr=dst_ptr)
     _check(load().tiga_prefix_validate(cache.ref, C.byref(_prefix(cache, group_ptr, group_len)), int(num_dst),
@@ -969,8 +969,8 @@ def tiga_mp_attention_prefix_fwd(cache: KvCache, q: torch.Tensor, dst_ptr: torch
     their keys and values are read once a group, for all of its rows.
 
     Group g is sequences group_ptr[g] to group_ptr[g + 1] (int32 [groups + 1] on the device), whose positions below
-    group_len[g] (int32 [groups]) hold the same, in the same pages or in copies.  New tokens lie behind them (NaN
-    otherwise).  Other arguments and results as tiga_mp_attention_paged_fwd."""
+    group_len[g] (int32 [groups]) hold the same, in the same pages or in copies.  New tokens lie behind them (NaN for a
+    sequence of whose own tokens some would be read once).  Other arguments and results as tiga_mp_attention_paged_fwd."""
     lib = load()
     axes = _axes(layout, (3,))
     heads, rows, qv = _new_rows(cache, q, "q", axes)
