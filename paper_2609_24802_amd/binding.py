@@ -1036,6 +1036,8 @@ def tiga_mp_cache_evict(cache: KvCache, weights: torch.Tensor, to: KvCache | Non
     positions: rotate later tokens by their true positions (tiga_mp_rotary_fwd) and append them unrotated.
     Returns kept: int32 [batch, kv_heads, keep], the positions that stayed, -1 past them."""
     lib = load()
+    if max(abs(int(keep)), abs(int(recent))) >= 1 << 31:  # the C arguments have 32 bits
+        raise ValueError("keep and recent must be below 2^31")
     _cells(cache, weights, "weights")
     if to is None:
         to, to_weights = cache, weights if to_weights is None else to_weights
