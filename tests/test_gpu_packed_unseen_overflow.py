@@ -58,3 +58,16 @@ def test_a_score_past_the_range(lib, row, key, H, Hk, D):
     R.assert_within(got["dq"][:, others][..., rest], out["dq"][:, others][..., rest], bound["dq"][:, others][..., rest], "dq")
     for n in ("dk", "dv"):
         R.assert_within(got[n][:, after], out[n][:, after], bound[n][:, after], n)
+
+
+@pytest.mark.parametrize("row,key", PLACES)
+@pytest.mark.parametrize("H,Hk,D", FORMS)
+def test_a_query_and_a_key_that_it_does_not_see(lib, row, key, H, Hk, D):
+    """Their score is past the range, and no pair's."""
+    s = Packed([20, 300, 40], H, Hk, D, BF16, seed=33)
+    i, j = s.ptr[1] + row, s.ptr[1] + key
+    s.q[:, :, 7] = 0
+    s.k[:, :, 7] = 0
+    s.q[0, i, 7] = BIG
+    s.k[0, j, 7] = BIG
+    check(lib, s, f"{(row, key, H, Hk, D)}")
