@@ -507,8 +507,11 @@ size_t tiga_mp_attention_packed_bwd_workspace(const tiga_packed *rel);
  * sequences.  A query or cotangent that is not finite reaches its own dq and the dk,
  * dv of the tokens that it sees; a key or value the dq of the rows that see it, and
  * by way of those rows the dk, dv of what they see.
+ * P and ds enter the products rounded to the input type: two roundings of half a
+ * step, which few tokens do not average out.
  * Deterministic (no atomics).  Requirements and errors as the forward; besides, at
- * most 2^24 - 1 tiles of 128 rows of a source head. */
+ * most 2^24 - 1 tiles of 128 rows (heads / kv_heads to a token), counted over all
+ * source heads, with one more for each sequence and a few for parts. */
 int tiga_mp_attention_packed_bwd(const tiga_packed *rel, const tiga_view *q, const tiga_view *k, const tiga_view *v,
                                  const tiga_view *y, const float *lse, const tiga_view *dy, float scale,
                                  const tiga_view *dq, const tiga_view *dk, const tiga_view *dv, void *ws,

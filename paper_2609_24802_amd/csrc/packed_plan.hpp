@@ -36,8 +36,10 @@ __device__ __forceinline__ int64_t pieces_upto(int32_t m, int32_t cut) {
 }
 // Writes the tables.  Sequences are taken 64 at a time (blockIdx.x), whose places start at or behind what the sequences before
 // them need at most.  Of 64, the tiles with the most levels come first: a piece of level L stands behind the sum of
-// pieces_upto(tiles) - pieces_upto(L) of those with more.  Batches of more than 64 are not cut.  (Every block finding its own
-// piece so took 12 us of each kernel's 49 to 65 for 100 short sequences of 16 heads.)
+// pieces_upto(tiles) - pieces_upto(L) of those with more.  Batches of more than 64 are not cut, whose 64 at a time do not know the
+// others' work: a long sequence of few heads is slow among them (dq, dk and dv of one of 10,000 tokens, 4 heads over one of 128,
+// beside 63 of 50 tokens 458 us, beside 64 of them 1412).  (Every block finding its own piece so took 12 us of each kernel's 49
+// to 65 for 100 short sequences of 16 heads.)
 __global__ __launch_bounds__(kPlanThreads) void packed_plan_kernel(const int32_t *ptr, int32_t num_rows, int32_t batch, int32_t kv_heads,
                                                                Pieces by_rows, Pieces by_keys) {
     const Pieces p = blockIdx.z == 0 ? by_rows : by_keys;

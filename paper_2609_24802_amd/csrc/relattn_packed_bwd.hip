@@ -10,10 +10,14 @@
 // are cut along the streamed axis leave fp32 sums in the workspace, which packed_reduce_kernel adds in order.
 //
 // Measured (MI355X): 16,384 tokens of ragged sequences, 16 heads over 4 of width 128, bf16: dq 955 to 1032 us (1.16 to 1.25
-// PFLOP/s), dk and dv 1617 to 1741 (0.92 to 1.0; a large library product reaches 1.24 in the same minutes), the order 8, the
+// PFLOP/s), dk and dv 1617 to 1792 (0.9 to 1.0; a large library product reaches 1.24 in the same minutes), the order 8, the
 // parts' sums 8: bound by the matrix cores and, in dk and dv, whose two accumulators leave one wavefront to a SIMD, by LDS
 // reads beside them.  Short sequences (61 with 8001 tokens in all, 16 heads of width 64, f16): order 8, peaks 8, dq 39, dk
-// and dv 48, each launch's own start and drain against 131 MB (27).
+// and dv 48, sums of no parts 4, where 131 MB take 27: dk and dv form whole squares of 128 x 128, 21 GFLOP where the pairs
+// that exist need 9, and P and DS are formed in both launches.
+//
+// P and DS enter the products in the input type (relattn_bwd.hpp).  Where a gradient is a sum of few ds, their rounding is not
+// averaged out: of 7 rows in 4 sequences, bf16, dq and dk were 0.003 off where fp32 rounded once is 0.0018.
 #include "packed_plan.hpp"
 #include "relattn.hpp"
 #include "relattn_bwd.hpp"
