@@ -477,7 +477,7 @@ typedef struct {
 } tiga_packed;
 
 /* Workspace bytes for tiga_mp_attention_packed_fwd (0 on error; at most about
- * 75 MB).  One sized for a call holds every smaller one. */
+ * 70 MB and 67 KB a head).  One sized for a call holds every smaller one. */
 size_t tiga_mp_attention_packed_fwd_workspace(const tiga_packed *rel);
 
 /* The online-softmax reducer over the triangular relation of every packed
@@ -496,8 +496,8 @@ int tiga_mp_attention_packed_fwd(const tiga_packed *rel, const tiga_view *q, con
                                  float scale, const tiga_view *y, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* Workspace bytes for tiga_mp_attention_packed_bwd (0 on error): about 8 bytes a
- * row and head, and from some hundred rows on up to about 140 MB for parts of long
- * sequences.  One sized for a call holds every smaller one. */
+ * row and head, and from some hundred rows on up to about 135 MB and 0.2 MB a head
+ * for parts of long sequences.  One sized for a call holds every smaller one. */
 size_t tiga_mp_attention_packed_bwd_workspace(const tiga_packed *rel);
 
 /* Vector-Jacobian product of tiga_mp_attention_packed_fwd, from its y and lse;
